@@ -23,6 +23,10 @@
  *    must stay valid and unmodified until that work completes (e.g. until
  *    mixrt_sync()).  The same inputs give bitwise identical outputs.
  *  - Arrays are dense, row-major, in the layouts stated per field.
+ *
+ * Beside the path it has the operators of a network that refines rendered
+ * views (group norm, activations kept in 8 bits with the gradients computed
+ * from them, rotary positions); see their section below.
  */
 #ifndef MIXRT_H
 #define MIXRT_H
@@ -43,8 +47,8 @@ enum mixrt_status {
     MIXRT_EUNSUPPORTED = -4   /* valid request outside what this build serves */
 };
 
-/* Element types of stored arrays. */
-enum mixrt_dtype { MIXRT_F32 = 0, MIXRT_F16 = 1, MIXRT_U8 = 2 };
+/* Element types of stored arrays (MIXRT_BF16: the refiner's operators only). */
+enum mixrt_dtype { MIXRT_F32 = 0, MIXRT_F16 = 1, MIXRT_U8 = 2, MIXRT_BF16 = 3 };
 
 /* Displacement forms (Eq. 2). */
 enum mixrt_disp_mode {
@@ -419,6 +423,155 @@ int mixrt_raycast(mixrt_ctx *ctx, const mixrt_mesh *mesh, int32_t views, int32_t
  * (MIXRT_EUNSUPPORTED beyond); other arguments as for mixrt_raycast. */
 int mixrt_rasterize(mixrt_ctx *ctx, const mixrt_mesh *mesh, int32_t views, int32_t W, int32_t H,
                     const mixrt_camera *cams, float *out_g0, float *out_g1);
+
+/* ---- a view refiner's operators -------------------------------------------- */
+
+/* A refiner is a network that runs on rendered views: per-pixel layers on
+ * feature maps [views][H*W][channels] (channels last, as the frames are) and
+ * layers on patch tokens whose position is (view, row, column).  These entry
+ * points serve and train it: group norm with an activation, activations kept
+ * in 8 bits for the backward pass, the gradients computed from them, and
+ * rotary positions with several axes.  They use no context memory: where a
+ * call needs device scratch, the caller passes a workspace of the size that
+ * the *_workspace function (pure host) states, 16-byte aligned, with any
+ * contents; it must not be shared by calls that run at the same time.  Empty
+ * arrays (no image, pixel, row or token) are valid.  Sums and statistics are
+ * held in 32 bits or more; a result is rounded once to its type, to nearest
+ * even. */
+
+/* Activations. */
+enum mixrt_act {
+    MIXRT_ACT_NONE = 0,
+    MIXRT_ACT_RELU = 1,
+    MIXRT_ACT_SILU = 2,   /* z / (1 + exp(-z)) */
+    MIXRT_ACT_GELU = 3    /* z (1 + erf(z / sqrt 2)) / 2 */
+};
+
+#define MIXRT_MAX_CHANNELS 4096
+#define MIXRT_MAX_AXES 8
+#define MIXRT_KEPT_GROUP 32
+
+/* A feature map in device memory: element (image, pixel, channel) at
+ * data[image * image_stride + pixel * pixel_stride + channel].  Strides in
+ * elements, at least 0 for inputs (0 repeats an image or a pixel); the
+ * elements of an output must not overlap.  Aligned to its element type. */
+typedef struct {
+    void *data;
+    int64_t image_stride, pixel_stride;
+} mixrt_map;
+
+/* Group norm with an activation: the channels of each image are split into
+ * groups of C/G consecutive ones; over a group's pixels and channels
+ *   mean, var = mean of (x - mean)^2, rstd = 1 / sqrt(var + eps),
+ *   y = act(gamma_c (x - mean) rstd + beta_c). */
+typedef struct {
+    int32_t images;      /* 0..65535 */
+    int32_t channels;    /* C, 1..MIXRT_MAX_CHANNELS */
+    int64_t pixels;      /* per image, >= 0, pixels * C < 2^40 */
+    int32_t groups;      /* G, divides C */
+    int32_t dtype;       /* of x, y, dy and dx: MIXRT_F32, _F16 or _BF16 */
+    int32_t act;         /* mixrt_act */
+    float eps;           /* >= 0, finite */
+    const float *gamma;  /* device [C], or NULL: 1 */
+    const float *beta;   /* device [C], or NULL: 0 */
+} mixrt_norm;
+
+/* Rows of activations kept in 8 bits.  MIXRT_KEPT_GROUP consecutive channels
+ * of a row (the last group may be shorter) share one power of two 2^e: with
+ * a = max |x| over the group, e is the least integer for which a 2^-e rounds
+ * to at most 127, and at least -126 (F32, BF16) or -24 (F16);
+ * code = x 2^-e rounded to nearest even, |code| at most 63 where 64 * 2^e
+ * would overflow dtype.  exps holds e + 127; a group with an infinity or a
+ * NaN has exps 255 and codes 0 and reads back as NaN.  A value code * 2^e is
+ * exact in dtype, so products with it need no further rounding. */
+typedef struct {
+    int64_t rows;        /* >= 0, rows * channels < 2^40 */
+    int32_t channels;    /* 1..MIXRT_MAX_CHANNELS */
+    int32_t dtype;       /* of the activations: MIXRT_F32, _F16 or _BF16 */
+    int8_t *codes;       /* device [rows][channels] */
+    uint8_t *exps;       /* device [rows][ceil(channels / MIXRT_KEPT_GROUP)] */
+} mixrt_kept;
+
+/* Workspace bytes of the norm's entry points (one size serves both). */
+int mixrt_norm_workspace(const mixrt_norm *norm, size_t *bytes);
+
+/* y = act(norm(x)).  stats (device float [images][G][2], 8-byte aligned):
+ * (mean, rstd), written if not NULL; an image without pixels gets
+ * (0, 1 / sqrt(eps)).  kept (or NULL): x as images * pixels rows, written.
+ * y may be x (the same data and strides). */
+int mixrt_norm_forward(mixrt_ctx *ctx, const mixrt_norm *norm, const mixrt_map *x,
+                       const mixrt_map *y, float *stats, const mixrt_kept *kept,
+                       void *workspace, size_t workspace_bytes);
+
+/* Gradients of mixrt_norm_forward at dy, with stats as it wrote them, at the
+ * values of kept or, where kept is NULL, of x (exactly one of the two).  With
+ * xh = (x - mean) rstd and dz = dy act'(gamma xh + beta):
+ *   dbeta_c = sum dz, dgamma_c = sum dz xh (over images and pixels),
+ *   dx = rstd (gamma dz - mean_group(gamma dz) - xh mean_group(gamma dz xh)).
+ * relu's slope at 0 is 0.  dgamma, dbeta: device float [C], each may be NULL;
+ * dx may be NULL, or dy (the same data and strides). */
+int mixrt_norm_backward(mixrt_ctx *ctx, const mixrt_norm *norm, const mixrt_map *dy,
+                        const mixrt_map *x, const mixrt_kept *kept, const float *stats,
+                        const mixrt_map *dx, float *dgamma, float *dbeta, void *workspace,
+                        size_t workspace_bytes);
+
+/* Keep rows of activations in 8 bits, and read them back: row r of x or out
+ * at r * row_stride elements.  out has type out_dtype (the value rounded to
+ * it where it is not kept->dtype). */
+int mixrt_kept_pack(mixrt_ctx *ctx, const mixrt_kept *kept, const void *x, int64_t row_stride);
+int mixrt_kept_unpack(mixrt_ctx *ctx, const mixrt_kept *kept, int32_t out_dtype, void *out,
+                      int64_t row_stride);
+
+/* Gradients of a per-pixel linear layer y = x W + b whose input x was kept:
+ *   dw[i][o] = sum over rows of x[row][i] dy[row][o],  db[o] = sum of dy[row][o].
+ * dy: device [rows][outs] of type kept->dtype, row r at r * dy_stride
+ * elements; dw: device float [channels][outs]; db: device float [outs] or
+ * NULL; outs 1..MIXRT_MAX_CHANNELS. */
+int mixrt_linear_grad_workspace(const mixrt_kept *kept, int32_t outs, size_t *bytes);
+int mixrt_linear_grad(mixrt_ctx *ctx, const mixrt_kept *kept, int32_t outs, const void *dy,
+                      int64_t dy_stride, float *dw, float *db, void *workspace,
+                      size_t workspace_bytes);
+
+/* Which elements of a head form pair j of a rotary position. */
+enum mixrt_rotary_layout {
+    MIXRT_ROTARY_HALVES = 0,  /* (j, pairs + j) */
+    MIXRT_ROTARY_PAIRS = 1    /* (2 j, 2 j + 1) */
+};
+
+/* Rotary positions with several axes: pair j of every head of a token turns
+ * by angle_j = pos[token][axis[j]] * freq[j] (one product in 32 bits):
+ *   (x1, x2) -> (x1 cos - x2 sin, x2 cos + x1 sin);
+ * elements past the pairs are copied.  inverse != 0 turns by -angle: the
+ * gradient's map. */
+typedef struct {
+    int64_t tokens;       /* >= 0, < 2^31 */
+    int32_t axes;         /* 1..MIXRT_MAX_AXES */
+    int32_t pairs;        /* 0..head_dim / 2 */
+    int32_t layout;       /* mixrt_rotary_layout */
+    int32_t inverse;
+    const float *pos;     /* device [tokens][axes] */
+    const float *freq;    /* device [pairs] */
+    const uint8_t *axis;  /* device [pairs], each below axes (a larger one is
+                             taken as axes - 1) */
+} mixrt_rotary;
+
+/* Heads to turn: element (token, head, d) at token * token_stride +
+ * head * head_stride + d; out may be x with x's strides. */
+typedef struct {
+    int32_t heads;        /* >= 0, at most 65535 */
+    int32_t head_dim;     /* 1..1024 */
+    int32_t dtype;        /* MIXRT_F32, _F16 or _BF16 */
+    const void *x;
+    void *out;
+    int64_t x_token_stride, x_head_stride, out_token_stride, out_head_stride;
+} mixrt_heads;
+
+/* Turn up to MIXRT_MAX_HEADS_ARRAYS arrays of heads (queries and keys) of the
+ * same tokens in one launch; heads: host array of n descriptors with one
+ * dtype, outputs apart from each other. */
+#define MIXRT_MAX_HEADS_ARRAYS 2
+int mixrt_rotary_apply(mixrt_ctx *ctx, const mixrt_rotary *rotary, const mixrt_heads *heads,
+                       int32_t n);
 
 /* ---- errors ------------------------------------------------------------------- */
 

@@ -19,21 +19,9 @@
 #include <string>
 
 #include "mixrt_common.hpp"
+#include "mixrt_ctx.hpp"
 #include "mixrt_launch.hpp"
 #include "mixrt_mesh.hpp"
-
-struct mixrt_ctx {
-    int device = 0;
-    hipStream_t stream = nullptr;
-    uint32_t flags = 0;
-    int32_t tile_stripe = 0;
-    int32_t early_stop_chunk = 0;
-    int32_t block_levels = 0;
-    unsigned int *work = nullptr;   // device: the render kernels' work counters
-    int cus = 0;
-    int64_t l2_bytes = 0;
-    std::string err;
-};
 
 // The work counters of mixrt_render_noalloc: one array per device (each
 // device holds its own copy), found with hipGetSymbolAddress at set-up.
@@ -47,9 +35,58 @@ struct mixrt_mesh {
     mixrt_mesh_info info{};
 };
 
-namespace {
+namespace mixrt {
 
 thread_local std::string t_err;
+
+int fail(mixrt_ctx *ctx, int code, const char *fmt, ...)
+{
+    char buf[512];
+    va_list ap;
+    va_start(ap, fmt);
+    vsnprintf(buf, sizeof buf, fmt, ap);
+    va_end(ap);
+    t_err = buf;
+    if (ctx) ctx->err = buf;
+    return code;
+}
+
+void clear_err(mixrt_ctx *ctx)
+{
+    t_err.clear();
+    if (ctx) ctx->err.clear();
+}
+
+int finish_launch(mixrt_ctx *ctx, hipError_t e, const char *what)
+{
+    if (e != hipSuccess)
+        return fail(ctx, MIXRT_EDEVICE, "%s: launch failed: %s", what, hipGetErrorString(e));
+    if (ctx->flags & MIXRT_FLAG_SYNC_CHECK) {
+        e = hipStreamSynchronize(ctx->stream);
+        if (e == hipSuccess) e = hipGetLastError();
+        if (e != hipSuccess)
+            return fail(ctx, MIXRT_EDEVICE, "%s: device error: %s", what, hipGetErrorString(e));
+    }
+    return MIXRT_OK;
+}
+
+int bind_device(mixrt_ctx *ctx)
+{
+    hipError_t e = hipSetDevice(ctx->device);
+    if (e != hipSuccess)
+        return fail(ctx, MIXRT_EDEVICE, "hipSetDevice(%d): %s", ctx->device, hipGetErrorString(e));
+    return MIXRT_OK;
+}
+
+}  // namespace mixrt
+
+namespace {
+
+using mixrt::bind_device;
+using mixrt::clear_err;
+using mixrt::fail;
+using mixrt::finish_launch;
+using mixrt::t_err;
 
 // Device address of `scratch` on each device that a context was created on
 // (null: not set up).  In host code the array's name stands for a host-side
@@ -73,24 +110,6 @@ hipError_t scratch_setup(int device)
     if (e != hipSuccess) return e;
     g_scratch[device].store(ptr);
     return hipSuccess;
-}
-
-int fail(mixrt_ctx *ctx, int code, const char *fmt, ...)
-{
-    char buf[512];
-    va_list ap;
-    va_start(ap, fmt);
-    vsnprintf(buf, sizeof buf, fmt, ap);
-    va_end(ap);
-    t_err = buf;
-    if (ctx) ctx->err = buf;
-    return code;
-}
-
-void clear_err(mixrt_ctx *ctx)
-{
-    t_err.clear();
-    if (ctx) ctx->err.clear();
 }
 
 bool aligned16(const void *p) { return ((uintptr_t)p & 15u) == 0; }
@@ -373,27 +392,6 @@ void fill_grid_params(mixrt::GridParams &gp, const mixrt_hash_grid *g)
             gp.n_dense = l + 1;  // resolutions increase, so dense levels are a prefix
         }
     }
-}
-
-int finish_launch(mixrt_ctx *ctx, hipError_t e, const char *what)
-{
-    if (e != hipSuccess)
-        return fail(ctx, MIXRT_EDEVICE, "%s: launch failed: %s", what, hipGetErrorString(e));
-    if (ctx->flags & MIXRT_FLAG_SYNC_CHECK) {
-        e = hipStreamSynchronize(ctx->stream);
-        if (e == hipSuccess) e = hipGetLastError();
-        if (e != hipSuccess)
-            return fail(ctx, MIXRT_EDEVICE, "%s: device error: %s", what, hipGetErrorString(e));
-    }
-    return MIXRT_OK;
-}
-
-int bind_device(mixrt_ctx *ctx)
-{
-    hipError_t e = hipSetDevice(ctx->device);
-    if (e != hipSuccess)
-        return fail(ctx, MIXRT_EDEVICE, "hipSetDevice(%d): %s", ctx->device, hipGetErrorString(e));
-    return MIXRT_OK;
 }
 
 }  // namespace

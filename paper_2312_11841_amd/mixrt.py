@@ -21,13 +21,16 @@ MIXRT_EINVAL = -1
 MIXRT_ENOMEM = -2
 MIXRT_EDEVICE = -3
 MIXRT_EUNSUPPORTED = -4
-MIXRT_F32, MIXRT_F16, MIXRT_U8 = 0, 1, 2
+MIXRT_F32, MIXRT_F16, MIXRT_U8, MIXRT_BF16 = 0, 1, 2, 3
 MIXRT_DISP_ALONG_RAY, MIXRT_DISP_SH_VEC3, MIXRT_DISP_NONE = 0, 1, 2
 _DISP = {"ray": MIXRT_DISP_ALONG_RAY, "vec3": MIXRT_DISP_SH_VEC3, "none": MIXRT_DISP_NONE}
 MIXRT_FLAG_SYNC_CHECK = 1
 MIXRT_FLAG_BLOCKS_FULL, MIXRT_FLAG_BLOCKS_TWO = 2, 4
 _BLOCKS = {None: 0, "full": MIXRT_FLAG_BLOCKS_FULL, "two": MIXRT_FLAG_BLOCKS_TWO}
 MAX_VIEWS, MAX_LEVELS, MAX_LAYERS = 16, 32, 8
+ACTS = {"none": 0, "relu": 1, "silu": 2, "gelu": 3}
+ROTARY_LAYOUTS = {"halves": 0, "pairs": 1}
+KEPT_GROUP = 32     # channels that share a scale in the 8-bit form
 
 # Every symbol include/mixrt.h declares.
 EXPORTS = (
@@ -38,6 +41,9 @@ EXPORTS = (
     "mixrt_debug_hash_encode", "mixrt_debug_mlp", "mixrt_debug_composite",
     "mixrt_mesh_plan", "mixrt_mesh_create", "mixrt_mesh_get_info", "mixrt_mesh_destroy",
     "mixrt_raycast", "mixrt_rasterize",
+    "mixrt_norm_workspace", "mixrt_norm_forward", "mixrt_norm_backward",
+    "mixrt_kept_pack", "mixrt_kept_unpack",
+    "mixrt_linear_grad_workspace", "mixrt_linear_grad", "mixrt_rotary_apply",
     "mixrt_status_string", "mixrt_last_error", "mixrt_thread_error",
 )
 RAY_T_MIN = 1e-4
@@ -107,6 +113,34 @@ class MeshInfo(C.Structure):
                 ("n_faces", C.c_int64), ("n_refs", C.c_int64), ("device_bytes", C.c_int64)]
 
 
+class Norm(C.Structure):
+    _fields_ = [("images", C.c_int32), ("channels", C.c_int32), ("pixels", C.c_int64),
+                ("groups", C.c_int32), ("dtype", C.c_int32), ("act", C.c_int32),
+                ("eps", C.c_float), ("gamma", C.c_void_p), ("beta", C.c_void_p)]
+
+
+class Map(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("image_stride", C.c_int64), ("pixel_stride", C.c_int64)]
+
+
+class Kept(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("channels", C.c_int32), ("dtype", C.c_int32),
+                ("codes", C.c_void_p), ("exps", C.c_void_p)]
+
+
+class Rotary(C.Structure):
+    _fields_ = [("tokens", C.c_int64), ("axes", C.c_int32), ("pairs", C.c_int32),
+                ("layout", C.c_int32), ("inverse", C.c_int32), ("pos", C.c_void_p),
+                ("freq", C.c_void_p), ("axis", C.c_void_p)]
+
+
+class Heads(C.Structure):
+    _fields_ = [("heads", C.c_int32), ("head_dim", C.c_int32), ("dtype", C.c_int32),
+                ("x", C.c_void_p), ("out", C.c_void_p), ("x_token_stride", C.c_int64),
+                ("x_head_stride", C.c_int64), ("out_token_stride", C.c_int64),
+                ("out_head_stride", C.c_int64)]
+
+
 _libs = {}
 
 
@@ -161,6 +195,19 @@ def lib(variant=None):
                                         C.POINTER(Camera), P, P]),
             "mixrt_rasterize": (C.c_int, [P, P, C.c_int32, C.c_int32, C.c_int32,
                                           C.POINTER(Camera), P, P]),
+            "mixrt_norm_workspace": (C.c_int, [C.POINTER(Norm), C.POINTER(C.c_size_t)]),
+            "mixrt_norm_forward": (C.c_int, [P, C.POINTER(Norm), C.POINTER(Map), C.POINTER(Map),
+                                             P, C.POINTER(Kept), P, C.c_size_t]),
+            "mixrt_norm_backward": (C.c_int, [P, C.POINTER(Norm), C.POINTER(Map), C.POINTER(Map),
+                                              C.POINTER(Kept), P, C.POINTER(Map), P, P, P,
+                                              C.c_size_t]),
+            "mixrt_kept_pack": (C.c_int, [P, C.POINTER(Kept), P, I64]),
+            "mixrt_kept_unpack": (C.c_int, [P, C.POINTER(Kept), C.c_int32, P, I64]),
+            "mixrt_linear_grad_workspace": (C.c_int, [C.POINTER(Kept), C.c_int32,
+                                                      C.POINTER(C.c_size_t)]),
+            "mixrt_linear_grad": (C.c_int, [P, C.POINTER(Kept), C.c_int32, P, I64, P, P, P,
+                                            C.c_size_t]),
+            "mixrt_rotary_apply": (C.c_int, [P, C.POINTER(Rotary), C.POINTER(Heads), C.c_int32]),
             "mixrt_status_string": (C.c_char_p, [C.c_int]),
             "mixrt_last_error": (C.c_char_p, [P]),
             "mixrt_thread_error": (C.c_char_p, []),
@@ -400,6 +447,118 @@ class DeviceMesh:
             pass
 
 
+# --- arrays of the refiner's operators ---------------------------------------------
+
+_CODES = {}     # torch dtype -> mixrt_dtype, filled at the first use of torch
+
+
+def _elem_code(dtype, name: str) -> int:
+    if not _CODES:
+        import torch
+        _CODES.update({torch.float32: MIXRT_F32, torch.float16: MIXRT_F16,
+                       torch.bfloat16: MIXRT_BF16})
+    code = _CODES.get(dtype)
+    if code is None:
+        raise ValueError(f"{name}: dtype {dtype}, expected float32, float16 or bfloat16")
+    return code
+
+
+def _on_gpu(t, name: str, device: int):
+    import torch
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name}: expected a torch.Tensor, got {type(t).__name__}")
+    if t.get_device() != device:
+        raise ValueError(f"{name}: on {t.device}, expected cuda:{device}")
+
+
+def _like(t, name: str, shape, dtype, device: int):
+    """Check an output or second input against the array it belongs to."""
+    _on_gpu(t, name, device)
+    if t.dtype != dtype:
+        raise ValueError(f"{name}: dtype {t.dtype}, expected {dtype}")
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {tuple(shape)}")
+
+
+def _run(shape, stride, name: str):
+    """(elements, stride) of some dimensions taken as one, or ValueError if
+    their strides do not allow it."""
+    count, step, span = 1, 0, 0
+    for n, s in zip(reversed(shape), reversed(stride)):
+        if n != 1 and count == 1:
+            step, span = s, s * n
+        elif n != 1:
+            if n and count and s != span:
+                raise ValueError(f"{name}: strides {tuple(stride)} of dimensions "
+                                 f"{tuple(shape)} do not make one")
+            span *= n
+        count *= n
+    return count, step
+
+
+def _as_map(t, name: str):
+    """(images, pixels, channels, Map) of a tensor [images, ..., channels]."""
+    if t.dim() < 2:
+        raise ValueError(f"{name}: {t.dim()} dimensions, expected [images, ..., channels]")
+    shape, stride = t.shape, t.stride()
+    if stride[-1] != 1 and shape[-1] > 1:
+        raise ValueError(f"{name}: channels are not neighbours (stride {stride[-1]})")
+    if len(shape) == 3:
+        pixels, step = shape[1], stride[1]
+    else:
+        pixels, step = _run(shape[1:-1], stride[1:-1], name)
+    return shape[0], pixels, shape[-1], Map(t.data_ptr(), stride[0], step)
+
+
+def _as_rows(t, name: str):
+    """(rows, channels, row stride) of a tensor [..., channels]."""
+    if t.dim() < 1:
+        raise ValueError(f"{name}: no dimensions, expected [..., channels]")
+    shape, stride = t.shape, t.stride()
+    if stride[-1] != 1 and shape[-1] > 1:
+        raise ValueError(f"{name}: channels are not neighbours (stride {stride[-1]})")
+    if len(shape) == 2:
+        return shape[0], shape[1], stride[0]
+    rows, step = _run(shape[:-1], stride[:-1], name)
+    return rows, shape[-1], step
+
+
+def _per_channel(t, name: str, channels: int, device: int) -> int:
+    """Address of a float32 vector of one value per channel (None: 0)."""
+    if t is None:
+        return 0
+    import torch
+    _like(t, name, (channels,), torch.float32, device)
+    if channels > 1 and t.stride(0) != 1:
+        raise ValueError(f"{name}: not contiguous")
+    return t.data_ptr()
+
+
+@dataclass
+class Checkpoint:
+    """Activations kept in 8 bits: codes int8 [rows, channels], exps uint8
+    [rows, ceil(channels / 32)] (both contiguous), and the activations' type.
+    A value is codes * 2^(exps - 127) of its group of 32 channels; exps 255
+    marks a group that held an infinity or a NaN and reads back as NaN."""
+
+    codes: object
+    exps: object
+    dtype: object
+
+    def descriptor(self, device: int) -> Kept:
+        import torch
+        _on_gpu(self.codes, "codes", device)
+        if self.codes.dim() != 2 or self.codes.dtype != torch.int8:
+            raise ValueError(f"codes: {self.codes.dtype} with {self.codes.dim()} dimensions, "
+                             "expected int8 [rows, channels]")
+        rows, channels = self.codes.shape
+        _like(self.exps, "exps", (rows, -(-channels // KEPT_GROUP)), torch.uint8, device)
+        if not (self.codes.is_contiguous() and self.exps.is_contiguous()):
+            raise ValueError("codes or exps: not contiguous")
+        return Kept(rows, channels, _elem_code(self.dtype, "checkpoint"),
+                    self.codes.data_ptr(), self.exps.data_ptr())
+
+
 # --- the library handle ------------------------------------------------------------
 
 class Renderer:
@@ -576,6 +735,211 @@ class Renderer:
         self._check(self._L.mixrt_debug_composite(self._h, _ptr(srgb), rays, C.byref(smp), bgc,
                                                 _ptr(out)))
         return out
+
+
+    # -- the refiner's operators
+    def _empty(self, shape, dtype):
+        """Device memory for an output.  Taken on this context's stream, so
+        that memory released to another stream is not handed out early."""
+        import torch
+        dev = torch.device("cuda", self.device)
+        if torch.cuda.current_stream(dev).cuda_stream == self.stream.cuda_stream:
+            return torch.empty(shape, dtype=dtype, device=dev)
+        with torch.cuda.stream(self.stream):
+            return torch.empty(shape, dtype=dtype, device=dev)
+
+    def _workspace(self, size: int):
+        """This context's scratch, at least size bytes.  Its calls run one
+        after another on its stream, so they share it."""
+        import torch
+        ws = getattr(self, "_ws", None)
+        if ws is None or ws.numel() < size:
+            ws = self._ws = self._empty((max(size, 1 << 16),), torch.uint8)
+        return ws
+
+    def _checkpoint(self, rows: int, channels: int, dtype) -> Checkpoint:
+        import torch
+        return Checkpoint(self._empty((rows, channels), torch.int8),
+                          self._empty((rows, -(-channels // KEPT_GROUP)), torch.uint8), dtype)
+
+    def _norm(self, x, groups, gamma, beta, eps, act, name):
+        """(descriptor, map of x, workspace) of a norm over x."""
+        _on_gpu(x, name, self.device)
+        images, pixels, channels, xmap = _as_map(x, name)
+        if act not in ACTS:
+            raise ValueError(f"act: {act!r}, expected one of {tuple(ACTS)}")
+        d = Norm(images, channels, pixels, int(groups), _elem_code(x.dtype, name), ACTS[act],
+                 float(eps), _per_channel(gamma, "gamma", channels, self.device),
+                 _per_channel(beta, "beta", channels, self.device))
+        size = C.c_size_t()
+        if self._L.mixrt_norm_workspace(C.byref(d), C.byref(size)) != MIXRT_OK:
+            raise MixrtError(MIXRT_EINVAL, self._L.mixrt_thread_error().decode())
+        return d, xmap, self._workspace(size.value)
+
+    def _norm_forward(self, x, groups, gamma, beta, eps, act, out, stats, kept):
+        d, xmap, ws = self._norm(x, groups, gamma, beta, eps, act, "x")
+        if out is None:
+            out = self._empty(x.shape, x.dtype)
+        else:
+            _like(out, "out", x.shape, x.dtype, self.device)
+        ymap = _as_map(out, "out")[3]
+        kd = None if kept is None else C.byref(kept.descriptor(self.device))
+        self._check(self._L.mixrt_norm_forward(self._h, C.byref(d), C.byref(xmap), C.byref(ymap),
+                                               _ptr(stats), kd, ws.data_ptr(), ws.numel()))
+        return out
+
+    def group_norm(self, x, groups: int, gamma=None, beta=None, *, eps: float = 1e-5,
+                   act: str = "none", out=None):
+        """act(group norm) of feature maps x [images, ..., channels] (float32,
+        float16 or bfloat16, channels last; a slice of a wider map will do).
+        gamma, beta: float32 [channels] or None.  out: x's shape and type, or
+        x itself."""
+        return self._norm_forward(x, groups, gamma, beta, eps, act, out, None, None)
+
+    def group_norm_train(self, x, groups: int, gamma=None, beta=None, *, eps: float = 1e-5,
+                         act: str = "none", out=None):
+        """(y, stats, kept) for a training step: y as group_norm gives it, the
+        groups' (mean, 1 / deviation) as float32 [images, groups, 2], and x
+        kept in 8 bits, which the same passes over x write."""
+        import torch
+        _on_gpu(x, "x", self.device)
+        images, pixels, channels, _ = _as_map(x, "x")
+        stats = self._empty((images, int(groups), 2), torch.float32)
+        kept = self._checkpoint(images * pixels, channels, x.dtype)
+        return self._norm_forward(x, groups, gamma, beta, eps, act, out, stats, kept), stats, kept
+
+    def group_norm_backward(self, dy, saved, stats, gamma=None, beta=None, *, act: str = "none",
+                            out=None):
+        """(dx, dgamma, dbeta) of group_norm_train at dy; saved: its kept form
+        of x, or x itself.  dgamma, dbeta: float32 [channels].  out: where dx
+        goes (dy itself will do)."""
+        import torch
+        if not isinstance(stats, torch.Tensor) or stats.dim() != 3:
+            raise ValueError("stats: expected a torch.Tensor [images, groups, 2]")
+        d, dmap, ws = self._norm(dy, stats.shape[1], gamma, beta, 0.0, act, "dy")
+        _like(stats, "stats", (d.images, d.groups, 2), torch.float32, self.device)
+        if not stats.is_contiguous():
+            raise ValueError("stats: not contiguous")
+        xd = kd = None
+        if isinstance(saved, Checkpoint):
+            kd = C.byref(saved.descriptor(self.device))
+        else:
+            _like(saved, "saved", dy.shape, dy.dtype, self.device)
+            xd = C.byref(_as_map(saved, "saved")[3])
+        if out is None:
+            out = self._empty(dy.shape, dy.dtype)
+        else:
+            _like(out, "out", dy.shape, dy.dtype, self.device)
+        grads = self._empty((2, d.channels), torch.float32)
+        dgamma, dbeta = grads[0], grads[1]
+        self._check(self._L.mixrt_norm_backward(
+            self._h, C.byref(d), C.byref(dmap), xd, kd, stats.data_ptr(),
+            C.byref(_as_map(out, "out")[3]), dgamma.data_ptr(), dbeta.data_ptr(), ws.data_ptr(),
+            ws.numel()))
+        return out, dgamma, dbeta
+
+    def checkpoint_pack(self, x) -> Checkpoint:
+        """x [..., channels] kept in 8 bits."""
+        _on_gpu(x, "x", self.device)
+        rows, channels, stride = _as_rows(x, "x")
+        _elem_code(x.dtype, "x")
+        kept = self._checkpoint(rows, channels, x.dtype)
+        kd = kept.descriptor(self.device)
+        self._check(self._L.mixrt_kept_pack(self._h, C.byref(kd), x.data_ptr(), stride))
+        return kept
+
+    def checkpoint_unpack(self, kept: Checkpoint, dtype=None, out=None):
+        """The kept values [rows, channels], in the activations' type or
+        another float type."""
+        kd = kept.descriptor(self.device)
+        if out is None:
+            out = self._empty((kd.rows, kd.channels), kept.dtype if dtype is None else dtype)
+        else:
+            _like(out, "out", (kd.rows, kd.channels), dtype or out.dtype, self.device)
+        stride = _as_rows(out, "out")[2]
+        self._check(self._L.mixrt_kept_unpack(self._h, C.byref(kd), _elem_code(out.dtype, "out"),
+                                              out.data_ptr(), stride))
+        return out
+
+    def linear_weight_grad(self, kept: Checkpoint, dy, bias: bool = True):
+        """(dw, db) of a linear layer y = x w + b over rows, from its kept
+        input and dy [..., outs]: float32 [channels, outs] and [outs] (None
+        without bias)."""
+        import torch
+        kd = kept.descriptor(self.device)
+        _on_gpu(dy, "dy", self.device)
+        if dy.dtype != kept.dtype:
+            raise ValueError(f"dy: dtype {dy.dtype}, expected the checkpoint's {kept.dtype}")
+        rows, outs, stride = _as_rows(dy, "dy")
+        if rows != kd.rows:
+            raise ValueError(f"dy: {rows} rows, the checkpoint has {kd.rows}")
+        size = C.c_size_t()
+        if self._L.mixrt_linear_grad_workspace(C.byref(kd), outs, C.byref(size)) != MIXRT_OK:
+            raise MixrtError(MIXRT_EINVAL, self._L.mixrt_thread_error().decode())
+        ws = self._workspace(size.value)
+        dw = self._empty((kd.channels, outs), torch.float32)
+        db = self._empty((outs,), torch.float32) if bias else None
+        self._check(self._L.mixrt_linear_grad(self._h, C.byref(kd), outs, dy.data_ptr(), stride,
+                                              dw.data_ptr(), _ptr(db), ws.data_ptr(), ws.numel()))
+        return dw, db
+
+    def rotary(self, heads, pos, freq, axis, *, layout: str = "halves", inverse: bool = False,
+               out=None):
+        """The arrays of heads (one tensor [tokens..., heads, D], or a tuple
+        of up to two: queries and keys) turned by their tokens' positions, as
+        a tuple or one tensor likewise.  pos: float32 [tokens..., axes]; freq:
+        float32 [pairs]; axis: uint8 [pairs], the axis each pair turns with;
+        layout: "halves" pairs element j with j + pairs, "pairs" 2 j with
+        2 j + 1.  inverse: the other way round (the gradient's map).  out:
+        tensors to write, each may be its input."""
+        import torch
+        single = isinstance(heads, torch.Tensor)
+        arrays = (heads,) if single else tuple(heads)
+        outs = (None,) * len(arrays) if out is None else ((out,) if single else tuple(out))
+        if len(outs) != len(arrays) or not 1 <= len(arrays) <= 2:
+            raise ValueError(f"{len(arrays)} arrays and {len(outs)} outputs, expected 1 or 2")
+        if layout not in ROTARY_LAYOUTS:
+            raise ValueError(f"layout: {layout!r}, expected one of {tuple(ROTARY_LAYOUTS)}")
+        for t, name, dt in ((pos, "pos", torch.float32), (freq, "freq", torch.float32),
+                            (axis, "axis", torch.uint8)):
+            _on_gpu(t, name, self.device)
+            if t.dtype != dt or not t.is_contiguous():
+                raise ValueError(f"{name}: {t.dtype}, expected contiguous {dt}")
+        if pos.dim() < 1 or freq.dim() != 1 or axis.shape != freq.shape:
+            raise ValueError(f"pos {tuple(pos.shape)}, freq {tuple(freq.shape)}, axis "
+                             f"{tuple(axis.shape)}: expected [..., axes], [pairs], [pairs]")
+        axes, pairs = pos.shape[-1], freq.shape[0]
+        if axes < 1:
+            raise ValueError("pos: no axes")
+        tokens = pos.numel() // axes
+        d = Rotary(tokens, axes, pairs, ROTARY_LAYOUTS[layout], int(bool(inverse)),
+                   pos.data_ptr(), freq.data_ptr(), axis.data_ptr())
+        descs, got = (Heads * len(arrays))(), []
+        for i, (x, o) in enumerate(zip(arrays, outs)):
+            name = f"heads[{i}]"
+            _on_gpu(x, name, self.device)
+            if x.dim() < 2:
+                raise ValueError(f"{name}: {x.dim()} dimensions, expected [..., heads, D]")
+            if o is None:
+                o = self._empty(x.shape, x.dtype)
+            else:
+                _like(o, f"out[{i}]", x.shape, x.dtype, self.device)
+            got.append(o)
+            code, ends = _elem_code(x.dtype, name), []
+            for t in (x, o):
+                shape, stride = t.shape, t.stride()
+                if stride[-1] != 1 and shape[-1] > 1:
+                    raise ValueError(f"{name}: elements of a head are not neighbours")
+                if len(shape) == 3:
+                    n, step = shape[0], stride[0]
+                else:
+                    n, step = _run(shape[:-2], stride[:-2], name)
+                if n != tokens:
+                    raise ValueError(f"{name}: {n} tokens, pos has {tokens}")
+                ends += [step, stride[-2]]
+            descs[i] = Heads(x.shape[-2], x.shape[-1], code, x.data_ptr(), o.data_ptr(), *ends)
+        self._check(self._L.mixrt_rotary_apply(self._h, C.byref(d), descs, len(arrays)))
+        return got[0] if single else tuple(got)
 
 
 def validate(gbuf, cams, disp, grid, mlp, smp):

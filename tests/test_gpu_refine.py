@@ -1,0 +1,500 @@
+"""The refiner's operators on the GPU against 64-bit statements on the CPU
+(tests/refine_ref.py, which derives the bounds): group norm with its
+activations and gradients, activations kept in 8 bits, the weight gradient of
+a linear layer from them, and rotary positions."""
+import math
+
+import pytest
+
+import refine_ref as ref
+from paper_2312_11841_amd import mixrt
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+DT = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
+
+
+@pytest.fixture(scope="module")
+def r():
+    r = mixrt.Renderer(0, sync_check=True)
+    yield r
+    r.close()
+
+
+def say(*a):
+    print(*a, flush=True)
+
+
+def _gen(seed):
+    return torch.Generator().manual_seed(seed)
+
+
+def _maps(g, N, P, C, dtype, pad=0, level=0.5):
+    """A feature map on the GPU (with pad, a slice of a wider one)."""
+    x = torch.randn((N, P, C + pad), generator=g) + level * torch.randn((C + pad,), generator=g)
+    return x.to(dtype).to("cuda:0")[..., :C]
+
+
+def _inside(got, want, bound, what):
+    got = got.double().cpu()
+    assert got.shape == want.shape, what
+    nan = torch.isnan(want)
+    assert torch.equal(torch.isnan(got), nan), what
+    over = ((got - want).abs() - bound)[~nan]
+    assert over.numel() == 0 or float(over.max()) <= 0, (what, float(over.max()))
+
+
+# --- group norm ---------------------------------------------------------------------
+
+# images, pixels, channels, groups: one element; one pixel; one channel; odd
+# channels; groups narrower than, straddling and wider than a vector; rows of
+# one and of several blocks; more vectors than a block has threads
+SHAPES = [(1, 1, 1, 1), (2, 1, 8, 2), (1, 77, 1, 1), (3, 50, 3, 3), (2, 131, 12, 4),
+          (1, 513, 20, 4), (2, 300, 24, 3), (1, 1961, 33, 11), (1, 4096, 16, 4), (2, 700, 64, 8),
+          (1, 40, 96, 1), (5, 9, 40, 5), (1, 19, 2056, 1), (1, 5, 4096, 32), (1, 20000, 32, 8)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("shape", SHAPES, ids=str)
+def test_norm_and_gradients(r, shape, dtype):
+    N, P, C, G = shape
+    i = SHAPES.index(shape)
+    kind = ["none", "silu", "gelu", "relu"][i % 4]
+    pad = [0, 1, 8][i % 3]
+    dt = DT[dtype]
+    say("norm", shape, dtype, kind, pad)
+    g = _gen(i)
+    x = _maps(g, N, P, C, dt, pad)
+    affine = i % 5 != 0
+    gamma = (1 + 0.3 * torch.randn((C,), generator=g)).cuda() if affine else None
+    beta = (0.3 * torch.randn((C,), generator=g)).cuda() if affine else None
+    cpu = lambda t: None if t is None else t.cpu()  # noqa: E731
+    y = r.group_norm(x, G, gamma, beta, eps=1e-4, act=kind)
+    want, bound, mean, rstd = ref.norm(x.cpu(), G, cpu(gamma), cpu(beta), 1e-4, kind, dt)
+    _inside(y, want, bound, "y")
+
+    yt, stats, kept = r.group_norm_train(x, G, gamma, beta, eps=1e-4, act=kind)
+    assert torch.equal(yt, y)
+    scale = x.double().abs().amax().cpu() + 1
+    _inside(stats[..., 0], mean, 4 * ref.U * scale, "mean")
+    _inside(stats[..., 1], rstd, 8 * ref.U * rstd * (1 + (rstd * 1e-2) ** 2), "rstd")
+    codes, exps, values = ref.keep(x.cpu().reshape(-1, C)[:200])
+    assert torch.equal(kept.codes[:200].cpu(), codes)
+    assert torch.equal(kept.exps[:200].cpu(), exps)
+
+    back = "gelu" if kind == "relu" else kind   # relu's jump: its own test
+    dy = (0.1 * torch.randn((N, P, C), generator=g) + 0.01).to(dt).cuda()
+    xk = r.checkpoint_unpack(kept).reshape(N, P, C)
+    for saved, at in ((kept, xk), (x, x)):
+        dx, dgamma, dbeta = r.group_norm_backward(dy, saved, stats, gamma, beta, act=back)
+        want, bound = ref.norm_back(dy.cpu(), at.cpu(), stats.cpu(), cpu(gamma), cpu(beta), back,
+                                    dt)
+        for name, got in (("dx", dx), ("dgamma", dgamma), ("dbeta", dbeta)):
+            _inside(got, want[name], bound[name], name)
+
+
+def test_relu_gradient_away_from_its_jump(r):
+    g = _gen(3)
+    x = _maps(g, 2, 400, 16, torch.float32)
+    y, stats, _ = r.group_norm_train(x, 4, act="relu")
+    z = r.group_norm(x, 4)
+    dy = torch.randn((2, 400, 16), generator=g).cuda()
+    dy[z.abs() < 1e-4] = 0      # either side of the jump gives the same
+    dx, dgamma, dbeta = r.group_norm_backward(dy, x, stats, act="relu")
+    want, bound = ref.norm_back(dy.cpu(), x.cpu(), stats.cpu(), None, None, "relu", torch.float32)
+    for name, got in (("dx", dx), ("dgamma", dgamma), ("dbeta", dbeta)):
+        _inside(got, want[name], bound[name], name)
+
+
+@pytest.mark.parametrize("kind", ["none", "silu", "gelu"])
+def test_norm_gradient_against_differences(r, kind):
+    """Central differences of sum(dy * y), in 64 bits, in random directions:
+    the formula's gradients are the function's."""
+    g = _gen(11)
+    N, P, C, G = 2, 37, 12, 3
+    x = torch.randn((N, P, C), generator=g)
+    gamma, beta = 1 + 0.3 * torch.randn((C,), generator=g), 0.3 * torch.randn((C,), generator=g)
+    dy = torch.randn((N, P, C), generator=g)
+    _, stats, _ = r.group_norm_train(x.cuda(), G, gamma.cuda(), beta.cuda(), eps=1e-3, act=kind)
+    dx, dgamma, dbeta = (t.double().cpu() for t in r.group_norm_backward(
+        dy.cuda(), x.cuda(), stats, gamma.cuda(), beta.cuda(), act=kind))
+    f = lambda a, b, c: float((dy.double() * ref.norm(  # noqa: E731
+        a, G, b, c, 1e-3, kind, torch.float32)[0]).sum())
+    for i, grad in enumerate((dx, dgamma, dbeta)):
+        v = torch.randn(grad.shape, generator=g).double()
+        at = [x.double(), gamma.double(), beta.double()]
+        h = 1e-4
+        ends = []
+        for s in (h, -h):
+            moved = list(at)
+            moved[i] = at[i] + s * v
+            ends.append(f(*moved))
+        num, ana = (ends[0] - ends[1]) / (2 * h), float((grad * v).sum())
+        # truncation h^2 times third derivatives of order 1 per element, and
+        # the 32-bit gradient's own error
+        assert abs(num - ana) <= 1e-5 * float((grad.abs() * v.abs()).sum()) + 1e-5, (i, num, ana)
+
+
+def test_norm_far_mean_and_constant_groups(r):
+    """A mean 4000 deviations away keeps the variance; a constant group has
+    none and its output is beta."""
+    g = _gen(5)
+    x = torch.randn((1, 3000, 8), generator=g) * 0.25 + 1000.0
+    x[..., 4:] = 7.0
+    beta = torch.randn((8,), generator=g)
+    y, stats, _ = r.group_norm_train(x.cuda(), 2, None, beta.cuda(), eps=1e-5)
+    want, bound, mean, rstd = ref.norm(x, 2, None, beta, 1e-5, "none", torch.float32)
+    _inside(y, want, bound, "y")
+    assert abs(float(stats[0, 0, 1]) / float(rstd[0, 0]) - 1) < 1e-6
+    assert torch.equal(y[..., 4:].cpu(), beta[4:].expand(1, 3000, 4))
+
+
+def test_norm_non_finite_values_stay_in_their_group(r):
+    g = _gen(6)
+    for bad in (math.nan, math.inf, -math.inf):
+        x = torch.randn((2, 100, 64), generator=g).to(torch.bfloat16).cuda()
+        x[1, 17, 20] = bad              # image 1, group 2 of 8
+        y, stats, kept = r.group_norm_train(x, 8, act="silu")
+        hit = torch.zeros((2, 100, 64), dtype=torch.bool)
+        hit[1, :, 16:24] = True
+        assert torch.equal(torch.isnan(y).cpu(), hit)
+        v = torch.isnan(r.checkpoint_unpack(kept)).cpu().reshape(2, 100, 64)
+        kept_hit = torch.zeros_like(hit)
+        kept_hit[1, 17, :32] = True     # its 32 channels of that pixel
+        assert torch.equal(v, kept_hit)
+
+
+def test_norm_empty_arrays(r):
+    for N, P in ((0, 5), (3, 0)):
+        x = torch.empty((N, P, 8), dtype=torch.float16, device="cuda")
+        y, stats, kept = r.group_norm_train(x, 2, eps=0.25)
+        assert y.shape == x.shape and kept.codes.shape == (0, 8)
+        assert torch.equal(stats.cpu(), torch.tensor([0.0, 2.0]).expand(N, 2, 2))
+        dx, dgamma, dbeta = r.group_norm_backward(x, kept, stats)
+        assert dx.shape == x.shape
+        assert float(dgamma.abs().sum()) == 0.0 == float(dbeta.abs().sum())
+
+
+def test_norm_layouts_in_place_and_images(r):
+    """4-d maps, a crop of channels as output, in place, repeated inputs, and
+    images interleaved by pixel give what dense arrays give."""
+    g = _gen(8)
+    x = torch.randn((2, 6, 7, 24), generator=g).to(torch.float16).cuda()
+    want = r.group_norm(x, 3, act="gelu")
+    wider = torch.zeros((2, 6, 7, 31), dtype=torch.float16, device="cuda")
+    out = r.group_norm(x, 3, act="gelu", out=wider[..., 5:29])
+    assert torch.equal(out, want) and float(wider[..., :5].abs().sum()) == 0
+    assert float(wider[..., 29:].abs().sum()) == 0
+    inter = torch.empty((42, 2, 24), dtype=torch.float16, device="cuda")
+    view = inter.transpose(0, 1)
+    view.copy_(x.reshape(2, 42, 24))
+    assert torch.equal(r.group_norm(view, 3, act="gelu", out=view), want.reshape(2, 42, 24))
+    one = x[:1].expand(3, 6, 7, 24)
+    assert torch.equal(r.group_norm(one, 3, act="gelu"), want[:1].expand(3, 6, 7, 24))
+    dy = torch.randn((2, 6, 7, 24), generator=g).to(torch.float16).cuda()
+    _, stats, kept = r.group_norm_train(x, 3)
+    dx = r.group_norm_backward(dy, kept, stats)[0]
+    assert torch.equal(r.group_norm_backward(dy, kept, stats, out=dy)[0], dx)
+
+
+def test_norm_offsets_past_32_bits(r):
+    """Images 2^31 + 16 elements apart in one buffer."""
+    g = _gen(9)
+    buf = torch.empty((2 ** 31 + 16 + 64 * 16,), dtype=torch.float16, device="cuda")
+    x = buf.as_strided((2, 64, 16), (2 ** 31 + 16, 16, 1))
+    small = torch.randn((2, 64, 16), generator=g).to(torch.float16).cuda()
+    x.copy_(small)
+    want = r.group_norm(small, 4, act="silu")
+    assert torch.equal(r.group_norm(x, 4, act="silu"), want)
+    assert torch.equal(r.group_norm(x, 4, act="silu", out=x), want)
+
+
+def test_outputs_are_the_same_bits_again_and_on_another_stream(r):
+    g = _gen(10)
+    x = _maps(g, 1, 30000, 48, torch.bfloat16)
+    dy = _maps(g, 1, 30000, 48, torch.bfloat16)
+
+    def step(rr):
+        y, stats, kept = rr.group_norm_train(x, 6, act="silu")
+        grads = rr.group_norm_backward(dy, kept, stats, act="silu")
+        lin = rr.linear_weight_grad(kept, dy.reshape(-1, 48))
+        return (y, stats, kept.codes, kept.exps, *grads, *lin)
+
+    first = step(r)
+    for got in step(r), step(r):
+        assert all(torch.equal(a, b) for a, b in zip(first, got))
+    torch.cuda.synchronize()
+    other = mixrt.Renderer(0, stream=torch.cuda.Stream())
+    try:
+        got = step(other)
+        other.sync()
+        assert all(torch.equal(a, b) for a, b in zip(first, got))
+    finally:
+        other.close()
+
+
+def test_a_captured_step_replays(r):
+    """One training step recorded into a graph gives the eager outputs on
+    every replay, with eager work between the replays."""
+    g = _gen(12)
+    x, dy = _maps(g, 1, 5000, 32, torch.float16), _maps(g, 1, 5000, 32, torch.float16)
+    q = _maps(g, 100, 4, 64, torch.float16)
+    pos = torch.randint(0, 50, (100, 3), generator=g).float().cuda()
+    freq = torch.rand((32,), generator=g).cuda()
+    axis = torch.randint(0, 3, (32,), generator=g).to(torch.uint8).cuda()
+    stream = torch.cuda.Stream()
+    c = mixrt.Renderer(0, stream=stream)
+
+    def step():
+        y, stats, kept = c.group_norm_train(x, 8, act="silu")
+        return (y, *c.group_norm_backward(dy, kept, stats, act="silu"),
+                *c.linear_weight_grad(kept, dy.reshape(-1, 32)), c.rotary(q, pos, freq, axis))
+
+    try:
+        torch.cuda.synchronize()
+        want = [t.clone() for t in step()]     # also takes the workspace
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            outs = step()
+        for rep in range(4):
+            for o in outs:
+                o.zero_()
+            torch.cuda.synchronize()
+            graph.replay()
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(outs, want)), rep
+            r.group_norm(x, 8)
+    finally:
+        c.close()
+
+
+# --- activations in 8 bits -----------------------------------------------------------
+
+KEPT = [(1, 1), (3, 4), (7, 31), (65, 32), (40, 33), (129, 64), (53, 43), (300, 24), (17, 257),
+        (9, 1024), (2, 4096)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("shape", KEPT, ids=str)
+def test_kept_rows(r, shape, dtype):
+    rows, C = shape
+    dt = DT[dtype]
+    say("kept", shape, dtype)
+    g = _gen(rows * C)
+    # rows over many magnitudes; a row of zeros, of the least and of the
+    # greatest values, of halves between codes, and non-finite groups
+    x = torch.randn((rows, C), generator=g) * torch.exp(4 * torch.randn((rows, 1), generator=g))
+    if dtype == "f16":
+        x = x.clamp(-60000, 60000)
+    if rows > 6:
+        x[1] = 0
+        x[2] = torch.finfo(dt).max * torch.rand((C,), generator=g)
+        x[2, 0] = torch.finfo(dt).max
+        x[3] = ref.TINY[dt] * torch.randint(0, 9, (C,), generator=g)
+        x[4] = torch.randint(-255, 256, (C,), generator=g) * 0.5
+        x[5, C // 2] = math.nan
+        x[6, C - 1] = -math.inf
+    x = x.to(dt).cuda()
+    kept = r.checkpoint_pack(x)
+    codes, exps, values = ref.keep(x.cpu())
+    assert torch.equal(kept.codes.cpu(), codes)
+    assert torch.equal(kept.exps.cpu(), exps)
+    for odt in DT.values():
+        out = r.checkpoint_unpack(kept, dtype=odt)
+        want = values.to(odt) if odt != torch.float32 else values.float()
+        assert torch.equal(torch.nan_to_num(out.cpu().float(), nan=12345.0),
+                           torch.nan_to_num(want.float(), nan=12345.0)), odt
+    own = r.checkpoint_unpack(kept).double().cpu()
+    ok = torch.isfinite(values)
+    assert torch.equal(own[ok], values[ok])          # exact in its own type
+    # strided rows in and out
+    wide = torch.zeros((rows, C + 3), dtype=dt, device="cuda")
+    wide[:, 2:2 + C] = x
+    again = r.checkpoint_pack(wide[:, 2:2 + C])
+    assert torch.equal(again.codes, kept.codes) and torch.equal(again.exps, kept.exps)
+    wide.zero_()
+    r.checkpoint_unpack(kept, out=wide[:, 2:2 + C])
+    assert float(wide[:, :2].float().abs().sum()) == 0 == float(wide[:, -1].float().abs().sum())
+
+
+def test_kept_no_rows(r):
+    kept = r.checkpoint_pack(torch.empty((0, 40), device="cuda"))
+    assert kept.exps.shape == (0, 2) and r.checkpoint_unpack(kept).shape == (0, 40)
+    dw, db = r.linear_weight_grad(kept, torch.empty((0, 5), device="cuda"))
+    assert float(dw.abs().sum()) == 0.0 == float(db.abs().sum()) and dw.shape == (40, 5)
+
+
+# rows, channels, outs: one element, one row, ragged tiles each way, several
+# tiles, rows of one and of many parts
+LINEAR = [(1, 1, 1), (1, 64, 64), (31, 4, 8), (100, 33, 5), (130, 24, 67), (333, 130, 64),
+          (2000, 64, 64), (5000, 16, 4), (777, 100, 320), (257, 512, 36), (70001, 48, 12)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("shape", LINEAR, ids=str)
+def test_linear_weight_gradient(r, shape, dtype):
+    rows, C, outs = shape
+    dt = DT[dtype]
+    say("linear", shape, dtype)
+    g = _gen(rows + C + outs)
+    x = (torch.randn((rows, C), generator=g) * torch.exp(torch.randn((rows, 1), generator=g)))
+    kept = r.checkpoint_pack(x.to(dt).cuda())
+    buf = torch.randn((rows, outs + 3), generator=g).to(dt).cuda()
+    dy = buf[:, 1:1 + outs] if rows % 2 else buf[:, :outs].contiguous()
+    dw, db = r.linear_weight_grad(kept, dy)
+    xv, dv = r.checkpoint_unpack(kept).double().cpu(), dy.double().cpu()
+    # products are exact; a wave adds at most rows / parts of them one after
+    # another in 32 bits, the rest is joined: 4 u sqrt(rows) covers the walk,
+    # with the sum of magnitudes as its scale
+    scale = 4 * ref.U * math.sqrt(rows) + 8 * ref.U
+    _inside(dw, xv.t() @ dv, scale * (xv.abs().t() @ dv.abs()), "dw")
+    _inside(db, dv.sum(0), scale * dv.abs().sum(0), "db")
+    only, none = r.linear_weight_grad(kept, dy, bias=False)
+    assert none is None and torch.equal(only, dw)
+
+
+def test_linear_gradient_of_non_finite_rows(r):
+    """A group that was not finite makes its channels' weights NaN, no others."""
+    g = _gen(2)
+    x = torch.randn((50, 80), generator=g)
+    x[7, 40] = math.inf
+    kept = r.checkpoint_pack(x.cuda())
+    dw, db = r.linear_weight_grad(kept, torch.randn((50, 16), generator=g).cuda())
+    nan = torch.zeros((80, 16), dtype=torch.bool)
+    nan[32:64] = True
+    assert torch.equal(torch.isnan(dw).cpu(), nan) and bool(torch.isfinite(db).all())
+
+
+# --- rotary positions ----------------------------------------------------------------
+
+# tokens, heads, kv heads, D, pairs
+ROTARY = [(1, 32, 8, 128, 64), (1, 1, 1, 2, 1), (5, 3, 1, 80, 36), (130, 12, 3, 72, 36),
+          (77, 4, 2, 64, 32), (1000, 8, 8, 32, 16), (9, 2, 1, 33, 15), (20, 2, 2, 16, 0),
+          (3, 1, 1, 1024, 512), (600, 1, 1, 96, 44)]
+
+
+@pytest.mark.parametrize("layout", ["halves", "pairs"])
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("shape", ROTARY, ids=str)
+def test_rotary(r, shape, dtype, layout):
+    T, H, K, D, pairs = shape
+    dt = DT[dtype]
+    say("rotary", shape, dtype, layout)
+    g = _gen(T + D)
+    axes = 1 + T % 4
+    pos = torch.randint(-40, 300, (T, axes), generator=g).float().cuda() * 0.5
+    freq = torch.exp(-9 * torch.rand((pairs,), generator=g)).cuda()
+    axis = torch.randint(0, axes, (pairs,), generator=g).to(torch.uint8).cuda()
+    q = torch.randn((T, H, D), generator=g).to(dt).cuda()
+    # keys as a slice of heads laid out head-major in a wider buffer
+    k = torch.randn((K, T, D + 5), generator=g).to(dt).cuda()[..., 2:2 + D].transpose(0, 1)
+    tq, tk = r.rotary((q, k), pos, freq, axis, layout=layout)
+    for x, got in ((q, tq), (k, tk)):
+        want, bound = ref.turn(x.cpu(), pos.cpu(), freq.cpu(), axis.cpu(), layout, False, dt)
+        _inside(got, want, bound, "turned")
+    back = r.rotary(q, pos, freq, axis, layout=layout, inverse=True)
+    want, bound = ref.turn(q.cpu(), pos.cpu(), freq.cpu(), axis.cpu(), layout, True, dt)
+    _inside(back, want, bound, "inverse")
+    again = q.clone()
+    assert r.rotary(again, pos, freq, axis, layout=layout, out=again) is again
+    assert torch.equal(again, tq)
+    kk = k.clone(memory_format=torch.preserve_format)
+    into = torch.zeros((T, K + 1, D + 1), dtype=dt, device="cuda")
+    r.rotary(kk, pos, freq, axis, layout=layout, out=into[:, 1:, 1:])
+    assert torch.equal(into[:, 1:, 1:], tk)
+    assert float(into[:, 0].float().abs().sum()) == 0 == float(into[..., 0].float().abs().sum())
+
+
+def test_rotary_gradient_is_the_inverse_turn(r):
+    """<turn(x), dy> = <x, inverse turn(dy)>, and the differences of a linear
+    map are the map itself."""
+    g = _gen(4)
+    pos = torch.randint(0, 100, (60, 3), generator=g).float().cuda()
+    freq = torch.rand((20,), generator=g).cuda()
+    axis = torch.randint(0, 3, (20,), generator=g).to(torch.uint8).cuda()
+    x, dy = (torch.randn((60, 4, 48), generator=g).cuda() for _ in range(2))
+    for layout in ("halves", "pairs"):
+        a = r.rotary(x, pos, freq, axis, layout=layout).double() * dy.double()
+        b = x.double() * r.rotary(dy, pos, freq, axis, layout=layout, inverse=True).double()
+        size = float((x.double().abs() * dy.double().abs()).sum())
+        assert abs(float(a.sum() - b.sum())) <= 16 * ref.U * size
+
+
+def test_rotary_leading_dimensions_and_nothing(r):
+    g = _gen(7)
+    x = torch.randn((2, 3, 4, 5, 16), generator=g).cuda()
+    pos = torch.randint(0, 9, (2, 3, 4, 2), generator=g).float().cuda()
+    freq, axis = torch.rand((8,), generator=g).cuda(), torch.zeros(8, dtype=torch.uint8).cuda()
+    got = r.rotary(x, pos, freq, axis)
+    flat = r.rotary(x.reshape(24, 5, 16), pos.reshape(24, 2), freq, axis)
+    assert torch.equal(got.reshape(24, 5, 16), flat)
+    none = r.rotary((x[:0].reshape(0, 5, 16),), pos[:0].reshape(0, 2), freq, axis)
+    assert none[0].shape == (0, 5, 16)
+    q, k = r.rotary((flat, flat[:, :0]), pos.reshape(24, 2), freq, axis)
+    assert k.shape == (24, 0, 16) and q.shape == flat.shape
+
+
+def test_large_positions_keep_their_angle(r):
+    """Angles of 10^5 and more: the sine is of the 32-bit product, reduced
+    without loss."""
+    pos = torch.tensor([[1e5], [123456.0], [3e7]]).cuda()
+    freq, axis = torch.tensor([1.0, 0.37]).cuda(), torch.zeros(2, dtype=torch.uint8).cuda()
+    x = torch.ones((3, 1, 4)).cuda()
+    want, bound = ref.turn(x.cpu(), pos.cpu(), freq.cpu(), axis.cpu(), "halves", False,
+                           torch.float32)
+    _inside(r.rotary(x, pos, freq, axis), want, bound, "turned")
+
+
+# --- refusals by the binding (tensors are on the GPU here) ---------------------------
+
+def test_binding_refuses_wrong_tensors(r):
+    x = torch.zeros((2, 5, 8), device="cuda")
+    with pytest.raises(ValueError, match="dtype"):
+        r.group_norm(x.double(), 2)
+    with pytest.raises(ValueError, match="neighbours"):
+        r.group_norm(x.transpose(1, 2), 1)
+    with pytest.raises(ValueError, match="do not make one"):
+        r.group_norm(torch.zeros((2, 5, 6, 8), device="cuda")[:, :, :4], 2)
+    with pytest.raises(ValueError, match="expected cuda"):
+        r.group_norm(x.cpu(), 2)
+    with pytest.raises(ValueError, match="gamma"):
+        r.group_norm(x, 2, torch.ones(7, device="cuda"))
+    with pytest.raises(ValueError, match="gamma"):
+        r.group_norm(x, 2, torch.ones(8, device="cuda", dtype=torch.float16))
+    with pytest.raises(ValueError, match="act"):
+        r.group_norm(x, 2, act="swish")
+    with pytest.raises(ValueError, match="out"):
+        r.group_norm(x, 2, out=x[:1])
+    with pytest.raises(mixrt.MixrtError, match="groups"):
+        r.group_norm(x, 3)
+    with pytest.raises(mixrt.MixrtError, match="overlap"):
+        r.group_norm(x, 2, out=torch.zeros(8, device="cuda").expand(2, 5, 8))
+    y, stats, kept = r.group_norm_train(x, 2)
+    with pytest.raises(ValueError, match="stats"):
+        r.group_norm_backward(x, kept, stats[:1])
+    with pytest.raises(mixrt.MixrtError, match="kept"):
+        r.group_norm_backward(x[:1].contiguous(), kept, stats[:1].contiguous())
+    with pytest.raises(mixrt.MixrtError, match="dx is x"):
+        r.group_norm_backward(x.clone(), x, stats, out=x)
+    with pytest.raises(ValueError, match="rows"):
+        r.linear_weight_grad(kept, x[0])
+    with pytest.raises(ValueError, match="dtype"):
+        r.linear_weight_grad(kept, x.reshape(10, 8).half())
+    bad = mixrt.Checkpoint(kept.codes, kept.exps[:5], torch.float32)
+    with pytest.raises(ValueError, match="exps"):
+        r.checkpoint_unpack(bad)
+    freq, axis = torch.ones(2, device="cuda"), torch.zeros(2, device="cuda", dtype=torch.uint8)
+    pos = torch.zeros((5, 1), device="cuda")
+    h = torch.zeros((5, 2, 4), device="cuda")
+    with pytest.raises(ValueError, match="tokens"):
+        r.rotary(h, pos[:4], freq, axis)
+    with pytest.raises(ValueError, match="axis"):
+        r.rotary(h, pos, freq, axis.int())
+    with pytest.raises(mixrt.MixrtError, match="pairs"):
+        r.rotary(h, pos, torch.ones(3, device="cuda"), torch.zeros(3, device="cuda").byte())
+    with pytest.raises(mixrt.MixrtError, match="dtype"):
+        r.rotary((h, h.half()), pos, freq, axis)
+    with pytest.raises(mixrt.MixrtError, match="overlap"):
+        r.rotary(h, pos, freq, axis, out=torch.zeros(4, device="cuda").expand(5, 2, 4))
