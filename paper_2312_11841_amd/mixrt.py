@@ -449,14 +449,14 @@ class DeviceMesh:
 
 # --- arrays of the refiner's operators ---------------------------------------------
 
-_CODES = {}     # torch dtype -> mixrt_dtype, filled at the first use of torch
+_CODES = {}     # torch dtype -> mixrt_dtype, and the types of kept arrays; filled at first use
 
 
 def _elem_code(dtype, name: str) -> int:
     if not _CODES:
         import torch
         _CODES.update({torch.float32: MIXRT_F32, torch.float16: MIXRT_F16,
-                       torch.bfloat16: MIXRT_BF16})
+                       torch.bfloat16: MIXRT_BF16, "codes": torch.int8, "exps": torch.uint8})
     code = _CODES.get(dtype)
     if code is None:
         raise ValueError(f"{name}: dtype {dtype}, expected float32, float16 or bfloat16")
@@ -464,10 +464,11 @@ def _elem_code(dtype, name: str) -> int:
 
 
 def _on_gpu(t, name: str, device: int):
-    import torch
-    if not isinstance(t, torch.Tensor):
-        raise TypeError(f"{name}: expected a torch.Tensor, got {type(t).__name__}")
-    if t.get_device() != device:
+    try:
+        here = t.get_device() == device
+    except AttributeError:
+        raise TypeError(f"{name}: expected a torch.Tensor, got {type(t).__name__}") from None
+    if not here:
         raise ValueError(f"{name}: on {t.device}, expected cuda:{device}")
 
 
@@ -527,11 +528,47 @@ def _per_channel(t, name: str, channels: int, device: int) -> int:
     """Address of a float32 vector of one value per channel (None: 0)."""
     if t is None:
         return 0
-    import torch
-    _like(t, name, (channels,), torch.float32, device)
-    if channels > 1 and t.stride(0) != 1:
+    _on_gpu(t, name, device)
+    if t.dim() != 1 or t.shape[0] != channels or _elem_code(t.dtype, name) != MIXRT_F32:
+        raise ValueError(f"{name}: {t.dtype} {tuple(t.shape)}, expected float32 ({channels},)")
+    if not t.is_contiguous():
         raise ValueError(f"{name}: not contiguous")
     return t.data_ptr()
+
+
+class _Plan:
+    """What a call's descriptors hold besides addresses; see Renderer._plan."""
+
+
+def _rotary_plan(arrays, outs, pos, freq, axis, layout, inverse):
+    if not 1 <= len(arrays) <= 2:
+        raise ValueError(f"{len(arrays)} arrays of heads, expected 1 or 2")
+    if layout not in ROTARY_LAYOUTS:
+        raise ValueError(f"layout: {layout!r}, expected one of {tuple(ROTARY_LAYOUTS)}")
+    if pos.dim() < 1 or pos.shape[-1] < 1 or freq.dim() != 1 or axis.shape != freq.shape:
+        raise ValueError(f"pos {tuple(pos.shape)}, freq {tuple(freq.shape)}, axis "
+                         f"{tuple(axis.shape)}: expected [..., axes], [pairs], [pairs]")
+    axes = pos.shape[-1]
+    tokens = pos.numel() // axes
+    p = _Plan()
+    p.rotary = Rotary(tokens, axes, freq.shape[0], ROTARY_LAYOUTS[layout], int(bool(inverse)))
+    p.rotary_ref = C.byref(p.rotary)
+    p.heads = (Heads * len(arrays))()
+    for i, (x, o) in enumerate(zip(arrays, outs)):
+        name = f"heads[{i}]"
+        if x.dim() < 2:
+            raise ValueError(f"{name}: {x.dim()} dimensions, expected [..., heads, D]")
+        ends = []
+        for t in (x, o):
+            shape, stride = t.shape, t.stride()
+            if stride[-1] != 1 and shape[-1] > 1:
+                raise ValueError(f"{name}: elements of a head are not neighbours")
+            n, step = _run(shape[:-2], stride[:-2], name)
+            if n != tokens:
+                raise ValueError(f"{name}: {n} tokens, pos has {tokens}")
+            ends += [step, stride[-2]]
+        p.heads[i] = Heads(x.shape[-2], x.shape[-1], _elem_code(x.dtype, name), 0, 0, *ends)
+    return p
 
 
 @dataclass
@@ -546,17 +583,19 @@ class Checkpoint:
     dtype: object
 
     def descriptor(self, device: int) -> Kept:
-        import torch
-        _on_gpu(self.codes, "codes", device)
-        if self.codes.dim() != 2 or self.codes.dtype != torch.int8:
-            raise ValueError(f"codes: {self.codes.dtype} with {self.codes.dim()} dimensions, "
-                             "expected int8 [rows, channels]")
-        rows, channels = self.codes.shape
-        _like(self.exps, "exps", (rows, -(-channels // KEPT_GROUP)), torch.uint8, device)
-        if not (self.codes.is_contiguous() and self.exps.is_contiguous()):
-            raise ValueError("codes or exps: not contiguous")
-        return Kept(rows, channels, _elem_code(self.dtype, "checkpoint"),
-                    self.codes.data_ptr(), self.exps.data_ptr())
+        codes, exps = self.codes, self.exps
+        _on_gpu(codes, "codes", device)
+        _on_gpu(exps, "exps", device)
+        code = _elem_code(self.dtype, "checkpoint")
+        if codes.dim() != 2 or codes.dtype is not _CODES["codes"] or not codes.is_contiguous():
+            raise ValueError(f"codes: {codes.dtype} {tuple(codes.shape)}, expected contiguous "
+                             "int8 [rows, channels]")
+        rows, channels = codes.shape
+        want = (rows, -(-channels // KEPT_GROUP))
+        if exps.shape != want or exps.dtype is not _CODES["exps"] or not exps.is_contiguous():
+            raise ValueError(f"exps: {exps.dtype} {tuple(exps.shape)}, expected contiguous "
+                             f"uint8 {want}")
+        return Kept(rows, channels, code, codes.data_ptr(), exps.data_ptr())
 
 
 # --- the library handle ------------------------------------------------------------
@@ -591,6 +630,8 @@ class Renderer:
         if rc != MIXRT_OK:
             raise MixrtError(rc, self._L.mixrt_thread_error().decode())
         self._h = h
+        self._dev, self._raw_stream = torch.device("cuda", device), int(stream.cuda_stream)
+        self._ws = None     # the refiner's operators' scratch: (address, bytes)
 
     def _check(self, rc: int):
         if rc != MIXRT_OK:
@@ -738,54 +779,90 @@ class Renderer:
 
 
     # -- the refiner's operators
+    #
+    # What a call's descriptors hold besides addresses follows from the
+    # arrays' shapes, strides and types: it is checked and laid out once for
+    # each of them (a plan) and a call fills in its addresses.  Building the
+    # descriptors anew takes 10 us and more, the launch of a small call 5.
+    def _plan(self, key, make):
+        plans = self.__dict__.setdefault("_plans", {})
+        plan = plans.get(key)
+        if plan is None:
+            plan = make()
+            if len(plans) >= 256:
+                plans.clear()
+            plans[key] = plan
+        return plan
+
     def _empty(self, shape, dtype):
         """Device memory for an output.  Taken on this context's stream, so
         that memory released to another stream is not handed out early."""
         import torch
-        dev = torch.device("cuda", self.device)
-        if torch.cuda.current_stream(dev).cuda_stream == self.stream.cuda_stream:
-            return torch.empty(shape, dtype=dtype, device=dev)
+        if torch.cuda.current_stream(self.device).cuda_stream == self._raw_stream:
+            return torch.empty(shape, dtype=dtype, device=self._dev)
         with torch.cuda.stream(self.stream):
-            return torch.empty(shape, dtype=dtype, device=dev)
+            return torch.empty(shape, dtype=dtype, device=self._dev)
 
     def _workspace(self, size: int):
-        """This context's scratch, at least size bytes.  Its calls run one
-        after another on its stream, so they share it."""
-        import torch
-        ws = getattr(self, "_ws", None)
-        if ws is None or ws.numel() < size:
-            ws = self._ws = self._empty((max(size, 1 << 16),), torch.uint8)
-        return ws
+        """(address, bytes) of this context's scratch, at least size bytes.
+        Its calls run one after another on its stream, so they share it."""
+        if self._ws is None or self._ws[1] < size:
+            import torch
+            self._ws_memory = self._empty((max(size, 1 << 16),), torch.uint8)
+            self._ws = (self._ws_memory.data_ptr(), self._ws_memory.numel())
+        return self._ws
 
     def _checkpoint(self, rows: int, channels: int, dtype) -> Checkpoint:
         import torch
         return Checkpoint(self._empty((rows, channels), torch.int8),
                           self._empty((rows, -(-channels // KEPT_GROUP)), torch.uint8), dtype)
 
-    def _norm(self, x, groups, gamma, beta, eps, act, name):
-        """(descriptor, map of x, workspace) of a norm over x."""
-        _on_gpu(x, name, self.device)
-        images, pixels, channels, xmap = _as_map(x, name)
-        if act not in ACTS:
-            raise ValueError(f"act: {act!r}, expected one of {tuple(ACTS)}")
-        d = Norm(images, channels, pixels, int(groups), _elem_code(x.dtype, name), ACTS[act],
-                 float(eps), _per_channel(gamma, "gamma", channels, self.device),
-                 _per_channel(beta, "beta", channels, self.device))
+    def _size(self, fn, *args) -> int:
         size = C.c_size_t()
-        if self._L.mixrt_norm_workspace(C.byref(d), C.byref(size)) != MIXRT_OK:
-            raise MixrtError(MIXRT_EINVAL, self._L.mixrt_thread_error().decode())
-        return d, xmap, self._workspace(size.value)
+        rc = fn(*args, C.byref(size))
+        if rc != MIXRT_OK:
+            raise MixrtError(rc, self._L.mixrt_thread_error().decode())
+        return size.value
 
-    def _norm_forward(self, x, groups, gamma, beta, eps, act, out, stats, kept):
-        d, xmap, ws = self._norm(x, groups, gamma, beta, eps, act, "x")
+    def _norm(self, x, groups, eps, act, name):
+        """The plan of a norm over x, with x's address filled in."""
+        _on_gpu(x, name, self.device)
+
+        def make():
+            images, pixels, channels, xmap = _as_map(x, name)
+            if act not in ACTS:
+                raise ValueError(f"act: {act!r}, expected one of {tuple(ACTS)}")
+            p = _Plan()
+            p.norm = Norm(images, channels, pixels, int(groups), _elem_code(x.dtype, name),
+                          ACTS[act], float(eps), 0, 0)
+            p.bytes = self._size(self._L.mixrt_norm_workspace, C.byref(p.norm))
+            p.x, p.channels = xmap, channels
+            p.out = Map(0, pixels * channels, channels)     # a dense output
+            p.norm_ref, p.x_ref, p.out_ref = (C.byref(t) for t in (p.norm, p.x, p.out))
+            p.stats, p.rows = (images, int(groups), 2), images * pixels
+            return p
+
+        p = self._plan((name, x.shape, x.stride(), x.dtype, groups, eps, act), make)
+        p.x.data = x.data_ptr()
+        return p
+
+    def _norm_out(self, p, like, out, name):
+        """(the output, its map's reference)."""
         if out is None:
-            out = self._empty(x.shape, x.dtype)
-        else:
-            _like(out, "out", x.shape, x.dtype, self.device)
-        ymap = _as_map(out, "out")[3]
+            out = self._empty(like.shape, like.dtype)
+            p.out.data = out.data_ptr()
+            return out, p.out_ref
+        _like(out, name, like.shape, like.dtype, self.device)
+        return out, C.byref(_as_map(out, name)[3])
+
+    def _norm_forward(self, p, x, gamma, beta, out, stats, kept):
+        p.norm.gamma = _per_channel(gamma, "gamma", p.channels, self.device)
+        p.norm.beta = _per_channel(beta, "beta", p.channels, self.device)
+        out, out_ref = self._norm_out(p, x, out, "out")
         kd = None if kept is None else C.byref(kept.descriptor(self.device))
-        self._check(self._L.mixrt_norm_forward(self._h, C.byref(d), C.byref(xmap), C.byref(ymap),
-                                               _ptr(stats), kd, ws.data_ptr(), ws.numel()))
+        ws, size = self._workspace(p.bytes)
+        self._check(self._L.mixrt_norm_forward(self._h, p.norm_ref, p.x_ref, out_ref, stats, kd,
+                                               ws, size))
         return out
 
     def group_norm(self, x, groups: int, gamma=None, beta=None, *, eps: float = 1e-5,
@@ -794,7 +871,8 @@ class Renderer:
         float16 or bfloat16, channels last; a slice of a wider map will do).
         gamma, beta: float32 [channels] or None.  out: x's shape and type, or
         x itself."""
-        return self._norm_forward(x, groups, gamma, beta, eps, act, out, None, None)
+        p = self._norm(x, groups, eps, act, "x")
+        return self._norm_forward(p, x, gamma, beta, out, None, None)
 
     def group_norm_train(self, x, groups: int, gamma=None, beta=None, *, eps: float = 1e-5,
                          act: str = "none", out=None):
@@ -802,11 +880,10 @@ class Renderer:
         groups' (mean, 1 / deviation) as float32 [images, groups, 2], and x
         kept in 8 bits, which the same passes over x write."""
         import torch
-        _on_gpu(x, "x", self.device)
-        images, pixels, channels, _ = _as_map(x, "x")
-        stats = self._empty((images, int(groups), 2), torch.float32)
-        kept = self._checkpoint(images * pixels, channels, x.dtype)
-        return self._norm_forward(x, groups, gamma, beta, eps, act, out, stats, kept), stats, kept
+        p = self._norm(x, groups, eps, act, "x")
+        stats = self._empty(p.stats, torch.float32)
+        kept = self._checkpoint(p.rows, p.channels, x.dtype)
+        return (self._norm_forward(p, x, gamma, beta, out, stats.data_ptr(), kept), stats, kept)
 
     def group_norm_backward(self, dy, saved, stats, gamma=None, beta=None, *, act: str = "none",
                             out=None):
@@ -816,8 +893,8 @@ class Renderer:
         import torch
         if not isinstance(stats, torch.Tensor) or stats.dim() != 3:
             raise ValueError("stats: expected a torch.Tensor [images, groups, 2]")
-        d, dmap, ws = self._norm(dy, stats.shape[1], gamma, beta, 0.0, act, "dy")
-        _like(stats, "stats", (d.images, d.groups, 2), torch.float32, self.device)
+        p = self._norm(dy, stats.shape[1], 0.0, act, "dy")
+        _like(stats, "stats", p.stats, torch.float32, self.device)
         if not stats.is_contiguous():
             raise ValueError("stats: not contiguous")
         xd = kd = None
@@ -826,16 +903,16 @@ class Renderer:
         else:
             _like(saved, "saved", dy.shape, dy.dtype, self.device)
             xd = C.byref(_as_map(saved, "saved")[3])
-        if out is None:
-            out = self._empty(dy.shape, dy.dtype)
-        else:
-            _like(out, "out", dy.shape, dy.dtype, self.device)
-        grads = self._empty((2, d.channels), torch.float32)
-        dgamma, dbeta = grads[0], grads[1]
-        self._check(self._L.mixrt_norm_backward(
-            self._h, C.byref(d), C.byref(dmap), xd, kd, stats.data_ptr(),
-            C.byref(_as_map(out, "out")[3]), dgamma.data_ptr(), dbeta.data_ptr(), ws.data_ptr(),
-            ws.numel()))
+        p.norm.gamma = _per_channel(gamma, "gamma", p.channels, self.device)
+        p.norm.beta = _per_channel(beta, "beta", p.channels, self.device)
+        out, out_ref = self._norm_out(p, dy, out, "out")
+        grads = self._empty((2, p.channels), torch.float32)
+        at = grads.data_ptr()
+        ws, size = self._workspace(p.bytes)
+        self._check(self._L.mixrt_norm_backward(self._h, p.norm_ref, p.x_ref, xd, kd,
+                                                stats.data_ptr(), out_ref, at,
+                                                at + 4 * p.channels, ws, size))
+        dgamma, dbeta = grads.unbind(0)
         return out, dgamma, dbeta
 
     def checkpoint_pack(self, x) -> Checkpoint:
@@ -854,9 +931,10 @@ class Renderer:
         kd = kept.descriptor(self.device)
         if out is None:
             out = self._empty((kd.rows, kd.channels), kept.dtype if dtype is None else dtype)
+            stride = kd.channels
         else:
             _like(out, "out", (kd.rows, kd.channels), dtype or out.dtype, self.device)
-        stride = _as_rows(out, "out")[2]
+            stride = _as_rows(out, "out")[2]
         self._check(self._L.mixrt_kept_unpack(self._h, C.byref(kd), _elem_code(out.dtype, "out"),
                                               out.data_ptr(), stride))
         return out
@@ -873,14 +951,14 @@ class Renderer:
         rows, outs, stride = _as_rows(dy, "dy")
         if rows != kd.rows:
             raise ValueError(f"dy: {rows} rows, the checkpoint has {kd.rows}")
-        size = C.c_size_t()
-        if self._L.mixrt_linear_grad_workspace(C.byref(kd), outs, C.byref(size)) != MIXRT_OK:
-            raise MixrtError(MIXRT_EINVAL, self._L.mixrt_thread_error().decode())
-        ws = self._workspace(size.value)
+        ref = C.byref(kd)
+        need = self._plan(("linear", kd.rows, kd.channels, kd.dtype, outs),
+                          lambda: self._size(self._L.mixrt_linear_grad_workspace, ref, outs))
+        ws, size = self._workspace(need)
         dw = self._empty((kd.channels, outs), torch.float32)
         db = self._empty((outs,), torch.float32) if bias else None
-        self._check(self._L.mixrt_linear_grad(self._h, C.byref(kd), outs, dy.data_ptr(), stride,
-                                              dw.data_ptr(), _ptr(db), ws.data_ptr(), ws.numel()))
+        self._check(self._L.mixrt_linear_grad(self._h, ref, outs, dy.data_ptr(), stride,
+                                              dw.data_ptr(), _ptr(db), ws, size))
         return dw, db
 
     def rotary(self, heads, pos, freq, axis, *, layout: str = "halves", inverse: bool = False,
@@ -895,51 +973,32 @@ class Renderer:
         import torch
         single = isinstance(heads, torch.Tensor)
         arrays = (heads,) if single else tuple(heads)
-        outs = (None,) * len(arrays) if out is None else ((out,) if single else tuple(out))
-        if len(outs) != len(arrays) or not 1 <= len(arrays) <= 2:
-            raise ValueError(f"{len(arrays)} arrays and {len(outs)} outputs, expected 1 or 2")
-        if layout not in ROTARY_LAYOUTS:
-            raise ValueError(f"layout: {layout!r}, expected one of {tuple(ROTARY_LAYOUTS)}")
         for t, name, dt in ((pos, "pos", torch.float32), (freq, "freq", torch.float32),
                             (axis, "axis", torch.uint8)):
             _on_gpu(t, name, self.device)
             if t.dtype != dt or not t.is_contiguous():
                 raise ValueError(f"{name}: {t.dtype}, expected contiguous {dt}")
-        if pos.dim() < 1 or freq.dim() != 1 or axis.shape != freq.shape:
-            raise ValueError(f"pos {tuple(pos.shape)}, freq {tuple(freq.shape)}, axis "
-                             f"{tuple(axis.shape)}: expected [..., axes], [pairs], [pairs]")
-        axes, pairs = pos.shape[-1], freq.shape[0]
-        if axes < 1:
-            raise ValueError("pos: no axes")
-        tokens = pos.numel() // axes
-        d = Rotary(tokens, axes, pairs, ROTARY_LAYOUTS[layout], int(bool(inverse)),
-                   pos.data_ptr(), freq.data_ptr(), axis.data_ptr())
-        descs, got = (Heads * len(arrays))(), []
-        for i, (x, o) in enumerate(zip(arrays, outs)):
-            name = f"heads[{i}]"
-            _on_gpu(x, name, self.device)
-            if x.dim() < 2:
-                raise ValueError(f"{name}: {x.dim()} dimensions, expected [..., heads, D]")
-            if o is None:
-                o = self._empty(x.shape, x.dtype)
-            else:
+        for x in arrays:
+            _on_gpu(x, "heads", self.device)
+        if out is None:
+            outs = tuple(self._empty(x.shape, x.dtype) for x in arrays)
+            ends = None
+        else:
+            outs = (out,) if single else tuple(out)
+            if len(outs) != len(arrays):
+                raise ValueError(f"{len(arrays)} arrays and {len(outs)} outputs")
+            for i, (x, o) in enumerate(zip(arrays, outs)):
                 _like(o, f"out[{i}]", x.shape, x.dtype, self.device)
-            got.append(o)
-            code, ends = _elem_code(x.dtype, name), []
-            for t in (x, o):
-                shape, stride = t.shape, t.stride()
-                if stride[-1] != 1 and shape[-1] > 1:
-                    raise ValueError(f"{name}: elements of a head are not neighbours")
-                if len(shape) == 3:
-                    n, step = shape[0], stride[0]
-                else:
-                    n, step = _run(shape[:-2], stride[:-2], name)
-                if n != tokens:
-                    raise ValueError(f"{name}: {n} tokens, pos has {tokens}")
-                ends += [step, stride[-2]]
-            descs[i] = Heads(x.shape[-2], x.shape[-1], code, x.data_ptr(), o.data_ptr(), *ends)
-        self._check(self._L.mixrt_rotary_apply(self._h, C.byref(d), descs, len(arrays)))
-        return got[0] if single else tuple(got)
+            ends = tuple(o.stride() for o in outs)
+        key = ("rotary", pos.shape, freq.shape, axis.shape, layout, bool(inverse), ends,
+               *((x.shape, x.stride(), x.dtype) for x in arrays))
+        p = self._plan(key, lambda: _rotary_plan(arrays, outs, pos, freq, axis, layout, inverse))
+        p.rotary.pos, p.rotary.freq = pos.data_ptr(), freq.data_ptr()
+        p.rotary.axis = axis.data_ptr()
+        for d, x, o in zip(p.heads, arrays, outs):
+            d.x, d.out = x.data_ptr(), o.data_ptr()
+        self._check(self._L.mixrt_rotary_apply(self._h, p.rotary_ref, p.heads, len(arrays)))
+        return outs[0] if single else outs
 
 
 def validate(gbuf, cams, disp, grid, mlp, smp):
