@@ -104,7 +104,9 @@ typedef float f4 __attribute__((ext_vector_type(4)));
 typedef _Float16 h8 __attribute__((ext_vector_type(8)));
 typedef __bf16 b8 __attribute__((ext_vector_type(8)));
 typedef float f8 __attribute__((ext_vector_type(8)));
+typedef _Float16 h2 __attribute__((ext_vector_type(2)));
 
+// 8 rows of one channel: an MFMA operand of a lane.
 template <typename T> struct Frag;
 template <> struct Frag<f16> { typedef h8 type; };
 template <> struct Frag<bf16> { typedef b8 type; };
@@ -130,48 +132,222 @@ struct LinearK {
     const int8_t *codes;
     const uint8_t *exps;
     const void *dy;
-    int64_t rows, dy_stride, part;   // part: rows of one block
+    int64_t rows, dy_stride;
+    int64_t part;     // rows of one block
+    int64_t whole;    // rows whose vectors stay inside the arrays
     int C, outs, per_row;
+    int ty, parts;    // tiles of dw along its channels, parts of the rows
     float *sums;      // [parts][C * outs + outs]
 };
 
-// 4 channels of a row; what lies past the array's end is 0.
-template <bool WHOLE>
-__device__ __forceinline__ uint32_t load_codes(const int8_t *p, int left)
-{
-    if (WHOLE) return left > 0 ? *(const uint32_t *)p : 0u;
-    uint32_t v = 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-        if (i < left) v |= (uint32_t)(uint8_t)p[i] << (8 * i);
-    return v;
-}
+// A lane's share of a step as it is in memory: 4 channels (a word) and 4 outs
+// (kWords words) of 8 rows.
+template <typename T>
+struct LinearStep {
+    static constexpr int kWords = sizeof(T);
+    uint32_t code[8], byte[8], dy[8][kWords];
+};
 
-template <typename T, bool WHOLE>
-__device__ __forceinline__ Pack<T, 4> load_dy(const T *p, int left)
+template <int N>
+struct __attribute__((packed, aligned(1))) Words {   // loads may start at any byte
+    uint32_t v[N];
+};
+
+// Where a lane's channels and outs lie in its quarter's rows.  Lanes past the
+// channels or the outs take the row's start: what they compute is not stored.
+struct LinearOffsets {
+    uint32_t code, byte, dy;
+};
+
+// row (the step's first) is the same for the wave, so the addresses are scalar
+// ones with a 32-bit offset of the lane's own, in bytes.
+template <typename T>
+__device__ __forceinline__ void load_step(LinearStep<T> &s, int64_t row, const LinearOffsets &o,
+                                          const LinearK &k)
 {
-    Pack<T, 4> v;
-    if (WHOLE) {
-        if (left > 0) return *(const Pack<T, 4> *)p;
+    constexpr int W = LinearStep<T>::kWords;
+    const int8_t *codes = k.codes + row * k.C;
+    const uint8_t *exps = k.exps + row * k.per_row;
+    const char *dy = (const char *)k.dy + row * k.dy_stride * sizeof(T);
+    // the offsets are made new to the compiler here, so that it sees 32-bit
+    // ones beside the loads and uses the scalar address form (else it keeps
+    // them as 64 bits and adds each address in vector registers)
+    uint32_t oc = o.code, ob = o.byte, od = o.dy;
+    asm("" : "+v"(oc), "+v"(ob), "+v"(od));
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v.v[i] = (T)0.0f;
-        return v;
+    for (int i = 0; i < 8; ++i) {
+        s.code[i] = ((const Words<1> *)(codes + oc))->v[0];
+        s.byte[i] = exps[ob];
+        const Words<W> d = *(const Words<W> *)(dy + od);
+#pragma unroll
+        for (int w = 0; w < W; ++w) s.dy[i][w] = d.v[w];
+        codes += k.C;
+        exps += k.per_row;
+        dy += k.dy_stride * sizeof(T);
     }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v.v[i] = i < left ? p[i] : (T)0.0f;
-    return v;
 }
 
-// WC, WO: the channels and outs are multiples of 4.
-template <typename T, bool WC, bool WO>
-__global__ __launch_bounds__(kThreads) void linear_grad_kernel(LinearK k)
+// The same near the arrays' end.  row: the lane's first.  Rows from r1 on
+// read the last row and count as 0 (2^e of byte 0 is 0); a vector that would
+// pass the end of its array starts earlier and is shifted down.
+template <typename T>
+__device__ __forceinline__ void load_last(LinearStep<T> &s, int64_t row, int64_t r1, int ci,
+                                          int co, const LinearK &k)
+{
+    constexpr int W = LinearStep<T>::kWords;
+    const int64_t n_code = k.rows * k.C, n_dy = (k.rows - 1) * k.dy_stride + k.outs;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const bool in = row + i < r1;
+        const int64_t r = in ? row + i : r1 - 1;
+        const int64_t ac = r * k.C + ci, ad = r * k.dy_stride + co;
+        const int over_c = (int)max(ac + 4 - n_code, (int64_t)0);
+        const int over_d = (int)max(ad + 4 - n_dy, (int64_t)0);
+        s.code[i] = ((const Words<1> *)(k.codes + ac - over_c))->v[0] >> (8 * over_c);
+        const uint32_t byte = k.exps[r * k.per_row + ci / kKeptGroup];
+        s.byte[i] = in ? byte : 0u;
+        const Words<W> d = *(const Words<W> *)((const T *)k.dy + ad - over_d);
+        uint32_t v[W];
+#pragma unroll
+        for (int w = 0; w < W; ++w) v[w] = d.v[w];
+        if (W == 2) {
+            const uint64_t both = (((uint64_t)v[W - 1] << 32) | v[0]) >> (16 * over_d);
+            v[0] = (uint32_t)both;
+            v[W - 1] = (uint32_t)(both >> 32);
+        } else {
+#pragma unroll
+            for (int t = 0; t < 3; ++t)
+                if (over_d > t)
+#pragma unroll
+                    for (int w = 0; w + 1 < W; ++w) v[w] = v[w + 1];
+        }
+#pragma unroll
+        for (int w = 0; w < W; ++w) s.dy[i][w] = in ? v[w] : 0u;
+    }
+}
+
+// The scales of 8 rows, as the conversion below takes them.
+template <typename T> struct Scales {
+    float v[8];
+    __device__ __forceinline__ explicit Scales(const uint32_t (&byte)[8])
+    {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = kept_scale(byte[i]);
+    }
+};
+template <> struct Scales<f16> {
+    h2 v[4];
+    __device__ __forceinline__ explicit Scales(const uint32_t (&byte)[8])
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            v[i] = (h2){(f16)kept_scale(byte[2 * i]), (f16)kept_scale(byte[2 * i + 1])};
+    }
+};
+
+// Element m of 8 rows' codes as an operand.  u: the codes plus 128, as bytes.
+// In 32 bits: u 2^e - 128 2^e, without rounding; its upper half is the bf16.
+__device__ __forceinline__ f8 code_frag(const uint32_t (&u)[8], const Scales<float> &s, int m)
+{
+    f8 a;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        a[i] = fmaf((float)((u[i] >> (8 * m)) & 255u), s.v[i], -128.0f * s.v[i]);
+    return a;
+}
+__device__ __forceinline__ b8 code_frag(const uint32_t (&u)[8], const Scales<bf16> &s, int m)
+{
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float lo = fmaf((float)((u[2 * i] >> (8 * m)) & 255u), s.v[2 * i],
+                              -128.0f * s.v[2 * i]);
+        const float hi = fmaf((float)((u[2 * i + 1] >> (8 * m)) & 255u), s.v[2 * i + 1],
+                              -128.0f * s.v[2 * i + 1]);
+        w[i] = __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u);
+    }
+    return __builtin_bit_cast(b8, w);
+}
+// In f16, two rows at once: the byte u below 0x64 is 1024 + u; less 1152 it is
+// the code, and its product with 2^e is exact.
+__device__ __forceinline__ h8 code_frag(const uint32_t (&u)[8], const Scales<f16> &s, int m)
+{
+    h2 w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t pair = __builtin_amdgcn_perm(u[2 * i + 1], u[2 * i],
+                                                    0x0c040c00u + 0x00010001u * m) |
+                              0x64006400u;
+        w[i] = (__builtin_bit_cast(h2, pair) - (f16)1152.0f) * s.v[i];
+    }
+    return __builtin_bit_cast(h8, w);
+}
+
+// Element n of 8 rows of dy as an operand.
+template <typename T>
+__device__ __forceinline__ typename Frag<T>::type dy_frag(const LinearStep<T> &s, int n)
 {
     typedef typename Frag<T>::type F;
+    if constexpr (sizeof(T) == 4) {
+        F b;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) b[i] = __uint_as_float(s.dy[i][n]);
+        return b;
+    } else {
+        const uint32_t sel = n & 1 ? 0x07060302u : 0x05040100u;
+        uint4 w;
+        w.x = __builtin_amdgcn_perm(s.dy[1][n >> 1], s.dy[0][n >> 1], sel);
+        w.y = __builtin_amdgcn_perm(s.dy[3][n >> 1], s.dy[2][n >> 1], sel);
+        w.z = __builtin_amdgcn_perm(s.dy[5][n >> 1], s.dy[4][n >> 1], sel);
+        w.w = __builtin_amdgcn_perm(s.dy[7][n >> 1], s.dy[6][n >> 1], sel);
+        return __builtin_bit_cast(F, w);
+    }
+}
+
+template <typename T>
+__device__ __forceinline__ void multiply_step(const LinearStep<T> &s, bool biased, f4 (&acc)[4][4],
+                                              f4 (&bias)[4])
+{
+    typedef typename Frag<T>::type F;
+    const Scales<T> sc(s.byte);
+    uint32_t u[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) u[i] = s.code[i] ^ 0x80808080u;
+    F b[4];
+#pragma unroll
+    for (int n = 0; n < 4; ++n) b[n] = dy_frag(s, n);
+#pragma unroll
+    for (int m = 0; m < 4; ++m) {
+        const F a = code_frag(u, sc, m);
+#pragma unroll
+        for (int n = 0; n < 4; ++n) acc[m][n] = mac(a, b[n], acc[m][n]);
+    }
+    if (biased) {
+        F ones;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) ones[i] = (T)1.0f;
+#pragma unroll
+        for (int n = 0; n < 4; ++n) bias[n] = mac(ones, b[n], bias[n]);
+    }
+}
+
+template <typename T>
+__global__ __launch_bounds__(kThreads) void linear_grad_kernel(LinearK k)
+{
     __shared__ float sh[kTile * kTile + kTile];
-    const int wave = threadIdx.x / 64, lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x & 63;
     const int q = lane >> 4, c = lane & 15;
-    const int ci = blockIdx.y * kTile + 4 * c, co = blockIdx.z * kTile + 4 * c;
-    const int lc = k.C - ci, lo = k.outs - co;   // channels left from here
+    // Blocks are dealt to the 8 XCDs in turn; a run of them along the channels
+    // reads the same rows of dy, so each XCD takes one such run after another
+    // and finds dy (and, across its few tiles of dy, the codes) in its L2.
+    const int nb = gridDim.x, x = blockIdx.x & 7;
+    int at = x * (nb >> 3) + min(x, nb & 7) + (blockIdx.x >> 3);
+    const int ty = at % k.ty;
+    at /= k.ty;
+    const int part = at % k.parts, tz = at / k.parts;
+    int ci = ty * kTile + 4 * c, co = tz * kTile + 4 * c;
+    if (ci >= k.C) ci = 0;
+    if (co >= k.outs) co = 0;
     f4 acc[4][4], bias[4];
 #pragma unroll
     for (int m = 0; m < 4; ++m) {
@@ -179,40 +355,52 @@ __global__ __launch_bounds__(kThreads) void linear_grad_kernel(LinearK k)
 #pragma unroll
         for (int n = 0; n < 4; ++n) acc[m][n] = (f4)0.0f;
     }
-    F ones;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) ones[i] = (T)1.0f;
-    const int64_t r1 = min(((int64_t)blockIdx.x + 1) * k.part, k.rows);
-    for (int64_t r0 = (int64_t)blockIdx.x * k.part + wave * kRows; r0 < r1; r0 += 4 * kRows) {
-        uint32_t code[8], byte[8];
-        Pack<T, 4> dy[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int64_t row = r0 + 8 * q + i;
-            const bool in = row < r1;
-            code[i] = in ? load_codes<WC>(k.codes + row * k.C + ci, lc) : 0u;
-            byte[i] = in && lc > 0 ? k.exps[row * k.per_row + ci / kKeptGroup] : 0u;
-            dy[i] = load_dy<T, WO>((const T *)k.dy + row * k.dy_stride + co, in ? lo : 0);
-        }
-        F a[4], b[4];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            // code * 2^e from the code plus 128: u s - 128 s is exact
-            const float s = kept_scale(byte[i]), off = -128.0f * s;
-            const uint32_t u = code[i] ^ 0x80808080u;
-#pragma unroll
-            for (int m = 0; m < 4; ++m) {
-                a[m][i] = (T)fmaf((float)((u >> (8 * m)) & 255u), s, off);
-                b[m][i] = dy[i].v[m];
+    const bool biased = ty == 0;
+    const int64_t first = part * k.part, r1 = min(first + k.part, k.rows);
+    const int64_t whole = min(r1, k.whole);
+    int64_t r0 = first + wave * kRows;
+    const int n = r0 + kRows <= whole ? (int)((whole - r0 - kRows) / (4 * kRows)) + 1 : 0;
+    const LinearOffsets off{(uint32_t)(8 * q * k.C + ci),
+                            (uint32_t)(8 * q * k.per_row + ci / kKeptGroup),
+                            (uint32_t)(8 * q * (uint32_t)k.dy_stride + co) * (uint32_t)sizeof(T)};
+    if (n > 0) {
+        // Two steps are on their way while one is multiplied.  The loads past
+        // the last step repeat it: a condition around them would end the
+        // overlap, since waits are counted.
+        const auto load = [&](LinearStep<T> &s, int i) {
+            load_step(s, r0 + (int64_t)min(i, n - 1) * (4 * kRows), off, k);
+        };
+        LinearStep<T> s0, s1;
+        load(s0, 0);
+        if constexpr (sizeof(T) == 4) {   // one step: the registers hold no more
+            for (int i = 0;; i += 2) {
+                load(s1, i + 1);
+                multiply_step(s0, biased, acc, bias);
+                if (i + 1 >= n) break;
+                load(s0, i + 2);
+                multiply_step(s1, biased, acc, bias);
+                if (i + 2 >= n) break;
             }
+        } else {
+        LinearStep<T> s2;
+        load(s1, 1);
+        for (int i = 0;; i += 3) {
+            load(s2, i + 2);
+            multiply_step(s0, biased, acc, bias);
+            if (i + 1 >= n) break;
+            load(s0, i + 3);
+            multiply_step(s1, biased, acc, bias);
+            if (i + 2 >= n) break;
+            load(s1, i + 4);
+            multiply_step(s2, biased, acc, bias);
+            if (i + 3 >= n) break;
         }
-#pragma unroll
-        for (int m = 0; m < 4; ++m)
-#pragma unroll
-            for (int n = 0; n < 4; ++n) acc[m][n] = mac(a[m], b[n], acc[m][n]);
-        if (blockIdx.y == 0)
-#pragma unroll
-            for (int n = 0; n < 4; ++n) bias[n] = mac(ones, b[n], bias[n]);
+        }
+    }
+    for (r0 += (int64_t)n * (4 * kRows); r0 < r1; r0 += 4 * kRows) {
+        LinearStep<T> s;
+        load_last(s, r0 + 8 * q, r1, ci, co, k);
+        multiply_step(s, biased, acc, bias);
     }
     // the waves add in turn: a tile's row m (channel 4 m + i) is in quarter
     // m / 4, register m % 4, its column n (out 4 n + j) in lane n
@@ -236,48 +424,108 @@ __global__ __launch_bounds__(kThreads) void linear_grad_kernel(LinearK k)
         }
         __syncthreads();
     }
-    float *out = k.sums + (int64_t)blockIdx.x * ((int64_t)k.C * k.outs + k.outs);
-    const int o = threadIdx.x & 63, og = blockIdx.z * kTile + o;
+    float *out = k.sums + (int64_t)part * ((int64_t)k.C * k.outs + k.outs);
+    const int o = threadIdx.x & 63, og = tz * kTile + o;
     if (og < k.outs) {
         for (int i = threadIdx.x >> 6; i < kTile; i += 4) {
-            const int cg = blockIdx.y * kTile + i;
+            const int cg = ty * kTile + i;
             if (cg < k.C) out[(int64_t)cg * k.outs + og] = sh[i * kTile + o];
         }
-        if (blockIdx.y == 0 && threadIdx.x < 64)
+        if (biased && threadIdx.x < 64)
             out[(int64_t)k.C * k.outs + og] = sh[kTile * kTile + o];
     }
 }
 
-// Adds the parts, in order.  n: values of one part; the last outs are db.
-__global__ __launch_bounds__(kThreads) void linear_join_kernel(const float *sums, int64_t n,
-                                                               int64_t weights, int parts,
-                                                               float *dw, float *db)
+// Arrays shorter than a vector: a thread's sum for each weight.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void linear_tiny_kernel(LinearK k, float *dw, float *db)
 {
     const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-    if (i >= n) return;
-    double v = 0.0;
-    for (int p = 0; p < parts; ++p) v += (double)sums[(int64_t)p * n + i];
-    if (i < weights)
-        dw[i] = (float)v;
+    const int64_t c = i / k.outs;
+    if (c > k.C) return;
+    const int o = (int)(i - c * k.outs);
+    float v = 0.0f;
+    for (int64_t r = 0; r < k.rows; ++r) {
+        const float d = (float)((const T *)k.dy)[r * k.dy_stride + o];
+        const float x = c < k.C ? (float)k.codes[r * k.C + c] *
+                                      kept_scale(k.exps[r * k.per_row + c / kKeptGroup])
+                                : 1.0f;
+        v = fmaf(x, d, v);
+    }
+    if (c < k.C)
+        dw[i] = v;
     else if (db)
-        db[i - weights] = (float)v;
+        db[o] = v;
 }
+
+// Adds the parts.  n: values of one part; the last outs are db.  ACROSS
+// threads take every ACROSSth part of a value each, then their sums are added
+// in order.
+template <int ACROSS, int THREADS>
+__global__ __launch_bounds__(THREADS) void linear_join_kernel(const float *sums, int64_t n,
+                                                              int64_t weights, int parts,
+                                                              float *dw, float *db)
+{
+    constexpr int kValues = THREADS / ACROSS;
+    __shared__ float sh[ACROSS][kValues + 1];
+    const int o = threadIdx.x % kValues, a = threadIdx.x / kValues;
+    const int64_t i = (int64_t)blockIdx.x * kValues + o;
+    float v = 0.0f;
+    if (i < n)
+#pragma unroll 8
+        for (int p = a; p < parts; p += ACROSS) v += sums[(int64_t)p * n + i];
+    if (ACROSS > 1) {
+        sh[a][o] = v;
+        for (int half = ACROSS / 2; half > 0; half /= 2) {
+            __syncthreads();
+            if (a < half) sh[a][o] += sh[a + half][o];
+        }
+        v = sh[0][o];
+    }
+    if (a == 0 && i < n) {
+        if (i < weights)
+            dw[i] = v;
+        else if (db)
+            db[i - weights] = v;
+    }
+}
+
+constexpr int kResident = 512;   // blocks of linear_grad_kernel on the card at once
 
 struct LinearPlan {
     int parts, ty, tz;
     int64_t part;
 };
 
+// How many parts the rows are split into: enough to fill the card, in whole
+// rounds of the blocks it holds at once (2 a CU by their registers), and not
+// so many that adding their sums costs more.  In units of a step of a full
+// card, about 1 us: a block takes its steps and about 3 for its start and end;
+// writing and reading a part of n sums takes n / 500,000.  (3600 rows, 512 x
+// 1536, f16: see below.)
 LinearPlan linear_plan(int64_t rows, int C, int outs)
 {
     LinearPlan p;
     p.ty = (C + kTile - 1) / kTile;
     p.tz = (outs + kTile - 1) / kTile;
-    const int64_t most = (rows + 4 * kRows - 1) / (4 * kRows);   // a step for every wave
-    int64_t parts = 768 / ((int64_t)p.ty * p.tz);
-    if (parts > most) parts = most;
-    if (parts < 1) parts = 1;
-    p.part = ((rows + parts - 1) / parts + kRows - 1) / kRows * kRows;
+    const int tiles = p.ty * p.tz;
+    const int64_t steps = (rows + 4 * kRows - 1) / (4 * kRows);
+    const double sums = ((double)C * outs + outs) / 500000.0;
+    int64_t best = 1;
+    double least = 0.0;
+    for (int rounds = 1; rounds <= 8; ++rounds) {
+        int64_t parts = (int64_t)rounds * kResident / tiles;
+        if (parts > steps) parts = steps;
+        if (parts < 1) parts = 1;
+        const int64_t each = (steps + parts - 1) / parts;
+        const int64_t need = (parts * tiles + kResident - 1) / kResident;
+        const double cost = (double)need * (double)(each + 3) + sums * (double)parts;
+        if (rounds == 1 || cost < least) {
+            least = cost;
+            best = parts;
+        }
+    }
+    p.part = ((rows + best - 1) / best + kRows - 1) / kRows * kRows;
     if (p.part < 1) p.part = kRows;
     p.parts = rows > 0 ? (int)((rows + p.part - 1) / p.part) : 1;
     return p;
@@ -355,20 +603,35 @@ hipError_t launch_linear_grad(int dtype, int64_t rows, int C, int outs, const in
                               float *db, void *ws, hipStream_t stream)
 {
     const LinearPlan p = linear_plan(rows, C, outs);
-    LinearK k{codes, exps, dy, rows, dy_stride, p.part, C, outs, kept_groups(C), (float *)ws};
-    const dim3 grid(p.parts, p.ty, p.tz);
-    // whole 4-byte loads of codes need rows that start at a multiple of 4
-    const bool wc = C % 4 == 0 && ((uintptr_t)codes & 3u) == 0, wo = outs % 4 == 0;
+    // A vector of 4 that is not whole in its row goes on into the next rows: at
+    // most 3 of them (rows of one element), and none where rows of dy repeat.
+    int64_t whole = rows;
+    if (C % 4 || outs % 4) whole = rows - 3;
+    if (outs % 4 && dy_stride < outs) whole = 0;
+    if (dy_stride >= (1 << 24)) whole = 0;   // the lanes' offsets are 32 bits
+    LinearK k{codes,          exps, dy,   rows,    dy_stride,  p.part, whole, C, outs,
+              kept_groups(C), p.ty, p.parts, (float *)ws};
+    const int grid = p.parts * p.ty * p.tz;
+    const int64_t weights = (int64_t)C * outs, n = weights + outs;
+    const bool tiny = rows * C < 4 || (rows - 1) * dy_stride + outs < 4;
     with_type(dtype, [&](auto *t) {
         typedef std::remove_pointer_t<decltype(t)> T;
-        if (wc && wo) linear_grad_kernel<T, true, true><<<grid, kThreads, 0, stream>>>(k);
-        else if (wc) linear_grad_kernel<T, true, false><<<grid, kThreads, 0, stream>>>(k);
-        else if (wo) linear_grad_kernel<T, false, true><<<grid, kThreads, 0, stream>>>(k);
-        else linear_grad_kernel<T, false, false><<<grid, kThreads, 0, stream>>>(k);
+        if (tiny)
+            linear_tiny_kernel<T><<<blocks(n, kThreads), kThreads, 0, stream>>>(k, dw, db);
+        else
+            linear_grad_kernel<T><<<grid, kThreads, 0, stream>>>(k);
     });
-    const int64_t weights = (int64_t)C * outs, n = weights + outs;
-    linear_join_kernel<<<blocks(n, kThreads), kThreads, 0, stream>>>(k.sums, n, weights, p.parts,
-                                                                     dw, db);
+    // many parts of few weights: 32 threads a value (4160 values of 506 parts
+    // 4.7 us, against 120 with one); few parts: one (788,000 values of 2 parts
+    // 53 us with 32)
+    if (tiny)
+        ;
+    else if (p.parts > 8)
+        linear_join_kernel<32, 1024><<<blocks(n, 32), 1024, 0, stream>>>(k.sums, n, weights,
+                                                                         p.parts, dw, db);
+    else
+        linear_join_kernel<1, 256><<<blocks(n, 256), 256, 0, stream>>>(k.sums, n, weights, p.parts,
+                                                                       dw, db);
     return hipGetLastError();
 }
 
