@@ -21,8 +21,8 @@ INCLUDE = os.path.join(ROOT, "include")
 OBJ_DIR = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libmixrt.so")
 COMMON_SOURCES = ["mixrt_api.cpp", "mixrt_mesh.cpp", "mixrt_stages.hip", "mixrt_raycast.hip",
-                  "mixrt_raster.hip", "mixrt_refine_api.cpp", "mixrt_norm.hip", "mixrt_kept.hip",
-                  "mixrt_rotary.hip"]
+                  "mixrt_raster.hip", "mixrt_refine_api.cpp", "mixrt_norm.hip",
+                  "mixrt_norm_back.hip", "mixrt_kept.hip", "mixrt_rotary.hip"]
 RENDER_SOURCE = "mixrt_render.hip"
 SOURCES = COMMON_SOURCES + [RENDER_SOURCE]
 MB_LIB = os.path.join(PKG, "libmixrt_microbench.so")

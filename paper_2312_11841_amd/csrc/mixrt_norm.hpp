@@ -1,0 +1,306 @@
+// Group norm with an activation on channels-last feature maps: what the forward
+// (mixrt_norm.hip) and the backward (mixrt_norm_back.hip) share.
+//
+// A row is a pixel's C channels.  Threads take vectors of V channels; a block's
+// threads lie over `lanes` vectors of a row and over R rows, so that a thread
+// keeps its channels (and their constants) while it walks down the image.
+//
+// Large images: sums over parts of the image, their join, then the normalised
+// rows: three launches that read x twice.  Where an image has few parts, the
+// blocks of the last launch join them themselves (two launches).  Small images,
+// forward: one launch, whose blocks each sum up all rows of a few groups and
+// then write a share of them.  A launch takes about 4 us beside its work.
+// Joins add in a fixed order: the same inputs give the same bits.
+#pragma once
+
+#include "mixrt_refine.hpp"
+
+#include <type_traits>
+
+namespace mixrt {
+
+inline constexpr int kThreads = 256;
+inline constexpr int kSmallThreads = 1024;
+inline constexpr int kJoinThreads = 1024;
+// Rows a thread loads before it uses the first.  Backward: two, or the
+// registers leave too few waves.
+inline constexpr int kAhead = 4, kBackAhead = 2;
+inline constexpr int kFoldChannels = 512;   // most channels (and groups) of a join by the blocks
+
+struct NormK {
+    int N, C, G, Cg;
+    int64_t P;
+    int lanes, R;
+    int S;              // parts of an image (of the sums that are joined)
+    int slabs;
+    float eps;
+    const float *gamma, *beta;
+    MapK x, y, dy, dx;
+    float *stats;       // never null here: the caller's or the workspace's
+    int8_t *codes;
+    uint8_t *exps;
+    float *dgamma, *dbeta;
+    void *sums;         // forward: double2 [N][S * slabs][G]; backward: float2 [N][S][C]
+    float *means;       // backward: [N][G][2]: the group means of gamma dz and gamma dz xh
+    float2 *channels;   // backward: [N][C]: each image's sums of dz and dz xh
+};
+
+// exp(x) as 2^(x log2 e), to a few units in the last place.
+__device__ __forceinline__ float fast_exp(float x)
+{
+    return __builtin_amdgcn_exp2f(x * 1.4426950408889634f);
+}
+
+// erf(z / sqrt 2) with e = exp(-z^2 / 2): Abramowitz and Stegun 7.1.26, to
+// 1.5e-7, whose factor exp(-x^2) is the normal density that gelu's slope needs
+// as well.
+__device__ __forceinline__ float erf_sqrt2(float z, float e)
+{
+    const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f * 0.70710678f, fabsf(z), 1.0f));
+    float p = fmaf(1.061405429f, t, -1.453152027f);
+    p = fmaf(p, t, 1.421413741f);
+    p = fmaf(p, t, -0.284496736f);
+    p = fmaf(p, t, 0.254829592f);
+    return copysignf(fmaf(-p * t, e, 1.0f), z);
+}
+
+template <int ACT>
+__device__ __forceinline__ float act(float z)
+{
+    if (ACT == kActRelu) return z > 0.0f ? z : (z <= 0.0f ? 0.0f : z);   // keeps a NaN
+    if (ACT == kActSilu) return z * __builtin_amdgcn_rcpf(1.0f + fast_exp(-z));
+    if (ACT == kActGelu) {
+        const float h = 0.5f * z;
+        return fmaf(h, erf_sqrt2(z, fast_exp(-h * z)), h);
+    }
+    return z;
+}
+
+template <int ACT>
+__device__ __forceinline__ float act_slope(float z)
+{
+    if (ACT == kActRelu) return z > 0.0f ? 1.0f : (z <= 0.0f ? 0.0f : z);
+    if (ACT == kActSilu) {
+        const float s = __builtin_amdgcn_rcpf(1.0f + fast_exp(-z));
+        return fmaf(fmaf(-z, s, z), s, s);   // s (1 + z (1 - s)); z (1 - s) stays finite
+    }
+    if (ACT == kActGelu) {
+        const float e = fast_exp(-0.5f * z * z);
+        return fmaf(z * e, 0.39894228040143268f, fmaf(0.5f, erf_sqrt2(z, e), 0.5f));
+    }
+    return 1.0f;
+}
+
+// A thread's constants, those of its V channels in one image, around
+// t = x - mean: z = t scale + beta with scale = rstd gamma.
+template <int V>
+struct Channels {
+    float mean[V], scale[V], be[V], rstd[V];
+    // stats: (mean, rstd) of the image's groups; c0: the first channel
+    __device__ __forceinline__ void set(const NormK &k, const float *stats, int c0)
+    {
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const float *st = stats + 2 * ((c0 + i) / k.Cg);
+            const float ga = k.gamma ? k.gamma[c0 + i] : 1.0f;
+            be[i] = k.beta ? k.beta[c0 + i] : 0.0f;
+            mean[i] = st[0];
+            rstd[i] = st[1];
+            scale[i] = rstd[i] * ga;
+        }
+    }
+};
+
+// Walks a block's rows: runs of U * R rows, every `parts`th of them from run
+// `at`, so that the blocks' runs of one time are neighbours in memory.  load(p)
+// of a thread's U rows first, then use(p, what it gave).
+template <typename D, int U, typename LOAD, typename USE>
+__device__ __forceinline__ void walk(int64_t at, int64_t parts, int r, int R, int64_t P, LOAD load,
+                                     USE use)
+{
+    const int64_t run = (int64_t)U * R;
+    int64_t p = at * run + r;
+    for (; p + (int64_t)(U - 1) * R < P; p += parts * run) {
+        D d[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) d[u] = load(p + (int64_t)u * R);
+#pragma unroll
+        for (int u = 0; u < U; ++u) use(p + (int64_t)u * R, d[u]);
+    }
+    // the image's last run, where it is not whole: this block's if any
+    if (U > 1)
+        for (int u = 0; u < U && p < P; ++u, p += R) use(p, load(p));
+}
+
+// Adds the R rows' values of every lane; thread (0, j) ends with the sum.
+// v: shared [K][kThreads].
+template <int K, typename A>
+__device__ __forceinline__ void join_rows(A (*v)[kThreads], int lanes, int R, int j, int r)
+{
+    for (int n = R; n > 1;) {
+        const int half = (n + 1) / 2;
+        __syncthreads();
+        if (r < n - half)
+#pragma unroll
+            for (int k = 0; k < K; ++k) v[k][r * lanes + j] += v[k][(r + half) * lanes + j];
+        n = half;
+    }
+    __syncthreads();
+}
+
+__device__ __forceinline__ double wave_sum(double v)
+{
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) v += __shfl_xor(v, d);
+    return v;
+}
+
+// (mean, rstd) from a group's sums of x and x^2 over m elements.
+__device__ __forceinline__ float2 group_stats(const NormK &k, double s, double q)
+{
+    const double m = (double)k.P * k.Cg, mean = k.P > 0 ? s / m : 0.0;
+    double var = k.P > 0 ? q / m - mean * mean : 0.0;
+    if (var < 0.0) var = 0.0;   // a NaN stays
+    return make_float2((float)mean, (float)(1.0 / sqrt(var + (double)k.eps)));
+}
+
+// --- plans ------------------------------------------------------------------------
+
+struct NormPlan {
+    enum Way { kSmall, kFold, kLarge } way;
+    int chunk;      // small: channels of a block
+    int V;          // channels of a vector
+    int lanes;      // vectors of a row in one slab or chunk (threads across a row)
+    int slabs;      // slabs of a row
+    int R;          // rows of one step of a block
+    int S;          // parts an image is split into for the sums
+    int share;      // blocks that share an image's rows when they are written
+};
+
+inline int64_t gcd(int64_t a, int64_t b) { return b ? gcd(b, a % b) : a; }
+
+inline constexpr int64_t kSmallBytes = 192 << 10;
+inline constexpr int64_t kSmallRow = 32;   // least bytes of a row that a block reads
+
+// pad: x is kept in the same pass; a row takes whole kept groups of lanes, so
+// that the lanes of a group are aligned neighbours.
+inline NormPlan norm_plan(int N, int64_t P, int C, int G, int dtype, bool pad, bool back)
+{
+    NormPlan p{};
+    const int size = dtype == kF32 ? 4 : 2, Cg = C / G;
+    const auto atmost = [](int64_t v, int64_t hi) { return v > hi ? hi : v < 1 ? 1 : v; };
+    if (!back) {
+        p.V = 16 / size;
+        while (Cg % p.V) p.V >>= 1;
+        int64_t chunk = pad ? (int64_t)Cg / gcd(Cg, kKeptGroup) * kKeptGroup : Cg;
+        while (chunk * size < kSmallRow && chunk < C) chunk += Cg;
+        if (chunk > C) chunk = C;
+        const int64_t vecs = pad ? (chunk + kKeptGroup - 1) / kKeptGroup * (kKeptGroup / p.V)
+                                 : chunk / p.V;
+        if (vecs <= kSmallThreads && P * chunk * size <= kSmallBytes) {
+            p.way = NormPlan::kSmall;
+            p.chunk = (int)chunk;
+            p.lanes = (int)vecs;
+            p.slabs = 1;
+            p.R = kSmallThreads / p.lanes;
+            p.S = 1;
+            const int64_t blocks = (int64_t)N * ((C + chunk - 1) / chunk);
+            p.share = (int)atmost(512 / (blocks > 0 ? blocks : 1), (P + p.R - 1) / p.R);
+            return p;
+        }
+    }
+    p.V = 16 / size;
+    while (C % p.V) p.V >>= 1;
+    const int wide = pad ? kept_groups(C) * (kKeptGroup / p.V) : C / p.V;
+    p.lanes = wide < kThreads ? wide : kThreads;
+    p.slabs = (wide + p.lanes - 1) / p.lanes;
+    p.R = kThreads / p.lanes;
+    const int64_t run = (int64_t)p.R * (back ? kBackAhead : kAhead), runs = (P + run - 1) / run;
+    // few runs: as many parts as runs, or half as many, joined by the blocks
+    // that write
+    const int64_t fold = runs <= 32 ? runs : (runs + 1) / 2;
+    if (C <= kFoldChannels && fold <= 32 && (int64_t)N * fold <= 256 &&
+        fold * (back ? C : G * p.slabs) <= 4096) {
+        p.way = NormPlan::kFold;
+        p.S = p.share = (int)atmost(fold, 32);
+        return p;
+    }
+    p.way = NormPlan::kLarge;
+    // sums: 4 blocks a CU, at least one a CU for every image; writing: two
+    // runs a block forward, 3 blocks a CU backward
+    const int64_t images = N > 0 ? (int64_t)N * p.slabs : 1;
+    int64_t S = 1024 / images;
+    if (S < 256 && images < 64) S = 256;
+    p.S = (int)atmost(S, runs);
+    p.share = back ? (int)atmost(768 / images, runs) : (int)atmost((runs + 1) / 2, 1 << 20);
+    return p;
+}
+
+inline NormK norm_args(const NormLaunch &L, const NormPlan &p)
+{
+    NormK k{};
+    k.N = L.N;
+    k.C = L.C;
+    k.G = L.G;
+    k.Cg = L.C / L.G;
+    k.P = L.P;
+    k.lanes = p.lanes;
+    k.R = p.R;
+    k.S = p.S;
+    k.slabs = p.slabs;
+    k.eps = L.eps;
+    k.gamma = L.gamma;
+    k.beta = L.beta;
+    k.x = L.x;
+    k.y = L.y;
+    k.dy = L.dy;
+    k.dx = L.dx;
+    k.stats = L.stats;
+    k.codes = L.codes;
+    k.exps = L.exps;
+    k.dgamma = L.dgamma;
+    k.dbeta = L.dbeta;
+    return k;
+}
+
+inline size_t up16(size_t n) { return (n + 15) & ~(size_t)15; }
+
+// Workspace: group values (float [N][G][2]), channel values (float2 [N][C],
+// backward), then the parts' sums.
+inline size_t group_bytes(int N, int G) { return up16((size_t)N * G * 8); }
+inline size_t channel_bytes(int N, int C) { return up16((size_t)N * C * 8); }
+
+// f(integral_constant<ACT>) for the activation.
+template <typename F>
+void with_act(int act, F f)
+{
+    switch (act) {
+    case kActNone: f(std::integral_constant<int, kActNone>()); break;
+    case kActRelu: f(std::integral_constant<int, kActRelu>()); break;
+    case kActSilu: f(std::integral_constant<int, kActSilu>()); break;
+    default: f(std::integral_constant<int, kActGelu>()); break;
+    }
+}
+
+// f((T *)0, integral_constant<V>) for the element type and vector width.
+template <typename F>
+void with_type(int dtype, int V, F f)
+{
+    if (dtype == kF32) {
+        if (V == 4) f((float *)0, std::integral_constant<int, 4>());
+        else if (V == 2) f((float *)0, std::integral_constant<int, 2>());
+        else f((float *)0, std::integral_constant<int, 1>());
+    } else if (dtype == kF16) {
+        if (V == 8) f((f16 *)0, std::integral_constant<int, 8>());
+        else if (V == 4) f((f16 *)0, std::integral_constant<int, 4>());
+        else if (V == 2) f((f16 *)0, std::integral_constant<int, 2>());
+        else f((f16 *)0, std::integral_constant<int, 1>());
+    } else {
+        if (V == 8) f((bf16 *)0, std::integral_constant<int, 8>());
+        else if (V == 4) f((bf16 *)0, std::integral_constant<int, 4>());
+        else if (V == 2) f((bf16 *)0, std::integral_constant<int, 2>());
+        else f((bf16 *)0, std::integral_constant<int, 1>());
+    }
+}
+
+}  // namespace mixrt
