@@ -6,15 +6,15 @@ namespace {
 
 // Adds a row's vector to sums of x and x^2, in 64 bits: the difference of
 // squares then keeps 32-bit accuracy for a mean up to 2^14 deviations away.
-// A = 1: the vector lies in one group.
+// Each of the A sums takes V / A channels, which lie in one group.
 template <typename T, int V, int A>
 __device__ __forceinline__ void add_squares(const Pack<T, V> &x, double (&s)[A], double (&q)[A])
 {
 #pragma unroll
     for (int i = 0; i < V; ++i) {
         const double d = (double)(float)x.v[i];
-        s[A == 1 ? 0 : i] += d;
-        q[A == 1 ? 0 : i] = fma(d, d, q[A == 1 ? 0 : i]);
+        s[i / (V / A)] += d;
+        q[i / (V / A)] = fma(d, d, q[i / (V / A)]);
     }
 }
 
@@ -50,12 +50,12 @@ __device__ __forceinline__ void write_row(T *y, const Channels<V> &c, const Pack
     store_vec<T, V>(y, f);
 }
 
-// Sums per group over one part of an image.  ONE: a vector lies in one group.
-// KEEP: x is also written in its 8-bit form.
-template <typename T, int V, bool ONE, bool KEEP>
+// Sums per group over one part of an image.  A: sums of x (and of x^2) that a
+// thread holds.  KEEP: x is also written in its 8-bit form.
+template <typename T, int V, int A, bool KEEP>
 __global__ __launch_bounds__(kThreads) void norm_sums_kernel(NormK k)
 {
-    constexpr int A = ONE ? 1 : V;   // accumulator pairs of a thread
+    constexpr int W = V / A;   // channels of a sum
     __shared__ double sh[2 * A][kThreads];
     const int t = threadIdx.x, slab = blockIdx.y, n = blockIdx.z;
     const int r = t / k.lanes, j = t - r * k.lanes;
@@ -89,9 +89,9 @@ __global__ __launch_bounds__(kThreads) void norm_sums_kernel(NormK k)
         lo = max(lo, 0);
         hi = min(hi, k.lanes * V);
         double2 v = make_double2(0.0, 0.0);
-        for (int c = lo; c < hi; c += ONE ? V : 1) {
-            v.x += sh[ONE ? 0 : c % V][c / V];
-            v.y += sh[A + (ONE ? 0 : c % V)][c / V];
+        for (int c = lo; c < hi; c += W) {
+            v.x += sh[c % V / W][c / V];
+            v.y += sh[A + c % V / W][c / V];
         }
         out[g] = v;
     }
@@ -232,18 +232,17 @@ __global__ __launch_bounds__(kSmallThreads) void norm_small_kernel(NormK k, int 
                         });
 }
 
-template <typename T, int V>
+// The sums with as few accumulators as the groups allow: one where a vector
+// lies in a group, one a group where whole groups lie in a vector.
+template <typename T, int V, int A>
 void forward_sums(const NormK &k, dim3 grid, hipStream_t s)
 {
-    const bool one = k.Cg % V == 0, keep = k.codes != nullptr;
-    if (one && keep)
-        norm_sums_kernel<T, V, true, true><<<grid, kThreads, 0, s>>>(k);
-    else if (one)
-        norm_sums_kernel<T, V, true, false><<<grid, kThreads, 0, s>>>(k);
-    else if (keep)
-        norm_sums_kernel<T, V, false, true><<<grid, kThreads, 0, s>>>(k);
+    if constexpr (A < V)
+        if (k.Cg % (V / A) != 0) return forward_sums<T, V, 2 * A>(k, grid, s);
+    if (k.codes)
+        norm_sums_kernel<T, V, A, true><<<grid, kThreads, 0, s>>>(k);
     else
-        norm_sums_kernel<T, V, false, false><<<grid, kThreads, 0, s>>>(k);
+        norm_sums_kernel<T, V, A, false><<<grid, kThreads, 0, s>>>(k);
 }
 
 }  // namespace
@@ -290,7 +289,7 @@ hipError_t launch_norm_forward(const NormLaunch &L, hipStream_t stream)
     with_type(L.dtype, p.V, [&](auto *t, auto v) {
         typedef std::remove_pointer_t<decltype(t)> T;
         constexpr int V = decltype(v)::value;
-        forward_sums<T, V>(k, dim3(p.S, p.slabs, L.N), stream);
+        forward_sums<T, V, 1>(k, dim3(p.S, p.slabs, L.N), stream);
     });
     if (p.way == NormPlan::kLarge)
         norm_stats_kernel<<<dim3((L.G + kJoinGroups - 1) / kJoinGroups, L.N), kJoinThreads, 0,

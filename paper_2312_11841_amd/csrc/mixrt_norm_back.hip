@@ -79,11 +79,12 @@ __global__ __launch_bounds__(kThreads) void norm_back_sums_kernel(NormK k)
 }
 
 // Joins an image's parts: every channel's sums, from them its groups' means.
-// A block takes `groups` whole groups; its threads lie over 32 channels at a
-// time and over the parts.
+// A block takes `groups` whole groups; its threads lie over kAcross channels
+// at a time and over the parts.
+template <int kAcross>
 __global__ __launch_bounds__(kJoinThreads) void norm_back_join_kernel(NormK k, int groups)
 {
-    constexpr int kAcross = 32, kDown = kJoinThreads / kAcross;
+    constexpr int kDown = kJoinThreads / kAcross;
     __shared__ double sh[2][kDown][kAcross + 1];
     const int n = blockIdx.y, g0 = blockIdx.x * groups;
     const int c_end = min((g0 + groups) * k.Cg, k.C);
@@ -139,6 +140,10 @@ __global__ __launch_bounds__(kJoinThreads) void norm_back_join_kernel(NormK k, i
     }
 }
 
+// Up to this many images, dx's first block adds up dgamma and dbeta as well (a
+// launch less, 4 us); beyond, and without dx, a kernel of its own.
+constexpr int kAffineImages = 64;
+
 // dgamma and dbeta of several images (or of none): a wave for each channel.
 __global__ __launch_bounds__(kThreads) void norm_affine_kernel(NormK k)
 {
@@ -158,8 +163,8 @@ __global__ __launch_bounds__(kThreads) void norm_affine_kernel(NormK k)
     }
 }
 
-// dx.  FOLD: the block joins the image's few parts itself; the first block
-// also writes dgamma and dbeta, over all images.
+// dx; the first block also writes dgamma and dbeta, over all images.  FOLD:
+// the block joins the image's few parts itself.
 template <typename T, int V, int ACT, bool KEPT, bool FOLD>
 __global__ __launch_bounds__(kThreads) void norm_back_apply_kernel(NormK k)
 {
@@ -208,6 +213,18 @@ __global__ __launch_bounds__(kThreads) void norm_back_apply_kernel(NormK k)
         __syncthreads();
         means = folded;
     }
+    if (!FOLD && k.N > 1 && k.N <= kAffineImages && n == 0 && blockIdx.x == 0 && blockIdx.y == 0)
+        for (int c = t; c < k.C; c += kThreads) {
+            double a = 0.0, b = 0.0;
+#pragma unroll 8
+            for (int i = 0; i < k.N; ++i) {
+                const float2 d = k.channels[(int64_t)i * k.C + c];
+                a += (double)d.x;
+                b += (double)d.y;
+            }
+            if (k.dbeta) k.dbeta[c] = (float)a;
+            if (k.dgamma) k.dgamma[c] = (float)b;
+        }
     if (r >= k.R || c0 >= k.C || !k.dx.data) return;
     Channels<V> c;
     c.set(k, k.stats + 2 * (int64_t)n * k.G, c0);
@@ -259,9 +276,14 @@ hipError_t launch_norm_backward(const NormLaunch &L, hipStream_t stream)
                 else
                     norm_back_sums_kernel<T, V, ACT, false><<<sums, kThreads, 0, stream>>>(k);
                 if (!fold) {
-                    const int groups = k.Cg >= 32 ? 1 : 32 / k.Cg;
-                    norm_back_join_kernel<<<dim3((L.G + groups - 1) / groups, L.N), kJoinThreads,
-                                            0, stream>>>(k, groups);
+                    // narrow blocks, so that their chains of loads are short;
+                    // wide ones where a group has many channels to go through
+                    const int groups = k.Cg >= 8 ? 1 : 8 / k.Cg;
+                    const dim3 joins((L.G + groups - 1) / groups, L.N);
+                    if (k.Cg <= 32)
+                        norm_back_join_kernel<8><<<joins, kJoinThreads, 0, stream>>>(k, groups);
+                    else
+                        norm_back_join_kernel<64><<<joins, kJoinThreads, 0, stream>>>(k, groups);
                     if (!L.dx.data) return;
                 }
                 if (L.codes && fold)
@@ -278,7 +300,7 @@ hipError_t launch_norm_backward(const NormLaunch &L, hipStream_t stream)
                         <<<grid, kThreads, 0, stream>>>(k);
             });
         });
-    if (L.N == 0 || (!fold && L.N > 1))
+    if (L.N == 0 || (!fold && (L.N > kAffineImages || (L.N > 1 && !L.dx.data))))
         if (L.dgamma || L.dbeta)
             norm_affine_kernel<<<(L.C + kThreads / 64 - 1) / (kThreads / 64), kThreads, 0,
                                  stream>>>(k);
