@@ -9,81 +9,102 @@ namespace {
 
 constexpr int kThreads = 256;
 
-// One kept group (32 channels of a row) per 32/V neighbouring lanes, groups in
-// the order of the scale bytes; a block takes kPackSteps steps of its threads
-// at a time, and further such runs where the grid is at its most.
-constexpr int kPackSteps = 8;
-constexpr int64_t kMostBlocks = 1 << 20;
+// Packing and reading back are streams: L neighbouring lanes of V channels
+// take a kept group (rows narrower than a group only as many lanes as they
+// need), groups in the order of the scale bytes.  A block takes kPackSteps
+// steps of its threads and ends; larger runs and loads ahead were slower (64
+// channels of a 720p frame in bf16, both ways: 65 us at 4 steps, 66 at 8, 73 at
+// 16, 81 with 8 loads ahead; the copy's rate for its 358 MB makes 62).
+constexpr int kPackSteps = 4;
+constexpr int64_t kMostBlocks = 1 << 20;   // then blocks take further runs
 
-template <typename T, int V>
+// Where a lane is: its group, counted from the block's first row, and channels.
+struct KeptLane {
+    int64_t row, group;   // group: the scale byte's index
+    int c0, left;         // left: channels from c0 to the row's end, 0 past the last group
+    __device__ __forceinline__ KeptLane(int64_t row0, uint32_t g, int64_t groups, int C,
+                                        int per_row, int at)
+    {
+        const uint32_t dr = per_row == 1 ? g : g / (uint32_t)per_row;
+        row = row0 + dr;
+        group = row0 * per_row + g;
+        c0 = (int)(g - dr * per_row) * kKeptGroup + at;
+        left = group < groups ? C - c0 : 0;
+    }
+};
+
+// Calls f(lane) for the steps of the runs that are this block's.
+template <int V, int L, typename F>
+__device__ __forceinline__ void walk_groups(int64_t groups, int C, int per_row, F f)
+{
+    constexpr int kStep = kThreads / L;   // groups of a step
+    constexpr int64_t kRun = (int64_t)kStep * kPackSteps;
+    for (int64_t first = (int64_t)blockIdx.x * kRun; first < groups;
+         first += (int64_t)gridDim.x * kRun) {
+        const int64_t row0 = first / per_row;
+        const uint32_t at0 = (uint32_t)(first - row0 * per_row) + threadIdx.x / L;
+#pragma unroll 1
+        for (int s = 0; s < kPackSteps; ++s)
+            f(KeptLane(row0, at0 + s * kStep, groups, C, per_row, (int)(threadIdx.x % L) * V));
+    }
+}
+
+// A vector may start at any element; where the row ends inside it (never with
+// WHOLE), its elements are moved one by one.
+template <typename T, int V, int L, bool WHOLE>
 __global__ __launch_bounds__(kThreads) void kept_pack_kernel(const T *x, int64_t stride,
                                                              int64_t groups, int C, int per_row,
                                                              int8_t *codes, uint8_t *exps)
 {
-    constexpr int L = kKeptGroup / V;            // lanes of a group
-    constexpr int kStep = kThreads / L;          // groups of a step
-    const uint32_t slot = threadIdx.x / L, lane = threadIdx.x % L;
-    for (int64_t first = (int64_t)blockIdx.x * (kStep * kPackSteps); first < groups;
-         first += (int64_t)gridDim.x * (kStep * kPackSteps)) {
-    const int64_t row0 = first / per_row;
-    const uint32_t at0 = (uint32_t)(first - row0 * per_row);
-#pragma unroll
-    for (int s = 0; s < kPackSteps; ++s) {
-        const uint32_t g = at0 + s * kStep + slot;   // counted from row0's first group
-        if (row0 * per_row + g >= groups) return;     // the whole group's lanes
-        const uint32_t dr = g / (uint32_t)per_row;
-        const int64_t row = row0 + dr;
-        const int c0 = (int)(g - dr * per_row) * kKeptGroup + (int)lane * V;
-        const bool in = c0 < C;
+    walk_groups<V, L>(groups, C, per_row, [&](const KeptLane &l) {
+        const T *p = x + l.row * stride + l.c0;
         float f[V];
-        if (in)
-            load_vec<T, V>(x + row * stride + c0, f);
+        if (l.left >= V)
+            load_vec<T, V>(p, f);
         else
 #pragma unroll
-            for (int i = 0; i < V; ++i) f[i] = 0.0f;
+            for (int i = 0; i < V; ++i) f[i] = !WHOLE && i < l.left ? (float)p[i] : 0.0f;
         uint32_t top = 0;
 #pragma unroll
         for (int i = 0; i < V; ++i) top = max(top, __float_as_uint(f[i]) & 0x7fffffffu);
 #pragma unroll
-        for (int d = 1; d < L; d <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, d));
+        for (int e = 1; e < L; e <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, e));
         const uint32_t byte = kept_byte<T>(top);
-        if (in) {
-            Pack<int8_t, V> out;
+        Pack<int8_t, V> out;
 #pragma unroll
-            for (int i = 0; i < V; ++i) out.v[i] = (int8_t)kept_code<T>(f[i], byte);
-            *(Pack<int8_t, V> *)(codes + row * C + c0) = out;
-        }
-        if (lane == 0) exps[row0 * per_row + g] = (uint8_t)byte;
-    }
-    }
+        for (int i = 0; i < V; ++i) out.v[i] = (int8_t)kept_code<T>(f[i], byte);
+        int8_t *q = codes + l.row * C + l.c0;
+        if (l.left >= V)
+            *(Pack<int8_t, V> *)q = out;
+        else if (!WHOLE)
+#pragma unroll
+            for (int i = 0; i < V; ++i)
+                if (i < l.left) q[i] = out.v[i];
+        if (threadIdx.x % L == 0 && l.left > 0) exps[l.group] = (uint8_t)byte;
+    });
 }
 
-template <typename T, int V>
+template <typename T, int V, int L, bool WHOLE>
 __global__ __launch_bounds__(kThreads) void kept_unpack_kernel(const int8_t *codes,
-                                                               const uint8_t *exps, int64_t rows,
+                                                               const uint8_t *exps, int64_t groups,
                                                                int C, int per_row, T *out,
                                                                int64_t stride)
 {
-    const uint32_t vecs = (uint32_t)C / V;
-    for (int64_t first = (int64_t)blockIdx.x * (kThreads * kPackSteps); first < rows * vecs;
-         first += (int64_t)gridDim.x * (kThreads * kPackSteps)) {
-    const int64_t row0 = first / vecs;
-    const uint32_t at0 = (uint32_t)(first - row0 * vecs);
+    walk_groups<V, L>(groups, C, per_row, [&](const KeptLane &l) {
+        if (l.left <= 0) return;
+        const int8_t *q = codes + l.row * C + l.c0;
+        const float scale = kept_scale(exps[l.group]);
+        T *p = out + l.row * stride + l.c0;
+        if (l.left >= V) {
+            const Pack<int8_t, V> v = *(const Pack<int8_t, V> *)q;
+            float f[V];
 #pragma unroll
-    for (int s = 0; s < kPackSteps; ++s) {
-        const uint32_t v = at0 + s * kThreads + threadIdx.x;
-        const uint32_t dr = v / vecs;
-        const int64_t row = row0 + dr;
-        if (row >= rows) return;
-        const int c0 = (int)(v - dr * vecs) * V;
-        const Pack<int8_t, V> q = *(const Pack<int8_t, V> *)(codes + row * C + c0);
-        const float sc = kept_scale(exps[row * per_row + c0 / kKeptGroup]);
-        float f[V];
-#pragma unroll
-        for (int i = 0; i < V; ++i) f[i] = (float)q.v[i] * sc;
-        store_vec<T, V>(out + row * stride + c0, f);
-    }
-    }
+            for (int i = 0; i < V; ++i) f[i] = (float)v.v[i] * scale;
+            store_vec<T, V>(p, f);
+        } else if (!WHOLE) {
+            for (int i = 0; i < l.left; ++i) p[i] = (T)((float)q[i] * scale);
+        }
+    });
 }
 
 // --- the weight gradient of a linear layer -----------------------------------------
@@ -532,17 +553,6 @@ LinearPlan linear_plan(int64_t rows, int C, int outs)
 }
 
 template <typename F>
-void with_vector(int C, int widest, F f)
-{
-    int V = widest;
-    while (C % V) V >>= 1;
-    if (V == 8) f(std::integral_constant<int, 8>());
-    else if (V == 4) f(std::integral_constant<int, 4>());
-    else if (V == 2) f(std::integral_constant<int, 2>());
-    else f(std::integral_constant<int, 1>());
-}
-
-template <typename F>
 void with_type(int dtype, F f)
 {
     if (dtype == kF32) f((float *)0);
@@ -558,6 +568,26 @@ unsigned blocks(int64_t n, int64_t per)
 
 }  // namespace
 
+namespace {
+
+// f(lanes of a group, whether vectors end with the row) for rows of C channels
+// in vectors of V.
+template <int V, typename F>
+void with_lanes(int C, F f)
+{
+    auto go = [&](auto l) {
+        if (C % V == 0) f(l, std::true_type());
+        else f(l, std::false_type());
+    };
+    if (C <= V) go(std::integral_constant<int, 1>());
+    else if (C <= 2 * V) go(std::integral_constant<int, 2>());
+    else if constexpr (V == 8) go(std::integral_constant<int, 4>());
+    else if (C <= 4 * V) go(std::integral_constant<int, 4>());
+    else go(std::integral_constant<int, 8>());
+}
+
+}  // namespace
+
 hipError_t launch_kept_pack(int dtype, int64_t rows, int C, const void *x, int64_t stride,
                             int8_t *codes, uint8_t *exps, hipStream_t stream)
 {
@@ -566,11 +596,12 @@ hipError_t launch_kept_pack(int dtype, int64_t rows, int C, const void *x, int64
     const int64_t groups = rows * per_row;
     with_type(dtype, [&](auto *t) {
         typedef std::remove_pointer_t<decltype(t)> T;
-        with_vector(C, sizeof(T) == 4 ? 4 : 8, [&](auto v) {
-            constexpr int V = decltype(v)::value;
-            const int64_t per = (int64_t)kThreads * V / kKeptGroup * kPackSteps;
-            kept_pack_kernel<T, V><<<blocks(groups, per), kThreads, 0, stream>>>(
-                (const T *)x, stride, groups, C, per_row, codes, exps);
+        constexpr int V = sizeof(T) == 4 ? 4 : 8;
+        with_lanes<V>(C, [&](auto l, auto whole) {
+            constexpr int L = decltype(l)::value;
+            kept_pack_kernel<T, V, L, decltype(whole)::value>
+                <<<blocks(groups, (int64_t)kThreads / L * kPackSteps), kThreads, 0, stream>>>(
+                    (const T *)x, stride, groups, C, per_row, codes, exps);
         });
     });
     return hipGetLastError();
@@ -580,13 +611,16 @@ hipError_t launch_kept_unpack(int out_dtype, int64_t rows, int C, const int8_t *
                               const uint8_t *exps, void *out, int64_t stride, hipStream_t stream)
 {
     if (rows == 0) return hipSuccess;
+    const int per_row = kept_groups(C);
+    const int64_t groups = rows * per_row;
     with_type(out_dtype, [&](auto *t) {
         typedef std::remove_pointer_t<decltype(t)> T;
-        with_vector(C, sizeof(T) == 4 ? 4 : 8, [&](auto v) {
-            constexpr int V = decltype(v)::value;
-            kept_unpack_kernel<T, V>
-                <<<blocks(rows * (C / V), (int64_t)kThreads * kPackSteps), kThreads, 0, stream>>>(
-                    codes, exps, rows, C, kept_groups(C), (T *)out, stride);
+        constexpr int V = sizeof(T) == 4 ? 4 : 8;
+        with_lanes<V>(C, [&](auto l, auto whole) {
+            constexpr int L = decltype(l)::value;
+            kept_unpack_kernel<T, V, L, decltype(whole)::value>
+                <<<blocks(groups, (int64_t)kThreads / L * kPackSteps), kThreads, 0, stream>>>(
+                    codes, exps, groups, C, per_row, (T *)out, stride);
         });
     });
     return hipGetLastError();
