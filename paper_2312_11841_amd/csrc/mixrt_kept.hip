@@ -124,14 +124,12 @@ constexpr int kRows = 32;     // rows of a step
 typedef float f4 __attribute__((ext_vector_type(4)));
 typedef _Float16 h8 __attribute__((ext_vector_type(8)));
 typedef __bf16 b8 __attribute__((ext_vector_type(8)));
-typedef float f8 __attribute__((ext_vector_type(8)));
 typedef _Float16 h2 __attribute__((ext_vector_type(2)));
 
 // 8 rows of one channel: an MFMA operand of a lane.
 template <typename T> struct Frag;
 template <> struct Frag<f16> { typedef h8 type; };
 template <> struct Frag<bf16> { typedef b8 type; };
-template <> struct Frag<float> { typedef f8 type; };
 
 __device__ __forceinline__ f4 mac(h8 a, h8 b, f4 c)
 {
@@ -141,14 +139,6 @@ __device__ __forceinline__ f4 mac(b8 a, b8 b, f4 c)
 {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
-// rows 8 q + i for the lanes' quarters q, one i at a time
-__device__ __forceinline__ f4 mac(f8 a, f8 b, f4 c)
-{
-#pragma unroll
-    for (int i = 0; i < 8; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[i], b[i], c, 0, 0, 0);
-    return c;
-}
-
 struct LinearK {
     const int8_t *codes;
     const uint8_t *exps;
@@ -157,7 +147,7 @@ struct LinearK {
     int64_t part;     // rows of one block
     int64_t whole;    // rows whose vectors stay inside the arrays
     int C, outs, per_row;
-    int ty, parts;    // tiles of dw along its channels, parts of the rows
+    int ty, tz;       // tiles of dw along its channels and its outs
     float *sums;      // [parts][C * outs + outs]
 };
 
@@ -266,39 +256,33 @@ template <> struct Scales<f16> {
     }
 };
 
-// Element m of 8 rows' codes as an operand.  u: the codes plus 128, as bytes.
-// In 32 bits: u 2^e - 128 2^e, without rounding; its upper half is the bf16.
-__device__ __forceinline__ f8 code_frag(const uint32_t (&u)[8], const Scales<float> &s, int m)
+// Element m of 8 rows' codes as an operand.  bf16: the product with 2^e in 32
+// bits, without rounding; its upper half is the bf16.
+__device__ __forceinline__ float code_value(uint32_t code, int m, float scale)
 {
-    f8 a;
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-        a[i] = fmaf((float)((u[i] >> (8 * m)) & 255u), s.v[i], -128.0f * s.v[i]);
-    return a;
+    return (float)(int8_t)(code >> (8 * m)) * scale;
 }
-__device__ __forceinline__ b8 code_frag(const uint32_t (&u)[8], const Scales<bf16> &s, int m)
+__device__ __forceinline__ b8 code_frag(const uint32_t (&code)[8], const Scales<bf16> &s, int m)
 {
     uint32_t w[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const float lo = fmaf((float)((u[2 * i] >> (8 * m)) & 255u), s.v[2 * i],
-                              -128.0f * s.v[2 * i]);
-        const float hi = fmaf((float)((u[2 * i + 1] >> (8 * m)) & 255u), s.v[2 * i + 1],
-                              -128.0f * s.v[2 * i + 1]);
-        w[i] = __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u);
-    }
+    for (int i = 0; i < 4; ++i)
+        w[i] = __builtin_amdgcn_perm(
+            __float_as_uint(code_value(code[2 * i + 1], m, s.v[2 * i + 1])),
+            __float_as_uint(code_value(code[2 * i], m, s.v[2 * i])), 0x07060302u);
     return __builtin_bit_cast(b8, w);
 }
-// In f16, two rows at once: the byte u below 0x64 is 1024 + u; less 1152 it is
-// the code, and its product with 2^e is exact.
-__device__ __forceinline__ h8 code_frag(const uint32_t (&u)[8], const Scales<f16> &s, int m)
+// f16: two rows at once.  The byte of code + 128 (its top bit turned) below
+// 0x64 is the f16 1024 + 128 + code; less 1152 it is the code, and its product
+// with 2^e is exact.
+__device__ __forceinline__ h8 code_frag(const uint32_t (&code)[8], const Scales<f16> &s, int m)
 {
     h2 w[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const uint32_t pair = __builtin_amdgcn_perm(u[2 * i + 1], u[2 * i],
-                                                    0x0c040c00u + 0x00010001u * m) |
-                              0x64006400u;
+        const uint32_t pair = __builtin_amdgcn_perm(code[2 * i + 1], code[2 * i],
+                                                    0x0c040c00u + 0x00010001u * m) ^
+                              0x64806480u;
         w[i] = (__builtin_bit_cast(h2, pair) - (f16)1152.0f) * s.v[i];
     }
     return __builtin_bit_cast(h8, w);
@@ -309,20 +293,13 @@ template <typename T>
 __device__ __forceinline__ typename Frag<T>::type dy_frag(const LinearStep<T> &s, int n)
 {
     typedef typename Frag<T>::type F;
-    if constexpr (sizeof(T) == 4) {
-        F b;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) b[i] = __uint_as_float(s.dy[i][n]);
-        return b;
-    } else {
-        const uint32_t sel = n & 1 ? 0x07060302u : 0x05040100u;
-        uint4 w;
-        w.x = __builtin_amdgcn_perm(s.dy[1][n >> 1], s.dy[0][n >> 1], sel);
-        w.y = __builtin_amdgcn_perm(s.dy[3][n >> 1], s.dy[2][n >> 1], sel);
-        w.z = __builtin_amdgcn_perm(s.dy[5][n >> 1], s.dy[4][n >> 1], sel);
-        w.w = __builtin_amdgcn_perm(s.dy[7][n >> 1], s.dy[6][n >> 1], sel);
-        return __builtin_bit_cast(F, w);
-    }
+    const uint32_t sel = n & 1 ? 0x07060302u : 0x05040100u;
+    uint4 w;
+    w.x = __builtin_amdgcn_perm(s.dy[1][n >> 1], s.dy[0][n >> 1], sel);
+    w.y = __builtin_amdgcn_perm(s.dy[3][n >> 1], s.dy[2][n >> 1], sel);
+    w.z = __builtin_amdgcn_perm(s.dy[5][n >> 1], s.dy[4][n >> 1], sel);
+    w.w = __builtin_amdgcn_perm(s.dy[7][n >> 1], s.dy[6][n >> 1], sel);
+    return __builtin_bit_cast(F, w);
 }
 
 template <typename T>
@@ -331,15 +308,12 @@ __device__ __forceinline__ void multiply_step(const LinearStep<T> &s, bool biase
 {
     typedef typename Frag<T>::type F;
     const Scales<T> sc(s.byte);
-    uint32_t u[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) u[i] = s.code[i] ^ 0x80808080u;
     F b[4];
 #pragma unroll
     for (int n = 0; n < 4; ++n) b[n] = dy_frag(s, n);
 #pragma unroll
     for (int m = 0; m < 4; ++m) {
-        const F a = code_frag(u, sc, m);
+        const F a = code_frag(s.code, sc, m);
 #pragma unroll
         for (int n = 0; n < 4; ++n) acc[m][n] = mac(a, b[n], acc[m][n]);
     }
@@ -352,20 +326,45 @@ __device__ __forceinline__ void multiply_step(const LinearStep<T> &s, bool biase
     }
 }
 
+// f32: a step's rows 8 q + i of the lanes' quarters q, one i at a time.
+template <>
+__device__ __forceinline__ void multiply_step(const LinearStep<float> &s, bool biased,
+                                              f4 (&acc)[4][4], f4 (&bias)[4])
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float sc = kept_scale(s.byte[i]);
+        float b[4];
+#pragma unroll
+        for (int n = 0; n < 4; ++n) b[n] = __uint_as_float(s.dy[i][n]);
+#pragma unroll
+        for (int m = 0; m < 4; ++m) {
+            const float a = code_value(s.code[i], m, sc);
+#pragma unroll
+            for (int n = 0; n < 4; ++n)
+                acc[m][n] = __builtin_amdgcn_mfma_f32_16x16x4f32(a, b[n], acc[m][n], 0, 0, 0);
+        }
+        if (biased)
+#pragma unroll
+            for (int n = 0; n < 4; ++n)
+                bias[n] = __builtin_amdgcn_mfma_f32_16x16x4f32(1.0f, b[n], bias[n], 0, 0, 0);
+    }
+}
+
 template <typename T>
 __global__ __launch_bounds__(kThreads) void linear_grad_kernel(LinearK k)
 {
     __shared__ float sh[kTile * kTile + kTile];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x & 63;
     const int q = lane >> 4, c = lane & 15;
-    // Blocks are dealt to the 8 XCDs in turn; a run of them along the channels
-    // reads the same rows of dy, so each XCD takes one such run after another
-    // and finds dy (and, across its few tiles of dy, the codes) in its L2.
+    // Blocks are dealt to the 8 XCDs in turn.  Each XCD takes a run of a part's
+    // tiles, which read the same rows at the same time and find them in its L2
+    // (100,000 rows, 512 x 512, bf16: codes read by every XCD take 134 us)
     const int nb = gridDim.x, x = blockIdx.x & 7;
     int at = x * (nb >> 3) + min(x, nb & 7) + (blockIdx.x >> 3);
     const int ty = at % k.ty;
     at /= k.ty;
-    const int part = at % k.parts, tz = at / k.parts;
+    const int tz = at % k.tz, part = at / k.tz;
     int ci = ty * kTile + 4 * c, co = tz * kTile + 4 * c;
     if (ci >= k.C) ci = 0;
     if (co >= k.outs) co = 0;
@@ -391,19 +390,8 @@ __global__ __launch_bounds__(kThreads) void linear_grad_kernel(LinearK k)
         const auto load = [&](LinearStep<T> &s, int i) {
             load_step(s, r0 + (int64_t)min(i, n - 1) * (4 * kRows), off, k);
         };
-        LinearStep<T> s0, s1;
+        LinearStep<T> s0, s1, s2;
         load(s0, 0);
-        if constexpr (sizeof(T) == 4) {   // one step: the registers hold no more
-            for (int i = 0;; i += 2) {
-                load(s1, i + 1);
-                multiply_step(s0, biased, acc, bias);
-                if (i + 1 >= n) break;
-                load(s0, i + 2);
-                multiply_step(s1, biased, acc, bias);
-                if (i + 2 >= n) break;
-            }
-        } else {
-        LinearStep<T> s2;
         load(s1, 1);
         for (int i = 0;; i += 3) {
             load(s2, i + 2);
@@ -415,7 +403,6 @@ __global__ __launch_bounds__(kThreads) void linear_grad_kernel(LinearK k)
             load(s1, i + 4);
             multiply_step(s2, biased, acc, bias);
             if (i + 3 >= n) break;
-        }
         }
     }
     for (r0 += (int64_t)n * (4 * kRows); r0 < r1; r0 += 4 * kRows) {
@@ -644,7 +631,7 @@ hipError_t launch_linear_grad(int dtype, int64_t rows, int C, int outs, const in
     if (outs % 4 && dy_stride < outs) whole = 0;
     if (dy_stride >= (1 << 24)) whole = 0;   // the lanes' offsets are 32 bits
     LinearK k{codes,          exps, dy,   rows,    dy_stride,  p.part, whole, C, outs,
-              kept_groups(C), p.ty, p.parts, (float *)ws};
+              kept_groups(C), p.ty, p.tz, (float *)ws};
     const int grid = p.parts * p.ty * p.tz;
     const int64_t weights = (int64_t)C * outs, n = weights + outs;
     const bool tiny = rows * C < 4 || (rows - 1) * dy_stride + outs < 4;

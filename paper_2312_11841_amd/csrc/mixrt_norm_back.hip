@@ -168,32 +168,58 @@ __global__ __launch_bounds__(kThreads) void norm_affine_kernel(NormK k)
 template <typename T, int V, int ACT, bool KEPT, bool FOLD>
 __global__ __launch_bounds__(kThreads) void norm_back_apply_kernel(NormK k)
 {
-    __shared__ double ca[FOLD ? kFoldChannels : 1], cb[FOLD ? kFoldChannels : 1];
+    __shared__ double ca[FOLD ? kFoldChannels : 1], cx[FOLD ? kFoldChannels : 1];
     __shared__ float2 folded[FOLD ? kFoldChannels : 1];
     const int t = threadIdx.x, n = blockIdx.z;
     const int r = t / k.lanes, j = t - r * k.lanes;
     const int c0 = (blockIdx.y * k.lanes + j) * V;
     const float2 *means = (const float2 *)k.means + (int64_t)n * k.G;
     if (FOLD) {
+        // threads over the channels and, where those are few, over the parts
         const float2 *v = (const float2 *)k.sums;
-        const auto add = [&](int c, int image, double &a, double &b) {
+        __shared__ double2 across[kThreads];
+        const int width = min(k.C, kThreads), down = kThreads / width;
+        const int cl = t % width, dl = t / width;
+        const auto add = [&](int c, int image, double2 &s) {
+            if (c < k.C && dl < down)
 #pragma unroll 8
-            for (int i = 0; i < k.S; ++i) {
-                const float2 d = v[((int64_t)image * k.S + i) * k.C + c];
-                a += (double)d.x;
-                b += (double)d.y;
-            }
+                for (int i = dl; i < k.S; i += down) {
+                    const float2 d = v[((int64_t)image * k.S + i) * k.C + c];
+                    s.x += (double)d.x;
+                    s.y += (double)d.y;
+                }
         };
-        for (int c = t; c < k.C; c += kThreads) {
-            double a = 0.0, b = 0.0;
-            add(c, n, a, b);
-            const double ga = k.gamma ? (double)k.gamma[c] : 1.0;
-            ca[c] = ga * a;
-            cb[c] = ga * b;
-            if (n == 0 && blockIdx.x == 0 && blockIdx.y == 0) {
-                for (int i = 1; i < k.N; ++i) add(c, i, a, b);
-                if (k.dbeta) k.dbeta[c] = (float)a;
-                if (k.dgamma) k.dgamma[c] = (float)b;
+        const auto join = [&](double2 s) {   // in the first thread of a channel
+            across[t] = s;
+            __syncthreads();
+            s = make_double2(0.0, 0.0);
+            if (dl == 0)
+                for (int i = 0; i < down; ++i) {
+                    s.x += across[i * width + cl].x;
+                    s.y += across[i * width + cl].y;
+                }
+            __syncthreads();
+            return s;
+        };
+        const bool all = n == 0 && blockIdx.x == 0 && blockIdx.y == 0;
+        for (int cb = 0; cb < k.C; cb += width) {
+            const int c = cb + cl;
+            double2 own = make_double2(0.0, 0.0);
+            add(c, n, own);
+            own = join(own);
+            if (dl == 0 && c < k.C) {
+                const double ga = k.gamma ? (double)k.gamma[c] : 1.0;
+                ca[c] = ga * own.x;
+                cx[c] = ga * own.y;
+            }
+            if (all) {
+                double2 rest = make_double2(0.0, 0.0);
+                for (int i = 1; i < k.N; ++i) add(c, i, rest);
+                rest = join(rest);
+                if (dl == 0 && c < k.C) {
+                    if (k.dbeta) k.dbeta[c] = (float)(own.x + rest.x);
+                    if (k.dgamma) k.dgamma[c] = (float)(own.y + rest.y);
+                }
             }
         }
         __syncthreads();
@@ -201,7 +227,7 @@ __global__ __launch_bounds__(kThreads) void norm_back_apply_kernel(NormK k)
             double a = 0.0, b = 0.0;
             for (int i = t & 63; i < k.Cg; i += 64) {
                 a += ca[g * k.Cg + i];
-                b += cb[g * k.Cg + i];
+                b += cx[g * k.Cg + i];
             }
             a = wave_sum(a);
             b = wave_sum(b);
@@ -230,12 +256,11 @@ __global__ __launch_bounds__(kThreads) void norm_back_apply_kernel(NormK k)
     c.set(k, k.stats + 2 * (int64_t)n * k.G, c0);
     // rstd (gamma dz - ma - xh mb) = scale dz - (rstd ma + (x - mean) rstd^2 mb)
     float ma[V], mb[V];
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-        const float2 m = means[(c0 + i) / k.Cg];
+    for_groups<V>(k, c0, [&](int i, int g) {
+        const float2 m = means[g];
         ma[i] = c.rstd[i] * m.x;
         mb[i] = c.rstd[i] * (c.rstd[i] * m.y);
-    }
+    });
     T *dx = (T *)k.dx.data + n * k.dx.image + c0;
     walk<BackRow<T, V, KEPT>, kBackAhead>(
         blockIdx.x, gridDim.x, r, k.R, k.P,
