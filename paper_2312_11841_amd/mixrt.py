@@ -608,7 +608,8 @@ class Checkpoint:
 # --- the library handle ------------------------------------------------------------
 
 class Renderer:
-    """One mixrt context bound to a device and a HIP stream."""
+    """One mixrt context bound to a device and a HIP stream; its calls come
+    from one thread at a time."""
 
     def __init__(self, device: int = 0, stream=None, sync_check: bool = False, blocks=None,
                  tile_stripe: int = 0, early_stop_chunk: int = 0, block_levels: int = 0,
@@ -638,7 +639,8 @@ class Renderer:
             raise MixrtError(rc, self._L.mixrt_thread_error().decode())
         self._h = h
         self._dev, self._raw_stream = torch.device("cuda", device), int(stream.cuda_stream)
-        self._ws = None     # the refiner's operators' scratch: (address, bytes)
+        # the refiner's operators' scratch: (address, bytes), and its memory
+        self._ws, self._ws_memory = None, []
 
     def _check(self, rc: int):
         if rc != MIXRT_OK:
@@ -824,11 +826,15 @@ class Renderer:
 
     def _workspace(self, size: int):
         """(address, bytes) of this context's scratch, at least size bytes.
-        Its calls run one after another on its stream, so they share it."""
+        Its calls run one after another on its stream, so they share it.  A
+        smaller one that it grew out of stays allocated, since a captured graph
+        may still write there; sizes at least double, so that all of them
+        together take less than twice the last."""
         if self._ws is None or self._ws[1] < size:
             import torch
-            self._ws_memory = self._empty((max(size, 1 << 16),), torch.uint8)
-            self._ws = (self._ws_memory.data_ptr(), self._ws_memory.numel())
+            last = self._ws[1] if self._ws else 1 << 15
+            self._ws_memory.append(self._empty((max(size, 2 * last),), torch.uint8))
+            self._ws = (self._ws_memory[-1].data_ptr(), self._ws_memory[-1].numel())
         return self._ws
 
     def _checkpoint(self, rows: int, channels: int, dtype) -> Checkpoint:

@@ -270,6 +270,40 @@ def test_a_captured_step_replays(r):
         c.close()
 
 
+def test_a_graph_survives_a_larger_call(r):
+    """A context's scratch may grow after a capture: replays still give the
+    eager outputs."""
+    g = _gen(13)
+    x = _maps(g, 1, 30000, 32, torch.float16)
+    big = _maps(g, 2, 70000, 64, torch.float16)
+    stream = torch.cuda.Stream()
+    c = mixrt.Renderer(0, stream=stream)
+    try:
+        torch.cuda.synchronize()
+        want = c.group_norm(x, 8, act="gelu").clone()
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            out = c.group_norm(x, 8, act="gelu")
+        before = c._ws
+        c.group_norm(big, 64, act="silu")
+        kept = c.checkpoint_pack(big)
+        c.linear_weight_grad(kept, big.reshape(-1, 64))
+        assert c._ws[0] != before[0]
+        c.sync()
+        fill = [torch.full((1 << 20,), 1e30, device="cuda") for _ in range(8)]
+        torch.cuda.synchronize()
+        for _ in range(3):
+            out.zero_()
+            torch.cuda.synchronize()
+            graph.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(out, want)
+            assert all(bool((f == 1e30).all()) for f in fill)
+    finally:
+        c.close()
+
+
 # --- activations in 8 bits -----------------------------------------------------------
 
 KEPT = [(1, 1), (3, 4), (7, 31), (65, 32), (40, 33), (129, 64), (53, 43), (300, 24), (17, 257),
