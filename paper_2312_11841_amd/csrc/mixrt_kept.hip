@@ -70,9 +70,7 @@ __global__ __launch_bounds__(kThreads) void kept_pack_kernel(const T *x, int64_t
 #pragma unroll
         for (int e = 1; e < L; e <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, e));
         const uint32_t byte = kept_byte<T>(top);
-        Pack<int8_t, V> out;
-#pragma unroll
-        for (int i = 0; i < V; ++i) out.v[i] = (int8_t)kept_code<T>(f[i], byte);
+        const Pack<int8_t, V> out = kept_codes<T, V>(f, byte);
         int8_t *q = codes + l.row * C + l.c0;
         if (l.left >= V)
             *(Pack<int8_t, V> *)q = out;

@@ -24,18 +24,19 @@ template <typename T, int V>
 __device__ __forceinline__ void keep_row(const NormK &k, int64_t row, int c0, bool in,
                                          const Pack<T, V> &x)
 {
+    float f[V];
     uint32_t top = 0;
 #pragma unroll
-    for (int i = 0; i < V; ++i) top = max(top, __float_as_uint((float)x.v[i]) & 0x7fffffffu);
+    for (int i = 0; i < V; ++i) {
+        f[i] = (float)x.v[i];
+        top = max(top, __float_as_uint(f[i]) & 0x7fffffffu);
+    }
     if (!in) top = 0;
 #pragma unroll
     for (int d = 1; d < kKeptGroup / V; d <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, d));
     const uint32_t byte = kept_byte<T>(top);
     if (!in) return;
-    Pack<int8_t, V> out;
-#pragma unroll
-    for (int i = 0; i < V; ++i) out.v[i] = (int8_t)kept_code<T>((float)x.v[i], byte);
-    *(Pack<int8_t, V> *)(k.codes + row * k.C + c0) = out;
+    *(Pack<int8_t, V> *)(k.codes + row * k.C + c0) = kept_codes<T, V>(f, byte);
     if (c0 % kKeptGroup == 0)
         k.exps[row * kept_groups(k.C) + c0 / kKeptGroup] = (uint8_t)byte;
 }

@@ -22,9 +22,11 @@ namespace mixrt {
 inline constexpr int kThreads = 256;
 inline constexpr int kSmallThreads = 1024;
 inline constexpr int kJoinThreads = 1024;
-// Rows a thread loads before it uses the first.  Backward: two, or the
-// registers leave too few waves.
-inline constexpr int kAhead = 4, kBackAhead = 2;
+// Rows a thread loads before it uses the first.  The backward's sums take one
+// at a time: they are bound by their arithmetic and gain from more waves (8 x
+// 360p x 64 in bf16: 95 us, with two 106, four 135; its writing 136 with one,
+// 123 with two, 104 with four).
+inline constexpr int kAhead = 4;
 inline constexpr int kFoldChannels = 512;   // most channels (and groups) of a join by the blocks
 
 struct NormK {
@@ -237,7 +239,7 @@ inline NormPlan norm_plan(int N, int64_t P, int C, int G, int dtype, bool pad, b
     p.lanes = wide < kThreads ? wide : kThreads;
     p.slabs = (wide + p.lanes - 1) / p.lanes;
     p.R = kThreads / p.lanes;
-    const int64_t run = (int64_t)p.R * (back ? kBackAhead : kAhead), runs = (P + run - 1) / run;
+    const int64_t run = (int64_t)p.R * kAhead, runs = (P + run - 1) / run;
     // few runs: as many parts as runs, or half as many, joined by the blocks
     // that write (16 channels of 320 x 180 in f16, 57 parts: 12.2 us, joined by
     // a launch 13.6; backward, 32 channels of 160 x 90, 57 parts: 19.1 and 18.2,

@@ -49,7 +49,7 @@ __global__ __launch_bounds__(kThreads) void norm_back_sums_kernel(NormK k)
     if (r < k.R && c0 < k.C) {
         Channels<V> c;
         c.set(k, k.stats + 2 * (int64_t)n * k.G, c0);
-        walk<BackRow<T, V, KEPT>, kBackAhead>(
+        walk<BackRow<T, V, KEPT>, 1>(
             blockIdx.x, gridDim.x, r, k.R, k.P,
             [&](int64_t p) { return load_back<T, V, KEPT>(k, n, p, c0); },
             [&](int64_t, const BackRow<T, V, KEPT> &d) {
@@ -262,7 +262,7 @@ __global__ __launch_bounds__(kThreads) void norm_back_apply_kernel(NormK k)
         mb[i] = c.rstd[i] * (c.rstd[i] * m.y);
     });
     T *dx = (T *)k.dx.data + n * k.dx.image + c0;
-    walk<BackRow<T, V, KEPT>, kBackAhead>(
+    walk<BackRow<T, V, KEPT>, kAhead>(
         blockIdx.x, gridDim.x, r, k.R, k.P,
         [&](int64_t p) { return load_back<T, V, KEPT>(k, n, p, c0); },
         [&](int64_t p, const BackRow<T, V, KEPT> &d) {

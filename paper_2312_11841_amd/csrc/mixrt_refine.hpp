@@ -116,15 +116,25 @@ __device__ __forceinline__ uint32_t kept_byte(uint32_t bits)
     return bits >= 0x7f800000u ? 255u : (uint32_t)(e + 127);
 }
 
-// The code of x at a scale byte.  kTop: 64 * 2^kTop is not finite in T, so the
-// code stops at 63 there.
-template <typename T>
-__device__ __forceinline__ int kept_code(float x, uint32_t byte)
+// The codes of V values at their group's scale byte.  x 2^-e is exact; added to
+// 1.5 * 2^23 it leaves its nearest integer (halves to even) in the sum's low
+// bits, and by the choice of e that is at most 127 in magnitude.  2^-e is taken
+// as 0 for byte 255, whose codes are then 0 (a NaN's low bits are).  From kTop
+// on, where 64 * 2^e is not finite in T, the codes stop at 63.
+template <typename T, int V>
+__device__ __forceinline__ Pack<int8_t, V> kept_codes(const float (&x)[V], uint32_t byte)
 {
-    const float inv = __uint_as_float((254u - byte) << 23);   // 2^-e
-    const float cap = byte >= (uint32_t)(KeptRange<T>::kTop + 127) ? 63.0f : 127.0f;
-    const float q = fminf(fmaxf(rintf(x * inv), -cap), cap);
-    return byte == 255u ? 0 : (int)q;
+    const float inv = byte == 255u ? 0.0f : __uint_as_float((254u - byte) << 23);
+    Pack<int8_t, V> q;
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+        q.v[i] = (int8_t)(__float_as_uint(fmaf(x[i], inv, 12582912.0f)) & 255u);
+    // (a branch for the wave: as a choice for each lane it costs two steps a value)
+    if (__builtin_amdgcn_ballot_w64(byte >= (uint32_t)(KeptRange<T>::kTop + 127)) != 0 &&
+        byte >= (uint32_t)(KeptRange<T>::kTop + 127))
+#pragma unroll
+        for (int i = 0; i < V; ++i) q.v[i] = (int8_t)max(min((int)q.v[i], 63), -63);
+    return q;
 }
 
 }  // namespace mixrt
