@@ -449,13 +449,6 @@ class DeviceMesh:
 
 # --- arrays of the refiner's operators ---------------------------------------------
 
-def _current_stream(device: int) -> int:
-    """The handle of torch's current stream on a device."""
-    import torch
-    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)   # 0.1 us; the public way 1 us
-    return raw(device) if raw else torch.cuda.current_stream(device).cuda_stream
-
-
 _CODES = {}     # torch dtype -> mixrt_dtype, and the types of kept arrays; filled at first use
 
 
@@ -638,7 +631,11 @@ class Renderer:
         if rc != MIXRT_OK:
             raise MixrtError(rc, self._L.mixrt_thread_error().decode())
         self._h = h
-        self._dev, self._raw_stream = torch.device("cuda", device), int(stream.cuda_stream)
+        self._torch, self._dev = torch, torch.device("cuda", device)
+        self._raw_stream = int(stream.cuda_stream)
+        # the handle of torch's current stream (0.1 us; the public way takes 1)
+        self._current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+            lambda d: torch.cuda.current_stream(d).cuda_stream)
         # the refiner's operators' scratch: (address, bytes), and its memory
         self._ws, self._ws_memory = None, []
 
@@ -803,25 +800,18 @@ class Renderer:
             plans[key] = plan
         return plan
 
-    def _own_stream(self) -> bool:
-        """Whether torch's current stream is this context's: what is allocated
-        then is released to the same stream."""
-        return _current_stream(self.device) == self._raw_stream
-
     def _empty(self, shape, dtype):
         """Device memory for an output.  Taken on this context's stream, so
         that memory released to another stream is not handed out early."""
-        import torch
-        if self._own_stream():
-            return torch.empty(shape, dtype=dtype, device=self._dev)
-        with torch.cuda.stream(self.stream):
-            return torch.empty(shape, dtype=dtype, device=self._dev)
+        if self._current_stream(self.device) == self._raw_stream:
+            return self._torch.empty(shape, dtype=dtype, device=self._dev)
+        with self._torch.cuda.stream(self.stream):
+            return self._torch.empty(shape, dtype=dtype, device=self._dev)
 
     def _empty_like(self, t):
         """_empty of t's shape and type, dense."""
-        if t.is_contiguous() and self._own_stream():
-            import torch
-            return torch.empty_like(t)
+        if t.is_contiguous() and self._current_stream(self.device) == self._raw_stream:
+            return self._torch.empty_like(t)
         return self._empty(t.shape, t.dtype)
 
     def _workspace(self, size: int):
@@ -831,16 +821,14 @@ class Renderer:
         may still write there; sizes at least double, so that all of them
         together take less than twice the last."""
         if self._ws is None or self._ws[1] < size:
-            import torch
             last = self._ws[1] if self._ws else 1 << 15
-            self._ws_memory.append(self._empty((max(size, 2 * last),), torch.uint8))
+            self._ws_memory.append(self._empty((max(size, 2 * last),), self._torch.uint8))
             self._ws = (self._ws_memory[-1].data_ptr(), self._ws_memory[-1].numel())
         return self._ws
 
     def _checkpoint(self, rows: int, channels: int, dtype) -> Checkpoint:
-        import torch
-        return Checkpoint(self._empty((rows, channels), torch.int8),
-                          self._empty((rows, -(-channels // KEPT_GROUP)), torch.uint8), dtype)
+        return Checkpoint(self._empty((rows, channels), self._torch.int8),
+                          self._empty((rows, -(-channels // KEPT_GROUP)), self._torch.uint8), dtype)
 
     def _size(self, fn, *args) -> int:
         size = C.c_size_t()
@@ -904,9 +892,8 @@ class Renderer:
         """(y, stats, kept) for a training step: y as group_norm gives it, the
         groups' (mean, 1 / deviation) as float32 [images, groups, 2], and x
         kept in 8 bits, which the same passes over x write."""
-        import torch
         p = self._norm(x, groups, eps, act, "x")
-        stats = self._empty(p.stats, torch.float32)
+        stats = self._empty(p.stats, self._torch.float32)
         kept = self._checkpoint(p.rows, p.channels, x.dtype)
         return (self._norm_forward(p, x, gamma, beta, out, stats.data_ptr(), kept), stats, kept)
 
@@ -915,11 +902,10 @@ class Renderer:
         """(dx, dgamma, dbeta) of group_norm_train at dy; saved: its kept form
         of x, or x itself.  dgamma, dbeta: float32 [channels].  out: where dx
         goes (dy itself will do)."""
-        import torch
-        if not isinstance(stats, torch.Tensor) or stats.dim() != 3:
+        if not isinstance(stats, self._torch.Tensor) or stats.dim() != 3:
             raise ValueError("stats: expected a torch.Tensor [images, groups, 2]")
         p = self._norm(dy, stats.shape[1], 0.0, act, "dy")
-        _like(stats, "stats", p.stats, torch.float32, self.device)
+        _like(stats, "stats", p.stats, self._torch.float32, self.device)
         if not stats.is_contiguous():
             raise ValueError("stats: not contiguous")
         xd = kd = None
@@ -931,7 +917,7 @@ class Renderer:
         p.norm.gamma = _per_channel(gamma, "gamma", p.channels, self.device)
         p.norm.beta = _per_channel(beta, "beta", p.channels, self.device)
         out, out_ref = self._norm_out(p, dy, out, "out")
-        grads = self._empty((2, p.channels), torch.float32)
+        grads = self._empty((2, p.channels), self._torch.float32)
         at = grads.data_ptr()
         ws, size = self._workspace(p.bytes)
         self._check(self._L.mixrt_norm_backward(self._h, p.norm_ref, p.x_ref, xd, kd,
@@ -968,7 +954,6 @@ class Renderer:
         """(dw, db) of a linear layer y = x w + b over rows, from its kept
         input and dy [..., outs]: float32 [channels, outs] and [outs] (None
         without bias)."""
-        import torch
         kd = kept.descriptor(self.device)
         _on_gpu(dy, "dy", self.device)
         if dy.dtype != kept.dtype:
@@ -980,8 +965,8 @@ class Renderer:
         need = self._plan(("linear", kd.rows, kd.channels, kd.dtype, outs),
                           lambda: self._size(self._L.mixrt_linear_grad_workspace, ref, outs))
         ws, size = self._workspace(need)
-        dw = self._empty((kd.channels, outs), torch.float32)
-        db = self._empty((outs,), torch.float32) if bias else None
+        dw = self._empty((kd.channels, outs), self._torch.float32)
+        db = self._empty((outs,), self._torch.float32) if bias else None
         self._check(self._L.mixrt_linear_grad(self._h, ref, outs, dy.data_ptr(), stride,
                                               dw.data_ptr(), _ptr(db), ws, size))
         return dw, db
@@ -995,11 +980,10 @@ class Renderer:
         layout: "halves" pairs element j with j + pairs, "pairs" 2 j with
         2 j + 1.  inverse: the other way round (the gradient's map).  out:
         tensors to write, each may be its input."""
-        import torch
-        single = isinstance(heads, torch.Tensor)
+        single = isinstance(heads, self._torch.Tensor)
         arrays = (heads,) if single else tuple(heads)
-        for t, name, dt in ((pos, "pos", torch.float32), (freq, "freq", torch.float32),
-                            (axis, "axis", torch.uint8)):
+        for t, name, dt in ((pos, "pos", self._torch.float32), (freq, "freq", self._torch.float32),
+                            (axis, "axis", self._torch.uint8)):
             _on_gpu(t, name, self.device)
             if t.dtype != dt or not t.is_contiguous():
                 raise ValueError(f"{name}: {t.dtype}, expected contiguous {dt}")
