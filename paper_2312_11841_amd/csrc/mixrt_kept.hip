@@ -146,7 +146,10 @@ struct LinearK {
     int64_t whole;    // rows whose vectors stay inside the arrays
     int C, outs, per_row;
     int ty, tz;       // tiles of dw along its channels and its outs
-    float *sums;      // [parts][C * outs + outs]
+    // where a part's sums go: parts of C * outs weights and outs column sums,
+    // or, of one part, dw and db (which may be null)
+    float *sums, *bias;
+    int64_t stride;
 };
 
 // A lane's share of a step as it is in memory: 4 channels (a word) and 4 outs
@@ -430,15 +433,15 @@ __global__ __launch_bounds__(kThreads) void linear_grad_kernel(LinearK k)
         }
         __syncthreads();
     }
-    float *out = k.sums + (int64_t)part * ((int64_t)k.C * k.outs + k.outs);
+    float *const out = k.sums + (int64_t)part * k.stride;
     const int o = threadIdx.x & 63, og = tz * kTile + o;
     if (og < k.outs) {
         for (int i = threadIdx.x >> 6; i < kTile; i += 4) {
             const int cg = ty * kTile + i;
             if (cg < k.C) out[(int64_t)cg * k.outs + og] = sh[i * kTile + o];
         }
-        if (biased && threadIdx.x < 64)
-            out[(int64_t)k.C * k.outs + og] = sh[kTile * kTile + o];
+        if (biased && k.bias && threadIdx.x < 64)
+            k.bias[(int64_t)part * k.stride + og] = sh[kTile * kTile + o];
     }
 }
 
@@ -496,19 +499,20 @@ __global__ __launch_bounds__(THREADS) void linear_join_kernel(const float *sums,
     }
 }
 
-constexpr int kResident = 512;   // blocks of linear_grad_kernel on the card at once
+constexpr int kCus = 256;
 
 struct LinearPlan {
     int parts, ty, tz;
     int64_t part;
 };
 
-// How many parts the rows are split into: enough to fill the card, in whole
-// rounds of the blocks it holds at once (2 a CU by their registers), and not
-// so many that adding their sums costs more.  In units of a step of a full
-// card, about 1 us: a block takes its steps and about 3 for its start and end;
-// writing and reading a part of n sums takes n / 500,000.  (3600 rows, 512 x
-// 1536, f16: see below.)
+// How many parts the rows are split into.  The time is estimated in steps of a
+// block, about 1.2 us while a CU holds two blocks (as many as their registers
+// allow) and 0.6 of that while it holds one; a block takes about 3 more for its
+// start and its end, a join about 5, and writing and reading n sums n / 500,000.
+// One part needs no join.  (720p rows, 64 x 64: 256 parts 40.6 us, 512 41.2, 128
+// 50.8; 3600 rows, 512 x 1536, f16: one part 21.6, two with their join 24.2,
+// five 29.6; 100,000 rows, 512 x 512: 8 parts 121, 4 143, 16 140.)
 LinearPlan linear_plan(int64_t rows, int C, int outs)
 {
     LinearPlan p;
@@ -519,14 +523,15 @@ LinearPlan linear_plan(int64_t rows, int C, int outs)
     const double sums = ((double)C * outs + outs) / 500000.0;
     int64_t best = 1;
     double least = 0.0;
-    for (int rounds = 1; rounds <= 8; ++rounds) {
-        int64_t parts = (int64_t)rounds * kResident / tiles;
+    for (int filled = 0; filled <= 16; ++filled) {   // blocks a CU; 0: one part
+        int64_t parts = (int64_t)filled * kCus / tiles;
         if (parts > steps) parts = steps;
         if (parts < 1) parts = 1;
         const int64_t each = (steps + parts - 1) / parts;
-        const int64_t need = (parts * tiles + kResident - 1) / kResident;
-        const double cost = (double)need * (double)(each + 3) + sums * (double)parts;
-        if (rounds == 1 || cost < least) {
+        const int64_t turns = (parts * tiles + 2 * kCus - 1) / (2 * kCus);
+        const double load = parts * tiles <= kCus ? 0.6 : (double)turns;
+        const double cost = load * (double)(each + 3) + (parts > 1 ? 5.0 + sums * (double)parts : 0.0);
+        if (filled == 0 || cost < least) {
             least = cost;
             best = parts;
         }
@@ -614,7 +619,7 @@ hipError_t launch_kept_unpack(int out_dtype, int64_t rows, int C, const int8_t *
 size_t linear_grad_workspace(int64_t rows, int C, int outs, int)
 {
     const LinearPlan p = linear_plan(rows, C, outs);
-    return (size_t)p.parts * ((size_t)C * outs + outs) * sizeof(float);
+    return p.parts > 1 ? (size_t)p.parts * ((size_t)C * outs + outs) * sizeof(float) : 0;
 }
 
 hipError_t launch_linear_grad(int dtype, int64_t rows, int C, int outs, const int8_t *codes,
@@ -628,10 +633,12 @@ hipError_t launch_linear_grad(int dtype, int64_t rows, int C, int outs, const in
     if (C % 4 || outs % 4) whole = rows - 3;
     if (outs % 4 && dy_stride < outs) whole = 0;
     if (dy_stride >= (1 << 24)) whole = 0;   // the lanes' offsets are 32 bits
-    LinearK k{codes,          exps, dy,   rows,    dy_stride,  p.part, whole, C, outs,
-              kept_groups(C), p.ty, p.tz, (float *)ws};
-    const int grid = p.parts * p.ty * p.tz;
     const int64_t weights = (int64_t)C * outs, n = weights + outs;
+    float *const sums = (float *)ws;
+    const bool one = p.parts == 1;
+    const LinearK k{codes, exps, dy, rows, dy_stride, p.part, whole, C, outs, kept_groups(C),
+                    p.ty,  p.tz, one ? dw : sums, one ? db : sums + weights, n};
+    const int grid = p.parts * p.ty * p.tz;
     const bool tiny = rows * C < 4 || (rows - 1) * dy_stride + outs < 4;
     with_type(dtype, [&](auto *t) {
         typedef std::remove_pointer_t<decltype(t)> T;
@@ -643,13 +650,13 @@ hipError_t launch_linear_grad(int dtype, int64_t rows, int C, int outs, const in
     // many parts of few weights: 32 threads a value (4160 values of 506 parts
     // 4.7 us, against 120 with one); few parts: one (788,000 values of 2 parts
     // 53 us with 32)
-    if (tiny)
+    if (tiny || one)
         ;
     else if (p.parts > 8)
-        linear_join_kernel<32, 1024><<<blocks(n, 32), 1024, 0, stream>>>(k.sums, n, weights,
+        linear_join_kernel<32, 1024><<<blocks(n, 32), 1024, 0, stream>>>(sums, n, weights,
                                                                          p.parts, dw, db);
     else
-        linear_join_kernel<1, 256><<<blocks(n, 256), 256, 0, stream>>>(k.sums, n, weights, p.parts,
+        linear_join_kernel<1, 256><<<blocks(n, 256), 256, 0, stream>>>(sums, n, weights, p.parts,
                                                                        dw, db);
     return hipGetLastError();
 }
