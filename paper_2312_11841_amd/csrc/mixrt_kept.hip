@@ -115,6 +115,13 @@ __global__ __launch_bounds__(kThreads) void kept_unpack_kernel(const int8_t *cod
 // holds a 64 x 64 block of dw (16 tiles); the rows are split over blocks and
 // over the 4 waves of a block, which add theirs in LDS; a second kernel adds
 // the blocks' sums in a fixed order.
+//
+// What bounds it: few weights, the stream of codes and dy (720p rows, 64 x 64,
+// bf16: 179 MB in 36 us of kernel, 5.0 TB/s); many weights, the vector memory
+// path through which every tile's rows go again, busy 80% of the time (100,000
+// rows, 512 x 512, bf16: 121 us, 433 TFLOP/s; 3600 rows, 512 x 1536, f16: 21
+// us).  Wide loads turned by way of LDS instead took 110 us and 22, and 250
+// against 210 in f32 (100,000 rows, 320 x 320).
 
 constexpr int kTile = 64;     // channels of a wave's block of dw, each way
 constexpr int kRows = 32;     // rows of a step
@@ -355,7 +362,7 @@ __device__ __forceinline__ void multiply_step(const LinearStep<float> &s, bool b
 template <typename T>
 __global__ __launch_bounds__(kThreads) void linear_grad_kernel(LinearK k)
 {
-    __shared__ float sh[kTile * kTile + kTile];
+    __shared__ __align__(16) float sh[2][kTile * kTile + kTile];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x & 63;
     const int q = lane >> 4, c = lane & 15;
     // Blocks are dealt to the 8 XCDs in turn.  Each XCD takes a run of a part's
@@ -411,25 +418,27 @@ __global__ __launch_bounds__(kThreads) void linear_grad_kernel(LinearK k)
         load_last(s, r0 + 8 * q, r1, ci, co, k);
         multiply_step(s, biased, acc, bias);
     }
-    // the waves add in turn: a tile's row m (channel 4 m + i) is in quarter
-    // m / 4, register m % 4, its column n (out 4 n + j) in lane n
-    for (int w = 0; w < 4; ++w) {
-        if (wave == w) {
+    // Two waves store their sums, the other two add theirs, and the halves are
+    // added on the way out.  A tile's row m (channel 4 m + i) is in quarter
+    // m / 4, register m % 4, its column n (outs 4 n + j) in lane n: a lane's four
+    // neighbours go at once (one at a time, and the waves one after another,
+    // 0.5 to 0.8 us more a call).
+    for (int w = 0; w < 4; w += 2) {
+        if ((wave & 2) == w) {
+            float *const mine = sh[wave & 1];
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        float *p = &sh[(4 * (4 * q + e) + i) * kTile + 4 * c + j];
-                        *p = w == 0 ? acc[i][j][e] : *p + acc[i][j][e];
-                    }
-            if (q == 0)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    float *p = &sh[kTile * kTile + 4 * c + j];
-                    *p = w == 0 ? bias[j][0] : *p + bias[j][0];
+                for (int e = 0; e < 4; ++e) {
+                    f4 *const p = (f4 *)&mine[(4 * (4 * q + e) + i) * kTile + 4 * c];
+                    const f4 v = {acc[i][0][e], acc[i][1][e], acc[i][2][e], acc[i][3][e]};
+                    *p = w == 0 ? v : *p + v;
                 }
+            if (q == 0) {
+                f4 *const p = (f4 *)&mine[kTile * kTile + 4 * c];
+                const f4 v = {bias[0][0], bias[1][0], bias[2][0], bias[3][0]};
+                *p = w == 0 ? v : *p + v;
+            }
         }
         __syncthreads();
     }
@@ -438,10 +447,11 @@ __global__ __launch_bounds__(kThreads) void linear_grad_kernel(LinearK k)
     if (og < k.outs) {
         for (int i = threadIdx.x >> 6; i < kTile; i += 4) {
             const int cg = ty * kTile + i;
-            if (cg < k.C) out[(int64_t)cg * k.outs + og] = sh[i * kTile + o];
+            if (cg < k.C) out[(int64_t)cg * k.outs + og] = sh[0][i * kTile + o] + sh[1][i * kTile + o];
         }
         if (biased && k.bias && threadIdx.x < 64)
-            k.bias[(int64_t)part * k.stride + og] = sh[kTile * kTile + o];
+            k.bias[(int64_t)part * k.stride + og] =
+                sh[0][kTile * kTile + o] + sh[1][kTile * kTile + o];
     }
 }
 
