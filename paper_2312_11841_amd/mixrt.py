@@ -540,7 +540,13 @@ class _Plan:
     """What a call's descriptors hold besides addresses; see Renderer._plan."""
 
 
-def _rotary_plan(arrays, outs, pos, freq, axis, layout, inverse):
+def _rotary_plan(arrays, outs, pos, freq, axis, layout, inverse, device):
+    import torch
+    for t, name, dt in ((pos, "pos", torch.float32), (freq, "freq", torch.float32),
+                        (axis, "axis", torch.uint8)):
+        _on_gpu(t, name, device)
+        if t.dtype != dt or not t.is_contiguous():
+            raise ValueError(f"{name}: {t.dtype}, expected contiguous {dt}")
     if not 1 <= len(arrays) <= 2:
         raise ValueError(f"{len(arrays)} arrays of heads, expected 1 or 2")
     if layout not in ROTARY_LAYOUTS:
@@ -556,6 +562,7 @@ def _rotary_plan(arrays, outs, pos, freq, axis, layout, inverse):
     p.heads = (Heads * len(arrays))()
     for i, (x, o) in enumerate(zip(arrays, outs)):
         name = f"heads[{i}]"
+        _on_gpu(x, name, device)
         if x.dim() < 2:
             raise ValueError(f"{name}: {x.dim()} dimensions, expected [..., heads, D]")
         ends = []
@@ -804,6 +811,9 @@ class Renderer:
         """Device memory for an output.  Taken on this context's stream, so
         that memory released to another stream is not handed out early."""
         if self._current_stream(self.device) == self._raw_stream:
+            if len(shape) == 2:     # a third less than empty
+                return self._torch.empty_strided(shape, (shape[1], 1), dtype=dtype,
+                                                 device=self._dev)
             return self._torch.empty(shape, dtype=dtype, device=self._dev)
         with self._torch.cuda.stream(self.stream):
             return self._torch.empty(shape, dtype=dtype, device=self._dev)
@@ -929,11 +939,18 @@ class Renderer:
     def checkpoint_pack(self, x) -> Checkpoint:
         """x [..., channels] kept in 8 bits."""
         _on_gpu(x, "x", self.device)
-        rows, channels, stride = _as_rows(x, "x")
-        _elem_code(x.dtype, "x")
-        kept = self._checkpoint(rows, channels, x.dtype)
-        kd = kept.descriptor(self.device)
-        self._check(self._L.mixrt_kept_pack(self._h, C.byref(kd), x.data_ptr(), stride))
+
+        def make():
+            p = _Plan()
+            p.rows, p.channels, p.stride = _as_rows(x, "x")
+            p.kept = Kept(p.rows, p.channels, _elem_code(x.dtype, "x"), 0, 0)
+            p.kept_ref = C.byref(p.kept)
+            return p
+
+        p = self._plan(("pack", x.shape, x.stride(), x.dtype), make)
+        kept = self._checkpoint(p.rows, p.channels, x.dtype)
+        p.kept.codes, p.kept.exps = kept.codes.data_ptr(), kept.exps.data_ptr()
+        self._check(self._L.mixrt_kept_pack(self._h, p.kept_ref, x.data_ptr(), p.stride))
         return kept
 
     def checkpoint_unpack(self, kept: Checkpoint, dtype=None, out=None):
@@ -982,26 +999,27 @@ class Renderer:
         tensors to write, each may be its input."""
         single = isinstance(heads, self._torch.Tensor)
         arrays = (heads,) if single else tuple(heads)
-        for t, name, dt in ((pos, "pos", self._torch.float32), (freq, "freq", self._torch.float32),
-                            (axis, "axis", self._torch.uint8)):
-            _on_gpu(t, name, self.device)
-            if t.dtype != dt or not t.is_contiguous():
-                raise ValueError(f"{name}: {t.dtype}, expected contiguous {dt}")
-        for x in arrays:
-            _on_gpu(x, "heads", self.device)
+        # all that the checks look at is in the key, so they run once for each
+        try:
+            key = ("rotary", layout, inverse,
+                   pos.shape, pos.stride(), pos.dtype, pos.get_device(),
+                   freq.shape, freq.stride(), freq.dtype, freq.get_device(),
+                   axis.shape, axis.stride(), axis.dtype, axis.get_device())
+            for x in arrays:
+                key += (x.shape, x.stride(), x.dtype, x.get_device())
+        except AttributeError:
+            raise TypeError("heads, pos, freq and axis: expected torch.Tensors") from None
         if out is None:
             outs = tuple([self._empty_like(x) for x in arrays])
-            ends = None
         else:
             outs = (out,) if single else tuple(out)
             if len(outs) != len(arrays):
                 raise ValueError(f"{len(arrays)} arrays and {len(outs)} outputs")
             for i, (x, o) in enumerate(zip(arrays, outs)):
                 _like(o, f"out[{i}]", x.shape, x.dtype, self.device)
-            ends = tuple(o.stride() for o in outs)
-        key = ("rotary", pos.shape, freq.shape, axis.shape, layout, bool(inverse), ends,
-               *((x.shape, x.stride(), x.dtype) for x in arrays))
-        p = self._plan(key, lambda: _rotary_plan(arrays, outs, pos, freq, axis, layout, inverse))
+                key += (o.stride(),)
+        p = self._plan(key, lambda: _rotary_plan(arrays, outs, pos, freq, axis, layout, inverse,
+                                                 self.device))
         p.rotary.pos, p.rotary.freq = pos.data_ptr(), freq.data_ptr()
         p.rotary.axis = axis.data_ptr()
         for d, x, o in zip(p.heads, arrays, outs):
