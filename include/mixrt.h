@@ -436,9 +436,9 @@ int mixrt_rasterize(mixrt_ctx *ctx, const mixrt_mesh *mesh, int32_t views, int32
  * the *_workspace function (pure host) states, 16-byte aligned, with any
  * contents; it must not be shared by calls that run at the same time.  An
  * output overlaps no input and no other output, but where a field says that
- * it may be an input.  Empty arrays (no image, pixel, row or token) are valid.  Sums and statistics are
- * held in 32 bits or more; a result is rounded once to its type, to nearest
- * even. */
+ * it may be an input.  Empty arrays (no image, pixel, row or token) are valid.
+ * Sums and statistics are held in 32 bits or more; a result is rounded once to
+ * its type, to nearest even. */
 
 /* Activations. */
 enum mixrt_act {

@@ -1,4 +1,5 @@
-"""MI355X (gfx950) implementation of MixRT's per-pixel rendering path.
+"""MI355X (gfx950) implementation of MixRT's per-pixel rendering path, and of
+the operators of a network that refines the rendered views.
 
 - `mixrt`: ctypes binding of libmixrt.so (the C ABI of include/mixrt.h).
 - `synth`: seeded synthetic inputs shaped like the paper's workloads.

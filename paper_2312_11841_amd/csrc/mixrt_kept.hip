@@ -14,7 +14,8 @@ constexpr int kThreads = 256;
 // need), groups in the order of the scale bytes.  A block takes kPackSteps
 // steps of its threads and ends; larger runs and loads ahead were slower (64
 // channels of a 720p frame in bf16, both ways: 65 us at 4 steps, 66 at 8, 73 at
-// 16, 81 with 8 loads ahead; the copy's rate for its 358 MB makes 62).
+// 16, 81 with 8 loads ahead; the copy's rate for its 358 MB makes 62).  Now 60:
+// packing 33 us of kernel (5.4 TB/s), reading back 27 (6.5).
 constexpr int kPackSteps = 4;
 constexpr int64_t kMostBlocks = 1 << 20;   // then blocks take further runs
 
@@ -120,8 +121,8 @@ __global__ __launch_bounds__(kThreads) void kept_unpack_kernel(const int8_t *cod
 // bf16: 179 MB in 36 us of kernel, 5.0 TB/s); many weights, the vector memory
 // path through which every tile's rows go again, busy 80% of the time (100,000
 // rows, 512 x 512, bf16: 121 us, 433 TFLOP/s; 3600 rows, 512 x 1536, f16: 21
-// us).  Wide loads turned by way of LDS instead took 110 us and 22, and 250
-// against 210 in f32 (100,000 rows, 320 x 320).
+// us).  Wide loads turned by way of LDS instead took 110 us of the first, no
+// less of the second, and 250 against 210 us in f32 (100,000 rows, 320 x 320).
 
 constexpr int kTile = 64;     // channels of a wave's block of dw, each way
 constexpr int kRows = 32;     // rows of a step

@@ -51,7 +51,9 @@ __device__ __forceinline__ void write_row(T *y, const Channels<V> &c, const Pack
     store_vec<T, V>(y, f);
 }
 
-// Sums per group over one part of an image.  A: sums of x (and of x^2) that a
+// Sums per group over one part of an image.  Bound by the stream of x: 8 x 1080p
+// x 16 channels in f16, 531 MB in 123 us (4.3 TB/s); with 512 to 4096 blocks the
+// call differs by 1%, and with two or eight rows ahead by 1 and 5%.  A: sums of x (and of x^2) that a
 // thread holds.  KEEP: x is also written in its 8-bit form.
 template <typename T, int V, int A, bool KEEP>
 __global__ __launch_bounds__(kThreads) void norm_sums_kernel(NormK k)
@@ -145,7 +147,8 @@ __global__ __launch_bounds__(kJoinThreads) void norm_stats_kernel(NormK k)
     });
 }
 
-// The normalised and activated rows.  FOLD: the block joins the image's few
+// The normalised and activated rows, a stream of x and y (8 x 1080p x 16 in f16,
+// 1062 MB in 166 us, 6.4 TB/s).  FOLD: the block joins the image's few
 // parts itself (and the first one stores what it got).
 template <typename T, int V, int ACT, bool FOLD>
 __global__ __launch_bounds__(kThreads) void norm_apply_kernel(NormK k)
@@ -181,7 +184,9 @@ __global__ __launch_bounds__(kThreads) void norm_apply_kernel(NormK k)
 // whole kept groups where x is kept) of one image, lanes over its vectors, R
 // rows at a time.  It sums up all rows, then writes (and keeps) every
 // gridDim.z-th R rows.  A vector lies in one group.  In place (y is x) a block
-// would sum up what another has written: then one block does it all.
+// would sum up what another has written: then one block does it all.  Bound by
+// the launch and one chain of loads, joins and stores (64 x 64 x 16 in f32, 6.2
+// us of kernel; in two launches 9.3 a call against 7.1).
 template <typename T, int V, int ACT, bool KEEP>
 __global__ __launch_bounds__(kSmallThreads) void norm_small_kernel(NormK k, int chunk)
 {

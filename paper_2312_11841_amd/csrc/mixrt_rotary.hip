@@ -3,7 +3,12 @@
 // A block takes a run of tokens (and, where there are few, a run of heads):
 // first its threads work out the cosines and sines of its tokens' pairs into
 // LDS, once for all heads and both arrays, then they walk over the heads'
-// elements in memory order.
+// elements in memory order.  The sines are sincosf's, of the angle as rounded to
+// 32 bits; the turn is in 32 bits and rounded once.
+//
+// What bounds it: the stream of the heads (65,280 tokens, 16 heads of 64 and as
+// many keys, bf16: 535 MB in 93 us, 5.7 TB/s); with few tokens the launch (one
+// token, 4 us of kernel).
 #include "mixrt_refine.hpp"
 
 #include <type_traits>

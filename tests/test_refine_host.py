@@ -145,3 +145,18 @@ def test_norm_statement_against_autograd():
                                gamma.detach(), beta.detach(), kind, torch.float32)
         for a, b in zip(grads, (got["dx"], got["dgamma"], got["dbeta"])):
             assert torch.allclose(a, b, atol=1e-11)
+
+
+@pytest.mark.parametrize("source", ["mixrt_norm", "mixrt_norm_back", "mixrt_kept",
+                                    "mixrt_rotary"])
+def test_kernels_use_no_scratch(source):
+    """No register spills, and no scratch memory that the HIP runtime would
+    allocate at a kernel's first launch (which a captured call could not)."""
+    from paper_2312_11841_amd import build
+    from test_abi_host import _kernel_private_segments
+    obj = os.path.join(build.OBJ_DIR, source + ".o")
+    if not os.path.exists(obj):
+        pytest.skip("library objects not built")
+    sizes = _kernel_private_segments(obj)
+    assert sizes, source
+    assert {k: v for k, v in sizes.items() if v} == {}
