@@ -456,6 +456,120 @@ __global__ __launch_bounds__(kThreads) void linear_grad_kernel(LinearK k)
     }
 }
 
+// Few channels and outs on one side (a frame has 4) and not many on the other:
+// a tile of 64 would be mostly empty.  L neighbouring lanes take a row, each CT
+// of its channels and OT of its outs, and keep the CT * OT = 64 sums themselves
+// (921,600 rows in 16 bits, us a call, by tiles and so: 16 channels, 4 outs 24.4,
+// 13.3; 32 and 4 23.9, 16.4; 15 and 3 29.6, 14.7; 4 and 32 23.3, 20.4).  Bound by
+// the vector memory path, as a lane's rows lie apart; rows in flight hide the
+// rest.
+constexpr int kFew = 4, kMany = 16;   // a lane's channels and outs, either way
+constexpr int kNarrowLanes = 4;       // most lanes of a row
+constexpr int kNarrowAhead = 4;       // rows a lane loads before it uses the first
+
+template <int CT, int OT, typename T>
+struct NarrowRow {
+    Pack<int8_t, CT> code;
+    uint8_t byte;
+    Pack<T, OT> dy;
+};
+
+template <typename T, int CT, int OT, int L>
+__global__ __launch_bounds__(kThreads) void linear_narrow_kernel(LinearK k)
+{
+    static_assert(CT * OT == 64 && kKeptGroup % CT == 0, "a sum for each lane, one kept group");
+    constexpr int kDown = kThreads / L;   // rows of a step
+    __shared__ float sh[kThreads / 64][L][64 + OT];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x / 64, l = lane % L;
+    // lanes past the channels or the outs take the row's start: what they
+    // compute is not stored
+    const bool in = CT > OT ? l * CT < k.C : l * OT < k.outs;
+    const int c0 = in && CT > OT ? l * CT : 0, o0 = in && OT > CT ? l * OT : 0;
+    float acc[64], bias[OT];
+#pragma unroll
+    for (int i = 0; i < 64; ++i) acc[i] = 0.0f;
+#pragma unroll
+    for (int j = 0; j < OT; ++j) bias[j] = 0.0f;
+    const int64_t first = blockIdx.x * k.part, r1 = min(first + k.part, k.rows);
+    // vectors that pass a row's end take elements of the next rows, which only
+    // meet sums that are not stored; near the arrays' end, element by element
+    const auto load = [&](int64_t r, bool vectors) {
+        NarrowRow<CT, OT, T> d;
+        const int8_t *x = k.codes + r * k.C + c0;
+        const T *dy = (const T *)k.dy + r * k.dy_stride + o0;
+        d.byte = k.exps[r * k.per_row + c0 / kKeptGroup];
+        if (vectors) {
+            d.code = *(const Pack<int8_t, CT> *)x;
+            d.dy = *(const Pack<T, OT> *)dy;
+        } else {
+#pragma unroll
+            for (int i = 0; i < CT; ++i) d.code.v[i] = c0 + i < k.C ? x[i] : (int8_t)0;
+#pragma unroll
+            for (int j = 0; j < OT; ++j) d.dy.v[j] = o0 + j < k.outs ? dy[j] : (T)0.0f;
+        }
+        return d;
+    };
+    const auto add = [&](const NarrowRow<CT, OT, T> &d) {
+        const float scale = kept_scale(d.byte);
+        float y[OT];
+#pragma unroll
+        for (int j = 0; j < OT; ++j) {
+            y[j] = (float)d.dy.v[j];
+            bias[j] += y[j];
+        }
+#pragma unroll
+        for (int i = 0; i < CT; ++i) {
+            const float x = (float)d.code.v[i] * scale;
+#pragma unroll
+            for (int j = 0; j < OT; ++j) acc[i * OT + j] = fmaf(x, y[j], acc[i * OT + j]);
+        }
+    };
+    int64_t r = first + threadIdx.x / L;
+    const int64_t whole = min(r1, k.whole);
+    for (; r + (kNarrowAhead - 1) * kDown < whole; r += kNarrowAhead * kDown) {
+        NarrowRow<CT, OT, T> d[kNarrowAhead];
+#pragma unroll
+        for (int u = 0; u < kNarrowAhead; ++u) d[u] = load(r + u * kDown, true);
+        __builtin_amdgcn_sched_barrier(0);   // else the loads sink to their uses
+#pragma unroll
+        for (int u = 0; u < kNarrowAhead; ++u) add(d[u]);
+    }
+    for (; r < r1; r += kDown) add(load(r, r < whole));
+    // the sums over a wave's lanes: each step halves the sums that a lane still
+    // holds; it ends with L of them, from (lane rounded down to L) on
+#pragma unroll
+    for (int d = 32; d >= L; d >>= 1)
+#pragma unroll
+        for (int i = 0; i < d; ++i) {
+            const bool up = (lane & d) != 0;
+            const float keep = up ? acc[i + d] : acc[i], send = up ? acc[i] : acc[i + d];
+            acc[i] = keep + __shfl_xor(send, d);
+        }
+#pragma unroll
+    for (int a = 0; a < L; ++a) sh[wave][l][lane - l + a] = acc[a];
+#pragma unroll
+    for (int j = 0; j < OT; ++j) {
+#pragma unroll
+        for (int d = 32; d >= L; d >>= 1) bias[j] += __shfl_xor(bias[j], d);
+        if (lane < L) sh[wave][l][64 + j] = bias[j];
+    }
+    __syncthreads();
+    float *const out = k.sums + (int64_t)blockIdx.x * k.stride;
+    for (int t = threadIdx.x; t < L * (64 + OT); t += kThreads) {
+        const int at = t / (64 + OT), e = t - at * (64 + OT);
+        float v = 0.0f;
+        for (int w = 0; w < kThreads / 64; ++w) v += sh[w][at][e];
+        const int o = (OT > CT ? at * OT : 0) + (e < 64 ? e % OT : e - 64);
+        const int c = (CT > OT ? at * CT : 0) + e / OT;
+        if (o >= k.outs) continue;
+        if (e < 64) {
+            if (c < k.C) out[(int64_t)c * k.outs + o] = v;
+        } else if (k.bias && (OT > CT || at == 0)) {
+            k.bias[(int64_t)blockIdx.x * k.stride + o] = v;
+        }
+    }
+}
+
 // Arrays shorter than a vector: a thread's sum for each weight.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void linear_tiny_kernel(LinearK k, float *dw, float *db)
@@ -512,21 +626,40 @@ __global__ __launch_bounds__(THREADS) void linear_join_kernel(const float *sums,
 
 constexpr int kCus = 256;
 
+constexpr int kNarrowBlocks = 512;
+
 struct LinearPlan {
     int parts, ty, tz;
     int64_t part;
+    int narrow;   // lanes of a row, 0: tiles of 64
 };
 
 // How many parts the rows are split into.  The time is estimated in steps of a
 // block, about 1.2 us while a CU holds two blocks (as many as their registers
 // allow) and 0.6 of that while it holds one; a block takes about 3 more for its
 // start and its end, a join about 5, and writing and reading n sums n / 500,000.
-// One part needs no join.  (720p rows, 64 x 64: 256 parts 40.6 us, 512 41.2, 128
+// One part needs no join.  Narrow layers: two runs of loads a lane, and 2 blocks a
+// CU at most (2,000,000 rows of one: 21 us, 31 with 1, 26 with 3).  (720p rows, 64 x 64: 256 parts 40.6 us, 512 41.2, 128
 // 50.8; 3600 rows, 512 x 1536, f16: one part 21.6, two with their join 24.2,
 // five 29.6; 100,000 rows, 512 x 512: 8 parts 121, 4 143, 16 140.)
-LinearPlan linear_plan(int64_t rows, int C, int outs)
+LinearPlan linear_plan(int64_t rows, int C, int outs, int dtype)
 {
     LinearPlan p;
+    p.narrow = 0;
+    // (64 channels, 4 outs: 27.8 us in f16 where tiles take 24.6; in f32 tiles of
+    // 4 x 48 take 92 and this 40)
+    const int few = C < outs ? C : outs, many = C < outs ? outs : C;
+    if (few <= kFew && many <= kMany * kNarrowLanes && (C <= 3 * kMany || dtype == kF32)) {
+        p.narrow = many <= kMany ? 1 : many <= 2 * kMany ? 2 : 4;
+        p.ty = p.tz = 1;
+        const int64_t run = (int64_t)kThreads / p.narrow * 2 * kNarrowAhead;
+        int64_t parts = (rows + run - 1) / run;
+        if (parts > kNarrowBlocks) parts = kNarrowBlocks;
+        if (parts < 1) parts = 1;
+        p.part = (rows + parts - 1) / parts;
+        p.parts = (int)parts;
+        return p;
+    }
     p.ty = (C + kTile - 1) / kTile;
     p.tz = (outs + kTile - 1) / kTile;
     const int tiles = p.ty * p.tz;
@@ -627,9 +760,9 @@ hipError_t launch_kept_unpack(int out_dtype, int64_t rows, int C, const int8_t *
     return hipGetLastError();
 }
 
-size_t linear_grad_workspace(int64_t rows, int C, int outs, int)
+size_t linear_grad_workspace(int64_t rows, int C, int outs, int dtype)
 {
-    const LinearPlan p = linear_plan(rows, C, outs);
+    const LinearPlan p = linear_plan(rows, C, outs, dtype);
     return p.parts > 1 ? (size_t)p.parts * ((size_t)C * outs + outs) * sizeof(float) : 0;
 }
 
@@ -637,13 +770,15 @@ hipError_t launch_linear_grad(int dtype, int64_t rows, int C, int outs, const in
                               const uint8_t *exps, const void *dy, int64_t dy_stride, float *dw,
                               float *db, void *ws, hipStream_t stream)
 {
-    const LinearPlan p = linear_plan(rows, C, outs);
-    // A vector of 4 that is not whole in its row goes on into the next rows: at
-    // most 3 of them (rows of one element), and none where rows of dy repeat.
+    const LinearPlan p = linear_plan(rows, C, outs, dtype);
+    // A vector of 4 (16 where a lane takes whole rows) that is not whole in its
+    // row goes on into the next rows: at most 3 (15) of them, rows of one
+    // element, and none where rows of dy repeat.
+    const int vc = p.narrow && outs <= C ? kMany : 4, vo = p.narrow && outs > C ? kMany : 4;
     int64_t whole = rows;
-    if (C % 4 || outs % 4) whole = rows - 3;
-    if (outs % 4 && dy_stride < outs) whole = 0;
-    if (dy_stride >= (1 << 24)) whole = 0;   // the lanes' offsets are 32 bits
+    if (C % vc || outs % vo) whole = rows - (p.narrow ? kMany - 1 : 3);
+    if (outs % vo && dy_stride < outs) whole = 0;
+    if (!p.narrow && dy_stride >= (1 << 24)) whole = 0;   // the lanes' offsets are 32 bits
     const int64_t weights = (int64_t)C * outs, n = weights + outs;
     float *const sums = (float *)ws;
     const bool one = p.parts == 1;
@@ -653,7 +788,24 @@ hipError_t launch_linear_grad(int dtype, int64_t rows, int C, int outs, const in
     const bool tiny = rows * C < 4 || (rows - 1) * dy_stride + outs < 4;
     with_type(dtype, [&](auto *t) {
         typedef std::remove_pointer_t<decltype(t)> T;
-        if (tiny)
+        auto narrow = [&](auto ct, auto ot, auto l) {
+            constexpr int CT = decltype(ct)::value, OT = decltype(ot)::value;
+            constexpr int L = decltype(l)::value;
+            linear_narrow_kernel<T, CT, OT, L><<<grid, kThreads, 0, stream>>>(k);
+        };
+        auto with_side = [&](auto l) {
+            const std::integral_constant<int, kFew> few;
+            const std::integral_constant<int, kMany> many;
+            if (outs <= C) narrow(many, few, l);
+            else narrow(few, many, l);
+        };
+        if (p.narrow == 1)
+            with_side(std::integral_constant<int, 1>());
+        else if (p.narrow == 2)
+            with_side(std::integral_constant<int, 2>());
+        else if (p.narrow == 4)
+            with_side(std::integral_constant<int, 4>());
+        else if (tiny)
             linear_tiny_kernel<T><<<blocks(n, kThreads), kThreads, 0, stream>>>(k, dw, db);
         else
             linear_grad_kernel<T><<<grid, kThreads, 0, stream>>>(k);

@@ -389,6 +389,19 @@ def test_linear_weight_gradient(r, shape, dtype):
     assert none is None and torch.equal(only, dw)
 
 
+# few channels on one side: rows dealt to lanes, in one part and several, and
+# the widths on both sides of that rule
+NARROW = [(0, 8, 4), (1, 4, 4), (3, 1, 2), (255, 16, 4), (2049, 32, 3), (2048, 5, 4), (9001, 4, 32),
+          (4097, 2, 40), (100001, 24, 4), (3000, 48, 4), (3000, 4, 48), (70000, 4, 4),
+          (8191, 64, 4), (3000, 3, 64), (1, 512, 1), (2, 1, 500), (3000, 65, 4)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("shape", NARROW, ids=str)
+def test_linear_weight_gradient_of_narrow_layers(r, shape, dtype):
+    test_linear_weight_gradient(r, shape, dtype)
+
+
 def test_linear_gradient_of_non_finite_rows(r):
     """A group that was not finite makes its channels' weights NaN, no others."""
     g = _gen(2)
