@@ -122,7 +122,8 @@ __global__ __launch_bounds__(kThreads) void kept_unpack_kernel(const int8_t *cod
 // path through which every tile's rows go again, busy 80% of the time (100,000
 // rows, 512 x 512, bf16: 121 us, 433 TFLOP/s; 3600 rows, 512 x 1536, f16: 21
 // us).  Wide loads turned by way of LDS instead took 110 us of the first, no
-// less of the second, and 250 against 210 us in f32 (100,000 rows, 320 x 320).
+// less of the second, and 250 against 210 us in f32 (100,000 rows, 320 x 320; now
+// 187, 110 TFLOP/s).
 
 constexpr int kTile = 64;     // channels of a wave's block of dw, each way
 constexpr int kRows = 32;     // rows of a step
@@ -335,7 +336,9 @@ __device__ __forceinline__ void multiply_step(const LinearStep<T> &s, bool biase
     }
 }
 
-// f32: a step's rows 8 q + i of the lanes' quarters q, one i at a time.
+// f32: a step's rows 8 q + i of the lanes' quarters q, one i at a time.  bias:
+// the lane's own sums, in element 0, added beside the matrix unit (by it they
+// are a fifth of its work: 921,600 rows, 64 x 64, 102 us a call and 83).
 template <>
 __device__ __forceinline__ void multiply_step(const LinearStep<float> &s, bool biased,
                                               f4 (&acc)[4][4], f4 (&bias)[4])
@@ -355,8 +358,7 @@ __device__ __forceinline__ void multiply_step(const LinearStep<float> &s, bool b
         }
         if (biased)
 #pragma unroll
-            for (int n = 0; n < 4; ++n)
-                bias[n] = __builtin_amdgcn_mfma_f32_16x16x4f32(1.0f, b[n], bias[n], 0, 0, 0);
+            for (int n = 0; n < 4; ++n) bias[n][0] += b[n];
     }
 }
 
@@ -398,6 +400,7 @@ __global__ __launch_bounds__(kThreads) void linear_grad_kernel(LinearK k)
         // overlap, since waits are counted.
         const auto load = [&](LinearStep<T> &s, int i) {
             load_step(s, r0 + (int64_t)min(i, n - 1) * (4 * kRows), off, k);
+            __builtin_amdgcn_sched_barrier(0);   // else loads may sink to their uses
         };
         LinearStep<T> s0, s1, s2;
         load(s0, 0);
@@ -419,6 +422,12 @@ __global__ __launch_bounds__(kThreads) void linear_grad_kernel(LinearK k)
         load_last(s, r0 + 8 * q, r1, ci, co, k);
         multiply_step(s, biased, acc, bias);
     }
+    if (sizeof(T) == 4)   // the quarters' column sums
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            bias[j][0] += __shfl_xor(bias[j][0], 16);
+            bias[j][0] += __shfl_xor(bias[j][0], 32);
+        }
     // Two waves store their sums, the other two add theirs, and the halves are
     // added on the way out.  A tile's row m (channel 4 m + i) is in quarter
     // m / 4, register m % 4, its column n (outs 4 n + j) in lane n: a lane's four

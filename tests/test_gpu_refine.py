@@ -402,6 +402,17 @@ def test_linear_weight_gradient_of_narrow_layers(r, shape, dtype):
     test_linear_weight_gradient(r, shape, dtype)
 
 
+# widths around the tiles and their halves
+TILES = [(300, 24, 40), (1025, 33, 48), (129, 48, 20), (5000, 96, 96), (77, 31, 47), (2000, 7, 130),
+         (640, 65, 31), (4100, 20, 35), (33, 40, 5), (130, 5, 500)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", TILES, ids=str)
+def test_linear_weight_gradient_around_the_tiles(r, shape, dtype):
+    test_linear_weight_gradient(r, shape, dtype)
+
+
 def test_linear_gradient_of_non_finite_rows(r):
     """A group that was not finite makes its channels' weights NaN, no others."""
     g = _gen(2)
