@@ -118,12 +118,12 @@ __global__ __launch_bounds__(kThreads) void kept_unpack_kernel(const int8_t *cod
 // the blocks' sums in a fixed order.
 //
 // What bounds it: few weights, the stream of codes and dy (720p rows, 64 x 64,
-// bf16: 179 MB in 36 us of kernel, 5.0 TB/s); many weights, the vector memory
+// bf16: 179 MB in 35 us of kernel, 5.1 TB/s); many weights, the vector memory
 // path through which every tile's rows go again, busy 80% of the time (100,000
 // rows, 512 x 512, bf16: 121 us, 433 TFLOP/s; 3600 rows, 512 x 1536, f16: 21
 // us).  Wide loads turned by way of LDS instead took 110 us of the first, no
-// less of the second, and 250 against 210 us in f32 (100,000 rows, 320 x 320; now
-// 187, 110 TFLOP/s).
+// less of the second, and 250 us where f32 takes 187 (100,000 rows, 320 x 320; 110
+// TFLOP/s).
 
 constexpr int kTile = 64;     // channels of a wave's block of dw, each way
 constexpr int kRows = 32;     // rows of a step
@@ -647,10 +647,11 @@ struct LinearPlan {
 // block, about 1.2 us while a CU holds two blocks (as many as their registers
 // allow) and 0.6 of that while it holds one; a block takes about 3 more for its
 // start and its end, a join about 5, and writing and reading n sums n / 500,000.
-// One part needs no join.  Narrow layers: two runs of loads a lane, and 2 blocks a
-// CU at most (2,000,000 rows of one: 21 us, 31 with 1, 26 with 3).  (720p rows, 64 x 64: 256 parts 40.6 us, 512 41.2, 128
+// One part needs no join.  (720p rows, 64 x 64: 256 parts 40.6 us, 512 41.2, 128
 // 50.8; 3600 rows, 512 x 1536, f16: one part 21.6, two with their join 24.2,
-// five 29.6; 100,000 rows, 512 x 512: 8 parts 121, 4 143, 16 140.)
+// five 29.6; 100,000 rows, 512 x 512: 8 parts 121, 4 143, 16 140.)  Narrow layers:
+// two runs of loads a lane at least, and 2 blocks a CU at most (2,000,000 rows of
+// one by one: 9 us more a call with 1, 4 with 3).
 LinearPlan linear_plan(int64_t rows, int C, int outs, int dtype)
 {
     LinearPlan p;
