@@ -795,7 +795,7 @@ hipError_t launch_linear_grad(int dtype, int64_t rows, int C, int outs, const in
     const LinearK k{codes, exps, dy, rows, dy_stride, p.part, whole, C, outs, kept_groups(C),
                     p.ty,  p.tz, one ? dw : sums, one ? db : sums + weights, n};
     const int grid = p.parts * p.ty * p.tz;
-    const bool tiny = rows * C < 4 || (rows - 1) * dy_stride + outs < 4;
+    const bool tiny = !p.narrow && (rows * C < 4 || (rows - 1) * dy_stride + outs < 4);
     with_type(dtype, [&](auto *t) {
         typedef std::remove_pointer_t<decltype(t)> T;
         auto narrow = [&](auto ct, auto ot, auto l) {

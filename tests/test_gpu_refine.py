@@ -413,6 +413,51 @@ def test_linear_weight_gradient_around_the_tiles(r, shape, dtype):
     test_linear_weight_gradient(r, shape, dtype)
 
 
+@pytest.mark.parametrize("widths", [(8, 3), (4, 4), (40, 4), (4, 20), (64, 33), (33, 64)], ids=str)
+def test_linear_gradient_of_repeated_rows(r, widths):
+    """A gradient that every row shares (stride 0) gives what its copies give:
+    the same values are added in the same order."""
+    C, outs = widths
+    g = _gen(C * outs)
+    kept = r.checkpoint_pack(torch.randn((3001, C), generator=g).to(torch.bfloat16).cuda())
+    dy = torch.randn((1, outs), generator=g).to(torch.bfloat16).cuda().expand(3001, outs)
+    say("linear, repeated rows", widths)
+    for got, want in zip(r.linear_weight_grad(kept, dy),
+                         r.linear_weight_grad(kept, dy.contiguous())):
+        assert torch.equal(got, want)
+
+
+def test_rows_past_32_bits(r):
+    """Rows, tokens and heads 2^31 + 24 elements apart in one buffer."""
+    far = 2 ** 31 + 24
+    g = _gen(10)
+    buf = torch.empty((far + 64,), dtype=torch.float16, device="cuda")
+    for C, outs in ((64, 64), (16, 4), (24, 64)):
+        x = buf.as_strided((2, C), (far, 1))
+        near = torch.randn((2, C), generator=g).to(torch.float16).cuda()
+        x.copy_(near)
+        say("far rows", C, outs)
+        kept, want = r.checkpoint_pack(x), r.checkpoint_pack(near)
+        assert torch.equal(kept.codes, want.codes) and torch.equal(kept.exps, want.exps)
+        assert torch.equal(r.checkpoint_unpack(kept, out=x), r.checkpoint_unpack(want))
+        dy = buf.as_strided((2, outs), (far, 1))
+        near = torch.randn((2, outs), generator=g).to(torch.float16).cuda()
+        dy.copy_(near)
+        for got, w in zip(r.linear_weight_grad(kept, dy), r.linear_weight_grad(want, near)):
+            assert torch.equal(got, w)
+    freq = torch.rand((8,), generator=g).cuda()
+    axis = torch.zeros((8,), dtype=torch.uint8, device="cuda")
+    near = torch.randn((2, 1, 16), generator=g).to(torch.float16).cuda()
+    for tokens in (2, 1):     # far tokens, then far heads
+        near = near.reshape(tokens, 2 // tokens, 16)
+        pos = torch.arange(1, tokens + 1, device="cuda").float().reshape(tokens, 1)
+        x = buf.as_strided(near.shape, (far, far, 1))
+        x.copy_(near)
+        want = r.rotary(near, pos, freq, axis)
+        assert torch.equal(r.rotary(x, pos, freq, axis), want)
+        assert torch.equal(r.rotary(x, pos, freq, axis, out=x), want)
+
+
 def test_linear_gradient_of_non_finite_rows(r):
     """A group that was not finite makes its channels' weights NaN, no others."""
     g = _gen(2)
