@@ -457,7 +457,8 @@ __global__ __launch_bounds__(kThreads) void linear_grad_kernel(LinearK k)
     if (og < k.outs) {
         for (int i = threadIdx.x >> 6; i < kTile; i += 4) {
             const int cg = ty * kTile + i;
-            if (cg < k.C) out[(int64_t)cg * k.outs + og] = sh[0][i * kTile + o] + sh[1][i * kTile + o];
+            if (cg < k.C)
+                out[(int64_t)cg * k.outs + og] = sh[0][i * kTile + o] + sh[1][i * kTile + o];
         }
         if (biased && k.bias && threadIdx.x < 64)
             k.bias[(int64_t)part * k.stride + og] =
@@ -579,16 +580,18 @@ __global__ __launch_bounds__(kThreads) void linear_narrow_kernel(LinearK k)
     }
 }
 
-// Arrays shorter than a vector: a thread's sum for each weight.
+// Arrays shorter than a vector (few elements, or one short row of dy that all
+// rows share): a thread's sum for each weight of a part.
 template <typename T>
-__global__ __launch_bounds__(kThreads) void linear_tiny_kernel(LinearK k, float *dw, float *db)
+__global__ __launch_bounds__(kThreads) void linear_tiny_kernel(LinearK k)
 {
     const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-    const int64_t c = i / k.outs;
+    const int64_t c = i / k.outs, part = blockIdx.y;
     if (c > k.C) return;
     const int o = (int)(i - c * k.outs);
+    const int64_t first = part * k.part, r1 = min(first + k.part, k.rows);
     float v = 0.0f;
-    for (int64_t r = 0; r < k.rows; ++r) {
+    for (int64_t r = first; r < r1; ++r) {
         const float d = (float)((const T *)k.dy)[r * k.dy_stride + o];
         const float x = c < k.C ? (float)k.codes[r * k.C + c] *
                                       kept_scale(k.exps[r * k.per_row + c / kKeptGroup])
@@ -596,9 +599,9 @@ __global__ __launch_bounds__(kThreads) void linear_tiny_kernel(LinearK k, float 
         v = fmaf(x, d, v);
     }
     if (c < k.C)
-        dw[i] = v;
-    else if (db)
-        db[o] = v;
+        k.sums[part * k.stride + i] = v;
+    else if (k.bias)
+        k.bias[part * k.stride + o] = v;
 }
 
 // Adds the parts.  n: values of one part; the last outs are db.  ACROSS
@@ -684,7 +687,8 @@ LinearPlan linear_plan(int64_t rows, int C, int outs, int dtype)
         const int64_t each = (steps + parts - 1) / parts;
         const int64_t turns = (parts * tiles + 2 * kCus - 1) / (2 * kCus);
         const double load = parts * tiles <= kCus ? 0.6 : (double)turns;
-        const double cost = load * (double)(each + 3) + (parts > 1 ? 5.0 + sums * (double)parts : 0.0);
+        const double join = parts > 1 ? 5.0 + sums * (double)parts : 0.0;
+        const double cost = load * (double)(each + 3) + join;
         if (filled == 0 || cost < least) {
             least = cost;
             best = parts;
@@ -795,7 +799,7 @@ hipError_t launch_linear_grad(int dtype, int64_t rows, int C, int outs, const in
     const LinearK k{codes, exps, dy, rows, dy_stride, p.part, whole, C, outs, kept_groups(C),
                     p.ty,  p.tz, one ? dw : sums, one ? db : sums + weights, n};
     const int grid = p.parts * p.ty * p.tz;
-    const bool tiny = !p.narrow && (rows * C < 4 || (rows - 1) * dy_stride + outs < 4);
+    const bool tiny = rows * C < 4 || (rows - 1) * dy_stride + outs < 4;
     with_type(dtype, [&](auto *t) {
         typedef std::remove_pointer_t<decltype(t)> T;
         auto narrow = [&](auto ct, auto ot, auto l) {
@@ -816,16 +820,16 @@ hipError_t launch_linear_grad(int dtype, int64_t rows, int C, int outs, const in
         else if (p.narrow == 4)
             with_side(std::integral_constant<int, 4>());
         else if (tiny)
-            linear_tiny_kernel<T><<<blocks(n, kThreads), kThreads, 0, stream>>>(k, dw, db);
+            linear_tiny_kernel<T>
+                <<<dim3(blocks(n, kThreads), p.parts), kThreads, 0, stream>>>(k);
         else
             linear_grad_kernel<T><<<grid, kThreads, 0, stream>>>(k);
     });
     // many parts of few weights: 32 threads a value (4160 values of 506 parts
     // 4.7 us, against 120 with one); few parts: one (788,000 values of 2 parts
     // 53 us with 32)
-    if (tiny || one)
-        ;
-    else if (p.parts > 8)
+    if (one) return hipGetLastError();
+    if (p.parts > 8)
         linear_join_kernel<32, 1024><<<blocks(n, 32), 1024, 0, stream>>>(sums, n, weights,
                                                                          p.parts, dw, db);
     else

@@ -427,6 +427,19 @@ def test_linear_gradient_of_repeated_rows(r, widths):
         assert torch.equal(got, want)
 
 
+def test_linear_gradient_of_one_short_repeated_row(r):
+    """A dy of fewer elements than a vector, for many channels and rows."""
+    g = _gen(12)
+    x = torch.randn((5003, 130), generator=g).to(torch.float16).cuda()
+    kept = r.checkpoint_pack(x)
+    dy = torch.randn((1, 2), generator=g).to(torch.float16).cuda().expand(5003, 2)
+    dw, db = r.linear_weight_grad(kept, dy)
+    xv, dv = r.checkpoint_unpack(kept).double().cpu(), dy.double().cpu()
+    scale = 4 * ref.U * math.sqrt(5003) + 8 * ref.U     # as for the other widths
+    _inside(dw, xv.t() @ dv, scale * (xv.abs().t() @ dv.abs()), "dw")
+    _inside(db, dv.sum(0), scale * dv.abs().sum(0), "db")
+
+
 def test_rows_past_32_bits(r):
     """Rows, tokens and heads 2^31 + 24 elements apart in one buffer."""
     far = 2 ** 31 + 24
