@@ -118,22 +118,24 @@ __device__ __forceinline__ uint32_t kept_byte(uint32_t bits)
 
 // The codes of V values at their group's scale byte.  x 2^-e is exact; added to
 // 1.5 * 2^23 it leaves its nearest integer (halves to even) in the sum's low
-// bits, and by the choice of e that is at most 127 in magnitude.  2^-e is taken
-// as 0 for byte 255, whose codes are then 0 (a NaN's low bits are).  From kTop
-// on, where 64 * 2^e is not finite in T, the codes stop at 63.
+// bits, and by the choice of e that is at most 127 in magnitude.  From kTop on,
+// where 64 * 2^e is not finite in T, the codes stop at 63; at byte 255 they are
+// 0, whatever the sum made of an infinity or of a NaN and its payload.
 template <typename T, int V>
 __device__ __forceinline__ Pack<int8_t, V> kept_codes(const float (&x)[V], uint32_t byte)
 {
-    const float inv = byte == 255u ? 0.0f : __uint_as_float((254u - byte) << 23);
+    const float inv = __uint_as_float((254u - byte) << 23);   // 2^-e
     Pack<int8_t, V> q;
 #pragma unroll
     for (int i = 0; i < V; ++i)
         q.v[i] = (int8_t)(__float_as_uint(fmaf(x[i], inv, 12582912.0f)) & 255u);
     // (a branch for the wave: as a choice for each lane it costs two steps a value)
     if (__builtin_amdgcn_ballot_w64(byte >= (uint32_t)(KeptRange<T>::kTop + 127)) != 0 &&
-        byte >= (uint32_t)(KeptRange<T>::kTop + 127))
+        byte >= (uint32_t)(KeptRange<T>::kTop + 127)) {
+        const int most = byte == 255u ? 0 : 63;
 #pragma unroll
-        for (int i = 0; i < V; ++i) q.v[i] = (int8_t)max(min((int)q.v[i], 63), -63);
+        for (int i = 0; i < V; ++i) q.v[i] = (int8_t)max(min((int)q.v[i], most), -most);
+    }
     return q;
 }
 
