@@ -127,6 +127,14 @@ __global__ __launch_bounds__(kThreads) void kept_unpack_kernel(const int8_t *cod
 
 constexpr int kTile = 64;     // channels of a wave's block of dw, each way
 constexpr int kRows = 32;     // rows of a step
+// Steps of a wave whose sums stay in registers, where a part is one chain of them
+// (kOneChain at most) and where it is several, which move on to LDS in turn.  32
+// steps are 1024 rows added one after another in 32 bits in f32 (a matrix
+// instruction adds its 4 rows so), 128 are as many matrix instructions of 32 rows
+// in 16 bits.  Without it a wide layer of many rows, which is one part, lost its
+// lower bits (921,600 equal rows, 2048 x 2048 in f32: off by 2.3e-3).
+template <typename T> constexpr int kOneChain = sizeof(T) == 4 ? 32 : 128;
+template <typename T> constexpr int kChainSteps = sizeof(T) == 4 ? 27 : 120;   // 3 n
 
 typedef float f4 __attribute__((ext_vector_type(4)));
 typedef _Float16 h8 __attribute__((ext_vector_type(8)));
@@ -362,10 +370,11 @@ __device__ __forceinline__ void multiply_step(const LinearStep<float> &s, bool b
     }
 }
 
-template <typename T>
+// CHAINS: a part has more steps than one chain.
+template <typename T, bool CHAINS>
 __global__ __launch_bounds__(kThreads) void linear_grad_kernel(LinearK k)
 {
-    __shared__ __align__(16) float sh[2][kTile * kTile + kTile];
+    __shared__ __align__(16) float sh[CHAINS ? 4 : 2][kTile * kTile + kTile];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x & 63;
     const int q = lane >> 4, c = lane & 15;
     // Blocks are dealt to the 8 XCDs in turn.  Each XCD takes a run of a part's
@@ -380,12 +389,40 @@ __global__ __launch_bounds__(kThreads) void linear_grad_kernel(LinearK k)
     if (ci >= k.C) ci = 0;
     if (co >= k.outs) co = 0;
     f4 acc[4][4], bias[4];
+    const auto clear = [&] {
 #pragma unroll
-    for (int m = 0; m < 4; ++m) {
-        bias[m] = (f4)0.0f;
+        for (int m = 0; m < 4; ++m) {
+            bias[m] = (f4)0.0f;
 #pragma unroll
-        for (int n = 0; n < 4; ++n) acc[m][n] = (f4)0.0f;
-    }
+            for (int n = 0; n < 4; ++n) acc[m][n] = (f4)0.0f;
+        }
+    };
+    clear();
+    // Puts this wave's sums into its place in LDS or adds them there.  A tile's
+    // row m (channel 4 m + i) is in quarter m / 4, register m % 4, its column n
+    // (outs 4 n + j) in lane n: a lane's four neighbours go at once (one at a
+    // time, and the waves one after another, 0.5 to 0.8 us more a call).
+    const auto move = [&](float *mine, bool store) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                f4 *const p = (f4 *)&mine[(4 * (4 * q + e) + i) * kTile + 4 * c];
+                const f4 v = {acc[i][0][e], acc[i][1][e], acc[i][2][e], acc[i][3][e]};
+                *p = store ? v : *p + v;
+            }
+        if (sizeof(T) == 4)   // the quarters' column sums
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                bias[j][0] += __shfl_xor(bias[j][0], 16);
+                bias[j][0] += __shfl_xor(bias[j][0], 32);
+            }
+        if (q == 0) {
+            f4 *const p = (f4 *)&mine[kTile * kTile + 4 * c];
+            const f4 v = {bias[0][0], bias[1][0], bias[2][0], bias[3][0]};
+            *p = store ? v : *p + v;
+        }
+    };
     const bool biased = ty == 0;
     const int64_t first = part * k.part, r1 = min(first + k.part, k.rows);
     const int64_t whole = min(r1, k.whole);
@@ -394,6 +431,7 @@ __global__ __launch_bounds__(kThreads) void linear_grad_kernel(LinearK k)
     const LinearOffsets off{(uint32_t)(8 * q * k.C + ci),
                             (uint32_t)(8 * q * k.per_row + ci / kKeptGroup),
                             (uint32_t)(8 * q * (uint32_t)k.dy_stride + co) * (uint32_t)sizeof(T)};
+    bool moved = false;   // this wave has sums in LDS
     if (n > 0) {
         // Two steps are on their way while one is multiplied.  The loads past
         // the last step repeat it: a condition around them would end the
@@ -405,64 +443,77 @@ __global__ __launch_bounds__(kThreads) void linear_grad_kernel(LinearK k)
         LinearStep<T> s0, s1, s2;
         load(s0, 0);
         load(s1, 1);
-        for (int i = 0;; i += 3) {
-            load(s2, i + 2);
-            multiply_step(s0, biased, acc, bias);
-            if (i + 1 >= n) break;
-            load(s0, i + 3);
-            multiply_step(s1, biased, acc, bias);
-            if (i + 2 >= n) break;
-            load(s1, i + 4);
-            multiply_step(s2, biased, acc, bias);
-            if (i + 3 >= n) break;
+        // (two forms of one loop: the first takes 10% less where a part is one
+        // chain in 16 bits, the second where it is several in f32)
+        if (!CHAINS)
+            for (int i = 0;; i += 3) {
+                load(s2, i + 2);
+                multiply_step(s0, biased, acc, bias);
+                if (i + 1 >= n) break;
+                load(s0, i + 3);
+                multiply_step(s1, biased, acc, bias);
+                if (i + 2 >= n) break;
+                load(s1, i + 4);
+                multiply_step(s2, biased, acc, bias);
+                if (i + 3 >= n) break;
+            }
+        else {
+            int i = 0;
+            while (i + 3 <= n) {
+                const int end = min(i + kChainSteps<T>, n);
+                for (; i + 3 <= end; i += 3) {
+                    load(s2, i + 2);
+                    multiply_step(s0, biased, acc, bias);
+                    load(s0, i + 3);
+                    multiply_step(s1, biased, acc, bias);
+                    load(s1, i + 4);
+                    multiply_step(s2, biased, acc, bias);
+                }
+                move(sh[wave], !moved);
+                clear();
+                moved = true;
+            }
+            if (i < n) multiply_step(s0, biased, acc, bias);
+            if (i + 1 < n) multiply_step(s1, biased, acc, bias);
         }
     }
+    // (rows near the arrays' end, or all where vectors cannot be used)
+    int tail = 0;
     for (r0 += (int64_t)n * (4 * kRows); r0 < r1; r0 += 4 * kRows) {
+        if (CHAINS && ++tail % kChainSteps<T> == 0) {
+            move(sh[wave], !moved);
+            clear();
+            moved = true;
+        }
         LinearStep<T> s;
         load_last(s, r0 + 8 * q, r1, ci, co, k);
         multiply_step(s, biased, acc, bias);
     }
-    if (sizeof(T) == 4)   // the quarters' column sums
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            bias[j][0] += __shfl_xor(bias[j][0], 16);
-            bias[j][0] += __shfl_xor(bias[j][0], 32);
-        }
-    // Two waves store their sums, the other two add theirs, and the halves are
-    // added on the way out.  A tile's row m (channel 4 m + i) is in quarter
-    // m / 4, register m % 4, its column n (outs 4 n + j) in lane n: a lane's four
-    // neighbours go at once (one at a time, and the waves one after another,
-    // 0.5 to 0.8 us more a call).
-    for (int w = 0; w < 4; w += 2) {
-        if ((wave & 2) == w) {
-            float *const mine = sh[wave & 1];
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    f4 *const p = (f4 *)&mine[(4 * (4 * q + e) + i) * kTile + 4 * c];
-                    const f4 v = {acc[i][0][e], acc[i][1][e], acc[i][2][e], acc[i][3][e]};
-                    *p = w == 0 ? v : *p + v;
-                }
-            if (q == 0) {
-                f4 *const p = (f4 *)&mine[kTile * kTile + 4 * c];
-                const f4 v = {bias[0][0], bias[1][0], bias[2][0], bias[3][0]};
-                *p = w == 0 ? v : *p + v;
-            }
-        }
+    if (CHAINS) {
+        move(sh[wave], !moved);
         __syncthreads();
+    } else {
+        // two waves store their sums, the other two add theirs, and the halves
+        // are added on the way out
+        for (int w = 0; w < 4; w += 2) {
+            if ((wave & 2) == w) move(sh[wave & 1], w == 0);
+            __syncthreads();
+        }
     }
+    const auto sum = [&](int at) {
+        const float v = sh[0][at] + sh[1][at];
+        return CHAINS ? v + (sh[CHAINS ? 2 : 0][at] + sh[CHAINS ? 3 : 0][at]) : v;
+    };
     float *const out = k.sums + (int64_t)part * k.stride;
     const int o = threadIdx.x & 63, og = tz * kTile + o;
     if (og < k.outs) {
         for (int i = threadIdx.x >> 6; i < kTile; i += 4) {
             const int cg = ty * kTile + i;
             if (cg < k.C)
-                out[(int64_t)cg * k.outs + og] = sh[0][i * kTile + o] + sh[1][i * kTile + o];
+                out[(int64_t)cg * k.outs + og] = sum(i * kTile + o);
         }
         if (biased && k.bias && threadIdx.x < 64)
-            k.bias[(int64_t)part * k.stride + og] =
-                sh[0][kTile * kTile + o] + sh[1][kTile * kTile + o];
+            k.bias[(int64_t)part * k.stride + og] = sum(kTile * kTile + o);
     }
 }
 
@@ -590,18 +641,18 @@ __global__ __launch_bounds__(kThreads) void linear_tiny_kernel(LinearK k)
     if (c > k.C) return;
     const int o = (int)(i - c * k.outs);
     const int64_t first = part * k.part, r1 = min(first + k.part, k.rows);
-    float v = 0.0f;
+    double v = 0.0;   // a part may have many rows
     for (int64_t r = first; r < r1; ++r) {
         const float d = (float)((const T *)k.dy)[r * k.dy_stride + o];
         const float x = c < k.C ? (float)k.codes[r * k.C + c] *
                                       kept_scale(k.exps[r * k.per_row + c / kKeptGroup])
                                 : 1.0f;
-        v = fmaf(x, d, v);
+        v = fma((double)x, (double)d, v);
     }
     if (c < k.C)
-        k.sums[part * k.stride + i] = v;
+        k.sums[part * k.stride + i] = (float)v;
     else if (k.bias)
-        k.bias[part * k.stride + o] = v;
+        k.bias[part * k.stride + o] = (float)v;
 }
 
 // Adds the parts.  n: values of one part; the last outs are db.  ACROSS
@@ -639,6 +690,7 @@ __global__ __launch_bounds__(THREADS) void linear_join_kernel(const float *sums,
 constexpr int kCus = 256;
 
 constexpr int kNarrowBlocks = 512;
+constexpr int kNarrowRows = 1024;   // about as many rows a lane adds up in 32 bits
 
 struct LinearPlan {
     int parts, ty, tz;
@@ -667,7 +719,8 @@ LinearPlan linear_plan(int64_t rows, int C, int outs, int dtype)
         p.ty = p.tz = 1;
         const int64_t run = (int64_t)kThreads / p.narrow * 2 * kNarrowAhead;
         int64_t parts = (rows + run - 1) / run;
-        if (parts > kNarrowBlocks) parts = kNarrowBlocks;
+        const int64_t least = rows / ((int64_t)kThreads / p.narrow * kNarrowRows);
+        if (parts > kNarrowBlocks) parts = least > kNarrowBlocks ? least : kNarrowBlocks;
         if (parts < 1) parts = 1;
         p.part = (rows + parts - 1) / parts;
         p.parts = (int)parts;
@@ -822,8 +875,10 @@ hipError_t launch_linear_grad(int dtype, int64_t rows, int C, int outs, const in
         else if (tiny)
             linear_tiny_kernel<T>
                 <<<dim3(blocks(n, kThreads), p.parts), kThreads, 0, stream>>>(k);
+        else if (p.part > (int64_t)kOneChain<T> * 4 * kRows)
+            linear_grad_kernel<T, true><<<grid, kThreads, 0, stream>>>(k);
         else
-            linear_grad_kernel<T><<<grid, kThreads, 0, stream>>>(k);
+            linear_grad_kernel<T, false><<<grid, kThreads, 0, stream>>>(k);
     });
     // many parts of few weights: 32 threads a value (4160 values of 506 parts
     // 4.7 us, against 120 with one); few parts: one (788,000 values of 2 parts

@@ -68,3 +68,85 @@ def test_a_nan_of_any_bits_is_kept_as_one(r, dtype):
             want = held.any(0)[:, None].expand(width, outs)
             assert torch.equal(torch.isnan(dw).cpu(), want)
             assert bool(torch.isfinite(dw.cpu()[~want]).all())
+
+
+# --- sums over very many rows ---------------------------------------------------------
+#
+# m equal terms added one after another in 32 bits are off by at most u m / 2 of
+# the sum: the k-th addition rounds k terms.
+
+@pytest.mark.parametrize("dtype", list(DT))
+def test_linear_gradient_of_many_equal_rows(r, dtype):
+    """A wide layer over 921,600 rows, all of them the same: its rows are one
+    part.  At most 1024 additions of a wave go one after another, then its sums
+    are moved on."""
+    rows, width = 921_600, 2048
+    dt = DT[dtype]
+    say("equal rows", dtype)
+    codes = torch.full((rows, width), 64, dtype=torch.int8, device="cuda")
+    exps = torch.full((rows, width // 32), 127 - 6, dtype=torch.uint8, device="cuda")
+    dy = torch.full((1, 1), 0.1, dtype=dt, device="cuda")
+    each = float(dy.double())
+    # (the columns of dy are neighbours in one row that all rows share)
+    dy = dy.expand(1, width).contiguous().expand(rows, width)
+    dw, db = r.linear_weight_grad(mixrt.Checkpoint(codes, exps, dt), dy)
+    want = rows * each
+    bound = ref.U * (1024 / 2 + 57 + 16)
+    for got in (dw, db):
+        off = float((got.double() / want - 1).abs().max())
+        say(f"off by {off / ref.U:.0f} u, may be {bound / ref.U:.0f}")
+        assert off <= bound
+
+
+def test_linear_gradient_of_many_rows_and_a_short_gradient(r):
+    """Two outs that all rows share, 130 channels: a thread's sum a weight."""
+    rows, width = 1 << 24, 130
+    codes = torch.full((rows, width), 64, dtype=torch.int8, device="cuda")
+    exps = torch.full((rows, 5), 127 - 6, dtype=torch.uint8, device="cuda")
+    dy = torch.full((1, 2), 0.1, dtype=torch.float16, device="cuda")
+    each = float(dy[0, 0].double())
+    dw, db = r.linear_weight_grad(mixrt.Checkpoint(codes, exps, torch.float16),
+                                  dy.expand(rows, 2))
+    for got in (dw, db):
+        off = float((got.double() / (rows * each) - 1).abs().max())
+        say(f"off by {off / ref.U:.0f} u")
+        # a part in 64 bits, rounded; up to 4096 parts by 32 threads and a tree
+        assert off <= ref.U * (128 / 2 + 8)
+
+
+@pytest.mark.parametrize("shared", [False, True])
+@pytest.mark.parametrize("dtype", list(DT))
+def test_linear_gradient_of_long_ragged_parts(r, dtype, shared):
+    """Widths that are no multiples of a vector, in parts of several chains;
+    with rows of dy that repeat, which are read without vectors past the row."""
+    rows, width, outs = 30_011, 1101, 1030
+    dt = DT[dtype]
+    say("long parts", dtype, shared)
+    g = torch.Generator("cuda").manual_seed(3)
+    kept = r.checkpoint_pack(torch.randn((rows, width), generator=g, device="cuda").to(dt))
+    dy = torch.randn((1 if shared else rows, outs), generator=g, device="cuda").to(dt)
+    dy = dy.expand(rows, outs)
+    dw, db = r.linear_weight_grad(kept, dy)
+    xv, dv = r.checkpoint_unpack(kept).double(), dy.double().contiguous()
+    # 1024 additions, the moves to LDS of four waves, the sums of the waves
+    scale = ref.U * (1024 + 2 * 16 + 8)
+    xt = xv.t().contiguous()
+    assert bool(((dw.double() - xt @ dv).abs() <= scale * (xt.abs() @ dv.abs())).all())
+    assert bool(((db.double() - dv.sum(0)).abs() <= scale * dv.abs().sum(0)).all())
+
+
+def test_linear_gradient_of_very_many_narrow_rows(r):
+    """2^28 equal rows of one channel and four outs: about 1024 rows a lane,
+    then 32 lanes' and blocks' sums in trees and runs."""
+    rows = 1 << 28
+    codes = torch.full((rows, 1), 64, dtype=torch.int8, device="cuda")
+    exps = torch.full((rows, 1), 127 - 6, dtype=torch.uint8, device="cuda")
+    dy = torch.full((1, 4), 0.1, device="cuda")
+    dw, db = r.linear_weight_grad(mixrt.Checkpoint(codes, exps, torch.float32),
+                                  dy.expand(rows, 4))
+    want = rows * float(dy[0, 0].double())
+    for got in (dw, db):
+        off = float((got.double() / want - 1).abs().max())
+        say(f"off by {off / ref.U:.0f} u")
+        # a lane's rows; 6 steps of a wave, 4 waves, 32 parts a thread, 5 steps
+        assert off <= ref.U * ((1024 + 32) / 2 + 6 + 4 + 5)
