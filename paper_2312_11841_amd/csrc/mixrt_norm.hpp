@@ -27,6 +27,9 @@ inline constexpr int kJoinThreads = 1024;
 // 360p x 64 in bf16: 95 us, with two 106, four 135; its writing 136 with one,
 // 123 with two, 104 with four).
 inline constexpr int kAhead = 4;
+// Most rows that a thread of the backward's sums adds up in 32 bits: each addition
+// rounds what is there, so equal terms are off by half as many units at most.
+inline constexpr int kBackRows = 128;
 inline constexpr int kFoldChannels = 512;   // most channels (and groups) of a join by the blocks
 
 struct NormK {
@@ -257,6 +260,8 @@ inline NormPlan norm_plan(int N, int64_t P, int C, int G, int dtype, bool pad, b
     const int64_t images = N > 0 ? (int64_t)N * p.slabs : 1;
     int64_t S = 1024 / images;
     if (S < 256 && images < 64) S = 256;
+    const int64_t least = (P + (int64_t)p.R * kBackRows - 1) / ((int64_t)p.R * kBackRows);
+    if (back && S < least) S = least;
     p.S = (int)atmost(S, runs);
     p.share = back ? (int)atmost(768 / images, runs) : (int)atmost((runs + 1) / 2, 1 << 20);
     return p;

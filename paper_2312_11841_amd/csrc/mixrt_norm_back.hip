@@ -36,8 +36,8 @@ __device__ __forceinline__ BackRow<T, V, KEPT> load_back(const NormK &k, int n, 
 }
 
 // Sums of dz and dz xh per channel over one part of an image: in 32 bits within
-// a thread, whose rows are few (63 of a 1080p image of 16 channels), in 64 bits
-// where the parts are joined.  Bound by its arithmetic, 13 steps, an exponential
+// a thread, whose rows are kBackRows at most, and in up to 8 steps over a block's
+// rows; in 64 bits where the parts are joined.  Bound by its arithmetic, 13 steps, an exponential
 // and a reciprocal an element (8 x 360p x 64 channels in bf16, silu: 361 MB in
 // 101 us, 3.6 TB/s).
 template <typename T, int V, int ACT, bool KEPT>

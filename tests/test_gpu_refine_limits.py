@@ -150,3 +150,33 @@ def test_linear_gradient_of_very_many_narrow_rows(r):
         say(f"off by {off / ref.U:.0f} u")
         # a lane's rows; 6 steps of a wave, 4 waves, 32 parts a thread, 5 steps
         assert off <= ref.U * ((1024 + 32) / 2 + 6 + 4 + 5)
+
+
+@pytest.mark.parametrize("dtype", list(DT))
+def test_norm_gradient_of_many_equal_rows(r, dtype):
+    """128 images of 131,072 equal pixels, wide rows: at most 128 rows of a
+    thread are added in 32 bits, then in 64.  (The map is one pixel that
+    repeats; dx is not asked for.)"""
+    N, P, width, G = 128, 1 << 17, 1024, 8
+    dt = DT[dtype]
+    say("equal pixels", dtype)
+    dy = torch.full((width,), 0.1, dtype=dt, device="cuda")
+    x = torch.full((width,), 0.75, dtype=dt, device="cuda")
+    stats = torch.tensor([0.25, 1.7], device="cuda").repeat(N, G, 1)
+    norm = mixrt.Norm(N, width, P, G, CODE[dtype], 0, 1e-5, 0, 0)
+    size = C.c_size_t()
+    assert r._L.mixrt_norm_workspace(C.byref(norm), C.byref(size)) == 0
+    ws = torch.empty((size.value,), dtype=torch.uint8, device="cuda")
+    grads = torch.zeros((2, width), device="cuda")
+    one = lambda t: C.byref(mixrt.Map(t.data_ptr(), 0, 0))  # noqa: E731
+    r._check(r._L.mixrt_norm_backward(r._h, C.byref(norm), one(dy), one(x), None,
+                                      stats.data_ptr(), None, grads[0].data_ptr(),
+                                      grads[1].data_ptr(), ws.data_ptr(), size.value))
+    r.sync()
+    d = float(dy[0].double())
+    xh = 0.5 * float(stats[0, 0, 1].double())
+    for got, want, terms in ((grads[0], N * P * d * xh, 4), (grads[1], N * P * d, 2)):
+        off = float((got.double() / want - 1).abs().max())
+        say(f"off by {off / ref.U:.0f} u")
+        # 128 rows, up to 8 steps that join a block's rows, the term and its sum
+        assert off <= ref.U * (128 / 2 + 8 + terms)
