@@ -643,8 +643,9 @@ class Renderer:
         # the handle of torch's current stream (0.1 us; the public way takes 1)
         self._current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
             lambda d: torch.cuda.current_stream(d).cuda_stream)
-        # the refiner's operators' scratch: (address, bytes), and its memory
-        self._ws, self._ws_memory = None, []
+        self._is_capturing = torch.cuda.is_current_stream_capturing
+        # the refiner's operators' scratch: see _workspace
+        self._ws = None
 
     def _check(self, rc: int):
         if rc != MIXRT_OK:
@@ -654,6 +655,7 @@ class Renderer:
         if getattr(self, "_h", None):
             self._L.mixrt_destroy(self._h)
             self._h = None
+            self._ws = None
 
     def __del__(self):
         try:
@@ -807,6 +809,13 @@ class Renderer:
             plans[key] = plan
         return plan
 
+    def _capturing(self) -> bool:
+        """Whether a graph captures this context's stream."""
+        if self._current_stream(self.device) == self._raw_stream:
+            return self._is_capturing()
+        with self._torch.cuda.stream(self.stream):
+            return self._is_capturing()
+
     def _empty(self, shape, dtype):
         """Device memory for an output.  Taken on this context's stream, so
         that memory released to another stream is not handed out early."""
@@ -825,15 +834,18 @@ class Renderer:
         return self._empty(t.shape, t.dtype)
 
     def _workspace(self, size: int):
-        """(address, bytes) of this context's scratch, at least size bytes.
-        Its calls run one after another on its stream, so they share it.  A
-        smaller one that it grew out of stays allocated, since a captured graph
-        may still write there; sizes at least double, so that all of them
-        together take less than twice the last."""
+        """(address, bytes) of scratch for one call, at least size bytes, and
+        its memory, to be held until the launch.  Eager calls run one after
+        another on this context's stream and share one array.  A call that a
+        graph captures has its own, from the graph's memory: a replay may run
+        beside eager calls and beside other graphs."""
+        if self._capturing():
+            t = self._empty((max(size, 16),), self._torch.uint8)
+            return t.data_ptr(), t.numel(), t
         if self._ws is None or self._ws[1] < size:
             last = self._ws[1] if self._ws else 1 << 15
-            self._ws_memory.append(self._empty((max(size, 2 * last),), self._torch.uint8))
-            self._ws = (self._ws_memory[-1].data_ptr(), self._ws_memory[-1].numel())
+            t = self._empty((max(size, 2 * last),), self._torch.uint8)
+            self._ws = (t.data_ptr(), t.numel(), t)
         return self._ws
 
     def _checkpoint(self, rows: int, channels: int, dtype) -> Checkpoint:
@@ -883,9 +895,9 @@ class Renderer:
         p.norm.beta = _per_channel(beta, "beta", p.channels, self.device)
         out, out_ref = self._norm_out(p, x, out, "out")
         kd = None if kept is None else C.byref(kept.descriptor(self.device))
-        ws, size = self._workspace(p.bytes)
+        ws = self._workspace(p.bytes)
         self._check(self._L.mixrt_norm_forward(self._h, p.norm_ref, p.x_ref, out_ref, stats, kd,
-                                               ws, size))
+                                               ws[0], ws[1]))
         return out
 
     def group_norm(self, x, groups: int, gamma=None, beta=None, *, eps: float = 1e-5,
@@ -929,10 +941,10 @@ class Renderer:
         out, out_ref = self._norm_out(p, dy, out, "out")
         grads = self._empty((2, p.channels), self._torch.float32)
         at = grads.data_ptr()
-        ws, size = self._workspace(p.bytes)
+        ws = self._workspace(p.bytes)
         self._check(self._L.mixrt_norm_backward(self._h, p.norm_ref, p.x_ref, xd, kd,
                                                 stats.data_ptr(), out_ref, at,
-                                                at + 4 * p.channels, ws, size))
+                                                at + 4 * p.channels, ws[0], ws[1]))
         dgamma, dbeta = grads.unbind(0)
         return out, dgamma, dbeta
 
@@ -981,11 +993,11 @@ class Renderer:
         ref = C.byref(kd)
         need = self._plan(("linear", kd.rows, kd.channels, kd.dtype, outs),
                           lambda: self._size(self._L.mixrt_linear_grad_workspace, ref, outs))
-        ws, size = self._workspace(need)
+        ws = self._workspace(need)
         dw = self._empty((kd.channels, outs), self._torch.float32)
         db = self._empty((outs,), self._torch.float32) if bias else None
         self._check(self._L.mixrt_linear_grad(self._h, ref, outs, dy.data_ptr(), stride,
-                                              dw.data_ptr(), _ptr(db), ws, size))
+                                              dw.data_ptr(), _ptr(db), ws[0], ws[1]))
         return dw, db
 
     def rotary(self, heads, pos, freq, axis, *, layout: str = "halves", inverse: bool = False,

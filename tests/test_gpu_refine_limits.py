@@ -180,3 +180,64 @@ def test_norm_gradient_of_many_equal_rows(r, dtype):
         say(f"off by {off / ref.U:.0f} u")
         # 128 rows, up to 8 steps that join a block's rows, the term and its sum
         assert off <= ref.U * (128 / 2 + 8 + terms)
+
+
+# --- scratch of captured calls ---------------------------------------------------------
+
+def test_a_captured_call_has_scratch_of_its_own(r):
+    """A replay may run beside eager calls or another graph of the same
+    context: it must not write where they do."""
+    g = _gen(2)
+    x = torch.randn((1, 30000, 32), generator=g).to(torch.float16).cuda()
+    dy = torch.randn((1, 30000, 32), generator=g).to(torch.float16).cuda()
+    stream = torch.cuda.Stream()
+    c = mixrt.Renderer(0, stream=stream)
+
+    def step():
+        y, stats, kept = c.group_norm_train(x, 8, act="silu")
+        return (y, *c.group_norm_backward(dy, kept, stats, act="silu"),
+                *c.linear_weight_grad(kept, dy.reshape(-1, 32)))
+
+    try:
+        torch.cuda.synchronize()
+        want = [t.clone() for t in step()]
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            outs = step()
+        assert all(torch.equal(a, b) for a, b in zip(step(), want))
+        scratch = c._ws[2]
+        for _ in range(3):
+            scratch.fill_(77)
+            for o in outs:
+                o.zero_()
+            torch.cuda.synchronize()
+            graph.replay()
+            torch.cuda.synchronize()
+            assert bool((scratch == 77).all())
+            assert all(torch.equal(a, b) for a, b in zip(outs, want))
+    finally:
+        c.close()
+    assert c._ws is None     # given back
+
+
+def test_a_capture_before_any_eager_call(r):
+    """The first call of a context may be a captured one."""
+    x = torch.randn((1, 30000, 32), generator=_gen(3)).to(torch.bfloat16).cuda()
+    want = r.group_norm(x, 8, act="relu")
+    stream = torch.cuda.Stream()
+    c = mixrt.Renderer(0, stream=stream)
+    try:
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            out = c.group_norm(x, 8, act="relu")
+        again = c.group_norm(x, 8, act="relu")
+        for _ in range(3):
+            out.zero_()
+            torch.cuda.synchronize()
+            graph.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(out, want) and torch.equal(again, want)
+    finally:
+        c.close()
