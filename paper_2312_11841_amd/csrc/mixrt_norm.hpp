@@ -215,7 +215,11 @@ inline NormPlan norm_plan(int N, int64_t P, int C, int G, int dtype, bool pad, b
 {
     NormPlan p{};
     const int size = dtype == kF32 ? 4 : 2, Cg = C / G;
-    const auto atmost = [](int64_t v, int64_t hi) { return v > hi ? hi : v < 1 ? 1 : v; };
+    // (1 where there are no pixels: a grid has a block)
+    const auto atmost = [](int64_t v, int64_t hi) {
+        if (v > hi) v = hi;
+        return v < 1 ? 1 : v;
+    };
     if (!back) {
         p.V = 16 / size;
         while (Cg % p.V) p.V >>= 1;

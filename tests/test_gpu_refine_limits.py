@@ -241,3 +241,38 @@ def test_a_capture_before_any_eager_call(r):
             assert torch.equal(out, want) and torch.equal(again, want)
     finally:
         c.close()
+
+
+# --- maps without pixels -----------------------------------------------------------------
+
+@pytest.mark.parametrize("shape", [(3, 0, 1024, 8), (1, 0, 4095, 1), (2, 0, 640, 640),
+                                   (70, 0, 8, 2)], ids=str)
+def test_maps_without_pixels(r, shape):
+    """Wide maps too: statistics of nothing, gradients 0."""
+    N, P, width, G = shape
+    say("no pixels", shape)
+    for dt in DT.values():
+        x = torch.empty((N, P, width), dtype=dt, device="cuda")
+        y, stats, kept = r.group_norm_train(x, G, eps=0.25)
+        assert y.shape == x.shape
+        assert torch.equal(stats.cpu(), torch.tensor([0.0, 2.0]).expand(N, G, 2))
+        for saved in (kept, x):
+            dx, dgamma, dbeta = r.group_norm_backward(x, saved, stats)
+            assert dx.shape == x.shape
+            assert float(dgamma.abs().sum()) == 0.0 == float(dbeta.abs().sum())
+
+
+def test_maps_without_pixels_from_c(r):
+    """Maps at addresses of their own, of which nothing is read."""
+    some = torch.zeros((64,), device="cuda")
+    norm = mixrt.Norm(2, 8, 0, 2, mixrt.MIXRT_F32, 1, 0.25, 0, 0)
+    stats = torch.zeros((2, 2, 2), device="cuda")
+    size = C.c_size_t()
+    assert r._L.mixrt_norm_workspace(C.byref(norm), C.byref(size)) == 0
+    ws = torch.empty((size.value,), dtype=torch.uint8, device="cuda")
+    r._check(r._L.mixrt_norm_forward(
+        r._h, C.byref(norm), C.byref(mixrt.Map(some.data_ptr(), 0, 8)),
+        C.byref(mixrt.Map(some.data_ptr() + 128, 0, 8)), stats.data_ptr(), None, ws.data_ptr(),
+        size.value))
+    r.sync()
+    assert torch.equal(stats.cpu(), torch.tensor([0.0, 2.0]).expand(2, 2, 2))
