@@ -557,7 +557,7 @@ def _rotary_plan(arrays, outs, pos, freq, axis, layout, inverse, device):
     axes = pos.shape[-1]
     tokens = pos.numel() // axes
     p = _Plan()
-    p.rotary = Rotary(tokens, axes, freq.shape[0], ROTARY_LAYOUTS[layout], int(bool(inverse)))
+    p.rotary = Rotary(tokens, axes, freq.shape[0], ROTARY_LAYOUTS[layout], int(inverse))
     p.rotary_ref = C.byref(p.rotary)
     p.heads = (Heads * len(arrays))()
     for i, (x, o) in enumerate(zip(arrays, outs)):
@@ -862,22 +862,26 @@ class Renderer:
     def _norm(self, x, groups, eps, act, name):
         """The plan of a norm over x, with x's address filled in."""
         _on_gpu(x, name, self.device)
+        # plain numbers: a tensor in the key would be known by its identity
+        whole, eps = int(groups), float(eps)
+        if whole != groups:
+            raise ValueError(f"groups: {groups!r}, expected a whole number")
 
         def make():
             images, pixels, channels, xmap = _as_map(x, name)
             if act not in ACTS:
                 raise ValueError(f"act: {act!r}, expected one of {tuple(ACTS)}")
             p = _Plan()
-            p.norm = Norm(images, channels, pixels, int(groups), _elem_code(x.dtype, name),
-                          ACTS[act], float(eps), 0, 0)
+            p.norm = Norm(images, channels, pixels, whole, _elem_code(x.dtype, name),
+                          ACTS[act], eps, 0, 0)
             p.bytes = self._size(self._L.mixrt_norm_workspace, C.byref(p.norm))
             p.x, p.channels = xmap, channels
             p.out = Map(0, pixels * channels, channels)     # a dense output
             p.norm_ref, p.x_ref, p.out_ref = (C.byref(t) for t in (p.norm, p.x, p.out))
-            p.stats, p.rows = (images, int(groups), 2), images * pixels
+            p.stats, p.rows = (images, whole, 2), images * pixels
             return p
 
-        p = self._plan((name, x.shape, x.stride(), x.dtype, groups, eps, act), make)
+        p = self._plan((name, x.shape, x.stride(), x.dtype, whole, eps, act), make)
         p.x.data = x.data_ptr()
         return p
 
@@ -1011,6 +1015,7 @@ class Renderer:
         tensors to write, each may be its input."""
         single = isinstance(heads, self._torch.Tensor)
         arrays = (heads,) if single else tuple(heads)
+        inverse = bool(inverse)
         # all that the checks look at is in the key, so they run once for each
         try:
             key = ("rotary", layout, inverse,

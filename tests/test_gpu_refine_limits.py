@@ -276,3 +276,32 @@ def test_maps_without_pixels_from_c(r):
         size.value))
     r.sync()
     assert torch.equal(stats.cpu(), torch.tensor([0.0, 2.0]).expand(2, 2, 2))
+
+
+# --- arguments that change between calls -----------------------------------------------
+
+def test_an_epsilon_that_changes_in_place(r):
+    x = torch.randn((1, 50, 8), generator=_gen(4)).cuda()
+    eps = torch.tensor(1e-3)
+    first = r.group_norm(x, 2, eps=eps)
+    assert torch.equal(first, r.group_norm(x, 2, eps=float(eps)))
+    eps.fill_(4.0)
+    assert torch.equal(r.group_norm(x, 2, eps=eps), r.group_norm(x, 2, eps=4.0))
+    groups = torch.tensor(2)
+    first = r.group_norm(x, groups)
+    groups.fill_(4)
+    assert torch.equal(r.group_norm(x, groups), r.group_norm(x, 4))
+    assert not torch.equal(first, r.group_norm(x, 4))
+    with pytest.raises(ValueError, match="groups"):
+        r.group_norm(x, 2.5)
+
+
+def test_a_direction_that_changes_in_place(r):
+    x = torch.randn((5, 2, 8), generator=_gen(5)).cuda()
+    pos, freq = torch.arange(5.0, device="cuda")[:, None], torch.ones(4, device="cuda")
+    axis = torch.zeros(4, dtype=torch.uint8, device="cuda")
+    way = torch.tensor(False)
+    assert torch.equal(r.rotary(x, pos, freq, axis, inverse=way), r.rotary(x, pos, freq, axis))
+    way.fill_(True)
+    assert torch.equal(r.rotary(x, pos, freq, axis, inverse=way),
+                       r.rotary(x, pos, freq, axis, inverse=True))
