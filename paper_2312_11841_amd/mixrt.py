@@ -477,7 +477,7 @@ def _like(t, name: str, shape, dtype, device: int):
     _on_gpu(t, name, device)
     if t.dtype != dtype:
         raise ValueError(f"{name}: dtype {t.dtype}, expected {dtype}")
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != shape:
         raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {tuple(shape)}")
 
 
@@ -529,7 +529,7 @@ def _per_channel(t, name: str, channels: int, device: int) -> int:
     if t is None:
         return 0
     _on_gpu(t, name, device)
-    if t.dim() != 1 or t.shape[0] != channels or _elem_code(t.dtype, name) != MIXRT_F32:
+    if t.shape != (channels,) or _elem_code(t.dtype, name) != MIXRT_F32:
         raise ValueError(f"{name}: {t.dtype} {tuple(t.shape)}, expected float32 ({channels},)")
     if not t.is_contiguous():
         raise ValueError(f"{name}: not contiguous")
@@ -605,6 +605,32 @@ class Checkpoint:
         return Kept(rows, channels, code, codes.data_ptr(), exps.data_ptr())
 
 
+_underived = None
+
+
+def _without_derivative(name: str, outs, inputs):
+    """outs as results of inputs that a graph follows: torch's backward pass
+    raises when it gets here, where it would else leave the gradients out."""
+    global _underived
+    if _underived is None:
+        import torch
+
+        class Underived(torch.autograd.Function):
+            @staticmethod
+            def forward(ctx, name, n, *tensors):
+                ctx.name = name
+                return tuple(t.detach() for t in tensors[:n])
+
+            @staticmethod
+            def backward(ctx, *grads):
+                raise RuntimeError(
+                    f"{ctx.name}: no derivative in torch's graph; call it in a "
+                    "torch.autograd.Function with its gradient's call, or on detached tensors")
+
+        _underived = Underived
+    return _underived.apply(name, len(outs), *outs, *inputs)
+
+
 # --- the library handle ------------------------------------------------------------
 
 class Renderer:
@@ -643,9 +669,10 @@ class Renderer:
         # the handle of torch's current stream (0.1 us; the public way takes 1)
         self._current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
             lambda d: torch.cuda.current_stream(d).cuda_stream)
-        self._is_capturing = torch.cuda.is_current_stream_capturing
-        # the refiner's operators' scratch: see _workspace
-        self._ws = None
+        self._is_capturing = getattr(torch._C, "_cuda_isCurrentStreamCapturing", None) or (
+            torch.cuda.is_current_stream_capturing)
+        # the refiner's operators' scratch and plans: see _workspace and _plan
+        self._ws, self._plans = None, {}
 
     def _check(self, rc: int):
         if rc != MIXRT_OK:
@@ -799,27 +826,24 @@ class Renderer:
     # arrays' shapes, strides and types: it is checked and laid out once for
     # each of them (a plan) and a call fills in its addresses.  Building the
     # descriptors anew takes 10 us and more, the launch of a small call 5.
-    def _plan(self, key, make):
-        plans = self.__dict__.setdefault("_plans", {})
-        plan = plans.get(key)
+    def _plan(self, key, make, *args):
+        plan = self._plans.get(key)
         if plan is None:
-            plan = make()
-            if len(plans) >= 256:
-                plans.clear()
-            plans[key] = plan
+            plan = make(*args)
+            if len(self._plans) >= 256:
+                self._plans.clear()
+            self._plans[key] = plan
         return plan
 
-    def _capturing(self) -> bool:
-        """Whether a graph captures this context's stream."""
-        if self._current_stream(self.device) == self._raw_stream:
-            return self._is_capturing()
-        with self._torch.cuda.stream(self.stream):
-            return self._is_capturing()
+    def _here(self) -> bool:
+        """Whether torch's current stream is this context's."""
+        return self._current_stream(self.device) == self._raw_stream
 
-    def _empty(self, shape, dtype):
+    def _empty(self, shape, dtype, here=None):
         """Device memory for an output.  Taken on this context's stream, so
-        that memory released to another stream is not handed out early."""
-        if self._current_stream(self.device) == self._raw_stream:
+        that memory released to another stream is not handed out early.  here:
+        see _here, for callers that have asked."""
+        if self._here() if here is None else here:
             if len(shape) == 2:     # a third less than empty
                 return self._torch.empty_strided(shape, (shape[1], 1), dtype=dtype,
                                                  device=self._dev)
@@ -827,19 +851,24 @@ class Renderer:
         with self._torch.cuda.stream(self.stream):
             return self._torch.empty(shape, dtype=dtype, device=self._dev)
 
-    def _empty_like(self, t):
-        """_empty of t's shape and type, dense."""
-        if t.is_contiguous() and self._current_stream(self.device) == self._raw_stream:
+    def _empty_like(self, t, here: bool):
+        """_empty of t's shape and type, dense; here: see _here."""
+        if here and t.is_contiguous():
             return self._torch.empty_like(t)
         return self._empty(t.shape, t.dtype)
 
-    def _workspace(self, size: int):
+    def _workspace(self, size: int, here: bool):
         """(address, bytes) of scratch for one call, at least size bytes, and
         its memory, to be held until the launch.  Eager calls run one after
         another on this context's stream and share one array.  A call that a
         graph captures has its own, from the graph's memory: a replay may run
         beside eager calls and beside other graphs."""
-        if self._capturing():
+        if here:
+            captured = self._is_capturing()
+        else:
+            with self._torch.cuda.stream(self.stream):
+                captured = self._is_capturing()
+        if captured:
             t = self._empty((max(size, 16),), self._torch.uint8)
             return t.data_ptr(), t.numel(), t
         if self._ws is None or self._ws[1] < size:
@@ -848,9 +877,24 @@ class Renderer:
             self._ws = (t.data_ptr(), t.numel(), t)
         return self._ws
 
-    def _checkpoint(self, rows: int, channels: int, dtype) -> Checkpoint:
-        return Checkpoint(self._empty((rows, channels), self._torch.int8),
-                          self._empty((rows, -(-channels // KEPT_GROUP)), self._torch.uint8), dtype)
+    def _checkpoint(self, rows: int, channels: int, dtype, here=None) -> Checkpoint:
+        return Checkpoint(self._empty((rows, channels), self._torch.int8, here),
+                          self._empty((rows, -(-channels // KEPT_GROUP)), self._torch.uint8, here),
+                          dtype)
+
+    def _result(self, name: str, outs, inputs):
+        """The outputs of a call of whose inputs (tensors, or None for some)
+        one requires a gradient.  (The callers ask for that first: 0.1 us.)"""
+        if self._torch.is_grad_enabled():
+            return _without_derivative(name, outs, [t for t in inputs if t is not None])
+        return outs
+
+    def _refuse_out(self, name: str, inputs):
+        """An output that the caller gave cannot carry a graph."""
+        if self._torch.is_grad_enabled() and any(t is not None and t.requires_grad
+                                                 for t in inputs):
+            raise RuntimeError(f"{name}: no derivative for out=..., but an input requires a "
+                               "gradient; call it under torch.no_grad() or on detached tensors")
 
     def _size(self, fn, *args) -> int:
         size = C.c_size_t()
@@ -863,45 +907,51 @@ class Renderer:
         """The plan of a norm over x, with x's address filled in."""
         _on_gpu(x, name, self.device)
         # plain numbers: a tensor in the key would be known by its identity
-        whole, eps = int(groups), float(eps)
-        if whole != groups:
-            raise ValueError(f"groups: {groups!r}, expected a whole number")
-
-        def make():
-            images, pixels, channels, xmap = _as_map(x, name)
-            if act not in ACTS:
-                raise ValueError(f"act: {act!r}, expected one of {tuple(ACTS)}")
-            p = _Plan()
-            p.norm = Norm(images, channels, pixels, whole, _elem_code(x.dtype, name),
-                          ACTS[act], eps, 0, 0)
-            p.bytes = self._size(self._L.mixrt_norm_workspace, C.byref(p.norm))
-            p.x, p.channels = xmap, channels
-            p.out = Map(0, pixels * channels, channels)     # a dense output
-            p.norm_ref, p.x_ref, p.out_ref = (C.byref(t) for t in (p.norm, p.x, p.out))
-            p.stats, p.rows = (images, whole, 2), images * pixels
-            return p
-
-        p = self._plan((name, x.shape, x.stride(), x.dtype, whole, eps, act), make)
+        if type(groups) is not int or type(eps) is not float:
+            whole, eps = int(groups), float(eps)
+            if whole != groups:
+                raise ValueError(f"groups: {groups!r}, expected a whole number")
+            groups = whole
+        key = (name, x.shape, x.stride(), x.dtype, groups, eps, act)
+        p = self._plans.get(key)
+        if p is None:
+            p = self._plan(key, self._norm_plan, x, groups, eps, act, name)
         p.x.data = x.data_ptr()
         return p
 
-    def _norm_out(self, p, like, out, name):
+    def _norm_plan(self, x, groups, eps, act, name):
+        images, pixels, channels, xmap = _as_map(x, name)
+        if act not in ACTS:
+            raise ValueError(f"act: {act!r}, expected one of {tuple(ACTS)}")
+        p = _Plan()
+        p.norm = Norm(images, channels, pixels, groups, _elem_code(x.dtype, name), ACTS[act],
+                      eps, 0, 0)
+        p.bytes = self._size(self._L.mixrt_norm_workspace, C.byref(p.norm))
+        p.x, p.channels = xmap, channels
+        p.out = Map(0, pixels * channels, channels)     # a dense output
+        p.norm_ref, p.x_ref, p.out_ref = (C.byref(t) for t in (p.norm, p.x, p.out))
+        p.stats, p.rows = (images, groups, 2), images * pixels
+        return p
+
+    def _norm_out(self, p, like, out, name, here):
         """(the output, its map's reference)."""
         if out is None:
-            out = self._empty_like(like)
+            out = self._empty_like(like, here)
             p.out.data = out.data_ptr()
             return out, p.out_ref
         _like(out, name, like.shape, like.dtype, self.device)
         return out, C.byref(_as_map(out, name)[3])
 
-    def _norm_forward(self, p, x, gamma, beta, out, stats, kept):
+    def _norm_forward(self, p, x, gamma, beta, out, stats, kept, here):
         p.norm.gamma = _per_channel(gamma, "gamma", p.channels, self.device)
         p.norm.beta = _per_channel(beta, "beta", p.channels, self.device)
-        out, out_ref = self._norm_out(p, x, out, "out")
+        out, out_ref = self._norm_out(p, x, out, "out", here)
         kd = None if kept is None else C.byref(kept.descriptor(self.device))
-        ws = self._workspace(p.bytes)
-        self._check(self._L.mixrt_norm_forward(self._h, p.norm_ref, p.x_ref, out_ref, stats, kd,
-                                               ws[0], ws[1]))
+        ws = self._workspace(p.bytes, here)
+        rc = self._L.mixrt_norm_forward(self._h, p.norm_ref, p.x_ref, out_ref, stats, kd, ws[0],
+                                        ws[1])
+        if rc:
+            self._check(rc)
         return out
 
     def group_norm(self, x, groups: int, gamma=None, beta=None, *, eps: float = 1e-5,
@@ -911,7 +961,13 @@ class Renderer:
         gamma, beta: float32 [channels] or None.  out: x's shape and type, or
         x itself."""
         p = self._norm(x, groups, eps, act, "x")
-        return self._norm_forward(p, x, gamma, beta, out, None, None)
+        if out is not None:
+            self._refuse_out("group_norm", (x, gamma, beta))
+        y = self._norm_forward(p, x, gamma, beta, out, None, None, self._here())
+        if (x.requires_grad or gamma is not None and gamma.requires_grad
+                or beta is not None and beta.requires_grad):
+            return self._result("group_norm", (y,), (x, gamma, beta))[0]
+        return y
 
     def group_norm_train(self, x, groups: int, gamma=None, beta=None, *, eps: float = 1e-5,
                          act: str = "none", out=None):
@@ -919,9 +975,16 @@ class Renderer:
         groups' (mean, 1 / deviation) as float32 [images, groups, 2], and x
         kept in 8 bits, which the same passes over x write."""
         p = self._norm(x, groups, eps, act, "x")
-        stats = self._empty(p.stats, self._torch.float32)
-        kept = self._checkpoint(p.rows, p.channels, x.dtype)
-        return (self._norm_forward(p, x, gamma, beta, out, stats.data_ptr(), kept), stats, kept)
+        if out is not None:
+            self._refuse_out("group_norm_train", (x, gamma, beta))
+        here = self._here()
+        stats = self._empty(p.stats, self._torch.float32, here)
+        kept = self._checkpoint(p.rows, p.channels, x.dtype, here)
+        y = self._norm_forward(p, x, gamma, beta, out, stats.data_ptr(), kept, here)
+        if (x.requires_grad or gamma is not None and gamma.requires_grad
+                or beta is not None and beta.requires_grad):
+            y, stats = self._result("group_norm_train", (y, stats), (x, gamma, beta))
+        return y, stats, kept
 
     def group_norm_backward(self, dy, saved, stats, gamma=None, beta=None, *, act: str = "none",
                             out=None):
@@ -940,20 +1003,30 @@ class Renderer:
         else:
             _like(saved, "saved", dy.shape, dy.dtype, self.device)
             xd = C.byref(_as_map(saved, "saved")[3])
+        x = None if xd is None else saved
+        if out is not None:
+            self._refuse_out("group_norm_backward", (dy, stats, gamma, beta, x))
         p.norm.gamma = _per_channel(gamma, "gamma", p.channels, self.device)
         p.norm.beta = _per_channel(beta, "beta", p.channels, self.device)
-        out, out_ref = self._norm_out(p, dy, out, "out")
-        grads = self._empty((2, p.channels), self._torch.float32)
+        here = self._here()
+        out, out_ref = self._norm_out(p, dy, out, "out", here)
+        grads = self._empty((2, p.channels), self._torch.float32, here)
         at = grads.data_ptr()
-        ws = self._workspace(p.bytes)
-        self._check(self._L.mixrt_norm_backward(self._h, p.norm_ref, p.x_ref, xd, kd,
-                                                stats.data_ptr(), out_ref, at,
-                                                at + 4 * p.channels, ws[0], ws[1]))
+        ws = self._workspace(p.bytes, here)
+        rc = self._L.mixrt_norm_backward(self._h, p.norm_ref, p.x_ref, xd, kd, stats.data_ptr(),
+                                         out_ref, at, at + 4 * p.channels, ws[0], ws[1])
+        if rc:
+            self._check(rc)
         dgamma, dbeta = grads.unbind(0)
+        if (dy.requires_grad or stats.requires_grad
+                or gamma is not None and gamma.requires_grad
+                or beta is not None and beta.requires_grad or x is not None and x.requires_grad):
+            return self._result("group_norm_backward", (out, dgamma, dbeta),
+                                (dy, stats, gamma, beta, x))
         return out, dgamma, dbeta
 
     def checkpoint_pack(self, x) -> Checkpoint:
-        """x [..., channels] kept in 8 bits."""
+        """x [..., channels] kept in 8 bits; the codes carry no gradient."""
         _on_gpu(x, "x", self.device)
 
         def make():
@@ -964,7 +1037,7 @@ class Renderer:
             return p
 
         p = self._plan(("pack", x.shape, x.stride(), x.dtype), make)
-        kept = self._checkpoint(p.rows, p.channels, x.dtype)
+        kept = self._checkpoint(p.rows, p.channels, x.dtype, self._here())
         p.kept.codes, p.kept.exps = kept.codes.data_ptr(), kept.exps.data_ptr()
         self._check(self._L.mixrt_kept_pack(self._h, p.kept_ref, x.data_ptr(), p.stride))
         return kept
@@ -997,11 +1070,16 @@ class Renderer:
         ref = C.byref(kd)
         need = self._plan(("linear", kd.rows, kd.channels, kd.dtype, outs),
                           lambda: self._size(self._L.mixrt_linear_grad_workspace, ref, outs))
-        ws = self._workspace(need)
-        dw = self._empty((kd.channels, outs), self._torch.float32)
-        db = self._empty((outs,), self._torch.float32) if bias else None
+        here = self._here()
+        ws = self._workspace(need, here)
+        dw = self._empty((kd.channels, outs), self._torch.float32, here)
+        db = self._empty((outs,), self._torch.float32, here) if bias else None
         self._check(self._L.mixrt_linear_grad(self._h, ref, outs, dy.data_ptr(), stride,
                                               dw.data_ptr(), _ptr(db), ws[0], ws[1]))
+        if dy.requires_grad and bias:
+            return self._result("linear_weight_grad", (dw, db), (dy,))
+        if dy.requires_grad:
+            return self._result("linear_weight_grad", (dw,), (dy,))[0], None
         return dw, db
 
     def rotary(self, heads, pos, freq, axis, *, layout: str = "halves", inverse: bool = False,
@@ -1027,8 +1105,10 @@ class Renderer:
         except AttributeError:
             raise TypeError("heads, pos, freq and axis: expected torch.Tensors") from None
         if out is None:
-            outs = tuple([self._empty_like(x) for x in arrays])
+            here = self._here()
+            outs = tuple([self._empty_like(x, here) for x in arrays])
         else:
+            self._refuse_out("rotary", (*arrays, pos, freq))
             outs = (out,) if single else tuple(out)
             if len(outs) != len(arrays):
                 raise ValueError(f"{len(arrays)} arrays and {len(outs)} outputs")
@@ -1042,6 +1122,9 @@ class Renderer:
         for d, x, o in zip(p.heads, arrays, outs):
             d.x, d.out = x.data_ptr(), o.data_ptr()
         self._check(self._L.mixrt_rotary_apply(self._h, p.rotary_ref, p.heads, len(arrays)))
+        if (arrays[0].requires_grad or arrays[-1].requires_grad or pos.requires_grad
+                or freq.requires_grad):
+            outs = self._result("rotary", outs, (*arrays, pos, freq))
         return outs[0] if single else outs
 
 

@@ -305,3 +305,47 @@ def test_a_direction_that_changes_in_place(r):
     way.fill_(True)
     assert torch.equal(r.rotary(x, pos, freq, axis, inverse=way),
                        r.rotary(x, pos, freq, axis, inverse=True))
+
+
+# --- gradients that a graph asks for ----------------------------------------------------
+
+def test_a_gradient_is_refused_rather_than_dropped(r):
+    """The calls have no derivative for torch's graph: a backward pass that
+    reaches one says so, and values are as without a graph."""
+    g = _gen(6)
+    x = torch.randn((1, 50, 8), generator=g).cuda()
+    gamma = torch.ones(8, device="cuda")
+    q = torch.randn((5, 2, 8), generator=g).cuda()
+    pos, freq = torch.arange(5.0, device="cuda")[:, None], torch.ones(4, device="cuda")
+    axis = torch.zeros(4, dtype=torch.uint8, device="cuda")
+    _, stats, kept = r.group_norm_train(x, 2, gamma)
+    calls = {
+        "group_norm": (lambda a: r.group_norm(a, 2, gamma), x),
+        "group_norm gamma": (lambda a: r.group_norm(x, 2, a), gamma),
+        "group_norm_train": (lambda a: r.group_norm_train(a, 2, gamma)[0], x),
+        "group_norm_train stats": (lambda a: r.group_norm_train(a, 2, gamma)[1], x),
+        "group_norm_backward": (lambda a: r.group_norm_backward(a, kept, stats, gamma)[0], x),
+        "group_norm_backward dgamma": (lambda a: r.group_norm_backward(a, kept, stats,
+                                                                       gamma)[1], x),
+        "linear_weight_grad": (lambda a: r.linear_weight_grad(kept, a)[0], x),
+        "rotary": (lambda a: r.rotary(a, pos, freq, axis), q),
+        "rotary keys": (lambda a: r.rotary((q, a), pos, freq, axis)[1], q),
+    }
+    for name, (call, at) in calls.items():
+        want = call(at)
+        assert not want.requires_grad, name
+        leaf = at.clone().requires_grad_()
+        with torch.no_grad():
+            assert not call(leaf).requires_grad, name
+        got = call(leaf)
+        assert torch.equal(got, want), name
+        other = torch.ones((), device="cuda", requires_grad=True)
+        with pytest.raises(RuntimeError, match=name.split()[0]):
+            (got * other).sum().backward()
+        assert leaf.grad is None, name
+        if name in ("group_norm", "rotary"):
+            with pytest.raises(RuntimeError, match="out"):
+                if name == "rotary":
+                    r.rotary(leaf, pos, freq, axis, out=torch.empty_like(q))
+                else:
+                    r.group_norm(leaf, 2, gamma, out=torch.empty_like(x))
