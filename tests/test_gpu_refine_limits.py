@@ -349,3 +349,50 @@ def test_a_gradient_is_refused_rather_than_dropped(r):
                     r.rotary(leaf, pos, freq, axis, out=torch.empty_like(q))
                 else:
                     r.group_norm(leaf, 2, gamma, out=torch.empty_like(x))
+
+
+# --- the activations' tails ----------------------------------------------------------------
+
+def _at(r, z, act):
+    """(act(z), its slope) by the norm's kernels: with gamma 0, z is beta."""
+    z = z.float().cuda()
+    width = z.numel()
+    x = torch.linspace(-1, 1, width, device="cuda").reshape(1, 1, width)
+    gamma = torch.zeros(width, device="cuda")
+    y, stats, _ = r.group_norm_train(x, 1, gamma, z, act=act)
+    slope = r.group_norm_backward(torch.ones_like(x), x, stats, gamma, z, act=act)[2]
+    return y.double().cpu().reshape(-1), slope.double().cpu()
+
+
+def test_gelu_keeps_its_relative_accuracy_in_the_negative_tail(r):
+    """Half of erfc(|z| / sqrt 2) is good to (24 + 2 z^2) u: its exponent z^2 / 2
+    carries three roundings, which act on the value z^2 / 2 times each; 2.6 u of
+    the polynomial, 9 for its argument, the rest for the operations."""
+    z = torch.linspace(-8, 8, 4001).float().double()
+    y, slope = _at(r, z, "gelu")
+    half = 0.5 * torch.erfc(z.abs() / math.sqrt(2))
+    phi = torch.where(z < 0, half, 1 - half)
+    density = torch.exp(-z * z / 2) / math.sqrt(2 * math.pi)
+    rel = ref.U * (24 + 2 * z * z)
+    want = z * phi
+    bound = z.abs() * half * rel + 2 * ref.U * want.abs()
+    assert bool(((y - want).abs() <= bound).all()), float(((y - want).abs() / bound).max())
+    want = phi + z * density
+    bound = (half + z.abs() * density) * rel + 2 * ref.U * (phi + want.abs())
+    assert bool(((slope - want).abs() <= bound).all()), float(((slope - want).abs() / bound).max())
+
+
+def test_silu_keeps_its_relative_accuracy_in_the_negative_tail(r):
+    """exp(-z) is good to (2 |z| + 4) u, as its argument in bits is a rounded
+    product with a rounded constant; four more operations.  The slope
+    s (1 + z (1 - s)) is a sum of s and z s (1 - s)."""
+    z = torch.linspace(-80, 40, 4001).float().double()
+    y, slope = _at(r, z, "silu")
+    s = torch.sigmoid(z)
+    rel = ref.U * (2 * z.abs() + 12)
+    assert bool(((y - z * s).abs() <= (z * s).abs() * rel).all())
+    rest = torch.sigmoid(-z)
+    want = s + z * s * rest
+    # the kernel forms 1 - s as a difference: u of z beside what it leaves
+    bound = (s + z.abs() * s * rest) * rel + 4 * ref.U * z.abs() * s
+    assert bool(((slope - want).abs() <= bound).all()), float(((slope - want).abs() / bound).max())
