@@ -396,3 +396,26 @@ def test_silu_keeps_its_relative_accuracy_in_the_negative_tail(r):
     # the kernel forms 1 - s as a difference: u of z beside what it leaves
     bound = (s + z.abs() * s * rest) * rel + 4 * ref.U * z.abs() * s
     assert bool(((slope - want).abs() <= bound).all()), float(((slope - want).abs() / bound).max())
+
+
+# --- activations of extreme size ---------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("size", [1e24, 1e-24, 1e34, 1e-34])
+def test_gradient_of_activations_of_extreme_size(r, size, dtype):
+    """1 / deviation squared leaves the range of 32 bits; dx does not."""
+    g = _gen(7)
+    shapes = [(1, 64, 8, 2), (2, 20000, 16, 2)]
+    for N, P, width, G in shapes:
+        x0 = torch.randn((N, P, width), generator=g)
+        x = (x0 * size).to(DT[dtype]).cuda()
+        dy = (x0 + 0.1 * torch.randn((N, P, width), generator=g)).to(DT[dtype]).cuda()
+        _, stats, _ = r.group_norm_train(x, G, eps=0.0, act="silu")
+        gamma, beta = torch.ones(width), torch.zeros(width)
+        for kind in ("none", "silu"):
+            dx, dgamma, dbeta = r.group_norm_backward(dy, x, stats, act=kind)
+            want, bound = ref.norm_back(dy.cpu(), x.cpu(), stats.cpu(), gamma, beta, kind,
+                                        DT[dtype])
+            for name, got in (("dx", dx), ("dgamma", dgamma), ("dbeta", dbeta)):
+                over = (got.double().cpu() - want[name]).abs() - bound[name]
+                assert float(over.max()) <= 0, (size, kind, name, P)
