@@ -122,7 +122,7 @@ __global__ __launch_bounds__(kThreads) void kept_unpack_kernel(const int8_t *cod
 // path through which every tile's rows go again, busy 80% of the time (100,000
 // rows, 512 x 512, bf16: 121 us, 433 TFLOP/s; 3600 rows, 512 x 1536, f16: 21
 // us).  Wide loads turned by way of LDS instead took 110 us of the first, no
-// less of the second, and 250 us where f32 takes 187 (100,000 rows, 320 x 320; 110
+// less of the second, and 250 us where f32 takes 183 (100,000 rows, 320 x 320; 112
 // TFLOP/s).
 
 constexpr int kTile = 64;     // channels of a wave's block of dw, each way
@@ -705,8 +705,9 @@ struct LinearPlan {
 // One part needs no join.  (720p rows, 64 x 64: 256 parts 40.6 us, 512 41.2, 128
 // 50.8; 3600 rows, 512 x 1536, f16: one part 21.6, two with their join 24.2,
 // five 29.6; 100,000 rows, 512 x 512: 8 parts 121, 4 143, 16 140.)  Narrow layers:
-// two runs of loads a lane at least, and 2 blocks a CU at most (2,000,000 rows of
-// one by one: 9 us more a call with 1, 4 with 3).
+// two runs of loads a lane at least, and 2 blocks a CU (2,000,000 rows of one by
+// one: 9 us more a call with 1, 4 with 3) or as many parts as leave a lane about
+// kNarrowRows rows.
 LinearPlan linear_plan(int64_t rows, int C, int outs, int dtype)
 {
     LinearPlan p;

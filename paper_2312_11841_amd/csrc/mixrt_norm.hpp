@@ -23,9 +23,8 @@ inline constexpr int kThreads = 256;
 inline constexpr int kSmallThreads = 1024;
 inline constexpr int kJoinThreads = 1024;
 // Rows a thread loads before it uses the first.  The backward's sums take one
-// at a time: they are bound by their arithmetic and gain from more waves (8 x
-// 360p x 64 in bf16: 95 us, with two 106, four 135; its writing 136 with one,
-// 123 with two, 104 with four).
+// at a time: they gain more from more waves (8 x 360p x 64 in bf16: 97 us, with
+// two 106, four 135; its writing 136 with one, 123 with two, 104 with four).
 inline constexpr int kAhead = 4;
 // Most rows that a thread of the backward's sums adds up in 32 bits: each addition
 // rounds what is there, so equal terms are off by half as many units at most.

@@ -50,9 +50,9 @@ __device__ __forceinline__ bool far_deviation(const float (&rstd)[V])
 
 // Sums of dz and dz xh per channel over one part of an image: in 32 bits within
 // a thread, whose rows are kBackRows at most, and in up to 8 steps over a block's
-// rows; in 64 bits where the parts are joined.  Bound by its arithmetic, 13 steps, an exponential
-// and a reciprocal an element (8 x 360p x 64 channels in bf16, silu: 361 MB in
-// 101 us, 3.6 TB/s).
+// rows; in 64 bits where the parts are joined.  Bound by the vector memory path
+// (8 x 360p x 64 channels in bf16, silu: 361 MB in 97 us, 3.7 TB/s; data return
+// busy 82% of the time, ALUs 53%, waves waiting for loads 74% of theirs).
 template <typename T, int V, int ACT, bool KEPT>
 __global__ __launch_bounds__(kThreads) void norm_back_sums_kernel(NormK k)
 {
@@ -189,7 +189,7 @@ __global__ __launch_bounds__(kThreads) void norm_affine_kernel(NormK k)
 
 // dx; the first block also writes dgamma and dbeta, over all images.  FOLD:
 // the block joins the image's few parts itself.  Bound by its stream (8 x 360p x
-// 64 channels in bf16: 597 MB in 108 us, 5.5 TB/s).
+// 64 channels in bf16: 597 MB in 106 us, 5.6 TB/s).
 template <typename T, int V, int ACT, bool KEPT, bool FOLD>
 __global__ __launch_bounds__(kThreads) void norm_back_apply_kernel(NormK k)
 {
