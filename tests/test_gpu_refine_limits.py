@@ -419,3 +419,18 @@ def test_gradient_of_activations_of_extreme_size(r, size, dtype):
             for name, got in (("dx", dx), ("dgamma", dgamma), ("dbeta", dbeta)):
                 over = (got.double().cpu() - want[name]).abs() - bound[name]
                 assert float(over.max()) <= 0, (size, kind, name, P)
+
+
+@pytest.mark.parametrize("act", ["none", "relu", "silu", "gelu"])
+def test_activations_of_values_that_are_not_finite(r, act):
+    """A NaN stays one in the value and in the slope; plus infinity is its own
+    value where the activation is not a step."""
+    z = torch.tensor([math.nan, math.inf, 1e30, -1e30, 0.0])
+    y, slope = _at(r, z, act)
+    assert math.isnan(y[0]) and (act == "none" or math.isnan(slope[0]))
+    assert y[1] == math.inf
+    assert y[2] == float(z[2].double()) and y[4] == 0.0
+    assert float(y[3]) == (float(z[3].double()) if act == "none" else 0.0)
+    if act != "none":
+        assert slope[2] == 1.0 and slope[3] == 0.0
+        assert slope[4] == (0.0 if act == "relu" else 0.5)
