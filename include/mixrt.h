@@ -430,8 +430,9 @@ int mixrt_rasterize(mixrt_ctx *ctx, const mixrt_mesh *mesh, int32_t views, int32
  * feature maps [views][H*W][channels] (channels last, as the frames are) and
  * layers on patch tokens whose position is (view, row, column).  These entry
  * points serve and train it: group norm with an activation, activations kept
- * in 8 bits for the backward pass, the gradients computed from them, and
- * rotary positions with several axes.  They use no context memory: where a
+ * in 8 bits for the backward pass, the gradients computed from them, rotary
+ * positions with several axes (alone, or with a norm of each head in the same
+ * pass), and attention with a learned bias by relative position.  They use no context memory: where a
  * call needs device scratch, the caller passes a workspace of the size that
  * the *_workspace function (pure host) states, 16-byte aligned, with any
  * contents; it must not be shared by calls that run at the same time.  An
@@ -573,6 +574,117 @@ typedef struct {
 #define MIXRT_MAX_HEADS_ARRAYS 2
 int mixrt_rotary_apply(mixrt_ctx *ctx, const mixrt_rotary *rotary, const mixrt_heads *heads,
                        int32_t n);
+
+/* Heads normed one by one and turned in the same pass: with
+ * r = 1 / sqrt(mean over the head's elements of x^2 + eps),
+ *   out = turn(x r weight), the turn as in mixrt_rotary_apply.
+ * weight: device float [head_dim], shared by the array's heads, or NULL: 1.
+ * Backward, at the gradient dy of out, with u = dy turned back, t = u weight
+ * and xh = x r:
+ *   dx = r (t - xh mean(t xh)),  dweight[d] = sum over tokens and heads u xh. */
+typedef struct {
+    int32_t heads;        /* >= 0, at most 65535 */
+    int32_t head_dim;     /* 1..1024 */
+    int32_t dtype;        /* of x, dy and out: MIXRT_F32, _F16 or _BF16 */
+    const float *weight;
+    const void *x;
+    const void *dy;       /* backward only */
+    void *out;            /* forward: out, may be x with x's strides; backward:
+                             dx, may be dy with dy's strides, or NULL */
+    float *dweight;       /* backward: device float [head_dim], or NULL */
+    int64_t x_token_stride, x_head_stride, dy_token_stride, dy_head_stride, out_token_stride,
+        out_head_stride;
+} mixrt_normed_heads;
+
+/* rotary.inverse is not read.  eps >= 0, finite.  Arguments else as for
+ * mixrt_rotary_apply; workspace bytes of the backward pass (pure host: data
+ * is not read, of the arrays heads, head_dim and dtype count). */
+int mixrt_rotary_norm_apply(mixrt_ctx *ctx, const mixrt_rotary *rotary, float eps,
+                            const mixrt_normed_heads *heads, int32_t n);
+int mixrt_rotary_norm_workspace(const mixrt_rotary *rotary, const mixrt_normed_heads *heads,
+                                int32_t n, size_t *bytes);
+int mixrt_rotary_norm_backward(mixrt_ctx *ctx, const mixrt_rotary *rotary, float eps,
+                               const mixrt_normed_heads *heads, int32_t n, void *workspace,
+                               size_t workspace_bytes);
+
+#define MIXRT_MAX_ATTENTION_DIM 128
+#define MIXRT_MAX_BIAS_AXES 3
+#define MIXRT_MAX_BIAS_BUCKETS 32
+#define MIXRT_MAX_BIAS_REACH 127
+
+/* Attention of queries to keys and values of their own number (a view's tokens
+ * to those of other views, or to themselves):
+ *   S[i][j] = scale q_i k_j + bias_ij,  P = softmax of S's rows over j < lens[b],
+ *   out_i = sum_j P_ij v_j.
+ * Query head h reads key head h / (heads / kv_heads).  A row for which no key
+ * is left (lens 0, or a bias of -infinity everywhere) gives 0. */
+typedef struct {
+    int32_t batch;        /* 0..65535 */
+    int32_t heads;        /* 1..65535 */
+    int32_t kv_heads;     /* divides heads */
+    int32_t head_dim;     /* 1..MIXRT_MAX_ATTENTION_DIM */
+    int32_t dtype;        /* of all heads: MIXRT_F32, _F16 or _BF16 */
+    float scale;          /* > 0, finite */
+    int64_t queries;      /* >= 0, < 2^30 */
+    int64_t keys;         /* >= 0, < 2^30 */
+    const int32_t *lens;  /* device [batch]: valid keys of each entry, or NULL:
+                             all (below 0 is taken as 0, above keys as keys).
+                             Keys and values behind are never read. */
+} mixrt_attention;
+
+/* A learned bias by the buckets of relative positions: with the distance
+ * d = k_pos[j][a] - q_pos[i][a] of each axis, cut to -reach .. reach,
+ *   bias_ij of head h = sum over axes of table[a][buckets[a][d + reach]][h]. */
+typedef struct {
+    int32_t axes;             /* 1..MIXRT_MAX_BIAS_AXES */
+    int32_t count;            /* buckets of an axis, 1..MIXRT_MAX_BIAS_BUCKETS */
+    int32_t reach;            /* 0..MIXRT_MAX_BIAS_REACH */
+    const float *table;       /* device [axes][count][heads] */
+    const uint8_t *buckets;   /* device [axes][2 reach + 1], each below count (a
+                                 larger one is taken as count - 1) */
+    const int32_t *q_pos;     /* device [queries][axes] of each entry */
+    const int32_t *k_pos;     /* device [keys][axes] of each entry */
+    int64_t q_pos_stride;     /* elements from an entry's positions to the next's, */
+    int64_t k_pos_stride;     /* 0: the same for all */
+} mixrt_relative_bias;
+
+/* Heads of a sequence in device memory: element (entry, token, head, d) at
+ * data[entry * batch_stride + token * token_stride + head * head_stride + d].
+ * Strides in elements, at least 0 for inputs; the elements of an output must
+ * not overlap.  Aligned to its element type. */
+typedef struct {
+    void *data;
+    int64_t batch_stride, token_stride, head_stride;
+} mixrt_sequence;
+
+/* Workspace bytes of a forward (backward = 0) or backward call. */
+int mixrt_attention_workspace(const mixrt_attention *att, const mixrt_relative_bias *bias,
+                              int32_t backward, size_t *bytes);
+
+/* out = attention.  For a backward pass: lse (device float [batch][heads]
+ * [queries], or NULL): log2 of the sum of 2^(S log2(e)) of each row, +infinity
+ * for a row without keys; rest (device [batch][queries][heads][head_dim] of
+ * dtype, or NULL; F16 and BF16 only): what rounding took from out, in F16 times
+ * 4096.  bias: NULL for none. */
+int mixrt_attention_forward(mixrt_ctx *ctx, const mixrt_attention *att,
+                            const mixrt_relative_bias *bias, const mixrt_sequence *q,
+                            const mixrt_sequence *k, const mixrt_sequence *v,
+                            const mixrt_sequence *out, float *lse, void *rest, void *workspace,
+                            size_t workspace_bytes);
+
+/* Gradients at dout, with out, lse and rest as the forward call wrote them (rest
+ * NULL for F32 only):
+ *   dP = dout v, dS = P (dP - sum_d dout out), dq = scale dS k,
+ *   dk = scale dS^T q and dv = P^T dout, summed over the query heads of a key
+ *   head, 0 for keys behind lens; dtable (device float [axes][count][heads], or
+ *   NULL): the sum of dS over the entries' pairs of each bucket. */
+int mixrt_attention_backward(mixrt_ctx *ctx, const mixrt_attention *att,
+                             const mixrt_relative_bias *bias, const mixrt_sequence *dout,
+                             const mixrt_sequence *q, const mixrt_sequence *k,
+                             const mixrt_sequence *v, const mixrt_sequence *out,
+                             const float *lse, const void *rest, const mixrt_sequence *dq,
+                             const mixrt_sequence *dk, const mixrt_sequence *dv, float *dtable,
+                             void *workspace, size_t workspace_bytes);
 
 /* ---- errors ------------------------------------------------------------------- */
 

@@ -22,7 +22,9 @@ OBJ_DIR = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libmixrt.so")
 COMMON_SOURCES = ["mixrt_api.cpp", "mixrt_mesh.cpp", "mixrt_stages.hip", "mixrt_raycast.hip",
                   "mixrt_raster.hip", "mixrt_refine_api.cpp", "mixrt_norm.hip",
-                  "mixrt_norm_back.hip", "mixrt_kept.hip", "mixrt_rotary.hip"]
+                  "mixrt_norm_back.hip", "mixrt_kept.hip", "mixrt_rotary.hip",
+                  "mixrt_rotary_norm.hip", "mixrt_attend_api.cpp", "mixrt_attend_f32.hip",
+                  "mixrt_attend_f16.hip", "mixrt_attend_bf16.hip"]
 RENDER_SOURCE = "mixrt_render.hip"
 SOURCES = COMMON_SOURCES + [RENDER_SOURCE]
 MB_LIB = os.path.join(PKG, "libmixrt_microbench.so")
@@ -59,7 +61,8 @@ def variant_lib(name: str) -> str:
 
 def build(verbose: bool = False, extra=(), variants: bool = True) -> str:
     os.makedirs(OBJ_DIR, exist_ok=True)
-    jobs = [(s, ()) for s in COMMON_SOURCES + [RENDER_SOURCE] + MB_SOURCES]
+    # (the longest first)
+    jobs = [(s, ()) for s in COMMON_SOURCES[::-1] + [RENDER_SOURCE] + MB_SOURCES]
     if variants:
         jobs += [(RENDER_SOURCE, (f"-D{d}",)) for d in VARIANTS.values()]
     with ThreadPoolExecutor(max_workers=min(8, os.cpu_count() or 1)) as ex:

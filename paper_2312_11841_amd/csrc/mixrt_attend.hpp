@@ -1,0 +1,76 @@
+// The refiner's attention: launch interface between the C ABI
+// (mixrt_attend_api.cpp) and the kernels (mixrt_attend_kernels.hpp, built for
+// one element type each).
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+namespace mixrt {
+
+inline constexpr int kMaxBiasAxes = 3;
+inline constexpr int kMaxBuckets = 32;
+inline constexpr int kMaxReach = 127;
+inline constexpr int kMaxAttendDim = 128;
+
+// An array of heads [batch][token][head][d]: strides in elements.
+struct SeqK {
+    void *data;
+    int64_t batch, token, head;
+};
+
+struct BiasK {
+    int axes;                 // 0: none
+    int buckets, reach;
+    const float *table;       // [axes][buckets][heads]
+    const uint8_t *map;       // [axes][2 reach + 1]
+    const int32_t *qpos, *kpos;   // [tokens][axes]
+    int64_t qbatch, kbatch;   // elements from one batch entry's to the next's
+};
+
+struct AttendK {
+    int B, H, Hk, D, Tq, Tk;
+    int dtype;
+    float scale;              // of q k, times log2(e)
+    float plain_scale;
+    const int32_t *lens;      // [B] or null
+    BiasK bias;
+    SeqK q, k, v, o;
+    void *rest;               // [B][Tq][H][D], dense, or null
+    float *lse;               // [B][H][Tq] or null
+    // backward
+    SeqK dout, dq, dk, dv;
+    float *dtable;
+    // how the work is dealt (see AttendPlan)
+    int pack, blocks, splits, per;
+    float *part, *part_lse, *delta, *part_table;
+};
+
+// How a call is split.  Forward: a block takes cols columns (a column is a
+// token and one of pack heads that share their keys) and per keys; queries'
+// gradient: likewise, pack 1; keys' gradient: a block takes cols keys and per
+// (head of the group, token) rows.
+struct AttendPlan {
+    int narrow;               // forward: one wave a block (few columns)
+    int pack;
+    int cols, blocks;         // columns of a block, blocks of one head
+    int splits, per;
+};
+
+AttendPlan plan_attend(int B, int H, int Hk, int64_t Tq, int64_t Tk, int D, int dtype, int axes);
+AttendPlan plan_attend_dq(int B, int H, int Hk, int64_t Tq, int64_t Tk, int D, int dtype, int axes);
+AttendPlan plan_attend_dkv(int B, int H, int Hk, int64_t Tq, int64_t Tk, int D, int dtype,
+                           int axes);
+
+// Launches of one element type.
+hipError_t launch_attend_f32(const AttendK &k, int stage, hipStream_t stream);
+hipError_t launch_attend_f16(const AttendK &k, int stage, hipStream_t stream);
+hipError_t launch_attend_bf16(const AttendK &k, int stage, hipStream_t stream);
+enum { kAttendForward, kAttendBackQ, kAttendBackKV };
+
+inline int attend_elem(int dtype) { return dtype == 0 ? 4 : 2; }
+// Head widths the kernels are built for: multiples of 32.
+inline int attend_dim(int D) { return D <= 32 ? 32 : D <= 64 ? 64 : D <= 96 ? 96 : 128; }
+
+}  // namespace mixrt

@@ -1,0 +1,543 @@
+// C ABI of the refiner's attention and of its heads' norm (declared in
+// include/mixrt.h): checks of their descriptors (pure host code), how a call is
+// split, and the launches of the kernels in mixrt_attend_*.hip and
+// mixrt_rotary_norm.hip on the context's stream.
+#include "mixrt.h"
+
+#include <cmath>
+
+#include "mixrt_attend.hpp"
+#include "mixrt_ctx.hpp"
+#include "mixrt_refine.hpp"
+
+namespace mixrt {
+namespace {
+
+constexpr int kCUs = 256;
+
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// Keys (or rows) that one chain of 32-bit sums takes at most, a multiple of 64: the
+// matrix instructions of float32 add two terms, those of the 16-bit types 16, and a
+// chain is about 1024 or 2048 of them, so that its roundings stay below the result's.
+int64_t longest(int dtype) { return attend_elem(dtype) == 4 ? 2048 : 32768; }
+
+// Splits of a walk over n rows so that about want blocks run, none shorter than
+// least, and none longer than the type's chains; per is a multiple of step.
+void split(int64_t n, int64_t blocks, int64_t want, int64_t least, int64_t most, int64_t step,
+           int *splits, int *per)
+{
+    int64_t s = blocks > 0 ? want / blocks : 1;
+    if (s > n / least) s = n / least;
+    if (s < ceil_div(n, most)) s = ceil_div(n, most);
+    if (s < 1) s = 1;
+    int64_t p = ceil_div(ceil_div(n, s), step) * step;
+    if (p < step) p = step;
+    *per = (int)p;
+    *splits = (int)(n > 0 ? ceil_div(n, p) : 1);
+}
+
+}  // namespace
+
+AttendPlan plan_attend(int B, int H, int Hk, int64_t Tq, int64_t Tk, int D, int dtype, int axes)
+{
+    AttendPlan p{};
+    p.pack = 1;
+    // few queries: the heads that share keys lie beside each other in the columns
+    if (Tq <= 16)
+        for (int n = 2; n <= 8; ++n)
+            if (H / Hk % n == 0 && Tq * n <= 32) p.pack = n;
+    const int64_t cols = Tq * p.pack, heads = (int64_t)B * (H / p.pack);
+    p.narrow = cols <= 32;
+    p.cols = p.narrow ? 32 : 128;
+    if (attend_elem(dtype) == 2 && D <= 64 && !p.narrow && heads * ceil_div(cols, 256) >= kCUs)
+        p.cols = 256;
+    p.blocks = (int)ceil_div(cols, p.cols);
+    if (p.blocks < 1) p.blocks = 1;
+    split(Tk, heads * p.blocks, p.narrow ? 4 * kCUs : 2 * kCUs, p.narrow ? 128 : 512,
+          longest(dtype), 64, &p.splits, &p.per);
+    return p;
+}
+
+AttendPlan plan_attend_dq(int B, int H, int Hk, int64_t Tq, int64_t Tk, int D, int dtype, int axes)
+{
+    AttendPlan p{};
+    p.pack = 1;
+    p.cols = 128;
+    const int64_t heads = (int64_t)B * H;
+    if (attend_elem(dtype) == 2 && D <= 64 && heads * ceil_div(Tq, 256) >= kCUs) p.cols = 256;
+    p.blocks = (int)ceil_div(Tq, p.cols);
+    if (p.blocks < 1) p.blocks = 1;
+    split(Tk, heads * p.blocks, 2 * kCUs, 512, longest(dtype), 32, &p.splits, &p.per);
+    return p;
+}
+
+AttendPlan plan_attend_dkv(int B, int H, int Hk, int64_t Tq, int64_t Tk, int D, int dtype,
+                           int axes)
+{
+    AttendPlan p{};
+    p.pack = 1;
+    p.cols = 128;
+    p.blocks = (int)ceil_div(Tk, p.cols);
+    if (p.blocks < 1) p.blocks = 1;
+    // in tiles of 32 rows, the group's heads one after another
+    const int64_t tiles = H / Hk * ceil_div(Tq, 32);
+    split(tiles, (int64_t)B * Hk * p.blocks, 2 * kCUs, 16, longest(dtype) / 32, 1, &p.splits,
+          &p.per);
+    return p;
+}
+
+}  // namespace mixrt
+
+namespace {
+
+using mixrt::AttendPlan;
+using mixrt::bind_device;
+using mixrt::clear_err;
+using mixrt::fail;
+using mixrt::finish_launch;
+
+constexpr int64_t kMaxElements = (int64_t)1 << 40;
+constexpr int64_t kMaxStride = (int64_t)1 << 40;
+constexpr int64_t kMaxTokens = (int64_t)1 << 30;
+constexpr int kMaxHeads = 65535;
+constexpr int kMaxHeadDim = 1024;
+
+bool aligned(const void *p, size_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
+
+int elem_size(int dtype)
+{
+    return dtype == MIXRT_F32 ? 4 : dtype == MIXRT_F16 || dtype == MIXRT_BF16 ? 2 : 0;
+}
+
+int check_workspace(mixrt_ctx *ctx, const void *ws, size_t have, size_t need)
+{
+    if (have < need)
+        return fail(ctx, MIXRT_EINVAL, "workspace of %zu bytes, needs %zu", have, need);
+    if (need && !ws) return fail(ctx, MIXRT_EINVAL, "workspace is NULL");
+    if (!aligned(ws, 16)) return fail(ctx, MIXRT_EINVAL, "workspace not 16-byte aligned");
+    return MIXRT_OK;
+}
+
+// --- attention --------------------------------------------------------------------
+
+int check_attention(mixrt_ctx *ctx, const mixrt_attention *a)
+{
+    if (!a) return fail(ctx, MIXRT_EINVAL, "attention is NULL");
+    if (a->batch < 0) return fail(ctx, MIXRT_EINVAL, "attention.batch=%d", a->batch);
+    if (a->batch > 65535)
+        return fail(ctx, MIXRT_EUNSUPPORTED, "attention.batch=%d above 65535", a->batch);
+    if (a->heads < 1 || a->kv_heads < 1 || a->heads % a->kv_heads)
+        return fail(ctx, MIXRT_EINVAL, "attention.heads=%d for kv_heads=%d", a->heads,
+                    a->kv_heads);
+    if (a->heads > kMaxHeads)
+        return fail(ctx, MIXRT_EUNSUPPORTED, "attention.heads=%d above %d", a->heads, kMaxHeads);
+    if (a->head_dim < 1) return fail(ctx, MIXRT_EINVAL, "attention.head_dim=%d", a->head_dim);
+    if (a->head_dim > MIXRT_MAX_ATTENTION_DIM)
+        return fail(ctx, MIXRT_EUNSUPPORTED, "attention.head_dim=%d above %d", a->head_dim,
+                    MIXRT_MAX_ATTENTION_DIM);
+    if (!elem_size(a->dtype))
+        return fail(ctx, MIXRT_EUNSUPPORTED, "attention.dtype=%d (F32, F16 or BF16)", a->dtype);
+    if (!(a->scale > 0.0f) || !std::isfinite(a->scale))
+        return fail(ctx, MIXRT_EINVAL, "attention.scale=%g", a->scale);
+    if (a->queries < 0 || a->keys < 0)
+        return fail(ctx, MIXRT_EINVAL, "attention.queries=%lld, keys=%lld", (long long)a->queries,
+                    (long long)a->keys);
+    if (a->queries >= kMaxTokens || a->keys >= kMaxTokens)
+        return fail(ctx, MIXRT_EUNSUPPORTED, "attention: 2^30 queries or keys or more");
+    const int64_t rows = (int64_t)a->batch * a->heads;
+    if (rows > 0 && ((a->queries > a->keys ? a->queries : a->keys) + 1) > kMaxTokens / rows)
+        return fail(ctx, MIXRT_EUNSUPPORTED, "attention: 2^30 rows of heads or more");
+    if (!aligned(a->lens, 4)) return fail(ctx, MIXRT_EINVAL, "attention.lens not 4-byte aligned");
+    // a grid's blocks are counted in 32 bits
+    for (auto plan : {mixrt::plan_attend, mixrt::plan_attend_dq, mixrt::plan_attend_dkv}) {
+        const AttendPlan p = plan(a->batch, a->heads, a->kv_heads, a->queries, a->keys,
+                                  a->head_dim, a->dtype, 0);
+        if (rows * p.blocks >= ((int64_t)1 << 30) / p.splits)
+            return fail(ctx, MIXRT_EUNSUPPORTED, "attention: %lld queries and %lld keys are too "
+                        "many blocks", (long long)a->queries, (long long)a->keys);
+    }
+    return MIXRT_OK;
+}
+
+int check_bias(mixrt_ctx *ctx, const mixrt_attention *a, const mixrt_relative_bias *b, bool data)
+{
+    if (!b) return MIXRT_OK;
+    if (b->axes < 1 || b->axes > MIXRT_MAX_BIAS_AXES)
+        return fail(ctx, MIXRT_EUNSUPPORTED, "bias.axes=%d outside 1..%d", b->axes,
+                    MIXRT_MAX_BIAS_AXES);
+    if (b->count < 1 || b->count > MIXRT_MAX_BIAS_BUCKETS)
+        return fail(ctx, MIXRT_EUNSUPPORTED, "bias.count=%d outside 1..%d", b->count,
+                    MIXRT_MAX_BIAS_BUCKETS);
+    if (b->reach < 0 || b->reach > MIXRT_MAX_BIAS_REACH)
+        return fail(ctx, MIXRT_EUNSUPPORTED, "bias.reach=%d outside 0..%d", b->reach,
+                    MIXRT_MAX_BIAS_REACH);
+    if (!data) return MIXRT_OK;
+    if (!b->table || !b->buckets) return fail(ctx, MIXRT_EINVAL, "bias.table or buckets is NULL");
+    if ((a->queries && !b->q_pos) || (a->keys && !b->k_pos))
+        return fail(ctx, MIXRT_EINVAL, "bias.q_pos or k_pos is NULL");
+    if (!aligned(b->table, 4) || !aligned(b->q_pos, 4) || !aligned(b->k_pos, 4))
+        return fail(ctx, MIXRT_EINVAL, "bias.table, q_pos or k_pos not 4-byte aligned");
+    if (b->q_pos_stride < 0 || b->q_pos_stride >= kMaxStride || b->k_pos_stride < 0 ||
+        b->k_pos_stride >= kMaxStride)
+        return fail(ctx, MIXRT_EINVAL, "bias: position strides %lld, %lld",
+                    (long long)b->q_pos_stride, (long long)b->k_pos_stride);
+    return MIXRT_OK;
+}
+
+// An array of heads that a call reads or, with out, writes: an output's elements lie
+// apart, nested in some order of its three dimensions.
+int check_sequence(mixrt_ctx *ctx, const mixrt_attention *a, const mixrt_sequence *s, bool queries,
+                   const char *name, bool out)
+{
+    if (!s) return fail(ctx, MIXRT_EINVAL, "%s is NULL", name);
+    const int64_t n[3] = {a->batch, queries ? a->queries : a->keys,
+                          queries ? a->heads : a->kv_heads};
+    if (n[0] == 0 || n[1] == 0) return MIXRT_OK;
+    if (!s->data) return fail(ctx, MIXRT_EINVAL, "%s.data is NULL", name);
+    if (!aligned(s->data, elem_size(a->dtype)))
+        return fail(ctx, MIXRT_EINVAL, "%s.data not aligned to its element", name);
+    const int64_t st[3] = {s->batch_stride, s->token_stride, s->head_stride};
+    for (int i = 0; i < 3; ++i)
+        if (st[i] < 0 || st[i] >= kMaxStride || (st[i] && n[i] > kMaxElements / st[i]))
+            return fail(ctx, MIXRT_EINVAL, "%s: strides %lld, %lld, %lld", name, (long long)st[0],
+                        (long long)st[1], (long long)st[2]);
+    if (!out) return MIXRT_OK;
+    static const int orders[6][3] = {{0, 1, 2}, {0, 2, 1}, {1, 0, 2},
+                                     {1, 2, 0}, {2, 0, 1}, {2, 1, 0}};
+    for (const auto &order : orders) {
+        int64_t span = a->head_dim;
+        bool apart = true;
+        for (int i = 2; i >= 0; --i) {      // the innermost dimension first
+            const int d = order[i];
+            if (n[d] == 1) continue;
+            apart = apart && st[d] >= span;
+            span += (n[d] - 1) * st[d];
+        }
+        if (apart) return MIXRT_OK;
+    }
+    return fail(ctx, MIXRT_EINVAL, "%s: strides %lld, %lld, %lld make heads overlap", name,
+                (long long)st[0], (long long)st[1], (long long)st[2]);
+}
+
+size_t round16(size_t n) { return (n + 15) / 16 * 16; }
+
+// Where a call's scratch lies in its workspace; total bytes.
+struct Scratch {
+    size_t part, part_lse, delta, table, total;
+};
+
+Scratch scratch_of(const mixrt_attention *a, const mixrt_relative_bias *b, bool backward)
+{
+    const int axes = b ? b->axes : 0;
+    const size_t rows = (size_t)a->batch * a->heads * a->queries;
+    const size_t keys = (size_t)a->batch * a->kv_heads * a->keys;
+    Scratch s{};
+    size_t at = 0;
+    auto take = [&](size_t bytes) {
+        const size_t from = at;
+        at += round16(bytes);
+        return from;
+    };
+    auto plan = [&](auto fn) {
+        return fn(a->batch, a->heads, a->kv_heads, a->queries, a->keys, a->head_dim, a->dtype,
+                  axes);
+    };
+    if (!backward) {
+        const AttendPlan p = plan(mixrt::plan_attend);
+        if (p.splits > 1) {
+            s.part = take((size_t)p.splits * rows * a->head_dim * 4);
+            s.part_lse = take((size_t)p.splits * rows * 4);
+        }
+    } else {
+        const AttendPlan pq = plan(mixrt::plan_attend_dq), pk = plan(mixrt::plan_attend_dkv);
+        size_t part = pq.splits > 1 ? (size_t)pq.splits * rows * a->head_dim * 4 : 0;
+        const size_t both = pk.splits > 1 ? (size_t)pk.splits * keys * a->head_dim * 8 : 0;
+        s.part = take(part > both ? part : both);
+        s.delta = take(rows * 4);
+        if (axes)
+            s.table = take((size_t)a->batch * a->heads * pq.splits * pq.blocks * axes * b->count *
+                           4);
+    }
+    s.total = at;
+    return s;
+}
+
+mixrt::SeqK seq_k(const mixrt_sequence *s)
+{
+    return mixrt::SeqK{s->data, s->batch_stride, s->token_stride, s->head_stride};
+}
+
+mixrt::AttendK attend_k(const mixrt_attention *a, const mixrt_relative_bias *b)
+{
+    mixrt::AttendK k{};
+    k.B = a->batch;
+    k.H = a->heads;
+    k.Hk = a->kv_heads;
+    k.D = a->head_dim;
+    k.Tq = (int)a->queries;
+    k.Tk = (int)a->keys;
+    k.dtype = a->dtype;
+    k.plain_scale = a->scale;
+    k.scale = a->scale * 1.4426950408889634f;
+    k.lens = a->lens;
+    if (b)
+        k.bias = mixrt::BiasK{b->axes,  b->count, b->reach,        b->table,       b->buckets,
+                              b->q_pos, b->k_pos, b->q_pos_stride, b->k_pos_stride};
+    return k;
+}
+
+hipError_t launch_attend(const mixrt::AttendK &k, int stage, hipStream_t stream)
+{
+    if (k.dtype == mixrt::kF32) return mixrt::launch_attend_f32(k, stage, stream);
+    if (k.dtype == mixrt::kF16) return mixrt::launch_attend_f16(k, stage, stream);
+    return mixrt::launch_attend_bf16(k, stage, stream);
+}
+
+// --- heads normed and turned ----------------------------------------------------------
+
+int check_normed(mixrt_ctx *ctx, const mixrt_rotary *r, float eps, const mixrt_normed_heads *heads,
+                 int32_t n, bool backward, bool data, mixrt::RotaryNormLaunch &L)
+{
+    if (!r) return fail(ctx, MIXRT_EINVAL, "rotary is NULL");
+    if (r->tokens < 0) return fail(ctx, MIXRT_EINVAL, "rotary.tokens=%lld", (long long)r->tokens);
+    if (r->tokens >= ((int64_t)1 << 31))
+        return fail(ctx, MIXRT_EUNSUPPORTED, "rotary: 2^31 tokens or more");
+    if (r->axes < 1 || r->axes > MIXRT_MAX_AXES)
+        return fail(ctx, MIXRT_EUNSUPPORTED, "rotary.axes=%d outside 1..%d", r->axes,
+                    MIXRT_MAX_AXES);
+    if (r->layout != MIXRT_ROTARY_HALVES && r->layout != MIXRT_ROTARY_PAIRS)
+        return fail(ctx, MIXRT_EUNSUPPORTED, "rotary.layout=%d", r->layout);
+    if (r->pairs < 0) return fail(ctx, MIXRT_EINVAL, "rotary.pairs=%d", r->pairs);
+    if (!(eps >= 0.0f) || !std::isfinite(eps)) return fail(ctx, MIXRT_EINVAL, "eps=%g", eps);
+    if (n < 1 || n > MIXRT_MAX_HEADS_ARRAYS)
+        return fail(ctx, MIXRT_EINVAL, "n=%d outside 1..%d", n, MIXRT_MAX_HEADS_ARRAYS);
+    if (!heads) return fail(ctx, MIXRT_EINVAL, "heads is NULL");
+    if (data && r->pairs > 0 && r->tokens > 0) {
+        if (!r->pos || !r->freq || !r->axis)
+            return fail(ctx, MIXRT_EINVAL, "rotary.pos, freq or axis is NULL");
+        if (!aligned(r->pos, 4) || !aligned(r->freq, 4))
+            return fail(ctx, MIXRT_EINVAL, "rotary.pos or freq not 4-byte aligned");
+    }
+    L.tokens = r->tokens;
+    L.axes = r->axes;
+    L.pairs = r->pairs;
+    L.layout = r->layout;
+    L.dtype = heads[0].dtype;
+    L.eps = eps;
+    L.pos = r->pos;
+    L.freq = r->freq;
+    L.axis = r->axis;
+    L.n = n;
+    if (!elem_size(L.dtype))
+        return fail(ctx, MIXRT_EUNSUPPORTED, "heads[0].dtype=%d (F32, F16 or BF16)", L.dtype);
+    for (int i = 0; i < n; ++i) {
+        const mixrt_normed_heads &h = heads[i];
+        if (h.dtype != L.dtype)
+            return fail(ctx, MIXRT_EINVAL, "heads[%d].dtype=%d beside %d", i, h.dtype, L.dtype);
+        if (h.heads < 0 || h.heads > kMaxHeads)
+            return fail(ctx, MIXRT_EUNSUPPORTED, "heads[%d].heads=%d outside 0..%d", i, h.heads,
+                        kMaxHeads);
+        if (h.head_dim < 1 || h.head_dim > kMaxHeadDim)
+            return fail(ctx, MIXRT_EUNSUPPORTED, "heads[%d].head_dim=%d outside 1..%d", i,
+                        h.head_dim, kMaxHeadDim);
+        if (2 * (int64_t)r->pairs > h.head_dim)
+            return fail(ctx, MIXRT_EINVAL, "heads[%d].head_dim=%d for %d pairs", i, h.head_dim,
+                        r->pairs);
+        L.a[i] = mixrt::NormedHeadsK{h.heads,
+                                     h.head_dim,
+                                     h.x,
+                                     h.dy,
+                                     h.out,
+                                     h.weight,
+                                     h.dweight,
+                                     h.x_token_stride,
+                                     h.x_head_stride,
+                                     h.dy_token_stride,
+                                     h.dy_head_stride,
+                                     h.out_token_stride,
+                                     h.out_head_stride};
+        if (!data) continue;
+        if (!aligned(h.weight, 4) || !aligned(h.dweight, 4))
+            return fail(ctx, MIXRT_EINVAL, "heads[%d].weight or dweight not 4-byte aligned", i);
+        if (h.heads == 0 || r->tokens == 0) continue;   // none of its heads are touched
+        const bool writes = !backward || h.out;
+        if (!h.x || (backward && !h.dy) || (!backward && !h.out))
+            return fail(ctx, MIXRT_EINVAL, "heads[%d].x, dy or out is NULL", i);
+        const size_t size = elem_size(h.dtype);
+        if (!aligned(h.x, size) || !aligned(h.out, size) || (backward && !aligned(h.dy, size)))
+            return fail(ctx, MIXRT_EINVAL, "heads[%d].x, dy or out not aligned to its element", i);
+        const int64_t D = h.head_dim, H = h.heads, T = r->tokens;
+        const int64_t st[6] = {h.x_token_stride,   h.x_head_stride,   h.dy_token_stride,
+                               h.dy_head_stride,   h.out_token_stride, h.out_head_stride};
+        for (int s = 0; s < 6; ++s) {
+            if ((s / 2 == 1 && !backward) || (s / 2 == 2 && !writes)) continue;
+            const int64_t count = s % 2 ? H : T;
+            if (st[s] < 0 || st[s] >= kMaxStride || (st[s] && count > kMaxElements / st[s]))
+                return fail(ctx, MIXRT_EINVAL, "heads[%d]: stride %lld", i, (long long)st[s]);
+        }
+        if (!writes) continue;
+        // the output's rows apart: heads inside a token, or tokens inside a head
+        const int64_t ot = h.out_token_stride, oh = h.out_head_stride;
+        const bool inner = (H == 1 || oh >= D) && (T == 1 || ot >= (H - 1) * oh + D);
+        const bool outer = (T == 1 || ot >= D) && (H == 1 || oh >= (T - 1) * ot + D);
+        if (!inner && !outer)
+            return fail(ctx, MIXRT_EINVAL, "heads[%d]: out strides %lld, %lld make rows overlap",
+                        i, (long long)ot, (long long)oh);
+        const void *in = backward ? h.dy : h.x;
+        const int64_t it = backward ? h.dy_token_stride : h.x_token_stride;
+        const int64_t ih = backward ? h.dy_head_stride : h.x_head_stride;
+        if (in == h.out && ((T > 1 && it != ot) || (H > 1 && ih != oh)))
+            return fail(ctx, MIXRT_EINVAL, "heads[%d]: out is its input with other strides", i);
+        if (backward && h.x == h.out)
+            return fail(ctx, MIXRT_EINVAL, "heads[%d]: dx is x", i);
+    }
+    return MIXRT_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int mixrt_rotary_norm_apply(mixrt_ctx *ctx, const mixrt_rotary *rotary, float eps,
+                            const mixrt_normed_heads *heads, int32_t n)
+{
+    if (!ctx) return fail(nullptr, MIXRT_EINVAL, "ctx is NULL");
+    clear_err(ctx);
+    mixrt::RotaryNormLaunch L{};
+    int rc;
+    if ((rc = check_normed(ctx, rotary, eps, heads, n, false, true, L))) return rc;
+    if ((rc = bind_device(ctx))) return rc;
+    return finish_launch(ctx, mixrt::launch_rotary_norm(L, ctx->stream), "rotary_norm");
+}
+
+int mixrt_rotary_norm_workspace(const mixrt_rotary *rotary, const mixrt_normed_heads *heads,
+                                int32_t n, size_t *bytes)
+{
+    clear_err(nullptr);
+    if (!bytes) return fail(nullptr, MIXRT_EINVAL, "bytes is NULL");
+    *bytes = 0;
+    mixrt::RotaryNormLaunch L{};
+    if (int rc = check_normed(nullptr, rotary, 0.0f, heads, n, true, false, L)) return rc;
+    *bytes = mixrt::rotary_norm_workspace(L);
+    return MIXRT_OK;
+}
+
+int mixrt_rotary_norm_backward(mixrt_ctx *ctx, const mixrt_rotary *rotary, float eps,
+                               const mixrt_normed_heads *heads, int32_t n, void *workspace,
+                               size_t workspace_bytes)
+{
+    if (!ctx) return fail(nullptr, MIXRT_EINVAL, "ctx is NULL");
+    clear_err(ctx);
+    mixrt::RotaryNormLaunch L{};
+    int rc;
+    if ((rc = check_normed(ctx, rotary, eps, heads, n, true, true, L))) return rc;
+    if ((rc = check_workspace(ctx, workspace, workspace_bytes, mixrt::rotary_norm_workspace(L))))
+        return rc;
+    if ((rc = bind_device(ctx))) return rc;
+    L.ws = (float *)workspace;
+    return finish_launch(ctx, mixrt::launch_rotary_norm_back(L, ctx->stream),
+                         "rotary_norm_backward");
+}
+
+int mixrt_attention_workspace(const mixrt_attention *att, const mixrt_relative_bias *bias,
+                              int32_t backward, size_t *bytes)
+{
+    clear_err(nullptr);
+    if (!bytes) return fail(nullptr, MIXRT_EINVAL, "bytes is NULL");
+    *bytes = 0;
+    int rc;
+    if ((rc = check_attention(nullptr, att)) || (rc = check_bias(nullptr, att, bias, false)))
+        return rc;
+    *bytes = scratch_of(att, bias, backward != 0).total;
+    return MIXRT_OK;
+}
+
+int mixrt_attention_forward(mixrt_ctx *ctx, const mixrt_attention *att,
+                            const mixrt_relative_bias *bias, const mixrt_sequence *q,
+                            const mixrt_sequence *k, const mixrt_sequence *v,
+                            const mixrt_sequence *out, float *lse, void *rest, void *workspace,
+                            size_t workspace_bytes)
+{
+    if (!ctx) return fail(nullptr, MIXRT_EINVAL, "ctx is NULL");
+    clear_err(ctx);
+    int rc;
+    if ((rc = check_attention(ctx, att)) || (rc = check_bias(ctx, att, bias, true)) ||
+        (rc = check_sequence(ctx, att, q, true, "q", false)) ||
+        (rc = check_sequence(ctx, att, k, false, "k", false)) ||
+        (rc = check_sequence(ctx, att, v, false, "v", false)) ||
+        (rc = check_sequence(ctx, att, out, true, "out", true)))
+        return rc;
+    if (!aligned(lse, 4)) return fail(ctx, MIXRT_EINVAL, "lse not 4-byte aligned");
+    if (rest && att->dtype == MIXRT_F32) return fail(ctx, MIXRT_EINVAL, "rest for F32");
+    if (!aligned(rest, 2)) return fail(ctx, MIXRT_EINVAL, "rest not aligned to its element");
+    const Scratch s = scratch_of(att, bias, false);
+    if ((rc = check_workspace(ctx, workspace, workspace_bytes, s.total))) return rc;
+    if ((rc = bind_device(ctx))) return rc;
+    if (att->batch == 0 || att->queries == 0) return MIXRT_OK;
+    mixrt::AttendK a = attend_k(att, bias);
+    a.q = seq_k(q);
+    a.k = seq_k(k);
+    a.v = seq_k(v);
+    a.o = seq_k(out);
+    a.lse = lse;
+    a.rest = rest;
+    a.part = (float *)((char *)workspace + s.part);
+    a.part_lse = (float *)((char *)workspace + s.part_lse);
+    return finish_launch(ctx, launch_attend(a, mixrt::kAttendForward, ctx->stream),
+                         "attention_forward");
+}
+
+int mixrt_attention_backward(mixrt_ctx *ctx, const mixrt_attention *att,
+                             const mixrt_relative_bias *bias, const mixrt_sequence *dout,
+                             const mixrt_sequence *q, const mixrt_sequence *k,
+                             const mixrt_sequence *v, const mixrt_sequence *out,
+                             const float *lse, const void *rest, const mixrt_sequence *dq,
+                             const mixrt_sequence *dk, const mixrt_sequence *dv, float *dtable,
+                             void *workspace, size_t workspace_bytes)
+{
+    if (!ctx) return fail(nullptr, MIXRT_EINVAL, "ctx is NULL");
+    clear_err(ctx);
+    int rc;
+    if ((rc = check_attention(ctx, att)) || (rc = check_bias(ctx, att, bias, true)) ||
+        (rc = check_sequence(ctx, att, dout, true, "dout", false)) ||
+        (rc = check_sequence(ctx, att, q, true, "q", false)) ||
+        (rc = check_sequence(ctx, att, k, false, "k", false)) ||
+        (rc = check_sequence(ctx, att, v, false, "v", false)) ||
+        (rc = check_sequence(ctx, att, out, true, "out", false)) ||
+        (rc = check_sequence(ctx, att, dq, true, "dq", true)) ||
+        (rc = check_sequence(ctx, att, dk, false, "dk", true)) ||
+        (rc = check_sequence(ctx, att, dv, false, "dv", true)))
+        return rc;
+    if (dtable && !bias) return fail(ctx, MIXRT_EINVAL, "dtable without a bias");
+    if (!aligned(lse, 4) || !aligned(dtable, 4))
+        return fail(ctx, MIXRT_EINVAL, "lse or dtable not 4-byte aligned");
+    if (!aligned(rest, 2)) return fail(ctx, MIXRT_EINVAL, "rest not aligned to its element");
+    if (rest && att->dtype == MIXRT_F32) return fail(ctx, MIXRT_EINVAL, "rest for F32");
+    const bool rows = att->batch > 0 && att->queries > 0;
+    if (rows && (!lse || (!rest && att->dtype != MIXRT_F32)))
+        return fail(ctx, MIXRT_EINVAL, "lse or rest is NULL");
+    const Scratch s = scratch_of(att, bias, true);
+    if ((rc = check_workspace(ctx, workspace, workspace_bytes, s.total))) return rc;
+    if ((rc = bind_device(ctx))) return rc;
+    mixrt::AttendK a = attend_k(att, bias);
+    a.dout = seq_k(dout);
+    a.q = seq_k(q);
+    a.k = seq_k(k);
+    a.v = seq_k(v);
+    a.o = seq_k(out);
+    a.lse = (float *)lse;
+    a.rest = (void *)rest;
+    a.dq = seq_k(dq);
+    a.dk = seq_k(dk);
+    a.dv = seq_k(dv);
+    a.dtable = dtable;
+    a.part = (float *)((char *)workspace + s.part);
+    a.delta = (float *)((char *)workspace + s.delta);
+    a.part_table = (float *)((char *)workspace + s.table);
+    hipError_t e = launch_attend(a, mixrt::kAttendBackQ, ctx->stream);
+    if (e == hipSuccess) e = launch_attend(a, mixrt::kAttendBackKV, ctx->stream);
+    return finish_launch(ctx, e, "attention_backward");
+}
+
+}  // extern "C"

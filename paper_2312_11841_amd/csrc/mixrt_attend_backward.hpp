@@ -1,0 +1,591 @@
+// Attention, backward: two walks that each form the weights and their gradients
+// again, one with the queries in the lanes (their gradient, and the bias table's),
+// one with the keys (the gradients of keys and values).  Nothing is added by
+// several blocks to one place, so the sums' order is fixed.
+#pragma once
+
+#include "mixrt_attend_tile.hpp"
+
+namespace mixrt {
+namespace {
+
+// Rows of a bias table's gradient that a walk over the keys sums in 32 bits before
+// they move on to 64.
+constexpr int kHistRows = 1024;
+
+// acc[d][column] += sum over the tile's rows of tile[row][d] p[row][column].
+template <typename T, int DP, int NC>
+__device__ __forceinline__ void add_cols(const T *tile, int lane, const f32x16 (&p)[NC],
+                                         f32x16 (&acc)[NC][DP / 32])
+{
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+            for (int n = 0; n < NC; ++n) col_mul<DP>(tile, lane, d, p[n], acc[n][d]);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            typename Matrix<T>::frag f[NC];
+#pragma unroll
+            for (int n = 0; n < NC; ++n) f[n] = round_rows<T>(p[n], e);
+#pragma unroll
+            for (int d = 0; d < DP / 32; ++d) {
+                const auto a = col_frag<T, DP>(tile, lane, d, e);
+#pragma unroll
+                for (int n = 0; n < NC; ++n) acc[n][d] = Matrix<T>::mul(a, f[n], acc[n][d]);
+            }
+        }
+    }
+}
+
+template <int NC, int ND>
+__device__ __forceinline__ void clear(f32x16 (&a)[NC][ND])
+{
+#pragma unroll
+    for (int n = 0; n < NC; ++n)
+#pragma unroll
+        for (int d = 0; d < ND; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) a[n][d][i] = 0.0f;
+}
+
+template <typename T, int DP>
+__device__ __forceinline__ f32x16 row_mul(const T *tile, int lane,
+                                          const typename Matrix<T>::frag (&b)[kPairs<T, DP>])
+{
+    f32x16 s;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[i] = 0.0f;
+#pragma unroll
+    for (int c = 0; c < kPairs<T, DP>; ++c)
+        s = Matrix<T>::mul(row_frag<T, DP>(tile, lane, c), b[c], s);
+    return s;
+}
+
+// A column's sums, times a factor, to its row of an output.
+template <typename T, int DP>
+__device__ __forceinline__ void store_column(T *row, int half, int D, const f32x16 (&a)[DP / 32],
+                                             float by)
+{
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            store_quad<T>(row, 32 * d + 8 * e + 4 * half, D, a[d][4 * e] * by, a[d][4 * e + 1] * by,
+                          a[d][4 * e + 2] * by, a[d][4 * e + 3] * by);
+}
+
+// --- the queries' gradient -----------------------------------------------------------
+
+template <typename T, int DP, int NC, bool BIAS>
+__global__ __launch_bounds__(256) void attend_dq_kernel(AttendK k)
+{
+    typedef typename Matrix<T>::frag frag;
+    constexpr int ROWS = 32, THREADS = 256;
+    constexpr int TILE = ROWS * kStride<T, DP>;
+    // (two of the widest tiles and the table's sums are more than a CU's 160 KB)
+    constexpr int BUFS = BIAS && sizeof(T) == 4 && DP == 128 ? 1 : 2;
+    __shared__ __attribute__((aligned(16))) T tiles[BUFS][2][TILE];
+    __shared__ float2 dense[BIAS ? kMaxBiasAxes * kReachRow : 1];   // bias, place in hist
+    __shared__ __attribute__((aligned(16))) int32_t kpos[2][BIAS ? kMaxBiasAxes * ROWS : 4];
+    extern __shared__ float hist[];     // [wave][entry][lane]
+
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
+    const int block = near_block();
+    int id = block;
+    const int rb = id % k.blocks;
+    id /= k.blocks;
+    const int split = id % k.splits;
+    id /= k.splits;
+    const int h = id % k.H, b = id / k.H;
+    const int kvh = h / (k.H / k.Hk);
+    const int len = valid_keys(k.lens, b, k.Tk);
+    const int first = split * k.per, last = min(len, first + k.per);
+    const int entries = BIAS ? k.bias.axes * k.bias.buckets : 0;
+
+    int t[NC];
+    bool there[NC];
+    frag q[NC][kPairs<T, DP>], dout[NC][kPairs<T, DP>];
+    float lse[NC], delta[NC];
+    int qpos[NC][kMaxBiasAxes];
+#pragma unroll
+    for (int n = 0; n < NC; ++n) {
+        t[n] = ((rb * 4 + wave) * NC + n) * 32 + (lane & 31);
+        there[n] = t[n] < k.Tq;
+        const int64_t tt = t[n];
+        load_column<T, DP>(q[n], (const T *)k.q.data + b * k.q.batch + tt * k.q.token +
+                                     h * k.q.head, there[n], half, k.D);
+        load_column<T, DP>(dout[n], (const T *)k.dout.data + b * k.dout.batch + tt * k.dout.token +
+                                        h * k.dout.head, there[n], half, k.D);
+        // delta = sum_d dout o, with what rounding took from o
+        float sum = 0.0f;
+        {
+            frag o[kPairs<T, DP>], rest[kPairs<T, DP>];
+            load_column<T, DP>(o, (const T *)k.o.data + b * k.o.batch + tt * k.o.token +
+                                      h * k.o.head, there[n], half, k.D);
+            if (sizeof(T) == 2)
+                load_column<T, DP>(rest, (const T *)k.rest + ((b * (int64_t)k.Tq + tt) * k.H + h) *
+                                                                 k.D, there[n], half, k.D);
+#pragma unroll
+            for (int c = 0; c < kPairs<T, DP>; ++c)
+#pragma unroll
+                for (int i = 0; i < kChunk<T>; ++i) {
+                    float x = (float)o[c][i];
+                    if (sizeof(T) == 2) x += (float)rest[c][i] * (1.0f / kRestScale<T>);
+                    sum = fmaf((float)dout[n][c][i], x, sum);
+                }
+        }
+        delta[n] = half_sum(sum);
+        const int64_t row = ((int64_t)b * k.H + h) * k.Tq + tt;
+        lse[n] = there[n] ? k.lse[row] : INFINITY;
+        if (there[n] && half == 0 && split == 0) k.delta[row] = delta[n];
+#pragma unroll
+        for (int a = 0; a < kMaxBiasAxes; ++a)
+            qpos[n][a] = BIAS && there[n] && a < k.bias.axes
+                             ? k.bias.qpos[b * k.bias.qbatch + tt * k.bias.axes + a]
+                             : 0;
+    }
+    if (BIAS) {
+        const int each = 2 * k.bias.reach + 1;
+        for (int i = threadIdx.x; i < k.bias.axes * each; i += THREADS) {
+            const int a = i / each, d = i - a * each;
+            const int e = a * k.bias.buckets + min((int)k.bias.map[i], k.bias.buckets - 1);
+            dense[a * kReachRow + d] = make_float2(k.bias.table[(int64_t)e * k.H + h] * kLog2e,
+                                                   __int_as_float(64 * e));
+        }
+        for (int i = threadIdx.x; i < 4 * 64 * entries; i += THREADS) hist[i] = 0.0f;
+    }
+    float *mine = hist + wave * 64 * entries + lane;
+    double table = 0.0;         // thread e: entry e's sum of the block
+
+    f32x16 acc[NC][DP / 32];
+    clear(acc);
+    const T *kp = (const T *)k.k.data + b * k.k.batch + kvh * k.k.head;
+    const T *vp = (const T *)k.v.data + b * k.v.batch + kvh * k.v.head;
+    const int32_t *pp = BIAS ? k.bias.kpos + b * k.bias.kbatch : nullptr;
+    Stage<T, DP, ROWS, THREADS> sk, sv;
+    StagePos<ROWS> sp;
+    if (first < last) {
+        sk.fetch(kp, k.k.token, first, last, k.D);
+        sv.fetch(vp, k.v.token, first, last, k.D);
+        if (BIAS) sp.fetch(pp, k.bias.axes, first, last);
+        sk.put(tiles[0][0]);
+        sv.put(tiles[0][1]);
+        if (BIAS) sp.put(kpos[0], k.bias.axes);
+    }
+    __syncthreads();
+    int cur = 0, counted = 0;
+    for (int row0 = first; row0 < last; row0 += ROWS, cur ^= BUFS - 1) {
+        const bool more = row0 + ROWS < last;
+        if (more) {
+            sk.fetch(kp, k.k.token, row0 + ROWS, last, k.D);
+            sv.fetch(vp, k.v.token, row0 + ROWS, last, k.D);
+            if (BIAS) sp.fetch(pp, k.bias.axes, row0 + ROWS, last);
+        }
+        const T *kt = tiles[cur][0], *vt = tiles[cur][1];
+        f32x16 s[NC], g[NC];
+#pragma unroll
+        for (int n = 0; n < NC; ++n)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[n][i] = g[n][i] = 0.0f;
+#pragma unroll
+        for (int c = 0; c < kPairs<T, DP>; ++c) {
+            const frag a = row_frag<T, DP>(kt, lane, c), v = row_frag<T, DP>(vt, lane, c);
+#pragma unroll
+            for (int n = 0; n < NC; ++n) {
+                s[n] = Matrix<T>::mul(a, q[n][c], s[n]);
+                g[n] = Matrix<T>::mul(v, dout[n][c], g[n]);
+            }
+        }
+        if (BIAS) {
+#pragma unroll
+            for (int n = 0; n < NC; ++n)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[n][i] *= k.scale;
+            for (int a = 0; a < k.bias.axes; ++a)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int p = kpos[cur][a * ROWS + tile_row(i, half)];
+#pragma unroll
+                    for (int n = 0; n < NC; ++n) {
+                        const int at = a == 0 ? qpos[n][0] : a == 1 ? qpos[n][1] : qpos[n][2];
+                        s[n][i] += dense[a * kReachRow + bias_at(p, at, k.bias.reach)].x;
+                    }
+                }
+        }
+        const float unit = BIAS ? 1.0f : k.scale;
+#pragma unroll
+        for (int n = 0; n < NC; ++n)
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                g[n][i] = __builtin_amdgcn_exp2f(fmaf(s[n][i], unit, -lse[n])) *
+                          (g[n][i] - delta[n]);
+        if (!more && row0 + ROWS > last) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                if (row0 + tile_row(i, half) >= last)
+#pragma unroll
+                    for (int n = 0; n < NC; ++n) g[n][i] = 0.0f;
+        }
+        add_cols<T, DP, NC>(kt, lane, g, acc);
+        if (BIAS) {
+            for (int a = 0; a < k.bias.axes; ++a)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int p = kpos[cur][a * ROWS + tile_row(i, half)];
+#pragma unroll
+                    for (int n = 0; n < NC; ++n) {
+                        const int at = a == 0 ? qpos[n][0] : a == 1 ? qpos[n][1] : qpos[n][2];
+                        const int e = __float_as_int(
+                            dense[a * kReachRow + bias_at(p, at, k.bias.reach)].y);
+                        // (the lane's own place: no other adds there)
+                        __hip_atomic_fetch_add(mine + e, there[n] ? g[n][i] : 0.0f,
+                                               __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+                    }
+                }
+            counted += ROWS;
+        }
+        if (BUFS == 1) __syncthreads();
+        if (more) {
+            sk.put(tiles[cur ^ (BUFS - 1)][0]);
+            sv.put(tiles[cur ^ (BUFS - 1)][1]);
+            if (BIAS) sp.put(kpos[cur ^ (BUFS - 1)], k.bias.axes);
+        }
+        __syncthreads();
+        if (BIAS && (counted == kHistRows || !more)) {
+            // each entry's places of all lanes; threads start at different lanes,
+            // as the same lane of all entries lies in one bank
+            if ((int)threadIdx.x < entries) {
+                float sum = 0.0f;
+#pragma unroll 1
+                for (int w = 0; w < 4; ++w) {
+                    float *at = hist + (w * entries + threadIdx.x) * 64;
+#pragma unroll 4
+                    for (int i = 0; i < 64; ++i) {
+                        const int l = (i + threadIdx.x) & 63;
+                        sum += at[l];
+                        at[l] = 0.0f;
+                    }
+                }
+                table += sum;
+            }
+            counted = 0;
+            __syncthreads();
+        }
+    }
+    if (BIAS && (int)threadIdx.x < entries)
+        k.part_table[(int64_t)block * entries + threadIdx.x] = (float)table;
+#pragma unroll
+    for (int n = 0; n < NC; ++n) {
+        if (!there[n]) continue;
+        if (k.splits > 1) {
+            const int64_t rows = (int64_t)k.B * k.H * k.Tq;
+            const int64_t row = ((int64_t)b * k.H + h) * k.Tq + t[n];
+            store_column<float, DP>(k.part + (split * rows + row) * k.D, half, k.D, acc[n],
+                                    k.plain_scale);
+        } else {
+            store_column<T, DP>((T *)k.dq.data + b * k.dq.batch + (int64_t)t[n] * k.dq.token +
+                                    h * k.dq.head, half, k.D, acc[n], k.plain_scale);
+        }
+    }
+}
+
+// --- the gradients of keys and values ---------------------------------------------------
+
+// lse and delta of a tile's queries.
+template <int ROWS>
+struct StageSums {
+    float lse, delta;
+    __device__ __forceinline__ void fetch(const float *l, const float *d, int first, int limit)
+    {
+        const int row = first + (int)threadIdx.x;
+        const bool there = threadIdx.x < ROWS && row < limit;
+        lse = there ? l[row] : INFINITY;     // a row that is not there has weights 0
+        delta = there ? d[row] : 0.0f;
+    }
+    __device__ __forceinline__ void put(float *at) const
+    {
+        if (threadIdx.x < ROWS) {
+            at[threadIdx.x] = lse;
+            at[ROWS + threadIdx.x] = delta;
+        }
+    }
+};
+
+template <typename T, int DP, int NC, bool BIAS>
+__global__ __launch_bounds__(256) void attend_dkv_kernel(AttendK k)
+{
+    typedef typename Matrix<T>::frag frag;
+    constexpr int ROWS = 32, THREADS = 256;
+    constexpr int TILE = ROWS * kStride<T, DP>;
+    __shared__ __attribute__((aligned(16))) T tiles[2][2][TILE];
+    __shared__ float dense[BIAS ? kMaxBiasAxes * kReachRow : 1];
+    __shared__ __attribute__((aligned(16))) int32_t qpos[2][BIAS ? kMaxBiasAxes * ROWS : 4];
+    __shared__ __attribute__((aligned(16))) float sums[2][2 * ROWS];
+
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
+    int id = near_block();
+    const int rb = id % k.blocks;
+    id /= k.blocks;
+    const int split = id % k.splits;
+    id /= k.splits;
+    const int kvh = id % k.Hk, b = id / k.Hk;
+    const int G = k.H / k.Hk;
+    const int len = valid_keys(k.lens, b, k.Tk);
+    // tiles of the group's heads, one head after another
+    const int a_head = max((k.Tq + ROWS - 1) / ROWS, 1);
+    const int first = split * k.per;
+    int last = min(k.Tq > 0 ? G * a_head : 0, first + k.per);
+    if (rb * 128 * NC >= len) last = first;
+
+    int t[NC];
+    bool there[NC], seen[NC];
+    frag key[NC][kPairs<T, DP>], val[NC][kPairs<T, DP>];
+    int kpos[NC][kMaxBiasAxes];
+#pragma unroll
+    for (int n = 0; n < NC; ++n) {
+        t[n] = ((rb * 4 + wave) * NC + n) * 32 + (lane & 31);
+        there[n] = t[n] < k.Tk;
+        seen[n] = t[n] < len;
+        const int64_t tt = t[n];
+        load_column<T, DP>(key[n], (const T *)k.k.data + b * k.k.batch + tt * k.k.token +
+                                       kvh * k.k.head, seen[n], half, k.D);
+        load_column<T, DP>(val[n], (const T *)k.v.data + b * k.v.batch + tt * k.v.token +
+                                       kvh * k.v.head, seen[n], half, k.D);
+#pragma unroll
+        for (int a = 0; a < kMaxBiasAxes; ++a)
+            kpos[n][a] = BIAS && seen[n] && a < k.bias.axes
+                             ? k.bias.kpos[b * k.bias.kbatch + tt * k.bias.axes + a]
+                             : 0;
+    }
+    f32x16 dk[NC][DP / 32], dv[NC][DP / 32];
+    clear(dk);
+    clear(dv);
+
+    const T *qp = (const T *)k.q.data + b * k.q.batch;
+    const T *gp = (const T *)k.dout.data + b * k.dout.batch;
+    const int64_t sums0 = (int64_t)b * k.H * k.Tq;
+    const int32_t *pp = BIAS ? k.bias.qpos + b * k.bias.qbatch : nullptr;
+    Stage<T, DP, ROWS, THREADS> sq, sg;
+    StagePos<ROWS> sp;
+    StageSums<ROWS> ss;
+    // the tile that is fetched next: head of the group, first row
+    int fg = first / a_head, ft = first % a_head * ROWS;
+    auto fetch = [&]() {
+        const int h = kvh * G + fg;
+        sq.fetch(qp + h * k.q.head, k.q.token, ft, k.Tq, k.D);
+        sg.fetch(gp + h * k.dout.head, k.dout.token, ft, k.Tq, k.D);
+        const int64_t at = sums0 + (int64_t)h * k.Tq;
+        ss.fetch(k.lse + at, k.delta + at, ft, k.Tq);
+        if (BIAS) sp.fetch(pp, k.bias.axes, ft, k.Tq);
+        ft += ROWS;
+        if (ft >= k.Tq) {
+            ft = 0;
+            ++fg;
+        }
+    };
+    auto put = [&](int to) {
+        sq.put(tiles[to][0]);
+        sg.put(tiles[to][1]);
+        ss.put(sums[to]);
+        if (BIAS) sp.put(qpos[to], k.bias.axes);
+    };
+    int head = -1;              // whose bias is in LDS
+    int at_head = first / a_head, left = a_head - first % a_head;
+    if (first < last) {
+        fetch();
+        put(0);
+    }
+    __syncthreads();
+    int cur = 0;
+    for (int i0 = first; i0 < last; ++i0, cur ^= 1) {
+        const bool more = i0 + 1 < last;
+        if (more) fetch();
+        if (BIAS && head != at_head) {      // (the same for the whole block)
+            load_bias(dense, k.bias, kvh * G + at_head, k.H, THREADS);
+            head = at_head;
+            __syncthreads();
+        }
+        const T *qt = tiles[cur][0], *gt = tiles[cur][1];
+        const float *sm = sums[cur];
+        f32x16 p[NC], g[NC];
+#pragma unroll
+        for (int n = 0; n < NC; ++n) {
+            p[n] = row_mul<T, DP>(qt, lane, key[n]);
+            g[n] = row_mul<T, DP>(gt, lane, val[n]);
+        }
+        if (BIAS) {
+#pragma unroll
+            for (int n = 0; n < NC; ++n)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) p[n][i] *= k.scale;
+            for (int a = 0; a < k.bias.axes; ++a)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int at = qpos[cur][a * ROWS + tile_row(i, half)];
+#pragma unroll
+                    for (int n = 0; n < NC; ++n) {
+                        const int mine = a == 0 ? kpos[n][0] : a == 1 ? kpos[n][1] : kpos[n][2];
+                        p[n][i] += dense[a * kReachRow + bias_at(mine, at, k.bias.reach)];
+                    }
+                }
+        }
+        const float unit = BIAS ? 1.0f : k.scale;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const float lse = sm[tile_row(i, half)], delta = sm[ROWS + tile_row(i, half)];
+#pragma unroll
+            for (int n = 0; n < NC; ++n) {
+                p[n][i] = __builtin_amdgcn_exp2f(fmaf(p[n][i], unit, -lse));
+                g[n][i] = p[n][i] * (g[n][i] - delta);
+            }
+        }
+        add_cols<T, DP, NC>(gt, lane, p, dv);
+        add_cols<T, DP, NC>(qt, lane, g, dk);
+        if (--left == 0) {
+            ++at_head;
+            left = a_head;
+        }
+        if (more) put(cur ^ 1);
+        __syncthreads();
+    }
+#pragma unroll
+    for (int n = 0; n < NC; ++n) {
+        if (!there[n]) continue;
+        if (!seen[n]) {
+#pragma unroll
+            for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) dk[n][d][i] = dv[n][d][i] = 0.0f;
+        }
+        const int64_t tt = t[n];
+        if (k.splits > 1) {
+            const int64_t rows = (int64_t)k.B * k.Hk * k.Tk;
+            const int64_t row = ((int64_t)b * k.Hk + kvh) * k.Tk + tt;
+            store_column<float, DP>(k.part + (split * rows + row) * k.D, half, k.D, dk[n],
+                                    k.plain_scale);
+            store_column<float, DP>(k.part + ((k.splits + split) * rows + row) * k.D, half, k.D,
+                                    dv[n], 1.0f);
+        } else {
+            store_column<T, DP>((T *)k.dk.data + b * k.dk.batch + tt * k.dk.token +
+                                    kvh * k.dk.head, half, k.D, dk[n], k.plain_scale);
+            store_column<T, DP>((T *)k.dv.data + b * k.dv.batch + tt * k.dv.token +
+                                    kvh * k.dv.head, half, k.D, dv[n], 1.0f);
+        }
+    }
+}
+
+// --- joins ----------------------------------------------------------------------------
+
+// out[b][t][h][d] = sum of the splits' parts [split][b][h][t][d], a quad a thread;
+// with blockIdx.y = 1 the second array's parts, which follow.
+template <typename T>
+__global__ __launch_bounds__(256) void attend_sum_kernel(const float *part, int splits, int B,
+                                                         int H, int Tn, int D, SeqK one, SeqK two)
+{
+    const int quads = (D + 3) / 4;
+    const int64_t rows = (int64_t)B * H * Tn;
+    const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (at >= rows * quads) return;
+    const int64_t row = at / quads;
+    const int d = (int)(at - row * quads) * 4;
+    const SeqK out = blockIdx.y ? two : one;
+    const float *p = part + ((int64_t)blockIdx.y * splits * rows + row) * D + d;
+    float a[4] = {0, 0, 0, 0};
+    for (int s = 0; s < splits; ++s, p += rows * D) {
+        if (d + 4 <= D) {
+            float f[4];
+            load_vec<float, 4>(p, f);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) a[i] += f[i];
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (d + i < D) a[i] += p[i];
+        }
+    }
+    const int64_t bh = row / Tn;
+    const int t = (int)(row - bh * Tn), b = (int)(bh / H), h = (int)(bh - (int64_t)b * H);
+    store_quad<T>((T *)out.data + b * out.batch + (int64_t)t * out.token + h * out.head, d, D, a[0],
+                  a[1], a[2], a[3]);
+}
+
+// dtable[entry][h] = sum over the entries' blocks of head h, in 64 bits.
+__global__ __launch_bounds__(256) void attend_table_kernel(const float *part, int B, int H,
+                                                           int each, int entries, float *dtable)
+{
+    __shared__ double sums[256];
+    const int e = blockIdx.x, h = blockIdx.y;
+    // block ((b H + h) each + i) of the queries' gradient
+    double a = 0.0;
+    for (int64_t i = threadIdx.x; i < (int64_t)B * each; i += 256) {
+        const int64_t b = i / each;
+        a += part[((b * H + h) * each + (i - b * each)) * entries + e];
+    }
+    sums[threadIdx.x] = a;
+    for (int n = 128; n > 0; n >>= 1) {
+        __syncthreads();
+        if ((int)threadIdx.x < n) sums[threadIdx.x] += sums[threadIdx.x + n];
+    }
+    if (threadIdx.x == 0) dtable[(int64_t)e * H + h] = (float)sums[0];
+}
+
+template <typename T>
+hipError_t launch_sum(const AttendK &k, int H, int64_t Tn, const SeqK &one, const SeqK &two, int n,
+                      hipStream_t stream)
+{
+    const int64_t quads = (int64_t)k.B * H * Tn * ((k.D + 3) / 4);
+    if (quads == 0) return hipSuccess;
+    attend_sum_kernel<T><<<dim3((unsigned)((quads + 255) / 256), n), 256, 0, stream>>>(
+        k.part, k.splits, k.B, H, (int)Tn, k.D, one, two);
+    return hipGetLastError();
+}
+
+template <typename T, int DP>
+hipError_t launch_back_q(const AttendK &k, const AttendPlan &p, hipStream_t stream)
+{
+    const unsigned grid = (unsigned)((int64_t)k.B * k.H * k.splits * k.blocks);
+    const int entries = k.bias.axes * k.bias.buckets;
+    auto go = [&](auto nc) {
+        constexpr int NC = decltype(nc)::value;
+        if (grid == 0) return;
+        if (k.bias.axes)
+            attend_dq_kernel<T, DP, NC, true><<<grid, 256, 1024 * entries, stream>>>(k);
+        else
+            attend_dq_kernel<T, DP, NC, false><<<grid, 256, 0, stream>>>(k);
+    };
+    typedef std::integral_constant<int, 1> one;
+    if constexpr (sizeof(T) == 2 && DP <= 64) {
+        if (p.cols == 256)
+            go(std::integral_constant<int, 2>());
+        else
+            go(one());
+    } else
+        go(one());
+    hipError_t e = hipGetLastError();
+    if (e == hipSuccess && k.splits > 1) e = launch_sum<T>(k, k.H, k.Tq, k.dq, k.dq, 1, stream);
+    if (e == hipSuccess && entries && k.dtable) {
+        attend_table_kernel<<<dim3(entries, k.H), 256, 0, stream>>>(
+            k.part_table, k.B, k.H, k.splits * k.blocks, entries, k.dtable);
+        e = hipGetLastError();
+    }
+    return e;
+}
+
+template <typename T, int DP>
+hipError_t launch_back_kv(const AttendK &k, const AttendPlan &p, hipStream_t stream)
+{
+    const unsigned grid = (unsigned)((int64_t)k.B * k.Hk * k.splits * k.blocks);
+    if (grid == 0) return hipSuccess;
+    if (k.bias.axes)
+        attend_dkv_kernel<T, DP, 1, true><<<grid, 256, 0, stream>>>(k);
+    else
+        attend_dkv_kernel<T, DP, 1, false><<<grid, 256, 0, stream>>>(k);
+    hipError_t e = hipGetLastError();
+    if (e == hipSuccess && k.splits > 1) e = launch_sum<T>(k, k.Hk, k.Tk, k.dk, k.dv, 2, stream);
+    return e;
+}
+
+}  // namespace
+}  // namespace mixrt

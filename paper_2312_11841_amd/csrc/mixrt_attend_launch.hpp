@@ -1,0 +1,39 @@
+// One element type's attention launches by the heads' padded width.
+#pragma once
+
+#include <type_traits>
+
+#include "mixrt_attend_forward.hpp"
+
+#include "mixrt_attend_backward.hpp"
+
+namespace mixrt {
+namespace {
+
+template <typename T>
+hipError_t launch_attend(AttendK k, int stage, hipStream_t stream)
+{
+    auto plan = stage == kAttendForward ? plan_attend
+                : stage == kAttendBackQ ? plan_attend_dq
+                                        : plan_attend_dkv;
+    const AttendPlan p = plan(k.B, k.H, k.Hk, k.Tq, k.Tk, k.D, k.dtype, k.bias.axes);
+    k.pack = p.pack;
+    k.blocks = p.blocks;
+    k.splits = p.splits;
+    k.per = p.per;
+    auto go = [&](auto dp) {
+        constexpr int DP = decltype(dp)::value;
+        if (stage == kAttendForward) return launch_forward<T, DP>(k, p, stream);
+        if (stage == kAttendBackQ) return launch_back_q<T, DP>(k, p, stream);
+        return launch_back_kv<T, DP>(k, p, stream);
+    };
+    switch (attend_dim(k.D)) {
+    case 32: return go(std::integral_constant<int, 32>());
+    case 64: return go(std::integral_constant<int, 64>());
+    case 96: return go(std::integral_constant<int, 96>());
+    default: return go(std::integral_constant<int, 128>());
+    }
+}
+
+}  // namespace
+}  // namespace mixrt

@@ -1,6 +1,6 @@
 // The view refiner's operators: launch interface between the C ABI
-// (mixrt_refine_api.cpp) and the kernels (mixrt_norm.hip, mixrt_kept.hip,
-// mixrt_rotary.hip), and the element access the kernels share.
+// (mixrt_refine_api.cpp, mixrt_attend_api.cpp) and the kernels (mixrt_norm.hip,
+// mixrt_kept.hip, mixrt_rotary.hip, mixrt_rotary_norm.hip), and the element access the kernels share.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -63,6 +63,31 @@ struct RotaryLaunch {
 };
 
 hipError_t launch_rotary(const RotaryLaunch &L, hipStream_t stream);
+
+// Heads normed and turned.  Forward: x, out; backward: x, dy, out (dx, or null) and
+// dw (or null).
+struct NormedHeadsK {
+    int heads, D;
+    const void *x, *dy;
+    void *out;
+    const float *w;           // [D], or null: 1
+    float *dw;
+    int64_t xt, xh, dt, dh, ot, oh;
+};
+
+struct RotaryNormLaunch {
+    int64_t tokens;
+    int axes, pairs, layout, dtype, n;
+    float eps;
+    const float *pos, *freq;
+    const uint8_t *axis;
+    NormedHeadsK a[2];
+    float *ws;
+};
+
+size_t rotary_norm_workspace(const RotaryNormLaunch &L);
+hipError_t launch_rotary_norm(const RotaryNormLaunch &L, hipStream_t stream);
+hipError_t launch_rotary_norm_back(const RotaryNormLaunch &L, hipStream_t stream);
 
 // --- element access -----------------------------------------------------------
 

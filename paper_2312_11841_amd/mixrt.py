@@ -30,6 +30,7 @@ _BLOCKS = {None: 0, "full": MIXRT_FLAG_BLOCKS_FULL, "two": MIXRT_FLAG_BLOCKS_TWO
 MAX_VIEWS, MAX_LEVELS, MAX_LAYERS = 16, 32, 8
 ACTS = {"none": 0, "relu": 1, "silu": 2, "gelu": 3}
 ROTARY_LAYOUTS = {"halves": 0, "pairs": 1}
+MAX_ATTENTION_DIM, MAX_BIAS_AXES, MAX_BIAS_BUCKETS, MAX_BIAS_REACH = 128, 3, 32, 127
 KEPT_GROUP = 32     # channels that share a scale in the 8-bit form
 
 # Every symbol include/mixrt.h declares.
@@ -44,6 +45,8 @@ EXPORTS = (
     "mixrt_norm_workspace", "mixrt_norm_forward", "mixrt_norm_backward",
     "mixrt_kept_pack", "mixrt_kept_unpack",
     "mixrt_linear_grad_workspace", "mixrt_linear_grad", "mixrt_rotary_apply",
+    "mixrt_rotary_norm_apply", "mixrt_rotary_norm_workspace", "mixrt_rotary_norm_backward",
+    "mixrt_attention_workspace", "mixrt_attention_forward", "mixrt_attention_backward",
     "mixrt_status_string", "mixrt_last_error", "mixrt_thread_error",
 )
 RAY_T_MIN = 1e-4
@@ -141,6 +144,33 @@ class Heads(C.Structure):
                 ("out_head_stride", C.c_int64)]
 
 
+class NormedHeads(C.Structure):
+    _fields_ = [("heads", C.c_int32), ("head_dim", C.c_int32), ("dtype", C.c_int32),
+                ("weight", C.c_void_p), ("x", C.c_void_p), ("dy", C.c_void_p),
+                ("out", C.c_void_p), ("dweight", C.c_void_p), ("x_token_stride", C.c_int64),
+                ("x_head_stride", C.c_int64), ("dy_token_stride", C.c_int64),
+                ("dy_head_stride", C.c_int64), ("out_token_stride", C.c_int64),
+                ("out_head_stride", C.c_int64)]
+
+
+class Attention(C.Structure):
+    _fields_ = [("batch", C.c_int32), ("heads", C.c_int32), ("kv_heads", C.c_int32),
+                ("head_dim", C.c_int32), ("dtype", C.c_int32), ("scale", C.c_float),
+                ("queries", C.c_int64), ("keys", C.c_int64), ("lens", C.c_void_p)]
+
+
+class RelativeBiasDesc(C.Structure):
+    _fields_ = [("axes", C.c_int32), ("count", C.c_int32), ("reach", C.c_int32),
+                ("table", C.c_void_p), ("buckets", C.c_void_p), ("q_pos", C.c_void_p),
+                ("k_pos", C.c_void_p), ("q_pos_stride", C.c_int64),
+                ("k_pos_stride", C.c_int64)]
+
+
+class Sequence(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("batch_stride", C.c_int64),
+                ("token_stride", C.c_int64), ("head_stride", C.c_int64)]
+
+
 _libs = {}
 
 
@@ -208,6 +238,25 @@ def lib(variant=None):
             "mixrt_linear_grad": (C.c_int, [P, C.POINTER(Kept), C.c_int32, P, I64, P, P, P,
                                             C.c_size_t]),
             "mixrt_rotary_apply": (C.c_int, [P, C.POINTER(Rotary), C.POINTER(Heads), C.c_int32]),
+            "mixrt_rotary_norm_apply": (C.c_int, [P, C.POINTER(Rotary), C.c_float,
+                                                  C.POINTER(NormedHeads), C.c_int32]),
+            "mixrt_rotary_norm_workspace": (C.c_int, [C.POINTER(Rotary), C.POINTER(NormedHeads),
+                                                      C.c_int32, C.POINTER(C.c_size_t)]),
+            "mixrt_rotary_norm_backward": (C.c_int, [P, C.POINTER(Rotary), C.c_float,
+                                                     C.POINTER(NormedHeads), C.c_int32, P,
+                                                     C.c_size_t]),
+            "mixrt_attention_workspace": (C.c_int, [C.POINTER(Attention),
+                                                    C.POINTER(RelativeBiasDesc), C.c_int32,
+                                                    C.POINTER(C.c_size_t)]),
+            "mixrt_attention_forward": (C.c_int, [P, C.POINTER(Attention),
+                                                  C.POINTER(RelativeBiasDesc),
+                                                  *[C.POINTER(Sequence)] * 4, P, P, P,
+                                                  C.c_size_t]),
+            "mixrt_attention_backward": (C.c_int, [P, C.POINTER(Attention),
+                                                   C.POINTER(RelativeBiasDesc),
+                                                   *[C.POINTER(Sequence)] * 5, P, P,
+                                                   *[C.POINTER(Sequence)] * 3, P, P,
+                                                   C.c_size_t]),
             "mixrt_status_string": (C.c_char_p, [C.c_int]),
             "mixrt_last_error": (C.c_char_p, [P]),
             "mixrt_thread_error": (C.c_char_p, []),
@@ -576,6 +625,117 @@ def _rotary_plan(arrays, outs, pos, freq, axis, layout, inverse, device):
             ends += [step, stride[-2]]
         p.heads[i] = Heads(x.shape[-2], x.shape[-1], _elem_code(x.dtype, name), 0, 0, *ends)
     return p
+
+
+def _rotary_norm_plan(arrays, outs, grads, weights, pos, freq, axis, layout, device):
+    """The descriptors of rotary_norm (grads None) or of its backward pass."""
+    p = _rotary_plan(arrays, outs, pos, freq, axis, layout, False, device)
+    tokens = p.rotary.tokens
+    p.normed = (NormedHeads * len(arrays))()
+    for i, (h, x) in enumerate(zip(p.heads, arrays)):
+        dt, dh = 0, 0
+        if grads is not None:
+            g = grads[i]
+            if g.stride(-1) != 1 and g.shape[-1] > 1:
+                raise ValueError(f"grads[{i}]: elements of a head are not neighbours")
+            dt, dh = _run(g.shape[:-2], g.stride()[:-2], f"grads[{i}]")[1], g.stride(-2)
+        p.normed[i] = NormedHeads(h.heads, h.head_dim, h.dtype, 0, 0, 0, 0, 0, h.x_token_stride,
+                                  h.x_head_stride, dt, dh, h.out_token_stride, h.out_head_stride)
+        _per_channel(weights[i], f"weights[{i}]", x.shape[-1], device)
+    p.tokens = tokens
+    return p
+
+
+@dataclass
+class RelativeBias:
+    """A learned bias of attention by the buckets of relative positions: for each
+    axis a, table[a, buckets[a, d + reach], head] of the distance
+    d = k_pos[j, a] - q_pos[i, a], cut to -reach .. reach.  table: float32
+    [axes, count, heads]; buckets: uint8 [axes, 2 reach + 1] (see
+    distance_buckets); q_pos, k_pos: int32 [tokens, axes], or [batch, tokens, axes]
+    with an entry's own (all contiguous)."""
+
+    table: object
+    buckets: object
+    q_pos: object
+    k_pos: object
+
+
+def distance_buckets(count: int, reach: int, near=None):
+    """Buckets of the distances -reach .. reach, uint8 [2 reach + 1] on the host,
+    for RelativeBias.buckets: the first half of the count buckets for distances up
+    to 0, the rest for those above; in each half the near smallest (a half of them
+    by default) hold one distance each, the others distances that grow as their
+    logarithm, up to reach."""
+    if not 1 <= count <= MAX_BIAS_BUCKETS or not 0 <= reach <= MAX_BIAS_REACH:
+        raise ValueError(f"{count} buckets to distance {reach}: at most {MAX_BIAS_BUCKETS} "
+                         f"and {MAX_BIAS_REACH}")
+    import torch
+    half = (count + 1) // 2
+    near = max(1, half // 2) if near is None else near
+    if not 1 <= near <= half:
+        raise ValueError(f"near={near}: 1 to {half} of {count} buckets")
+
+    def of(n: int, buckets: int) -> int:
+        # the last b with (reach + 1 over near)^((b - near) / (buckets - near)) near <= n
+        if n < near or buckets <= near:
+            return min(n, buckets - 1)
+        b = near
+        while (b + 1 < buckets and near ** (buckets - b - 1) * (reach + 1) ** (b + 1 - near)
+               <= n ** (buckets - near)):
+            b += 1
+        return b
+
+    left = [of(n, half) for n in range(reach + 1)]
+    right = [half + of(n - 1, count - half) if count > half else left[n]
+             for n in range(1, reach + 1)]
+    return torch.tensor(left[::-1] + right, dtype=torch.uint8)
+
+
+@dataclass
+class AttentionSaved:
+    """What attention_backward needs of attention_train besides its output: lse
+    float32 [batch, heads, queries], and what rounding took from the output
+    (float16 and bfloat16; None for float32)."""
+
+    lse: object
+    rest: object
+
+
+def _as_sequence(t, name: str):
+    """The strides of heads [batch, tokens, heads, D] (a Sequence without data)."""
+    if t.dim() != 4:
+        raise ValueError(f"{name}: {t.dim()} dimensions, expected [batch, tokens, heads, D]")
+    b, n, h, d = t.stride()
+    if d != 1 and t.shape[3] > 1:
+        raise ValueError(f"{name}: elements of a head are not neighbours (stride {d})")
+    return Sequence(0, b, n, h)
+
+
+def _bias_desc(bias, B, Tq, Tk, heads, device):
+    if not isinstance(bias, RelativeBias):
+        raise TypeError(f"bias: expected a RelativeBias, got {type(bias).__name__}")
+    import torch
+    for name, dt in (("table", torch.float32), ("buckets", torch.uint8), ("q_pos", torch.int32),
+                     ("k_pos", torch.int32)):
+        t = getattr(bias, name)
+        _on_gpu(t, f"bias.{name}", device)
+        if t.dtype != dt or not t.is_contiguous():
+            raise ValueError(f"bias.{name}: {t.dtype}, expected contiguous {dt}")
+    table, buckets = bias.table, bias.buckets
+    if table.dim() != 3 or table.shape[2] != heads:
+        raise ValueError(f"bias.table: {tuple(table.shape)}, expected [axes, count, {heads}]")
+    axes = table.shape[0]
+    if buckets.dim() != 2 or buckets.shape[0] != axes or buckets.shape[1] % 2 != 1:
+        raise ValueError(f"bias.buckets: {tuple(buckets.shape)}, expected [{axes}, 2 reach + 1]")
+    steps = []
+    for name, n in (("q_pos", Tq), ("k_pos", Tk)):
+        t = getattr(bias, name)
+        if t.shape != (n, axes) and t.shape != (B, n, axes):
+            raise ValueError(f"bias.{name}: {tuple(t.shape)}, expected [{n}, {axes}] or "
+                             f"[{B}, {n}, {axes}]")
+        steps.append(n * axes if t.dim() == 3 else 0)
+    return RelativeBiasDesc(axes, table.shape[1], buckets.shape[1] // 2, 0, 0, 0, 0, *steps)
 
 
 @dataclass
@@ -1126,6 +1286,281 @@ class Renderer:
                 or freq.requires_grad):
             outs = self._result("rotary", outs, (*arrays, pos, freq))
         return outs[0] if single else outs
+
+
+    # -- the refiner's attention
+
+    def _normed_key(self, name, arrays, grads, weights, pos, freq, axis, layout):
+        try:
+            key = (name, layout, pos.shape, pos.stride(), pos.dtype, pos.get_device(),
+                   freq.shape, freq.stride(), freq.dtype, freq.get_device(),
+                   axis.shape, axis.stride(), axis.dtype, axis.get_device())
+            for x in (*arrays, *grads):
+                key += (x.shape, x.stride(), x.dtype, x.get_device())
+            for w in weights:
+                key += (None if w is None else
+                        (w.shape, w.stride(), w.dtype, w.get_device()),)
+        except AttributeError:
+            raise TypeError("heads, weights, pos, freq and axis: expected torch.Tensors") from None
+        return key
+
+    def _as_arrays(self, heads, weights):
+        single = isinstance(heads, self._torch.Tensor)
+        arrays = (heads,) if single else tuple(heads)
+        if weights is None:
+            weights = (None,) * len(arrays)
+        else:
+            weights = (weights,) if single else tuple(weights)
+        if len(weights) != len(arrays):
+            raise ValueError(f"{len(arrays)} arrays and {len(weights)} weights")
+        return single, arrays, weights
+
+    def rotary_norm(self, heads, weights, pos, freq, axis, *, eps: float = 1e-6,
+                    layout: str = "halves", out=None):
+        """Heads normed one by one and turned, in one pass: x / sqrt(mean(x^2) +
+        eps) * weight over each head, then rotary.  heads, pos, freq, axis, layout
+        and out as in rotary; weights: a float32 [D] (or None) for each array of
+        heads, likewise one or a tuple, or None for none."""
+        single, arrays, weights = self._as_arrays(heads, weights)
+        key = self._normed_key("rotary_norm", arrays, (), weights, pos, freq, axis, layout)
+        if out is None:
+            here = self._here()
+            outs = tuple([self._empty_like(x, here) for x in arrays])
+        else:
+            self._refuse_out("rotary_norm", (*arrays, *weights, pos, freq))
+            outs = (out,) if single else tuple(out)
+            if len(outs) != len(arrays):
+                raise ValueError(f"{len(arrays)} arrays and {len(outs)} outputs")
+            for i, (x, o) in enumerate(zip(arrays, outs)):
+                _like(o, f"out[{i}]", x.shape, x.dtype, self.device)
+                key += (o.stride(),)
+        p = self._plans.get(key)
+        if p is None:
+            p = self._plan(key, lambda: _rotary_norm_plan(arrays, outs, None, weights, pos, freq,
+                                                          axis, layout, self.device))
+        p.rotary.pos, p.rotary.freq = pos.data_ptr(), freq.data_ptr()
+        p.rotary.axis = axis.data_ptr()
+        for d, x, o, w in zip(p.normed, arrays, outs, weights):
+            d.x, d.out = x.data_ptr(), o.data_ptr()
+            d.weight = 0 if w is None else w.data_ptr()
+        rc = self._L.mixrt_rotary_norm_apply(self._h, p.rotary_ref, eps, p.normed, len(arrays))
+        if rc:
+            self._check(rc)
+        if self._follows(*arrays, *weights, pos, freq):
+            outs = self._result("rotary_norm", outs, (*arrays, *weights, pos, freq))
+        return outs[0] if single else outs
+
+    def rotary_norm_backward(self, grads, heads, weights, pos, freq, axis, *, eps: float = 1e-6,
+                             layout: str = "halves", out=None):
+        """(dheads, dweights) of rotary_norm at grads, the gradients of its
+        outputs: each one tensor or a tuple, as heads is; dweights float32 [D].
+        The other arguments as rotary_norm had them; out: where dheads go (grads
+        themselves will do)."""
+        single, arrays, weights = self._as_arrays(heads, weights)
+        grads = (grads,) if single else tuple(grads)
+        if len(grads) != len(arrays):
+            raise ValueError(f"{len(arrays)} arrays and {len(grads)} gradients")
+        for i, (x, g) in enumerate(zip(arrays, grads)):
+            _like(g, f"grads[{i}]", x.shape, x.dtype, self.device)
+        key = self._normed_key("rotary_norm_backward", arrays, grads, weights, pos, freq, axis,
+                               layout)
+        here = self._here()
+        inputs = (*grads, *arrays, *weights, pos, freq)
+        if out is None:
+            outs = tuple([self._empty_like(x, here) for x in arrays])
+        else:
+            self._refuse_out("rotary_norm_backward", inputs)
+            outs = (out,) if single else tuple(out)
+            if len(outs) != len(arrays):
+                raise ValueError(f"{len(arrays)} arrays and {len(outs)} outputs")
+            for i, (x, o) in enumerate(zip(arrays, outs)):
+                _like(o, f"out[{i}]", x.shape, x.dtype, self.device)
+                key += (o.stride(),)
+        p = self._plans.get(key)
+        if p is None:
+            def make():
+                p = _rotary_norm_plan(arrays, outs, grads, weights, pos, freq, axis, layout,
+                                      self.device)
+                p.bytes = self._size(self._L.mixrt_rotary_norm_workspace, p.rotary_ref, p.normed,
+                                     len(arrays))
+                return p
+            p = self._plan(key, make)
+        p.rotary.pos, p.rotary.freq = pos.data_ptr(), freq.data_ptr()
+        p.rotary.axis = axis.data_ptr()
+        dweights = tuple([self._empty((x.shape[-1],), self._torch.float32, here) for x in arrays])
+        for d, x, g, o, w, dw in zip(p.normed, arrays, grads, outs, weights, dweights):
+            d.x, d.dy, d.out, d.dweight = x.data_ptr(), g.data_ptr(), o.data_ptr(), dw.data_ptr()
+            d.weight = 0 if w is None else w.data_ptr()
+        ws = self._workspace(p.bytes, here)
+        rc = self._L.mixrt_rotary_norm_backward(self._h, p.rotary_ref, eps, p.normed, len(arrays),
+                                                ws[0], ws[1])
+        if rc:
+            self._check(rc)
+        if self._follows(*inputs):
+            got = self._result("rotary_norm_backward", (*outs, *dweights), inputs)
+            outs, dweights = got[:len(arrays)], got[len(arrays):]
+        return (outs[0], dweights[0]) if single else (outs, dweights)
+
+    @staticmethod
+    def _follows(*inputs) -> bool:
+        for t in inputs:
+            if t is not None and t.requires_grad:
+                return True
+        return False
+
+    def _attention_plan(self, q, k, v, lens, bias, scale, backward: bool):
+        """The plan of a call over q, k and v, with their addresses, the lengths'
+        and the bias' filled in."""
+        try:
+            key = ("attention", backward, scale, q.shape, q.stride(), q.dtype, q.get_device(),
+                   k.shape, k.stride(), k.dtype, k.get_device(),
+                   v.shape, v.stride(), v.dtype, v.get_device())
+            if lens is not None:
+                key += (lens.shape, lens.stride(), lens.dtype, lens.get_device())
+            if bias is not None:
+                for t in (bias.table, bias.buckets, bias.q_pos, bias.k_pos):
+                    key += (t.shape, t.stride(), t.dtype, t.get_device())
+        except AttributeError:
+            raise TypeError("q, k, v and lens: expected torch.Tensors, bias: a "
+                            "RelativeBias of them") from None
+        p = self._plans.get(key)
+        if p is None:
+            p = self._plan(key, self._make_attention, q, k, v, lens, bias, scale, backward)
+        p.q.data, p.k.data, p.v.data = q.data_ptr(), k.data_ptr(), v.data_ptr()
+        if lens is not None:
+            p.att.lens = lens.data_ptr()
+        if bias is not None:
+            d = p.bias
+            d.table, d.buckets = bias.table.data_ptr(), bias.buckets.data_ptr()
+            d.q_pos, d.k_pos = bias.q_pos.data_ptr(), bias.k_pos.data_ptr()
+        return p
+
+    def _make_attention(self, q, k, v, lens, bias, scale, backward):
+        p = _Plan()
+        for t, name in ((q, "q"), (k, "k"), (v, "v")):
+            _on_gpu(t, name, self.device)
+        p.q, p.k, p.v = _as_sequence(q, "q"), _as_sequence(k, "k"), _as_sequence(v, "v")
+        B, Tq, H, D = q.shape
+        Tk, Hk = k.shape[1:3]
+        if k.shape != (B, Tk, Hk, D) or v.shape != k.shape or Hk < 1 or H % Hk:
+            raise ValueError(f"q {tuple(q.shape)}, k {tuple(k.shape)}, v {tuple(v.shape)}: "
+                             "expected [batch, queries, heads, D] and [batch, keys, kv_heads, D] "
+                             "with kv_heads a divisor of heads")
+        if k.dtype != q.dtype or v.dtype != q.dtype:
+            raise ValueError(f"q {q.dtype}, k {k.dtype}, v {v.dtype}: expected one dtype")
+        if lens is not None:
+            _on_gpu(lens, "lens", self.device)
+            if lens.shape != (B,) or lens.dtype != self._torch.int32 or not lens.is_contiguous():
+                raise ValueError(f"lens: {lens.dtype} {tuple(lens.shape)}, expected contiguous "
+                                 f"int32 ({B},)")
+        p.att = Attention(B, H, Hk, D, _elem_code(q.dtype, "q"),
+                          1.0 / D ** 0.5 if scale is None else float(scale), Tq, Tk, 0)
+        p.bias = None if bias is None else _bias_desc(bias, B, Tq, Tk, H, self.device)
+        p.att_ref = C.byref(p.att)
+        p.bias_ref = None if bias is None else C.byref(p.bias)
+        p.bytes = self._size(self._L.mixrt_attention_workspace, p.att_ref, p.bias_ref,
+                             int(backward))
+        p.q_ref, p.k_ref, p.v_ref = C.byref(p.q), C.byref(p.k), C.byref(p.v)
+        # dense outputs
+        p.o = Sequence(0, Tq * H * D, H * D, D)
+        p.o_ref = C.byref(p.o)
+        p.dk, p.dv = Sequence(0, Tk * Hk * D, Hk * D, D), Sequence(0, Tk * Hk * D, Hk * D, D)
+        p.dk_ref, p.dv_ref = C.byref(p.dk), C.byref(p.dv)
+        p.q_shape, p.k_shape, p.lse_shape = (B, Tq, H, D), (B, Tk, Hk, D), (B, H, Tq)
+        return p
+
+    def _attend(self, p, q, out, lse, rest, here):
+        if out is None:
+            out = self._empty(p.q_shape, q.dtype, here)
+            p.o.data = out.data_ptr()
+            out_ref = p.o_ref
+        else:
+            _like(out, "out", q.shape, q.dtype, self.device)
+            seq = _as_sequence(out, "out")
+            seq.data = out.data_ptr()
+            out_ref = C.byref(seq)
+        ws = self._workspace(p.bytes, here)
+        rc = self._L.mixrt_attention_forward(
+            self._h, p.att_ref, p.bias_ref, p.q_ref, p.k_ref, p.v_ref, out_ref,
+            None if lse is None else lse.data_ptr(), None if rest is None else rest.data_ptr(),
+            ws[0], ws[1])
+        if rc:
+            self._check(rc)
+        return out
+
+    def attention(self, q, k, v, *, lens=None, bias=None, scale=None, out=None):
+        """softmax(scale q k^T + bias) v of q [batch, queries, heads, D] over
+        k, v [batch, keys, kv_heads, D] (float32, float16 or bfloat16; D at most
+        128; slices of a joint projection will do); kv_heads divides heads.
+        lens: int32 [batch], the valid keys of each entry (what lies behind is
+        never read; an entry without keys gives 0); bias: a RelativeBias; scale:
+        1 / sqrt(D) by default.  out: q's shape and type."""
+        p = self._attention_plan(q, k, v, lens, bias, scale, False)
+        table = None if bias is None else bias.table
+        if out is not None:
+            self._refuse_out("attention", (q, k, v, table))
+        out = self._attend(p, q, out, None, None, self._here())
+        if self._follows(q, k, v, table):
+            return self._result("attention", (out,), (q, k, v, table))[0]
+        return out
+
+    def attention_train(self, q, k, v, *, lens=None, bias=None, scale=None, out=None):
+        """(out, saved) for a training step: out as attention gives it, and what
+        attention_backward needs besides (an AttentionSaved)."""
+        p = self._attention_plan(q, k, v, lens, bias, scale, False)
+        table = None if bias is None else bias.table
+        if out is not None:
+            self._refuse_out("attention_train", (q, k, v, table))
+        here = self._here()
+        lse = self._empty(p.lse_shape, self._torch.float32, here)
+        rest = (None if p.att.dtype == MIXRT_F32
+                else self._empty(p.q_shape, q.dtype, here))
+        out = self._attend(p, q, out, lse, rest, here)
+        if self._follows(q, k, v, table):
+            out = self._result("attention_train", (out,), (q, k, v, table))[0]
+        return out, AttentionSaved(lse, rest)
+
+    def attention_backward(self, dout, q, k, v, out, saved: AttentionSaved, *, lens=None,
+                           bias=None, scale=None):
+        """(dq, dk, dv) of attention_train at dout, or (dq, dk, dv, dtable) with a
+        bias (dtable float32, as the table is); out and saved as it gave them, the
+        other arguments as it had them.  Gradients of keys and values are summed
+        over the query heads that share them, and 0 behind lens."""
+        p = self._attention_plan(q, k, v, lens, bias, scale, True)
+        dev, f32 = self.device, self._torch.float32
+        _like(dout, "dout", q.shape, q.dtype, dev)
+        _like(out, "out", q.shape, q.dtype, dev)
+        if not isinstance(saved, AttentionSaved):
+            raise TypeError(f"saved: expected an AttentionSaved, got {type(saved).__name__}")
+        lse, rest = saved.lse, saved.rest
+        _like(lse, "saved.lse", p.lse_shape, f32, dev)
+        if not lse.is_contiguous():
+            raise ValueError("saved.lse: not contiguous")
+        if p.att.dtype != MIXRT_F32:
+            _like(rest, "saved.rest", q.shape, q.dtype, dev)
+            if not rest.is_contiguous():
+                raise ValueError("saved.rest: not contiguous")
+        dout_seq, out_seq = _as_sequence(dout, "dout"), _as_sequence(out, "out")
+        dout_seq.data, out_seq.data = dout.data_ptr(), out.data_ptr()
+        here = self._here()
+        dq = self._empty(p.q_shape, q.dtype, here)
+        dk, dv = (self._empty(p.k_shape, q.dtype, here) for _ in range(2))
+        table = None if bias is None else bias.table
+        dtable = None if bias is None else self._empty(table.shape, f32, here)
+        p.o.data, p.dk.data, p.dv.data = dq.data_ptr(), dk.data_ptr(), dv.data_ptr()
+        ws = self._workspace(p.bytes, here)
+        rc = self._L.mixrt_attention_backward(
+            self._h, p.att_ref, p.bias_ref, C.byref(dout_seq), p.q_ref, p.k_ref, p.v_ref,
+            C.byref(out_seq), lse.data_ptr(),
+            None if p.att.dtype == MIXRT_F32 else rest.data_ptr(), p.o_ref, p.dk_ref, p.dv_ref,
+            None if dtable is None else dtable.data_ptr(), ws[0], ws[1])
+        if rc:
+            self._check(rc)
+        grads = (dq, dk, dv) if bias is None else (dq, dk, dv, dtable)
+        inputs = (dout, q, k, v, out, table)
+        if self._follows(*inputs):
+            grads = tuple(self._result("attention_backward", grads, inputs))
+        return grads
 
 
 def validate(gbuf, cams, disp, grid, mlp, smp):
