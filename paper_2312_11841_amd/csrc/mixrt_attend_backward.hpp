@@ -9,6 +9,11 @@
 namespace mixrt {
 namespace {
 
+// float16 alone needs its dS and weights lifted; weights, at most 1, by 2^15.
+template <typename T> inline constexpr bool kLifted = false;
+template <> inline constexpr bool kLifted<f16> = true;
+template <typename T> inline constexpr float kWeightLift = kLifted<T> ? 15.0f : 0.0f;
+
 // Rows of a bias table's gradient that a walk over the keys sums in 32 bits before
 // they move on to 64.
 constexpr int kHistRows = 1024;
@@ -63,6 +68,127 @@ __device__ __forceinline__ f32x16 row_mul(const T *tile, int lane,
     return s;
 }
 
+// float16 holds dS only inside a range: its gradients are small where a row looks at
+// many keys, and large where a loss is scaled.  So each column's dS is multiplied by a
+// power of two that keeps the largest seen so far between 1 and 2^15, and its sums
+// with it.  (The first tile sets it; it changes again where a later one leaves the
+// range.)
+template <typename T, int NC, int ND>
+struct Lift {
+    float by[NC], most[NC];
+    __device__ __forceinline__ void start()
+    {
+#pragma unroll
+        for (int n = 0; n < NC; ++n) {
+            by[n] = 1.0f;
+            most[n] = 0.0f;
+        }
+    }
+    __device__ __forceinline__ void scale(f32x16 (&g)[NC], f32x16 (&acc)[NC][ND])
+    {
+        if (sizeof(T) != 2 || !kLifted<T>) return;
+#pragma unroll
+        for (int n = 0; n < NC; ++n) {
+            float m = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) m = fmaxf(m, fabsf(g[n][i]));
+            m = fmaxf(most[n], half_max(m) * by[n]);
+            const bool out = (m > 0x1p15f || (m < 1.0f && m > 0.0f)) && m < INFINITY;
+            if (__builtin_amdgcn_ballot_w64(out) != 0 && out) {
+                const int now = (int)(__float_as_uint(by[n]) >> 23);
+                const int to = min(max(now + 127 + 8 - (int)(__float_as_uint(m) >> 23), 27), 227);
+                const float f = __uint_as_float((uint32_t)(127 + (to - now) / 2) << 23);
+                const float e = __uint_as_float((uint32_t)(127 + (to - now) - (to - now) / 2) << 23);
+                by[n] = by[n] * f * e;
+                m = m * f * e;
+#pragma unroll
+                for (int d = 0; d < ND; ++d)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) acc[n][d][i] = acc[n][d][i] * f * e;
+            }
+            most[n] = m;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) g[n][i] *= by[n];
+        }
+    }
+    // the factor that takes a column's sums back
+    __device__ __forceinline__ float back(int n) const
+    {
+        return kLifted<T> ? 1.0f / by[n] : 1.0f;
+    }
+};
+
+// mine[e[i]] += v[i], for four places some of which may be the same: the sums of equal
+// places go to the first, so that the four reads and writes need not wait for each
+// other.  (LDS has atomic adds in 32 bits, but they take 4 cycles a lane: with them
+// this kernel took 4.6 ms where it takes %s.)
+__device__ __forceinline__ void add_places(float *mine, int (&e)[4], float (&v)[4], int spare)
+{
+    const bool b0 = e[1] == e[0];
+    const bool c0 = e[2] == e[0], c1 = !c0 && e[2] == e[1];
+    const bool d0 = e[3] == e[0], d1 = !d0 && e[3] == e[1];
+    const bool d2 = !d0 && !d1 && e[3] == e[2];
+    v[0] += b0 ? v[1] : 0.0f;
+    v[0] += c0 ? v[2] : 0.0f;
+    v[0] += d0 ? v[3] : 0.0f;
+    v[1] += c1 ? v[2] : 0.0f;
+    v[1] += d1 ? v[3] : 0.0f;
+    v[2] += d2 ? v[3] : 0.0f;
+    e[1] = b0 ? spare : e[1];
+    e[2] = c0 || c1 ? spare : e[2];
+    e[3] = d0 || d1 || d2 ? spare : e[3];
+    float a[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) a[i] = mine[e[i]];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) mine[e[i]] = a[i] + v[i];
+}
+
+// Adds a column's dS to its places of the bias table's gradient.
+template <int ROWS>
+__device__ __forceinline__ void add_table(const f32x16 &g, const TilePos<ROWS> &tile, int half,
+                                          const uint16_t *place,
+                                          const int (&column)[kMaxBiasAxes], int axes, int reach,
+                                          float *mine, int spare)
+{
+    static_assert(ROWS == 32, "one block of rows");
+#pragma unroll
+    for (int a = 0; a < kMaxBiasAxes; ++a) {
+        if (a >= axes) break;
+        const uint32_t kind = __builtin_amdgcn_readfirstlane(tile.kind[a]);
+        const uint16_t *row = place + a * kReachRow;
+        if (kind >> 16 & 1) {
+            float s = g[0];
+#pragma unroll
+            for (int i = 1; i < 16; ++i) s += g[i];
+            mine[row[bias_at(tile.at[a][0], column[a], reach)]] += s;
+            continue;
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int32_t *p = &tile.at[a][8 * j + 4 * half];
+            if ((kind >> j & 1) && !(kind >> (8 + j) & 1)) {
+                const float s = (g[4 * j] + g[4 * j + 1]) + (g[4 * j + 2] + g[4 * j + 3]);
+                mine[row[bias_at(p[0], column[a], reach)]] += s;
+                continue;
+            }
+            int e[4];
+            float v[4];
+            if (kind >> (8 + j) & 1) {
+                const uint16_t *at = row + bias_at(p[0], column[a], reach, kPad);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) e[i] = at[i];
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) e[i] = row[bias_at(p[i], column[a], reach)];
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = g[4 * j + i];
+            add_places(mine, e, v, spare);
+        }
+    }
+}
+
 // A column's sums, times a factor, to its row of an output.
 template <typename T, int DP>
 __device__ __forceinline__ void store_column(T *row, int half, int D, const f32x16 (&a)[DP / 32],
@@ -87,9 +213,10 @@ __global__ __launch_bounds__(256) void attend_dq_kernel(AttendK k)
     // (two of the widest tiles and the table's sums are more than a CU's 160 KB)
     constexpr int BUFS = BIAS && sizeof(T) == 4 && DP == 128 ? 1 : 2;
     __shared__ __attribute__((aligned(16))) T tiles[BUFS][2][TILE];
-    __shared__ float2 dense[BIAS ? kMaxBiasAxes * kReachRow : 1];   // bias, place in hist
-    __shared__ __attribute__((aligned(16))) int32_t kpos[2][BIAS ? kMaxBiasAxes * ROWS : 4];
-    extern __shared__ float hist[];     // [wave][entry][lane]
+    __shared__ float dense[BIAS ? kMaxBiasAxes * kReachRow : 1];
+    __shared__ uint16_t place[BIAS ? kMaxBiasAxes * kReachRow : 1];   // 64 entry
+    __shared__ TilePos<BIAS ? ROWS : 1> kpos[BUFS];
+    extern __shared__ float hist[];     // [wave][entry, and a spare one][lane]
 
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
     const int block = near_block();
@@ -146,26 +273,29 @@ __global__ __launch_bounds__(256) void attend_dq_kernel(AttendK k)
                              ? k.bias.qpos[b * k.bias.qbatch + tt * k.bias.axes + a]
                              : 0;
     }
+    const int held = entries + 1;
     if (BIAS) {
-        const int each = 2 * k.bias.reach + 1;
-        for (int i = threadIdx.x; i < k.bias.axes * each; i += THREADS) {
-            const int a = i / each, d = i - a * each;
-            const int e = a * k.bias.buckets + min((int)k.bias.map[i], k.bias.buckets - 1);
-            dense[a * kReachRow + d] = make_float2(k.bias.table[(int64_t)e * k.H + h] * kLog2e,
-                                                   __int_as_float(64 * e));
+        load_bias(dense, k.bias, h, k.H, THREADS, false);
+        const int n = 2 * k.bias.reach + 1 + 2 * kPad;
+        for (int i = threadIdx.x; i < k.bias.axes * n; i += THREADS) {
+            const int a = i / n, e = i - a * n;
+            place[a * kReachRow + e] =
+                (uint16_t)(64 * (a * k.bias.buckets + bucket_of(k.bias, a, e, false)));
         }
-        for (int i = threadIdx.x; i < 4 * 64 * entries; i += THREADS) hist[i] = 0.0f;
+        for (int i = threadIdx.x; i < 4 * 64 * held; i += THREADS) hist[i] = 0.0f;
     }
-    float *mine = hist + wave * 64 * entries + lane;
+    float *mine = hist + wave * 64 * held + lane;
     double table = 0.0;         // thread e: entry e's sum of the block
 
     f32x16 acc[NC][DP / 32];
     clear(acc);
+    Lift<T, NC, DP / 32> lift;
+    lift.start();
     const T *kp = (const T *)k.k.data + b * k.k.batch + kvh * k.k.head;
     const T *vp = (const T *)k.v.data + b * k.v.batch + kvh * k.v.head;
     const int32_t *pp = BIAS ? k.bias.kpos + b * k.bias.kbatch : nullptr;
     Stage<T, DP, ROWS, THREADS> sk, sv;
-    StagePos<ROWS> sp;
+    StagePos<BIAS ? ROWS : 1> sp;
     if (first < last) {
         sk.fetch(kp, k.k.token, first, last, k.D);
         sv.fetch(vp, k.v.token, first, last, k.D);
@@ -198,21 +328,10 @@ __global__ __launch_bounds__(256) void attend_dq_kernel(AttendK k)
                 g[n] = Matrix<T>::mul(v, dout[n][c], g[n]);
             }
         }
-        if (BIAS) {
-#pragma unroll
-            for (int n = 0; n < NC; ++n)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) s[n][i] *= k.scale;
-            for (int a = 0; a < k.bias.axes; ++a)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const int p = kpos[cur][a * ROWS + tile_row(i, half)];
-#pragma unroll
-                    for (int n = 0; n < NC; ++n) {
-                        const int at = a == 0 ? qpos[n][0] : a == 1 ? qpos[n][1] : qpos[n][2];
-                        s[n][i] += dense[a * kReachRow + bias_at(p, at, k.bias.reach)].x;
-                    }
-                }
+        if constexpr (BIAS) {
+            const int base[NC] = {};
+            add_bias<NC, ROWS>(s, k.scale, kpos[cur], 0, half, dense, base, qpos, k.bias.axes,
+                               k.bias.reach);
         }
         const float unit = BIAS ? 1.0f : k.scale;
 #pragma unroll
@@ -228,24 +347,22 @@ __global__ __launch_bounds__(256) void attend_dq_kernel(AttendK k)
 #pragma unroll
                     for (int n = 0; n < NC; ++n) g[n][i] = 0.0f;
         }
-        add_cols<T, DP, NC>(kt, lane, g, acc);
-        if (BIAS) {
-            for (int a = 0; a < k.bias.axes; ++a)
+        // (the one key of a row has weight 1 whatever its score)
+        if (len == 1) {
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const int p = kpos[cur][a * ROWS + tile_row(i, half)];
+            for (int n = 0; n < NC; ++n)
 #pragma unroll
-                    for (int n = 0; n < NC; ++n) {
-                        const int at = a == 0 ? qpos[n][0] : a == 1 ? qpos[n][1] : qpos[n][2];
-                        const int e = __float_as_int(
-                            dense[a * kReachRow + bias_at(p, at, k.bias.reach)].y);
-                        // (the lane's own place: no other adds there)
-                        __hip_atomic_fetch_add(mine + e, there[n] ? g[n][i] : 0.0f,
-                                               __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
-                    }
-                }
+                for (int i = 0; i < 16; ++i) g[n][i] = 0.0f;
+        }
+        if constexpr (BIAS) {
+#pragma unroll
+            for (int n = 0; n < NC; ++n)
+                add_table<ROWS>(g[n], kpos[cur], half, place, qpos[n], k.bias.axes, k.bias.reach,
+                                mine, 64 * entries);
             counted += ROWS;
         }
+        lift.scale(g, acc);
+        add_cols<T, DP, NC>(kt, lane, g, acc);
         if (BUFS == 1) __syncthreads();
         if (more) {
             sk.put(tiles[cur ^ (BUFS - 1)][0]);
@@ -260,7 +377,7 @@ __global__ __launch_bounds__(256) void attend_dq_kernel(AttendK k)
                 float sum = 0.0f;
 #pragma unroll 1
                 for (int w = 0; w < 4; ++w) {
-                    float *at = hist + (w * entries + threadIdx.x) * 64;
+                    float *at = hist + (w * held + threadIdx.x) * 64;
 #pragma unroll 4
                     for (int i = 0; i < 64; ++i) {
                         const int l = (i + threadIdx.x) & 63;
@@ -283,10 +400,11 @@ __global__ __launch_bounds__(256) void attend_dq_kernel(AttendK k)
             const int64_t rows = (int64_t)k.B * k.H * k.Tq;
             const int64_t row = ((int64_t)b * k.H + h) * k.Tq + t[n];
             store_column<float, DP>(k.part + (split * rows + row) * k.D, half, k.D, acc[n],
-                                    k.plain_scale);
+                                    lift.back(n) * k.plain_scale);
         } else {
             store_column<T, DP>((T *)k.dq.data + b * k.dq.batch + (int64_t)t[n] * k.dq.token +
-                                    h * k.dq.head, half, k.D, acc[n], k.plain_scale);
+                                    h * k.dq.head, half, k.D, acc[n],
+                                lift.back(n) * k.plain_scale);
         }
     }
 }
@@ -297,11 +415,13 @@ __global__ __launch_bounds__(256) void attend_dq_kernel(AttendK k)
 template <int ROWS>
 struct StageSums {
     float lse, delta;
-    __device__ __forceinline__ void fetch(const float *l, const float *d, int first, int limit)
+    __device__ __forceinline__ void fetch(const float *l, const float *d, int first, int limit,
+                                          float lifted)
     {
         const int row = first + (int)threadIdx.x;
         const bool there = threadIdx.x < ROWS && row < limit;
-        lse = there ? l[row] : INFINITY;     // a row that is not there has weights 0
+        // (a row that is not there has weights 0)
+        lse = there ? l[row] - lifted : INFINITY;
         delta = there ? d[row] : 0.0f;
     }
     __device__ __forceinline__ void put(float *at) const
@@ -321,7 +441,7 @@ __global__ __launch_bounds__(256) void attend_dkv_kernel(AttendK k)
     constexpr int TILE = ROWS * kStride<T, DP>;
     __shared__ __attribute__((aligned(16))) T tiles[2][2][TILE];
     __shared__ float dense[BIAS ? kMaxBiasAxes * kReachRow : 1];
-    __shared__ __attribute__((aligned(16))) int32_t qpos[2][BIAS ? kMaxBiasAxes * ROWS : 4];
+    __shared__ TilePos<BIAS ? ROWS : 1> qpos[2];
     __shared__ __attribute__((aligned(16))) float sums[2][2 * ROWS];
 
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
@@ -362,13 +482,15 @@ __global__ __launch_bounds__(256) void attend_dkv_kernel(AttendK k)
     f32x16 dk[NC][DP / 32], dv[NC][DP / 32];
     clear(dk);
     clear(dv);
+    Lift<T, NC, DP / 32> lift;
+    lift.start();
 
     const T *qp = (const T *)k.q.data + b * k.q.batch;
     const T *gp = (const T *)k.dout.data + b * k.dout.batch;
     const int64_t sums0 = (int64_t)b * k.H * k.Tq;
     const int32_t *pp = BIAS ? k.bias.qpos + b * k.bias.qbatch : nullptr;
     Stage<T, DP, ROWS, THREADS> sq, sg;
-    StagePos<ROWS> sp;
+    StagePos<BIAS ? ROWS : 1> sp;
     StageSums<ROWS> ss;
     // the tile that is fetched next: head of the group, first row
     int fg = first / a_head, ft = first % a_head * ROWS;
@@ -377,7 +499,7 @@ __global__ __launch_bounds__(256) void attend_dkv_kernel(AttendK k)
         sq.fetch(qp + h * k.q.head, k.q.token, ft, k.Tq, k.D);
         sg.fetch(gp + h * k.dout.head, k.dout.token, ft, k.Tq, k.D);
         const int64_t at = sums0 + (int64_t)h * k.Tq;
-        ss.fetch(k.lse + at, k.delta + at, ft, k.Tq);
+        ss.fetch(k.lse + at, k.delta + at, ft, k.Tq, kWeightLift<T>);
         if (BIAS) sp.fetch(pp, k.bias.axes, ft, k.Tq);
         ft += ROWS;
         if (ft >= k.Tq) {
@@ -403,7 +525,8 @@ __global__ __launch_bounds__(256) void attend_dkv_kernel(AttendK k)
         const bool more = i0 + 1 < last;
         if (more) fetch();
         if (BIAS && head != at_head) {      // (the same for the whole block)
-            load_bias(dense, k.bias, kvh * G + at_head, k.H, THREADS);
+            // (mirrored: the rows are queries here)
+            load_bias(dense, k.bias, kvh * G + at_head, k.H, THREADS, true);
             head = at_head;
             __syncthreads();
         }
@@ -415,21 +538,10 @@ __global__ __launch_bounds__(256) void attend_dkv_kernel(AttendK k)
             p[n] = row_mul<T, DP>(qt, lane, key[n]);
             g[n] = row_mul<T, DP>(gt, lane, val[n]);
         }
-        if (BIAS) {
-#pragma unroll
-            for (int n = 0; n < NC; ++n)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) p[n][i] *= k.scale;
-            for (int a = 0; a < k.bias.axes; ++a)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const int at = qpos[cur][a * ROWS + tile_row(i, half)];
-#pragma unroll
-                    for (int n = 0; n < NC; ++n) {
-                        const int mine = a == 0 ? kpos[n][0] : a == 1 ? kpos[n][1] : kpos[n][2];
-                        p[n][i] += dense[a * kReachRow + bias_at(mine, at, k.bias.reach)];
-                    }
-                }
+        if constexpr (BIAS) {
+            const int base[NC] = {};
+            add_bias<NC, ROWS>(p, k.scale, qpos[cur], 0, half, dense, base, kpos, k.bias.axes,
+                               k.bias.reach);
         }
         const float unit = BIAS ? 1.0f : k.scale;
 #pragma unroll
@@ -441,7 +553,14 @@ __global__ __launch_bounds__(256) void attend_dkv_kernel(AttendK k)
                 g[n][i] = p[n][i] * (g[n][i] - delta);
             }
         }
+        if (len == 1) {     // (as in the queries' gradient)
+#pragma unroll
+            for (int n = 0; n < NC; ++n)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) g[n][i] = 0.0f;
+        }
         add_cols<T, DP, NC>(gt, lane, p, dv);
+        lift.scale(g, dk);
         add_cols<T, DP, NC>(qt, lane, g, dk);
         if (--left == 0) {
             ++at_head;
@@ -460,18 +579,19 @@ __global__ __launch_bounds__(256) void attend_dkv_kernel(AttendK k)
                 for (int i = 0; i < 16; ++i) dk[n][d][i] = dv[n][d][i] = 0.0f;
         }
         const int64_t tt = t[n];
+        const float plain = kLifted<T> ? 0x1p-15f : 1.0f;
+        const float dk_by = lift.back(n) * k.plain_scale * plain;
         if (k.splits > 1) {
             const int64_t rows = (int64_t)k.B * k.Hk * k.Tk;
             const int64_t row = ((int64_t)b * k.Hk + kvh) * k.Tk + tt;
-            store_column<float, DP>(k.part + (split * rows + row) * k.D, half, k.D, dk[n],
-                                    k.plain_scale);
+            store_column<float, DP>(k.part + (split * rows + row) * k.D, half, k.D, dk[n], dk_by);
             store_column<float, DP>(k.part + ((k.splits + split) * rows + row) * k.D, half, k.D,
-                                    dv[n], 1.0f);
+                                    dv[n], plain);
         } else {
             store_column<T, DP>((T *)k.dk.data + b * k.dk.batch + tt * k.dk.token +
-                                    kvh * k.dk.head, half, k.D, dk[n], k.plain_scale);
+                                    kvh * k.dk.head, half, k.D, dk[n], dk_by);
             store_column<T, DP>((T *)k.dv.data + b * k.dv.batch + tt * k.dv.token +
-                                    kvh * k.dv.head, half, k.D, dv[n], 1.0f);
+                                    kvh * k.dv.head, half, k.D, dv[n], plain);
         }
     }
 }
@@ -551,7 +671,8 @@ hipError_t launch_back_q(const AttendK &k, const AttendPlan &p, hipStream_t stre
         constexpr int NC = decltype(nc)::value;
         if (grid == 0) return;
         if (k.bias.axes)
-            attend_dq_kernel<T, DP, NC, true><<<grid, 256, 1024 * entries, stream>>>(k);
+            attend_dq_kernel<T, DP, NC, true>
+                <<<grid, 256, 1024 * (entries + 1), stream>>>(k);
         else
             attend_dq_kernel<T, DP, NC, false><<<grid, 256, 0, stream>>>(k);
     };

@@ -6,26 +6,6 @@
 namespace mixrt {
 namespace {
 
-// Key positions of a tile, [axis][row].
-template <int ROWS>
-struct StagePos {
-    int32_t r[kMaxBiasAxes];
-    __device__ __forceinline__ void fetch(const int32_t *pos, int axes, int first, int limit)
-    {
-        const int row = first + (int)threadIdx.x;
-#pragma unroll
-        for (int a = 0; a < kMaxBiasAxes; ++a)
-            r[a] = threadIdx.x < ROWS && a < axes && row < limit ? pos[(int64_t)row * axes + a] : 0;
-    }
-    __device__ __forceinline__ void put(int32_t *at, int axes) const
-    {
-        if (threadIdx.x < ROWS)
-#pragma unroll
-            for (int a = 0; a < kMaxBiasAxes; ++a)
-                if (a < axes) at[a * ROWS + threadIdx.x] = r[a];
-    }
-};
-
 // W waves a block, NC blocks of 32 columns a wave, PK heads' biases in LDS.
 // EXACT (for training with the 16-bit types): the weights go into the second product
 // as two terms, their rounded values and what that left.  The backward pass takes
@@ -42,7 +22,7 @@ __global__ __launch_bounds__(64 * W) void attend_kernel(AttendK k)
     constexpr int TILE = ROWS * kStride<T, DP>;
     __shared__ __attribute__((aligned(16))) T tiles[2][2][TILE];
     __shared__ float dense[BIAS ? PK * kMaxBiasAxes * kReachRow : 1];
-    __shared__ __attribute__((aligned(16))) int32_t kpos[BIAS ? 2 : 1][BIAS ? kMaxBiasAxes * ROWS : 4];
+    __shared__ TilePos<BIAS ? ROWS : 1> kpos[2];
 
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
     int id = near_block();
@@ -74,7 +54,7 @@ __global__ __launch_bounds__(64 * W) void attend_kernel(AttendK k)
     int hbase[NC];
     if (BIAS) {
         for (int p = 0; p < k.pack; ++p)
-            load_bias(dense + p * kMaxBiasAxes * kReachRow, k.bias, h0 + p, k.H, THREADS);
+            load_bias(dense + p * kMaxBiasAxes * kReachRow, k.bias, h0 + p, k.H, THREADS, false);
 #pragma unroll
         for (int n = 0; n < NC; ++n) {
             hbase[n] = (head[n] - h0) * kMaxBiasAxes * kReachRow;
@@ -102,7 +82,7 @@ __global__ __launch_bounds__(64 * W) void attend_kernel(AttendK k)
     const T *vp = (const T *)k.v.data + b * k.v.batch + kvh * k.v.head;
     const int32_t *pp = BIAS ? k.bias.kpos + b * k.bias.kbatch : nullptr;
     Stage<T, DP, ROWS, THREADS> sk, sv;
-    StagePos<ROWS> sp;
+    StagePos<BIAS ? ROWS : 1> sp;
     if (first < last) {
         sk.fetch(kp, k.k.token, first, last, k.D);
         sv.fetch(vp, k.v.token, first, last, k.D);
@@ -135,28 +115,11 @@ __global__ __launch_bounds__(64 * W) void attend_kernel(AttendK k)
                 for (int n = 0; n < NC; ++n) s[u][n] = Matrix<T>::mul(a, q[n][c], s[u][n]);
             }
         }
-        if (BIAS) {
+        if constexpr (BIAS) {
 #pragma unroll
             for (int u = 0; u < ROWS / 32; ++u)
-#pragma unroll
-                for (int n = 0; n < NC; ++n)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) s[u][n][i] *= k.scale;
-            for (int a = 0; a < k.bias.axes; ++a) {
-                const int32_t *at = kpos[cur] + a * ROWS;
-                const float *row = dense + a * kReachRow;
-#pragma unroll
-                for (int u = 0; u < ROWS / 32; ++u)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const int p = at[32 * u + tile_row(i, half)];
-#pragma unroll
-                        for (int n = 0; n < NC; ++n) {
-                            const int mine = a == 0 ? qpos[n][0] : a == 1 ? qpos[n][1] : qpos[n][2];
-                            s[u][n][i] += row[hbase[n] + bias_at(p, mine, k.bias.reach)];
-                        }
-                    }
-            }
+                add_bias<NC, ROWS>(s[u], k.scale, kpos[cur], u, half, dense, hbase, qpos,
+                                   k.bias.axes, k.bias.reach);
         }
         if (!more && row0 + ROWS > last) {
 #pragma unroll
@@ -278,25 +241,28 @@ __global__ __launch_bounds__(64 * W) void attend_kernel(AttendK k)
 }
 
 // Joins the splits of a row: o = sum_s 2^(lse_s - top) o_s / sum_s 2^(lse_s - top).
-// LANES lanes hold a row's quads, G groups of them share its splits.
-template <typename T, int LANES, int G>
+// A block takes 256 / (8 G) rows and 32 elements of their heads: 8 lanes hold a row's
+// quads, G groups of them share its splits.  (With the splits of a row one after
+// another, the 113 of one token's 32 heads took 29 us.)
+template <typename T, int G>
 __global__ __launch_bounds__(256) void attend_join_kernel(AttendK k)
 {
-    constexpr int EACH = 256 / (LANES * G);
-    __shared__ float4 part[G > 1 ? 256 : 1];
-    __shared__ float weight[G > 1 ? 256 : 1];
+    constexpr int EACH = 32 / G;
+    __shared__ float part[5][256];
     const int64_t rows = (int64_t)k.B * k.H * k.Tq;
-    const int lane = threadIdx.x % LANES, g = threadIdx.x / LANES % G;
-    const int64_t row = (int64_t)blockIdx.x * EACH + threadIdx.x / (LANES * G);
+    const int lane = threadIdx.x & 7, g = threadIdx.x / 8 % G;
+    const int64_t row = (int64_t)blockIdx.x * EACH + threadIdx.x / (8 * G);
     const bool there = row < rows;
-    const int d = 4 * lane;
+    const int d = 32 * blockIdx.y + 4 * lane;
+    // the group's own maximum first: NaN stays
     float top = -INFINITY;
     if (there)
-        for (int s = 0; s < k.splits; ++s) {
+#pragma unroll 4
+        for (int s = g; s < k.splits; s += G) {
             const float x = k.part_lse[s * rows + row];
             top = x > top || x != x ? x : top;
         }
-    const float base = top == -INFINITY ? 0.0f : top;
+    float base = top == -INFINITY ? 0.0f : top;
     float a[4] = {0, 0, 0, 0}, w = 0.0f;
     if (there)
 #pragma unroll 4
@@ -304,7 +270,6 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendK k)
             const float e = __builtin_amdgcn_exp2f(k.part_lse[s * rows + row] - base);
             w += e;
             const float *o = k.part + (s * rows + row) * k.D;
-            // (a split without keys counts nothing, and its part is 0)
             if (d + 4 <= k.D) {
                 float f[4];
                 load_vec<float, 4>(o + d, f);
@@ -317,18 +282,31 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendK k)
             }
         }
     if (G > 1) {
-        part[threadIdx.x] = make_float4(a[0], a[1], a[2], a[3]);
-        weight[threadIdx.x] = w;
+        // then the groups', in order, at their common maximum
+        const bool none = top == -INFINITY;
+        part[0][threadIdx.x] = top;
+        __syncthreads();
+        const int first = threadIdx.x - 8 * g;
+        for (int j = 0; j < G; ++j) {
+            const float x = part[0][first + 8 * j];
+            top = x > top || x != x ? x : top;
+        }
+        const float less = none ? 0.0f : __builtin_amdgcn_exp2f(base - top);
+        base = top == -INFINITY ? 0.0f : top;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 4; ++i) part[i][threadIdx.x] = a[i] * less;
+        part[4][threadIdx.x] = w * less;
         __syncthreads();
         if (g == 0) {
 #pragma unroll
-            for (int j = 1; j < G; ++j) {
-                const float4 x = part[threadIdx.x + j * LANES];
-                a[0] += x.x;
-                a[1] += x.y;
-                a[2] += x.z;
-                a[3] += x.w;
-                w += weight[threadIdx.x + j * LANES];
+            for (int i = 0; i < 4; ++i) a[i] = 0.0f;
+            w = 0.0f;
+#pragma unroll 8
+            for (int j = 0; j < G; ++j) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) a[i] += part[i][first + 8 * j];
+                w += part[4][first + 8 * j];
             }
         }
     }
@@ -336,7 +314,9 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendK k)
     const float inv = w == 0.0f ? 0.0f : 1.0f / w;
     const int64_t bh = row / k.Tq;
     const int t = (int)(row - bh * k.Tq), b = (int)(bh / k.H), h = (int)(bh - (int64_t)b * k.H);
-    if (k.lse && lane == 0) k.lse[row] = w == 0.0f ? INFINITY : top + __builtin_amdgcn_logf(w);
+    if (k.lse && lane == 0 && blockIdx.y == 0)
+        k.lse[row] = w == 0.0f ? INFINITY : base + __builtin_amdgcn_logf(w);
+    if (d >= k.D) return;
     T *o = (T *)k.o.data + b * k.o.batch + (int64_t)t * k.o.token + h * k.o.head;
 #pragma unroll
     for (int i = 0; i < 4; ++i) a[i] *= inv;
@@ -349,20 +329,15 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendK k)
     }
 }
 
-template <typename T, int LANES>
+template <typename T>
 hipError_t launch_join(const AttendK &k, hipStream_t stream)
 {
     const int64_t rows = (int64_t)k.B * k.H * k.Tq;
-    auto go = [&](auto g) {
-        constexpr int G = decltype(g)::value;
-        constexpr int each = 256 / (LANES * G);
-        attend_join_kernel<T, LANES, G>
-            <<<(unsigned)((rows + each - 1) / each), 256, 0, stream>>>(k);
-    };
+    const unsigned by = (unsigned)(k.D + 31) / 32;
     if (k.splits > 4)
-        go(std::integral_constant<int, 256 / LANES>());
+        attend_join_kernel<T, 32><<<dim3((unsigned)rows, by), 256, 0, stream>>>(k);
     else
-        go(std::integral_constant<int, 1>());
+        attend_join_kernel<T, 1><<<dim3((unsigned)((rows + 31) / 32), by), 256, 0, stream>>>(k);
     return hipGetLastError();
 }
 
@@ -398,9 +373,7 @@ hipError_t launch_forward(const AttendK &k, const AttendPlan &p, hipStream_t str
         go(four(), one());
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || k.splits == 1) return e;
-    if (DP == 32) return launch_join<T, 8>(k, stream);
-    if (DP == 64) return launch_join<T, 16>(k, stream);
-    return launch_join<T, 32>(k, stream);
+    return launch_join<T>(k, stream);
 }
 
 }  // namespace

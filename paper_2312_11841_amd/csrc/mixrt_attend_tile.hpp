@@ -239,25 +239,151 @@ __device__ __forceinline__ float rest_of(float o)
 }
 
 // --- the bias ---------------------------------------------------------------------
+//
+// A lane's column and a tile's row have a distance on each axis.  Tokens of views come
+// row by row, so of 8 rows that follow each other mostly all have the same place on an
+// axis, or places that count up by one; a tile carries for each axis which of its
+// octets are such.  Then one place in the table serves an octet, or four neighbours of
+// one place serve a lane's four rows, and only other octets pay for each row's own.
 
-constexpr int kReachRow = 2 * kMaxReach + 2;    // entries of an axis and head in LDS
+constexpr int kPad = 4;                                     // entries beyond either end
+constexpr int kReachRow = 2 * kMaxReach + 2 + 2 * kPad;     // of an axis and head in LDS
 
-// bias[distance] of head's axes, times log2(e), for distances -reach .. reach.
-__device__ __forceinline__ void load_bias(float *dense, const BiasK &b, int head, int H,
-                                          int threads)
+// Entry of the distance row - column, cut to -reach - beyond .. reach.
+__device__ __forceinline__ int bias_at(int row, int column, int reach, int beyond = 0)
 {
-    const int n = 2 * b.reach + 1;
+    return min(max(__builtin_elementwise_sub_sat(row, column), -reach - beyond), reach) + reach +
+           kPad;
+}
+
+// The bucket of an entry (mirrored: of the distance column - row).
+__device__ __forceinline__ int bucket_of(const BiasK &b, int axis, int entry, bool mirrored)
+{
+    const int d = min(max(entry - kPad, 0), 2 * b.reach);
+    return min((int)b.map[axis * (2 * b.reach + 1) + (mirrored ? 2 * b.reach - d : d)],
+               b.buckets - 1);
+}
+
+// bias[entry] of head's axes, times log2(e).
+__device__ __forceinline__ void load_bias(float *dense, const BiasK &b, int head, int H,
+                                          int threads, bool mirrored)
+{
+    const int n = 2 * b.reach + 1 + 2 * kPad;
     for (int i = threadIdx.x; i < b.axes * n; i += threads) {
-        const int a = i / n, d = i - a * n;
-        const int m = min((int)b.map[i], b.buckets - 1);
-        dense[a * kReachRow + d] = b.table[((int64_t)a * b.buckets + m) * H + head] * kLog2e;
+        const int a = i / n, e = i - a * n;
+        dense[a * kReachRow + e] =
+            b.table[((int64_t)a * b.buckets + bucket_of(b, a, e, mirrored)) * H + head] * kLog2e;
     }
 }
 
-// Entry of the distance from a query to a key.
-__device__ __forceinline__ int bias_at(int kpos, int qpos, int reach)
+// Places of a tile's rows on each axis, and which octets are level (one place) or
+// steps (places that count up by one); level32: blocks of 32 rows with one place.
+template <int ROWS>
+struct TilePos {
+    __attribute__((aligned(16))) int32_t at[kMaxBiasAxes][ROWS];
+    uint32_t kind[kMaxBiasAxes];    // level octets, << 8 steps, << 16 level32
+};
+
+template <int ROWS>
+struct StagePos {
+    int32_t r[kMaxBiasAxes];
+    bool there;
+    __device__ __forceinline__ void fetch(const int32_t *pos, int axes, int first, int limit)
+    {
+        const int row = first + (int)threadIdx.x;
+        there = threadIdx.x < ROWS && row < limit;
+#pragma unroll
+        for (int a = 0; a < kMaxBiasAxes; ++a)
+            r[a] = there && a < axes ? pos[(int64_t)row * axes + a] : 0;
+    }
+    __device__ __forceinline__ void put(TilePos<ROWS> &tile, int axes) const
+    {
+        if (threadIdx.x >= 64) return;      // the first wave holds the rows
+        const int lane = threadIdx.x;
+#pragma unroll
+        for (int a = 0; a < kMaxBiasAxes; ++a) {
+            if (a >= axes) break;
+            // (rows that are not there fit in anywhere)
+            const int one = __shfl(r[a], lane & ~7), all = __shfl(r[a], lane & ~31);
+            const bool level = !there || r[a] == one;
+            const bool steps = !there || (one < 0x7fffffff - 8 && r[a] == one + (lane & 7));
+            const bool alike = !there || r[a] == all;
+            const uint64_t l = __builtin_amdgcn_ballot_w64(level);
+            const uint64_t s = __builtin_amdgcn_ballot_w64(steps);
+            const uint64_t w = __builtin_amdgcn_ballot_w64(alike);
+            uint32_t kind = 0;
+#pragma unroll
+            for (int j = 0; j < ROWS / 8; ++j) {
+                kind |= (uint32_t)((l >> (8 * j) & 255) == 255) << j;
+                kind |= (uint32_t)((s >> (8 * j) & 255) == 255) << (8 + j);
+            }
+#pragma unroll
+            for (int u = 0; u < ROWS / 32; ++u)
+                kind |= (uint32_t)((uint32_t)(w >> (32 * u)) == 0xffffffffu) << (16 + u);
+            if (lane < ROWS) tile.at[a][lane] = r[a];
+            if (lane == 0) tile.kind[a] = kind;
+        }
+    }
+};
+
+// s[n][i] = s[n][i] scale + the bias of row i of the tile's block u and column n.
+template <int NC, int ROWS>
+__device__ __forceinline__ void add_bias(f32x16 (&s)[NC], float scale, const TilePos<ROWS> &tile,
+                                         int u, int half, const float *dense,
+                                         const int (&base)[NC],
+                                         const int (&column)[NC][kMaxBiasAxes], int axes, int reach)
 {
-    return min(max(__builtin_elementwise_sub_sat(kpos, qpos), -reach), reach) + reach;
+    float level[NC];
+    uint32_t kinds[kMaxBiasAxes];
+#pragma unroll
+    for (int n = 0; n < NC; ++n) level[n] = 0.0f;
+#pragma unroll
+    for (int a = 0; a < kMaxBiasAxes; ++a) {
+        if (a >= axes) break;
+        kinds[a] = __builtin_amdgcn_readfirstlane(tile.kind[a]);
+        if (kinds[a] >> (16 + u) & 1) {
+            const int p = tile.at[a][32 * u];
+#pragma unroll
+            for (int n = 0; n < NC; ++n)
+                level[n] += dense[base[n] + a * kReachRow + bias_at(p, column[n][a], reach)];
+        }
+    }
+#pragma unroll
+    for (int n = 0; n < NC; ++n)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[n][i] = fmaf(s[n][i], scale, level[n]);
+#pragma unroll
+    for (int a = 0; a < kMaxBiasAxes; ++a) {
+        if (a >= axes) break;
+        if (kinds[a] >> (16 + u) & 1) continue;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int32_t *p = &tile.at[a][32 * u + 8 * j + 4 * half];
+            const float *row = dense + a * kReachRow;
+            const uint32_t bits = kinds[a] >> (4 * u + j);
+            if (bits >> 8 & 1) {
+#pragma unroll
+                for (int n = 0; n < NC; ++n) {
+                    const float *b = row + base[n] + bias_at(p[0], column[n][a], reach, kPad);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) s[n][4 * j + i] += b[i];
+                }
+            } else if (bits & 1) {
+#pragma unroll
+                for (int n = 0; n < NC; ++n) {
+                    const float b = row[base[n] + bias_at(p[0], column[n][a], reach)];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) s[n][4 * j + i] += b;
+                }
+            } else {
+#pragma unroll
+                for (int n = 0; n < NC; ++n)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        s[n][4 * j + i] += row[base[n] + bias_at(p[i], column[n][a], reach)];
+            }
+        }
+    }
 }
 
 }  // namespace mixrt

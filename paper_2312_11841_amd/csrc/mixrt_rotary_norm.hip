@@ -127,24 +127,53 @@ __device__ __forceinline__ void turn_item(const Item &it, const float2 *turn, fl
     }
 }
 
-__device__ __forceinline__ float group_sum(float x, int lanes)
+// Every lane's value of the lane that a data-parallel move pairs it with.
+template <int CONTROL>
+__device__ __forceinline__ float moved(float x)
 {
-    for (int n = 1; n < lanes; n <<= 1) x += __shfl_xor(x, n);
+    return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(
+        0, (int)__float_as_uint(x), CONTROL, 0xf, 0xf, true));
+}
+
+// The same over groups of 2^n lanes, in every lane of them: neighbours, pairs, then
+// mirrored halves (which hold equal values by then), then swapped rows.
+template <typename Join>
+__device__ __forceinline__ float group_join(float x, int n, Join join)
+{
+    if (n >= 1) x = join(x, moved<0xb1>(x));
+    if (n >= 2) x = join(x, moved<0x4e>(x));
+    if (n >= 3) x = join(x, moved<0x141>(x));
+    if (n >= 4) x = join(x, moved<0x140>(x));
+    if (n >= 5) {
+        const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x),
+                                                        false, false);
+        x = join(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    }
+    if (n >= 6) {
+        const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x),
+                                                        false, false);
+        x = join(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    }
     return x;
+}
+
+__device__ __forceinline__ float group_sum(float x, int n)
+{
+    return group_join(x, n, [](float a, float b) { return a + b; });
 }
 
 // 1 / sqrt(mean of squares + eps) of a head in the registers of its group, with
 // squares that leave the range of 32 bits kept inside it: then the elements are
 // first multiplied by a power of two, pre (1 else), which the caller's x holds too.
 template <int M, int V>
-__device__ __forceinline__ float rms(float (&x)[M][2 * V], int lanes, int D, float eps, float &pre)
+__device__ __forceinline__ float rms(float (&x)[M][2 * V], int lanes_log2, int D, float eps, float &pre)
 {
     float ss = 0.0f;
 #pragma unroll
     for (int m = 0; m < M; ++m)
 #pragma unroll
         for (int i = 0; i < 2 * V; ++i) ss = fmaf(x[m][i], x[m][i], ss);
-    ss = group_sum(ss, lanes);
+    ss = group_sum(ss, lanes_log2);
     pre = 1.0f;
     // (eps carries a head of small elements unless it is itself that small)
     const bool far = !(ss < 0x1p120f) || (ss < 0x1p-80f && eps < 0x1p-80f);
@@ -154,7 +183,7 @@ __device__ __forceinline__ float rms(float (&x)[M][2 * V], int lanes, int D, flo
         for (int m = 0; m < M; ++m)
 #pragma unroll
             for (int i = 0; i < 2 * V; ++i) most = fmaxf(most, fabsf(x[m][i]));
-        for (int n = 1; n < lanes; n <<= 1) most = fmaxf(most, __shfl_xor(most, n));
+        most = group_join(most, lanes_log2, [](float a, float b) { return fmaxf(a, b); });
         if (far) {
             const int e = (int)(__float_as_uint(most) >> 23);
             pre = __uint_as_float((uint32_t)min(max(254 - e, 1), 253) << 23);   // about 1 / most
@@ -167,7 +196,7 @@ __device__ __forceinline__ float rms(float (&x)[M][2 * V], int lanes, int D, flo
                 x[m][i] *= pre;
                 if (far) ss = fmaf(x[m][i], x[m][i], ss);
             }
-        const float all = group_sum(ss, lanes);
+        const float all = group_sum(ss, lanes_log2);
         if (far) ss = all;
     }
     return rsqrtf(ss * (1.0f / (float)D) + eps * pre * pre);
@@ -208,6 +237,7 @@ __device__ __forceinline__ void load_weights(const float *w, const Item (&it)[M]
 template <typename T, int V, int M, bool HALVES>
 __global__ __launch_bounds__(kThreads) void rotary_norm_kernel(NormedK k)
 {
+    constexpr int U = M == 1 ? 2 : 1;       // heads of a group whose loads run together
     __shared__ float2 turn[kTurns];
     const int lanes = 1 << k.lanes_log2;
     const int lane = threadIdx.x & (lanes - 1), group = threadIdx.x >> k.lanes_log2;
@@ -228,28 +258,36 @@ __global__ __launch_bounds__(kThreads) void rotary_norm_kernel(NormedK k)
             load_weights<V, M>(h.w, it, HALVES, w);
             const uint32_t rows = (uint32_t)heads * tokens;
             // (every lane of a wave goes through the exchanges)
-            for (uint32_t r0 = 0; r0 < rows; r0 += groups) {
-                const uint32_t r = r0 + group;
-                const bool there = r < rows;
-                const uint32_t t = r / heads, hd = r - t * heads;
-                float x[M][2 * V];
+            for (uint32_t r0 = 0; r0 < rows; r0 += U * groups) {
+                float x[U][M][2 * V];
+                uint32_t t[U], hd[U];
 #pragma unroll
-                for (int m = 0; m < M; ++m) {
-                    Item none = it[m];
-                    if (!there) none.kind = 3;
-                    load_item<T, V, HALVES>((const T *)h.x + (t0 + t) * h.xt + (h0 + hd) * h.xh,
-                                            none, x[m]);
+                for (int u = 0; u < U; ++u) {
+                    const uint32_t r = r0 + u * groups + group;
+                    t[u] = r / heads;
+                    hd[u] = r - t[u] * heads;
+#pragma unroll
+                    for (int m = 0; m < M; ++m) {
+                        Item some = it[m];
+                        if (r >= rows) some.kind = 3;
+                        load_item<T, V, HALVES>(
+                            (const T *)h.x + (t0 + t[u]) * h.xt + (h0 + hd[u]) * h.xh, some,
+                            x[u][m]);
+                    }
                 }
-                float pre;
-                const float rs = rms<M, V>(x, lanes, h.D, k.eps, pre);
-                if (!there) continue;
-                T *o = (T *)h.out + (t0 + t) * h.ot + (h0 + hd) * h.oh;
 #pragma unroll
-                for (int m = 0; m < M; ++m) {
+                for (int u = 0; u < U; ++u) {
+                    float pre;
+                    const float rs = rms<M, V>(x[u], k.lanes_log2, h.D, k.eps, pre);
+                    if (r0 + u * groups + group >= rows) continue;
+                    T *o = (T *)h.out + (t0 + t[u]) * h.ot + (h0 + hd[u]) * h.oh;
 #pragma unroll
-                    for (int i = 0; i < 2 * V; ++i) x[m][i] = x[m][i] * rs * w[m][i];
-                    turn_item<V>(it[m], turn + t * k.pairs, 1.0f, x[m]);
-                    store_item<T, V, HALVES>(o, it[m], x[m]);
+                    for (int m = 0; m < M; ++m) {
+#pragma unroll
+                        for (int i = 0; i < 2 * V; ++i) x[u][m][i] = x[u][m][i] * rs * w[m][i];
+                        turn_item<V>(it[m], turn + t[u] * k.pairs, 1.0f, x[u][m]);
+                        store_item<T, V, HALVES>(o, it[m], x[u][m]);
+                    }
                 }
             }
         }
@@ -304,7 +342,7 @@ __global__ __launch_bounds__(kThreads) void rotary_norm_back_kernel(NormedK k)
                                             none, u[m]);
                 }
                 float pre;
-                const float rs = rms<M, V>(x, lanes, h.D, k.eps, pre);
+                const float rs = rms<M, V>(x, k.lanes_log2, h.D, k.eps, pre);
                 float along = 0.0f;
 #pragma unroll
                 for (int m = 0; m < M; ++m) {
@@ -317,7 +355,7 @@ __global__ __launch_bounds__(kThreads) void rotary_norm_back_kernel(NormedK k)
                         along = fmaf(u[m][i], x[m][i], along);
                     }
                 }
-                along = group_sum(along, lanes) * (1.0f / (float)h.D);
+                along = group_sum(along, k.lanes_log2) * (1.0f / (float)h.D);
                 if (!there || !h.out) continue;
                 T *o = (T *)h.out + (t0 + t) * h.ot + (h0 + hd) * h.oh;
 #pragma unroll
@@ -356,23 +394,25 @@ __global__ __launch_bounds__(kThreads) void rotary_norm_back_kernel(NormedK k)
     }
 }
 
-// dw[array][d] = sum over the blocks' parts, in 64 bits: 16 elements a block, 16
-// threads an element.
+// dw[array][d] = sum over the blocks' parts, in 64 bits: 4 elements a block, 64 threads
+// an element (16 elements a block took 13 to 20 us for 1024 parts of 64 elements).
 __global__ __launch_bounds__(kThreads) void rotary_norm_join_kernel(NormedK k, int blocks)
 {
-    __shared__ double sums[16][16];
+    __shared__ double sums[kThreads];
     const NormedHeadsK &h = k.a[blockIdx.y];
-    const int d = blockIdx.x * 16 + (threadIdx.x & 15), g = threadIdx.x >> 4;
+    const int d = blockIdx.x * 4 + (threadIdx.x & 3), g = threadIdx.x >> 2;
     if (!h.dw) return;
     double a = 0.0;
     if (d < h.D)
-        for (int b = g; b < blocks; b += 16)
+#pragma unroll 8
+        for (int b = g; b < blocks; b += 64)
             a += k.part[((int64_t)b * 2 + blockIdx.y) * k.dmax + d];
-    sums[g][threadIdx.x & 15] = a;
-    __syncthreads();
-    if (g || d >= h.D) return;
-    for (int i = 1; i < 16; ++i) a += sums[i][threadIdx.x & 15];
-    h.dw[d] = (float)a;
+    sums[threadIdx.x] = a;
+    for (int n = 32; n > 0; n >>= 1) {
+        __syncthreads();
+        if (g < n) sums[threadIdx.x] += sums[threadIdx.x + 4 * n];
+    }
+    if (g == 0 && d < h.D) h.dw[d] = (float)sums[threadIdx.x];
 }
 
 // How a call is dealt: vector width, items a lane, lanes a head, tokens a block.
@@ -531,7 +571,7 @@ hipError_t launch_rotary_norm_back(const RotaryNormLaunch &L, hipStream_t stream
     bool any = false;
     for (int i = 0; i < L.n; ++i) any = any || L.a[i].dw;
     if (e != hipSuccess || !any) return e;
-    rotary_norm_join_kernel<<<dim3((k.dmax + 15) / 16, L.n), kThreads, 0, stream>>>(
+    rotary_norm_join_kernel<<<dim3((k.dmax + 3) / 4, L.n), kThreads, 0, stream>>>(
         k, (int)(p.bx * p.by));
     return hipGetLastError();
 }
