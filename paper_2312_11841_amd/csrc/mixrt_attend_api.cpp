@@ -50,8 +50,7 @@ AttendPlan plan_attend(int B, int H, int Hk, int64_t Tq, int64_t Tk, int D, int 
     const int64_t cols = Tq * p.pack, heads = (int64_t)B * (H / p.pack);
     p.narrow = cols <= 32;
     p.cols = p.narrow ? 32 : 128;
-    if (attend_elem(dtype) == 2 && D <= 64 && !p.narrow && heads * ceil_div(cols, 256) >= kCUs)
-        p.cols = 256;
+    if (attend_elem(dtype) == 2 && D <= 64 && axes == 0 && !p.narrow && cols > 1024) p.cols = 256;
     p.blocks = (int)ceil_div(cols, p.cols);
     if (p.blocks < 1) p.blocks = 1;
     split(Tk, heads * p.blocks, p.narrow ? 4 * kCUs : 2 * kCUs, p.narrow ? 128 : 512,

@@ -55,19 +55,6 @@ __device__ __forceinline__ void clear(f32x16 (&a)[NC][ND])
             for (int i = 0; i < 16; ++i) a[n][d][i] = 0.0f;
 }
 
-template <typename T, int DP>
-__device__ __forceinline__ f32x16 row_mul(const T *tile, int lane,
-                                          const typename Matrix<T>::frag (&b)[kPairs<T, DP>])
-{
-    f32x16 s;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) s[i] = 0.0f;
-#pragma unroll
-    for (int c = 0; c < kPairs<T, DP>; ++c)
-        s = Matrix<T>::mul(row_frag<T, DP>(tile, lane, c), b[c], s);
-    return s;
-}
-
 // float16 holds dS only inside a range: its gradients are small where a row looks at
 // many keys, and large where a loss is scaled.  So each column's dS is multiplied by a
 // power of two that keeps the largest seen so far between 1 and 2^15, and its sums

@@ -6,209 +6,83 @@
 namespace mixrt {
 namespace {
 
-// W waves a block, NC blocks of 32 columns a wave, PK heads' biases in LDS.
-// EXACT (for training with the 16-bit types): the weights go into the second product
-// as two terms, their rounded values and what that left.  The backward pass takes
-// delta = sum_j P_ij dP_ij from the output, and dS = P (dP - delta) cancels where a
-// row looks at few keys: an output from rounded weights would leave there the
-// rounding itself, not a small part of it.
-template <typename T, int DP, int W, int NC, bool BIAS, bool EXACT>
-__global__ __launch_bounds__(64 * W) void attend_kernel(AttendK k)
-{
-    typedef typename Matrix<T>::frag frag;
-    constexpr int ROWS = sizeof(T) == 2 && W > 1 ? 64 : 32;
-    constexpr int THREADS = 64 * W;
-    constexpr int PK = BIAS ? (W == 1 ? 8 : 1) : 1;
-    constexpr int TILE = ROWS * kStride<T, DP>;
-    __shared__ __attribute__((aligned(16))) T tiles[2][2][TILE];
-    __shared__ float dense[BIAS ? PK * kMaxBiasAxes * kReachRow : 1];
-    __shared__ TilePos<BIAS ? ROWS : 1> kpos[2];
+// Where a block's work lies: its columns' first head, batch entry, keys.
+struct ForwardWork {
+    int rb, split, h0, b, kvh, len, first, last;
+    __device__ __forceinline__ explicit ForwardWork(const AttendK &k)
+    {
+        int id = near_block();
+        rb = id % k.blocks;
+        id /= k.blocks;
+        split = id % k.splits;
+        id /= k.splits;
+        const int packs = k.H / k.pack;
+        h0 = id % packs * k.pack;
+        b = id / packs;
+        kvh = h0 / (k.H / k.Hk);
+        len = valid_keys(k.lens, b, k.Tk);
+        first = split * k.per;
+        last = min(len, first + k.per);
+    }
+};
 
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
-    int id = near_block();
-    const int rb = id % k.blocks;
-    id /= k.blocks;
-    const int split = id % k.splits;
-    id /= k.splits;
-    const int packs = k.H / k.pack;
-    const int h0 = id % packs * k.pack, b = id / packs;
-    const int kvh = h0 / (k.H / k.Hk);
-    const int len = valid_keys(k.lens, b, k.Tk);
-    const int first = split * k.per, last = min(len, first + k.per);
-
-    // the lane's columns
+// A lane's columns, a token and a head each.
+template <int NC>
+struct Columns {
     int t[NC], head[NC];
     bool there[NC];
-    frag q[NC][kPairs<T, DP>];
-#pragma unroll
-    for (int n = 0; n < NC; ++n) {
-        const int col = ((rb * W + wave) * NC + n) * 32 + (lane & 31);
-        t[n] = col / k.pack;
-        head[n] = h0 + col % k.pack;
-        there[n] = t[n] < k.Tq;
-        load_column<T, DP>(q[n], (const T *)k.q.data + b * k.q.batch + (int64_t)t[n] * k.q.token +
-                                     head[n] * k.q.head,
-                           there[n], half, k.D);
-    }
-    int qpos[NC][kMaxBiasAxes];
-    int hbase[NC];
-    if (BIAS) {
-        for (int p = 0; p < k.pack; ++p)
-            load_bias(dense + p * kMaxBiasAxes * kReachRow, k.bias, h0 + p, k.H, THREADS, false);
+    __device__ __forceinline__ Columns(const AttendK &k, const ForwardWork &w, int first, int lane)
+    {
 #pragma unroll
         for (int n = 0; n < NC; ++n) {
-            hbase[n] = (head[n] - h0) * kMaxBiasAxes * kReachRow;
+            const int col = first + 32 * n + (lane & 31);
+            t[n] = col / k.pack;
+            head[n] = w.h0 + col % k.pack;
+            there[n] = t[n] < k.Tq;
+        }
+    }
+    template <typename T, int DP>
+    __device__ __forceinline__ void load(const AttendK &k, int b, int half,
+                                         typename Matrix<T>::frag (&q)[NC][(kPairs<T, DP>)]) const
+    {
+#pragma unroll
+        for (int n = 0; n < NC; ++n)
+            load_column<T, DP>(q[n], (const T *)k.q.data + b * k.q.batch +
+                                         (int64_t)t[n] * k.q.token + head[n] * k.q.head,
+                               there[n], half, k.D);
+    }
+    __device__ __forceinline__ void places(const AttendK &k, int b,
+                                           int (&pos)[NC][kMaxBiasAxes]) const
+    {
+#pragma unroll
+        for (int n = 0; n < NC; ++n)
 #pragma unroll
             for (int a = 0; a < kMaxBiasAxes; ++a)
-                qpos[n][a] = there[n] && a < k.bias.axes
-                                 ? k.bias.qpos[b * k.bias.qbatch + (int64_t)t[n] * k.bias.axes + a]
-                                 : 0;
-        }
+                pos[n][a] = there[n] && a < k.bias.axes
+                                ? k.bias.qpos[b * k.bias.qbatch + (int64_t)t[n] * k.bias.axes + a]
+                                : 0;
     }
+};
 
-    f32x16 acc[NC][DP / 32];
-    float top[NC], sum[NC];     // in units of log2; sum: of the lane's own rows
-#pragma unroll
-    for (int n = 0; n < NC; ++n) {
-        top[n] = -INFINITY;
-        sum[n] = 0.0f;
-#pragma unroll
-        for (int d = 0; d < DP / 32; ++d)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) acc[n][d][i] = 0.0f;
-    }
-
-    const T *kp = (const T *)k.k.data + b * k.k.batch + kvh * k.k.head;
-    const T *vp = (const T *)k.v.data + b * k.v.batch + kvh * k.v.head;
-    const int32_t *pp = BIAS ? k.bias.kpos + b * k.bias.kbatch : nullptr;
-    Stage<T, DP, ROWS, THREADS> sk, sv;
-    StagePos<BIAS ? ROWS : 1> sp;
-    if (first < last) {
-        sk.fetch(kp, k.k.token, first, last, k.D);
-        sv.fetch(vp, k.v.token, first, last, k.D);
-        if (BIAS) sp.fetch(pp, k.bias.axes, first, last);
-        sk.put(tiles[0][0]);
-        sv.put(tiles[0][1]);
-        if (BIAS) sp.put(kpos[0], k.bias.axes);
-    }
-    __syncthreads();
-    int cur = 0;
-    for (int row0 = first; row0 < last; row0 += ROWS, cur ^= 1) {
-        const bool more = row0 + ROWS < last;
-        if (more) {
-            sk.fetch(kp, k.k.token, row0 + ROWS, last, k.D);
-            sv.fetch(vp, k.v.token, row0 + ROWS, last, k.D);
-            if (BIAS) sp.fetch(pp, k.bias.axes, row0 + ROWS, last);
-        }
-        const T *kt = tiles[cur][0], *vt = tiles[cur][1];
-        f32x16 s[ROWS / 32][NC];
-#pragma unroll
-        for (int u = 0; u < ROWS / 32; ++u) {
-#pragma unroll
-            for (int n = 0; n < NC; ++n)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) s[u][n][i] = 0.0f;
-#pragma unroll
-            for (int c = 0; c < kPairs<T, DP>; ++c) {
-                const frag a = row_frag<T, DP>(kt + u * 32 * kStride<T, DP>, lane, c);
-#pragma unroll
-                for (int n = 0; n < NC; ++n) s[u][n] = Matrix<T>::mul(a, q[n][c], s[u][n]);
-            }
-        }
-        if constexpr (BIAS) {
-#pragma unroll
-            for (int u = 0; u < ROWS / 32; ++u)
-                add_bias<NC, ROWS>(s[u], k.scale, kpos[cur], u, half, dense, hbase, qpos,
-                                   k.bias.axes, k.bias.reach);
-        }
-        if (!more && row0 + ROWS > last) {
-#pragma unroll
-            for (int u = 0; u < ROWS / 32; ++u)
-#pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (row0 + 32 * u + tile_row(i, half) >= last)
-#pragma unroll
-                        for (int n = 0; n < NC; ++n) s[u][n][i] = -INFINITY;
-        }
-        const float unit = BIAS ? 1.0f : k.scale;
-#pragma unroll
-        for (int n = 0; n < NC; ++n) {
-            float m = s[0][n][0];
-#pragma unroll
-            for (int u = 0; u < ROWS / 32; ++u)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) m = fmaxf(m, s[u][n][i]);
-            m = fmaxf(half_max(m) * unit, top[n]);
-            // (a row of -inf alone keeps weights 0)
-            const float base = m == -INFINITY ? 0.0f : m;
-            if (__builtin_amdgcn_ballot_w64(m != top[n]) != 0) {
-                const float less = __builtin_amdgcn_exp2f(top[n] - base);
-                sum[n] *= less;
-#pragma unroll
-                for (int d = 0; d < DP / 32; ++d)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) acc[n][d][i] *= less;
-                top[n] = m;
-            }
-            float add = 0.0f;
-#pragma unroll
-            for (int u = 0; u < ROWS / 32; ++u)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const float p = __builtin_amdgcn_exp2f(fmaf(s[u][n][i], unit, -base));
-                    s[u][n][i] = p;
-                    add += p;
-                }
-            sum[n] += add;
-        }
-#pragma unroll
-        for (int u = 0; u < ROWS / 32; ++u) {
-            const T *v = vt + u * 32 * kStride<T, DP>;
-            if constexpr (sizeof(T) == 4) {
-#pragma unroll
-                for (int d = 0; d < DP / 32; ++d)
-#pragma unroll
-                    for (int n = 0; n < NC; ++n) col_mul<DP>(v, lane, d, s[u][n], acc[n][d]);
-            } else {
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    frag p[NC], less[NC];
-#pragma unroll
-                    for (int n = 0; n < NC; ++n) {
-                        p[n] = round_rows<T>(s[u][n], e);
-                        if (EXACT) less[n] = left_rows<T>(s[u][n], p[n], e);
-                    }
-#pragma unroll
-                    for (int d = 0; d < DP / 32; ++d) {
-                        const frag a = col_frag<T, DP>(v, lane, d, e);
-#pragma unroll
-                        for (int n = 0; n < NC; ++n) {
-                            acc[n][d] = Matrix<T>::mul(a, p[n], acc[n][d]);
-                            if (EXACT) acc[n][d] = Matrix<T>::mul(a, less[n], acc[n][d]);
-                        }
-                    }
-                }
-            }
-        }
-        if (more) {
-            sk.put(tiles[cur ^ 1][0]);
-            sv.put(tiles[cur ^ 1][1]);
-            if (BIAS) sp.put(kpos[cur ^ 1], k.bias.axes);
-        }
-        __syncthreads();
-    }
-
+// The columns' results: sums of weighted values, of weights (the lane's own rows), and
+// the base of the weights, in units of log2.
+template <typename T, int DP, int NC>
+__device__ __forceinline__ void finish(const AttendK &k, const ForwardWork &w,
+                                       const Columns<NC> &c, int half,
+                                       const f32x16 (&acc)[NC][DP / 32], const float (&sum)[NC],
+                                       const float (&top)[NC])
+{
 #pragma unroll
     for (int n = 0; n < NC; ++n) {
         const float l = half_sum(sum[n]);
         const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-        if (!there[n]) continue;
-        const int64_t row = ((int64_t)b * k.H + head[n]) * k.Tq + t[n];
+        if (!c.there[n]) continue;
+        const int64_t row = ((int64_t)w.b * k.H + c.head[n]) * k.Tq + c.t[n];
         const float lse = top[n] + __builtin_amdgcn_logf(l);    // (log2)
         if (k.splits > 1) {
             const int64_t rows = (int64_t)k.B * k.H * k.Tq;
-            if (half == 0) k.part_lse[split * rows + row] = l == 0.0f ? -INFINITY : lse;
-            float *o = k.part + (split * rows + row) * k.D;
+            if (half == 0) k.part_lse[w.split * rows + row] = l == 0.0f ? -INFINITY : lse;
+            float *o = k.part + (w.split * rows + row) * k.D;
 #pragma unroll
             for (int d = 0; d < DP / 32; ++d)
 #pragma unroll
@@ -219,8 +93,9 @@ __global__ __launch_bounds__(64 * W) void attend_kernel(AttendK k)
             continue;
         }
         if (k.lse && half == 0) k.lse[row] = l == 0.0f ? INFINITY : lse;
-        T *o = (T *)k.o.data + b * k.o.batch + (int64_t)t[n] * k.o.token + head[n] * k.o.head;
-        T *rest = k.rest ? (T *)k.rest + (((int64_t)b * k.Tq + t[n]) * k.H + head[n]) * k.D
+        T *o = (T *)k.o.data + w.b * k.o.batch + (int64_t)c.t[n] * k.o.token +
+               c.head[n] * k.o.head;
+        T *rest = k.rest ? (T *)k.rest + (((int64_t)w.b * k.Tq + c.t[n]) * k.H + c.head[n]) * k.D
                          : nullptr;
 #pragma unroll
         for (int d = 0; d < DP / 32; ++d)
@@ -238,6 +113,309 @@ __global__ __launch_bounds__(64 * W) void attend_kernel(AttendK k)
                 }
             }
     }
+}
+
+// A new maximum of a column's scores (in units of log2) becomes the base of its weights
+// only where weights on the old one would pass 2^8: then the sums so far are brought to
+// it.  That is the first tile and few others.
+constexpr float kSlack = 8.0f;
+template <int ND>
+__device__ __forceinline__ void rebase(float m, float &top, float &sum, f32x16 (&acc)[ND])
+{
+    const bool out = m > top + kSlack;
+    if (__builtin_amdgcn_ballot_w64(out) == 0) return;
+    if (out) {
+        const float less = __builtin_amdgcn_exp2f(top - m);
+        sum *= less;
+#pragma unroll
+        for (int d = 0; d < ND; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[d][i] *= less;
+        top = m;
+    }
+}
+
+// The weights of a block of 32 rows, in place of the scores: 2^(s unit - base).
+__device__ __forceinline__ void weigh(f32x16 &s, float unit, float top, float &sum)
+{
+    // (a column whose scores are all -inf so far keeps weights 0)
+    const float base = top == -INFINITY ? 0.0f : top;
+    float add = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], unit, -base));
+        add += s[i];
+    }
+    sum += add;
+}
+
+__device__ __forceinline__ float most_of(const f32x16 &s)
+{
+    float m = s[0];
+#pragma unroll
+    for (int i = 1; i < 16; ++i) m = fmaxf(m, s[i]);
+    return half_max(m);
+}
+
+// Rows behind the last one have no weight.
+__device__ __forceinline__ void cut_rows(f32x16 &s, int row0, int half, int last)
+{
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+        if (row0 + tile_row(i, half) >= last) s[i] = -INFINITY;
+}
+
+// W waves a block, 32 columns a wave: float32, and few columns (W = 1, PK heads'
+// biases in LDS).  EXACT: see attend_flow_kernel.
+template <typename T, int DP, int W, bool BIAS, bool EXACT>
+__global__ __launch_bounds__(64 * W) void attend_kernel(AttendK k)
+{
+    typedef typename Matrix<T>::frag frag;
+    constexpr int ROWS = 32, THREADS = 64 * W, NC = 1;
+    constexpr int PK = BIAS ? (W == 1 ? 8 : 1) : 1;
+    constexpr int TILE = ROWS * kStride<T, DP>;
+    __shared__ __attribute__((aligned(16))) T tiles[2][2][TILE];
+    __shared__ float dense[BIAS ? PK * kMaxBiasAxes * kReachRow : 1];
+    __shared__ TilePos<BIAS ? ROWS : 1> kpos[2];
+
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
+    const ForwardWork w(k);
+    const T *kp = (const T *)k.k.data + w.b * k.k.batch + w.kvh * k.k.head;
+    const T *vp = (const T *)k.v.data + w.b * k.v.batch + w.kvh * k.v.head;
+    const int32_t *pp = BIAS ? k.bias.kpos + w.b * k.bias.kbatch : nullptr;
+    Stage<T, DP, ROWS, THREADS> sk, sv;
+    StagePos<BIAS ? ROWS : 1> sp;
+    if (w.first < w.last) {
+        sk.fetch(kp, k.k.token, w.first, w.last, k.D);
+        sv.fetch(vp, k.v.token, w.first, w.last, k.D);
+        if (BIAS) sp.fetch(pp, k.bias.axes, w.first, w.last);
+    }
+    const Columns<NC> c(k, w, (w.rb * W + wave) * 32, lane);
+    frag q[NC][kPairs<T, DP>];
+    c.template load<T, DP>(k, w.b, half, q);
+    int qpos[NC][kMaxBiasAxes], hbase[NC];
+    if (BIAS) {
+        for (int p = 0; p < k.pack; ++p)
+            load_bias(dense + p * kMaxBiasAxes * kReachRow, k.bias, w.h0 + p, k.H, THREADS, false);
+        hbase[0] = (c.head[0] - w.h0) * kMaxBiasAxes * kReachRow;
+        c.places(k, w.b, qpos);
+    }
+    f32x16 acc[NC][DP / 32];
+    float top[NC] = {-INFINITY}, sum[NC] = {0.0f};
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[0][d][i] = 0.0f;
+    if (w.first < w.last) {
+        sk.put(tiles[0][0]);
+        sv.put(tiles[0][1]);
+        if (BIAS) sp.put(kpos[0], k.bias.axes);
+    }
+    __syncthreads();
+    int cur = 0;
+    for (int row0 = w.first; row0 < w.last; row0 += ROWS, cur ^= 1) {
+        const bool more = row0 + ROWS < w.last;
+        if (more) {
+            sk.fetch(kp, k.k.token, row0 + ROWS, w.last, k.D);
+            sv.fetch(vp, k.v.token, row0 + ROWS, w.last, k.D);
+            if (BIAS) sp.fetch(pp, k.bias.axes, row0 + ROWS, w.last);
+        }
+        const T *kt = tiles[cur][0], *vt = tiles[cur][1];
+        f32x16 s[NC] = {row_mul<T, DP>(kt, lane, q[0])};
+        if constexpr (BIAS)
+            add_bias<NC, ROWS>(s, k.scale, kpos[cur], 0, half, dense, hbase, qpos, k.bias.axes,
+                               k.bias.reach);
+        if (row0 + ROWS > w.last) cut_rows(s[0], row0, half, w.last);
+        const float unit = BIAS ? 1.0f : k.scale;
+        rebase(most_of(s[0]) * unit, top[0], sum[0], acc[0]);
+        weigh(s[0], unit, top[0], sum[0]);
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (int d = 0; d < DP / 32; ++d) col_mul<DP>(vt, lane, d, s[0], acc[0][d]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const frag p = round_rows<T>(s[0], e);
+                frag less;
+                if (EXACT) less = left_rows<T>(s[0], p, e);
+#pragma unroll
+                for (int d = 0; d < DP / 32; ++d) {
+                    const frag a = col_frag<T, DP>(vt, lane, d, e);
+                    acc[0][d] = Matrix<T>::mul(a, p, acc[0][d]);
+                    if (EXACT) acc[0][d] = Matrix<T>::mul(a, less, acc[0][d]);
+                }
+            }
+        }
+        if (more) {
+            sk.put(tiles[cur ^ 1][0]);
+            sv.put(tiles[cur ^ 1][1]);
+            if (BIAS) sp.put(kpos[cur ^ 1], k.bias.axes);
+        }
+        __syncthreads();
+    }
+    finish<T, DP, NC>(k, w, c, half, acc, sum, top);
+}
+
+// Four waves a block, NC blocks of 32 columns a wave, for the 16-bit types.  There an
+// exponential costs as much of a SIMD's time as the products of a score with heads of
+// 64, so neither may wait for the other: a step forms the weights of 32 rows while the
+// matrix unit works on the scores of the next 32 and on the values of the last 32.
+// Keys lie in LDS one tile ahead, values stay one tile longer (rings of three).
+//
+// EXACT (for training): the weights go into the second product as two terms, their
+// rounded values and what that left.  The backward pass takes delta = sum_j P_ij dP_ij
+// from the output, and dS = P (dP - delta) cancels where a row looks at few keys: an
+// output from rounded weights would leave there the rounding itself, not a small part
+// of it.
+template <int DP> inline constexpr int kFlowWaves = DP <= 64 ? 2 : 1;   // a SIMD
+template <typename T, int DP, int NC, bool BIAS, bool EXACT>
+__global__ __launch_bounds__(256, kFlowWaves<DP>) void attend_flow_kernel(AttendK k)
+{
+    typedef typename Matrix<T>::frag frag;
+    constexpr int ROWS = DP <= 64 ? 64 : 32, SUBS = ROWS / 32, THREADS = 256;
+    constexpr int TILE = ROWS * kStride<T, DP>;
+    __shared__ __attribute__((aligned(16))) T ktiles[3][TILE];
+    __shared__ __attribute__((aligned(16))) T vtiles[3][TILE];
+    __shared__ __attribute__((aligned(16))) T nothing[32 * kStride<T, DP>];     // zeros
+    __shared__ float dense[BIAS ? kMaxBiasAxes * kReachRow : 1];
+    __shared__ TilePos<BIAS ? ROWS : 1> kpos[3];
+
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
+    const ForwardWork w(k);
+    const T *kp = (const T *)k.k.data + w.b * k.k.batch + w.kvh * k.k.head;
+    const T *vp = (const T *)k.v.data + w.b * k.v.batch + w.kvh * k.v.head;
+    const int32_t *pp = BIAS ? k.bias.kpos + w.b * k.bias.kbatch : nullptr;
+    Stage<T, DP, ROWS, THREADS> sk, sv;
+    StagePos<BIAS ? ROWS : 1> sp;
+    auto put_keys = [&](int row, int slot) {
+        sk.fetch(kp, k.k.token, row, w.last, k.D);
+        sk.put(ktiles[slot]);
+        if (BIAS) {
+            sp.fetch(pp, k.bias.axes, row, w.last);
+            sp.put(kpos[slot], k.bias.axes);
+        }
+    };
+    const Columns<NC> c(k, w, (w.rb * 4 + wave) * NC * 32, lane);
+    frag q[NC][kPairs<T, DP>];
+    int qpos[NC][kMaxBiasAxes], hbase[NC];
+    if (w.first < w.last) {
+        put_keys(w.first, 0);
+        put_keys(w.first + ROWS, 1);
+        sv.fetch(vp, k.v.token, w.first, w.last, k.D);
+        sv.put(vtiles[0]);
+    }
+    c.template load<T, DP>(k, w.b, half, q);
+    if (BIAS) {
+        load_bias(dense, k.bias, w.h0, k.H, THREADS, false);
+        c.places(k, w.b, qpos);
+#pragma unroll
+        for (int n = 0; n < NC; ++n) hbase[n] = 0;
+    }
+    f32x16 acc[NC][DP / 32], s[NC];
+    float top[NC], sum[NC];
+    frag p[NC][2], less[EXACT ? NC : 1][2];     // weights of the last 32 rows
+#pragma unroll
+    for (int n = 0; n < NC; ++n) {
+        top[n] = -INFINITY;
+        sum[n] = 0.0f;
+#pragma unroll
+        for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[n][d][i] = 0.0f;
+    }
+    for (int i = threadIdx.x; i < 32 * kStride<T, DP>; i += THREADS) nothing[i] = (T)0.0f;
+    __syncthreads();
+    if (w.first < w.last)
+#pragma unroll
+        for (int n = 0; n < NC; ++n) s[n] = row_mul<T, DP>(ktiles[0], lane, q[n]);
+
+    // acc += values of 32 rows, at weights p
+    auto add_values = [&](const T *v) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+#pragma unroll
+            for (int d = 0; d < DP / 32; ++d) {
+                const frag a = col_frag<T, DP>(v, lane, d, e);
+#pragma unroll
+                for (int n = 0; n < NC; ++n) {
+                    acc[n][d] = Matrix<T>::mul(a, p[n][e], acc[n][d]);
+                    if (EXACT) acc[n][d] = Matrix<T>::mul(a, less[n][e], acc[n][d]);
+                }
+            }
+    };
+    const float unit = BIAS ? 1.0f : k.scale;
+    // the values that p waits for: none yet
+    const T *held = nothing;
+#pragma unroll
+    for (int n = 0; n < NC; ++n)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            p[n][e] = frag{};
+            if (EXACT) less[n][e] = frag{};
+        }
+    int k0 = 0, k1 = 1, k2 = 2, v0 = 0, v1 = 1, v2 = 2;     // slots of this tile, the next ..
+    for (int row0 = w.first; row0 < w.last; row0 += ROWS) {
+        sk.fetch(kp, k.k.token, row0 + 2 * ROWS, w.last, k.D);
+        sv.fetch(vp, k.v.token, row0 + ROWS, w.last, k.D);
+        if (BIAS) sp.fetch(pp, k.bias.axes, row0 + 2 * ROWS, w.last);
+#pragma unroll
+        for (int u = 0; u < SUBS; ++u) {
+            if constexpr (BIAS)
+                add_bias<NC, ROWS>(s, k.scale, kpos[k0], u, half, dense, hbase, qpos, k.bias.axes,
+                                   k.bias.reach);
+            if (row0 + 32 * u + 32 > w.last)
+#pragma unroll
+                for (int n = 0; n < NC; ++n) cut_rows(s[n], row0 + 32 * u, half, w.last);
+            float m[NC];
+            bool out = false;
+#pragma unroll
+            for (int n = 0; n < NC; ++n) {
+                m[n] = most_of(s[n]) * unit;
+                out = out || m[n] > top[n] + kSlack;
+            }
+            if (__builtin_amdgcn_ballot_w64(out) != 0) {
+                // the values that wait have weights on the old base
+                add_values(held);
+                held = nothing;
+#pragma unroll
+                for (int n = 0; n < NC; ++n) rebase(m[n], top[n], sum[n], acc[n]);
+            }
+            const T *next = u + 1 < SUBS ? ktiles[k0] + 32 * (u + 1) * kStride<T, DP> : ktiles[k1];
+            f32x16 s2[NC];
+#pragma unroll
+            for (int n = 0; n < NC; ++n) s2[n] = row_mul<T, DP>(next, lane, q[n]);
+            add_values(held);
+#pragma unroll
+            for (int n = 0; n < NC; ++n) {
+                weigh(s[n], unit, top[n], sum[n]);
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    p[n][e] = round_rows<T>(s[n], e);
+                    if (EXACT) less[n][e] = left_rows<T>(s[n], p[n][e], e);
+                    // (formed here, not where they are used)
+                    asm volatile("" ::"v"(p[n][e]));
+                    if (EXACT) asm volatile("" ::"v"(less[n][e]));
+                }
+            }
+#pragma unroll
+            for (int n = 0; n < NC; ++n) s[n] = s2[n];
+            held = vtiles[v0] + 32 * u * kStride<T, DP>;
+        }
+        sk.put(ktiles[k2]);
+        sv.put(vtiles[v1]);
+        if (BIAS) sp.put(kpos[k2], k.bias.axes);
+        __syncthreads();
+        int x = k0;
+        k0 = k1;
+        k1 = k2;
+        k2 = x;
+        x = v0;
+        v0 = v1;
+        v1 = v2;
+        v2 = x;
+    }
+    add_values(held);
+    finish<T, DP, NC>(k, w, c, half, acc, sum, top);
 }
 
 // Joins the splits of a row: o = sum_s 2^(lse_s - top) o_s / sum_s 2^(lse_s - top).
@@ -342,35 +520,40 @@ hipError_t launch_join(const AttendK &k, hipStream_t stream)
 }
 
 template <typename T, int DP>
-hipError_t launch_forward(const AttendK &k, const AttendPlan &p, hipStream_t stream)
+hipError_t launch_forward(AttendK k, const AttendPlan &p, hipStream_t stream)
 {
+    const bool exact = sizeof(T) == 2 && k.rest;
+    // (64 columns a wave leave no registers for more than the plain products)
+    const bool twice = p.cols == 256 && !exact;
+    if (p.cols == 256 && !twice) k.blocks = (k.Tq + 127) / 128;
     const unsigned grid = (unsigned)((int64_t)k.B * (k.H / k.pack) * k.splits * k.blocks);
-    auto go = [&](auto w, auto nc) {
-        constexpr int W = decltype(w)::value, NC = decltype(nc)::value;
+    typedef std::true_type yes;
+    typedef std::false_type no;
+    auto variant = [&](auto go) {
         if constexpr (sizeof(T) == 2)
-            if (k.rest) {
-                if (k.bias.axes)
-                    attend_kernel<T, DP, W, NC, true, true><<<grid, 64 * W, 0, stream>>>(k);
-                else
-                    attend_kernel<T, DP, W, NC, false, true><<<grid, 64 * W, 0, stream>>>(k);
-                return;
-            }
-        if (k.bias.axes)
-            attend_kernel<T, DP, W, NC, true, false><<<grid, 64 * W, 0, stream>>>(k);
-        else
-            attend_kernel<T, DP, W, NC, false, false><<<grid, 64 * W, 0, stream>>>(k);
+            if (exact) return k.bias.axes ? go(yes(), yes()) : go(no(), yes());
+        return k.bias.axes ? go(yes(), no()) : go(no(), no());
     };
-    typedef std::integral_constant<int, 1> one;
-    typedef std::integral_constant<int, 4> four;
-    if (p.narrow)
-        go(one(), one());
-    else if constexpr (sizeof(T) == 2 && DP <= 64) {
-        if (p.cols == 256)
-            go(four(), std::integral_constant<int, 2>());
-        else
-            go(four(), one());
-    } else
-        go(four(), one());
+    auto simple = [&](auto w) {
+        constexpr int W = decltype(w)::value;
+        variant([&](auto bias, auto ex) {
+            attend_kernel<T, DP, W, decltype(bias)::value, decltype(ex)::value>
+                <<<grid, 64 * W, 0, stream>>>(k);
+        });
+    };
+    if (p.narrow) {
+        simple(std::integral_constant<int, 1>());
+    } else if constexpr (sizeof(T) == 4) {
+        simple(std::integral_constant<int, 4>());
+    } else if (twice) {
+        if constexpr (DP <= 64)
+            attend_flow_kernel<T, DP, 2, false, false><<<grid, 256, 0, stream>>>(k);
+    } else {
+        variant([&](auto bias, auto ex) {
+            attend_flow_kernel<T, DP, 1, decltype(bias)::value, decltype(ex)::value>
+                <<<grid, 256, 0, stream>>>(k);
+        });
+    }
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || k.splits == 1) return e;
     return launch_join<T>(k, stream);

@@ -84,6 +84,20 @@ __device__ __forceinline__ typename Matrix<T>::frag row_frag(const T *tile, int 
                                                (2 * c + (lane >> 5)) * kChunk<T>);
 }
 
+// S of 32 rows: operand A from LDS, B a lane's column.
+template <typename T, int DP>
+__device__ __forceinline__ f32x16 row_mul(const T *tile, int lane,
+                                          const typename Matrix<T>::frag (&b)[kPairs<T, DP>])
+{
+    f32x16 s;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[i] = 0.0f;
+#pragma unroll
+    for (int c = 0; c < kPairs<T, DP>; ++c)
+        s = Matrix<T>::mul(row_frag<T, DP>(tile, lane, c), b[c], s);
+    return s;
+}
+
 // acc[d][column] += sum over 32 rows of tile[row][32 block + d] p[row][column].
 template <int DP>
 __device__ __forceinline__ void col_mul(const float *tile, int lane, int block, const f32x16 &p,
@@ -163,6 +177,17 @@ struct Stage {
     __device__ __forceinline__ void fetch(const T *base, int64_t stride, int first, int limit,
                                           int D)
     {
+        if (kEven && D == DP && first + ROWS <= limit) {    // nothing to leave out
+#pragma unroll
+            for (int j = 0; j < kEach; ++j) {
+                const int at = threadIdx.x + j * THREADS;
+                r[j] = __builtin_bit_cast(
+                    u32x4, *(const Pack<T, kChunk<T>> *)(base + (int64_t)(first + at / kChunks) *
+                                                                    stride +
+                                                         at % kChunks * kChunk<T>));
+            }
+            return;
+        }
 #pragma unroll
         for (int j = 0; j < kEach; ++j) {
             const int at = threadIdx.x + j * THREADS;

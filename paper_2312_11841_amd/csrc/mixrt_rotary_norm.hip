@@ -18,6 +18,7 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kTurns = 2048;     // most (token, pair) turns of a block
 constexpr int64_t kMostBlocks = 1 << 20;
+constexpr int kParts = 1024;     // blocks of the backward pass, while lanes' sums stay short
 
 struct NormedK {
     int64_t tokens;
@@ -233,11 +234,13 @@ __device__ __forceinline__ void load_weights(const float *w, const Item (&it)[M]
     }
 }
 
-// What bounds it: the stream of the heads (see the figures at launch_rotary_norm).
+// Heads of a group whose loads run together: as many as hold 16 elements a lane.
+template <int V, int M> inline constexpr int kTogether = M > 1 || V == 8 ? 1 : V == 4 ? 2 : 4;
+
 template <typename T, int V, int M, bool HALVES>
 __global__ __launch_bounds__(kThreads) void rotary_norm_kernel(NormedK k)
 {
-    constexpr int U = M == 1 ? 2 : 1;       // heads of a group whose loads run together
+    constexpr int U = kTogether<V, M>;
     __shared__ float2 turn[kTurns];
     const int lanes = 1 << k.lanes_log2;
     const int lane = threadIdx.x & (lanes - 1), group = threadIdx.x >> k.lanes_log2;
@@ -245,26 +248,22 @@ __global__ __launch_bounds__(kThreads) void rotary_norm_kernel(NormedK k)
     for (int64_t t0 = (int64_t)blockIdx.x * k.run; t0 < k.tokens;
          t0 += (int64_t)gridDim.x * k.run) {
         const int tokens = (int)min((int64_t)k.run, k.tokens - t0);
-        fill_turns(k, t0, tokens, turn);
-        __syncthreads();
         for (int n = 0; n < k.n; ++n) {
             const NormedHeadsK &h = k.a[n];
-            const int h0 = blockIdx.y * k.per[n], heads = min(k.per[n], h.heads - h0);
-            if (heads <= 0) continue;
+            const int h0 = blockIdx.y * k.per[n], heads = max(min(k.per[n], h.heads - h0), 0);
             Item it[M];
             float w[M][2 * V];
 #pragma unroll
             for (int m = 0; m < M; ++m) it[m] = item_of<V, HALVES>(lane + m * lanes, k.pairs, h.D);
             load_weights<V, M>(h.w, it, HALVES, w);
             const uint32_t rows = (uint32_t)heads * tokens;
-            // (every lane of a wave goes through the exchanges)
-            for (uint32_t r0 = 0; r0 < rows; r0 += U * groups) {
-                float x[U][M][2 * V];
-                uint32_t t[U], hd[U];
+            float x[U][M][2 * V];
+            uint32_t t[U], hd[U];
+            auto load = [&](uint32_t r0) {
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
                     const uint32_t r = r0 + u * groups + group;
-                    t[u] = r / heads;
+                    t[u] = heads ? r / heads : 0;
                     hd[u] = r - t[u] * heads;
 #pragma unroll
                     for (int m = 0; m < M; ++m) {
@@ -275,6 +274,15 @@ __global__ __launch_bounds__(kThreads) void rotary_norm_kernel(NormedK k)
                             x[u][m]);
                     }
                 }
+            };
+            load(0);
+            if (n == 0) {       // (while the first heads are on their way)
+                fill_turns(k, t0, tokens, turn);
+                __syncthreads();
+            }
+            // (every lane of a wave goes through the exchanges)
+            for (uint32_t r0 = 0; r0 < rows; r0 += U * groups) {
+                if (r0) load(r0);
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
                     float pre;
@@ -302,12 +310,14 @@ __global__ __launch_bounds__(kThreads) void rotary_norm_kernel(NormedK k)
 template <typename T, int V, int M, bool HALVES>
 __global__ __launch_bounds__(kThreads) void rotary_norm_back_kernel(NormedK k)
 {
+    constexpr int U = kTogether<V, M>;
     __shared__ float2 turn[kTurns];
     __shared__ float sums[kThreads * 2 * V];
     const int lanes = 1 << k.lanes_log2;
     const int lane = threadIdx.x & (lanes - 1), group = threadIdx.x >> k.lanes_log2;
     const int groups = kThreads >> k.lanes_log2;
     float *part = k.part + ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * 2 * k.dmax;
+    int64_t filled = -1;        // the tokens whose sines are in LDS
     for (int n = 0; n < k.n; ++n) {
         const NormedHeadsK &h = k.a[n];
         const int h0 = blockIdx.y * k.per[n], heads = min(k.per[n], h.heads - h0);
@@ -323,47 +333,58 @@ __global__ __launch_bounds__(kThreads) void rotary_norm_back_kernel(NormedK k)
         for (int64_t t0 = (int64_t)blockIdx.x * k.run; t0 < k.tokens && heads > 0;
              t0 += (int64_t)gridDim.x * k.run) {
             const int tokens = (int)min((int64_t)k.run, k.tokens - t0);
-            __syncthreads();
-            fill_turns(k, t0, tokens, turn);
-            __syncthreads();
+            if (t0 != filled) {
+                __syncthreads();
+                fill_turns(k, t0, tokens, turn);
+                __syncthreads();
+                filled = t0;
+            }
             const uint32_t rows = (uint32_t)heads * tokens;
-            for (uint32_t r0 = 0; r0 < rows; r0 += groups) {
-                const uint32_t r = r0 + group;
-                const bool there = r < rows;
-                const uint32_t t = r / heads, hd = r - t * heads;
-                float x[M][2 * V], u[M][2 * V];
+            for (uint32_t r0 = 0; r0 < rows; r0 += U * groups) {
+                float x[U][M][2 * V], dy[U][M][2 * V];
+                uint32_t t[U], hd[U];
 #pragma unroll
-                for (int m = 0; m < M; ++m) {
-                    Item none = it[m];
-                    if (!there) none.kind = 3;
-                    load_item<T, V, HALVES>((const T *)h.x + (t0 + t) * h.xt + (h0 + hd) * h.xh,
-                                            none, x[m]);
-                    load_item<T, V, HALVES>((const T *)h.dy + (t0 + t) * h.dt + (h0 + hd) * h.dh,
-                                            none, u[m]);
-                }
-                float pre;
-                const float rs = rms<M, V>(x, k.lanes_log2, h.D, k.eps, pre);
-                float along = 0.0f;
+                for (int u = 0; u < U; ++u) {
+                    const uint32_t r = r0 + u * groups + group;
+                    t[u] = r / heads;
+                    hd[u] = r - t[u] * heads;
+                    const T *xp = (const T *)h.x + (t0 + t[u]) * h.xt + (h0 + hd[u]) * h.xh;
+                    const T *dp = (const T *)h.dy + (t0 + t[u]) * h.dt + (h0 + hd[u]) * h.dh;
 #pragma unroll
-                for (int m = 0; m < M; ++m) {
-                    if (there) turn_item<V>(it[m], turn + t * k.pairs, -1.0f, u[m]);
-#pragma unroll
-                    for (int i = 0; i < 2 * V; ++i) {
-                        x[m][i] *= rs;
-                        if (there) dw[m][i] = fmaf(u[m][i], x[m][i], dw[m][i]);
-                        u[m][i] *= w[m][i];
-                        along = fmaf(u[m][i], x[m][i], along);
+                    for (int m = 0; m < M; ++m) {
+                        Item some = it[m];
+                        if (r >= rows) some.kind = 3;
+                        load_item<T, V, HALVES>(xp, some, x[u][m]);
+                        load_item<T, V, HALVES>(dp, some, dy[u][m]);
                     }
                 }
-                along = group_sum(along, k.lanes_log2) * (1.0f / (float)h.D);
-                if (!there || !h.out) continue;
-                T *o = (T *)h.out + (t0 + t) * h.ot + (h0 + hd) * h.oh;
 #pragma unroll
-                for (int m = 0; m < M; ++m) {
+                for (int u = 0; u < U; ++u) {
+                    const bool there = r0 + u * groups + group < rows;
+                    float pre;
+                    const float rs = rms<M, V>(x[u], k.lanes_log2, h.D, k.eps, pre);
+                    float along = 0.0f;
 #pragma unroll
-                    for (int i = 0; i < 2 * V; ++i)
-                        x[m][i] = rs * fmaf(-x[m][i], along, u[m][i]) * pre;
-                    store_item<T, V, HALVES>(o, it[m], x[m]);
+                    for (int m = 0; m < M; ++m) {
+                        if (there) turn_item<V>(it[m], turn + t[u] * k.pairs, -1.0f, dy[u][m]);
+#pragma unroll
+                        for (int i = 0; i < 2 * V; ++i) {
+                            x[u][m][i] *= rs;
+                            if (there) dw[m][i] = fmaf(dy[u][m][i], x[u][m][i], dw[m][i]);
+                            dy[u][m][i] *= w[m][i];
+                            along = fmaf(dy[u][m][i], x[u][m][i], along);
+                        }
+                    }
+                    along = group_sum(along, k.lanes_log2) * (1.0f / (float)h.D);
+                    if (!there || !h.out) continue;
+                    T *o = (T *)h.out + (t0 + t[u]) * h.ot + (h0 + hd[u]) * h.oh;
+#pragma unroll
+                    for (int m = 0; m < M; ++m) {
+#pragma unroll
+                        for (int i = 0; i < 2 * V; ++i)
+                            x[u][m][i] = rs * fmaf(-x[u][m][i], along, dy[u][m][i]) * pre;
+                        store_item<T, V, HALVES>(o, it[m], x[u][m]);
+                    }
                 }
             }
         }
@@ -456,16 +477,26 @@ NormedPlan plan_normed(const RotaryNormLaunch &L, bool back)
     p.M = most <= 64 ? 1 : most <= 256 ? 4 : 8;   // (512 items at most)
     while ((1 << p.lanes_log2) * p.M < most) ++p.lanes_log2;
     const int64_t turns = L.pairs > 0 ? kTurns / L.pairs : 64;
-    int64_t run = elements > 0 ? 24 * kThreads / elements : 1;
+    // tokens of a block: forward about 24 elements a thread; backward all tokens in
+    // kParts blocks if their sines fit, since each block's sums are a part to join.
+    // Then more, so that the heads divide among the block's groups (65,280 tokens, 16
+    // heads of 64 and as many keys, forward: 3 tokens leave a quarter of each pass idle,
+    // 122 us, 4 take 106, 8 the same, 12 109)
+    int64_t run = back ? (L.tokens + kParts - 1) / kParts
+                       : elements > 0 ? 24 * kThreads / elements : 1;
+    const int groups = kThreads >> p.lanes_log2;
+    int64_t step = groups;
+    while (heads > 0 && step > 1 && heads * (step / 2) % groups == 0) step /= 2;
+    if (step <= 2 * run) run = (run + step - 1) / step * step;
     if (run > turns) run = turns;
     if (run < 1) run = 1;
     p.run = (int)run;
     int64_t bx = (L.tokens + run - 1) / run;
     if (back) {
-        // sums of about 1024 rows a lane at most, few parts to join
-        const int64_t rows = L.tokens * heads, groups = kThreads >> p.lanes_log2;
+        // (sums of about 1024 rows a lane at most)
+        const int64_t rows = L.tokens * heads;
         int64_t parts = rows / (groups * 1024);
-        if (parts < 1024) parts = 1024;
+        if (parts < kParts) parts = kParts;
         if (bx > parts) bx = parts;
     }
     if (bx > kMostBlocks) bx = kMostBlocks;
