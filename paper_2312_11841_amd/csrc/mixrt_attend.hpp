@@ -47,21 +47,27 @@ struct AttendK {
     float *part, *part_lse, *delta, *part_table;
 };
 
-// How a call is split.  Forward: a block takes cols columns (a column is a
-// token and one of pack heads that share their keys) and per keys; queries'
-// gradient: likewise, pack 1; keys' gradient: a block takes cols keys and per
-// (head of the group, token) rows.
+// How a call is dealt.  Forward: a block takes cols columns (a column is a token and
+// one of pack heads that share their keys) and per keys; queries' gradient: likewise,
+// pack 1; keys' gradient: a block takes cols keys and per tiles of 32 rows (the heads of
+// a group one after another).
 struct AttendPlan {
-    int narrow;               // forward: one wave a block (few columns)
+    int shared;               // a block's waves share 32 columns and divide the rows
     int pack;
     int cols, blocks;         // columns of a block, blocks of one head
     int splits, per;
 };
 
-AttendPlan plan_attend(int B, int H, int Hk, int64_t Tq, int64_t Tk, int D, int dtype, int axes);
-AttendPlan plan_attend_dq(int B, int H, int Hk, int64_t Tq, int64_t Tk, int D, int dtype, int axes);
+// LDS of the queries' gradient for the bias table's: a place an entry, and one more,
+// of each lane.
+inline int attend_hist_bytes(int entries) { return 1024 * (entries + 1); }
+
+AttendPlan plan_attend(int B, int H, int Hk, int64_t Tq, int64_t Tk, int D, int dtype, int axes,
+                       int entries);
+AttendPlan plan_attend_dq(int B, int H, int Hk, int64_t Tq, int64_t Tk, int D, int dtype, int axes,
+                       int entries);
 AttendPlan plan_attend_dkv(int B, int H, int Hk, int64_t Tq, int64_t Tk, int D, int dtype,
-                           int axes);
+                           int axes, int entries);
 
 // Launches of one element type.
 hipError_t launch_attend_f32(const AttendK &k, int stage, hipStream_t stream);

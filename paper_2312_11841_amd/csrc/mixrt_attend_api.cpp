@@ -17,13 +17,13 @@ constexpr int kCUs = 256;
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-// Keys (or rows) that one chain of 32-bit sums takes at most, a multiple of 64: the
-// matrix instructions of float32 add two terms, those of the 16-bit types 16, and a
-// chain is about 1024 or 2048 of them, so that its roundings stay below the result's.
+// Rows that one chain of 32-bit sums takes at most, a multiple of 64: the matrix
+// instructions of float32 add two terms, those of the 16-bit types 16, and a chain is
+// about 1024 or 2048 of them, so that its roundings stay below the result's.
 int64_t longest(int dtype) { return attend_elem(dtype) == 4 ? 2048 : 32768; }
 
 // Splits of a walk over n rows so that about want blocks run, none shorter than
-// least, and none longer than the type's chains; per is a multiple of step.
+// least, and none longer than most; per is a multiple of step.
 void split(int64_t n, int64_t blocks, int64_t want, int64_t least, int64_t most, int64_t step,
            int *splits, int *per)
 {
@@ -37,9 +37,20 @@ void split(int64_t n, int64_t blocks, int64_t want, int64_t least, int64_t most,
     *splits = (int)(n > 0 ? ceil_div(n, p) : 1);
 }
 
+// Whether blocks of 128 columns are few for the chip, also when their walks of rows are
+// split: then blocks of 32 columns run, whose waves divide the rows.
+bool few(int64_t blocks, int64_t rows) { return blocks * (1 + rows / 1024) < kCUs; }
+
+int blocks_of(int64_t n, int cols)
+{
+    const int64_t b = ceil_div(n, cols);
+    return b < 1 ? 1 : (int)b;
+}
+
 }  // namespace
 
-AttendPlan plan_attend(int B, int H, int Hk, int64_t Tq, int64_t Tk, int D, int dtype, int axes)
+AttendPlan plan_attend(int B, int H, int Hk, int64_t Tq, int64_t Tk, int D, int dtype, int axes,
+                       int entries)
 {
     AttendPlan p{};
     p.pack = 1;
@@ -48,41 +59,44 @@ AttendPlan plan_attend(int B, int H, int Hk, int64_t Tq, int64_t Tk, int D, int 
         for (int n = 2; n <= 8; ++n)
             if (H / Hk % n == 0 && Tq * n <= 32) p.pack = n;
     const int64_t cols = Tq * p.pack, heads = (int64_t)B * (H / p.pack);
-    p.narrow = cols <= 32;
-    p.cols = p.narrow ? 32 : 128;
-    if (attend_elem(dtype) == 2 && D <= 64 && axes == 0 && !p.narrow && cols > 1024) p.cols = 256;
-    p.blocks = (int)ceil_div(cols, p.cols);
-    if (p.blocks < 1) p.blocks = 1;
-    split(Tk, heads * p.blocks, p.narrow ? 4 * kCUs : 2 * kCUs, p.narrow ? 128 : 512,
-          longest(dtype), 64, &p.splits, &p.per);
+    p.shared = cols <= 32 || few(heads * ceil_div(cols, 128), Tk);
+    p.cols = p.shared ? 32 : 128;
+    if (attend_elem(dtype) == 2 && D <= 64 && axes == 0 && !p.shared && cols > 1024) p.cols = 256;
+    p.blocks = blocks_of(cols, p.cols);
+    split(Tk, heads * p.blocks, 2 * kCUs, 512, longest(dtype), 128, &p.splits, &p.per);
     return p;
 }
 
-AttendPlan plan_attend_dq(int B, int H, int Hk, int64_t Tq, int64_t Tk, int D, int dtype, int axes)
+AttendPlan plan_attend_dq(int B, int H, int Hk, int64_t Tq, int64_t Tk, int D, int dtype, int axes,
+                          int entries)
 {
     AttendPlan p{};
     p.pack = 1;
-    p.cols = 128;
     const int64_t heads = (int64_t)B * H;
-    if (attend_elem(dtype) == 2 && D <= 64 && heads * ceil_div(Tq, 256) >= kCUs) p.cols = 256;
-    p.blocks = (int)ceil_div(Tq, p.cols);
-    if (p.blocks < 1) p.blocks = 1;
-    split(Tk, heads * p.blocks, 2 * kCUs, 512, longest(dtype), 32, &p.splits, &p.per);
+    p.shared = few(heads * ceil_div(Tq, 128), Tk);
+    // (a wave's own tiles beside the table's sums may be more than a CU's LDS; about
+    // 16 KB are other things)
+    const int tiles = 4 * 2 * 32 * (attend_dim(D) * attend_elem(dtype) + 16);
+    if (axes && tiles + attend_hist_bytes(entries) + 16384 > 163840) p.shared = 0;
+    p.cols = p.shared ? 32 : 128;
+    p.blocks = blocks_of(Tq, p.cols);
+    int64_t most = longest(dtype);
+    if (axes && p.shared && most > 4096) most = 4096;   // (1024 keys of a lane's table sums)
+    split(Tk, heads * p.blocks, 2 * kCUs, 512, most, 128, &p.splits, &p.per);
     return p;
 }
 
 AttendPlan plan_attend_dkv(int B, int H, int Hk, int64_t Tq, int64_t Tk, int D, int dtype,
-                           int axes)
+                           int axes, int entries)
 {
     AttendPlan p{};
     p.pack = 1;
-    p.cols = 128;
-    p.blocks = (int)ceil_div(Tk, p.cols);
-    if (p.blocks < 1) p.blocks = 1;
-    // in tiles of 32 rows, the group's heads one after another
+    const int64_t heads = (int64_t)B * Hk;
+    p.shared = few(heads * ceil_div(Tk, 128), H / Hk * Tq);
+    p.cols = p.shared ? 32 : 128;
+    p.blocks = blocks_of(Tk, p.cols);
     const int64_t tiles = H / Hk * ceil_div(Tq, 32);
-    split(tiles, (int64_t)B * Hk * p.blocks, 2 * kCUs, 16, longest(dtype) / 32, 1, &p.splits,
-          &p.per);
+    split(tiles, heads * p.blocks, 2 * kCUs, 16, longest(dtype) / 32, 4, &p.splits, &p.per);
     return p;
 }
 
@@ -120,7 +134,37 @@ int check_workspace(mixrt_ctx *ctx, const void *ws, size_t have, size_t need)
 
 // --- attention --------------------------------------------------------------------
 
-int check_attention(mixrt_ctx *ctx, const mixrt_attention *a)
+int check_bias(mixrt_ctx *ctx, const mixrt_relative_bias *b)
+{
+    if (!b) return MIXRT_OK;
+    if (b->axes < 1 || b->axes > MIXRT_MAX_BIAS_AXES)
+        return fail(ctx, MIXRT_EUNSUPPORTED, "bias.axes=%d outside 1..%d", b->axes,
+                    MIXRT_MAX_BIAS_AXES);
+    if (b->count < 1 || b->count > MIXRT_MAX_BIAS_BUCKETS)
+        return fail(ctx, MIXRT_EUNSUPPORTED, "bias.count=%d outside 1..%d", b->count,
+                    MIXRT_MAX_BIAS_BUCKETS);
+    if (b->reach < 0 || b->reach > MIXRT_MAX_BIAS_REACH)
+        return fail(ctx, MIXRT_EUNSUPPORTED, "bias.reach=%d outside 0..%d", b->reach,
+                    MIXRT_MAX_BIAS_REACH);
+    return MIXRT_OK;
+}
+
+int check_bias_data(mixrt_ctx *ctx, const mixrt_attention *a, const mixrt_relative_bias *b)
+{
+    if (!b) return MIXRT_OK;
+    if (!b->table || !b->buckets) return fail(ctx, MIXRT_EINVAL, "bias.table or buckets is NULL");
+    if ((a->queries && !b->q_pos) || (a->keys && !b->k_pos))
+        return fail(ctx, MIXRT_EINVAL, "bias.q_pos or k_pos is NULL");
+    if (!aligned(b->table, 4) || !aligned(b->q_pos, 4) || !aligned(b->k_pos, 4))
+        return fail(ctx, MIXRT_EINVAL, "bias.table, q_pos or k_pos not 4-byte aligned");
+    if (b->q_pos_stride < 0 || b->q_pos_stride >= kMaxStride || b->k_pos_stride < 0 ||
+        b->k_pos_stride >= kMaxStride)
+        return fail(ctx, MIXRT_EINVAL, "bias: position strides %lld, %lld",
+                    (long long)b->q_pos_stride, (long long)b->k_pos_stride);
+    return MIXRT_OK;
+}
+
+int check_attention(mixrt_ctx *ctx, const mixrt_attention *a, const mixrt_relative_bias *b)
 {
     if (!a) return fail(ctx, MIXRT_EINVAL, "attention is NULL");
     if (a->batch < 0) return fail(ctx, MIXRT_EINVAL, "attention.batch=%d", a->batch);
@@ -151,36 +195,12 @@ int check_attention(mixrt_ctx *ctx, const mixrt_attention *a)
     // a grid's blocks are counted in 32 bits
     for (auto plan : {mixrt::plan_attend, mixrt::plan_attend_dq, mixrt::plan_attend_dkv}) {
         const AttendPlan p = plan(a->batch, a->heads, a->kv_heads, a->queries, a->keys,
-                                  a->head_dim, a->dtype, 0);
+                                  a->head_dim, a->dtype, b ? b->axes : 0,
+                                  b ? b->axes * b->count : 0);
         if (rows * p.blocks >= ((int64_t)1 << 30) / p.splits)
             return fail(ctx, MIXRT_EUNSUPPORTED, "attention: %lld queries and %lld keys are too "
                         "many blocks", (long long)a->queries, (long long)a->keys);
     }
-    return MIXRT_OK;
-}
-
-int check_bias(mixrt_ctx *ctx, const mixrt_attention *a, const mixrt_relative_bias *b, bool data)
-{
-    if (!b) return MIXRT_OK;
-    if (b->axes < 1 || b->axes > MIXRT_MAX_BIAS_AXES)
-        return fail(ctx, MIXRT_EUNSUPPORTED, "bias.axes=%d outside 1..%d", b->axes,
-                    MIXRT_MAX_BIAS_AXES);
-    if (b->count < 1 || b->count > MIXRT_MAX_BIAS_BUCKETS)
-        return fail(ctx, MIXRT_EUNSUPPORTED, "bias.count=%d outside 1..%d", b->count,
-                    MIXRT_MAX_BIAS_BUCKETS);
-    if (b->reach < 0 || b->reach > MIXRT_MAX_BIAS_REACH)
-        return fail(ctx, MIXRT_EUNSUPPORTED, "bias.reach=%d outside 0..%d", b->reach,
-                    MIXRT_MAX_BIAS_REACH);
-    if (!data) return MIXRT_OK;
-    if (!b->table || !b->buckets) return fail(ctx, MIXRT_EINVAL, "bias.table or buckets is NULL");
-    if ((a->queries && !b->q_pos) || (a->keys && !b->k_pos))
-        return fail(ctx, MIXRT_EINVAL, "bias.q_pos or k_pos is NULL");
-    if (!aligned(b->table, 4) || !aligned(b->q_pos, 4) || !aligned(b->k_pos, 4))
-        return fail(ctx, MIXRT_EINVAL, "bias.table, q_pos or k_pos not 4-byte aligned");
-    if (b->q_pos_stride < 0 || b->q_pos_stride >= kMaxStride || b->k_pos_stride < 0 ||
-        b->k_pos_stride >= kMaxStride)
-        return fail(ctx, MIXRT_EINVAL, "bias: position strides %lld, %lld",
-                    (long long)b->q_pos_stride, (long long)b->k_pos_stride);
     return MIXRT_OK;
 }
 
@@ -239,8 +259,8 @@ Scratch scratch_of(const mixrt_attention *a, const mixrt_relative_bias *b, bool 
         return from;
     };
     auto plan = [&](auto fn) {
-        return fn(a->batch, a->heads, a->kv_heads, a->queries, a->keys, a->head_dim, a->dtype,
-                  axes);
+        return fn(a->batch, a->heads, a->kv_heads, a->queries, a->keys, a->head_dim, a->dtype, axes,
+                  axes ? axes * b->count : 0);
     };
     if (!backward) {
         const AttendPlan p = plan(mixrt::plan_attend);
@@ -446,7 +466,7 @@ int mixrt_attention_workspace(const mixrt_attention *att, const mixrt_relative_b
     if (!bytes) return fail(nullptr, MIXRT_EINVAL, "bytes is NULL");
     *bytes = 0;
     int rc;
-    if ((rc = check_attention(nullptr, att)) || (rc = check_bias(nullptr, att, bias, false)))
+    if ((rc = check_bias(nullptr, bias)) || (rc = check_attention(nullptr, att, bias)))
         return rc;
     *bytes = scratch_of(att, bias, backward != 0).total;
     return MIXRT_OK;
@@ -461,7 +481,8 @@ int mixrt_attention_forward(mixrt_ctx *ctx, const mixrt_attention *att,
     if (!ctx) return fail(nullptr, MIXRT_EINVAL, "ctx is NULL");
     clear_err(ctx);
     int rc;
-    if ((rc = check_attention(ctx, att)) || (rc = check_bias(ctx, att, bias, true)) ||
+    if ((rc = check_bias(ctx, bias)) || (rc = check_attention(ctx, att, bias)) ||
+        (rc = check_bias_data(ctx, att, bias)) ||
         (rc = check_sequence(ctx, att, q, true, "q", false)) ||
         (rc = check_sequence(ctx, att, k, false, "k", false)) ||
         (rc = check_sequence(ctx, att, v, false, "v", false)) ||
@@ -498,7 +519,8 @@ int mixrt_attention_backward(mixrt_ctx *ctx, const mixrt_attention *att,
     if (!ctx) return fail(nullptr, MIXRT_EINVAL, "ctx is NULL");
     clear_err(ctx);
     int rc;
-    if ((rc = check_attention(ctx, att)) || (rc = check_bias(ctx, att, bias, true)) ||
+    if ((rc = check_bias(ctx, bias)) || (rc = check_attention(ctx, att, bias)) ||
+        (rc = check_bias_data(ctx, att, bias)) ||
         (rc = check_sequence(ctx, att, dout, true, "dout", false)) ||
         (rc = check_sequence(ctx, att, q, true, "q", false)) ||
         (rc = check_sequence(ctx, att, k, false, "k", false)) ||

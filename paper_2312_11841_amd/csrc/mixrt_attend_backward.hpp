@@ -191,21 +191,25 @@ __device__ __forceinline__ void store_column(T *row, int half, int D, const f32x
 
 // --- the queries' gradient -----------------------------------------------------------
 
-template <typename T, int DP, int NC, bool BIAS>
+template <typename T, int DP, int NC, bool BIAS, bool SHARED>
 __global__ __launch_bounds__(256) void attend_dq_kernel(AttendK k)
 {
     typedef typename Matrix<T>::frag frag;
-    constexpr int ROWS = 32, THREADS = 256;
+    static_assert(!SHARED || NC == 1, "waves share 32 columns");
+    constexpr int ROWS = 32, THREADS = 256, WAVES = SHARED ? 4 : 1;
     constexpr int TILE = ROWS * kStride<T, DP>;
     // (two of the widest tiles and the table's sums are more than a CU's 160 KB)
-    constexpr int BUFS = BIAS && sizeof(T) == 4 && DP == 128 ? 1 : 2;
-    __shared__ __attribute__((aligned(16))) T tiles[BUFS][2][TILE];
+    constexpr int BUFS = SHARED || (BIAS && sizeof(T) == 4 && DP == 128) ? 1 : 2;
+    __shared__ __attribute__((aligned(16))) T tiles[WAVES][BUFS][2][TILE];
     __shared__ float dense[BIAS ? kMaxBiasAxes * kReachRow : 1];
     __shared__ uint16_t place[BIAS ? kMaxBiasAxes * kReachRow : 1];   // 64 entry
-    __shared__ TilePos<BIAS ? ROWS : 1> kpos[BUFS];
+    __shared__ TilePos<BIAS ? ROWS : 1> kpos[WAVES][BUFS];
     extern __shared__ float hist[];     // [wave][entry, and a spare one][lane]
 
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
+    const Team<SHARED> team;
+    const int lane = team.lane, wave = team.wave, half = team.half;
+    const int me = team.mine(), stager = team.stager();
+    constexpr int STEP = Team<SHARED>::kStep * ROWS;
     const int block = near_block();
     int id = block;
     const int rb = id % k.blocks;
@@ -225,7 +229,7 @@ __global__ __launch_bounds__(256) void attend_dq_kernel(AttendK k)
     int qpos[NC][kMaxBiasAxes];
 #pragma unroll
     for (int n = 0; n < NC; ++n) {
-        t[n] = ((rb * 4 + wave) * NC + n) * 32 + (lane & 31);
+        t[n] = ((SHARED ? rb : rb * 4 + wave) * NC + n) * 32 + (lane & 31);
         there[n] = t[n] < k.Tq;
         const int64_t tt = t[n];
         load_column<T, DP>(q[n], (const T *)k.q.data + b * k.q.batch + tt * k.q.token +
@@ -253,7 +257,7 @@ __global__ __launch_bounds__(256) void attend_dq_kernel(AttendK k)
         delta[n] = half_sum(sum);
         const int64_t row = ((int64_t)b * k.H + h) * k.Tq + tt;
         lse[n] = there[n] ? k.lse[row] : INFINITY;
-        if (there[n] && half == 0 && split == 0) k.delta[row] = delta[n];
+        if (there[n] && half == 0 && split == 0 && me == 0) k.delta[row] = delta[n];
 #pragma unroll
         for (int a = 0; a < kMaxBiasAxes; ++a)
             qpos[n][a] = BIAS && there[n] && a < k.bias.axes
@@ -262,7 +266,7 @@ __global__ __launch_bounds__(256) void attend_dq_kernel(AttendK k)
     }
     const int held = entries + 1;
     if (BIAS) {
-        load_bias(dense, k.bias, h, k.H, THREADS, false);
+        load_bias(dense, k.bias, h, k.H, threadIdx.x, THREADS, false);
         const int n = 2 * k.bias.reach + 1 + 2 * kPad;
         for (int i = threadIdx.x; i < k.bias.axes * n; i += THREADS) {
             const int a = i / n, e = i - a * n;
@@ -281,26 +285,47 @@ __global__ __launch_bounds__(256) void attend_dq_kernel(AttendK k)
     const T *kp = (const T *)k.k.data + b * k.k.batch + kvh * k.k.head;
     const T *vp = (const T *)k.v.data + b * k.v.batch + kvh * k.v.head;
     const int32_t *pp = BIAS ? k.bias.kpos + b * k.bias.kbatch : nullptr;
-    Stage<T, DP, ROWS, THREADS> sk, sv;
+    Stage<T, DP, ROWS, Team<SHARED>::kStagers> sk, sv;
     StagePos<BIAS ? ROWS : 1> sp;
-    if (first < last) {
-        sk.fetch(kp, k.k.token, first, last, k.D);
-        sv.fetch(vp, k.v.token, first, last, k.D);
-        if (BIAS) sp.fetch(pp, k.bias.axes, first, last);
-        sk.put(tiles[0][0]);
-        sv.put(tiles[0][1]);
-        if (BIAS) sp.put(kpos[0], k.bias.axes);
+    auto fetch = [&](int row) {
+        sk.fetch(stager, kp, k.k.token, row, last, k.D);
+        sv.fetch(stager, vp, k.v.token, row, last, k.D);
+        if (BIAS) sp.fetch(stager, pp, k.bias.axes, row, last);
+    };
+    auto put = [&](int to) {
+        sk.put(stager, tiles[me][to][0]);
+        sv.put(stager, tiles[me][to][1]);
+        if (BIAS) sp.put(stager, kpos[me][to], k.bias.axes);
+    };
+    const int row1 = first + me * ROWS;
+    if (row1 < last) {
+        fetch(row1);
+        put(0);
     }
-    __syncthreads();
-    int cur = 0, counted = 0;
-    for (int row0 = first; row0 < last; row0 += ROWS, cur ^= BUFS - 1) {
-        const bool more = row0 + ROWS < last;
-        if (more) {
-            sk.fetch(kp, k.k.token, row0 + ROWS, last, k.D);
-            sv.fetch(vp, k.v.token, row0 + ROWS, last, k.D);
-            if (BIAS) sp.fetch(pp, k.bias.axes, row0 + ROWS, last);
+    if (SHARED && BIAS) __syncthreads();    // (the bias and hist are the block's)
+    team.meet();
+    // each entry's places of all lanes; threads start at different lanes, as the same
+    // lane of all entries lies in one bank
+    auto collect = [&]() {
+        if ((int)threadIdx.x >= entries) return;
+        float sum = 0.0f;
+#pragma unroll 1
+        for (int w = 0; w < 4; ++w) {
+            float *at = hist + (w * held + threadIdx.x) * 64;
+#pragma unroll 4
+            for (int i = 0; i < 64; ++i) {
+                const int l = (i + threadIdx.x) & 63;
+                sum += at[l];
+                at[l] = 0.0f;
+            }
         }
-        const T *kt = tiles[cur][0], *vt = tiles[cur][1];
+        table += sum;
+    };
+    int cur = 0, counted = 0;
+    for (int row0 = row1; row0 < last; row0 += STEP, cur ^= BUFS - 1) {
+        const bool more = row0 + STEP < last;
+        if (more && (!SHARED || kAhead<T, DP>)) fetch(row0 + STEP);
+        const T *kt = tiles[me][cur][0], *vt = tiles[me][cur][1];
         f32x16 s[NC], g[NC];
 #pragma unroll
         for (int n = 0; n < NC; ++n)
@@ -317,7 +342,7 @@ __global__ __launch_bounds__(256) void attend_dq_kernel(AttendK k)
         }
         if constexpr (BIAS) {
             const int base[NC] = {};
-            add_bias<NC, ROWS>(s, k.scale, kpos[cur], 0, half, dense, base, qpos, k.bias.axes,
+            add_bias<NC, ROWS>(s, k.scale, kpos[me][cur], 0, half, dense, base, qpos, k.bias.axes,
                                k.bias.reach);
         }
         const float unit = BIAS ? 1.0f : k.scale;
@@ -327,71 +352,67 @@ __global__ __launch_bounds__(256) void attend_dq_kernel(AttendK k)
             for (int i = 0; i < 16; ++i)
                 g[n][i] = __builtin_amdgcn_exp2f(fmaf(s[n][i], unit, -lse[n])) *
                           (g[n][i] - delta[n]);
-        if (!more && row0 + ROWS > last) {
+        if (row0 + ROWS > last) {
+            rare();
 #pragma unroll
             for (int i = 0; i < 16; ++i)
                 if (row0 + tile_row(i, half) >= last)
 #pragma unroll
                     for (int n = 0; n < NC; ++n) g[n][i] = 0.0f;
         }
-        // (the one key of a row has weight 1 whatever its score)
-        if (len == 1) {
-#pragma unroll
-            for (int n = 0; n < NC; ++n)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) g[n][i] = 0.0f;
-        }
         if constexpr (BIAS) {
 #pragma unroll
             for (int n = 0; n < NC; ++n)
-                add_table<ROWS>(g[n], kpos[cur], half, place, qpos[n], k.bias.axes, k.bias.reach,
+                add_table<ROWS>(g[n], kpos[me][cur], half, place, qpos[n], k.bias.axes, k.bias.reach,
                                 mine, 64 * entries);
             counted += ROWS;
         }
         lift.scale(g, acc);
         add_cols<T, DP, NC>(kt, lane, g, acc);
-        if (BUFS == 1) __syncthreads();
+        if (BUFS == 1) team.meet();
         if (more) {
-            sk.put(tiles[cur ^ (BUFS - 1)][0]);
-            sv.put(tiles[cur ^ (BUFS - 1)][1]);
-            if (BIAS) sp.put(kpos[cur ^ (BUFS - 1)], k.bias.axes);
+            if (SHARED && !kAhead<T, DP>) fetch(row0 + STEP);
+            put(cur ^ (BUFS - 1));
         }
-        __syncthreads();
-        if (BIAS && (counted == kHistRows || !more)) {
-            // each entry's places of all lanes; threads start at different lanes,
-            // as the same lane of all entries lies in one bank
-            if ((int)threadIdx.x < entries) {
-                float sum = 0.0f;
-#pragma unroll 1
-                for (int w = 0; w < 4; ++w) {
-                    float *at = hist + (w * held + threadIdx.x) * 64;
-#pragma unroll 4
-                    for (int i = 0; i < 64; ++i) {
-                        const int l = (i + threadIdx.x) & 63;
-                        sum += at[l];
-                        at[l] = 0.0f;
-                    }
-                }
-                table += sum;
-            }
+        team.meet();
+        if (BIAS && !SHARED && counted == kHistRows) {
+            collect();
             counted = 0;
             __syncthreads();
         }
     }
-    if (BIAS && (int)threadIdx.x < entries)
-        k.part_table[(int64_t)block * entries + threadIdx.x] = (float)table;
+    // the one key of a row has weight 1 whatever its score: no gradient
+    const float some = len == 1 ? 0.0f : 1.0f;
+    if (BIAS) {
+        __syncthreads();
+        collect();
+        if ((int)threadIdx.x < entries)
+            k.part_table[(int64_t)block * entries + threadIdx.x] = some * (float)table;
+    }
+    const int64_t rows = (int64_t)k.B * k.H * k.Tq;
+    if constexpr (SHARED) {
+        float f[DP / 8];
+        join_waves<DP>((float *)&tiles[0][0][0][0], lane, wave, acc[0], lift.back(0), f);
+        if (!there[0]) return;
+        const int d = (2 * wave + half) * (DP / 8);
+        const int64_t row = ((int64_t)b * k.H + h) * k.Tq + t[0];
+        if (k.splits > 1)
+            store_run<float>(k.part + (split * rows + row) * k.D, d, k.D, f, some * k.plain_scale);
+        else
+            store_run<T>((T *)k.dq.data + b * k.dq.batch + (int64_t)t[0] * k.dq.token +
+                             h * k.dq.head, d, k.D, f, some * k.plain_scale);
+        return;
+    }
 #pragma unroll
     for (int n = 0; n < NC; ++n) {
         if (!there[n]) continue;
+        const float by = some * lift.back(n) * k.plain_scale;
         if (k.splits > 1) {
-            const int64_t rows = (int64_t)k.B * k.H * k.Tq;
             const int64_t row = ((int64_t)b * k.H + h) * k.Tq + t[n];
-            store_column<float, DP>(k.part + (split * rows + row) * k.D, half, k.D, acc[n],
-                                    lift.back(n) * k.plain_scale);
+            store_column<float, DP>(k.part + (split * rows + row) * k.D, half, k.D, acc[n], by);
         } else {
             store_column<T, DP>((T *)k.dq.data + b * k.dq.batch + (int64_t)t[n] * k.dq.token +
-                                    h * k.dq.head, half, k.D, acc[n],
-                                lift.back(n) * k.plain_scale);
+                                    h * k.dq.head, half, k.D, acc[n], by);
         }
     }
 }
@@ -402,36 +423,39 @@ __global__ __launch_bounds__(256) void attend_dq_kernel(AttendK k)
 template <int ROWS>
 struct StageSums {
     float lse, delta;
-    __device__ __forceinline__ void fetch(const float *l, const float *d, int first, int limit,
-                                          float lifted)
+    __device__ __forceinline__ void fetch(int thread, const float *l, const float *d, int first,
+                                          int limit, float lifted)
     {
-        const int row = first + (int)threadIdx.x;
-        const bool there = threadIdx.x < ROWS && row < limit;
+        const int row = first + thread;
+        const bool there = thread < ROWS && row < limit;
         // (a row that is not there has weights 0)
         lse = there ? l[row] - lifted : INFINITY;
         delta = there ? d[row] : 0.0f;
     }
-    __device__ __forceinline__ void put(float *at) const
+    __device__ __forceinline__ void put(int thread, float *at) const
     {
-        if (threadIdx.x < ROWS) {
-            at[threadIdx.x] = lse;
-            at[ROWS + threadIdx.x] = delta;
+        if (thread < ROWS) {
+            at[thread] = lse;
+            at[ROWS + thread] = delta;
         }
     }
 };
 
-template <typename T, int DP, int NC, bool BIAS>
+template <typename T, int DP, int NC, bool BIAS, bool SHARED>
 __global__ __launch_bounds__(256) void attend_dkv_kernel(AttendK k)
 {
     typedef typename Matrix<T>::frag frag;
-    constexpr int ROWS = 32, THREADS = 256;
-    constexpr int TILE = ROWS * kStride<T, DP>;
-    __shared__ __attribute__((aligned(16))) T tiles[2][2][TILE];
-    __shared__ float dense[BIAS ? kMaxBiasAxes * kReachRow : 1];
-    __shared__ TilePos<BIAS ? ROWS : 1> qpos[2];
-    __shared__ __attribute__((aligned(16))) float sums[2][2 * ROWS];
+    static_assert(!SHARED || NC == 1, "waves share 32 columns");
+    constexpr int ROWS = 32, WAVES = SHARED ? 4 : 1, BUFS = SHARED ? 1 : 2;
+    constexpr int TILE = ROWS * kStride<T, DP>, STEP = Team<SHARED>::kStep;
+    __shared__ __attribute__((aligned(16))) T tiles[WAVES][BUFS][2][TILE];
+    __shared__ float dense[WAVES][BIAS ? kMaxBiasAxes * kReachRow : 1];
+    __shared__ TilePos<BIAS ? ROWS : 1> qpos[WAVES][BUFS];
+    __shared__ __attribute__((aligned(16))) float sums[WAVES][BUFS][2 * ROWS];
 
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
+    const Team<SHARED> team;
+    const int lane = team.lane, wave = team.wave, half = team.half;
+    const int me = team.mine(), stager = team.stager();
     int id = near_block();
     const int rb = id % k.blocks;
     id /= k.blocks;
@@ -444,7 +468,7 @@ __global__ __launch_bounds__(256) void attend_dkv_kernel(AttendK k)
     const int a_head = max((k.Tq + ROWS - 1) / ROWS, 1);
     const int first = split * k.per;
     int last = min(k.Tq > 0 ? G * a_head : 0, first + k.per);
-    if (rb * 128 * NC >= len) last = first;
+    if (rb * (SHARED ? 32 : 128 * NC) >= len) last = first;
 
     int t[NC];
     bool there[NC], seen[NC];
@@ -452,7 +476,7 @@ __global__ __launch_bounds__(256) void attend_dkv_kernel(AttendK k)
     int kpos[NC][kMaxBiasAxes];
 #pragma unroll
     for (int n = 0; n < NC; ++n) {
-        t[n] = ((rb * 4 + wave) * NC + n) * 32 + (lane & 31);
+        t[n] = ((SHARED ? rb : rb * 4 + wave) * NC + n) * 32 + (lane & 31);
         there[n] = t[n] < k.Tk;
         seen[n] = t[n] < len;
         const int64_t tt = t[n];
@@ -476,49 +500,44 @@ __global__ __launch_bounds__(256) void attend_dkv_kernel(AttendK k)
     const T *gp = (const T *)k.dout.data + b * k.dout.batch;
     const int64_t sums0 = (int64_t)b * k.H * k.Tq;
     const int32_t *pp = BIAS ? k.bias.qpos + b * k.bias.qbatch : nullptr;
-    Stage<T, DP, ROWS, THREADS> sq, sg;
+    Stage<T, DP, ROWS, Team<SHARED>::kStagers> sq, sg;
     StagePos<BIAS ? ROWS : 1> sp;
     StageSums<ROWS> ss;
-    // the tile that is fetched next: head of the group, first row
-    int fg = first / a_head, ft = first % a_head * ROWS;
-    auto fetch = [&]() {
-        const int h = kvh * G + fg;
-        sq.fetch(qp + h * k.q.head, k.q.token, ft, k.Tq, k.D);
-        sg.fetch(gp + h * k.dout.head, k.dout.token, ft, k.Tq, k.D);
+    auto fetch = [&](int i) {       // tile i: a head of the group, its rows
+        const int g = i / a_head, row = (i - g * a_head) * ROWS;
+        const int h = kvh * G + g;
+        sq.fetch(stager, qp + h * k.q.head, k.q.token, row, k.Tq, k.D);
+        sg.fetch(stager, gp + h * k.dout.head, k.dout.token, row, k.Tq, k.D);
         const int64_t at = sums0 + (int64_t)h * k.Tq;
-        ss.fetch(k.lse + at, k.delta + at, ft, k.Tq, kWeightLift<T>);
-        if (BIAS) sp.fetch(pp, k.bias.axes, ft, k.Tq);
-        ft += ROWS;
-        if (ft >= k.Tq) {
-            ft = 0;
-            ++fg;
-        }
+        ss.fetch(stager, k.lse + at, k.delta + at, row, k.Tq, kWeightLift<T>);
+        if (BIAS) sp.fetch(stager, pp, k.bias.axes, row, k.Tq);
     };
     auto put = [&](int to) {
-        sq.put(tiles[to][0]);
-        sg.put(tiles[to][1]);
-        ss.put(sums[to]);
-        if (BIAS) sp.put(qpos[to], k.bias.axes);
+        sq.put(stager, tiles[me][to][0]);
+        sg.put(stager, tiles[me][to][1]);
+        ss.put(stager, sums[me][to]);
+        if (BIAS) sp.put(stager, qpos[me][to], k.bias.axes);
     };
     int head = -1;              // whose bias is in LDS
-    int at_head = first / a_head, left = a_head - first % a_head;
-    if (first < last) {
-        fetch();
+    const int first1 = first + me;
+    if (first1 < last) {
+        fetch(first1);
         put(0);
     }
-    __syncthreads();
+    team.meet();
     int cur = 0;
-    for (int i0 = first; i0 < last; ++i0, cur ^= 1) {
-        const bool more = i0 + 1 < last;
-        if (more) fetch();
-        if (BIAS && head != at_head) {      // (the same for the whole block)
+    for (int i0 = first1; i0 < last; i0 += STEP, cur ^= BUFS - 1) {
+        const bool more = i0 + STEP < last;
+        if (more && (!SHARED || kAhead<T, DP>)) fetch(i0 + STEP);
+        if (BIAS && head != i0 / a_head) {      // (the same for all that share it)
+            head = i0 / a_head;
             // (mirrored: the rows are queries here)
-            load_bias(dense, k.bias, kvh * G + at_head, k.H, THREADS, true);
-            head = at_head;
-            __syncthreads();
+            load_bias(dense[me], k.bias, kvh * G + head, k.H, stager, Team<SHARED>::kStagers,
+                      true);
+            team.meet();
         }
-        const T *qt = tiles[cur][0], *gt = tiles[cur][1];
-        const float *sm = sums[cur];
+        const T *qt = tiles[me][cur][0], *gt = tiles[me][cur][1];
+        const float *sm = sums[me][cur];
         f32x16 p[NC], g[NC];
 #pragma unroll
         for (int n = 0; n < NC; ++n) {
@@ -527,8 +546,8 @@ __global__ __launch_bounds__(256) void attend_dkv_kernel(AttendK k)
         }
         if constexpr (BIAS) {
             const int base[NC] = {};
-            add_bias<NC, ROWS>(p, k.scale, qpos[cur], 0, half, dense, base, kpos, k.bias.axes,
-                               k.bias.reach);
+            add_bias<NC, ROWS>(p, k.scale, qpos[me][cur], 0, half, dense[me], base, kpos,
+                               k.bias.axes, k.bias.reach);
         }
         const float unit = BIAS ? 1.0f : k.scale;
 #pragma unroll
@@ -540,21 +559,41 @@ __global__ __launch_bounds__(256) void attend_dkv_kernel(AttendK k)
                 g[n][i] = p[n][i] * (g[n][i] - delta);
             }
         }
-        if (len == 1) {     // (as in the queries' gradient)
-#pragma unroll
-            for (int n = 0; n < NC; ++n)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) g[n][i] = 0.0f;
-        }
         add_cols<T, DP, NC>(gt, lane, p, dv);
         lift.scale(g, dk);
         add_cols<T, DP, NC>(qt, lane, g, dk);
-        if (--left == 0) {
-            ++at_head;
-            left = a_head;
+        if (BUFS == 1) team.meet();
+        if (more) {
+            if (SHARED && !kAhead<T, DP>) fetch(i0 + STEP);
+            put(cur ^ (BUFS - 1));
         }
-        if (more) put(cur ^ 1);
-        __syncthreads();
+        team.meet();
+    }
+    // (one key: as in the queries' gradient)
+    const float plain = kLifted<T> ? 0x1p-15f : 1.0f;
+    const float scale = len == 1 ? 0.0f : k.plain_scale * plain;
+    const int64_t rows = (int64_t)k.B * k.Hk * k.Tk;
+    if constexpr (SHARED) {
+        float f[DP / 8], e[DP / 8];
+        float *room = (float *)&tiles[0][0][0][0];
+        join_waves<DP>(room, lane, wave, dk[0], lift.back(0), f);
+        join_waves<DP>(room, lane, wave, dv[0], 1.0f, e);
+        if (!there[0]) return;
+        if (!seen[0])
+#pragma unroll
+            for (int i = 0; i < DP / 8; ++i) e[i] = f[i] = 0.0f;
+        const int d = (2 * wave + half) * (DP / 8);
+        const int64_t tt = t[0], row = ((int64_t)b * k.Hk + kvh) * k.Tk + tt;
+        if (k.splits > 1) {
+            store_run<float>(k.part + (split * rows + row) * k.D, d, k.D, f, scale);
+            store_run<float>(k.part + ((k.splits + split) * rows + row) * k.D, d, k.D, e, plain);
+        } else {
+            store_run<T>((T *)k.dk.data + b * k.dk.batch + tt * k.dk.token + kvh * k.dk.head, d,
+                         k.D, f, scale);
+            store_run<T>((T *)k.dv.data + b * k.dv.batch + tt * k.dv.token + kvh * k.dv.head, d,
+                         k.D, e, plain);
+        }
+        return;
     }
 #pragma unroll
     for (int n = 0; n < NC; ++n) {
@@ -566,17 +605,15 @@ __global__ __launch_bounds__(256) void attend_dkv_kernel(AttendK k)
                 for (int i = 0; i < 16; ++i) dk[n][d][i] = dv[n][d][i] = 0.0f;
         }
         const int64_t tt = t[n];
-        const float plain = kLifted<T> ? 0x1p-15f : 1.0f;
-        const float dk_by = lift.back(n) * k.plain_scale * plain;
+        const float by = lift.back(n) * scale;
         if (k.splits > 1) {
-            const int64_t rows = (int64_t)k.B * k.Hk * k.Tk;
             const int64_t row = ((int64_t)b * k.Hk + kvh) * k.Tk + tt;
-            store_column<float, DP>(k.part + (split * rows + row) * k.D, half, k.D, dk[n], dk_by);
+            store_column<float, DP>(k.part + (split * rows + row) * k.D, half, k.D, dk[n], by);
             store_column<float, DP>(k.part + ((k.splits + split) * rows + row) * k.D, half, k.D,
                                     dv[n], plain);
         } else {
             store_column<T, DP>((T *)k.dk.data + b * k.dk.batch + tt * k.dk.token +
-                                    kvh * k.dk.head, half, k.D, dk[n], dk_by);
+                                    kvh * k.dk.head, half, k.D, dk[n], by);
             store_column<T, DP>((T *)k.dv.data + b * k.dv.batch + tt * k.dv.token +
                                     kvh * k.dv.head, half, k.D, dv[n], plain);
         }
@@ -654,23 +691,23 @@ hipError_t launch_back_q(const AttendK &k, const AttendPlan &p, hipStream_t stre
 {
     const unsigned grid = (unsigned)((int64_t)k.B * k.H * k.splits * k.blocks);
     const int entries = k.bias.axes * k.bias.buckets;
-    auto go = [&](auto nc) {
+    typedef std::true_type yes;
+    typedef std::false_type no;
+    auto go = [&](auto nc, auto shared) {
         constexpr int NC = decltype(nc)::value;
+        constexpr bool S = decltype(shared)::value;
         if (grid == 0) return;
         if (k.bias.axes)
-            attend_dq_kernel<T, DP, NC, true>
-                <<<grid, 256, 1024 * (entries + 1), stream>>>(k);
+            attend_dq_kernel<T, DP, NC, true, S>
+                <<<grid, 256, attend_hist_bytes(entries), stream>>>(k);
         else
-            attend_dq_kernel<T, DP, NC, false><<<grid, 256, 0, stream>>>(k);
+            attend_dq_kernel<T, DP, NC, false, S><<<grid, 256, 0, stream>>>(k);
     };
     typedef std::integral_constant<int, 1> one;
-    if constexpr (sizeof(T) == 2 && DP <= 64) {
-        if (p.cols == 256)
-            go(std::integral_constant<int, 2>());
-        else
-            go(one());
-    } else
-        go(one());
+    if (p.shared)
+        go(one(), yes());
+    else
+        go(one(), no());
     hipError_t e = hipGetLastError();
     if (e == hipSuccess && k.splits > 1) e = launch_sum<T>(k, k.H, k.Tq, k.dq, k.dq, 1, stream);
     if (e == hipSuccess && entries && k.dtable) {
@@ -686,10 +723,16 @@ hipError_t launch_back_kv(const AttendK &k, const AttendPlan &p, hipStream_t str
 {
     const unsigned grid = (unsigned)((int64_t)k.B * k.Hk * k.splits * k.blocks);
     if (grid == 0) return hipSuccess;
+    auto go = [&](auto bias, auto shared) {
+        attend_dkv_kernel<T, DP, 1, decltype(bias)::value, decltype(shared)::value>
+            <<<grid, 256, 0, stream>>>(k);
+    };
+    typedef std::true_type yes;
+    typedef std::false_type no;
     if (k.bias.axes)
-        attend_dkv_kernel<T, DP, 1, true><<<grid, 256, 0, stream>>>(k);
+        p.shared ? go(yes(), yes()) : go(yes(), no());
     else
-        attend_dkv_kernel<T, DP, 1, false><<<grid, 256, 0, stream>>>(k);
+        p.shared ? go(no(), yes()) : go(no(), no());
     hipError_t e = hipGetLastError();
     if (e == hipSuccess && k.splits > 1) e = launch_sum<T>(k, k.Hk, k.Tk, k.dk, k.dv, 2, stream);
     return e;

@@ -160,43 +160,103 @@ __device__ __forceinline__ float most_of(const f32x16 &s)
 // Rows behind the last one have no weight.
 __device__ __forceinline__ void cut_rows(f32x16 &s, int row0, int half, int last)
 {
+    rare();
 #pragma unroll
     for (int i = 0; i < 16; ++i)
         if (row0 + tile_row(i, half) >= last) s[i] = -INFINITY;
 }
 
-// W waves a block, 32 columns a wave: float32, and few columns (W = 1, PK heads'
-// biases in LDS).  EXACT: see attend_flow_kernel.
-template <typename T, int DP, int W, bool BIAS, bool EXACT>
-__global__ __launch_bounds__(64 * W) void attend_kernel(AttendK k)
+// The same where four waves share the columns: their sums are brought to one base and
+// joined in room.
+template <typename T, int DP>
+__device__ __forceinline__ void finish_shared(const AttendK &k, const ForwardWork &w,
+                                              const Columns<1> &c, const Team<true> &team,
+                                              const f32x16 (&acc)[DP / 32], float sum, float top,
+                                              float *room, float (&tops)[2][4][32])
+{
+    const int column = team.lane & 31, half = team.half;
+    sum = half_sum(sum);
+    if (half == 0) {
+        tops[0][team.wave][column] = top;
+        tops[1][team.wave][column] = sum;
+    }
+    __syncthreads();
+    float all = -INFINITY, l = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) all = fmaxf(all, tops[0][i][column]);
+    const float base = all == -INFINITY ? 0.0f : all;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        l += tops[1][i][column] * __builtin_amdgcn_exp2f(tops[0][i][column] - base);
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    float f[DP / 8];
+    join_waves<DP>(room, team.lane, team.wave, acc, __builtin_amdgcn_exp2f(top - base), f);
+    if (!c.there[0]) return;
+    const int d = (2 * team.wave + half) * (DP / 8);
+    const int64_t row = ((int64_t)w.b * k.H + c.head[0]) * k.Tq + c.t[0];
+    const float lse = base + __builtin_amdgcn_logf(l);
+    const bool first = team.wave == 0 && half == 0;
+    if (k.splits > 1) {
+        const int64_t rows = (int64_t)k.B * k.H * k.Tq;
+        if (first) k.part_lse[w.split * rows + row] = l == 0.0f ? -INFINITY : lse;
+        store_run<float>(k.part + (w.split * rows + row) * k.D, d, k.D, f, inv);
+        return;
+    }
+    if (k.lse && first) k.lse[row] = l == 0.0f ? INFINITY : lse;
+    store_run<T>((T *)k.o.data + w.b * k.o.batch + (int64_t)c.t[0] * k.o.token +
+                     c.head[0] * k.o.head, d, k.D, f, inv);
+    if (k.rest) {
+#pragma unroll
+        for (int i = 0; i < DP / 8; ++i) f[i] = rest_of<T>(f[i] * inv);
+        store_run<T>((T *)k.rest + (((int64_t)w.b * k.Tq + c.t[0]) * k.H + c.head[0]) * k.D, d,
+                     k.D, f, 1.0f);
+    }
+}
+
+// 32 columns a wave, or a block (SHARED): float32, and calls with few columns.
+// EXACT: see attend_flow_kernel.
+template <typename T, int DP, bool SHARED, bool BIAS, bool EXACT>
+__global__ __launch_bounds__(256) void attend_kernel(AttendK k)
 {
     typedef typename Matrix<T>::frag frag;
-    constexpr int ROWS = 32, THREADS = 64 * W, NC = 1;
-    constexpr int PK = BIAS ? (W == 1 ? 8 : 1) : 1;
+    constexpr int ROWS = 32, NC = 1, WAVES = SHARED ? 4 : 1, BUFS = SHARED ? 1 : 2;
+    constexpr int PK = BIAS && SHARED ? 8 : 1;      // heads that share the columns
     constexpr int TILE = ROWS * kStride<T, DP>;
-    __shared__ __attribute__((aligned(16))) T tiles[2][2][TILE];
+    // (two tiles of each wave are more than the 128 DP floats that joining them takes)
+    __shared__ __attribute__((aligned(16))) T tiles[WAVES][BUFS][2][TILE];
     __shared__ float dense[BIAS ? PK * kMaxBiasAxes * kReachRow : 1];
-    __shared__ TilePos<BIAS ? ROWS : 1> kpos[2];
+    __shared__ TilePos<BIAS ? ROWS : 1> kpos[WAVES][BUFS];
+    __shared__ float tops[2][4][32];
 
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
+    const Team<SHARED> team;
+    const int lane = team.lane, half = team.half, me = team.mine(), stager = team.stager();
+    constexpr int STEP = Team<SHARED>::kStep * ROWS;
     const ForwardWork w(k);
     const T *kp = (const T *)k.k.data + w.b * k.k.batch + w.kvh * k.k.head;
     const T *vp = (const T *)k.v.data + w.b * k.v.batch + w.kvh * k.v.head;
     const int32_t *pp = BIAS ? k.bias.kpos + w.b * k.bias.kbatch : nullptr;
-    Stage<T, DP, ROWS, THREADS> sk, sv;
+    Stage<T, DP, ROWS, Team<SHARED>::kStagers> sk, sv;
     StagePos<BIAS ? ROWS : 1> sp;
-    if (w.first < w.last) {
-        sk.fetch(kp, k.k.token, w.first, w.last, k.D);
-        sv.fetch(vp, k.v.token, w.first, w.last, k.D);
-        if (BIAS) sp.fetch(pp, k.bias.axes, w.first, w.last);
-    }
-    const Columns<NC> c(k, w, (w.rb * W + wave) * 32, lane);
+    auto fetch = [&](int row) {
+        sk.fetch(stager, kp, k.k.token, row, w.last, k.D);
+        sv.fetch(stager, vp, k.v.token, row, w.last, k.D);
+        if (BIAS) sp.fetch(stager, pp, k.bias.axes, row, w.last);
+    };
+    auto put = [&](int to) {
+        sk.put(stager, tiles[me][to][0]);
+        sv.put(stager, tiles[me][to][1]);
+        if (BIAS) sp.put(stager, kpos[me][to], k.bias.axes);
+    };
+    const int row1 = w.first + me * ROWS;
+    if (row1 < w.last) fetch(row1);
+    const Columns<NC> c(k, w, (SHARED ? w.rb : w.rb * 4 + team.wave) * 32, lane);
     frag q[NC][kPairs<T, DP>];
     c.template load<T, DP>(k, w.b, half, q);
     int qpos[NC][kMaxBiasAxes], hbase[NC];
     if (BIAS) {
         for (int p = 0; p < k.pack; ++p)
-            load_bias(dense + p * kMaxBiasAxes * kReachRow, k.bias, w.h0 + p, k.H, THREADS, false);
+            load_bias(dense + p * kMaxBiasAxes * kReachRow, k.bias, w.h0 + p, k.H, threadIdx.x,
+                      256, false);
         hbase[0] = (c.head[0] - w.h0) * kMaxBiasAxes * kReachRow;
         c.places(k, w.b, qpos);
     }
@@ -206,25 +266,18 @@ __global__ __launch_bounds__(64 * W) void attend_kernel(AttendK k)
     for (int d = 0; d < DP / 32; ++d)
 #pragma unroll
         for (int i = 0; i < 16; ++i) acc[0][d][i] = 0.0f;
-    if (w.first < w.last) {
-        sk.put(tiles[0][0]);
-        sv.put(tiles[0][1]);
-        if (BIAS) sp.put(kpos[0], k.bias.axes);
-    }
-    __syncthreads();
+    if (row1 < w.last) put(0);
+    if (SHARED && BIAS) __syncthreads();    // (the bias is the block's)
+    team.meet();
     int cur = 0;
-    for (int row0 = w.first; row0 < w.last; row0 += ROWS, cur ^= 1) {
-        const bool more = row0 + ROWS < w.last;
-        if (more) {
-            sk.fetch(kp, k.k.token, row0 + ROWS, w.last, k.D);
-            sv.fetch(vp, k.v.token, row0 + ROWS, w.last, k.D);
-            if (BIAS) sp.fetch(pp, k.bias.axes, row0 + ROWS, w.last);
-        }
-        const T *kt = tiles[cur][0], *vt = tiles[cur][1];
+    for (int row0 = row1; row0 < w.last; row0 += STEP, cur ^= BUFS - 1) {
+        const bool more = row0 + STEP < w.last;
+        if (more && (!SHARED || kAhead<T, DP>)) fetch(row0 + STEP);
+        const T *kt = tiles[me][cur][0], *vt = tiles[me][cur][1];
         f32x16 s[NC] = {row_mul<T, DP>(kt, lane, q[0])};
         if constexpr (BIAS)
-            add_bias<NC, ROWS>(s, k.scale, kpos[cur], 0, half, dense, hbase, qpos, k.bias.axes,
-                               k.bias.reach);
+            add_bias<NC, ROWS>(s, k.scale, kpos[me][cur], 0, half, dense, hbase, qpos,
+                               k.bias.axes, k.bias.reach);
         if (row0 + ROWS > w.last) cut_rows(s[0], row0, half, w.last);
         const float unit = BIAS ? 1.0f : k.scale;
         rebase(most_of(s[0]) * unit, top[0], sum[0], acc[0]);
@@ -247,13 +300,17 @@ __global__ __launch_bounds__(64 * W) void attend_kernel(AttendK k)
             }
         }
         if (more) {
-            sk.put(tiles[cur ^ 1][0]);
-            sv.put(tiles[cur ^ 1][1]);
-            if (BIAS) sp.put(kpos[cur ^ 1], k.bias.axes);
+            if (SHARED) team.meet();
+            if (SHARED && !kAhead<T, DP>) fetch(row0 + STEP);
+            put(cur ^ (BUFS - 1));
         }
-        __syncthreads();
+        team.meet();
     }
-    finish<T, DP, NC>(k, w, c, half, acc, sum, top);
+    if constexpr (SHARED)
+        finish_shared<T, DP>(k, w, c, team, acc[0], sum[0], top[0], (float *)&tiles[0][0][0][0],
+                             tops);
+    else
+        finish<T, DP, NC>(k, w, c, half, acc, sum, top);
 }
 
 // Four waves a block, NC blocks of 32 columns a wave, for the 16-bit types.  There an
@@ -288,11 +345,11 @@ __global__ __launch_bounds__(256, kFlowWaves<DP>) void attend_flow_kernel(Attend
     Stage<T, DP, ROWS, THREADS> sk, sv;
     StagePos<BIAS ? ROWS : 1> sp;
     auto put_keys = [&](int row, int slot) {
-        sk.fetch(kp, k.k.token, row, w.last, k.D);
-        sk.put(ktiles[slot]);
+        sk.fetch(threadIdx.x, kp, k.k.token, row, w.last, k.D);
+        sk.put(threadIdx.x, ktiles[slot]);
         if (BIAS) {
-            sp.fetch(pp, k.bias.axes, row, w.last);
-            sp.put(kpos[slot], k.bias.axes);
+            sp.fetch(threadIdx.x, pp, k.bias.axes, row, w.last);
+            sp.put(threadIdx.x, kpos[slot], k.bias.axes);
         }
     };
     const Columns<NC> c(k, w, (w.rb * 4 + wave) * NC * 32, lane);
@@ -301,12 +358,12 @@ __global__ __launch_bounds__(256, kFlowWaves<DP>) void attend_flow_kernel(Attend
     if (w.first < w.last) {
         put_keys(w.first, 0);
         put_keys(w.first + ROWS, 1);
-        sv.fetch(vp, k.v.token, w.first, w.last, k.D);
-        sv.put(vtiles[0]);
+        sv.fetch(threadIdx.x, vp, k.v.token, w.first, w.last, k.D);
+        sv.put(threadIdx.x, vtiles[0]);
     }
     c.template load<T, DP>(k, w.b, half, q);
     if (BIAS) {
-        load_bias(dense, k.bias, w.h0, k.H, THREADS, false);
+        load_bias(dense, k.bias, w.h0, k.H, threadIdx.x, THREADS, false);
         c.places(k, w.b, qpos);
 #pragma unroll
         for (int n = 0; n < NC; ++n) hbase[n] = 0;
@@ -355,9 +412,9 @@ __global__ __launch_bounds__(256, kFlowWaves<DP>) void attend_flow_kernel(Attend
         }
     int k0 = 0, k1 = 1, k2 = 2, v0 = 0, v1 = 1, v2 = 2;     // slots of this tile, the next ..
     for (int row0 = w.first; row0 < w.last; row0 += ROWS) {
-        sk.fetch(kp, k.k.token, row0 + 2 * ROWS, w.last, k.D);
-        sv.fetch(vp, k.v.token, row0 + ROWS, w.last, k.D);
-        if (BIAS) sp.fetch(pp, k.bias.axes, row0 + 2 * ROWS, w.last);
+        sk.fetch(threadIdx.x, kp, k.k.token, row0 + 2 * ROWS, w.last, k.D);
+        sv.fetch(threadIdx.x, vp, k.v.token, row0 + ROWS, w.last, k.D);
+        if (BIAS) sp.fetch(threadIdx.x, pp, k.bias.axes, row0 + 2 * ROWS, w.last);
 #pragma unroll
         for (int u = 0; u < SUBS; ++u) {
             if constexpr (BIAS)
@@ -401,9 +458,9 @@ __global__ __launch_bounds__(256, kFlowWaves<DP>) void attend_flow_kernel(Attend
             for (int n = 0; n < NC; ++n) s[n] = s2[n];
             held = vtiles[v0] + 32 * u * kStride<T, DP>;
         }
-        sk.put(ktiles[k2]);
-        sv.put(vtiles[v1]);
-        if (BIAS) sp.put(kpos[k2], k.bias.axes);
+        sk.put(threadIdx.x, ktiles[k2]);
+        sv.put(threadIdx.x, vtiles[v1]);
+        if (BIAS) sp.put(threadIdx.x, kpos[k2], k.bias.axes);
         __syncthreads();
         int x = k0;
         k0 = k1;
@@ -534,17 +591,16 @@ hipError_t launch_forward(AttendK k, const AttendPlan &p, hipStream_t stream)
             if (exact) return k.bias.axes ? go(yes(), yes()) : go(no(), yes());
         return k.bias.axes ? go(yes(), no()) : go(no(), no());
     };
-    auto simple = [&](auto w) {
-        constexpr int W = decltype(w)::value;
+    auto simple = [&](auto shared) {
         variant([&](auto bias, auto ex) {
-            attend_kernel<T, DP, W, decltype(bias)::value, decltype(ex)::value>
-                <<<grid, 64 * W, 0, stream>>>(k);
+            attend_kernel<T, DP, decltype(shared)::value, decltype(bias)::value,
+                          decltype(ex)::value><<<grid, 256, 0, stream>>>(k);
         });
     };
-    if (p.narrow) {
-        simple(std::integral_constant<int, 1>());
+    if (p.shared) {
+        simple(yes());
     } else if constexpr (sizeof(T) == 4) {
-        simple(std::integral_constant<int, 4>());
+        simple(no());
     } else if (twice) {
         if constexpr (DP <= 64)
             attend_flow_kernel<T, DP, 2, false, false><<<grid, 256, 0, stream>>>(k);

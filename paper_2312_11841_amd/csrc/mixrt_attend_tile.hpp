@@ -29,6 +29,11 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 template <typename T> inline constexpr int kChunk = 16 / (int)sizeof(T);
 template <typename T, int DP> inline constexpr int kStride = DP + kChunk<T>;
 
+// At the start of a branch that a wave takes seldom: keeps the compiler from working
+// out both sides for every tile (its selects made up a third of the forward kernel's
+// instructions).
+__device__ __forceinline__ void rare() { asm volatile(""); }
+
 __device__ __forceinline__ int tile_row(int i, int half) { return 8 * (i >> 2) + 4 * half + (i & 3); }
 
 // The value of the lane 32 further beside the lane's own, combined.
@@ -163,8 +168,22 @@ __device__ __forceinline__ u32x4 load_chunk(const T *row, int at, int D)
     return __builtin_bit_cast(u32x4, t);
 }
 
-// A tile of ROWS rows of a block of THREADS: fetched into registers, put into LDS
-// when the tile before is used up.
+// d = 32 block + 8 quad + 4 half + 0..3 of a column's result.
+template <typename T>
+__device__ __forceinline__ void store_quad(T *row, int d, int D, float a, float b, float c, float e)
+{
+    const float f[4] = {a, b, c, e};
+    if (d + 4 <= D) {
+        store_vec<T, 4>(row + d, f);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (d + i < D) row[d + i] = (T)f[i];
+    }
+}
+
+// A tile of ROWS rows, fetched by THREADS threads into registers and put into LDS when
+// the tile before is used up.
 template <typename T, int DP, int ROWS, int THREADS>
 struct Stage {
     static constexpr int kChunks = DP / kChunk<T>;
@@ -174,13 +193,13 @@ struct Stage {
     u32x4 r[kEach];
 
     // rows [first, limit) of the array at base, as far as the tile reaches
-    __device__ __forceinline__ void fetch(const T *base, int64_t stride, int first, int limit,
-                                          int D)
+    __device__ __forceinline__ void fetch(int thread, const T *base, int64_t stride, int first,
+                                          int limit, int D)
     {
         if (kEven && D == DP && first + ROWS <= limit) {    // nothing to leave out
 #pragma unroll
             for (int j = 0; j < kEach; ++j) {
-                const int at = threadIdx.x + j * THREADS;
+                const int at = thread + j * THREADS;
                 r[j] = __builtin_bit_cast(
                     u32x4, *(const Pack<T, kChunk<T>> *)(base + (int64_t)(first + at / kChunks) *
                                                                     stride +
@@ -190,23 +209,87 @@ struct Stage {
         }
 #pragma unroll
         for (int j = 0; j < kEach; ++j) {
-            const int at = threadIdx.x + j * THREADS;
+            const int at = thread + j * THREADS;
             const int row = at / kChunks, c = at % kChunks;
             r[j] = u32x4{0, 0, 0, 0};
             if ((kEven || at < kAll) && first + row < limit && c * kChunk<T> < D)
                 r[j] = load_chunk<T>(base + (int64_t)(first + row) * stride, c * kChunk<T>, D);
         }
     }
-    __device__ __forceinline__ void put(T *tile) const
+    __device__ __forceinline__ void put(int thread, T *tile) const
     {
 #pragma unroll
         for (int j = 0; j < kEach; ++j) {
-            const int at = threadIdx.x + j * THREADS;
+            const int at = thread + j * THREADS;
             if (kEven || at < kAll)
                 *(u32x4 *)(tile + at / kChunks * kStride<T, DP> + at % kChunks * kChunk<T>) = r[j];
         }
     }
 };
+
+// How a block's four waves divide its work.  Alone: a wave has columns of its own and
+// the tiles are the block's.  Shared, where a call has few columns: all waves have the
+// same 32 and every fourth tile each, staged by itself, and their sums are joined in
+// LDS at the end.
+template <bool SHARED>
+struct Team {
+    static constexpr int kStagers = SHARED ? 64 : 256;
+    static constexpr int kStep = SHARED ? 4 : 1;        // tiles from one to the next
+    int lane, wave, half;
+    __device__ __forceinline__ Team()
+        : lane(threadIdx.x & 63), wave(threadIdx.x >> 6), half(threadIdx.x >> 5 & 1)
+    {
+    }
+    __device__ __forceinline__ int stager() const { return SHARED ? lane : (int)threadIdx.x; }
+    __device__ __forceinline__ int mine() const { return SHARED ? wave : 0; }
+    // tiles written are there to be read, tiles read may be written
+    __device__ __forceinline__ void meet() const
+    {
+        if (SHARED) {
+            // (a wave's accesses to LDS take place in its order)
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+        } else {
+            __syncthreads();
+        }
+    }
+};
+
+// Whether a wave that stages alone has registers to fetch a tile ahead.
+template <typename T, int DP> inline constexpr bool kAhead = DP * sizeof(T) <= 256;
+
+// Joins the sums of four waves that share their columns: a lane gets DP / 8 of its
+// column's, from d = (2 wave + half) DP / 8 on.  room: 128 DP floats.
+template <int DP>
+__device__ __forceinline__ void join_waves(float *room, int lane, int wave,
+                                           const f32x16 (&acc)[DP / 32], float by,
+                                           float (&out)[DP / 8])
+{
+    const int half = lane >> 5, column = lane & 31;
+    __syncthreads();
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+            room[(wave * DP + 32 * d + tile_row(i, half)) * 32 + column] = acc[d][i] * by;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < DP / 8; ++i) {
+        const int d = (2 * wave + half) * (DP / 8) + i;
+        float s = 0.0f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) s += room[(w * DP + d) * 32 + column];
+        out[i] = s;
+    }
+}
+
+template <typename T, int N>
+__device__ __forceinline__ void store_run(T *row, int d, int D, const float (&f)[N], float by)
+{
+#pragma unroll
+    for (int i = 0; i < N; i += 4)
+        store_quad<T>(row, d + i, D, f[i] * by, f[i + 1] * by, f[i + 2] * by, f[i + 3] * by);
+}
 
 // Operand B of a column's head, from memory (zeros for a column that is not there).
 template <typename T, int DP>
@@ -219,20 +302,6 @@ __device__ __forceinline__ void load_column(typename Matrix<T>::frag (&f)[(kPair
         u32x4 x = {0, 0, 0, 0};
         if (there && at < D) x = load_chunk<T>(row, at, D);
         f[c] = __builtin_bit_cast(typename Matrix<T>::frag, x);
-    }
-}
-
-// d = 32 block + 8 quad + 4 half + 0..3 of a column's result.
-template <typename T>
-__device__ __forceinline__ void store_quad(T *row, int d, int D, float a, float b, float c, float e)
-{
-    const float f[4] = {a, b, c, e};
-    if (d + 4 <= D) {
-        store_vec<T, 4>(row + d, f);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (d + i < D) row[d + i] = (T)f[i];
     }
 }
 
@@ -291,10 +360,10 @@ __device__ __forceinline__ int bucket_of(const BiasK &b, int axis, int entry, bo
 
 // bias[entry] of head's axes, times log2(e).
 __device__ __forceinline__ void load_bias(float *dense, const BiasK &b, int head, int H,
-                                          int threads, bool mirrored)
+                                          int thread, int threads, bool mirrored)
 {
     const int n = 2 * b.reach + 1 + 2 * kPad;
-    for (int i = threadIdx.x; i < b.axes * n; i += threads) {
+    for (int i = thread; i < b.axes * n; i += threads) {
         const int a = i / n, e = i - a * n;
         dense[a * kReachRow + e] =
             b.table[((int64_t)a * b.buckets + bucket_of(b, a, e, mirrored)) * H + head] * kLog2e;
@@ -313,18 +382,19 @@ template <int ROWS>
 struct StagePos {
     int32_t r[kMaxBiasAxes];
     bool there;
-    __device__ __forceinline__ void fetch(const int32_t *pos, int axes, int first, int limit)
+    __device__ __forceinline__ void fetch(int thread, const int32_t *pos, int axes, int first,
+                                          int limit)
     {
-        const int row = first + (int)threadIdx.x;
-        there = threadIdx.x < ROWS && row < limit;
+        const int row = first + thread;
+        there = thread < ROWS && row < limit;
 #pragma unroll
         for (int a = 0; a < kMaxBiasAxes; ++a)
             r[a] = there && a < axes ? pos[(int64_t)row * axes + a] : 0;
     }
-    __device__ __forceinline__ void put(TilePos<ROWS> &tile, int axes) const
+    __device__ __forceinline__ void put(int thread, TilePos<ROWS> &tile, int axes) const
     {
-        if (threadIdx.x >= 64) return;      // the first wave holds the rows
-        const int lane = threadIdx.x;
+        if (thread >= 64) return;           // the first wave holds the rows
+        const int lane = thread;
 #pragma unroll
         for (int a = 0; a < kMaxBiasAxes; ++a) {
             if (a >= axes) break;
