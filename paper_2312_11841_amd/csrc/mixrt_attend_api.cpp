@@ -22,19 +22,51 @@ int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 // about 1024 or 2048 of them, so that its roundings stay below the result's.
 int64_t longest(int dtype) { return attend_elem(dtype) == 4 ? 2048 : 32768; }
 
-// Splits of a walk over n rows so that about want blocks run, none shorter than
-// least, and none longer than most; per is a multiple of step.
-void split(int64_t n, int64_t blocks, int64_t want, int64_t least, int64_t most, int64_t step,
-           int *splits, int *per)
+// Splits of a walk over n rows, none longer than most; per is a multiple of step.
+void divide(int64_t n, int64_t s, int64_t most, int64_t step, int *splits, int *per)
 {
-    int64_t s = blocks > 0 ? want / blocks : 1;
-    if (s > n / least) s = n / least;
     if (s < ceil_div(n, most)) s = ceil_div(n, most);
     if (s < 1) s = 1;
     int64_t p = ceil_div(ceil_div(n, s), step) * step;
     if (p < step) p = step;
     *per = (int)p;
     *splits = (int)(n > 0 ? ceil_div(n, p) : 1);
+}
+
+// Blocks that run together, by the registers and LDS that the kernels take.
+int64_t resident(int D, int dtype, int a_cu)
+{
+    return kCUs * (attend_dim(D) * attend_elem(dtype) <= 128 ? a_cu : 1);
+}
+
+// Splits of long walks: the blocks' rounds over the chip are whole, so s splits take
+// ceil(blocks s / slots) / (blocks s / slots) of what they could, and each is a part to
+// write and to join (about 1/25).  Two 720p views with two reference views each, 12 and
+// 3 heads of 64, bf16: the keys' gradient has 342 blocks for 512 slots; all of a
+// training step's calls take 1172 us with 1 split, 1122 with 2, 1139 with 3, 1029 with
+// 4, 1077 with 6.
+int64_t whole_rounds(int64_t n, int64_t blocks, int64_t slots, int64_t least)
+{
+    int64_t best = 1;
+    double low = 1e30;
+    for (int64_t s = 1; s <= 16 && blocks > 0 && (s == 1 || n / s >= least); ++s) {
+        const double rounds = (double)(blocks * s) / slots;
+        const double cost = std::ceil(rounds) / rounds + 0.04 * s;
+        if (cost < low) {
+            low = cost;
+            best = s;
+        }
+    }
+    return best;
+}
+
+// Splits where a block's waves share its columns: enough for two blocks a CU, of least
+// rows.  (One token of 32 heads of 128 over 14,400 keys of 8, bf16: 28 splits 20.7 us,
+// 57 19.4, 113 25.2.)
+int64_t enough(int64_t n, int64_t blocks, int64_t least)
+{
+    const int64_t s = blocks > 0 ? 2 * kCUs / blocks : 1;
+    return s < ceil_div(n, least) ? s : ceil_div(n, least);
 }
 
 // Whether blocks of 128 columns are few for the chip, also when their walks of rows are
@@ -63,7 +95,10 @@ AttendPlan plan_attend(int B, int H, int Hk, int64_t Tq, int64_t Tk, int D, int 
     p.cols = p.shared ? 32 : 128;
     if (attend_elem(dtype) == 2 && D <= 64 && axes == 0 && !p.shared && cols > 1024) p.cols = 256;
     p.blocks = blocks_of(cols, p.cols);
-    split(Tk, heads * p.blocks, 2 * kCUs, 512, longest(dtype), 128, &p.splits, &p.per);
+    const int64_t blocks = heads * p.blocks;
+    const int64_t s = p.shared ? enough(Tk, blocks, 256)
+                               : whole_rounds(Tk, blocks, resident(D, dtype, 2), 512);
+    divide(Tk, s, longest(dtype), p.shared ? 128 : 64, &p.splits, &p.per);
     return p;
 }
 
@@ -82,7 +117,11 @@ AttendPlan plan_attend_dq(int B, int H, int Hk, int64_t Tq, int64_t Tk, int D, i
     p.blocks = blocks_of(Tq, p.cols);
     int64_t most = longest(dtype);
     if (axes && p.shared && most > 4096) most = 4096;   // (1024 keys of a lane's table sums)
-    split(Tk, heads * p.blocks, 2 * kCUs, 512, most, 128, &p.splits, &p.per);
+    // (float32's products are so slow that a wave's second tile is worth a join)
+    const int64_t blocks = heads * p.blocks, least = attend_elem(dtype) == 4 ? 128 : 256;
+    const int64_t s = p.shared ? enough(Tk, blocks, least)
+                               : whole_rounds(Tk, blocks, resident(D, dtype, axes ? 1 : 3), 512);
+    divide(Tk, s, most, p.shared ? 128 : 32, &p.splits, &p.per);
     return p;
 }
 
@@ -96,7 +135,10 @@ AttendPlan plan_attend_dkv(int B, int H, int Hk, int64_t Tq, int64_t Tk, int D, 
     p.cols = p.shared ? 32 : 128;
     p.blocks = blocks_of(Tk, p.cols);
     const int64_t tiles = H / Hk * ceil_div(Tq, 32);
-    split(tiles, heads * p.blocks, 2 * kCUs, 16, longest(dtype) / 32, 4, &p.splits, &p.per);
+    const int64_t blocks = heads * p.blocks;
+    const int64_t s = p.shared ? enough(tiles, blocks, 8)
+                               : whole_rounds(tiles, blocks, resident(D, dtype, 2), 16);
+    divide(tiles, s, longest(dtype) / 32, p.shared ? 4 : 1, &p.splits, &p.per);
     return p;
 }
 
