@@ -44,6 +44,32 @@ __device__ __forceinline__ void add_cols(const T *tile, int lane, const f32x16 (
     }
 }
 
+// s += a-tile's rows times b, g += e-tile's rows times f.  The operands of 16-bit heads
+// of up to 64 elements are all read first: a wave is often alone on its SIMD, and would
+// wait for LDS before each product.
+template <typename T, int DP, int NC>
+__device__ __forceinline__ void pair_mul(const T *a, const T *e, int lane,
+                                         const typename Matrix<T>::frag (&b)[NC][(kPairs<T, DP>)],
+                                         const typename Matrix<T>::frag (&f)[NC][(kPairs<T, DP>)],
+                                         f32x16 (&s)[NC], f32x16 (&g)[NC])
+{
+    constexpr bool FIRST = sizeof(T) == 2 && DP <= 64;
+    typename Matrix<T>::frag x[kPairs<T, DP>], y[kPairs<T, DP>];
+#pragma unroll
+    for (int c = 0; c < kPairs<T, DP>; ++c) {
+        x[c] = row_frag<T, DP>(a, lane, c);
+        y[c] = row_frag<T, DP>(e, lane, c);
+    }
+    if (FIRST) __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int c = 0; c < kPairs<T, DP>; ++c)
+#pragma unroll
+        for (int n = 0; n < NC; ++n) {
+            s[n] = Matrix<T>::mul(x[c], b[n][c], s[n]);
+            g[n] = Matrix<T>::mul(y[c], f[n][c], g[n]);
+        }
+}
+
 template <int NC, int ND>
 __device__ __forceinline__ void clear(f32x16 (&a)[NC][ND])
 {
@@ -139,39 +165,68 @@ __device__ __forceinline__ void add_table(const f32x16 &g, const TilePos<ROWS> &
                                           float *mine, int spare)
 {
     static_assert(ROWS == 32, "one block of rows");
+    float quad[4];
+    int kind[kMaxBiasAxes], at[kMaxBiasAxes];
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        quad[j] = (g[4 * j] + g[4 * j + 1]) + (g[4 * j + 2] + g[4 * j + 3]);
+    // the axes on which all rows have one place, together: their places lie apart (the
+    // other axes add to the spare one)
+#pragma unroll
+    for (int a = 0; a < kMaxBiasAxes; ++a) {
+        kind[a] = tile.kind_of(a, 0);
+        at[a] = place[a * kReachRow + bias_at(tile.at[a][0], column[a], reach)];
+    }
+    float old[kMaxBiasAxes];
+#pragma unroll
+    for (int a = 0; a < kMaxBiasAxes; ++a) {
+        at[a] = a < axes && kind[a] == kLevel ? at[a] : spare;
+        old[a] = mine[at[a]];
+    }
+#pragma unroll
+    for (int a = 0; a < kMaxBiasAxes; ++a)
+        mine[at[a]] = old[a] + ((quad[0] + quad[1]) + (quad[2] + quad[3]));
 #pragma unroll
     for (int a = 0; a < kMaxBiasAxes; ++a) {
         if (a >= axes) break;
-        const uint32_t kind = __builtin_amdgcn_readfirstlane(tile.kind[a]);
+        if (kind[a] == kLevel) continue;
         const uint16_t *row = place + a * kReachRow;
-        if (kind >> 16 & 1) {
-            float s = g[0];
-#pragma unroll
-            for (int i = 1; i < 16; ++i) s += g[i];
-            mine[row[bias_at(tile.at[a][0], column[a], reach)]] += s;
-            continue;
-        }
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int32_t *p = &tile.at[a][8 * j + 4 * half];
-            if ((kind >> j & 1) && !(kind >> (8 + j) & 1)) {
-                const float s = (g[4 * j] + g[4 * j + 1]) + (g[4 * j + 2] + g[4 * j + 3]);
-                mine[row[bias_at(p[0], column[a], reach)]] += s;
-                continue;
-            }
+        const int32_t *p = &tile.at[a][4 * half];
+        if (kind[a] == kLevel8) {
             int e[4];
             float v[4];
-            if (kind >> (8 + j) & 1) {
-                const uint16_t *at = row + bias_at(p[0], column[a], reach, kPad);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) e[i] = at[i];
-            } else {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) e[i] = row[bias_at(p[i], column[a], reach)];
+            for (int j = 0; j < 4; ++j) {
+                e[j] = row[bias_at(p[8 * j], column[a], reach)];
+                v[j] = quad[j];
             }
+            add_places(mine, e, v, spare);
+            continue;
+        }
+        int e[4][4];
+        if (kind[a] == kSteps) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const uint16_t *q = row + bias_at(p[8 * j], column[a], reach, kPad);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) e[j][i] = q[i];
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) e[j][i] = row[bias_at(p[8 * j + i], column[a], reach)];
+        }
+        // (all 16 places are read before the first is added to)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            asm volatile("" : "+v"(e[j][0]), "+v"(e[j][1]), "+v"(e[j][2]), "+v"(e[j][3]));
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            float v[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) v[i] = g[4 * j + i];
-            add_places(mine, e, v, spare);
+            add_places(mine, e[j], v, spare);
         }
     }
 }
@@ -331,15 +386,7 @@ __global__ __launch_bounds__(256) void attend_dq_kernel(AttendK k)
         for (int n = 0; n < NC; ++n)
 #pragma unroll
             for (int i = 0; i < 16; ++i) s[n][i] = g[n][i] = 0.0f;
-#pragma unroll
-        for (int c = 0; c < kPairs<T, DP>; ++c) {
-            const frag a = row_frag<T, DP>(kt, lane, c), v = row_frag<T, DP>(vt, lane, c);
-#pragma unroll
-            for (int n = 0; n < NC; ++n) {
-                s[n] = Matrix<T>::mul(a, q[n][c], s[n]);
-                g[n] = Matrix<T>::mul(v, dout[n][c], g[n]);
-            }
-        }
+        pair_mul<T, DP, NC>(kt, vt, lane, q, dout, s, g);
         if constexpr (BIAS) {
             const int base[NC] = {};
             add_bias<NC, ROWS>(s, k.scale, kpos[me][cur], 0, half, dense, base, qpos, k.bias.axes,
@@ -540,10 +587,10 @@ __global__ __launch_bounds__(256) void attend_dkv_kernel(AttendK k)
         const float *sm = sums[me][cur];
         f32x16 p[NC], g[NC];
 #pragma unroll
-        for (int n = 0; n < NC; ++n) {
-            p[n] = row_mul<T, DP>(qt, lane, key[n]);
-            g[n] = row_mul<T, DP>(gt, lane, val[n]);
-        }
+        for (int n = 0; n < NC; ++n)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) p[n][i] = g[n][i] = 0.0f;
+        pair_mul<T, DP, NC>(qt, gt, lane, key, val, p, g);
         if constexpr (BIAS) {
             const int base[NC] = {};
             add_bias<NC, ROWS>(p, k.scale, qpos[me][cur], 0, half, dense[me], base, kpos,

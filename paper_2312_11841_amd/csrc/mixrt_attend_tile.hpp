@@ -335,10 +335,13 @@ __device__ __forceinline__ float rest_of(float o)
 // --- the bias ---------------------------------------------------------------------
 //
 // A lane's column and a tile's row have a distance on each axis.  Tokens of views come
-// row by row, so of 8 rows that follow each other mostly all have the same place on an
-// axis, or places that count up by one; a tile carries for each axis which of its
-// octets are such.  Then one place in the table serves an octet, or four neighbours of
-// one place serve a lane's four rows, and only other octets pay for each row's own.
+// row by row, so of 32 rows that follow each other mostly all have the same place on an
+// axis, or every 8 of them have places that count up by one, or one place.  A tile
+// carries for each axis which of these holds: then one place in the table serves 32
+// rows, four neighbours of one place a lane's four rows of an octet, or one place an
+// octet, and only blocks that mix them work out each row's own.  Each kind is one
+// stretch of code without branches, so that its reads of LDS run together (with a
+// branch an octet the bias' part waited for each read: DQTIMES).
 
 constexpr int kPad = 4;                                     // entries beyond either end
 constexpr int kReachRow = 2 * kMaxReach + 2 + 2 * kPad;     // of an axis and head in LDS
@@ -370,12 +373,17 @@ __device__ __forceinline__ void load_bias(float *dense, const BiasK &b, int head
     }
 }
 
-// Places of a tile's rows on each axis, and which octets are level (one place) or
-// steps (places that count up by one); level32: blocks of 32 rows with one place.
+enum { kMixed, kLevel, kSteps, kLevel8 };
+
+// Places of a tile's rows on each axis, and the kind of each block of 32 rows.
 template <int ROWS>
 struct TilePos {
     __attribute__((aligned(16))) int32_t at[kMaxBiasAxes][ROWS];
-    uint32_t kind[kMaxBiasAxes];    // level octets, << 8 steps, << 16 level32
+    uint32_t kind[kMaxBiasAxes];    // 2 bits a block
+    __device__ __forceinline__ int kind_of(int axis, int u) const
+    {
+        return __builtin_amdgcn_readfirstlane((int)kind[axis]) >> (2 * u) & 3;
+    }
 };
 
 template <int ROWS>
@@ -408,13 +416,12 @@ struct StagePos {
             const uint64_t w = __builtin_amdgcn_ballot_w64(alike);
             uint32_t kind = 0;
 #pragma unroll
-            for (int j = 0; j < ROWS / 8; ++j) {
-                kind |= (uint32_t)((l >> (8 * j) & 255) == 255) << j;
-                kind |= (uint32_t)((s >> (8 * j) & 255) == 255) << (8 + j);
+            for (int u = 0; u < ROWS / 32; ++u) {
+                const auto all_of = [&](uint64_t m) { return (uint32_t)(m >> (32 * u)) == ~0u; };
+                const uint32_t is = all_of(w) ? kLevel : all_of(s) ? kSteps : all_of(l) ? kLevel8
+                                                                                         : kMixed;
+                kind |= is << (2 * u);
             }
-#pragma unroll
-            for (int u = 0; u < ROWS / 32; ++u)
-                kind |= (uint32_t)((uint32_t)(w >> (32 * u)) == 0xffffffffu) << (16 + u);
             if (lane < ROWS) tile.at[a][lane] = r[a];
             if (lane == 0) tile.kind[a] = kind;
         }
@@ -428,20 +435,22 @@ __device__ __forceinline__ void add_bias(f32x16 (&s)[NC], float scale, const Til
                                          const int (&base)[NC],
                                          const int (&column)[NC][kMaxBiasAxes], int axes, int reach)
 {
+    // (an axis that is not there reads places in LDS too, and adds nothing)
     float level[NC];
-    uint32_t kinds[kMaxBiasAxes];
+    int kind[kMaxBiasAxes];
 #pragma unroll
-    for (int n = 0; n < NC; ++n) level[n] = 0.0f;
+    for (int a = 0; a < kMaxBiasAxes; ++a) kind[a] = tile.kind_of(a, u);
 #pragma unroll
-    for (int a = 0; a < kMaxBiasAxes; ++a) {
-        if (a >= axes) break;
-        kinds[a] = __builtin_amdgcn_readfirstlane(tile.kind[a]);
-        if (kinds[a] >> (16 + u) & 1) {
-            const int p = tile.at[a][32 * u];
+    for (int n = 0; n < NC; ++n) {
+        float b[kMaxBiasAxes];
 #pragma unroll
-            for (int n = 0; n < NC; ++n)
-                level[n] += dense[base[n] + a * kReachRow + bias_at(p, column[n][a], reach)];
-        }
+        for (int a = 0; a < kMaxBiasAxes; ++a)
+            b[a] = dense[base[n] + a * kReachRow +
+                         bias_at(tile.at[a][32 * u], column[n][a], reach)];
+        level[n] = 0.0f;
+#pragma unroll
+        for (int a = 0; a < kMaxBiasAxes; ++a)
+            level[n] += a < axes && kind[a] == kLevel ? b[a] : 0.0f;
     }
 #pragma unroll
     for (int n = 0; n < NC; ++n)
@@ -450,33 +459,32 @@ __device__ __forceinline__ void add_bias(f32x16 (&s)[NC], float scale, const Til
 #pragma unroll
     for (int a = 0; a < kMaxBiasAxes; ++a) {
         if (a >= axes) break;
-        if (kinds[a] >> (16 + u) & 1) continue;
+        const int32_t *p = &tile.at[a][32 * u + 4 * half];
+        const float *row = dense + a * kReachRow;
+        if (kind[a] == kSteps) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int32_t *p = &tile.at[a][32 * u + 8 * j + 4 * half];
-            const float *row = dense + a * kReachRow;
-            const uint32_t bits = kinds[a] >> (4 * u + j);
-            if (bits >> 8 & 1) {
+            for (int n = 0; n < NC; ++n)
 #pragma unroll
-                for (int n = 0; n < NC; ++n) {
-                    const float *b = row + base[n] + bias_at(p[0], column[n][a], reach, kPad);
+                for (int j = 0; j < 4; ++j) {
+                    const float *b = row + base[n] + bias_at(p[8 * j], column[n][a], reach, kPad);
 #pragma unroll
                     for (int i = 0; i < 4; ++i) s[n][4 * j + i] += b[i];
                 }
-            } else if (bits & 1) {
+        } else if (kind[a] == kLevel8) {
 #pragma unroll
-                for (int n = 0; n < NC; ++n) {
-                    const float b = row[base[n] + bias_at(p[0], column[n][a], reach)];
+            for (int n = 0; n < NC; ++n)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float b = row[base[n] + bias_at(p[8 * j], column[n][a], reach)];
 #pragma unroll
                     for (int i = 0; i < 4; ++i) s[n][4 * j + i] += b;
                 }
-            } else {
+        } else if (kind[a] == kMixed) {
 #pragma unroll
-                for (int n = 0; n < NC; ++n)
+            for (int n = 0; n < NC; ++n)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        s[n][4 * j + i] += row[base[n] + bias_at(p[i], column[n][a], reach)];
-            }
+                for (int i = 0; i < 16; ++i)
+                    s[n][i] += row[base[n] + bias_at(p[tile_row(i, 0)], column[n][a], reach)];
         }
     }
 }
