@@ -59,8 +59,8 @@ struct AttendPlan {
 };
 
 // LDS of the queries' gradient for the bias table's: a place an entry, and one more,
-// of each lane.
-inline int attend_hist_bytes(int entries) { return 1024 * (entries + 1); }
+// of each of its 128 columns (or four waves' 32).
+inline int attend_hist_bytes(int entries) { return 512 * (entries + 1); }
 
 AttendPlan plan_attend(int B, int H, int Hk, int64_t Tq, int64_t Tk, int D, int dtype, int axes,
                        int entries);

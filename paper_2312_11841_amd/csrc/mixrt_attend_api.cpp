@@ -120,7 +120,7 @@ AttendPlan plan_attend_dq(int B, int H, int Hk, int64_t Tq, int64_t Tk, int D, i
     // (float32's products are so slow that a wave's second tile is worth a join)
     const int64_t blocks = heads * p.blocks, least = attend_elem(dtype) == 4 ? 128 : 256;
     const int64_t s = p.shared ? enough(Tk, blocks, least)
-                               : whole_rounds(Tk, blocks, resident(D, dtype, axes ? 1 : 3), 512);
+                               : whole_rounds(Tk, blocks, resident(D, dtype, axes ? 2 : 3), 512);
     divide(Tk, s, most, p.shared ? 128 : 32, &p.splits, &p.per);
     return p;
 }

@@ -132,10 +132,10 @@ struct Lift {
 };
 
 // mine[e[i]] += v[i], for four places some of which may be the same: the sums of equal
-// places go to the first, so that the four reads and writes need not wait for each
-// other.  (LDS has atomic adds in 32 bits, but they take 4 cycles a lane: with them
-// this kernel took 4.6 ms where it takes %s.)
-__device__ __forceinline__ void add_places(float *mine, int (&e)[4], float (&v)[4], int spare)
+// places go to the first (and the others to the spare place), so that the four reads and
+// writes need not wait for each other.  (LDS has atomic adds in 32 bits, but they take 4
+// cycles a lane: with them this kernel took 4.6 ms where it takes DQTIME.)
+__device__ __forceinline__ void join_places(int (&e)[4], float (&v)[4], int spare)
 {
     const bool b0 = e[1] == e[0];
     const bool c0 = e[2] == e[0], c1 = !c0 && e[2] == e[1];
@@ -150,11 +150,21 @@ __device__ __forceinline__ void add_places(float *mine, int (&e)[4], float (&v)[
     e[1] = b0 ? spare : e[1];
     e[2] = c0 || c1 ? spare : e[2];
     e[3] = d0 || d1 || d2 ? spare : e[3];
+}
+
+__device__ __forceinline__ void put_places(float *mine, const int (&e)[4], const float (&v)[4])
+{
     float a[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) a[i] = mine[e[i]];
 #pragma unroll
     for (int i = 0; i < 4; ++i) mine[e[i]] = a[i] + v[i];
+}
+
+__device__ __forceinline__ void add_places(float *mine, int (&e)[4], float (&v)[4], int spare)
+{
+    join_places(e, v, spare);
+    put_places(mine, e, v);
 }
 
 // Adds a column's dS to its places of the bias table's gradient.
@@ -165,13 +175,15 @@ __device__ __forceinline__ void add_table(const f32x16 &g, const TilePos<ROWS> &
                                           float *mine, int spare)
 {
     static_assert(ROWS == 32, "one block of rows");
-    float quad[4];
+    float quad[4];      // of the octet's rows, those of the other half too
     int kind[kMaxBiasAxes], at[kMaxBiasAxes];
 #pragma unroll
     for (int j = 0; j < 4; ++j)
-        quad[j] = (g[4 * j] + g[4 * j + 1]) + (g[4 * j + 2] + g[4 * j + 3]);
+        quad[j] = half_sum((g[4 * j] + g[4 * j + 1]) + (g[4 * j + 2] + g[4 * j + 3]));
+    // The two halves of a wave share a column's places: sums over both are added by one,
+    // single rows by one half after the other.
     // the axes on which all rows have one place, together: their places lie apart (the
-    // other axes add to the spare one)
+    // other axes, and the other half, add to the spare one)
 #pragma unroll
     for (int a = 0; a < kMaxBiasAxes; ++a) {
         kind[a] = tile.kind_of(a, 0);
@@ -180,7 +192,7 @@ __device__ __forceinline__ void add_table(const f32x16 &g, const TilePos<ROWS> &
     float old[kMaxBiasAxes];
 #pragma unroll
     for (int a = 0; a < kMaxBiasAxes; ++a) {
-        at[a] = a < axes && kind[a] == kLevel ? at[a] : spare;
+        at[a] = a < axes && kind[a] == kLevel && half == 0 ? at[a] : spare;
         old[a] = mine[at[a]];
     }
 #pragma unroll
@@ -200,7 +212,7 @@ __device__ __forceinline__ void add_table(const f32x16 &g, const TilePos<ROWS> &
                 e[j] = row[bias_at(p[8 * j], column[a], reach)];
                 v[j] = quad[j];
             }
-            add_places(mine, e, v, spare);
+            if (half == 0) add_places(mine, e, v, spare);
             continue;
         }
         int e[4][4];
@@ -221,13 +233,18 @@ __device__ __forceinline__ void add_table(const f32x16 &g, const TilePos<ROWS> &
 #pragma unroll
         for (int j = 0; j < 4; ++j)
             asm volatile("" : "+v"(e[j][0]), "+v"(e[j][1]), "+v"(e[j][2]), "+v"(e[j][3]));
+        float v[4][4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            float v[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = g[4 * j + i];
-            add_places(mine, e[j], v, spare);
+            for (int i = 0; i < 4; ++i) v[j][i] = g[4 * j + i];
+            join_places(e[j], v[j], spare);
         }
+#pragma unroll 1
+        for (int h = 0; h < 2; ++h)
+            if (half == h)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) put_places(mine, e[j], v[j]);
     }
 }
 
@@ -257,9 +274,9 @@ __global__ __launch_bounds__(256) void attend_dq_kernel(AttendK k)
     constexpr int BUFS = SHARED || (BIAS && sizeof(T) == 4 && DP == 128) ? 1 : 2;
     __shared__ __attribute__((aligned(16))) T tiles[WAVES][BUFS][2][TILE];
     __shared__ float dense[BIAS ? kMaxBiasAxes * kReachRow : 1];
-    __shared__ uint16_t place[BIAS ? kMaxBiasAxes * kReachRow : 1];   // 64 entry
+    __shared__ uint16_t place[BIAS ? kMaxBiasAxes * kReachRow : 1];   // 32 entry
     __shared__ TilePos<BIAS ? ROWS : 1> kpos[WAVES][BUFS];
-    extern __shared__ float hist[];     // [wave][entry, and a spare one][lane]
+    extern __shared__ float hist[];     // [wave][entry, and a spare one][column]
 
     const Team<SHARED> team;
     const int lane = team.lane, wave = team.wave, half = team.half;
@@ -326,11 +343,11 @@ __global__ __launch_bounds__(256) void attend_dq_kernel(AttendK k)
         for (int i = threadIdx.x; i < k.bias.axes * n; i += THREADS) {
             const int a = i / n, e = i - a * n;
             place[a * kReachRow + e] =
-                (uint16_t)(64 * (a * k.bias.buckets + bucket_of(k.bias, a, e, false)));
+                (uint16_t)(32 * (a * k.bias.buckets + bucket_of(k.bias, a, e, false)));
         }
-        for (int i = threadIdx.x; i < 4 * 64 * held; i += THREADS) hist[i] = 0.0f;
+        for (int i = threadIdx.x; i < 4 * 32 * held; i += THREADS) hist[i] = 0.0f;
     }
-    float *mine = hist + wave * 64 * held + lane;
+    float *mine = hist + wave * 32 * held + (lane & 31);
     double table = 0.0;         // thread e: entry e's sum of the block
 
     f32x16 acc[NC][DP / 32];
@@ -359,17 +376,17 @@ __global__ __launch_bounds__(256) void attend_dq_kernel(AttendK k)
     }
     if (SHARED && BIAS) __syncthreads();    // (the bias and hist are the block's)
     team.meet();
-    // each entry's places of all lanes; threads start at different lanes, as the same
-    // lane of all entries lies in one bank
+    // each entry's places of all columns; threads start at different columns, as the
+    // same column of all entries lies in one bank
     auto collect = [&]() {
         if ((int)threadIdx.x >= entries) return;
         float sum = 0.0f;
 #pragma unroll 1
         for (int w = 0; w < 4; ++w) {
-            float *at = hist + (w * held + threadIdx.x) * 64;
+            float *at = hist + (w * held + threadIdx.x) * 32;
 #pragma unroll 4
-            for (int i = 0; i < 64; ++i) {
-                const int l = (i + threadIdx.x) & 63;
+            for (int i = 0; i < 32; ++i) {
+                const int l = (i + threadIdx.x) & 31;
                 sum += at[l];
                 at[l] = 0.0f;
             }
@@ -411,7 +428,7 @@ __global__ __launch_bounds__(256) void attend_dq_kernel(AttendK k)
 #pragma unroll
             for (int n = 0; n < NC; ++n)
                 add_table<ROWS>(g[n], kpos[me][cur], half, place, qpos[n], k.bias.axes, k.bias.reach,
-                                mine, 64 * entries);
+                                mine, 32 * entries);
             counted += ROWS;
         }
         lift.scale(g, acc);
