@@ -5,6 +5,7 @@
 #include "mixrt.h"
 
 #include <cmath>
+#include <initializer_list>
 
 #include "mixrt_attend.hpp"
 #include "mixrt_ctx.hpp"
@@ -281,6 +282,16 @@ int check_sequence(mixrt_ctx *ctx, const mixrt_attention *a, const mixrt_sequenc
                 (long long)st[0], (long long)st[1], (long long)st[2]);
 }
 
+// An output is none of the inputs.
+int check_apart(mixrt_ctx *ctx, const mixrt_sequence *out, const char *name,
+                std::initializer_list<const mixrt_sequence *> inputs)
+{
+    for (const mixrt_sequence *s : inputs)
+        if (out->data && out->data == s->data)
+            return fail(ctx, MIXRT_EINVAL, "%s is also another array", name);
+    return MIXRT_OK;
+}
+
 size_t round16(size_t n) { return (n + 15) / 16 * 16; }
 
 // Where a call's scratch lies in its workspace; total bytes.
@@ -530,6 +541,7 @@ int mixrt_attention_forward(mixrt_ctx *ctx, const mixrt_attention *att,
         (rc = check_sequence(ctx, att, v, false, "v", false)) ||
         (rc = check_sequence(ctx, att, out, true, "out", true)))
         return rc;
+    if (att->batch && att->queries && (rc = check_apart(ctx, out, "out", {q, k, v}))) return rc;
     if (!aligned(lse, 4)) return fail(ctx, MIXRT_EINVAL, "lse not 4-byte aligned");
     if (rest && att->dtype == MIXRT_F32) return fail(ctx, MIXRT_EINVAL, "rest for F32");
     if (!aligned(rest, 2)) return fail(ctx, MIXRT_EINVAL, "rest not aligned to its element");
@@ -571,6 +583,11 @@ int mixrt_attention_backward(mixrt_ctx *ctx, const mixrt_attention *att,
         (rc = check_sequence(ctx, att, dq, true, "dq", true)) ||
         (rc = check_sequence(ctx, att, dk, false, "dk", true)) ||
         (rc = check_sequence(ctx, att, dv, false, "dv", true)))
+        return rc;
+    if (att->batch &&
+        ((att->queries && (rc = check_apart(ctx, dq, "dq", {dout, q, k, v, out, dk, dv}))) ||
+         (att->keys && ((rc = check_apart(ctx, dk, "dk", {dout, q, k, v, out, dv})) ||
+                        (rc = check_apart(ctx, dv, "dv", {dout, q, k, v, out}))))))
         return rc;
     if (dtable && !bias) return fail(ctx, MIXRT_EINVAL, "dtable without a bias");
     if (!aligned(lse, 4) || !aligned(dtable, 4))

@@ -1322,6 +1322,7 @@ class Renderer:
         and out as in rotary; weights: a float32 [D] (or None) for each array of
         heads, likewise one or a tuple, or None for none."""
         single, arrays, weights = self._as_arrays(heads, weights)
+        eps = float(eps)
         key = self._normed_key("rotary_norm", arrays, (), weights, pos, freq, axis, layout)
         if out is None:
             here = self._here()
@@ -1357,6 +1358,7 @@ class Renderer:
         The other arguments as rotary_norm had them; out: where dheads go (grads
         themselves will do)."""
         single, arrays, weights = self._as_arrays(heads, weights)
+        eps = float(eps)
         grads = (grads,) if single else tuple(grads)
         if len(grads) != len(arrays):
             raise ValueError(f"{len(arrays)} arrays and {len(grads)} gradients")
@@ -1411,6 +1413,9 @@ class Renderer:
     def _attention_plan(self, q, k, v, lens, bias, scale, backward: bool):
         """The plan of a call over q, k and v, with their addresses, the lengths'
         and the bias' filled in."""
+        # (a tensor in the key would be known by its identity)
+        if scale is not None and type(scale) is not float:
+            scale = float(scale)
         try:
             key = ("attention", backward, scale, q.shape, q.stride(), q.dtype, q.get_device(),
                    k.shape, k.stride(), k.dtype, k.get_device(),
@@ -1454,7 +1459,7 @@ class Renderer:
                 raise ValueError(f"lens: {lens.dtype} {tuple(lens.shape)}, expected contiguous "
                                  f"int32 ({B},)")
         p.att = Attention(B, H, Hk, D, _elem_code(q.dtype, "q"),
-                          1.0 / D ** 0.5 if scale is None else float(scale), Tq, Tk, 0)
+                          1.0 / D ** 0.5 if scale is None else scale, Tq, Tk, 0)
         p.bias = None if bias is None else _bias_desc(bias, B, Tq, Tk, H, self.device)
         p.att_ref = C.byref(p.att)
         p.bias_ref = None if bias is None else C.byref(p.bias)
@@ -1505,8 +1510,10 @@ class Renderer:
         return out
 
     def attention_train(self, q, k, v, *, lens=None, bias=None, scale=None, out=None):
-        """(out, saved) for a training step: out as attention gives it, and what
-        attention_backward needs besides (an AttentionSaved)."""
+        """(out, saved) for a training step: attention's out, whose weights float16
+        and bfloat16 hold here to twice their bits (a row that looks at few keys
+        would else get the roundings as its gradient), and what attention_backward
+        needs besides (an AttentionSaved)."""
         p = self._attention_plan(q, k, v, lens, bias, scale, False)
         table = None if bias is None else bias.table
         if out is not None:
@@ -1517,7 +1524,7 @@ class Renderer:
                 else self._empty(p.q_shape, q.dtype, here))
         out = self._attend(p, q, out, lse, rest, here)
         if self._follows(q, k, v, table):
-            out = self._result("attention_train", (out,), (q, k, v, table))[0]
+            out, lse = self._result("attention_train", (out, lse), (q, k, v, table))
         return out, AttentionSaved(lse, rest)
 
     def attention_backward(self, dout, q, k, v, out, saved: AttentionSaved, *, lens=None,
@@ -1557,7 +1564,7 @@ class Renderer:
         if rc:
             self._check(rc)
         grads = (dq, dk, dv) if bias is None else (dq, dk, dv, dtable)
-        inputs = (dout, q, k, v, out, table)
+        inputs = (dout, q, k, v, out, lse, table)
         if self._follows(*inputs):
             grads = tuple(self._result("attention_backward", grads, inputs))
         return grads
