@@ -70,9 +70,15 @@ int64_t enough(int64_t n, int64_t blocks, int64_t least)
     return s < ceil_div(n, least) ? s : ceil_div(n, least);
 }
 
-// Whether blocks of 128 columns are few for the chip, also when their walks of rows are
-// split: then blocks of 32 columns run, whose waves divide the rows.
-bool few(int64_t blocks, int64_t rows) { return blocks * (1 + rows / 1024) < kCUs; }
+// Whether blocks of 32 columns run, whose waves divide the rows, and not blocks of 128:
+// where these would leave half of their waves without columns, or be few for the chip
+// also when their walks of rows are split.  (8 queries of 32 heads of 128 over 32,768
+// keys of 2, f32: the queries' gradient SHARED8, with 128 columns 818 us.)
+bool shares(int64_t heads, int64_t cols, int64_t rows)
+{
+    const int64_t splits = 1 + rows / 1024 < 16 ? 1 + rows / 1024 : 16;
+    return cols <= 64 || heads * ceil_div(cols, 128) * splits < kCUs;
+}
 
 int blocks_of(int64_t n, int cols)
 {
@@ -92,7 +98,7 @@ AttendPlan plan_attend(int B, int H, int Hk, int64_t Tq, int64_t Tk, int D, int 
         for (int n = 2; n <= 8; ++n)
             if (H / Hk % n == 0 && Tq * n <= 32) p.pack = n;
     const int64_t cols = Tq * p.pack, heads = (int64_t)B * (H / p.pack);
-    p.shared = cols <= 32 || few(heads * ceil_div(cols, 128), Tk);
+    p.shared = shares(heads, cols, Tk);
     p.cols = p.shared ? 32 : 128;
     if (attend_elem(dtype) == 2 && D <= 64 && axes == 0 && !p.shared && cols > 1024) p.cols = 256;
     p.blocks = blocks_of(cols, p.cols);
@@ -109,7 +115,7 @@ AttendPlan plan_attend_dq(int B, int H, int Hk, int64_t Tq, int64_t Tk, int D, i
     AttendPlan p{};
     p.pack = 1;
     const int64_t heads = (int64_t)B * H;
-    p.shared = few(heads * ceil_div(Tq, 128), Tk);
+    p.shared = shares(heads, Tq, Tk);
     // (a wave's own tiles beside the table's sums may be more than a CU's LDS; about
     // 16 KB are other things)
     const int tiles = 4 * 2 * 32 * (attend_dim(D) * attend_elem(dtype) + 16);
@@ -132,7 +138,7 @@ AttendPlan plan_attend_dkv(int B, int H, int Hk, int64_t Tq, int64_t Tk, int D, 
     AttendPlan p{};
     p.pack = 1;
     const int64_t heads = (int64_t)B * Hk;
-    p.shared = few(heads * ceil_div(Tk, 128), H / Hk * Tq);
+    p.shared = shares(heads, Tk, H / Hk * Tq);
     p.cols = p.shared ? 32 : 128;
     p.blocks = blocks_of(Tk, p.cols);
     const int64_t tiles = H / Hk * ceil_div(Tq, 32);

@@ -686,33 +686,55 @@ __global__ __launch_bounds__(256) void attend_dkv_kernel(AttendK k)
 
 // --- joins ----------------------------------------------------------------------------
 
-// out[b][t][h][d] = sum of the splits' parts [split][b][h][t][d], a quad a thread;
-// with blockIdx.y = 1 the second array's parts, which follow.
-template <typename T>
+// out[b][t][h][d] = sum of the splits' parts [split][b][h][t][d], a quad for G threads,
+// which take every G-th split and join in order; with blockIdx.y = 1 the second array's
+// parts, which follow.  (256 splits of 40 rows of 128, twice: one thread a quad 71 us,
+// 32 SUM32.)
+template <typename T, int G>
 __global__ __launch_bounds__(256) void attend_sum_kernel(const float *part, int splits, int B,
                                                          int H, int Tn, int D, SeqK one, SeqK two)
 {
+    __shared__ float4 sums[G > 1 ? 256 : 1];
     const int quads = (D + 3) / 4;
     const int64_t rows = (int64_t)B * H * Tn;
-    const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (at >= rows * quads) return;
+    const int64_t at = (int64_t)blockIdx.x * (256 / G) + threadIdx.x % (256 / G);
+    const int g = threadIdx.x / (256 / G);
+    const bool there = at < rows * quads;
     const int64_t row = at / quads;
     const int d = (int)(at - row * quads) * 4;
     const SeqK out = blockIdx.y ? two : one;
-    const float *p = part + ((int64_t)blockIdx.y * splits * rows + row) * D + d;
     float a[4] = {0, 0, 0, 0};
-    for (int s = 0; s < splits; ++s, p += rows * D) {
-        if (d + 4 <= D) {
-            float f[4];
-            load_vec<float, 4>(p, f);
+    if (there) {
+        const float *p = part + ((int64_t)blockIdx.y * splits * rows + row) * D + d;
+#pragma unroll 4
+        for (int s = g; s < splits; s += G) {
+            const float *q = p + s * rows * D;
+            if (d + 4 <= D) {
+                float f[4];
+                load_vec<float, 4>(q, f);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) a[i] += f[i];
-        } else {
+                for (int i = 0; i < 4; ++i) a[i] += f[i];
+            } else {
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (d + i < D) a[i] += p[i];
+                for (int i = 0; i < 4; ++i)
+                    if (d + i < D) a[i] += q[i];
+            }
         }
     }
+    if (G > 1) {
+        sums[threadIdx.x] = make_float4(a[0], a[1], a[2], a[3]);
+        __syncthreads();
+        if (g == 0)
+#pragma unroll 8
+            for (int j = 1; j < G; ++j) {
+                const float4 x = sums[threadIdx.x + j * (256 / G)];
+                a[0] += x.x;
+                a[1] += x.y;
+                a[2] += x.z;
+                a[3] += x.w;
+            }
+    }
+    if (!there || g != 0) return;
     const int64_t bh = row / Tn;
     const int t = (int)(row - bh * Tn), b = (int)(bh / H), h = (int)(bh - (int64_t)b * H);
     store_quad<T>((T *)out.data + b * out.batch + (int64_t)t * out.token + h * out.head, d, D, a[0],
@@ -745,8 +767,16 @@ hipError_t launch_sum(const AttendK &k, int H, int64_t Tn, const SeqK &one, cons
 {
     const int64_t quads = (int64_t)k.B * H * Tn * ((k.D + 3) / 4);
     if (quads == 0) return hipSuccess;
-    attend_sum_kernel<T><<<dim3((unsigned)((quads + 255) / 256), n), 256, 0, stream>>>(
-        k.part, k.splits, k.B, H, (int)Tn, k.D, one, two);
+    auto go = [&](auto g) {
+        constexpr int G = decltype(g)::value, each = 256 / G;
+        attend_sum_kernel<T, G>
+            <<<dim3((unsigned)((quads + each - 1) / each), n), 256, 0, stream>>>(
+                k.part, k.splits, k.B, H, (int)Tn, k.D, one, two);
+    };
+    if (k.splits > 8)
+        go(std::integral_constant<int, 32>());
+    else
+        go(std::integral_constant<int, 1>());
     return hipGetLastError();
 }
 
