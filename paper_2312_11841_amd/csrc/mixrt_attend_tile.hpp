@@ -148,6 +148,7 @@ __device__ __forceinline__ typename Matrix<T>::frag left_rows(const f32x16 &p,
                                                               typename Matrix<T>::frag f, int s)
 {
     typename Matrix<T>::frag g;
+    asm("" : "+v"(f));      // (taken from the pairs, not rounded once more one by one)
 #pragma unroll
     for (int i = 0; i < 8; ++i) g[i] = (T)(p[8 * s + i] - (float)f[i]);
     return g;
@@ -197,13 +198,15 @@ struct Stage {
                                           int limit, int D)
     {
         if (kEven && D == DP && first + ROWS <= limit) {    // nothing to leave out
+            // (the tile's place is the same for all threads, a thread's place in it for
+            // all tiles)
+            const char *tile = (const char *)(base + (int64_t)first * stride);
 #pragma unroll
             for (int j = 0; j < kEach; ++j) {
                 const int at = thread + j * THREADS;
+                const int64_t off = (int64_t)(at / kChunks) * stride + at % kChunks * kChunk<T>;
                 r[j] = __builtin_bit_cast(
-                    u32x4, *(const Pack<T, kChunk<T>> *)(base + (int64_t)(first + at / kChunks) *
-                                                                    stride +
-                                                         at % kChunks * kChunk<T>));
+                    u32x4, *(const Pack<T, kChunk<T>> *)(tile + off * (int64_t)sizeof(T)));
             }
             return;
         }
