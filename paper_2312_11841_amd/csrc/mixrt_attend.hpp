@@ -49,8 +49,8 @@ struct AttendK {
 
 // How a call is dealt.  Forward: a block takes cols columns (a column is a token and
 // one of pack heads that share their keys) and per keys; queries' gradient: likewise,
-// pack 1; keys' gradient: a block takes cols keys and per tiles of 32 rows (the heads of
-// a group one after another).
+// pack 1; keys' gradient: a block takes cols keys and per tiles of attend_kv_rows
+// (the heads of a group one after another).
 struct AttendPlan {
     int shared;               // a block's waves share 32 columns and divide the rows
     int pack;
@@ -78,5 +78,14 @@ enum { kAttendForward, kAttendBackQ, kAttendBackKV };
 inline int attend_elem(int dtype) { return dtype == 0 ? 4 : 2; }
 // Head widths the kernels are built for: multiples of 32.
 inline int attend_dim(int D) { return D <= 32 ? 32 : D <= 64 ? 64 : D <= 96 ? 96 : 128; }
+
+// Rows of a tile of the keys' gradient: 64 where two blocks of them still fit a CU's
+// registers (two 720p views with two reference views each, 12 and 3 heads of 64, bf16:
+// 399 us, with 32 rows 424; the queries' gradient, whose blocks are smaller, takes 303
+// with 32 and 330 with 64).
+constexpr int attend_kv_rows(int dim, int elem, bool shared)
+{
+    return !shared && elem == 2 && dim <= 64 ? 64 : 32;
+}
 
 }  // namespace mixrt

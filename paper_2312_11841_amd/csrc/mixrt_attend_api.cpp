@@ -141,11 +141,12 @@ AttendPlan plan_attend_dkv(int B, int H, int Hk, int64_t Tq, int64_t Tk, int D, 
     p.shared = shares(heads, Tk, H / Hk * Tq);
     p.cols = p.shared ? 32 : 128;
     p.blocks = blocks_of(Tk, p.cols);
-    const int64_t tiles = H / Hk * ceil_div(Tq, 32);
+    const int rows = attend_kv_rows(attend_dim(D), attend_elem(dtype), p.shared);
+    const int64_t tiles = H / Hk * ceil_div(Tq, rows);
     const int64_t blocks = heads * p.blocks;
     const int64_t s = p.shared ? enough(tiles, blocks, 8)
-                               : whole_rounds(tiles, blocks, resident(D, dtype, 2), 16);
-    divide(tiles, s, longest(dtype) / 32, p.shared ? 4 : 1, &p.splits, &p.per);
+                               : whole_rounds(tiles, blocks, resident(D, dtype, 2), 512 / rows);
+    divide(tiles, s, longest(dtype) / rows, p.shared ? 4 : 1, &p.splits, &p.per);
     return p;
 }
 

@@ -169,12 +169,12 @@ __device__ __forceinline__ void add_places(float *mine, int (&e)[4], float (&v)[
 
 // Adds a column's dS to its places of the bias table's gradient.
 template <int ROWS>
-__device__ __forceinline__ void add_table(const f32x16 &g, const TilePos<ROWS> &tile, int half,
+__device__ __forceinline__ void add_table(const f32x16 &g, const TilePos<ROWS> &tile, int u,
+                                          int half,
                                           const uint16_t *place,
                                           const int (&column)[kMaxBiasAxes], int axes, int reach,
                                           float *mine, int spare)
 {
-    static_assert(ROWS == 32, "one block of rows");
     float quad[4];      // of the octet's rows, those of the other half too
     int kind[kMaxBiasAxes], at[kMaxBiasAxes];
 #pragma unroll
@@ -186,8 +186,8 @@ __device__ __forceinline__ void add_table(const f32x16 &g, const TilePos<ROWS> &
     // other axes, and the other half, add to the spare one)
 #pragma unroll
     for (int a = 0; a < kMaxBiasAxes; ++a) {
-        kind[a] = tile.kind_of(a, 0);
-        at[a] = place[a * kReachRow + bias_at(tile.at[a][0], column[a], reach)];
+        kind[a] = tile.kind_of(a, u);
+        at[a] = place[a * kReachRow + bias_at(tile.at[a][32 * u], column[a], reach)];
     }
     float old[kMaxBiasAxes];
 #pragma unroll
@@ -203,7 +203,7 @@ __device__ __forceinline__ void add_table(const f32x16 &g, const TilePos<ROWS> &
         if (a >= axes) break;
         if (kind[a] == kLevel) continue;
         const uint16_t *row = place + a * kReachRow;
-        const int32_t *p = &tile.at[a][4 * half];
+        const int32_t *p = &tile.at[a][32 * u + 4 * half];
         if (kind[a] == kLevel8) {
             int e[4];
             float v[4];
@@ -359,14 +359,20 @@ __global__ __launch_bounds__(256) void attend_dq_kernel(AttendK k)
     const int32_t *pp = BIAS ? k.bias.kpos + b * k.bias.kbatch : nullptr;
     Stage<T, DP, ROWS, Team<SHARED>::kStagers> sk, sv;
     StagePos<BIAS ? ROWS : 1> sp;
+    // (all fetched and then put, or one array after the other)
+    constexpr bool AHEAD = !SHARED || kFetchAhead<T, DP>;
     auto fetch = [&](int row) {
         sk.fetch(stager, kp, k.k.token, row, last, k.D);
+        if (!AHEAD) sk.put(stager, tiles[me][0][0]);
         sv.fetch(stager, vp, k.v.token, row, last, k.D);
+        if (!AHEAD) sv.put(stager, tiles[me][0][1]);
         if (BIAS) sp.fetch(stager, pp, k.bias.axes, row, last);
     };
     auto put = [&](int to) {
-        sk.put(stager, tiles[me][to][0]);
-        sv.put(stager, tiles[me][to][1]);
+        if (AHEAD) {
+            sk.put(stager, tiles[me][to][0]);
+            sv.put(stager, tiles[me][to][1]);
+        }
         if (BIAS) sp.put(stager, kpos[me][to], k.bias.axes);
     };
     const int row1 = first + me * ROWS;
@@ -396,7 +402,7 @@ __global__ __launch_bounds__(256) void attend_dq_kernel(AttendK k)
     int cur = 0, counted = 0;
     for (int row0 = row1; row0 < last; row0 += STEP, cur ^= BUFS - 1) {
         const bool more = row0 + STEP < last;
-        if (more && (!SHARED || kAhead<T, DP>)) fetch(row0 + STEP);
+        if (more && AHEAD) fetch(row0 + STEP);
         const T *kt = tiles[me][cur][0], *vt = tiles[me][cur][1];
         f32x16 s[NC], g[NC];
 #pragma unroll
@@ -427,15 +433,15 @@ __global__ __launch_bounds__(256) void attend_dq_kernel(AttendK k)
         if constexpr (BIAS) {
 #pragma unroll
             for (int n = 0; n < NC; ++n)
-                add_table<ROWS>(g[n], kpos[me][cur], half, place, qpos[n], k.bias.axes, k.bias.reach,
+                add_table<ROWS>(g[n], kpos[me][cur], 0, half, place, qpos[n], k.bias.axes, k.bias.reach,
                                 mine, 32 * entries);
-            counted += ROWS;
         }
         lift.scale(g, acc);
         add_cols<T, DP, NC>(kt, lane, g, acc);
+        counted += ROWS;
         if (BUFS == 1) team.meet();
         if (more) {
-            if (SHARED && !kAhead<T, DP>) fetch(row0 + STEP);
+            if (!AHEAD) fetch(row0 + STEP);
             put(cur ^ (BUFS - 1));
         }
         team.meet();
@@ -510,7 +516,8 @@ __global__ __launch_bounds__(256) void attend_dkv_kernel(AttendK k)
 {
     typedef typename Matrix<T>::frag frag;
     static_assert(!SHARED || NC == 1, "waves share 32 columns");
-    constexpr int ROWS = 32, WAVES = SHARED ? 4 : 1, BUFS = SHARED ? 1 : 2;
+    constexpr int ROWS = attend_kv_rows(DP, sizeof(T), SHARED);
+    constexpr int WAVES = SHARED ? 4 : 1, BUFS = SHARED ? 1 : 2;
     constexpr int TILE = ROWS * kStride<T, DP>, STEP = Team<SHARED>::kStep;
     __shared__ __attribute__((aligned(16))) T tiles[WAVES][BUFS][2][TILE];
     __shared__ float dense[WAVES][BIAS ? kMaxBiasAxes * kReachRow : 1];
@@ -567,18 +574,25 @@ __global__ __launch_bounds__(256) void attend_dkv_kernel(AttendK k)
     Stage<T, DP, ROWS, Team<SHARED>::kStagers> sq, sg;
     StagePos<BIAS ? ROWS : 1> sp;
     StageSums<ROWS> ss;
-    auto fetch = [&](int i) {       // tile i: a head of the group, its rows
+    // tile i: a head of the group, its rows; all fetched and then put, or one array
+    // after the other
+    constexpr bool AHEAD = !SHARED || kFetchAhead<T, DP>;
+    auto fetch = [&](int i) {
         const int g = i / a_head, row = (i - g * a_head) * ROWS;
         const int h = kvh * G + g;
         sq.fetch(stager, qp + h * k.q.head, k.q.token, row, k.Tq, k.D);
+        if (!AHEAD) sq.put(stager, tiles[me][0][0]);
         sg.fetch(stager, gp + h * k.dout.head, k.dout.token, row, k.Tq, k.D);
+        if (!AHEAD) sg.put(stager, tiles[me][0][1]);
         const int64_t at = sums0 + (int64_t)h * k.Tq;
         ss.fetch(stager, k.lse + at, k.delta + at, row, k.Tq, kWeightLift<T>);
         if (BIAS) sp.fetch(stager, pp, k.bias.axes, row, k.Tq);
     };
     auto put = [&](int to) {
-        sq.put(stager, tiles[me][to][0]);
-        sg.put(stager, tiles[me][to][1]);
+        if (AHEAD) {
+            sq.put(stager, tiles[me][to][0]);
+            sg.put(stager, tiles[me][to][1]);
+        }
         ss.put(stager, sums[me][to]);
         if (BIAS) sp.put(stager, qpos[me][to], k.bias.axes);
     };
@@ -592,7 +606,7 @@ __global__ __launch_bounds__(256) void attend_dkv_kernel(AttendK k)
     int cur = 0;
     for (int i0 = first1; i0 < last; i0 += STEP, cur ^= BUFS - 1) {
         const bool more = i0 + STEP < last;
-        if (more && (!SHARED || kAhead<T, DP>)) fetch(i0 + STEP);
+        if (more && AHEAD) fetch(i0 + STEP);
         if (BIAS && head != i0 / a_head) {      // (the same for all that share it)
             head = i0 / a_head;
             // (mirrored: the rows are queries here)
@@ -600,35 +614,39 @@ __global__ __launch_bounds__(256) void attend_dkv_kernel(AttendK k)
                       true);
             team.meet();
         }
-        const T *qt = tiles[me][cur][0], *gt = tiles[me][cur][1];
-        const float *sm = sums[me][cur];
-        f32x16 p[NC], g[NC];
 #pragma unroll
-        for (int n = 0; n < NC; ++n)
+        for (int u = 0; u < ROWS / 32; ++u) {
+            const T *qt = tiles[me][cur][0] + u * 32 * kStride<T, DP>;
+            const T *gt = tiles[me][cur][1] + u * 32 * kStride<T, DP>;
+            const float *sm = sums[me][cur] + 32 * u;
+            f32x16 p[NC], g[NC];
 #pragma unroll
-            for (int i = 0; i < 16; ++i) p[n][i] = g[n][i] = 0.0f;
-        pair_mul<T, DP, NC>(qt, gt, lane, key, val, p, g);
-        if constexpr (BIAS) {
-            const int base[NC] = {};
-            add_bias<NC, ROWS>(p, k.scale, qpos[me][cur], 0, half, dense[me], base, kpos,
-                               k.bias.axes, k.bias.reach);
-        }
-        const float unit = BIAS ? 1.0f : k.scale;
+            for (int n = 0; n < NC; ++n)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const float lse = sm[tile_row(i, half)], delta = sm[ROWS + tile_row(i, half)];
-#pragma unroll
-            for (int n = 0; n < NC; ++n) {
-                p[n][i] = __builtin_amdgcn_exp2f(fmaf(p[n][i], unit, -lse));
-                g[n][i] = p[n][i] * (g[n][i] - delta);
+                for (int i = 0; i < 16; ++i) p[n][i] = g[n][i] = 0.0f;
+            pair_mul<T, DP, NC>(qt, gt, lane, key, val, p, g);
+            if constexpr (BIAS) {
+                const int base[NC] = {};
+                add_bias<NC, ROWS>(p, k.scale, qpos[me][cur], u, half, dense[me], base, kpos,
+                                   k.bias.axes, k.bias.reach);
             }
+            const float unit = BIAS ? 1.0f : k.scale;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const float lse = sm[tile_row(i, half)], delta = sm[ROWS + tile_row(i, half)];
+#pragma unroll
+                for (int n = 0; n < NC; ++n) {
+                    p[n][i] = __builtin_amdgcn_exp2f(fmaf(p[n][i], unit, -lse));
+                    g[n][i] = p[n][i] * (g[n][i] - delta);
+                }
+            }
+            add_cols<T, DP, NC>(gt, lane, p, dv);
+            lift.scale(g, dk);
+            add_cols<T, DP, NC>(qt, lane, g, dk);
         }
-        add_cols<T, DP, NC>(gt, lane, p, dv);
-        lift.scale(g, dk);
-        add_cols<T, DP, NC>(qt, lane, g, dk);
         if (BUFS == 1) team.meet();
         if (more) {
-            if (SHARED && !kAhead<T, DP>) fetch(i0 + STEP);
+            if (!AHEAD) fetch(i0 + STEP);
             put(cur ^ (BUFS - 1));
         }
         team.meet();

@@ -237,14 +237,20 @@ __global__ __launch_bounds__(256) void attend_kernel(AttendK k)
     const int32_t *pp = BIAS ? k.bias.kpos + w.b * k.bias.kbatch : nullptr;
     Stage<T, DP, ROWS, Team<SHARED>::kStagers> sk, sv;
     StagePos<BIAS ? ROWS : 1> sp;
+    // (all fetched and then put, or one array after the other)
+    constexpr bool AHEAD = !SHARED || kFetchAhead<T, DP>;
     auto fetch = [&](int row) {
         sk.fetch(stager, kp, k.k.token, row, w.last, k.D);
+        if (!AHEAD) sk.put(stager, tiles[me][0][0]);
         sv.fetch(stager, vp, k.v.token, row, w.last, k.D);
+        if (!AHEAD) sv.put(stager, tiles[me][0][1]);
         if (BIAS) sp.fetch(stager, pp, k.bias.axes, row, w.last);
     };
     auto put = [&](int to) {
-        sk.put(stager, tiles[me][to][0]);
-        sv.put(stager, tiles[me][to][1]);
+        if (AHEAD) {
+            sk.put(stager, tiles[me][to][0]);
+            sv.put(stager, tiles[me][to][1]);
+        }
         if (BIAS) sp.put(stager, kpos[me][to], k.bias.axes);
     };
     const int row1 = w.first + me * ROWS;
@@ -272,7 +278,7 @@ __global__ __launch_bounds__(256) void attend_kernel(AttendK k)
     int cur = 0;
     for (int row0 = row1; row0 < w.last; row0 += STEP, cur ^= BUFS - 1) {
         const bool more = row0 + STEP < w.last;
-        if (more && (!SHARED || kAhead<T, DP>)) fetch(row0 + STEP);
+        if (more && AHEAD) fetch(row0 + STEP);
         const T *kt = tiles[me][cur][0], *vt = tiles[me][cur][1];
         f32x16 s[NC] = {row_mul<T, DP>(kt, lane, q[0])};
         if constexpr (BIAS)
@@ -301,7 +307,7 @@ __global__ __launch_bounds__(256) void attend_kernel(AttendK k)
         }
         if (more) {
             if (SHARED) team.meet();
-            if (SHARED && !kAhead<T, DP>) fetch(row0 + STEP);
+            if (!AHEAD) fetch(row0 + STEP);
             put(cur ^ (BUFS - 1));
         }
         team.meet();

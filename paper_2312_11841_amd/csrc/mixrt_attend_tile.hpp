@@ -259,7 +259,7 @@ struct Team {
 };
 
 // Whether a wave that stages alone has registers to fetch a tile ahead.
-template <typename T, int DP> inline constexpr bool kAhead = DP * sizeof(T) <= 256;
+template <typename T, int DP> inline constexpr bool kFetchAhead = DP * sizeof(T) <= 256;
 
 // Joins the sums of four waves that share their columns: a lane gets DP / 8 of its
 // column's, from d = (2 wave + half) DP / 8 on.  room: 128 DP floats.
