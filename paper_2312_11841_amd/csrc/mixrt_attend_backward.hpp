@@ -51,20 +51,27 @@ template <typename T, int DP, int NC>
 __device__ __forceinline__ void pair_mul(const T *a, const T *e, int lane,
                                          const typename Matrix<T>::frag (&b)[NC][(kPairs<T, DP>)],
                                          const typename Matrix<T>::frag (&f)[NC][(kPairs<T, DP>)],
-                                         f32x16 (&s)[NC], f32x16 (&g)[NC])
+                                         f32x16 (&s)[NC], f32x16 (&g)[NC], int D)
 {
     constexpr bool FIRST = sizeof(T) == 2 && DP <= 64;
     typename Matrix<T>::frag x[kPairs<T, DP>], y[kPairs<T, DP>];
+    if (FIRST) {
 #pragma unroll
-    for (int c = 0; c < kPairs<T, DP>; ++c) {
-        x[c] = row_frag<T, DP>(a, lane, c);
-        y[c] = row_frag<T, DP>(e, lane, c);
+        for (int c = 0; c < kPairs<T, DP>; ++c) {
+            x[c] = row_frag<T, DP>(a, lane, c);
+            y[c] = row_frag<T, DP>(e, lane, c);
+        }
+        __builtin_amdgcn_sched_barrier(0);
     }
-    if (FIRST) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int c = 0; c < kPairs<T, DP>; ++c)
 #pragma unroll
         for (int n = 0; n < NC; ++n) {
+            if (DP < 128 && past<T>(c, D)) continue; // at 128 its branches cost registers
+            if (!FIRST) {
+                x[c] = row_frag<T, DP>(a, lane, c);
+                y[c] = row_frag<T, DP>(e, lane, c);
+            }
             s[n] = Matrix<T>::mul(x[c], b[n][c], s[n]);
             g[n] = Matrix<T>::mul(y[c], f[n][c], g[n]);
         }
@@ -409,7 +416,7 @@ __global__ __launch_bounds__(256) void attend_dq_kernel(AttendK k)
         for (int n = 0; n < NC; ++n)
 #pragma unroll
             for (int i = 0; i < 16; ++i) s[n][i] = g[n][i] = 0.0f;
-        pair_mul<T, DP, NC>(kt, vt, lane, q, dout, s, g);
+        pair_mul<T, DP, NC>(kt, vt, lane, q, dout, s, g, k.D);
         if constexpr (BIAS) {
             const int base[NC] = {};
             add_bias<NC, ROWS>(s, k.scale, kpos[me][cur], 0, half, dense, base, qpos, k.bias.axes,
@@ -624,7 +631,7 @@ __global__ __launch_bounds__(256) void attend_dkv_kernel(AttendK k)
             for (int n = 0; n < NC; ++n)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) p[n][i] = g[n][i] = 0.0f;
-            pair_mul<T, DP, NC>(qt, gt, lane, key, val, p, g);
+            pair_mul<T, DP, NC>(qt, gt, lane, key, val, p, g, k.D);
             if constexpr (BIAS) {
                 const int base[NC] = {};
                 add_bias<NC, ROWS>(p, k.scale, qpos[me][cur], u, half, dense[me], base, kpos,

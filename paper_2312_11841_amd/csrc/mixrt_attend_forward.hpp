@@ -280,7 +280,7 @@ __global__ __launch_bounds__(256) void attend_kernel(AttendK k)
         const bool more = row0 + STEP < w.last;
         if (more && AHEAD) fetch(row0 + STEP);
         const T *kt = tiles[me][cur][0], *vt = tiles[me][cur][1];
-        f32x16 s[NC] = {row_mul<T, DP>(kt, lane, q[0])};
+        f32x16 s[NC] = {row_mul<T, DP>(kt, lane, q[0], k.D)};
         if constexpr (BIAS)
             add_bias<NC, ROWS>(s, k.scale, kpos[me][cur], 0, half, dense, hbase, qpos,
                                k.bias.axes, k.bias.reach);
@@ -390,7 +390,7 @@ __global__ __launch_bounds__(256, kFlowWaves<DP>) void attend_flow_kernel(Attend
     __syncthreads();
     if (w.first < w.last)
 #pragma unroll
-        for (int n = 0; n < NC; ++n) s[n] = row_mul<T, DP>(ktiles[0], lane, q[n]);
+        for (int n = 0; n < NC; ++n) s[n] = row_mul<T, DP>(ktiles[0], lane, q[n], k.D);
 
     // acc += values of 32 rows, at weights p
     auto add_values = [&](const T *v) {
@@ -446,7 +446,7 @@ __global__ __launch_bounds__(256, kFlowWaves<DP>) void attend_flow_kernel(Attend
             const T *next = u + 1 < SUBS ? ktiles[k0] + 32 * (u + 1) * kStride<T, DP> : ktiles[k1];
             f32x16 s2[NC];
 #pragma unroll
-            for (int n = 0; n < NC; ++n) s2[n] = row_mul<T, DP>(next, lane, q[n]);
+            for (int n = 0; n < NC; ++n) s2[n] = row_mul<T, DP>(next, lane, q[n], k.D);
             add_values(held);
 #pragma unroll
             for (int n = 0; n < NC; ++n) {

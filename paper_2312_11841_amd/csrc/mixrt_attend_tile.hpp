@@ -81,6 +81,14 @@ template <> struct Matrix<float> {
 // Chunk pairs of a padded head: operands of one mul each.
 template <typename T, int DP> inline constexpr int kPairs = DP / (2 * kChunk<T>);
 
+// Whether chunk pair c is padding alone: float32's products, four of 64 cycles a pair,
+// leave it out (the 16-bit types' take 32 cycles, less than a branch gives).
+template <typename T>
+__device__ __forceinline__ bool past(int c, int D)
+{
+    return sizeof(T) == 4 && 2 * c * kChunk<T> >= D;
+}
+
 // Operand A of S: chunk pair c of tile row (lane % 32).
 template <typename T, int DP>
 __device__ __forceinline__ typename Matrix<T>::frag row_frag(const T *tile, int lane, int c)
@@ -92,14 +100,14 @@ __device__ __forceinline__ typename Matrix<T>::frag row_frag(const T *tile, int 
 // S of 32 rows: operand A from LDS, B a lane's column.
 template <typename T, int DP>
 __device__ __forceinline__ f32x16 row_mul(const T *tile, int lane,
-                                          const typename Matrix<T>::frag (&b)[kPairs<T, DP>])
+                                          const typename Matrix<T>::frag (&b)[kPairs<T, DP>], int D)
 {
     f32x16 s;
 #pragma unroll
     for (int i = 0; i < 16; ++i) s[i] = 0.0f;
 #pragma unroll
     for (int c = 0; c < kPairs<T, DP>; ++c)
-        s = Matrix<T>::mul(row_frag<T, DP>(tile, lane, c), b[c], s);
+        if (!past<T>(c, D)) s = Matrix<T>::mul(row_frag<T, DP>(tile, lane, c), b[c], s);
     return s;
 }
 
