@@ -351,8 +351,9 @@ __device__ __forceinline__ float rest_of(float o)
 // carries for each axis which of these holds: then one place in the table serves 32
 // rows, four neighbours of one place a lane's four rows of an octet, or one place an
 // octet, and only blocks that mix them work out each row's own.  Each kind is one
-// stretch of code without branches, so that its reads of LDS run together (with a
-// branch an octet the bias' part waited for each read: DQTIMES).
+// stretch of code without branches, so that its reads of LDS run together.  (With a
+// branch an octet they waited for each other: 8160 tokens among themselves, 16 heads of
+// 64 in bf16 and two axes took 897 us a call, without 750.)
 
 constexpr int kPad = 4;                                     // entries beyond either end
 constexpr int kReachRow = 2 * kMaxReach + 2 + 2 * kPad;     // of an axis and head in LDS
