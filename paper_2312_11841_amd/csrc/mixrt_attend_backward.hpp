@@ -343,7 +343,7 @@ __global__ __launch_bounds__(256) void attend_dq_kernel(AttendK k)
 #pragma unroll
                 for (int i = 0; i < kChunk<T>; ++i) {
                     float x = (float)o[c][i];
-                    if (sizeof(T) == 2) x += (float)rest[c][i] * (1.0f / kRestScale<T>);
+                    if (sizeof(T) == 2) x = whole_of<T>(o[c][i], rest[c][i]);
                     sum = fmaf((float)dout[n][c][i], x, sum);
                 }
         }

@@ -106,11 +106,7 @@ __device__ __forceinline__ void finish(const AttendK &k, const ForwardWork &w,
                 for (int i = 0; i < 4; ++i) f[i] = acc[n][d][4 * e + i] * inv;
                 const int at = 32 * d + 8 * e + 4 * half;
                 store_quad<T>(o, at, k.D, f[0], f[1], f[2], f[3]);
-                if (rest) {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) f[i] = rest_of<T>(f[i]);
-                    store_quad<T>(rest, at, k.D, f[0], f[1], f[2], f[3]);
-                }
+                if (rest) store_rest<T>(rest, at, k.D, f);
             }
     }
 }
@@ -206,10 +202,11 @@ __device__ __forceinline__ void finish_shared(const AttendK &k, const ForwardWor
     store_run<T>((T *)k.o.data + w.b * k.o.batch + (int64_t)c.t[0] * k.o.token +
                      c.head[0] * k.o.head, d, k.D, f, inv);
     if (k.rest) {
+        T *rest = (T *)k.rest + (((int64_t)w.b * k.Tq + c.t[0]) * k.H + c.head[0]) * k.D;
 #pragma unroll
-        for (int i = 0; i < DP / 8; ++i) f[i] = rest_of<T>(f[i] * inv);
-        store_run<T>((T *)k.rest + (((int64_t)w.b * k.Tq + c.t[0]) * k.H + c.head[0]) * k.D, d,
-                     k.D, f, 1.0f);
+        for (int i = 0; i < DP / 8; ++i) f[i] *= inv;
+#pragma unroll
+        for (int i = 0; i < DP / 8; i += 4) store_rest<T>(rest, d + i, k.D, f + i);
     }
 }
 
@@ -580,9 +577,7 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendK k)
     store_quad<T>(o, d, k.D, a[0], a[1], a[2], a[3]);
     if (k.rest) {
         T *rest = (T *)k.rest + (((int64_t)b * k.Tq + t) * k.H + h) * k.D;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) a[i] = rest_of<T>(a[i]);
-        store_quad<T>(rest, d, k.D, a[0], a[1], a[2], a[3]);
+        store_rest<T>(rest, d, k.D, a);
     }
 }
 

@@ -330,17 +330,49 @@ __device__ __forceinline__ int valid_keys(const int32_t *lens, int b, int Tk)
 }
 
 constexpr float kLog2e = 1.4426950408889634f;
-// (4096 for float16, whose remainders would be subnormal)
-template <typename T> inline constexpr float kRestScale = 1.0f;
-template <> inline constexpr float kRestScale<f16> = 4096.0f;
-
-// What is left of o when it is rounded to T, for the backward pass (nothing of an
-// o that is not finite).
+// What is left of o when it is rounded to T, for the backward pass (nothing of an o
+// that is not finite), in T's bits: of float16's 13 lost bits 11, times 4096 so that it
+// is not subnormal; of bfloat16's 16, whose exponent is o's own, all of them, as the
+// difference of the bits.  (Rounded to bfloat16, which keeps 8, it was most of the
+// error of a bias table's gradient.)
 template <typename T>
-__device__ __forceinline__ float rest_of(float o)
+__device__ __forceinline__ T rest_of(float o)
 {
-    const float x = (float)(T)o;
-    return __builtin_isfinite(x) ? (o - x) * kRestScale<T> : 0.0f;
+    const T x = (T)o;
+    if (!__builtin_isfinite((float)x)) return (T)0.0f;
+    if constexpr (std::is_same_v<T, bf16>) {
+        const uint32_t n = __float_as_uint(o) - __float_as_uint((float)x);
+        return __builtin_bit_cast(bf16, (int16_t)min(max((int)n, -32768), 32767));
+    } else {
+        return (T)((o - (float)x) * 4096.0f);
+    }
+}
+
+// o again.
+template <typename T>
+__device__ __forceinline__ float whole_of(T x, T rest)
+{
+    if constexpr (std::is_same_v<T, bf16>)
+        return __uint_as_float(__float_as_uint((float)x) +
+                               (uint32_t)(int)__builtin_bit_cast(int16_t, rest));
+    else
+        return (float)x + (float)rest * (1.0f / 4096.0f);
+}
+
+// What is left of four elements of a column's result to a dense row of D.
+template <typename T>
+__device__ __forceinline__ void store_rest(T *row, int d, int D, const float *o)
+{
+    Pack<T, 4> x;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x.v[i] = rest_of<T>(o[i]);
+    if (d + 4 <= D) {
+        *(Pack<T, 4> *)(row + d) = x;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (d + i < D) row[d + i] = x.v[i];
+    }
 }
 
 // --- the bias ---------------------------------------------------------------------

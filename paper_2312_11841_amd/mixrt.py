@@ -695,8 +695,8 @@ def distance_buckets(count: int, reach: int, near=None):
 @dataclass
 class AttentionSaved:
     """What attention_backward needs of attention_train besides its output: lse
-    float32 [batch, heads, queries], and what rounding took from the output
-    (float16 and bfloat16; None for float32)."""
+    float32 [batch, heads, queries], and the bits that rounding took from the
+    output (float16 and bfloat16, in a tensor of that type; None for float32)."""
 
     lse: object
     rest: object
