@@ -150,16 +150,25 @@ __device__ __forceinline__ typename Matrix<T>::frag round_rows(const f32x16 &p, 
     return f;
 }
 
-// What that rounding left of them, rounded in turn.
-template <typename T>
-__device__ __forceinline__ typename Matrix<T>::frag left_rows(const f32x16 &p,
-                                                              typename Matrix<T>::frag f, int s)
+// The same as a sum of TERMS: their rounded values, what that left, rounded in turn, ..
+template <typename T, int TERMS>
+__device__ __forceinline__ void split_rows(const f32x16 &p, int s,
+                                           typename Matrix<T>::frag (&f)[TERMS])
 {
-    typename Matrix<T>::frag g;
-    asm("" : "+v"(f));      // (taken from the pairs, not rounded once more one by one)
+    f[0] = round_rows<T>(p, s);
+    float left[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) g[i] = (T)(p[8 * s + i] - (float)f[i]);
-    return g;
+    for (int i = 0; i < 8; ++i) left[i] = p[8 * s + i];
+#pragma unroll
+    for (int n = 1; n < TERMS; ++n) {
+        // (taken from the pairs, not rounded once more one by one)
+        asm("" : "+v"(f[n - 1]));
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            left[i] -= (float)f[n - 1][i];
+            f[n][i] = (T)left[i];
+        }
+    }
 }
 
 // A row's chunk in registers: elements [at, at + chunk) of a head of D, zeros behind.
