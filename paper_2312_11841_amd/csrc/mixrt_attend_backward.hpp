@@ -787,24 +787,36 @@ __global__ __launch_bounds__(256) void attend_sum_kernel(const float *part, int 
                   a[1], a[2], a[3]);
 }
 
-// dtable[entry][h] = sum over the entries' blocks of head h, in 64 bits.
-__global__ __launch_bounds__(256) void attend_table_kernel(const float *part, int B, int H,
-                                                           int each, int entries, float *dtable)
+// dtable[axis][bucket][h] = sum over the parts of head h's blocks, in 64 bits: a block an
+// axis and head, 32 lanes its buckets, 32 groups of them every 32nd part.  A row's dS sum
+// to 0, and so do an axis' buckets; where all but one of them are 0 (one bucket, or one
+// distance for all pairs), that one is 0 as well and not what roundings left of its sum
+// (times 0, so that a NaN stays).
+__global__ __launch_bounds__(1024) void attend_table_kernel(const float *part, int B, int H,
+                                                            int each, int axes, int count,
+                                                            float *dtable)
 {
-    __shared__ double sums[256];
-    const int e = blockIdx.x, h = blockIdx.y;
+    static_assert(kMaxBuckets == 32);
+    __shared__ double sums[32][32];
+    const int axis = blockIdx.x, h = blockIdx.y, e = threadIdx.x & 31, g = threadIdx.x >> 5;
     // block ((b H + h) each + i) of the queries' gradient
     double a = 0.0;
-    for (int64_t i = threadIdx.x; i < (int64_t)B * each; i += 256) {
-        const int64_t b = i / each;
-        a += part[((b * H + h) * each + (i - b * each)) * entries + e];
-    }
-    sums[threadIdx.x] = a;
-    for (int n = 128; n > 0; n >>= 1) {
+    if (e < count)
+#pragma unroll 4
+        for (int64_t i = g; i < (int64_t)B * each; i += 32) {
+            const int64_t b = i / each;
+            a += part[((b * H + h) * each + (i - b * each)) * (axes * count) + axis * count + e];
+        }
+    sums[g][e] = a;
+    for (int n = 16; n > 0; n >>= 1) {
         __syncthreads();
-        if ((int)threadIdx.x < n) sums[threadIdx.x] += sums[threadIdx.x + n];
+        if (g < n) sums[g][e] += sums[g + n][e];
     }
-    if (threadIdx.x == 0) dtable[(int64_t)e * H + h] = (float)sums[0];
+    if (g != 0) return;
+    a = sums[0][e];
+    const uint32_t some = (uint32_t)__builtin_amdgcn_ballot_w64(a != 0.0);
+    if ((some & (some - 1)) == 0) a = fabs(a * 0.0);
+    if (e < count) dtable[((int64_t)axis * count + e) * H + h] = (float)a;
 }
 
 template <typename T>
@@ -851,8 +863,8 @@ hipError_t launch_back_q(const AttendK &k, const AttendPlan &p, hipStream_t stre
     hipError_t e = hipGetLastError();
     if (e == hipSuccess && k.splits > 1) e = launch_sum<T>(k, k.H, k.Tq, k.dq, k.dq, 1, stream);
     if (e == hipSuccess && entries && k.dtable) {
-        attend_table_kernel<<<dim3(entries, k.H), 256, 0, stream>>>(
-            k.part_table, k.B, k.H, k.splits * k.blocks, entries, k.dtable);
+        attend_table_kernel<<<dim3(k.bias.axes, k.H), 1024, 0, stream>>>(
+            k.part_table, k.B, k.H, k.splits * k.blocks, k.bias.axes, k.bias.buckets, k.dtable);
         e = hipGetLastError();
     }
     return e;

@@ -159,6 +159,32 @@ def test_attention_with_bias_and_gradients(r, shape, dtype):
     _check(r, q, k, v, dout, DT[dtype], bias=_bias(g, axes, count, reach, B, Tq, Tk, H, i % 2))
 
 
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_bias_of_one_bucket_has_no_gradient(r, dtype):
+    """A bias that all keys of a row share does not change its weights: the table's
+    gradient is 0 exactly with one bucket, with a reach of 0, and on an axis where all
+    tokens have one place; not a NaN's."""
+    B, Tq, Tk, H, Hk, D = 2, 70, 300, 4, 2, 32
+    g = _gen(77)
+    q, k, v, dout = _sequences(g, B, Tq, Tk, H, Hk, D, DT[dtype])
+    args = [t.cuda() for t in (q, k, v)]
+    for axes, count, reach, level in ((1, 1, 20, None), (2, 7, 0, None), (3, 9, 15, 1)):
+        say("one bucket", dtype, axes, count, reach, level)
+        bias = _bias(g, axes, count, reach, B, Tq, Tk, H)
+        if level is not None:
+            bias[2][:, level], bias[3][:, level] = 4, 9
+        on = _on_gpu(bias)
+        o, saved = r.attention_train(*args, bias=on)
+        table = r.attention_backward(dout.cuda(), *args, o, saved, bias=on)[3]
+        for a in range(axes):
+            assert bool((table[a] == 0).all()) == (level is None or a == level)
+        bad = dout.clone()
+        bad[1, 3, 2, 0] = math.nan
+        table = r.attention_backward(bad.cuda(), *args, o, saved, bias=on)[3].cpu()
+        assert all(bool(table[a, :, 2].isnan().any()) for a in range(axes))
+        assert not bool(table[:, :, 0].isnan().any())
+
+
 # --- masks, lengths and values that are not numbers ------------------------------------
 
 @pytest.mark.parametrize("biased", [False, True])
