@@ -651,7 +651,9 @@ typedef struct {
 /* Heads of a sequence in device memory: element (entry, token, head, d) at
  * data[entry * batch_stride + token * token_stride + head * head_stride + d].
  * Strides in elements, at least 0 for inputs; the elements of an output must
- * not overlap.  Aligned to its element type. */
+ * not overlap, and it shares no memory with the call's other arrays (slices of
+ * one joint array, apart in each of its tokens, will do).  Aligned to its
+ * element type. */
 typedef struct {
     void *data;
     int64_t batch_stride, token_stride, head_stride;

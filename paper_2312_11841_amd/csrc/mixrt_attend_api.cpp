@@ -289,13 +289,57 @@ int check_sequence(mixrt_ctx *ctx, const mixrt_attention *a, const mixrt_sequenc
                 (long long)st[0], (long long)st[1], (long long)st[2]);
 }
 
-// An output is none of the inputs.
-int check_apart(mixrt_ctx *ctx, const mixrt_sequence *out, const char *name,
-                std::initializer_list<const mixrt_sequence *> inputs)
+// An array of a call: queries' or keys' heads.
+struct Seen {
+    const mixrt_sequence *s;
+    bool queries;
+};
+
+// Whether two arrays certainly share no element: one lies behind the other, or both
+// repeat with some stride and take other parts of it (slices of one joint array).
+bool apart(const mixrt_attention *att, const Seen &a, const Seen &b)
 {
-    for (const mixrt_sequence *s : inputs)
-        if (out->data && out->data == s->data)
-            return fail(ctx, MIXRT_EINVAL, "%s is also another array", name);
+    const int64_t elem = elem_size(att->dtype), D = att->head_dim;
+    const Seen *both[2] = {&a, &b};
+    int64_t n[2][3], st[2][3], span[2];
+    for (int i = 0; i < 2; ++i) {
+        const mixrt_sequence *s = both[i]->s;
+        const int64_t ni[3] = {att->batch, both[i]->queries ? att->queries : att->keys,
+                               both[i]->queries ? att->heads : att->kv_heads};
+        const int64_t si[3] = {s->batch_stride, s->token_stride, s->head_stride};
+        span[i] = D;
+        for (int j = 0; j < 3; ++j) {
+            if (ni[j] == 0) return true;
+            n[i][j] = ni[j];
+            st[i][j] = si[j];
+            span[i] += (ni[j] - 1) * si[j];
+        }
+    }
+    const uint64_t pa = (uint64_t)(uintptr_t)a.s->data, pb = (uint64_t)(uintptr_t)b.s->data;
+    if (pa < pb ? pb - pa >= (uint64_t)(span[0] * elem) : pa - pb >= (uint64_t)(span[1] * elem))
+        return true;
+    const int64_t diff = (int64_t)(pb - pa);
+    if (diff % elem) return false;
+    for (int c = 0; c < 6; ++c) {
+        const int64_t s = st[c / 3][c % 3];
+        if (s <= 0 || n[c / 3][c % 3] == 1) continue;
+        int64_t part[2] = {D, D};       // of a repetition
+        for (int i = 0; i < 2; ++i)
+            for (int j = 0; j < 3; ++j)
+                if (st[i][j] % s) part[i] += (n[i][j] - 1) * st[i][j];
+        const int64_t m = (diff / elem % s + s) % s;
+        if (m >= part[0] && m + part[1] <= s) return true;
+    }
+    return false;
+}
+
+// An output shares no memory with the other arrays.
+int check_apart(mixrt_ctx *ctx, const mixrt_attention *att, const Seen &out, const char *name,
+                std::initializer_list<Seen> others)
+{
+    for (const Seen &s : others)
+        if (out.s->data && s.s->data && !apart(att, out, s))
+            return fail(ctx, MIXRT_EINVAL, "%s is also another array, or a part of one", name);
     return MIXRT_OK;
 }
 
@@ -548,7 +592,8 @@ int mixrt_attention_forward(mixrt_ctx *ctx, const mixrt_attention *att,
         (rc = check_sequence(ctx, att, v, false, "v", false)) ||
         (rc = check_sequence(ctx, att, out, true, "out", true)))
         return rc;
-    if (att->batch && att->queries && (rc = check_apart(ctx, out, "out", {q, k, v}))) return rc;
+    if ((rc = check_apart(ctx, att, {out, true}, "out", {{q, true}, {k, false}, {v, false}})))
+        return rc;
     if (!aligned(lse, 4)) return fail(ctx, MIXRT_EINVAL, "lse not 4-byte aligned");
     if (rest && att->dtype == MIXRT_F32) return fail(ctx, MIXRT_EINVAL, "rest for F32");
     if (!aligned(rest, 2)) return fail(ctx, MIXRT_EINVAL, "rest not aligned to its element");
@@ -591,10 +636,12 @@ int mixrt_attention_backward(mixrt_ctx *ctx, const mixrt_attention *att,
         (rc = check_sequence(ctx, att, dk, false, "dk", true)) ||
         (rc = check_sequence(ctx, att, dv, false, "dv", true)))
         return rc;
-    if (att->batch &&
-        ((att->queries && (rc = check_apart(ctx, dq, "dq", {dout, q, k, v, out, dk, dv}))) ||
-         (att->keys && ((rc = check_apart(ctx, dk, "dk", {dout, q, k, v, out, dv})) ||
-                        (rc = check_apart(ctx, dv, "dv", {dout, q, k, v, out}))))))
+    const Seen in_dout{dout, true}, in_q{q, true}, in_k{k, false}, in_v{v, false}, in_o{out, true};
+    if ((rc = check_apart(ctx, att, {dq, true}, "dq",
+                          {in_dout, in_q, in_k, in_v, in_o, {dk, false}, {dv, false}})) ||
+        (rc = check_apart(ctx, att, {dk, false}, "dk",
+                          {in_dout, in_q, in_k, in_v, in_o, {dv, false}})) ||
+        (rc = check_apart(ctx, att, {dv, false}, "dv", {in_dout, in_q, in_k, in_v, in_o})))
         return rc;
     if (dtable && !bias) return fail(ctx, MIXRT_EINVAL, "dtable without a bias");
     if (!aligned(lse, 4) || !aligned(dtable, 4))

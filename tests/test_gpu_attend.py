@@ -659,6 +659,38 @@ def test_binding_refuses_wrong_tensors(r):
         r.attention_backward(q.half(), *args, mixrt.AttentionSaved(saved.lse, None))
 
 
+def test_outputs_that_share_memory_with_inputs(r):
+    """An output over a part of an input is refused, one beside the inputs in a joint
+    array is not, and gives what an array of its own gives."""
+    g = _gen(31)
+    buf = torch.randn((2, 9, 4, 16), generator=g).cuda()
+    q, k = buf[:, :7], torch.randn((2, 7, 2, 16), generator=g).cuda()
+    for out in (buf[:, 1:8], buf[:, 2:]):
+        with pytest.raises(mixrt.MixrtError, match="also another"):
+            r.attention(q, k, k, out=out)
+    # half a head further
+    flat = torch.zeros(2 * 7 * 4 * 16 + 8, device="cuda")
+    with pytest.raises(mixrt.MixrtError, match="also another"):
+        r.attention(flat[:-8].view(2, 7, 4, 16), k, k, out=flat[8:].view(2, 7, 4, 16))
+    # heads of one token behind each other: q, out, k, v, in either order of dimensions
+    joint = torch.randn((2, 7, 4 + 4 + 2 + 2, 16), generator=g).cuda()
+    q, out, k, v = joint.split([4, 4, 2, 2], 2)
+    want = r.attention(q, k, v)
+    keep = [t.clone() for t in (q, k, v)]
+    r.attention(q, k, v, out=out)
+    assert torch.equal(out, want) and all(torch.equal(a, b) for a, b in zip(keep, (q, k, v)))
+    wide = torch.randn((2, 4, 7, 64), generator=g).cuda().transpose(1, 2)
+    q, out, k, v = wide.split(16, 3)
+    want = r.attention(q, k, v)
+    r.attention(q, k, v, out=out)
+    assert torch.equal(out, want)
+    # arrays behind each other in one allocation
+    rows = torch.randn((3, 2, 7, 4, 16), generator=g).cuda()
+    want = r.attention(rows[0], rows[1], rows[1])
+    r.attention(rows[0], rows[1], rows[1], out=rows[2])
+    assert torch.equal(rows[2], want)
+
+
 def test_binding_refuses_a_wrong_bias(r):
     q = torch.zeros((2, 5, 4, 16), device="cuda")
     table, buckets = torch.zeros((2, 3, 4)), torch.zeros((2, 9)).byte()
