@@ -348,8 +348,8 @@ __global__ __launch_bounds__(256) void attend_kernel(AttendK k)
 // of it.
 // With a bias in bfloat16 a third term, of 8 bits like the others: the table's gradient
 // is in 32 bits, and sums what would be left of many rows that cancel (3600 queries over
-// 7200 keys, 8 heads, three axes: a relative error of 1.7e-6 with two terms, 6.4e-7 with
-// three, and the training step 873 and 890 us).
+// 7200 keys, 8 heads, three axes: a relative error of 1.7e-6 with two terms, 6e-7 to
+// 8e-7 with three, and the training step 873 and 890 us).
 template <int DP> inline constexpr int kFlowWaves = DP <= 64 ? 2 : 1;   // a SIMD
 template <typename T, int DP, int NC, bool BIAS, bool EXACT>
 __global__ __launch_bounds__(256, kFlowWaves<DP>) void attend_flow_kernel(AttendK k)
@@ -394,7 +394,10 @@ __global__ __launch_bounds__(256, kFlowWaves<DP>) void attend_flow_kernel(Attend
 #pragma unroll
         for (int n = 0; n < NC; ++n) hbase[n] = 0;
     }
-    f32x16 acc[NC][DP / 32], s[NC];
+    // (the small terms of three have sums of their own: in one they would round the
+    // large one's three times as often)
+    constexpr int ND = DP / 32, LOW = kTerms<T, BIAS, EXACT> > 2 ? ND : 0;
+    f32x16 acc[NC][ND + LOW], s[NC];
     float top[NC], sum[NC];
     frag p[NC][2][kTerms<T, BIAS, EXACT>];      // weights of the last 32 rows
 #pragma unroll
@@ -402,7 +405,7 @@ __global__ __launch_bounds__(256, kFlowWaves<DP>) void attend_flow_kernel(Attend
         top[n] = -INFINITY;
         sum[n] = 0.0f;
 #pragma unroll
-        for (int d = 0; d < DP / 32; ++d)
+        for (int d = 0; d < ND + LOW; ++d)
 #pragma unroll
             for (int i = 0; i < 16; ++i) acc[n][d][i] = 0.0f;
     }
@@ -422,8 +425,10 @@ __global__ __launch_bounds__(256, kFlowWaves<DP>) void attend_flow_kernel(Attend
 #pragma unroll
                 for (int n = 0; n < NC; ++n)
 #pragma unroll
-                    for (const frag &term : p[n][e])
-                        acc[n][d] = Matrix<T>::mul(a, term, acc[n][d]);
+                    for (int i = 0; i < kTerms<T, BIAS, EXACT>; ++i) {
+                        const int at = i == 0 ? d : d + LOW;
+                        acc[n][at] = Matrix<T>::mul(a, p[n][e][i], acc[n][at]);
+                    }
             }
     };
     const float unit = BIAS ? 1.0f : k.scale;
@@ -496,7 +501,12 @@ __global__ __launch_bounds__(256, kFlowWaves<DP>) void attend_flow_kernel(Attend
         v2 = x;
     }
     add_values(held);
-    finish<T, DP, NC>(k, w, c, half, acc, sum, top);
+    f32x16 whole[NC][ND];
+#pragma unroll
+    for (int n = 0; n < NC; ++n)
+#pragma unroll
+        for (int d = 0; d < ND; ++d) whole[n][d] = LOW ? acc[n][d] + acc[n][d + LOW] : acc[n][d];
+    finish<T, DP, NC>(k, w, c, half, whole, sum, top);
 }
 
 // Joins the splits of a row: o = sum_s 2^(lse_s - top) o_s / sum_s 2^(lse_s - top).
