@@ -175,7 +175,16 @@ __device__ __forceinline__ void add_places(float *mine, int (&e)[4], float (&v)[
     put_places(mine, e, v);
 }
 
-// Adds a column's dS to its places of the bias table's gradient.
+// Orders the LDS accesses of a wave's halves: those before come before those after, in
+// every lane.  (A wave's accesses run in its order; this keeps the compiler's so.)
+__device__ __forceinline__ void halves_meet()
+{
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
+// Adds a column's dS to its places of the bias table's gradient.  The halves of a wave
+// share the places; from one tile to the next its caller's Team::meet() orders them.
 template <int ROWS>
 __device__ __forceinline__ void add_table(const f32x16 &g, const TilePos<ROWS> &tile, int u,
                                           int half,
@@ -249,10 +258,14 @@ __device__ __forceinline__ void add_table(const f32x16 &g, const TilePos<ROWS> &
             join_places(e[j], v[j], spare);
         }
 #pragma unroll 1
-        for (int h = 0; h < 2; ++h)
+        for (int h = 0; h < 2; ++h) {
             if (half == h)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) put_places(mine, e[j], v[j]);
+            // (what one half has written is there for the other to read: else the two
+            // turns are one to a compiler that looks at a single lane)
+            halves_meet();
+        }
     }
 }
 
