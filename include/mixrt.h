@@ -590,7 +590,9 @@ typedef struct {
     const void *x;
     const void *dy;       /* backward only */
     void *out;            /* forward: out, may be x with x's strides; backward:
-                             dx, may be dy with dy's strides, or NULL */
+                             dx, may be dy with dy's strides, or NULL; else it
+                             shares no memory with the call's other arrays, of
+                             either descriptor (slices of one joint array will do) */
     float *dweight;       /* backward: device float [head_dim], or NULL */
     int64_t x_token_stride, x_head_stride, dy_token_stride, dy_head_stride, out_token_stride,
         out_head_stride;

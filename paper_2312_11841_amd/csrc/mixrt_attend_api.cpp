@@ -5,8 +5,8 @@
 #include "mixrt.h"
 
 #include <cmath>
-#include <initializer_list>
 
+#include "mixrt_apart.hpp"
 #include "mixrt_attend.hpp"
 #include "mixrt_ctx.hpp"
 #include "mixrt_refine.hpp"
@@ -154,6 +154,7 @@ AttendPlan plan_attend_dkv(int B, int H, int Hk, int64_t Tq, int64_t Tk, int D, 
 
 namespace {
 
+using mixrt::Arrays;
 using mixrt::AttendPlan;
 using mixrt::bind_device;
 using mixrt::clear_err;
@@ -289,57 +290,38 @@ int check_sequence(mixrt_ctx *ctx, const mixrt_attention *a, const mixrt_sequenc
                 (long long)st[0], (long long)st[1], (long long)st[2]);
 }
 
-// An array of a call: queries' or keys' heads.
-struct Seen {
-    const mixrt_sequence *s;
-    bool queries;
-};
-
-// Whether two arrays certainly share no element: one lies behind the other, or both
-// repeat with some stride and take other parts of it (slices of one joint array).
-bool apart(const mixrt_attention *att, const Seen &a, const Seen &b)
+mixrt::Extent extent_of(const mixrt_attention *att, const mixrt_sequence *s, bool queries)
 {
-    const int64_t elem = elem_size(att->dtype), D = att->head_dim;
-    const Seen *both[2] = {&a, &b};
-    int64_t n[2][3], st[2][3], span[2];
-    for (int i = 0; i < 2; ++i) {
-        const mixrt_sequence *s = both[i]->s;
-        const int64_t ni[3] = {att->batch, both[i]->queries ? att->queries : att->keys,
-                               both[i]->queries ? att->heads : att->kv_heads};
-        const int64_t si[3] = {s->batch_stride, s->token_stride, s->head_stride};
-        span[i] = D;
-        for (int j = 0; j < 3; ++j) {
-            if (ni[j] == 0) return true;
-            n[i][j] = ni[j];
-            st[i][j] = si[j];
-            span[i] += (ni[j] - 1) * si[j];
-        }
-    }
-    const uint64_t pa = (uint64_t)(uintptr_t)a.s->data, pb = (uint64_t)(uintptr_t)b.s->data;
-    if (pa < pb ? pb - pa >= (uint64_t)(span[0] * elem) : pa - pb >= (uint64_t)(span[1] * elem))
-        return true;
-    const int64_t diff = (int64_t)(pb - pa);
-    if (diff % elem) return false;
-    for (int c = 0; c < 6; ++c) {
-        const int64_t s = st[c / 3][c % 3];
-        if (s <= 0 || n[c / 3][c % 3] == 1) continue;
-        int64_t part[2] = {D, D};       // of a repetition
-        for (int i = 0; i < 2; ++i)
-            for (int j = 0; j < 3; ++j)
-                if (st[i][j] % s) part[i] += (n[i][j] - 1) * st[i][j];
-        const int64_t m = (diff / elem % s + s) % s;
-        if (m >= part[0] && m + part[1] <= s) return true;
-    }
-    return false;
+    const int64_t size = elem_size(att->dtype);
+    return mixrt::Extent{(uint64_t)(uintptr_t)s->data, att->head_dim * size,
+                         {att->batch, queries ? att->queries : att->keys,
+                          queries ? att->heads : att->kv_heads},
+                         {s->batch_stride * size, s->token_stride * size, s->head_stride * size}};
+}
+
+// The arrays that a forward and a backward call share.
+void add_common(Arrays &m, const mixrt_attention *att, const mixrt_relative_bias *b,
+                const mixrt_sequence *q, const mixrt_sequence *k, const mixrt_sequence *v)
+{
+    m.add(extent_of(att, q, true), "q");
+    m.add(extent_of(att, k, false), "k");
+    m.add(extent_of(att, v, false), "v");
+    m.add(mixrt::flat_extent(att->lens, (int64_t)att->batch * 4), "lens");
+    if (!b) return;
+    const int64_t entries = att->batch > 0 ? att->batch - 1 : 0;
+    m.add(mixrt::flat_extent(b->table, (int64_t)b->axes * b->count * att->heads * 4), "table");
+    m.add(mixrt::flat_extent(b->buckets, (int64_t)b->axes * (2 * b->reach + 1)), "buckets");
+    m.add(mixrt::Extent{(uint64_t)(uintptr_t)b->q_pos, att->queries * b->axes * 4,
+                        {entries + 1, 1, 1}, {b->q_pos_stride * 4, 0, 0}}, "q_pos");
+    m.add(mixrt::Extent{(uint64_t)(uintptr_t)b->k_pos, att->keys * b->axes * 4,
+                        {entries + 1, 1, 1}, {b->k_pos_stride * 4, 0, 0}}, "k_pos");
 }
 
 // An output shares no memory with the other arrays.
-int check_apart(mixrt_ctx *ctx, const mixrt_attention *att, const Seen &out, const char *name,
-                std::initializer_list<Seen> others)
+int check_apart(mixrt_ctx *ctx, const Arrays &m)
 {
-    for (const Seen &s : others)
-        if (out.s->data && s.s->data && !apart(att, out, s))
-            return fail(ctx, MIXRT_EINVAL, "%s is also another array, or a part of one", name);
+    if (const Arrays::One *s = m.shared())
+        return fail(ctx, MIXRT_EINVAL, "%s is also another array, or a part of one", s->name);
     return MIXRT_OK;
 }
 
@@ -418,6 +400,36 @@ hipError_t launch_attend(const mixrt::AttendK &k, int stage, hipStream_t stream)
 }
 
 // --- heads normed and turned ----------------------------------------------------------
+
+// Blocks read heads while others write theirs: an output is its own array's input
+// (x forward, dy backward: each head is read before it is written, by the lanes that
+// write it) or shares memory with no other array of the call.
+int check_normed_apart(mixrt_ctx *ctx, const mixrt_rotary *r, const mixrt_normed_heads *heads,
+                       int32_t n, bool backward)
+{
+    auto extent = [&](const mixrt_normed_heads &h, const void *p, int64_t token, int64_t head) {
+        const int64_t size = elem_size(h.dtype);
+        return mixrt::Extent{(uint64_t)(uintptr_t)p, h.head_dim * size, {r->tokens, h.heads, 1},
+                             {token * size, head * size, 0}};
+    };
+    Arrays m;
+    m.add(mixrt::flat_extent(r->pos, r->pairs ? r->tokens * r->axes * 4 : 0), "pos");
+    m.add(mixrt::flat_extent(r->freq, (int64_t)r->pairs * 4), "freq");
+    m.add(mixrt::flat_extent(r->axis, r->pairs), "axis");
+    for (int i = 0; i < n; ++i) {
+        const mixrt_normed_heads &h = heads[i];
+        const bool in_place = h.out == (backward ? h.dy : h.x);
+        m.add(mixrt::flat_extent(h.weight, (int64_t)h.head_dim * 4), "weight");
+        if (backward || !in_place) m.add(extent(h, h.x, h.x_token_stride, h.x_head_stride), "x");
+        if (backward && !in_place)
+            m.add(extent(h, h.dy, h.dy_token_stride, h.dy_head_stride), "dy");
+        m.add(extent(h, h.out, h.out_token_stride, h.out_head_stride), backward ? "dx" : "out",
+              true);
+        if (backward)
+            m.add(mixrt::flat_extent(h.dweight, (int64_t)h.head_dim * 4), "dweight", true);
+    }
+    return check_apart(ctx, m);
+}
 
 int check_normed(mixrt_ctx *ctx, const mixrt_rotary *r, float eps, const mixrt_normed_heads *heads,
                  int32_t n, bool backward, bool data, mixrt::RotaryNormLaunch &L)
@@ -515,7 +527,7 @@ int check_normed(mixrt_ctx *ctx, const mixrt_rotary *r, float eps, const mixrt_n
         if (backward && h.x == h.out)
             return fail(ctx, MIXRT_EINVAL, "heads[%d]: dx is x", i);
     }
-    return MIXRT_OK;
+    return data ? check_normed_apart(ctx, r, heads, n, backward) : MIXRT_OK;
 }
 
 }  // namespace
@@ -592,8 +604,13 @@ int mixrt_attention_forward(mixrt_ctx *ctx, const mixrt_attention *att,
         (rc = check_sequence(ctx, att, v, false, "v", false)) ||
         (rc = check_sequence(ctx, att, out, true, "out", true)))
         return rc;
-    if ((rc = check_apart(ctx, att, {out, true}, "out", {{q, true}, {k, false}, {v, false}})))
-        return rc;
+    const int64_t rows = (int64_t)att->batch * att->heads * att->queries;
+    Arrays m;
+    add_common(m, att, bias, q, k, v);
+    m.add(extent_of(att, out, true), "out", true);
+    m.add(mixrt::flat_extent(lse, rows * 4), "lse", true);
+    m.add(mixrt::flat_extent(rest, rows * att->head_dim * 2), "rest", true);
+    if ((rc = check_apart(ctx, m))) return rc;
     if (!aligned(lse, 4)) return fail(ctx, MIXRT_EINVAL, "lse not 4-byte aligned");
     if (rest && att->dtype == MIXRT_F32) return fail(ctx, MIXRT_EINVAL, "rest for F32");
     if (!aligned(rest, 2)) return fail(ctx, MIXRT_EINVAL, "rest not aligned to its element");
@@ -636,13 +653,20 @@ int mixrt_attention_backward(mixrt_ctx *ctx, const mixrt_attention *att,
         (rc = check_sequence(ctx, att, dk, false, "dk", true)) ||
         (rc = check_sequence(ctx, att, dv, false, "dv", true)))
         return rc;
-    const Seen in_dout{dout, true}, in_q{q, true}, in_k{k, false}, in_v{v, false}, in_o{out, true};
-    if ((rc = check_apart(ctx, att, {dq, true}, "dq",
-                          {in_dout, in_q, in_k, in_v, in_o, {dk, false}, {dv, false}})) ||
-        (rc = check_apart(ctx, att, {dk, false}, "dk",
-                          {in_dout, in_q, in_k, in_v, in_o, {dv, false}})) ||
-        (rc = check_apart(ctx, att, {dv, false}, "dv", {in_dout, in_q, in_k, in_v, in_o})))
-        return rc;
+    const int64_t all = (int64_t)att->batch * att->heads * att->queries;
+    Arrays m;
+    add_common(m, att, bias, q, k, v);
+    m.add(extent_of(att, dout, true), "dout");
+    m.add(extent_of(att, out, true), "out");
+    m.add(mixrt::flat_extent(lse, all * 4), "lse");
+    m.add(mixrt::flat_extent(rest, all * att->head_dim * 2), "rest");
+    m.add(extent_of(att, dq, true), "dq", true);
+    m.add(extent_of(att, dk, false), "dk", true);
+    m.add(extent_of(att, dv, false), "dv", true);
+    if (bias)
+        m.add(mixrt::flat_extent(dtable, (int64_t)bias->axes * bias->count * att->heads * 4),
+              "dtable", true);
+    if ((rc = check_apart(ctx, m))) return rc;
     if (dtable && !bias) return fail(ctx, MIXRT_EINVAL, "dtable without a bias");
     if (!aligned(lse, 4) || !aligned(dtable, 4))
         return fail(ctx, MIXRT_EINVAL, "lse or dtable not 4-byte aligned");

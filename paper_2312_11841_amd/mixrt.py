@@ -1319,8 +1319,9 @@ class Renderer:
                     layout: str = "halves", out=None):
         """Heads normed one by one and turned, in one pass: x / sqrt(mean(x^2) +
         eps) * weight over each head, then rotary.  heads, pos, freq, axis, layout
-        and out as in rotary; weights: a float32 [D] (or None) for each array of
-        heads, likewise one or a tuple, or None for none."""
+        and out as in rotary (an output that is not its input shares no memory
+        with the other tensors); weights: a float32 [D] (or None) for each array
+        of heads, likewise one or a tuple, or None for none."""
         single, arrays, weights = self._as_arrays(heads, weights)
         eps = float(eps)
         key = self._normed_key("rotary_norm", arrays, (), weights, pos, freq, axis, layout)

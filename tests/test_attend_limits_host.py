@@ -1,6 +1,7 @@
 """The attention kernels' limits, without a GPU: the order of what lanes pass to each
-other."""
+other, and the rule that finds arrays which share memory."""
 import os
+import random
 import re
 import subprocess
 import tempfile
@@ -54,3 +55,77 @@ def test_a_wave_s_halves_add_to_shared_places_in_turn():
     text = _compile(HALVES, "--cuda-device-only", "-S")
     body = re.search(r"^(\S*halves\S*):(.*?)s_endpgm", text, re.S | re.M).group(2)
     assert "wave barrier" in body
+
+
+SHARED = r"""
+#include <cstdio>
+#include "mixrt_apart.hpp"
+int main()
+{
+    mixrt::Extent e[2];
+    long long at, run, n[3], st[3];
+    for (int i = 0;; i ^= 1) {
+        if (scanf("%lld %lld %lld %lld %lld %lld %lld %lld", &at, &run, n, n + 1, n + 2, st, st + 1,
+                  st + 2) != 8)
+            return 0;
+        e[i] = mixrt::Extent{(uint64_t)at, run, {n[0], n[1], n[2]}, {st[0], st[1], st[2]}};
+        if (i) printf("%d %d\n", mixrt::apart(e[0], e[1]), mixrt::apart(e[1], e[0]));
+    }
+}
+"""
+
+
+def _bytes(e):
+    at, run, n0, n1, n2, s0, s1, s2 = e
+    return {at + i * s0 + j * s1 + k * s2 + x for i in range(n0) for j in range(n1)
+            for k in range(n2) for x in range(run)}
+
+
+@pytest.fixture(scope="module")
+def apart():
+    """f([(extent, extent)]) -> [whether the rule calls them apart, either way round]."""
+    if not os.path.exists(build.HIPCC):
+        pytest.skip("no hipcc")
+    with tempfile.TemporaryDirectory() as d:
+        src, exe = os.path.join(d, "a.cpp"), os.path.join(d, "a")
+        with open(src, "w") as f:
+            f.write(SHARED)
+        subprocess.run(["g++", "-std=c++17", "-I", build.CSRC, src, "-o", exe], check=True)
+
+        def ask(pairs):
+            text = "\n".join(" ".join(map(str, e)) for p in pairs for e in p)
+            out = subprocess.run([exe], input=text, capture_output=True, text=True, check=True)
+            return [tuple(map(int, l.split())) for l in out.stdout.splitlines()]
+        yield ask
+
+
+def test_arrays_that_share_memory_are_found(apart):
+    """Small layouts, each against all of its bytes: what the rule calls apart is."""
+    rng = random.Random(3)
+    pairs = []
+    for _ in range(4000):
+        pairs.append(tuple((rng.randint(1, 60), rng.randint(1, 6), rng.randint(1, 4),
+                            rng.randint(1, 4), rng.randint(1, 3), rng.choice((0, 2, 6, 12, 24, 48)),
+                            rng.choice((0, 3, 6, 8, 12, 24)), rng.choice((0, 2, 4, 6)))
+                           for _ in range(2)))
+    got = apart(pairs)
+    assert len(got) == len(pairs)
+    for p, g in zip(pairs, got):
+        if any(g):
+            assert not _bytes(p[0]) & _bytes(p[1]), p
+    assert sum(all(g) for g in got) > 400
+
+
+def test_slices_of_one_joint_array_are_apart(apart):
+    """What programs have: arrays behind each other, heads of one token behind each
+    other, halves of each head, tokens of two parts, and what is not there."""
+    T, D = 7, 8
+    joint = [[(1, 4 * D, T, 1, 1, 12 * D, 0, 0), (1 + 4 * D, 4 * D, T, 1, 1, 12 * D, 0, 0)],
+             [(1, D, T, 4, 1, 12 * D, D, 0), (1 + 4 * D, D, T, 2, 1, 12 * D, D, 0)],
+             [(1, D, 2, T, 4, 8 * D * T, 8 * D, 2 * D),
+              (1 + D, D, 2, T, 4, 8 * D * T, 8 * D, 2 * D)],
+             [(1, D, T, 4, 1, D, 2 * T * D, 0), (1 + T * D, D, T, 4, 1, D, 2 * T * D, 0)],
+             [(1, 100, 1, 1, 1, 0, 0, 0), (101, 4, 1, 1, 1, 0, 0, 0)],
+             [(0, 100, 1, 1, 1, 0, 0, 0), (1, 100, 1, 1, 1, 0, 0, 0)],
+             [(1, 100, 0, 1, 1, 5, 0, 0), (1, 100, 1, 1, 1, 0, 0, 0)]]
+    assert apart(joint) == [(1, 1)] * len(joint)

@@ -1,0 +1,125 @@
+"""The refiner's attention on the GPU where its calls meet their limits: outputs that
+share memory, numbers at the ends of their types' ranges, many rows and keys.  Against
+the 64-bit statements of tests/attend_ref.py, whose docstring derives the bounds."""
+import math
+
+import pytest
+
+import attend_ref as ref
+from paper_2312_11841_amd import mixrt
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+DT = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
+
+
+@pytest.fixture(scope="module")
+def r():
+    r = mixrt.Renderer(0, sync_check=True)
+    yield r
+    r.close()
+
+
+def say(*a):
+    print(*a, flush=True)
+
+
+def _gen(seed):
+    return torch.Generator().manual_seed(seed)
+
+
+def _inside(got, want, what):
+    want, bound = want
+    got = got.double().cpu()
+    assert got.shape == want.shape, what
+    over = (got - want).abs() - bound
+    assert bool((over <= 0).all()), (what, float(over.max()))
+
+
+# --- outputs that share memory ------------------------------------------------------------
+
+def _place(T, D, axes=1):
+    g = _gen(1)
+    return (torch.randint(0, 9, (T, axes), generator=g).float().cuda(),
+            torch.rand(D // 2, generator=g).cuda(), torch.zeros(D // 2).byte().cuda())
+
+
+def test_normed_heads_over_other_arrays_are_refused(r):
+    """Blocks would read what others have written: refused before the launch."""
+    g = _gen(2)
+    T, H, D = 9, 3, 16
+    place = _place(T, D)
+    buf = torch.randn((T + 1, H, D), generator=g).cuda()
+    x, late = buf[:T], buf[1:]
+    y, z = (torch.randn((T, H, D), generator=g).cuda() for _ in range(2))
+    w = torch.ones(D, device="cuda")
+    over = pytest.raises(mixrt.MixrtError, match="also another")
+    with over:
+        r.rotary_norm((x, y), None, *place, out=(y, x))
+    with over:
+        r.rotary_norm(x, None, *place, out=late)
+    with over:
+        r.rotary_norm(late, None, *place, out=x)
+    with over:
+        r.rotary_norm((x, y), None, *place, out=(z, z))
+    with over:
+        r.rotary_norm((x, x), None, *place, out=(x, z))
+    with over:      # the weight in the output
+        r.rotary_norm(x, y.view(-1)[:D], *place, out=y)
+    dy = torch.randn((T, H, D), generator=g).cuda()
+    with over:
+        r.rotary_norm_backward((dy, z), (x, y), None, *place, out=(y, torch.empty_like(z)))
+    with over:
+        r.rotary_norm_backward((dy, z), (x, y), None, *place, out=(z, dy))
+    with over:
+        r.rotary_norm_backward(late, z, w, *place, out=x)
+    kept = [t.clone() for t in (buf, y, z, dy)]
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(kept, (buf, y, z, dy)))
+
+
+def test_normed_heads_in_place_and_in_joint_arrays(r):
+    """In place, and beside the inputs in one array: what arrays of their own give."""
+    g = _gen(3)
+    T, D = 37, 16
+    place = _place(T, D)
+    w = torch.rand(D, generator=g).cuda()
+    joint = torch.randn((T, 4 + 4 + 2 + 2, D), generator=g).cuda()
+    q, qo, k, ko = joint.split([4, 4, 2, 2], 1)
+    want = r.rotary_norm((q, k), (w, w), *place)
+    inputs = [q.clone(), k.clone()]
+    got = r.rotary_norm((q, k), (w, w), *place, out=(qo, ko))
+    assert all(torch.equal(a, b) for a, b in zip((*got, q, k), (*want, *inputs)))
+    back = r.rotary_norm_backward((qo, ko), (q, k), (w, w), *place)
+    dy = (qo.clone(), ko.clone())
+    got = r.rotary_norm_backward(dy, (q, k), (w, w), *place, out=(qo, ko))
+    for a, b in zip((*got[0], *got[1]), (*back[0], *back[1])):
+        assert torch.equal(a, b)
+    got = r.rotary_norm_backward(dy, (q, k), (w, w), *place, out=dy)
+    assert all(torch.equal(a, b) for a, b in zip(got[0], back[0]))
+    got = r.rotary_norm((q, k), (w, w), *place, out=(q, k))
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_attention_over_its_lengths_or_places_is_refused(r):
+    g = _gen(4)
+    q = torch.randn((2, 9, 2, 16), generator=g).cuda()
+    out = torch.zeros((2, 9, 2, 16), device="cuda")
+    table = torch.randn((1, 4, 2), generator=g).cuda()
+    buckets = torch.randint(0, 4, (1, 7), generator=g).byte().cuda()
+    pos = torch.arange(9, device="cuda").int()[:, None]
+    flat = out.view(-1)
+    inside = flat[40:48].view(1, 4, 2)
+    whole = flat.view(torch.int32)
+    over = pytest.raises(mixrt.MixrtError, match="also another")
+    with over:
+        r.attention(q, q, q, lens=whole[5:7], out=out)
+    for bias in ((inside, buckets, pos, pos), (table, buckets, whole[:9, None], pos),
+                 (table, buckets, pos, whole[9:18, None]),
+                 (table, flat.view(torch.uint8)[3:10][None], pos, pos)):
+        with over:
+            r.attention(q, q, q, bias=mixrt.RelativeBias(*bias), out=out)
+    bias = mixrt.RelativeBias(table, buckets, pos, pos)
+    want = r.attention(q, q, q, bias=bias)
+    assert torch.equal(r.attention(q, q, q, bias=bias, out=out), want)
