@@ -558,7 +558,8 @@ typedef struct {
 } mixrt_rotary;
 
 /* Heads to turn: element (token, head, d) at token * token_stride +
- * head * head_stride + d; out may be x with x's strides. */
+ * head * head_stride + d; out may be x with x's strides, and else shares no memory
+ * with the call's other arrays (slices of one joint array will do). */
 typedef struct {
     int32_t heads;        /* >= 0, at most 65535 */
     int32_t head_dim;     /* 1..1024 */

@@ -5,6 +5,7 @@
 
 #include <cmath>
 
+#include "mixrt_apart.hpp"
 #include "mixrt_ctx.hpp"
 #include "mixrt_refine.hpp"
 
@@ -397,6 +398,24 @@ int mixrt_rotary_apply(mixrt_ctx *ctx, const mixrt_rotary *r, const mixrt_heads 
         L.a[L.n++] = mixrt::HeadsK{h.heads, h.head_dim, h.x, h.out, h.x_token_stride,
                                    h.x_head_stride, ot, oh};
     }
+    // blocks read heads while others write theirs: an output is its own array's input or
+    // shares no memory with another array
+    mixrt::Arrays m;
+    m.add(mixrt::flat_extent(r->pos, r->pairs ? r->tokens * r->axes * 4 : 0), "pos");
+    m.add(mixrt::flat_extent(r->freq, (int64_t)r->pairs * 4), "freq");
+    m.add(mixrt::flat_extent(r->axis, r->pairs), "axis");
+    for (int i = 0; i < L.n; ++i) {
+        const mixrt::HeadsK &h = L.a[i];
+        const int64_t size = elem_size(L.dtype);
+        auto extent = [&](const void *p, int64_t token, int64_t head) {
+            return mixrt::Extent{(uint64_t)(uintptr_t)p, h.D * size, {L.tokens, h.heads, 1},
+                                 {token * size, head * size, 0}};
+        };
+        if (h.x != h.out) m.add(extent(h.x, h.xt, h.xh), "x");
+        m.add(extent(h.out, h.ot, h.oh), "out", true);
+    }
+    if (const mixrt::Arrays::One *s = m.shared())
+        return fail(ctx, MIXRT_EINVAL, "%s is also another array, or a part of one", s->name);
     if ((rc = bind_device(ctx))) return rc;
     return finish_launch(ctx, mixrt::launch_rotary(L, ctx->stream), "rotary");
 }

@@ -102,6 +102,25 @@ def test_normed_heads_in_place_and_in_joint_arrays(r):
     assert all(torch.equal(a, b) for a, b in zip(got, want))
 
 
+def test_turned_heads_over_other_arrays_are_refused(r):
+    g = _gen(5)
+    T, H, D = 9, 3, 16
+    place = _place(T, D)
+    buf = torch.randn((T + 1, H, D), generator=g).cuda()
+    x, late = buf[:T], buf[1:]
+    y = torch.randn((T, H, D), generator=g).cuda()
+    kept = [t.clone() for t in (buf, y)]
+    for heads, out in (((x, y), (y, x)), (x, late), (late, x), ((x, x), (x, y)),
+                       ((x, late), (y, y))):
+        with pytest.raises(mixrt.MixrtError, match="also another"):
+            r.rotary(heads, *place, out=out)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(kept, (buf, y)))
+    want = r.rotary((x, y), *place)
+    got = r.rotary((x, y), *place, out=(x, y))
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
 def test_attention_over_its_lengths_or_places_is_refused(r):
     g = _gen(4)
     q = torch.randn((2, 9, 2, 16), generator=g).cuda()
