@@ -58,6 +58,22 @@ struct AttendPlan {
     int splits, per;
 };
 
+// A launch holds fewer than 2^32 threads in x: blocks of 256 that a kernel whose grid is
+// its work may have; the kernels that join splits walk over theirs in fewer.
+inline constexpr int64_t kMostBlocks256 = ((int64_t)1 << 24) - 1;
+inline constexpr int64_t kMostJoinBlocks = 1 << 16;
+inline int64_t join_blocks(int64_t blocks)
+{
+    return blocks < kMostJoinBlocks ? blocks : kMostJoinBlocks;
+}
+
+// Blocks of a stage's launch (a training forward call has 128 columns a block where
+// others have 256).
+inline int64_t attend_blocks(const AttendPlan &p, int B, int heads)
+{
+    return (int64_t)B * (heads / p.pack) * p.splits * p.blocks * (p.cols == 256 ? 2 : 1);
+}
+
 // LDS of the queries' gradient for the bias table's: a place an entry, and one more,
 // of each of its 128 columns (or four waves' 32).
 inline int attend_hist_bytes(int entries) { return 512 * (entries + 1); }

@@ -243,14 +243,16 @@ int check_attention(mixrt_ctx *ctx, const mixrt_attention *a, const mixrt_relati
     if (rows > 0 && ((a->queries > a->keys ? a->queries : a->keys) + 1) > kMaxTokens / rows)
         return fail(ctx, MIXRT_EUNSUPPORTED, "attention: 2^30 rows of heads or more");
     if (!aligned(a->lens, 4)) return fail(ctx, MIXRT_EINVAL, "attention.lens not 4-byte aligned");
-    // a grid's blocks are counted in 32 bits
+    int stage = 0;
     for (auto plan : {mixrt::plan_attend, mixrt::plan_attend_dq, mixrt::plan_attend_dkv}) {
         const AttendPlan p = plan(a->batch, a->heads, a->kv_heads, a->queries, a->keys,
                                   a->head_dim, a->dtype, b ? b->axes : 0,
                                   b ? b->axes * b->count : 0);
-        if (rows * p.blocks >= ((int64_t)1 << 30) / p.splits)
-            return fail(ctx, MIXRT_EUNSUPPORTED, "attention: %lld queries and %lld keys are too "
-                        "many blocks", (long long)a->queries, (long long)a->keys);
+        if (mixrt::attend_blocks(p, a->batch, stage++ == 2 ? a->kv_heads : a->heads) >
+            mixrt::kMostBlocks256)
+            return fail(ctx, MIXRT_EUNSUPPORTED, "attention: %d entries of %d heads, %lld queries "
+                        "and %lld keys are too many blocks", a->batch, a->heads,
+                        (long long)a->queries, (long long)a->keys);
     }
     return MIXRT_OK;
 }

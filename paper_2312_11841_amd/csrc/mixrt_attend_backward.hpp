@@ -750,18 +750,15 @@ __global__ __launch_bounds__(256) void attend_dkv_kernel(AttendK k)
 // parts, which follow.  (256 splits of 40 rows of 128, twice: one thread a quad 71 us,
 // 32 threads 6.7.)
 template <typename T, int G>
-__global__ __launch_bounds__(256) void attend_sum_kernel(const float *part, int splits, int B,
-                                                         int H, int Tn, int D, SeqK one, SeqK two)
+__device__ __forceinline__ void sum_quad(const float *part, int splits, int64_t rows, int H,
+                                         int Tn, int D, const SeqK &out, int64_t at,
+                                         float4 (&sums)[G > 1 ? 256 : 1])
 {
-    __shared__ float4 sums[G > 1 ? 256 : 1];
     const int quads = (D + 3) / 4;
-    const int64_t rows = (int64_t)B * H * Tn;
-    const int64_t at = (int64_t)blockIdx.x * (256 / G) + threadIdx.x % (256 / G);
     const int g = threadIdx.x / (256 / G);
     const bool there = at < rows * quads;
     const int64_t row = at / quads;
     const int d = (int)(at - row * quads) * 4;
-    const SeqK out = blockIdx.y ? two : one;
     float a[4] = {0, 0, 0, 0};
     if (there) {
         const float *p = part + ((int64_t)blockIdx.y * splits * rows + row) * D + d;
@@ -798,6 +795,21 @@ __global__ __launch_bounds__(256) void attend_sum_kernel(const float *part, int 
     const int t = (int)(row - bh * Tn), b = (int)(bh / H), h = (int)(bh - (int64_t)b * H);
     store_quad<T>((T *)out.data + b * out.batch + (int64_t)t * out.token + h * out.head, d, D, a[0],
                   a[1], a[2], a[3]);
+}
+
+template <typename T, int G>
+__global__ __launch_bounds__(256) void attend_sum_kernel(const float *part, int splits, int B,
+                                                         int H, int Tn, int D, SeqK one, SeqK two)
+{
+    constexpr int EACH = 256 / G;
+    __shared__ float4 sums[G > 1 ? 256 : 1];
+    const int64_t rows = (int64_t)B * H * Tn, all = rows * ((D + 3) / 4);
+    for (int64_t first = (int64_t)blockIdx.x * EACH; first < all;
+         first += (int64_t)gridDim.x * EACH) {
+        sum_quad<T, G>(part, splits, rows, H, Tn, D, blockIdx.y ? two : one,
+                       first + threadIdx.x % EACH, sums);
+        if (G > 1) __syncthreads();     // (sums are read to the end)
+    }
 }
 
 // dtable[axis][bucket][h] = sum over the parts of head h's blocks, in 64 bits: a block an
@@ -841,7 +853,7 @@ hipError_t launch_sum(const AttendK &k, int H, int64_t Tn, const SeqK &one, cons
     auto go = [&](auto g) {
         constexpr int G = decltype(g)::value, each = 256 / G;
         attend_sum_kernel<T, G>
-            <<<dim3((unsigned)((quads + each - 1) / each), n), 256, 0, stream>>>(
+            <<<dim3((unsigned)join_blocks((quads + each - 1) / each), n), 256, 0, stream>>>(
                 k.part, k.splits, k.B, H, (int)Tn, k.D, one, two);
     };
     if (k.splits > 8)

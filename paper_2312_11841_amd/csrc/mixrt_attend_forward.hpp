@@ -514,13 +514,10 @@ __global__ __launch_bounds__(256, kFlowWaves<DP>) void attend_flow_kernel(Attend
 // quads, G groups of them share its splits.  (With the splits of a row one after
 // another, the 113 of one token's 32 heads took 29 us.)
 template <typename T, int G>
-__global__ __launch_bounds__(256) void attend_join_kernel(AttendK k)
+__device__ __forceinline__ void join_row(const AttendK &k, int64_t row, float (&part)[5][256])
 {
-    constexpr int EACH = 32 / G;
-    __shared__ float part[5][256];
     const int64_t rows = (int64_t)k.B * k.H * k.Tq;
     const int lane = threadIdx.x & 7, g = threadIdx.x / 8 % G;
-    const int64_t row = (int64_t)blockIdx.x * EACH + threadIdx.x / (8 * G);
     const bool there = row < rows;
     const int d = 32 * blockIdx.y + 4 * lane;
     // the group's own maximum first: NaN stays
@@ -596,15 +593,31 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendK k)
     }
 }
 
+template <typename T, int G>
+__global__ __launch_bounds__(256) void attend_join_kernel(AttendK k)
+{
+    constexpr int EACH = 32 / G;
+    __shared__ float part[5][256];
+    const int64_t rows = (int64_t)k.B * k.H * k.Tq;
+    for (int64_t r0 = (int64_t)blockIdx.x * EACH; r0 < rows; r0 += (int64_t)gridDim.x * EACH) {
+        join_row<T, G>(k, r0 + threadIdx.x / (8 * G), part);
+        if (G > 1) __syncthreads();     // (part is read to the end)
+    }
+}
+
 template <typename T>
 hipError_t launch_join(const AttendK &k, hipStream_t stream)
 {
     const int64_t rows = (int64_t)k.B * k.H * k.Tq;
-    const unsigned by = (unsigned)(k.D + 31) / 32;
+    auto go = [&](auto g) {
+        constexpr int G = decltype(g)::value, EACH = 32 / G;
+        const unsigned bx = (unsigned)join_blocks((rows + EACH - 1) / EACH);
+        attend_join_kernel<T, G><<<dim3(bx, (unsigned)(k.D + 31) / 32), 256, 0, stream>>>(k);
+    };
     if (k.splits > 4)
-        attend_join_kernel<T, 32><<<dim3((unsigned)rows, by), 256, 0, stream>>>(k);
+        go(std::integral_constant<int, 32>());
     else
-        attend_join_kernel<T, 1><<<dim3((unsigned)((rows + 31) / 32), by), 256, 0, stream>>>(k);
+        go(std::integral_constant<int, 1>());
     return hipGetLastError();
 }
 

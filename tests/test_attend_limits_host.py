@@ -1,5 +1,6 @@
 """The attention kernels' limits, without a GPU: the order of what lanes pass to each
-other, and the rule that finds arrays which share memory."""
+other, the rule that finds arrays which share memory, and the sizes of launches."""
+import ctypes as C
 import os
 import random
 import re
@@ -8,7 +9,7 @@ import tempfile
 
 import pytest
 
-from paper_2312_11841_amd import build
+from paper_2312_11841_amd import build, mixrt
 
 
 def _compile(source, *flags):
@@ -129,3 +130,62 @@ def test_slices_of_one_joint_array_are_apart(apart):
              [(0, 100, 1, 1, 1, 0, 0, 0), (1, 100, 1, 1, 1, 0, 0, 0)],
              [(1, 100, 0, 1, 1, 5, 0, 0), (1, 100, 1, 1, 1, 0, 0, 0)]]
     assert apart(joint) == [(1, 1)] * len(joint)
+
+
+# --- grids ------------------------------------------------------------------------------
+
+GRIDS = r"""
+#include <cstdio>
+#include "mixrt_attend.hpp"
+int main()
+{
+    long long n;
+    printf("%lld\n", (long long)mixrt::kMostBlocks256);
+    while (scanf("%lld", &n) == 1) printf("%lld\n", (long long)mixrt::join_blocks(n));
+}
+"""
+
+
+def test_no_launch_holds_2_to_the_32_threads_in_x():
+    """The blocks of a call's kernels are bounded by its checks, those of the kernels that
+    join splits by their own walk, whatever their rows."""
+    if not os.path.exists(build.HIPCC):
+        pytest.skip("no hipcc")
+    rows = [1, 7, 65535, 65536, 65537, 2 ** 24, 2 ** 30, 32 * 2 ** 30]
+    with tempfile.TemporaryDirectory() as d:
+        src, exe = os.path.join(d, "g.cpp"), os.path.join(d, "g")
+        with open(src, "w") as f:
+            f.write(GRIDS)
+        subprocess.run([build.HIPCC, "-x", "hip", "--cuda-host-only", "-O1", "-I", build.INCLUDE,
+                        "-I", build.CSRC, src, "-o", exe], check=True, capture_output=True)
+        most, *got = map(int, subprocess.run([exe], input=" ".join(map(str, rows)), text=True,
+                                             capture_output=True, check=True).stdout.split())
+    assert most * 256 < 2 ** 32
+    for n, g in zip(rows, got):
+        assert 1 <= g <= n and g * 256 < 2 ** 32
+
+
+def _workspace(backward=0, **kw):
+    d = dict(batch=1, heads=16, kv_heads=16, head_dim=64, dtype=mixrt.MIXRT_F32, scale=0.125,
+             queries=100, keys=300, lens=0)
+    size = C.c_size_t(7)
+    rc = mixrt.lib().mixrt_attention_workspace(C.byref(mixrt.Attention(**{**d, **kw})), None,
+                                               backward, C.byref(size))
+    return rc, size.value
+
+
+@pytest.mark.parametrize("backward", [0, 1])
+def test_calls_of_too_many_blocks_are_refused_and_others_not(backward):
+    """A call of one query an entry and head has a block for each: 2^24 of them are more
+    than a launch holds.  Calls of many rows and long keys are not too many blocks."""
+    for kw in (dict(batch=2 ** 15, heads=512, kv_heads=512, queries=1, keys=8),
+               dict(batch=65535, heads=257, kv_heads=257, queries=2, keys=8),
+               dict(batch=2 ** 15, heads=1024, kv_heads=512, queries=1, keys=8)):
+        assert _workspace(backward, **kw) == (-4, 0), kw
+        assert b"too many blocks" in mixrt.lib().mixrt_thread_error()
+    for kw in (dict(batch=128, queries=8193, keys=8193),
+               dict(batch=16, queries=16385, keys=16385, head_dim=128),
+               dict(batch=65535, heads=128, kv_heads=128, queries=1, keys=8),
+               dict(batch=1024, queries=1, keys=9000),
+               dict(queries=65536, keys=65536, head_dim=128)):
+        assert _workspace(backward, **kw)[0] == 0, kw

@@ -142,3 +142,31 @@ def test_attention_over_its_lengths_or_places_is_refused(r):
     bias = mixrt.RelativeBias(table, buckets, pos, pos)
     want = r.attention(q, q, q, bias=bias)
     assert torch.equal(r.attention(q, q, q, bias=bias, out=out), want)
+
+
+# --- many rows ------------------------------------------------------------------------------
+
+def test_joins_of_more_rows_than_a_launch_has_blocks(r):
+    """Nine and more splits of half a million rows (forward, queries' gradient), and of as
+    many rows of keys, are joined by blocks that take several rows each.  All heads are
+    alike, so one head is held against the statement and the others have its bits."""
+    g = _gen(6)
+    for H, Hk, Tq, Tk, D in ((8192, 1, 64, 16500, 5), (8256, 8256, 17000, 64, 2)):
+        say("heads", H, Hk, "queries", Tq, "keys", Tk)
+        q, dout = (torch.randn((1, Tq, 1, D), generator=g) for _ in range(2))
+        k, v = (torch.randn((1, Tk, 1, D), generator=g) for _ in range(2))
+        cq, cd = (t.cuda().expand(-1, -1, H, -1) for t in (q, dout))
+        ck, cv = (t.cuda().expand(-1, -1, Hk, -1) for t in (k, v))
+        o, saved = r.attention_train(cq, ck, cv)
+        dq, dk, dv = r.attention_backward(cd, cq, ck, cv, o, saved)
+        want = ref.attention(q, k, v, torch.float32, dout=dout)
+        for name, got in (("o", o), ("dq", dq), ("dk", dk), ("dv", dv)):
+            assert torch.equal(got, got[:, :, :1].expand_as(got)), name
+            value, bound = want[name]
+            if name in ("dk", "dv"):
+                # the sum over a group's equal heads: a head's bound holds (Tq + 64) u of
+                # the magnitudes' sum for its sums, and chains of 2048 rows and their
+                # joins are at most 20 times 64 + 64
+                share = H // Hk
+                value, bound = share * value, share * bound * (20 if share > 1 else 1)
+            _inside(got[:, :, :1], (value, bound), name)
