@@ -90,12 +90,14 @@ __device__ __forceinline__ void clear(f32x16 (&a)[NC][ND])
 
 // float16 holds dS only inside a range: its gradients are small where a row looks at
 // many keys, and large where a loss is scaled.  So each column's dS is multiplied by a
-// power of two that keeps the largest seen so far between 1 and 2^15, and its sums
-// with it.  (The first tile sets it; it changes again where a later one leaves the
-// range.)
+// power of two that brings the largest seen so far to 2^8..2^9 when it is chosen, and
+// its sums with it; it is chosen anew where that one leaves 1..2^15.  (The first tile
+// sets it, later ones seldom.)  The power is at most 2^100, and follows from the
+// largest dS itself and not from a product with the last power, which may not be
+// finite: a key may get weights of 2^-125 from the first queries and 1/2 from the next.
 template <typename T, int NC, int ND>
 struct Lift {
-    float by[NC], most[NC];
+    float by[NC], most[NC];     // the power; the largest |dS| so far
     __device__ __forceinline__ void start()
     {
 #pragma unroll
@@ -112,21 +114,23 @@ struct Lift {
             float m = 0.0f;
 #pragma unroll
             for (int i = 0; i < 16; ++i) m = fmaxf(m, fabsf(g[n][i]));
-            m = fmaxf(most[n], half_max(m) * by[n]);
-            const bool out = (m > 0x1p15f || (m < 1.0f && m > 0.0f)) && m < INFINITY;
+            m = fmaxf(most[n], half_max(m));
+            most[n] = m;
+            // (a product that is not finite is out of range too; an m that is not has no
+            // power)
+            const float lifted = m * by[n];
+            const bool out = (lifted > 0x1p15f || (lifted < 1.0f && m > 0.0f)) && m < INFINITY;
             if (__builtin_amdgcn_ballot_w64(out) != 0 && out) {
                 const int now = (int)(__float_as_uint(by[n]) >> 23);
-                const int to = min(max(now + 127 + 8 - (int)(__float_as_uint(m) >> 23), 27), 227);
+                const int to = min(max(127 + 127 + 8 - (int)(__float_as_uint(m) >> 23), 27), 227);
                 const float f = __uint_as_float((uint32_t)(127 + (to - now) / 2) << 23);
                 const float e = __uint_as_float((uint32_t)(127 + (to - now) - (to - now) / 2) << 23);
-                by[n] = by[n] * f * e;
-                m = m * f * e;
+                by[n] = __uint_as_float((uint32_t)to << 23);
 #pragma unroll
                 for (int d = 0; d < ND; ++d)
 #pragma unroll
                     for (int i = 0; i < 16; ++i) acc[n][d][i] = acc[n][d][i] * f * e;
             }
-            most[n] = m;
 #pragma unroll
             for (int i = 0; i < 16; ++i) g[n][i] *= by[n];
         }

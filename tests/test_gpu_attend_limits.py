@@ -170,3 +170,54 @@ def test_joins_of_more_rows_than_a_launch_has_blocks(r):
                 share = H // Hk
                 value, bound = share * value, share * bound * (20 if share > 1 else 1)
             _inside(got[:, :, :1], (value, bound), name)
+
+
+# --- the ends of float16's range ----------------------------------------------------------
+
+@pytest.mark.parametrize("wide", [False, True])
+def test_float16_gradients_that_jump_from_tile_to_tile(r, wide):
+    """Keys that get weights of 2^-125 from the first queries and one half from the last,
+    at a loss scaled by 2^15; queries whose first keys are as far and whose last are
+    near: their gradients are finite and keep their accuracy.  A call with few columns
+    and one with many (copies of the same heads)."""
+    H = 130 if wide else 1
+    for jump in ("queries", "keys"):
+        D = 8
+        if jump == "queries":
+            q = torch.zeros((1, 200, 1, D))
+            k, v = torch.zeros((1, 70, 1, D)), torch.zeros((1, 70, 1, D))
+            q[0, :197, 0, 0] = -43.0 * 2 ** 7
+            q[0, :, 0, 1] = 0.25
+            k[0, ::2, 0, 0], k[0, 1::2, 0, 0] = 2.0 ** -7, -2.0 ** -7
+            v[0, ::2, 0, 2], v[0, 1::2, 0, 2] = 64.0, -64.0
+            dout = torch.ones((1, 200, 1, D))
+            dout[0, 197:] = 2.0 ** 15
+            scale = 1.0
+        else:
+            q, dout = torch.zeros((1, 70, 1, D)), torch.full((1, 70, 1, D), 2.0 ** 15)
+            k, v = torch.zeros((1, 202, 1, D)), torch.zeros((1, 202, 1, D))
+            q[..., 0] = 30000.0
+            k[0, :200, 0, 0] = -12.0
+            k[0, 200, 0, 1], k[0, 201, 0, 1] = 2.0 ** -5, -2.0 ** -5
+            v[0, 200], v[0, 201] = 2.0 ** 14, -2.0 ** 14
+            scale = 2.0 ** -12
+        say(jump, H)
+        dt = torch.float16
+        q, k, v, dout = (t.to(dt) for t in (q, k, v, dout))
+        want = ref.attention(q, k, v, dt, scale=scale, dout=dout)
+        q, k, v, dout = (t.cuda().expand(-1, -1, H, -1) for t in (q, k, v, dout))
+        o, saved = r.attention_train(q, k, v, scale=scale)
+        grads = r.attention_backward(dout, q, k, v, o, saved, scale=scale)
+        for name, got in zip(("dq", "dk", "dv"), grads):
+            if jump == "keys" and name != "dq":
+                continue            # (70 queries' 2^14: out of float16's range)
+            assert float(want[name][0].abs().max()) < 65504
+            _inside(got[:, :, :1], want[name], (jump, name))
+            assert torch.equal(got, got[:, :, :1].expand_as(got))
+            exact = want[name][0]
+            if float(exact.norm()) == 0:
+                continue
+            off = float((got[:, :, :1].double().cpu() - exact).norm() / exact.norm())
+            say(name, off)
+            # a term's rounding and the result's, half a step each
+            assert off <= 2.0 ** -10, (jump, name)
