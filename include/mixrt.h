@@ -670,7 +670,7 @@ int mixrt_attention_workspace(const mixrt_attention *att, const mixrt_relative_b
  * [queries], or NULL): log2 of the sum of 2^(S log2(e)) of each row, +infinity
  * for a row without keys; rest (device [batch][queries][heads][head_dim] of
  * dtype's size, or NULL; F16 and BF16 only): what rounding took from out, in F16
- * times 4096, in BF16 as the difference of the bits, a 16-bit integer.  bias: NULL
+ * times 2048, in BF16 as the difference of the bits, a 16-bit integer.  bias: NULL
  * for none. */
 int mixrt_attention_forward(mixrt_ctx *ctx, const mixrt_attention *att,
                             const mixrt_relative_bias *bias, const mixrt_sequence *q,

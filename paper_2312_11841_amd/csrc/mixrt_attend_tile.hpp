@@ -340,8 +340,9 @@ __device__ __forceinline__ int valid_keys(const int32_t *lens, int b, int Tk)
 
 constexpr float kLog2e = 1.4426950408889634f;
 // What is left of o when it is rounded to T, for the backward pass (nothing of an o
-// that is not finite), in T's bits: of float16's 13 lost bits 11, times 4096 so that it
-// is not subnormal; of bfloat16's 16, whose exponent is o's own, all of them, as the
+// that is not finite), in T's bits: of float16's 13 lost bits 11, times 2048: it is then
+// subnormal only where o is below 2^-14, and at most 2^15 (half a step of an o below
+// 65520 is 16; times 4096 that would not be finite); of bfloat16's 16, whose exponent is o's own, all of them, as the
 // difference of the bits.  (Rounded to bfloat16, which keeps 8, it was most of the
 // error of a bias table's gradient.)
 template <typename T>
@@ -353,7 +354,7 @@ __device__ __forceinline__ T rest_of(float o)
         const uint32_t n = __float_as_uint(o) - __float_as_uint((float)x);
         return __builtin_bit_cast(bf16, (int16_t)min(max((int)n, -32768), 32767));
     } else {
-        return (T)((o - (float)x) * 4096.0f);
+        return (T)((o - (float)x) * 2048.0f);
     }
 }
 
@@ -365,7 +366,7 @@ __device__ __forceinline__ float whole_of(T x, T rest)
         return __uint_as_float(__float_as_uint((float)x) +
                                (uint32_t)(int)__builtin_bit_cast(int16_t, rest));
     else
-        return (float)x + (float)rest * (1.0f / 4096.0f);
+        return (float)x + (float)rest * (1.0f / 2048.0f);
 }
 
 // What is left of four elements of a column's result to a dense row of D.

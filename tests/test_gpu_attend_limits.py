@@ -221,3 +221,29 @@ def test_float16_gradients_that_jump_from_tile_to_tile(r, wide):
             say(name, off)
             # a term's rounding and the result's, half a step each
             assert off <= 2.0 ** -10, (jump, name)
+
+
+@pytest.mark.parametrize("wide", [False, True])
+def test_float16_outputs_whose_rounding_is_large(r, wide):
+    """Outputs of 32768 and more are rounded by up to 16: what that takes is kept for the
+    gradients in float16, and finite.  Two keys of one score with values 32768 and 32800
+    have 32784 between them, a tie."""
+    g = _gen(8)
+    H, Tq, D, dt = 130 if wide else 1, 70, 16, torch.float16
+    q = (0.3 * torch.randn((1, Tq, 1, D), generator=g)).to(dt)
+    k = torch.zeros((1, 2, 1, D), dtype=dt)
+    v = torch.tensor([32768.0, 32800.0]).view(1, 2, 1, 1).expand(1, 2, 1, D).to(dt).clone()
+    k[0, 1, 0, 8:] = 2.0 ** -6
+    q[..., :10, :, 8:] = 0
+    q[:, :10] = 0
+    v[..., 1::2] *= -1.9
+    dout = (2.0 ** -10 * torch.randn((1, Tq, 1, D), generator=g)).to(dt)
+    want = ref.attention(q, k, v, dt, dout=dout)
+    q, k, v, dout = (t.cuda().expand(-1, -1, H, -1) for t in (q, k, v, dout))
+    o, saved = r.attention_train(q, k, v)
+    assert bool(torch.isfinite(saved.rest).all()) and bool(torch.isfinite(o).all())
+    assert float(saved.rest.abs().max()) == 2.0 ** 15
+    _inside(o[:, :, :1], want["o"], "o")
+    for name, got in zip(("dq", "dk", "dv"), r.attention_backward(dout, q, k, v, o, saved)):
+        _inside(got[:, :, :1], want[name], name)
+        assert torch.equal(got, got[:, :, :1].expand_as(got))
