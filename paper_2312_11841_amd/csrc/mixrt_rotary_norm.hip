@@ -169,6 +169,9 @@ __device__ __forceinline__ float group_sum(float x, int n)
 // 1 / sqrt(mean of squares + eps) of a head in the registers of its group, with
 // squares that leave the range of 32 bits kept inside it: then the elements are
 // first multiplied by a power of two, pre (1 else), which the caller's x holds too.
+// It is about 1 over the larger of the largest element and sqrt(eps), so that neither
+// the squares nor eps pre^2 leave the range (elements far below sqrt(eps) do not count
+// beside it).
 template <int M, int V>
 __device__ __forceinline__ float rms(float (&x)[M][2 * V], int lanes_log2, int D, float eps, float &pre)
 {
@@ -189,8 +192,8 @@ __device__ __forceinline__ float rms(float (&x)[M][2 * V], int lanes_log2, int D
             for (int i = 0; i < 2 * V; ++i) most = fmaxf(most, fabsf(x[m][i]));
         most = group_join(most, lanes_log2, [](float a, float b) { return fmaxf(a, b); });
         if (far) {
-            const int e = (int)(__float_as_uint(most) >> 23);
-            pre = __uint_as_float((uint32_t)min(max(254 - e, 1), 253) << 23);   // about 1 / most
+            const int e = (int)(__float_as_uint(fmaxf(most, sqrtf(eps))) >> 23);
+            pre = __uint_as_float((uint32_t)min(max(254 - e, 1), 253) << 23);
             ss = 0.0f;
         }
 #pragma unroll

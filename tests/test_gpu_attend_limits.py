@@ -247,3 +247,33 @@ def test_float16_outputs_whose_rounding_is_large(r, wide):
     for name, got in zip(("dq", "dk", "dv"), r.attention_backward(dout, q, k, v, o, saved)):
         _inside(got[:, :, :1], want[name], name)
         assert torch.equal(got, got[:, :, :1].expand_as(got))
+
+
+# --- small epsilons -------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("log2", [-60, -79, -80, -81, -100, -120, -126, -140, -149])
+def test_normed_heads_with_a_small_epsilon(r, dtype, log2):
+    """Heads of zeros, of elements far below sqrt(eps), about it and far above, down to
+    the smallest epsilon there is: the head's size is that of eps where eps is larger."""
+    dt, eps = DT[dtype], 2.0 ** log2
+    g = _gen(9)
+    sizes = [0.0, 2.0 ** -140, 2.0 ** -126, 2.0 ** -115, 2.0 ** (log2 // 2 - 20),
+             2.0 ** (log2 // 2), 2.0 ** (log2 // 2 + 9), 2.0 ** -20, 1.0, 2.0 ** 14]
+    T, D = len(sizes), 48
+    x = torch.randn((T, 2, D), generator=g).clamp(-4, 4).double()
+    x = (x * torch.tensor(sizes).double()[:, None, None]).float().to(dt)
+    dy = torch.randn((T, 2, D), generator=g).to(dt)
+    w = 1 + 0.3 * torch.randn((D,), generator=g)
+    pos = torch.arange(float(T))[:, None]
+    freq, axis = torch.rand(D // 2, generator=g), torch.zeros(D // 2, dtype=torch.uint8)
+    place = (pos.cuda(), freq.cuda(), axis.cuda())
+    got = r.rotary_norm(x.cuda(), w.cuda(), *place, eps=eps)
+    _inside(got, ref.rotary_norm(x, w, pos, freq, axis, "halves", eps, dt), "out")
+    dx, dw = r.rotary_norm_backward(dy.cuda(), x.cuda(), w.cuda(), *place, eps=eps)
+    want, bound = ref.rotary_norm_back(dy, x, w, pos, freq, axis, "halves", eps, dt)
+    fits = want[0].abs() < 0.9 * torch.finfo(dt).max        # (others round to infinity)
+    off = (dx.double().cpu() - want[0]).abs()
+    assert bool((off <= bound[0])[fits].all()) and bool(fits.any())
+    assert bool((dx[0].float().abs() > 2.0 ** min(14, -log2 // 2 - 12)).any())
+    _inside(dw, (want[1], bound[1]), "dw")
