@@ -114,13 +114,12 @@ __device__ __forceinline__ void finish(const AttendK &k, const ForwardWork &w,
 // A new maximum of a column's scores (in units of log2) becomes the base of its weights
 // only where weights on the old one would pass 2^8: then the sums so far are brought to
 // it.  That is the first tile and few others.
-constexpr float kSlack = 8.0f;
+constexpr float kMost = 8.0f;
 template <int ND>
 __device__ __forceinline__ void rebase(float m, float &top, float &sum, f32x16 (&acc)[ND])
 {
-    const bool out = m > top + kSlack;
-    if (__builtin_amdgcn_ballot_w64(out) == 0) return;
-    if (out) {
+    // (the difference is exact where a large base makes the sum base + kMost round up)
+    if (m - top > kMost) {
         const float less = __builtin_amdgcn_exp2f(top - m);
         sum *= less;
 #pragma unroll
@@ -129,6 +128,20 @@ __device__ __forceinline__ void rebase(float m, float &top, float &sum, f32x16 (
             for (int i = 0; i < 16; ++i) acc[d][i] *= less;
         top = m;
     }
+}
+
+// Whether a wave's bases are so large that the product with unit, which a weight's
+// exponent does not round, has to be rounded as the maximum's is: else a weight could
+// pass its type's largest number by the maximum's rounding alone, from scores of 2^27 on
+// in float16, of 2^31 in 32 bits.  The scores are then rounded, and their unit is 1.
+__device__ __forceinline__ bool far_base(float top)
+{
+    return __builtin_amdgcn_ballot_w64(fabsf(top) >= 0x1p22f) != 0;
+}
+__device__ __forceinline__ void round_scores(f32x16 &s, float unit)
+{
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[i] *= unit;
 }
 
 // The weights of a block of 32 rows, in place of the scores: 2^(s unit - base).
@@ -284,6 +297,7 @@ __global__ __launch_bounds__(256) void attend_kernel(AttendK k)
     if (SHARED && BIAS) __syncthreads();    // (the bias is the block's)
     team.meet();
     int cur = 0;
+    bool far = false;       // (of the whole wave)
     for (int row0 = row1; row0 < w.last; row0 += STEP, cur ^= BUFS - 1) {
         const bool more = row0 + STEP < w.last;
         if (more && AHEAD) fetch(row0 + STEP);
@@ -293,9 +307,13 @@ __global__ __launch_bounds__(256) void attend_kernel(AttendK k)
             add_bias<NC, ROWS>(s, k.scale, kpos[me][cur], 0, half, dense, hbase, qpos,
                                k.bias.axes, k.bias.reach);
         if (row0 + ROWS > w.last) cut_rows(s[0], row0, half, w.last);
-        const float unit = BIAS ? 1.0f : k.scale;
-        rebase(most_of(s[0]) * unit, top[0], sum[0], acc[0]);
-        weigh(s[0], unit, top[0], sum[0]);
+        const float unit = BIAS ? 1.0f : k.scale, m = most_of(s[0]) * unit;
+        if (far || __builtin_amdgcn_ballot_w64(m > top[0] + kMost) != 0) {
+            rebase(m, top[0], sum[0], acc[0]);
+            far = !BIAS && far_base(top[0]);
+        }
+        if (far) round_scores(s[0], unit);
+        weigh(s[0], far ? 1.0f : unit, top[0], sum[0]);
         if constexpr (sizeof(T) == 4) {
 #pragma unroll
             for (int d = 0; d < DP / 32; ++d) col_mul<DP>(vt, lane, d, s[0], acc[0][d]);
@@ -432,6 +450,7 @@ __global__ __launch_bounds__(256, kFlowWaves<DP>) void attend_flow_kernel(Attend
             }
     };
     const float unit = BIAS ? 1.0f : k.scale;
+    bool far = false;       // (of the whole wave)
     // the values that p waits for: none yet
     const T *held = nothing;
 #pragma unroll
@@ -458,15 +477,23 @@ __global__ __launch_bounds__(256, kFlowWaves<DP>) void attend_flow_kernel(Attend
 #pragma unroll
             for (int n = 0; n < NC; ++n) {
                 m[n] = most_of(s[n]) * unit;
-                out = out || m[n] > top[n] + kSlack;
+                out = out || m[n] > top[n] + kMost;
             }
-            if (__builtin_amdgcn_ballot_w64(out) != 0) {
+            if (far || __builtin_amdgcn_ballot_w64(out) != 0) {
                 // the values that wait have weights on the old base
                 add_values(held);
                 held = nothing;
+                far = false;
 #pragma unroll
-                for (int n = 0; n < NC; ++n) rebase(m[n], top[n], sum[n], acc[n]);
+                for (int n = 0; n < NC; ++n) {
+                    rebase(m[n], top[n], sum[n], acc[n]);
+                    far = far || (!BIAS && far_base(top[n]));
+                }
+                if (far)
+#pragma unroll
+                    for (int n = 0; n < NC; ++n) round_scores(s[n], unit);
             }
+            const float by = far ? 1.0f : unit;
             const T *next = u + 1 < SUBS ? ktiles[k0] + 32 * (u + 1) * kStride<T, DP> : ktiles[k1];
             f32x16 s2[NC];
 #pragma unroll
@@ -474,7 +501,7 @@ __global__ __launch_bounds__(256, kFlowWaves<DP>) void attend_flow_kernel(Attend
             add_values(held);
 #pragma unroll
             for (int n = 0; n < NC; ++n) {
-                weigh(s[n], unit, top[n], sum[n]);
+                weigh(s[n], by, top[n], sum[n]);
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
                     split_rows<T>(s[n], e, p[n][e]);

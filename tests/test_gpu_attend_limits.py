@@ -277,3 +277,30 @@ def test_normed_heads_with_a_small_epsilon(r, dtype, log2):
     assert bool((off <= bound[0])[fits].all()) and bool(fits.any())
     assert bool((dx[0].float().abs() > 2.0 ** min(14, -log2 // 2 - 12)).any())
     _inside(dw, (want[1], bound[1]), "dw")
+
+
+# --- weights of any size --------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("shape", [(3, 40, 1), (130, 100, 130), (300, 100, 520)], ids=str)
+def test_scores_of_any_size(r, shape, dtype):
+    """Scores far beyond 2^24 (their roundings are more than a weight's whole range): each
+    query's best key, ahead by more than that, is its output, and nothing is infinite."""
+    dt = DT[dtype]
+    Tq, Tk, H = shape
+    g = _gen(10)
+    D = 16
+    size = {"f32": 1e15, "bf16": 1e15, "f16": 6e4}[dtype]
+    q = torch.randn((1, Tq, 1, D), generator=g).clamp(-1, 1).mul(size).to(dt)
+    k = torch.randn((1, Tk, 1, D), generator=g).clamp(-1, 1).mul(size).to(dt)
+    v = torch.randn((1, Tk, 1, D), generator=g).to(dt)
+    s = q[0, :, 0].double() @ k[0, :, 0].double().T
+    best, second = s.topk(2, 1).values.unbind(1)
+    clear = (best - second) > 1e-3 * best.abs()
+    assert float(clear.float().mean()) > 0.5
+    want = v[0, s.argmax(1), 0].float()
+    cq, ck, cv = (t.cuda().expand(-1, -1, H, -1) for t in (q, k, v))
+    for o in (r.attention(cq, ck, cv, scale=1.0), r.attention_train(cq, ck, cv, scale=1.0)[0]):
+        assert bool(torch.isfinite(o).all())
+        assert torch.equal(o, o[:, :, :1].expand_as(o))
+        assert torch.equal(o[0, clear.cuda(), 0].float().cpu(), want[clear])
