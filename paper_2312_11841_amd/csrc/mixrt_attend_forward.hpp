@@ -111,28 +111,39 @@ __device__ __forceinline__ void finish(const AttendK &k, const ForwardWork &w,
     }
 }
 
-// A new maximum of a column's scores (in units of log2) becomes the base of its weights
-// only where weights on the old one would pass 2^8: then the sums so far are brought to
-// it.  That is the first tile and few others.
-constexpr float kMost = 8.0f;
-template <int ND>
+// Weights are 2^(score - base), scores in units of log2.  float16 holds few powers of
+// two: there the base lies below the largest score when it is chosen, by 7, or by 11
+// where the output is trained on (EXACT), so that a weight counts down to 2^-32 or 2^-36
+// of the largest one's.  (Below half of float16's least, 2^-24, it is 0 in the product
+// with the values, and not in the weights' sum: on a base at the largest score 32,768
+// keys of 2^-26 beside one large key took 0.05% off the row.)  A walk adds at most
+// 32,768 keys, so what is lost is at most 2^-17 or 2^-21 of a row.  3600 queries over
+// 14,400 keys, 8 heads of 64: the same time with 7, with 11 155 to 172 us, as bases move
+// more often.
+template <typename T, bool EXACT>
+inline constexpr float kLow = !std::is_same_v<T, f16> ? 0.0f : EXACT ? 11.0f : 7.0f;
+// A new maximum moves the base only where weights on the old one would pass 2^8 (in
+// float16 2^15): then the sums so far are brought to it.  That is the first tile and
+// few others.
+template <typename T> inline constexpr float kMost = std::is_same_v<T, f16> ? 15.0f : 8.0f;
+template <typename T, bool EXACT, int ND>
 __device__ __forceinline__ void rebase(float m, float &top, float &sum, f32x16 (&acc)[ND])
 {
     // (the difference is exact where a large base makes the sum base + kMost round up)
-    if (m - top > kMost) {
-        const float less = __builtin_amdgcn_exp2f(top - m);
+    if (m - top > kMost<T>) {
+        const float to = m - kLow<T, EXACT>, less = __builtin_amdgcn_exp2f(top - to);
         sum *= less;
 #pragma unroll
         for (int d = 0; d < ND; ++d)
 #pragma unroll
             for (int i = 0; i < 16; ++i) acc[d][i] *= less;
-        top = m;
+        top = to;
     }
 }
 
 // Whether a wave's bases are so large that the product with unit, which a weight's
 // exponent does not round, has to be rounded as the maximum's is: else a weight could
-// pass its type's largest number by the maximum's rounding alone, from scores of 2^27 on
+// pass its type's largest number by the maximum's rounding alone, from scores of 2^23 on
 // in float16, of 2^31 in 32 bits.  The scores are then rounded, and their unit is 1.
 __device__ __forceinline__ bool far_base(float top)
 {
@@ -308,8 +319,8 @@ __global__ __launch_bounds__(256) void attend_kernel(AttendK k)
                                k.bias.axes, k.bias.reach);
         if (row0 + ROWS > w.last) cut_rows(s[0], row0, half, w.last);
         const float unit = BIAS ? 1.0f : k.scale, m = most_of(s[0]) * unit;
-        if (far || __builtin_amdgcn_ballot_w64(m > top[0] + kMost) != 0) {
-            rebase(m, top[0], sum[0], acc[0]);
+        if (far || __builtin_amdgcn_ballot_w64(m > top[0] + kMost<T>) != 0) {
+            rebase<T, EXACT>(m, top[0], sum[0], acc[0]);
             far = !BIAS && far_base(top[0]);
         }
         if (far) round_scores(s[0], unit);
@@ -477,7 +488,7 @@ __global__ __launch_bounds__(256, kFlowWaves<DP>) void attend_flow_kernel(Attend
 #pragma unroll
             for (int n = 0; n < NC; ++n) {
                 m[n] = most_of(s[n]) * unit;
-                out = out || m[n] > top[n] + kMost;
+                out = out || m[n] > top[n] + kMost<T>;
             }
             if (far || __builtin_amdgcn_ballot_w64(out) != 0) {
                 // the values that wait have weights on the old base
@@ -486,7 +497,7 @@ __global__ __launch_bounds__(256, kFlowWaves<DP>) void attend_flow_kernel(Attend
                 far = false;
 #pragma unroll
                 for (int n = 0; n < NC; ++n) {
-                    rebase(m[n], top[n], sum[n], acc[n]);
+                    rebase<T, EXACT>(m[n], top[n], sum[n], acc[n]);
                     far = far || (!BIAS && far_base(top[n]));
                 }
                 if (far)

@@ -1500,7 +1500,9 @@ class Renderer:
         128; slices of a joint projection will do); kv_heads divides heads.
         lens: int32 [batch], the valid keys of each entry (what lies behind is
         never read; an entry without keys gives 0); bias: a RelativeBias; scale:
-        1 / sqrt(D) by default.  out: q's shape and type."""
+        1 / sqrt(D) by default.  out: q's shape and type.  float16 and bfloat16
+        round a weight to their bits before its product with v (float16 holds it
+        down to 2^-32 of the row's largest); sums are in 32 bits."""
         p = self._attention_plan(q, k, v, lens, bias, scale, False)
         table = None if bias is None else bias.table
         if out is not None:
@@ -1512,9 +1514,9 @@ class Renderer:
 
     def attention_train(self, q, k, v, *, lens=None, bias=None, scale=None, out=None):
         """(out, saved) for a training step: attention's out, whose weights float16
-        and bfloat16 hold here to twice their bits (a row that looks at few keys
-        would else get the roundings as its gradient), and what attention_backward
-        needs besides (an AttentionSaved)."""
+        and bfloat16 hold here to twice their bits, float16 down to 2^-36 of a row's
+        largest (a row that looks at few keys would else get the roundings as its
+        gradient), and what attention_backward needs besides (an AttentionSaved)."""
         p = self._attention_plan(q, k, v, lens, bias, scale, False)
         table = None if bias is None else bias.table
         if out is not None:

@@ -281,6 +281,48 @@ def test_normed_heads_with_a_small_epsilon(r, dtype, log2):
 
 # --- weights of any size --------------------------------------------------------------------
 
+def _one_large_key(n, log2, large, at):
+    """One query and n + 1 keys of width 16: one of score 0, n of log2 log 2, their values
+    1 and large; the large one at place `at`."""
+    q = torch.zeros((1, 1, 1, 16))
+    q[..., 0] = 4.0
+    k, v = torch.zeros((1, n + 1, 1, 16)), torch.full((1, n + 1, 1, 16), float(large))
+    k[..., 0] = log2 * math.log(2)
+    k[0, at], v[0, at] = 0.0, 1.0
+    return q, k, v
+
+
+@pytest.mark.parametrize("heads,queries", [(1, 1), (520, 130)])
+def test_many_small_weights_beside_a_large_one_in_float16(r, heads, queries):
+    """Keys whose weights float16 cannot hold beside a larger one's are in the sum of
+    weights, so they have to be in the sum of values: 20,000 of 2^-26 (with their values
+    0.03 of 1) to 2^-33, in calls of one query and of many blocks.  Bound: a weight is
+    held to 2^-11 (to 2^-22 in training), or to half of 2^-24 / 2^7 of the largest (in training 2^-24 / 2^11), the
+    base's distance from it; 32-bit sums and scores, whose error is at most (16 + 32) u
+    times what their terms' sizes add up to."""
+    n, dt = 20000, torch.float16
+    for log2, large, at in ((-26, 100.0, 0), (-26, 100.0, n), (-30, 1000.0, 77),
+                            (-33, 60000.0, 0)):
+        q, k, v = (t.to(dt) for t in _one_large_key(n, log2, large, at))
+        s = (q[0, 0, 0, 0].double() * k[0, :, 0, 0].double()) / 4
+        p = torch.exp(s)
+        p = p / p.sum()
+        value = float((p * v[0, :, 0, 0].double()).sum())
+        sizes = p * v[0, :, 0, 0].double().abs()
+        off32 = float((sizes * (48 * ref.U * (s.abs() + 2))).sum()) + (n + 64) * ref.U * float(
+            sizes.sum())
+        cq = q.cuda().expand(1, queries, heads, -1)
+        ck, cv = (t.cuda().expand(-1, -1, heads, -1) for t in (k, v))
+        for train in (False, True):
+            o = r.attention_train(cq, ck, cv)[0] if train else r.attention(cq, ck, cv)
+            least = 2.0 ** (-36 if train else -32)
+            bound = off32 + least * float(v.double().abs().sum()) / 16 + 2.0 ** -11 * abs(value)
+            bound += 2.0 ** (-22 if train else -11) * float(sizes.sum())
+            off = (o.double() - value).abs().max()
+            say(heads, log2, large, train, f"{value:.6f} off {float(off):.2e} of {bound:.2e}")
+            assert float(off) <= bound
+
+
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
 @pytest.mark.parametrize("shape", [(3, 40, 1), (130, 100, 130), (300, 100, 520)], ids=str)
 def test_scores_of_any_size(r, shape, dtype):
