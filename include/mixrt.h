@@ -637,7 +637,9 @@ typedef struct {
 
 /* A learned bias by the buckets of relative positions: with the distance
  * d = k_pos[j][a] - q_pos[i][a] of each axis, cut to -reach .. reach,
- *   bias_ij of head h = sum over axes of table[a][buckets[a][d + reach]][h]. */
+ *   bias_ij of head h = sum over axes of table[a][buckets[a][d + reach]][h].
+ * A finite entry counts as at most 2^124 in size (a mask of the lowest float is
+ * finite: a row of nothing else has equal weights; -infinity leaves a pair out). */
 typedef struct {
     int32_t axes;             /* 1..MIXRT_MAX_BIAS_AXES */
     int32_t count;            /* buckets of an axis, 1..MIXRT_MAX_BIAS_BUCKETS */

@@ -415,15 +415,20 @@ __device__ __forceinline__ int bucket_of(const BiasK &b, int axis, int entry, bo
                b.buckets - 1);
 }
 
-// bias[entry] of head's axes, times log2(e).
+// bias[entry] of head's axes, times log2(e), a finite one at most 2^125: a mask of the
+// lowest float has to stay finite there, and where the axes' are added.
+constexpr float kMostBias = 0x1p125f;
 __device__ __forceinline__ void load_bias(float *dense, const BiasK &b, int head, int H,
                                           int thread, int threads, bool mirrored)
 {
     const int n = 2 * b.reach + 1 + 2 * kPad;
     for (int i = thread; i < b.axes * n; i += threads) {
         const int a = i / n, e = i - a * n;
-        dense[a * kReachRow + e] =
-            b.table[((int64_t)a * b.buckets + bucket_of(b, a, e, mirrored)) * H + head] * kLog2e;
+        const float entry =
+            b.table[((int64_t)a * b.buckets + bucket_of(b, a, e, mirrored)) * H + head];
+        float x = entry * kLog2e;
+        if (fabsf(x) > kMostBias && fabsf(entry) < INFINITY) x = copysignf(kMostBias, x);
+        dense[a * kReachRow + e] = x;
     }
 }
 

@@ -346,3 +346,59 @@ def test_scores_of_any_size(r, shape, dtype):
         assert bool(torch.isfinite(o).all())
         assert torch.equal(o, o[:, :, :1].expand_as(o))
         assert torch.equal(o[0, clear.cuda(), 0].float().cpu(), want[clear])
+
+
+# --- masks of the lowest number -------------------------------------------------------------
+
+def _banned(axes, H, reach, low):
+    """(table, buckets) that bans distances beyond reach on each axis with entry low."""
+    table = torch.zeros((axes, 2, H))
+    table[:, 1] = low
+    buckets = torch.zeros((axes, 2 * reach + 3), dtype=torch.uint8)
+    buckets[:, 0] = buckets[:, -1] = 1
+    return table, buckets
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("axes", [1, 3])
+@pytest.mark.parametrize("H", [2, 300])
+def test_masks_of_the_lowest_float(r, dtype, axes, H):
+    """A bias of the lowest float leaves its pairs out where a row has others, as
+    -infinity does; a row of nothing else has equal weights (their scores are lost
+    beside it), and is not empty.  On one axis and on several at once."""
+    dt, low = DT[dtype], torch.finfo(torch.float32).min
+    g = _gen(11)
+    Tq, Tk, D = 70, 90, 32
+    q = torch.randn((1, Tq, 1, D), generator=g).to(dt)
+    k, v = (torch.randn((1, Tk, 1, D), generator=g).to(dt) for _ in range(2))
+    table, buckets = _banned(axes, 1, 3, low)
+    places = [torch.arange(n, dtype=torch.int32)[:, None].repeat(1, axes) for n in (Tq, Tk)]
+    places[0][10:20] += 1000            # nobody near
+    cq, ck, cv = (t.cuda().expand(-1, -1, H, -1) for t in (q, k, v))
+
+    def call(entry, train):
+        t = torch.where(table == low, entry, table).expand(-1, -1, H).contiguous().cuda()
+        bias = mixrt.RelativeBias(t, buckets.cuda(), *[p.cuda() for p in places])
+        o = r.attention_train(cq, ck, cv, bias=bias) if train else r.attention(cq, ck, cv,
+                                                                             bias=bias)
+        o = (o[0] if train else o).double().cpu()
+        assert torch.equal(o.nan_to_num(7.0), o[:, :, :1].expand_as(o).nan_to_num(7.0))
+        return o[:, :, :1]
+
+    near = [i for i in range(Tq) if not 10 <= i < 20]
+    mean = v[0, :, 0].double().mean(0)
+    sizes = v[0, :, 0].double().abs().mean(0)
+    for train in (False, True):
+        got, bans = call(low, train), call(-math.inf, train)
+        assert torch.equal(got[:, near], bans[:, near])
+        assert float(bans[:, 10:20].abs().max()) == 0
+        # equal weights of 1 (a power of two in float16): sums in 32 bits, the rounded
+        # result
+        off = (got[0, 10:20, 0] - mean).abs()
+        bound = (Tk + 64) * ref.U * sizes + ref.HALF_UNIT[dt] * mean.abs() + ref.TINY[dt]
+        assert bool((off <= bound).all()), float((off - bound).max())
+    # a table of large and small entries of either sign, and NaN
+    for entry in (-1e38, 3e38):
+        got = call(entry, False)
+        assert bool(torch.isfinite(got).all())
+    assert bool(torch.isnan(call(math.nan, False)).all())
