@@ -633,6 +633,11 @@ typedef struct {
     const int32_t *lens;  /* device [batch]: valid keys of each entry, or NULL:
                              all (below 0 is taken as 0, above keys as keys).
                              Keys and values behind are never read. */
+    float *lse_rest;      /* device [batch][heads][queries], or NULL: what rounding
+                             takes from lse, which a forward call writes beside lse
+                             and a backward call reads (NULL: 0).  Weights formed
+                             from lse alone are off by |lse| 2^-24, relative: 1 for
+                             rows whose every score is 2^24, as a mask's may be. */
 } mixrt_attention;
 
 /* A learned bias by the buckets of relative positions: with the distance

@@ -59,7 +59,7 @@ struct Arrays {
         const char *name;
         bool out;
     };
-    One a[16];
+    One a[20];
     int n = 0;
     void add(const Extent &e, const char *name, bool out = false)
     {

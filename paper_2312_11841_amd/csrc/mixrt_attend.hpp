@@ -39,12 +39,14 @@ struct AttendK {
     SeqK q, k, v, o;
     void *rest;               // [B][Tq][H][D], dense, or null
     float *lse;               // [B][H][Tq] or null
+    float *lse_rest;          // the same, or null: what rounding took from lse
     // backward
     SeqK dout, dq, dk, dv;
     float *dtable;
     // how the work is dealt (see AttendPlan)
     int pack, blocks, splits, per;
-    float *part, *part_lse, *delta, *part_table;
+    float *part, *delta, *part_table;
+    float2 *part_lse;         // (lse and its rest)
 };
 
 // How a call is dealt.  Forward: a block takes cols columns (a column is a token and

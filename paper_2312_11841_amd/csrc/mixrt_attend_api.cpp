@@ -243,6 +243,8 @@ int check_attention(mixrt_ctx *ctx, const mixrt_attention *a, const mixrt_relati
     if (rows > 0 && ((a->queries > a->keys ? a->queries : a->keys) + 1) > kMaxTokens / rows)
         return fail(ctx, MIXRT_EUNSUPPORTED, "attention: 2^30 rows of heads or more");
     if (!aligned(a->lens, 4)) return fail(ctx, MIXRT_EINVAL, "attention.lens not 4-byte aligned");
+    if (!aligned(a->lse_rest, 4))
+        return fail(ctx, MIXRT_EINVAL, "attention.lse_rest not 4-byte aligned");
     int stage = 0;
     for (auto plan : {mixrt::plan_attend, mixrt::plan_attend_dq, mixrt::plan_attend_dkv}) {
         const AttendPlan p = plan(a->batch, a->heads, a->kv_heads, a->queries, a->keys,
@@ -354,7 +356,7 @@ Scratch scratch_of(const mixrt_attention *a, const mixrt_relative_bias *b, bool 
         const AttendPlan p = plan(mixrt::plan_attend);
         if (p.splits > 1) {
             s.part = take((size_t)p.splits * rows * a->head_dim * 4);
-            s.part_lse = take((size_t)p.splits * rows * 4);
+            s.part_lse = take((size_t)p.splits * rows * 8);
         }
     } else {
         const AttendPlan pq = plan(mixrt::plan_attend_dq), pk = plan(mixrt::plan_attend_dkv);
@@ -388,6 +390,7 @@ mixrt::AttendK attend_k(const mixrt_attention *a, const mixrt_relative_bias *b)
     k.plain_scale = a->scale;
     k.scale = a->scale * 1.4426950408889634f;
     k.lens = a->lens;
+    k.lse_rest = a->lse_rest;
     if (b)
         k.bias = mixrt::BiasK{b->axes,  b->count, b->reach,        b->table,       b->buckets,
                               b->q_pos, b->k_pos, b->q_pos_stride, b->k_pos_stride};
@@ -611,6 +614,7 @@ int mixrt_attention_forward(mixrt_ctx *ctx, const mixrt_attention *att,
     add_common(m, att, bias, q, k, v);
     m.add(extent_of(att, out, true), "out", true);
     m.add(mixrt::flat_extent(lse, rows * 4), "lse", true);
+    m.add(mixrt::flat_extent(lse ? att->lse_rest : nullptr, rows * 4), "lse_rest", true);
     m.add(mixrt::flat_extent(rest, rows * att->head_dim * 2), "rest", true);
     if ((rc = check_apart(ctx, m))) return rc;
     if (!aligned(lse, 4)) return fail(ctx, MIXRT_EINVAL, "lse not 4-byte aligned");
@@ -628,7 +632,7 @@ int mixrt_attention_forward(mixrt_ctx *ctx, const mixrt_attention *att,
     a.lse = lse;
     a.rest = rest;
     a.part = (float *)((char *)workspace + s.part);
-    a.part_lse = (float *)((char *)workspace + s.part_lse);
+    a.part_lse = (float2 *)((char *)workspace + s.part_lse);
     return finish_launch(ctx, launch_attend(a, mixrt::kAttendForward, ctx->stream),
                          "attention_forward");
 }
@@ -661,6 +665,7 @@ int mixrt_attention_backward(mixrt_ctx *ctx, const mixrt_attention *att,
     m.add(extent_of(att, dout, true), "dout");
     m.add(extent_of(att, out, true), "out");
     m.add(mixrt::flat_extent(lse, all * 4), "lse");
+    m.add(mixrt::flat_extent(att->lse_rest, all * 4), "lse_rest");
     m.add(mixrt::flat_extent(rest, all * att->head_dim * 2), "rest");
     m.add(extent_of(att, dq, true), "dq", true);
     m.add(extent_of(att, dk, false), "dk", true);

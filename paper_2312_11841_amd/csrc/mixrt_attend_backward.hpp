@@ -88,6 +88,23 @@ __device__ __forceinline__ void clear(f32x16 (&a)[NC][ND])
             for (int i = 0; i < 16; ++i) a[n][d][i] = 0.0f;
 }
 
+// The exponent of a pair's weight, s unit - lse - rest, where lse is so large that its
+// rounding counts (2^8 and more: 2^-16 of a weight): by three roundings, and from 2^22
+// on of the score first, as the forward pass has it.  A weight is at most 2^lifted,
+// whatever the roundings.  (In float32 what rounding took from lse counts always: it is
+// most of a small step's error, and the matrix unit leaves the time.)
+__device__ __forceinline__ bool large_sum(float lse)
+{
+    return fabsf(lse) >= 256.0f && fabsf(lse) < INFINITY;
+}
+__device__ __forceinline__ float exponent(float s, float unit, float lse, float rest, float lifted)
+{
+    const float whole = s * unit;
+    const float near = fmaf(s, unit, -lse), far = whole - lse;
+    const float x = (fabsf(lse) < 0x1p22f ? near : far) - rest;
+    return x > lifted ? lifted : x;
+}
+
 // float16 holds dS only inside a range: its gradients are small where a row looks at
 // many keys, and large where a loss is scaled.  So each column's dS is multiplied by a
 // power of two that brings the largest seen so far to 2^8..2^9 when it is chosen, and
@@ -335,7 +352,8 @@ __global__ __launch_bounds__(256) void attend_dq_kernel(AttendK k)
     int t[NC];
     bool there[NC];
     frag q[NC][kPairs<T, DP>], dout[NC][kPairs<T, DP>];
-    float lse[NC], delta[NC];
+    float lse[NC], lse_rest[NC], delta[NC];
+    bool large = false;         // (of the whole wave)
     int qpos[NC][kMaxBiasAxes];
 #pragma unroll
     for (int n = 0; n < NC; ++n) {
@@ -367,6 +385,8 @@ __global__ __launch_bounds__(256) void attend_dq_kernel(AttendK k)
         delta[n] = half_sum(sum);
         const int64_t row = ((int64_t)b * k.H + h) * k.Tq + tt;
         lse[n] = there[n] ? k.lse[row] : INFINITY;
+        lse_rest[n] = there[n] && k.lse_rest ? k.lse_rest[row] : 0.0f;
+        large = large || __builtin_amdgcn_ballot_w64(large_sum(lse[n])) != 0;
         if (there[n] && half == 0 && split == 0 && me == 0) k.delta[row] = delta[n];
 #pragma unroll
         for (int a = 0; a < kMaxBiasAxes; ++a)
@@ -454,12 +474,25 @@ __global__ __launch_bounds__(256) void attend_dq_kernel(AttendK k)
                                k.bias.reach);
         }
         const float unit = BIAS ? 1.0f : k.scale;
+        if (large) {
+            rare();
 #pragma unroll
-        for (int n = 0; n < NC; ++n)
+            for (int n = 0; n < NC; ++n)
 #pragma unroll
-            for (int i = 0; i < 16; ++i)
-                g[n][i] = __builtin_amdgcn_exp2f(fmaf(s[n][i], unit, -lse[n])) *
-                          (g[n][i] - delta[n]);
+                for (int i = 0; i < 16; ++i)
+                    s[n][i] = exponent(s[n][i], unit, lse[n], lse_rest[n], 0.0f);
+        }
+#pragma unroll
+        for (int n = 0; n < NC; ++n) {
+            const float by = large ? 1.0f : unit, less = large ? 0.0f : lse[n];
+            const float left = large ? 0.0f : lse_rest[n];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                float x = fmaf(s[n][i], by, -less);
+                if (sizeof(T) == 4) x -= left;
+                g[n][i] = __builtin_amdgcn_exp2f(x) * (g[n][i] - delta[n]);
+            }
+        }
         if (row0 + ROWS > last) {
             rare();
 #pragma unroll
@@ -534,25 +567,37 @@ __global__ __launch_bounds__(256) void attend_dq_kernel(AttendK k)
 // units 44%, LDS 48%, a fifth of that conflicts of the transposing loads.  The second:
 // 231 us, 21%, 39% and 36%.
 
-// lse and delta of a tile's queries.
+// lse, delta and what rounding took from lse of a tile's queries, and whether any lse is
+// large.
 template <int ROWS>
 struct StageSums {
-    float lse, delta;
-    __device__ __forceinline__ void fetch(int thread, const float *l, const float *d, int first,
-                                          int limit, float lifted)
+    static constexpr int kFloats = 3 * ROWS + 4;
+    float lse, delta, rest;
+    __device__ __forceinline__ void fetch(int thread, const float *l, const float *d,
+                                          const float *r, int first, int limit, float lifted)
     {
         const int row = first + thread;
         const bool there = thread < ROWS && row < limit;
         // (a row that is not there has weights 0)
-        lse = there ? l[row] - lifted : INFINITY;
-        delta = there ? d[row] : 0.0f;
+        lse = INFINITY;
+        delta = rest = 0.0f;
+        if (!there) return;
+        const float whole = l[row];
+        lse = whole - lifted;
+        delta = d[row];
+        if (r) rest = r[row];
+        if (lifted != 0.0f && whole < INFINITY) rest += (whole - lse) - lifted;
     }
     __device__ __forceinline__ void put(int thread, float *at) const
     {
         if (thread < ROWS) {
             at[thread] = lse;
             at[ROWS + thread] = delta;
+            at[2 * ROWS + thread] = rest;
         }
+        if (thread >= 64) return;           // the first wave holds the rows
+        const bool large = __builtin_amdgcn_ballot_w64(thread < ROWS && large_sum(lse)) != 0;
+        if (thread == 0) at[3 * ROWS] = large ? 1.0f : 0.0f;
     }
 };
 
@@ -567,7 +612,8 @@ __global__ __launch_bounds__(256) void attend_dkv_kernel(AttendK k)
     __shared__ __attribute__((aligned(16))) T tiles[WAVES][BUFS][2][TILE];
     __shared__ float dense[WAVES][BIAS ? kMaxBiasAxes * kReachRow : 1];
     __shared__ TilePos<BIAS ? ROWS : 1> qpos[WAVES][BUFS];
-    __shared__ __attribute__((aligned(16))) float sums[WAVES][BUFS][2 * ROWS];
+    __shared__ __attribute__((aligned(16))) float sums[WAVES][BUFS][StageSums<ROWS>::kFloats];
+    __shared__ float zeros[ROWS];
 
     const Team<SHARED> team;
     const int lane = team.lane, wave = team.wave, half = team.half;
@@ -630,7 +676,8 @@ __global__ __launch_bounds__(256) void attend_dkv_kernel(AttendK k)
         sg.fetch(stager, gp + h * k.dout.head, k.dout.token, row, k.Tq, k.D);
         if (!AHEAD) sg.put(stager, tiles[me][0][1]);
         const int64_t at = sums0 + (int64_t)h * k.Tq;
-        ss.fetch(stager, k.lse + at, k.delta + at, row, k.Tq, kWeightLift<T>);
+        ss.fetch(stager, k.lse + at, k.delta + at, k.lse_rest ? k.lse_rest + at : nullptr, row,
+                 k.Tq, kWeightLift<T>);
         if (BIAS) sp.fetch(stager, pp, k.bias.axes, row, k.Tq);
     };
     auto put = [&](int to) {
@@ -642,6 +689,7 @@ __global__ __launch_bounds__(256) void attend_dkv_kernel(AttendK k)
         if (BIAS) sp.put(stager, qpos[me][to], k.bias.axes);
     };
     int head = -1;              // whose bias is in LDS
+    if (lane < ROWS) zeros[lane] = 0.0f;    // (by each wave)
     const int first1 = first + me;
     if (first1 < last) {
         fetch(first1);
@@ -651,7 +699,9 @@ __global__ __launch_bounds__(256) void attend_dkv_kernel(AttendK k)
     int cur = 0;
     for (int i0 = first1; i0 < last; i0 += STEP, cur ^= BUFS - 1) {
         const bool more = i0 + STEP < last;
+        const float marked = sums[me][cur][3 * ROWS];
         if (more && AHEAD) fetch(i0 + STEP);
+        const bool large = __builtin_amdgcn_readfirstlane(__float_as_int(marked)) != 0;
         if (BIAS && head != i0 / a_head) {      // (the same for all that share it)
             head = i0 / a_head;
             // (mirrored: the rows are queries here)
@@ -676,12 +726,28 @@ __global__ __launch_bounds__(256) void attend_dkv_kernel(AttendK k)
                                    k.bias.axes, k.bias.reach);
             }
             const float unit = BIAS ? 1.0f : k.scale;
+            if (large) {
+                rare();
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int at = tile_row(i, half);
+#pragma unroll
+                    for (int n = 0; n < NC; ++n)
+                        p[n][i] = exponent(p[n][i], unit, sm[at], sm[2 * ROWS + at],
+                                           kWeightLift<T>);
+                }
+            }
+            const float by = large ? 1.0f : unit;
+            const float *less = large ? zeros : sm, *left = large ? zeros : sm + 2 * ROWS;
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                const float lse = sm[tile_row(i, half)], delta = sm[ROWS + tile_row(i, half)];
+                const int at = tile_row(i, half);
+                const float lse = less[at], delta = sm[ROWS + at];
 #pragma unroll
                 for (int n = 0; n < NC; ++n) {
-                    p[n][i] = __builtin_amdgcn_exp2f(fmaf(p[n][i], unit, -lse));
+                    float x = fmaf(p[n][i], by, -lse);
+                    if (sizeof(T) == 4) x -= left[at];
+                    p[n][i] = __builtin_amdgcn_exp2f(x);
                     g[n][i] = p[n][i] * (g[n][i] - delta);
                 }
             }

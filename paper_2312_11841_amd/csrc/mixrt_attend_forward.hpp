@@ -64,6 +64,22 @@ struct Columns {
     }
 };
 
+// log2 of a row's sum of weights: their base and the logarithm of their sum, as a 32-bit
+// number and what its rounding left.
+struct RowSum {
+    float lse, rest;
+    __device__ __forceinline__ RowSum(float top, float l, float none)
+    {
+        const float add = __builtin_amdgcn_logf(l);     // (log2)
+        lse = top + add;
+        const float got = lse - top;
+        rest = (top - (lse - got)) + (add - got);
+        if (l == 0.0f) lse = none;
+        // (no rest of what is not a finite number)
+        if (!(fabsf(lse) < INFINITY)) rest = 0.0f;
+    }
+};
+
 // The columns' results: sums of weighted values, of weights (the lane's own rows), and
 // the base of the weights, in units of log2.
 template <typename T, int DP, int NC>
@@ -78,10 +94,10 @@ __device__ __forceinline__ void finish(const AttendK &k, const ForwardWork &w,
         const float inv = l == 0.0f ? 0.0f : 1.0f / l;
         if (!c.there[n]) continue;
         const int64_t row = ((int64_t)w.b * k.H + c.head[n]) * k.Tq + c.t[n];
-        const float lse = top[n] + __builtin_amdgcn_logf(l);    // (log2)
+        const RowSum sums(top[n], l, k.splits > 1 ? -INFINITY : INFINITY);
         if (k.splits > 1) {
             const int64_t rows = (int64_t)k.B * k.H * k.Tq;
-            if (half == 0) k.part_lse[w.split * rows + row] = l == 0.0f ? -INFINITY : lse;
+            if (half == 0) k.part_lse[w.split * rows + row] = make_float2(sums.lse, sums.rest);
             float *o = k.part + (w.split * rows + row) * k.D;
 #pragma unroll
             for (int d = 0; d < DP / 32; ++d)
@@ -92,7 +108,10 @@ __device__ __forceinline__ void finish(const AttendK &k, const ForwardWork &w,
                                       acc[n][d][4 * e + 3] * inv);
             continue;
         }
-        if (k.lse && half == 0) k.lse[row] = l == 0.0f ? INFINITY : lse;
+        if (k.lse && half == 0) {
+            k.lse[row] = sums.lse;
+            if (k.lse_rest) k.lse_rest[row] = sums.rest;
+        }
         T *o = (T *)k.o.data + w.b * k.o.batch + (int64_t)c.t[n] * k.o.token +
                c.head[n] * k.o.head;
         T *rest = k.rest ? (T *)k.rest + (((int64_t)w.b * k.Tq + c.t[n]) * k.H + c.head[n]) * k.D
@@ -214,15 +233,18 @@ __device__ __forceinline__ void finish_shared(const AttendK &k, const ForwardWor
     if (!c.there[0]) return;
     const int d = (2 * team.wave + half) * (DP / 8);
     const int64_t row = ((int64_t)w.b * k.H + c.head[0]) * k.Tq + c.t[0];
-    const float lse = base + __builtin_amdgcn_logf(l);
+    const RowSum sums(base, l, k.splits > 1 ? -INFINITY : INFINITY);
     const bool first = team.wave == 0 && half == 0;
     if (k.splits > 1) {
         const int64_t rows = (int64_t)k.B * k.H * k.Tq;
-        if (first) k.part_lse[w.split * rows + row] = l == 0.0f ? -INFINITY : lse;
+        if (first) k.part_lse[w.split * rows + row] = make_float2(sums.lse, sums.rest);
         store_run<float>(k.part + (w.split * rows + row) * k.D, d, k.D, f, inv);
         return;
     }
-    if (k.lse && first) k.lse[row] = l == 0.0f ? INFINITY : lse;
+    if (k.lse && first) {
+        k.lse[row] = sums.lse;
+        if (k.lse_rest) k.lse_rest[row] = sums.rest;
+    }
     store_run<T>((T *)k.o.data + w.b * k.o.batch + (int64_t)c.t[0] * k.o.token +
                      c.head[0] * k.o.head, d, k.D, f, inv);
     if (k.rest) {
@@ -563,7 +585,7 @@ __device__ __forceinline__ void join_row(const AttendK &k, int64_t row, float (&
     if (there)
 #pragma unroll 4
         for (int s = g; s < k.splits; s += G) {
-            const float x = k.part_lse[s * rows + row];
+            const float x = k.part_lse[s * rows + row].x;
             top = x > top || x != x ? x : top;
         }
     float base = top == -INFINITY ? 0.0f : top;
@@ -571,7 +593,8 @@ __device__ __forceinline__ void join_row(const AttendK &k, int64_t row, float (&
     if (there)
 #pragma unroll 4
         for (int s = g; s < k.splits; s += G) {
-            const float e = __builtin_amdgcn_exp2f(k.part_lse[s * rows + row] - base);
+            const float2 lse = k.part_lse[s * rows + row];
+            const float e = __builtin_amdgcn_exp2f((lse.x - base) + lse.y);
             w += e;
             const float *o = k.part + (s * rows + row) * k.D;
             if (d + 4 <= k.D) {
@@ -618,8 +641,11 @@ __device__ __forceinline__ void join_row(const AttendK &k, int64_t row, float (&
     const float inv = w == 0.0f ? 0.0f : 1.0f / w;
     const int64_t bh = row / k.Tq;
     const int t = (int)(row - bh * k.Tq), b = (int)(bh / k.H), h = (int)(bh - (int64_t)b * k.H);
-    if (k.lse && lane == 0 && blockIdx.y == 0)
-        k.lse[row] = w == 0.0f ? INFINITY : base + __builtin_amdgcn_logf(w);
+    if (k.lse && lane == 0 && blockIdx.y == 0) {
+        const RowSum sums(base, w, INFINITY);
+        k.lse[row] = sums.lse;
+        if (k.lse_rest) k.lse_rest[row] = sums.rest;
+    }
     if (d >= k.D) return;
     T *o = (T *)k.o.data + b * k.o.batch + (int64_t)t * k.o.token + h * k.o.head;
 #pragma unroll

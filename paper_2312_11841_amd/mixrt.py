@@ -156,7 +156,8 @@ class NormedHeads(C.Structure):
 class Attention(C.Structure):
     _fields_ = [("batch", C.c_int32), ("heads", C.c_int32), ("kv_heads", C.c_int32),
                 ("head_dim", C.c_int32), ("dtype", C.c_int32), ("scale", C.c_float),
-                ("queries", C.c_int64), ("keys", C.c_int64), ("lens", C.c_void_p)]
+                ("queries", C.c_int64), ("keys", C.c_int64), ("lens", C.c_void_p),
+                ("lse_rest", C.c_void_p)]
 
 
 class RelativeBiasDesc(C.Structure):
@@ -695,11 +696,13 @@ def distance_buckets(count: int, reach: int, near=None):
 @dataclass
 class AttentionSaved:
     """What attention_backward needs of attention_train besides its output: lse
-    float32 [batch, heads, queries], and the bits that rounding took from the
-    output (float16 and bfloat16, in a tensor of that type; None for float32)."""
+    float32 [batch, heads, queries], the bits that rounding took from the output
+    (float16 and bfloat16, in a tensor of that type; None for float32), and what it
+    took from lse (None: nothing)."""
 
     lse: object
     rest: object
+    lse_rest: object = None
 
 
 def _as_sequence(t, name: str):
@@ -1460,7 +1463,7 @@ class Renderer:
                 raise ValueError(f"lens: {lens.dtype} {tuple(lens.shape)}, expected contiguous "
                                  f"int32 ({B},)")
         p.att = Attention(B, H, Hk, D, _elem_code(q.dtype, "q"),
-                          1.0 / D ** 0.5 if scale is None else scale, Tq, Tk, 0)
+                          1.0 / D ** 0.5 if scale is None else scale, Tq, Tk, 0, 0)
         p.bias = None if bias is None else _bias_desc(bias, B, Tq, Tk, H, self.device)
         p.att_ref = C.byref(p.att)
         p.bias_ref = None if bias is None else C.byref(p.bias)
@@ -1475,7 +1478,8 @@ class Renderer:
         p.q_shape, p.k_shape, p.lse_shape = (B, Tq, H, D), (B, Tk, Hk, D), (B, H, Tq)
         return p
 
-    def _attend(self, p, q, out, lse, rest, here):
+    def _attend(self, p, q, out, lse, lse_rest, rest, here):
+        p.att.lse_rest = 0 if lse_rest is None else lse_rest.data_ptr()
         if out is None:
             out = self._empty(p.q_shape, q.dtype, here)
             p.o.data = out.data_ptr()
@@ -1507,7 +1511,7 @@ class Renderer:
         table = None if bias is None else bias.table
         if out is not None:
             self._refuse_out("attention", (q, k, v, table))
-        out = self._attend(p, q, out, None, None, self._here())
+        out = self._attend(p, q, out, None, None, None, self._here())
         if self._follows(q, k, v, table):
             return self._result("attention", (out,), (q, k, v, table))[0]
         return out
@@ -1522,13 +1526,13 @@ class Renderer:
         if out is not None:
             self._refuse_out("attention_train", (q, k, v, table))
         here = self._here()
-        lse = self._empty(p.lse_shape, self._torch.float32, here)
+        lse, lse_rest = self._empty((2, *p.lse_shape), self._torch.float32, here).unbind(0)
         rest = (None if p.att.dtype == MIXRT_F32
                 else self._empty(p.q_shape, q.dtype, here))
-        out = self._attend(p, q, out, lse, rest, here)
+        out = self._attend(p, q, out, lse, lse_rest, rest, here)
         if self._follows(q, k, v, table):
             out, lse = self._result("attention_train", (out, lse), (q, k, v, table))
-        return out, AttentionSaved(lse, rest)
+        return out, AttentionSaved(lse, rest, lse_rest)
 
     def attention_backward(self, dout, q, k, v, out, saved: AttentionSaved, *, lens=None,
                            bias=None, scale=None):
@@ -1542,10 +1546,15 @@ class Renderer:
         _like(out, "out", q.shape, q.dtype, dev)
         if not isinstance(saved, AttentionSaved):
             raise TypeError(f"saved: expected an AttentionSaved, got {type(saved).__name__}")
-        lse, rest = saved.lse, saved.rest
+        lse, rest, lse_rest = saved.lse, saved.rest, saved.lse_rest
         _like(lse, "saved.lse", p.lse_shape, f32, dev)
         if not lse.is_contiguous():
             raise ValueError("saved.lse: not contiguous")
+        if lse_rest is not None:
+            _like(lse_rest, "saved.lse_rest", p.lse_shape, f32, dev)
+            if not lse_rest.is_contiguous():
+                raise ValueError("saved.lse_rest: not contiguous")
+        p.att.lse_rest = 0 if lse_rest is None else lse_rest.data_ptr()
         if p.att.dtype != MIXRT_F32:
             _like(rest, "saved.rest", q.shape, q.dtype, dev)
             if not rest.is_contiguous():

@@ -402,3 +402,92 @@ def test_masks_of_the_lowest_float(r, dtype, axes, H):
         got = call(entry, False)
         assert bool(torch.isfinite(got).all())
     assert bool(torch.isnan(call(math.nan, False)).all())
+
+
+def _uniform(q, k, v, dout, dt, scale):
+    """The statement where all weights of a row are equal: o, dq and dv are those of
+    queries of 0, dk follows from the same dS at the queries that there are."""
+    want = ref.attention(0 * q, k, v, dt, scale=scale, dout=dout)
+    p = 1 / k.shape[1]
+    dO, V, Q = (t[0, :, 0].double() for t in (dout, v, q))
+    dp = dO @ V.T
+    ds = p * (dp - dp.mean(1, keepdim=True))
+    off = (q.shape[3] + 64 + q.shape[1]) * ref.U + (
+        0 if dt == torch.float32 else ref.HALF_UNIT[dt])
+    off = off * p * (dp.abs() + dp.abs().mean(1, keepdim=True))
+    value = scale * (ds.T @ Q)[None, :, None]
+    bound = scale * (off.T @ Q.abs())[None, :, None]
+    want["dk"] = value, bound + ref.HALF_UNIT[dt] * value.abs() + ref.TINY[dt]
+    return want
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("low", [torch.finfo(torch.float32).min, -1e12])
+@pytest.mark.parametrize("shape", [(1, 700, 1), (70, 700, 1), (150, 300, 200),
+                                   (1, 4000, 3)], ids=str)
+def test_rows_of_masks_share_their_weights(r, shape, low, dtype):
+    """Rows whose every score is a mask's, of one call and of splits that are joined:
+    weights of 1 / keys, forward and in every gradient."""
+    Tq, Tk, H = shape
+    dt = DT[dtype]
+    g = _gen(12)
+    D, scale = 32, 0.25
+    q, dout = (torch.randn((1, Tq, 1, D), generator=g).to(dt) for _ in range(2))
+    k, v = (torch.randn((1, Tk, 1, D), generator=g).to(dt) for _ in range(2))
+    table, buckets = _banned(2, H, 3, low)
+    table[1, 1] = 0
+    places = [torch.arange(n, dtype=torch.int32)[:, None].repeat(1, 2) for n in (Tq, Tk)]
+    places[1][:, 0] += 10 ** 6          # nobody near
+    bias = mixrt.RelativeBias(*[t.cuda() for t in (table, buckets, *places)])
+    want = _uniform(q, k, v, dout, dt, scale)
+    cq, ck, cv, cd = (t.cuda().expand(-1, -1, H, -1) for t in (q, k, v, dout))
+    say(shape, low, dtype)
+    _inside(r.attention(cq, ck, cv, bias=bias, scale=scale)[:, :, :1], want["o"], "o")
+    o, saved = r.attention_train(cq, ck, cv, bias=bias, scale=scale)
+    _inside(o[:, :, :1], want["o"], "o of training")
+    grads = r.attention_backward(cd, cq, ck, cv, o, saved, bias=bias, scale=scale)
+    for name, got in zip(("dq", "dk", "dv"), grads):
+        assert torch.equal(got, got[:, :, :1].expand_as(got)), name
+        _inside(got[:, :, :1], want[name], name)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("size", [0.0, 60.0, 3000.0, 1e5, 1e6])
+@pytest.mark.parametrize("shape", [(40, 50, 1), (40, 900, 1), (200, 300, 200)], ids=str)
+def test_weights_of_large_scores_add_up_to_one(r, shape, size, dtype):
+    """Scores that all keys share up to a few units, of any size: a row's weights add up
+    to 1 in the backward pass, so that the gradients of all values add up to those of
+    all rows.  Each weight is off by its exponent's roundings (at most 8 of 2^-24 of
+    numbers below 32, whatever the scores' size) and its own to the type."""
+    Tq, Tk, H = shape
+    dt = DT[dtype]
+    g = _gen(13)
+    D = 16
+    q = torch.zeros((1, Tq, 1, D))
+    k, dout = torch.zeros((1, Tk, 1, D)), torch.rand((1, Tq, 1, D), generator=g).to(dt)
+    q[..., 0], k[..., 0] = math.sqrt(size), math.sqrt(size)
+    q[..., 1], k[..., 1] = 1.0, torch.randint(-3, 4, (1, Tk, 1), generator=g).float()
+    v = torch.randn((1, Tk, 1, D), generator=g).to(dt)
+    cq, ck, cv, cd = (t.to(dt).cuda().expand(-1, -1, H, -1) for t in (q, k, v, dout))
+    o, saved = r.attention_train(cq, ck, cv, scale=1.0)
+    dv = r.attention_backward(cd, cq, ck, cv, o, saved, scale=1.0)[2][0, :, 0].double().cpu()
+    want = dout[0, :, 0].double().sum(0)
+    off = (dv.sum(0) - want).abs().max()
+    sums = dout[0, :, 0].double().abs().sum(0).max()
+    room = (8 * 32 + 2 * (Tq + 64)) * ref.U + (0 if dtype == "f32" else 2 * ref.HALF_UNIT[dt])
+    say(size, dtype, f"{float(off / sums):.2e} of {room:.2e}")
+    assert float(off) <= room * float(sums)
+
+
+def test_what_rounding_took_from_lse_may_be_left_out(r):
+    """A caller that keeps lse alone gets the gradients within its rounding."""
+    g = _gen(14)
+    q, k, v, dout = (torch.randn((1, 50, 2, 16), generator=g).cuda() for _ in range(4))
+    o, saved = r.attention_train(q, k, v)
+    want = r.attention_backward(dout, q, k, v, o, saved)
+    got = r.attention_backward(dout, q, k, v, o, mixrt.AttentionSaved(saved.lse, saved.rest))
+    for a, b in zip(got, want):
+        assert float((a - b).abs().max()) <= 16 * ref.U * float(b.abs().max()) * 50
+    with pytest.raises(ValueError, match="lse_rest"):
+        r.attention_backward(dout, q, k, v, o, mixrt.AttentionSaved(
+            saved.lse, saved.rest, saved.lse_rest[:, :1]))
