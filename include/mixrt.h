@@ -669,7 +669,8 @@ typedef struct {
     int64_t batch_stride, token_stride, head_stride;
 } mixrt_sequence;
 
-/* Workspace bytes of a forward (backward = 0) or backward call. */
+/* Workspace bytes of a forward (backward = 0) or backward call: none where a walk
+ * fits one part; else a few times out's size (dk's and dv's) in 32 bits. */
 int mixrt_attention_workspace(const mixrt_attention *att, const mixrt_relative_bias *bias,
                               int32_t backward, size_t *bytes);
 

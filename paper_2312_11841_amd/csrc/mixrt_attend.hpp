@@ -43,22 +43,35 @@ struct AttendK {
     // backward
     SeqK dout, dq, dk, dv;
     float *dtable;
-    // how the work is dealt (see AttendPlan)
+    // how the work is dealt (see AttendPlan), and a pass of it: the row (tile) it starts
+    // from, parts of an array in scratch, the parts that its join reads (with what the
+    // passes before left, in the part behind its own), and whether it is the last
     int pack, blocks, splits, per;
+    int from, slots, parts, pass;
+    bool last;
     float *part, *delta, *part_table;
-    float2 *part_lse;         // (lse and its rest)
+    float2 *part_lse;         // (lse and its rest; what passes leave in two by turns)
+    double *table_sum;        // of the passes
 };
 
 // How a call is dealt.  Forward: a block takes cols columns (a column is a token and
 // one of pack heads that share their keys) and per keys; queries' gradient: likewise,
 // pack 1; keys' gradient: a block takes cols keys and per tiles of attend_kv_rows
-// (the heads of a group one after another).
+// (the heads of a group one after another).  A long walk runs in passes, one after
+// another, each of so many splits, whose join adds what the passes before left: the
+// scratch is then a few arrays' size, however long the walk.
 struct AttendPlan {
     int shared;               // a block's waves share 32 columns and divide the rows
     int pack;
     int cols, blocks;         // columns of a block, blocks of one head
-    int splits, per;
+    int splits, per, passes;
 };
+
+// Parts of an array in scratch.
+inline int attend_slots(const AttendPlan &p)
+{
+    return p.passes > 1 ? p.splits + 1 : p.splits > 1 ? p.splits : 0;
+}
 
 // A launch holds fewer than 2^32 threads in x: blocks of 256 that a kernel whose grid is
 // its work may have; the kernels that join splits walk over theirs in fewer.

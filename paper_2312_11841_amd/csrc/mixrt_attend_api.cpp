@@ -34,6 +34,23 @@ void divide(int64_t n, int64_t s, int64_t most, int64_t step, int *splits, int *
     *splits = (int)(n > 0 ? ceil_div(n, p) : 1);
 }
 
+// Splits of a long walk in passes.  A chain's length bounds a split's, so their number
+// grows with the walk, and with the rows the scratch would be their product (one entry,
+// 16 heads of 128, 65,536 tokens among themselves, f32: 32 parts, 17 GB).  So a pass has
+// at most four, or as many as the call runs at once, or a 64th of all, whose joins would
+// else add up roundings.
+void in_passes(AttendPlan *p, int64_t blocks, int64_t s)
+{
+    p->passes = 1;
+    int64_t most = s > 4 ? s : 4;
+    const int64_t fill = blocks > 0 ? ceil_div(8 * kCUs, blocks) : 1;
+    if (most < fill) most = fill;
+    if (most < ceil_div(p->splits, 64)) most = ceil_div(p->splits, 64);
+    if (p->shared || p->splits <= most) return;
+    p->passes = (int)ceil_div(p->splits, most);
+    p->splits = (int)ceil_div(p->splits, p->passes);
+}
+
 // Blocks that run together, by the registers and LDS that the kernels take.
 int64_t resident(int D, int dtype, int a_cu)
 {
@@ -106,6 +123,7 @@ AttendPlan plan_attend(int B, int H, int Hk, int64_t Tq, int64_t Tk, int D, int 
     const int64_t s = p.shared ? enough(Tk, blocks, 256)
                                : whole_rounds(Tk, blocks, resident(D, dtype, 2), 512);
     divide(Tk, s, longest(dtype), p.shared ? 128 : 64, &p.splits, &p.per);
+    in_passes(&p, blocks, s);
     return p;
 }
 
@@ -129,6 +147,7 @@ AttendPlan plan_attend_dq(int B, int H, int Hk, int64_t Tq, int64_t Tk, int D, i
     const int64_t s = p.shared ? enough(Tk, blocks, least)
                                : whole_rounds(Tk, blocks, resident(D, dtype, axes ? 2 : 3), 512);
     divide(Tk, s, most, p.shared ? 128 : 32, &p.splits, &p.per);
+    in_passes(&p, blocks, s);
     return p;
 }
 
@@ -147,6 +166,7 @@ AttendPlan plan_attend_dkv(int B, int H, int Hk, int64_t Tq, int64_t Tk, int D, 
     const int64_t s = p.shared ? enough(tiles, blocks, 8)
                                : whole_rounds(tiles, blocks, resident(D, dtype, 2), 512 / rows);
     divide(tiles, s, longest(dtype) / rows, p.shared ? 4 : 1, &p.splits, &p.per);
+    in_passes(&p, blocks, s);
     return p;
 }
 
@@ -333,7 +353,7 @@ size_t round16(size_t n) { return (n + 15) / 16 * 16; }
 
 // Where a call's scratch lies in its workspace; total bytes.
 struct Scratch {
-    size_t part, part_lse, delta, table, total;
+    size_t part, part_lse, delta, table, table_sum, total;
 };
 
 Scratch scratch_of(const mixrt_attention *a, const mixrt_relative_bias *b, bool backward)
@@ -354,19 +374,21 @@ Scratch scratch_of(const mixrt_attention *a, const mixrt_relative_bias *b, bool 
     };
     if (!backward) {
         const AttendPlan p = plan(mixrt::plan_attend);
-        if (p.splits > 1) {
-            s.part = take((size_t)p.splits * rows * a->head_dim * 4);
-            s.part_lse = take((size_t)p.splits * rows * 8);
+        if (const int slots = mixrt::attend_slots(p)) {
+            s.part = take((size_t)slots * rows * a->head_dim * 4);
+            s.part_lse = take((size_t)(slots + 1) * rows * 8);
         }
     } else {
         const AttendPlan pq = plan(mixrt::plan_attend_dq), pk = plan(mixrt::plan_attend_dkv);
-        size_t part = pq.splits > 1 ? (size_t)pq.splits * rows * a->head_dim * 4 : 0;
-        const size_t both = pk.splits > 1 ? (size_t)pk.splits * keys * a->head_dim * 8 : 0;
+        const size_t part = (size_t)mixrt::attend_slots(pq) * rows * a->head_dim * 4;
+        const size_t both = (size_t)mixrt::attend_slots(pk) * keys * a->head_dim * 8;
         s.part = take(part > both ? part : both);
         s.delta = take(rows * 4);
-        if (axes)
-            s.table = take((size_t)a->batch * a->heads * pq.splits * pq.blocks * axes * b->count *
-                           4);
+        if (axes) {
+            const size_t entries = (size_t)axes * b->count;
+            s.table = take((size_t)a->batch * a->heads * pq.splits * pq.blocks * entries * 4);
+            if (pq.passes > 1) s.table_sum = take(entries * a->heads * 8);
+        }
     }
     s.total = at;
     return s;
@@ -700,6 +722,7 @@ int mixrt_attention_backward(mixrt_ctx *ctx, const mixrt_attention *att,
     a.part = (float *)((char *)workspace + s.part);
     a.delta = (float *)((char *)workspace + s.delta);
     a.part_table = (float *)((char *)workspace + s.table);
+    a.table_sum = (double *)((char *)workspace + s.table_sum);
     hipError_t e = launch_attend(a, mixrt::kAttendBackQ, ctx->stream);
     if (e == hipSuccess) e = launch_attend(a, mixrt::kAttendBackKV, ctx->stream);
     return finish_launch(ctx, e, "attention_backward");

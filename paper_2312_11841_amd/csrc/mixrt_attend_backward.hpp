@@ -346,7 +346,7 @@ __global__ __launch_bounds__(256) void attend_dq_kernel(AttendK k)
     const int h = id % k.H, b = id / k.H;
     const int kvh = h / (k.H / k.Hk);
     const int len = valid_keys(k.lens, b, k.Tk);
-    const int first = split * k.per, last = min(len, first + k.per);
+    const int first = k.from + split * k.per, last = min(len, first + k.per);
     const int entries = BIAS ? k.bias.axes * k.bias.buckets : 0;
 
     int t[NC];
@@ -628,7 +628,7 @@ __global__ __launch_bounds__(256) void attend_dkv_kernel(AttendK k)
     const int len = valid_keys(k.lens, b, k.Tk);
     // tiles of the group's heads, one head after another
     const int a_head = max((k.Tq + ROWS - 1) / ROWS, 1);
-    const int first = split * k.per;
+    const int first = k.from + split * k.per;
     int last = min(k.Tq > 0 ? G * a_head : 0, first + k.per);
     if (rb * (SHARED ? 32 : 128 * NC) >= len) last = first;
 
@@ -779,7 +779,7 @@ __global__ __launch_bounds__(256) void attend_dkv_kernel(AttendK k)
         const int64_t tt = t[0], row = ((int64_t)b * k.Hk + kvh) * k.Tk + tt;
         if (k.splits > 1) {
             store_run<float>(k.part + (split * rows + row) * k.D, d, k.D, f, scale);
-            store_run<float>(k.part + ((k.splits + split) * rows + row) * k.D, d, k.D, e, plain);
+            store_run<float>(k.part + ((k.slots + split) * rows + row) * k.D, d, k.D, e, plain);
         } else {
             store_run<T>((T *)k.dk.data + b * k.dk.batch + tt * k.dk.token + kvh * k.dk.head, d,
                          k.D, f, scale);
@@ -802,7 +802,7 @@ __global__ __launch_bounds__(256) void attend_dkv_kernel(AttendK k)
         if (k.splits > 1) {
             const int64_t row = ((int64_t)b * k.Hk + kvh) * k.Tk + tt;
             store_column<float, DP>(k.part + (split * rows + row) * k.D, half, k.D, dk[n], by);
-            store_column<float, DP>(k.part + ((k.splits + split) * rows + row) * k.D, half, k.D,
+            store_column<float, DP>(k.part + ((k.slots + split) * rows + row) * k.D, half, k.D,
                                     dv[n], plain);
         } else {
             store_column<T, DP>((T *)k.dk.data + b * k.dk.batch + tt * k.dk.token +
@@ -817,10 +817,10 @@ __global__ __launch_bounds__(256) void attend_dkv_kernel(AttendK k)
 
 // out[b][t][h][d] = sum of the splits' parts [split][b][h][t][d], a quad for G threads,
 // which take every G-th split and join in order; with blockIdx.y = 1 the second array's
-// parts, which follow.  (256 splits of 40 rows of 128, twice: one thread a quad 71 us,
+// parts, which follow.  A pass that is not the last leaves its sum as a part.  (256 splits of 40 rows of 128, twice: one thread a quad 71 us,
 // 32 threads 6.7.)
 template <typename T, int G>
-__device__ __forceinline__ void sum_quad(const float *part, int splits, int64_t rows, int H,
+__device__ __forceinline__ void sum_quad(const float *part, int parts, int64_t rows, int H,
                                          int Tn, int D, const SeqK &out, int64_t at,
                                          float4 (&sums)[G > 1 ? 256 : 1])
 {
@@ -831,9 +831,9 @@ __device__ __forceinline__ void sum_quad(const float *part, int splits, int64_t 
     const int d = (int)(at - row * quads) * 4;
     float a[4] = {0, 0, 0, 0};
     if (there) {
-        const float *p = part + ((int64_t)blockIdx.y * splits * rows + row) * D + d;
+        const float *p = part + row * D + d;
 #pragma unroll 4
-        for (int s = g; s < splits; s += G) {
+        for (int s = g; s < parts; s += G) {
             const float *q = p + s * rows * D;
             if (d + 4 <= D) {
                 float f[4];
@@ -868,16 +868,17 @@ __device__ __forceinline__ void sum_quad(const float *part, int splits, int64_t 
 }
 
 template <typename T, int G>
-__global__ __launch_bounds__(256) void attend_sum_kernel(const float *part, int splits, int B,
-                                                         int H, int Tn, int D, SeqK one, SeqK two)
+__global__ __launch_bounds__(256) void attend_sum_kernel(const float *part, int slots, int parts,
+                                                         int B, int H, int Tn, int D, SeqK one,
+                                                         SeqK two)
 {
     constexpr int EACH = 256 / G;
     __shared__ float4 sums[G > 1 ? 256 : 1];
     const int64_t rows = (int64_t)B * H * Tn, all = rows * ((D + 3) / 4);
     for (int64_t first = (int64_t)blockIdx.x * EACH; first < all;
          first += (int64_t)gridDim.x * EACH) {
-        sum_quad<T, G>(part, splits, rows, H, Tn, D, blockIdx.y ? two : one,
-                       first + threadIdx.x % EACH, sums);
+        sum_quad<T, G>(part + (int64_t)blockIdx.y * slots * rows * D, parts, rows, H, Tn, D,
+                       blockIdx.y ? two : one, first + threadIdx.x % EACH, sums);
         if (G > 1) __syncthreads();     // (sums are read to the end)
     }
 }
@@ -886,9 +887,10 @@ __global__ __launch_bounds__(256) void attend_sum_kernel(const float *part, int 
 // axis and head, 32 lanes its buckets, 32 groups of them every 32nd part.  A row's dS sum
 // to 0, and so do an axis' buckets; where all but one of them are 0 (one bucket, or one
 // distance for all pairs), that one is 0 as well and not what roundings left of its sum
-// (times 0, so that a NaN stays).
+// (times 0, so that a NaN stays).  Passes add to held, the last one writes.
 __global__ __launch_bounds__(1024) void attend_table_kernel(const float *part, int B, int H,
                                                             int each, int axes, int count,
+                                                            double *held, bool more, bool last,
                                                             float *dtable)
 {
     static_assert(kMaxBuckets == 32);
@@ -909,9 +911,15 @@ __global__ __launch_bounds__(1024) void attend_table_kernel(const float *part, i
     }
     if (g != 0) return;
     a = sums[0][e];
+    const int64_t at = ((int64_t)axis * count + e) * H + h;
+    if (e < count && more) a += held[at];
+    if (!last) {
+        if (e < count) held[at] = a;
+        return;
+    }
     const uint32_t some = (uint32_t)__builtin_amdgcn_ballot_w64(a != 0.0);
     if ((some & (some - 1)) == 0) a = fabs(a * 0.0);
-    if (e < count) dtable[((int64_t)axis * count + e) * H + h] = (float)a;
+    if (e < count) dtable[at] = (float)a;
 }
 
 template <typename T>
@@ -922,9 +930,17 @@ hipError_t launch_sum(const AttendK &k, int H, int64_t Tn, const SeqK &one, cons
     if (quads == 0) return hipSuccess;
     auto go = [&](auto g) {
         constexpr int G = decltype(g)::value, each = 256 / G;
-        attend_sum_kernel<T, G>
-            <<<dim3((unsigned)join_blocks((quads + each - 1) / each), n), 256, 0, stream>>>(
-                k.part, k.splits, k.B, H, (int)Tn, k.D, one, two);
+        const dim3 grid((unsigned)join_blocks((quads + each - 1) / each), n);
+        if (k.last) {
+            attend_sum_kernel<T, G><<<grid, 256, 0, stream>>>(k.part, k.slots, k.parts, k.B, H,
+                                                              (int)Tn, k.D, one, two);
+            return;
+        }
+        const int64_t rows = (int64_t)k.B * H * Tn;
+        SeqK left{k.part + k.splits * rows * k.D, H * Tn * k.D, k.D, Tn * k.D}, more = left;
+        more.data = (float *)left.data + k.slots * rows * k.D;
+        attend_sum_kernel<float, G><<<grid, 256, 0, stream>>>(k.part, k.slots, k.parts, k.B, H,
+                                                              (int)Tn, k.D, left, more);
     };
     if (k.splits > 8)
         go(std::integral_constant<int, 32>());
@@ -959,7 +975,8 @@ hipError_t launch_back_q(const AttendK &k, const AttendPlan &p, hipStream_t stre
     if (e == hipSuccess && k.splits > 1) e = launch_sum<T>(k, k.H, k.Tq, k.dq, k.dq, 1, stream);
     if (e == hipSuccess && entries && k.dtable) {
         attend_table_kernel<<<dim3(k.bias.axes, k.H), 1024, 0, stream>>>(
-            k.part_table, k.B, k.H, k.splits * k.blocks, k.bias.axes, k.bias.buckets, k.dtable);
+            k.part_table, k.B, k.H, k.splits * k.blocks, k.bias.axes, k.bias.buckets, k.table_sum,
+            k.pass > 0, k.last, k.dtable);
         e = hipGetLastError();
     }
     return e;

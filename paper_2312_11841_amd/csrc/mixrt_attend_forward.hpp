@@ -21,7 +21,7 @@ struct ForwardWork {
         b = id / packs;
         kvh = h0 / (k.H / k.Hk);
         len = valid_keys(k.lens, b, k.Tk);
-        first = split * k.per;
+        first = k.from + split * k.per;
         last = min(len, first + k.per);
     }
 };
@@ -572,7 +572,8 @@ __global__ __launch_bounds__(256, kFlowWaves<DP>) void attend_flow_kernel(Attend
 // Joins the splits of a row: o = sum_s 2^(lse_s - top) o_s / sum_s 2^(lse_s - top).
 // A block takes 256 / (8 G) rows and 32 elements of their heads: 8 lanes hold a row's
 // quads, G groups of them share its splits.  (With the splits of a row one after
-// another, the 113 of one token's 32 heads took 29 us.)
+// another, the 113 of one token's 32 heads took 29 us.)  What the passes before left is
+// one part more, and of a pass that is not the last the result is the next one's.
 template <typename T, int G>
 __device__ __forceinline__ void join_row(const AttendK &k, int64_t row, float (&part)[5][256])
 {
@@ -580,20 +581,25 @@ __device__ __forceinline__ void join_row(const AttendK &k, int64_t row, float (&
     const int lane = threadIdx.x & 7, g = threadIdx.x / 8 % G;
     const bool there = row < rows;
     const int d = 32 * blockIdx.y + 4 * lane;
+    // (blocks that share a row read what one of them writes for the next pass, so there
+    // are two places for it)
+    const auto lse_of = [&](int s) {
+        return k.part_lse[(s + (s == k.splits ? (k.pass + 1) & 1 : 0)) * rows + row];
+    };
     // the group's own maximum first: NaN stays
     float top = -INFINITY;
     if (there)
 #pragma unroll 4
-        for (int s = g; s < k.splits; s += G) {
-            const float x = k.part_lse[s * rows + row].x;
+        for (int s = g; s < k.parts; s += G) {
+            const float x = lse_of(s).x;
             top = x > top || x != x ? x : top;
         }
     float base = top == -INFINITY ? 0.0f : top;
     float a[4] = {0, 0, 0, 0}, w = 0.0f;
     if (there)
 #pragma unroll 4
-        for (int s = g; s < k.splits; s += G) {
-            const float2 lse = k.part_lse[s * rows + row];
+        for (int s = g; s < k.parts; s += G) {
+            const float2 lse = lse_of(s);
             const float e = __builtin_amdgcn_exp2f((lse.x - base) + lse.y);
             w += e;
             const float *o = k.part + (s * rows + row) * k.D;
@@ -641,8 +647,17 @@ __device__ __forceinline__ void join_row(const AttendK &k, int64_t row, float (&
     const float inv = w == 0.0f ? 0.0f : 1.0f / w;
     const int64_t bh = row / k.Tq;
     const int t = (int)(row - bh * k.Tq), b = (int)(bh / k.H), h = (int)(bh - (int64_t)b * k.H);
-    if (k.lse && lane == 0 && blockIdx.y == 0) {
-        const RowSum sums(base, w, INFINITY);
+    const RowSum sums(base, w, k.last ? INFINITY : -INFINITY);
+    const bool first = lane == 0 && blockIdx.y == 0;
+    if (!k.last) {
+        if (first)
+            k.part_lse[(k.splits + (k.pass & 1)) * rows + row] = make_float2(sums.lse, sums.rest);
+        if (d < k.D)
+            store_quad<float>(k.part + (k.splits * rows + row) * k.D, d, k.D, a[0] * inv,
+                              a[1] * inv, a[2] * inv, a[3] * inv);
+        return;
+    }
+    if (k.lse && first) {
         k.lse[row] = sums.lse;
         if (k.lse_rest) k.lse_rest[row] = sums.rest;
     }

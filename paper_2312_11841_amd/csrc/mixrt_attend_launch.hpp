@@ -22,11 +22,19 @@ hipError_t launch_attend(AttendK k, int stage, hipStream_t stream)
     k.blocks = p.blocks;
     k.splits = p.splits;
     k.per = p.per;
+    k.slots = attend_slots(p);
     auto go = [&](auto dp) {
         constexpr int DP = decltype(dp)::value;
-        if (stage == kAttendForward) return launch_forward<T, DP>(k, p, stream);
-        if (stage == kAttendBackQ) return launch_back_q<T, DP>(k, p, stream);
-        return launch_back_kv<T, DP>(k, p, stream);
+        hipError_t e = hipSuccess;
+        for (k.pass = 0; k.pass < p.passes && e == hipSuccess; ++k.pass) {
+            k.from = k.pass * p.splits * p.per;
+            k.parts = p.splits + (k.pass > 0);
+            k.last = k.pass + 1 == p.passes;
+            e = stage == kAttendForward ? launch_forward<T, DP>(k, p, stream)
+                : stage == kAttendBackQ ? launch_back_q<T, DP>(k, p, stream)
+                                        : launch_back_kv<T, DP>(k, p, stream);
+        }
+        return e;
     };
     switch (attend_dim(k.D)) {
     case 32: return go(std::integral_constant<int, 32>());

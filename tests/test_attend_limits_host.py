@@ -189,3 +189,19 @@ def test_calls_of_too_many_blocks_are_refused_and_others_not(backward):
                dict(batch=1024, queries=1, keys=9000),
                dict(queries=65536, keys=65536, head_dim=128)):
         assert _workspace(backward, **kw)[0] == 0, kw
+
+
+@pytest.mark.parametrize("dtype,longest", [(mixrt.MIXRT_F32, 2048), (mixrt.MIXRT_BF16, 32768)])
+@pytest.mark.parametrize("tokens", [8192, 40000, 65536, 262144])
+def test_scratch_does_not_grow_with_the_square_of_the_tokens(tokens, dtype, longest):
+    """Walks run in passes: at most four parts and what the passes before left, and one
+    more for every 64 chains; the backward pass holds those of two arrays."""
+    H, D = 16, 128
+    array = 4 * H * D * tokens
+    parts = 5 + tokens // longest // 64
+    for backward in (0, 1):
+        rc, size = _workspace(backward, head_dim=D, heads=H, kv_heads=H, queries=tokens,
+                              keys=tokens, dtype=dtype)
+        assert rc == 0
+        sums = 16 * H * tokens * (parts + 1) + (1 << 20)
+        assert size <= (2 if backward else 1) * parts * array + sums, size / array

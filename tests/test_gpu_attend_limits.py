@@ -491,3 +491,42 @@ def test_what_rounding_took_from_lse_may_be_left_out(r):
     with pytest.raises(ValueError, match="lse_rest"):
         r.attention_backward(dout, q, k, v, o, mixrt.AttentionSaved(
             saved.lse, saved.rest, saved.lse_rest[:, :1]))
+
+
+# --- long walks, in passes -----------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype,queries,keys,length,axes", [
+    ("f32", 70, 8300, None, 0), ("f32", 70, 20000, None, 2), ("f32", 70, 20000, 9000, 0),
+    ("f32", 70, 20000, 100, 1), ("f32", 70, 20000, 0, 1), ("f32", 9000, 70, None, 0),
+    ("f32", 18000, 70, 66, 2), ("f16", 70, 140000, None, 1), ("bf16", 70, 140000, 100000, 0),
+    ("bf16", 140000, 70, None, 0), ("f16", 140000, 70, None, 1)])
+def test_walks_that_run_in_passes(r, dtype, queries, keys, length, axes):
+    """Many heads over walks of more than four splits: one head against the statement,
+    the others have its bits."""
+    dt, H, D = DT[dtype], 512, 12
+    g = _gen(15)
+    q, dout = (torch.randn((1, queries, 1, D), generator=g).to(dt) for _ in range(2))
+    k, v = (torch.randn((1, keys, 1, D), generator=g).to(dt) for _ in range(2))
+    lens = None if length is None else torch.tensor([length], dtype=torch.int32)
+    bias = on = None
+    if axes:
+        table = torch.randn((axes, 5, 1), generator=g)
+        buckets = torch.randint(0, 5, (axes, 21), generator=g).to(torch.uint8)
+        places = [torch.stack([torch.arange(n) % 40, torch.arange(n) // 40 % 40], 1)[:, :axes]
+                  .to(torch.int32).contiguous() for n in (queries, keys)]
+        bias = (table, buckets, *places)
+        on = mixrt.RelativeBias(*[t.cuda() for t in (
+            table.expand(-1, -1, H).contiguous(), buckets, *places)])
+    say(dtype, queries, keys, length, axes)
+    cq, ck, cv, cd = (t.cuda().expand(-1, -1, H, -1) for t in (q, k, v, dout))
+    kw = dict(lens=None if lens is None else lens.cuda(), bias=on)
+    want = ref.attention(q, k, v, dt, lens, bias, dout=dout)
+    served = ref.attention(q, k, v, dt, lens, bias)["o"]
+    _inside(r.attention(cq, ck, cv, **kw)[:, :, :1], served, "o")
+    o, saved = r.attention_train(cq, ck, cv, **kw)
+    grads = r.attention_backward(cd, cq, ck, cv, o, saved, **kw)
+    for name, got in zip(("o", "dq", "dk", "dv", "dtable"), (o, *grads)):
+        assert torch.equal(got, got[:, :, :1].expand_as(got)), name
+        _inside(got[:, :, :1], want[name], name)
+    for a, b in zip(grads, r.attention_backward(cd, cq, ck, cv, o, saved, **kw)):
+        assert torch.equal(a, b)
