@@ -1052,6 +1052,17 @@ class Renderer:
             return _without_derivative(name, outs, [t for t in inputs if t is not None])
         return outs
 
+    def _refuse_tangents(self, name: str, *inputs):
+        """A call inside forward_ad.dual_level() would drop its inputs' tangents, which
+        requires_grad does not show.  (Outside one this takes 0.1 us.)"""
+        ad = self._torch.autograd.forward_ad
+        if getattr(ad, "_current_level", 0) < 0:
+            return
+        for t in inputs:
+            if isinstance(t, self._torch.Tensor) and ad.unpack_dual(t).tangent is not None:
+                raise RuntimeError(f"{name}: no derivative in forward mode, but an input carries a "
+                                   "tangent; call it on the primal tensors")
+
     def _refuse_out(self, name: str, inputs):
         """An output that the caller gave cannot carry a graph."""
         if self._torch.is_grad_enabled() and any(t is not None and t.requires_grad
@@ -1124,6 +1135,7 @@ class Renderer:
         gamma, beta: float32 [channels] or None.  out: x's shape and type, or
         x itself."""
         p = self._norm(x, groups, eps, act, "x")
+        self._refuse_tangents("group_norm", x, gamma, beta)
         if out is not None:
             self._refuse_out("group_norm", (x, gamma, beta))
         y = self._norm_forward(p, x, gamma, beta, out, None, None, self._here())
@@ -1138,6 +1150,7 @@ class Renderer:
         groups' (mean, 1 / deviation) as float32 [images, groups, 2], and x
         kept in 8 bits, which the same passes over x write."""
         p = self._norm(x, groups, eps, act, "x")
+        self._refuse_tangents("group_norm_train", x, gamma, beta)
         if out is not None:
             self._refuse_out("group_norm_train", (x, gamma, beta))
         here = self._here()
@@ -1167,6 +1180,7 @@ class Renderer:
             _like(saved, "saved", dy.shape, dy.dtype, self.device)
             xd = C.byref(_as_map(saved, "saved")[3])
         x = None if xd is None else saved
+        self._refuse_tangents("group_norm_backward", dy, stats, gamma, beta, x)
         if out is not None:
             self._refuse_out("group_norm_backward", (dy, stats, gamma, beta, x))
         p.norm.gamma = _per_channel(gamma, "gamma", p.channels, self.device)
@@ -1225,6 +1239,7 @@ class Renderer:
         without bias)."""
         kd = kept.descriptor(self.device)
         _on_gpu(dy, "dy", self.device)
+        self._refuse_tangents("linear_weight_grad", dy)
         if dy.dtype != kept.dtype:
             raise ValueError(f"dy: dtype {dy.dtype}, expected the checkpoint's {kept.dtype}")
         rows, outs, stride = _as_rows(dy, "dy")
@@ -1267,6 +1282,7 @@ class Renderer:
                 key += (x.shape, x.stride(), x.dtype, x.get_device())
         except AttributeError:
             raise TypeError("heads, pos, freq and axis: expected torch.Tensors") from None
+        self._refuse_tangents("rotary", *arrays, pos, freq)
         if out is None:
             here = self._here()
             outs = tuple([self._empty_like(x, here) for x in arrays])
@@ -1328,6 +1344,7 @@ class Renderer:
         single, arrays, weights = self._as_arrays(heads, weights)
         eps = float(eps)
         key = self._normed_key("rotary_norm", arrays, (), weights, pos, freq, axis, layout)
+        self._refuse_tangents("rotary_norm", *arrays, *weights, pos, freq)
         if out is None:
             here = self._here()
             outs = tuple([self._empty_like(x, here) for x in arrays])
@@ -1372,6 +1389,7 @@ class Renderer:
                                layout)
         here = self._here()
         inputs = (*grads, *arrays, *weights, pos, freq)
+        self._refuse_tangents("rotary_norm_backward", *inputs)
         if out is None:
             outs = tuple([self._empty_like(x, here) for x in arrays])
         else:
@@ -1509,6 +1527,7 @@ class Renderer:
         down to 2^-32 of the row's largest); sums are in 32 bits."""
         p = self._attention_plan(q, k, v, lens, bias, scale, False)
         table = None if bias is None else bias.table
+        self._refuse_tangents("attention", q, k, v, table)
         if out is not None:
             self._refuse_out("attention", (q, k, v, table))
         out = self._attend(p, q, out, None, None, None, self._here())
@@ -1523,6 +1542,7 @@ class Renderer:
         gradient), and what attention_backward needs besides (an AttentionSaved)."""
         p = self._attention_plan(q, k, v, lens, bias, scale, False)
         table = None if bias is None else bias.table
+        self._refuse_tangents("attention_train", q, k, v, table)
         if out is not None:
             self._refuse_out("attention_train", (q, k, v, table))
         here = self._here()
@@ -1541,6 +1561,8 @@ class Renderer:
         other arguments as it had them.  Gradients of keys and values are summed
         over the query heads that share them, and 0 behind lens."""
         p = self._attention_plan(q, k, v, lens, bias, scale, True)
+        self._refuse_tangents("attention_backward", dout, q, k, v, out,
+                              None if bias is None else bias.table)
         dev, f32 = self.device, self._torch.float32
         _like(dout, "dout", q.shape, q.dtype, dev)
         _like(out, "out", q.shape, q.dtype, dev)
