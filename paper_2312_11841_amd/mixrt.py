@@ -1481,7 +1481,7 @@ class Renderer:
                 raise ValueError(f"lens: {lens.dtype} {tuple(lens.shape)}, expected contiguous "
                                  f"int32 ({B},)")
         p.att = Attention(B, H, Hk, D, _elem_code(q.dtype, "q"),
-                          1.0 / D ** 0.5 if scale is None else scale, Tq, Tk, 0, 0)
+                          1.0 / max(D, 1) ** 0.5 if scale is None else scale, Tq, Tk, 0, 0)
         p.bias = None if bias is None else _bias_desc(bias, B, Tq, Tk, H, self.device)
         p.att_ref = C.byref(p.att)
         p.bias_ref = None if bias is None else C.byref(p.bias)

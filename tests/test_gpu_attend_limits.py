@@ -530,3 +530,10 @@ def test_walks_that_run_in_passes(r, dtype, queries, keys, length, axes):
         _inside(got[:, :, :1], want[name], name)
     for a, b in zip(grads, r.attention_backward(cd, cq, ck, cv, o, saved, **kw)):
         assert torch.equal(a, b)
+
+
+def test_heads_without_elements_are_refused_by_name(r):
+    q = torch.zeros((1, 3, 2, 0), device="cuda")
+    for call in (r.attention, r.attention_train):
+        with pytest.raises(mixrt.MixrtError, match="head_dim"):
+            call(q, q, q)
