@@ -627,7 +627,7 @@ typedef struct {
     int32_t kv_heads;     /* divides heads */
     int32_t head_dim;     /* 1..MIXRT_MAX_ATTENTION_DIM */
     int32_t dtype;        /* of all heads: MIXRT_F32, _F16 or _BF16 */
-    float scale;          /* > 0, finite */
+    float scale;          /* > 0, at most 2^127 */
     int64_t queries;      /* >= 0, < 2^30 */
     int64_t keys;         /* >= 0, < 2^30 */
     const int32_t *lens;  /* device [batch]: valid keys of each entry, or NULL:

@@ -186,6 +186,7 @@ constexpr int64_t kMaxStride = (int64_t)1 << 40;
 constexpr int64_t kMaxTokens = (int64_t)1 << 30;
 constexpr int kMaxHeads = 65535;
 constexpr int kMaxHeadDim = 1024;
+constexpr float kLog2e = 1.4426950408889634f;
 
 bool aligned(const void *p, size_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
 
@@ -252,7 +253,8 @@ int check_attention(mixrt_ctx *ctx, const mixrt_attention *a, const mixrt_relati
                     MIXRT_MAX_ATTENTION_DIM);
     if (!elem_size(a->dtype))
         return fail(ctx, MIXRT_EUNSUPPORTED, "attention.dtype=%d (F32, F16 or BF16)", a->dtype);
-    if (!(a->scale > 0.0f) || !std::isfinite(a->scale))
+    // (scores are in units of log2)
+    if (!(a->scale > 0.0f) || !std::isfinite(a->scale * kLog2e))
         return fail(ctx, MIXRT_EINVAL, "attention.scale=%g", a->scale);
     if (a->queries < 0 || a->keys < 0)
         return fail(ctx, MIXRT_EINVAL, "attention.queries=%lld, keys=%lld", (long long)a->queries,
@@ -410,7 +412,7 @@ mixrt::AttendK attend_k(const mixrt_attention *a, const mixrt_relative_bias *b)
     k.Tk = (int)a->keys;
     k.dtype = a->dtype;
     k.plain_scale = a->scale;
-    k.scale = a->scale * 1.4426950408889634f;
+    k.scale = a->scale * kLog2e;
     k.lens = a->lens;
     k.lse_rest = a->lse_rest;
     if (b)

@@ -205,3 +205,10 @@ def test_scratch_does_not_grow_with_the_square_of_the_tokens(tokens, dtype, long
         assert rc == 0
         sums = 16 * H * tokens * (parts + 1) + (1 << 20)
         assert size <= (2 if backward else 1) * parts * array + sums, size / array
+
+
+def test_scales_that_leave_32_bits_in_units_of_log2_are_refused():
+    assert _workspace(scale=2.0 ** 127)[0] == 0
+    assert _workspace(scale=2.0 ** -149)[0] == 0
+    for scale in (3e38, 2.4e38):
+        assert _workspace(scale=scale) == (-1, 0)
