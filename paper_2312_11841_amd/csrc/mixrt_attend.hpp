@@ -1,6 +1,6 @@
 // The refiner's attention: launch interface between the C ABI
-// (mixrt_attend_api.cpp) and the kernels (mixrt_attend_kernels.hpp, built for
-// one element type each).
+// (mixrt_attend_api.cpp) and the kernels (mixrt_attend_forward.hpp and
+// mixrt_attend_backward.hpp, built for one element type each).
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -93,12 +93,12 @@ inline int64_t attend_blocks(const AttendPlan &p, int B, int heads)
 // of each of its 128 columns (or four waves' 32).
 inline int attend_hist_bytes(int entries) { return 512 * (entries + 1); }
 
-AttendPlan plan_attend(int B, int H, int Hk, int64_t Tq, int64_t Tk, int D, int dtype, int axes,
-                       int entries);
-AttendPlan plan_attend_dq(int B, int H, int Hk, int64_t Tq, int64_t Tk, int D, int dtype, int axes,
-                       int entries);
+// entries: of the bias' table, 0 without one (the keys' gradient keeps none of them).
+AttendPlan plan_attend(int B, int H, int Hk, int64_t Tq, int64_t Tk, int D, int dtype, int entries);
+AttendPlan plan_attend_dq(int B, int H, int Hk, int64_t Tq, int64_t Tk, int D, int dtype,
+                          int entries);
 AttendPlan plan_attend_dkv(int B, int H, int Hk, int64_t Tq, int64_t Tk, int D, int dtype,
-                           int axes, int entries);
+                           int entries);
 
 // Launches of one element type.
 hipError_t launch_attend_f32(const AttendK &k, int stage, hipStream_t stream);

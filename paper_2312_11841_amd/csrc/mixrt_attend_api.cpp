@@ -105,8 +105,7 @@ int blocks_of(int64_t n, int cols)
 
 }  // namespace
 
-AttendPlan plan_attend(int B, int H, int Hk, int64_t Tq, int64_t Tk, int D, int dtype, int axes,
-                       int entries)
+AttendPlan plan_attend(int B, int H, int Hk, int64_t Tq, int64_t Tk, int D, int dtype, int entries)
 {
     AttendPlan p{};
     p.pack = 1;
@@ -117,7 +116,7 @@ AttendPlan plan_attend(int B, int H, int Hk, int64_t Tq, int64_t Tk, int D, int 
     const int64_t cols = Tq * p.pack, heads = (int64_t)B * (H / p.pack);
     p.shared = shares(heads, cols, Tk);
     p.cols = p.shared ? 32 : 128;
-    if (attend_elem(dtype) == 2 && D <= 64 && axes == 0 && !p.shared && cols > 1024) p.cols = 256;
+    if (attend_elem(dtype) == 2 && D <= 64 && entries == 0 && !p.shared && cols > 1024) p.cols = 256;
     p.blocks = blocks_of(cols, p.cols);
     const int64_t blocks = heads * p.blocks;
     const int64_t s = p.shared ? enough(Tk, blocks, 256)
@@ -127,7 +126,7 @@ AttendPlan plan_attend(int B, int H, int Hk, int64_t Tq, int64_t Tk, int D, int 
     return p;
 }
 
-AttendPlan plan_attend_dq(int B, int H, int Hk, int64_t Tq, int64_t Tk, int D, int dtype, int axes,
+AttendPlan plan_attend_dq(int B, int H, int Hk, int64_t Tq, int64_t Tk, int D, int dtype,
                           int entries)
 {
     AttendPlan p{};
@@ -137,22 +136,21 @@ AttendPlan plan_attend_dq(int B, int H, int Hk, int64_t Tq, int64_t Tk, int D, i
     // (a wave's own tiles beside the table's sums may be more than a CU's LDS; about
     // 16 KB are other things)
     const int tiles = 4 * 2 * 32 * (attend_dim(D) * attend_elem(dtype) + 16);
-    if (axes && tiles + attend_hist_bytes(entries) + 16384 > 163840) p.shared = 0;
+    if (entries && tiles + attend_hist_bytes(entries) + 16384 > 163840) p.shared = 0;
     p.cols = p.shared ? 32 : 128;
     p.blocks = blocks_of(Tq, p.cols);
     int64_t most = longest(dtype);
-    if (axes && p.shared && most > 4096) most = 4096;   // (1024 keys of a lane's table sums)
+    if (entries && p.shared && most > 4096) most = 4096;   // (1024 keys of a lane's table sums)
     // (float32's products are so slow that a wave's second tile is worth a join)
     const int64_t blocks = heads * p.blocks, least = attend_elem(dtype) == 4 ? 128 : 256;
     const int64_t s = p.shared ? enough(Tk, blocks, least)
-                               : whole_rounds(Tk, blocks, resident(D, dtype, axes ? 2 : 3), 512);
+                               : whole_rounds(Tk, blocks, resident(D, dtype, entries ? 2 : 3), 512);
     divide(Tk, s, most, p.shared ? 128 : 32, &p.splits, &p.per);
     in_passes(&p, blocks, s);
     return p;
 }
 
-AttendPlan plan_attend_dkv(int B, int H, int Hk, int64_t Tq, int64_t Tk, int D, int dtype,
-                           int axes, int entries)
+AttendPlan plan_attend_dkv(int B, int H, int Hk, int64_t Tq, int64_t Tk, int D, int dtype, int)
 {
     AttendPlan p{};
     p.pack = 1;
@@ -270,8 +268,7 @@ int check_attention(mixrt_ctx *ctx, const mixrt_attention *a, const mixrt_relati
     int stage = 0;
     for (auto plan : {mixrt::plan_attend, mixrt::plan_attend_dq, mixrt::plan_attend_dkv}) {
         const AttendPlan p = plan(a->batch, a->heads, a->kv_heads, a->queries, a->keys,
-                                  a->head_dim, a->dtype, b ? b->axes : 0,
-                                  b ? b->axes * b->count : 0);
+                                  a->head_dim, a->dtype, b ? b->axes * b->count : 0);
         if (mixrt::attend_blocks(p, a->batch, stage++ == 2 ? a->kv_heads : a->heads) >
             mixrt::kMostBlocks256)
             return fail(ctx, MIXRT_EUNSUPPORTED, "attention: %d entries of %d heads, %lld queries "
@@ -371,7 +368,7 @@ Scratch scratch_of(const mixrt_attention *a, const mixrt_relative_bias *b, bool 
         return from;
     };
     auto plan = [&](auto fn) {
-        return fn(a->batch, a->heads, a->kv_heads, a->queries, a->keys, a->head_dim, a->dtype, axes,
+        return fn(a->batch, a->heads, a->kv_heads, a->queries, a->keys, a->head_dim, a->dtype,
                   axes ? axes * b->count : 0);
     };
     if (!backward) {

@@ -19,26 +19,22 @@ template <typename T> inline constexpr float kWeightLift = kLifted<T> ? 15.0f : 
 constexpr int kHistRows = 1024;
 
 // acc[d][column] += sum over the tile's rows of tile[row][d] p[row][column].
-template <typename T, int DP, int NC>
-__device__ __forceinline__ void add_cols(const T *tile, int lane, const f32x16 (&p)[NC],
-                                         f32x16 (&acc)[NC][DP / 32])
+template <typename T, int DP>
+__device__ __forceinline__ void add_cols(const T *tile, int lane, const f32x16 &p,
+                                         f32x16 (&acc)[DP / 32])
 {
     if constexpr (sizeof(T) == 4) {
 #pragma unroll
         for (int d = 0; d < DP / 32; ++d)
-#pragma unroll
-            for (int n = 0; n < NC; ++n) col_mul<DP>(tile, lane, d, p[n], acc[n][d]);
+            col_mul<DP>(tile, lane, d, p, acc[d]);
     } else {
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-            typename Matrix<T>::frag f[NC];
-#pragma unroll
-            for (int n = 0; n < NC; ++n) f[n] = round_rows<T>(p[n], e);
+            const typename Matrix<T>::frag f = round_rows<T>(p, e);
 #pragma unroll
             for (int d = 0; d < DP / 32; ++d) {
                 const auto a = col_frag<T, DP>(tile, lane, d, e);
-#pragma unroll
-                for (int n = 0; n < NC; ++n) acc[n][d] = Matrix<T>::mul(a, f[n], acc[n][d]);
+                acc[d] = Matrix<T>::mul(a, f, acc[d]);
             }
         }
     }
@@ -47,11 +43,11 @@ __device__ __forceinline__ void add_cols(const T *tile, int lane, const f32x16 (
 // s += a-tile's rows times b, g += e-tile's rows times f.  The operands of 16-bit heads
 // of up to 64 elements are all read first: a wave is often alone on its SIMD, and would
 // wait for LDS before each product.
-template <typename T, int DP, int NC>
+template <typename T, int DP>
 __device__ __forceinline__ void pair_mul(const T *a, const T *e, int lane,
-                                         const typename Matrix<T>::frag (&b)[NC][(kPairs<T, DP>)],
-                                         const typename Matrix<T>::frag (&f)[NC][(kPairs<T, DP>)],
-                                         f32x16 (&s)[NC], f32x16 (&g)[NC], int D)
+                                         const typename Matrix<T>::frag (&b)[(kPairs<T, DP>)],
+                                         const typename Matrix<T>::frag (&f)[(kPairs<T, DP>)],
+                                         f32x16 &s, f32x16 &g, int D)
 {
     constexpr bool FIRST = sizeof(T) == 2 && DP <= 64;
     typename Matrix<T>::frag x[kPairs<T, DP>], y[kPairs<T, DP>];
@@ -64,28 +60,24 @@ __device__ __forceinline__ void pair_mul(const T *a, const T *e, int lane,
         __builtin_amdgcn_sched_barrier(0);
     }
 #pragma unroll
-    for (int c = 0; c < kPairs<T, DP>; ++c)
-#pragma unroll
-        for (int n = 0; n < NC; ++n) {
-            if (DP < 128 && past<T>(c, D)) continue; // at 128 its branches cost registers
-            if (!FIRST) {
-                x[c] = row_frag<T, DP>(a, lane, c);
-                y[c] = row_frag<T, DP>(e, lane, c);
-            }
-            s[n] = Matrix<T>::mul(x[c], b[n][c], s[n]);
-            g[n] = Matrix<T>::mul(y[c], f[n][c], g[n]);
+    for (int c = 0; c < kPairs<T, DP>; ++c) {
+        if (DP < 128 && past<T>(c, D)) continue;    // at 128 its branches cost registers
+        if (!FIRST) {
+            x[c] = row_frag<T, DP>(a, lane, c);
+            y[c] = row_frag<T, DP>(e, lane, c);
         }
+        s = Matrix<T>::mul(x[c], b[c], s);
+        g = Matrix<T>::mul(y[c], f[c], g);
+    }
 }
 
-template <int NC, int ND>
-__device__ __forceinline__ void clear(f32x16 (&a)[NC][ND])
+template <int ND>
+__device__ __forceinline__ void clear(f32x16 (&a)[ND])
 {
 #pragma unroll
-    for (int n = 0; n < NC; ++n)
+    for (int d = 0; d < ND; ++d)
 #pragma unroll
-        for (int d = 0; d < ND; ++d)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) a[n][d][i] = 0.0f;
+        for (int i = 0; i < 16; ++i) a[d][i] = 0.0f;
 }
 
 // The exponent of a pair's weight, s unit - lse - rest, where lse is so large that its
@@ -112,50 +104,44 @@ __device__ __forceinline__ float exponent(float s, float unit, float lse, float 
 // sets it, later ones seldom.)  The power is at most 2^100, and follows from the
 // largest dS itself and not from a product with the last power, which may not be
 // finite: a key may get weights of 2^-125 from the first queries and 1/2 from the next.
-template <typename T, int NC, int ND>
+template <typename T, int ND>
 struct Lift {
-    float by[NC], most[NC];     // the power; the largest |dS| so far
+    float by, most;     // the power; the largest |dS| so far
     __device__ __forceinline__ void start()
     {
-#pragma unroll
-        for (int n = 0; n < NC; ++n) {
-            by[n] = 1.0f;
-            most[n] = 0.0f;
-        }
+        by = 1.0f;
+        most = 0.0f;
     }
-    __device__ __forceinline__ void scale(f32x16 (&g)[NC], f32x16 (&acc)[NC][ND])
+    __device__ __forceinline__ void scale(f32x16 &g, f32x16 (&acc)[ND])
     {
         if (sizeof(T) != 2 || !kLifted<T>) return;
+        float m = 0.0f;
 #pragma unroll
-        for (int n = 0; n < NC; ++n) {
-            float m = 0.0f;
+        for (int i = 0; i < 16; ++i) m = fmaxf(m, fabsf(g[i]));
+        m = fmaxf(most, half_max(m));
+        most = m;
+        // (a product that is not finite is out of range too; an m that is not has no
+        // power)
+        const float lifted = m * by;
+        const bool out = (lifted > 0x1p15f || (lifted < 1.0f && m > 0.0f)) && m < INFINITY;
+        if (__builtin_amdgcn_ballot_w64(out) != 0 && out) {
+            const int now = (int)(__float_as_uint(by) >> 23);
+            const int to = min(max(127 + 127 + 8 - (int)(__float_as_uint(m) >> 23), 27), 227);
+            const float f = __uint_as_float((uint32_t)(127 + (to - now) / 2) << 23);
+            const float e = __uint_as_float((uint32_t)(127 + (to - now) - (to - now) / 2) << 23);
+            by = __uint_as_float((uint32_t)to << 23);
 #pragma unroll
-            for (int i = 0; i < 16; ++i) m = fmaxf(m, fabsf(g[n][i]));
-            m = fmaxf(most[n], half_max(m));
-            most[n] = m;
-            // (a product that is not finite is out of range too; an m that is not has no
-            // power)
-            const float lifted = m * by[n];
-            const bool out = (lifted > 0x1p15f || (lifted < 1.0f && m > 0.0f)) && m < INFINITY;
-            if (__builtin_amdgcn_ballot_w64(out) != 0 && out) {
-                const int now = (int)(__float_as_uint(by[n]) >> 23);
-                const int to = min(max(127 + 127 + 8 - (int)(__float_as_uint(m) >> 23), 27), 227);
-                const float f = __uint_as_float((uint32_t)(127 + (to - now) / 2) << 23);
-                const float e = __uint_as_float((uint32_t)(127 + (to - now) - (to - now) / 2) << 23);
-                by[n] = __uint_as_float((uint32_t)to << 23);
+            for (int d = 0; d < ND; ++d)
 #pragma unroll
-                for (int d = 0; d < ND; ++d)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) acc[n][d][i] = acc[n][d][i] * f * e;
-            }
-#pragma unroll
-            for (int i = 0; i < 16; ++i) g[n][i] *= by[n];
+                for (int i = 0; i < 16; ++i) acc[d][i] = acc[d][i] * f * e;
         }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) g[i] *= by;
     }
     // the factor that takes a column's sums back
-    __device__ __forceinline__ float back(int n) const
+    __device__ __forceinline__ float back() const
     {
-        return kLifted<T> ? 1.0f / by[n] : 1.0f;
+        return kLifted<T> ? 1.0f / by : 1.0f;
     }
 };
 
@@ -318,11 +304,10 @@ __device__ __forceinline__ void store_column(T *row, int half, int D, const f32x
 // 31%: the table's sums take LDS, so two blocks run on a CU, and their waves wait 43% of
 // their time, for reads of places that the adds before have written.
 
-template <typename T, int DP, int NC, bool BIAS, bool SHARED>
+template <typename T, int DP, bool BIAS, bool SHARED>
 __global__ __launch_bounds__(256) void attend_dq_kernel(AttendK k)
 {
     typedef typename Matrix<T>::frag frag;
-    static_assert(!SHARED || NC == 1, "waves share 32 columns");
     constexpr int ROWS = 32, THREADS = 256, WAVES = SHARED ? 4 : 1;
     constexpr int TILE = ROWS * kStride<T, DP>;
     // (two of the widest tiles and the table's sums are more than a CU's 160 KB)
@@ -349,51 +334,44 @@ __global__ __launch_bounds__(256) void attend_dq_kernel(AttendK k)
     const int first = k.from + split * k.per, last = min(len, first + k.per);
     const int entries = BIAS ? k.bias.axes * k.bias.buckets : 0;
 
-    int t[NC];
-    bool there[NC];
-    frag q[NC][kPairs<T, DP>], dout[NC][kPairs<T, DP>];
-    float lse[NC], lse_rest[NC], delta[NC];
-    bool large = false;         // (of the whole wave)
-    int qpos[NC][kMaxBiasAxes];
+    const int t = (SHARED ? rb : rb * 4 + wave) * 32 + (lane & 31);
+    const bool there = t < k.Tq;
+    const int64_t tt = t;
+    frag q[kPairs<T, DP>], dout[kPairs<T, DP>];
+    load_column<T, DP>(q, (const T *)k.q.data + b * k.q.batch + tt * k.q.token + h * k.q.head,
+                       there, half, k.D);
+    load_column<T, DP>(dout, (const T *)k.dout.data + b * k.dout.batch + tt * k.dout.token +
+                                 h * k.dout.head, there, half, k.D);
+    // delta = sum_d dout o, with what rounding took from o
+    float sum = 0.0f;
+    {
+        frag o[kPairs<T, DP>], rest[kPairs<T, DP>];
+        load_column<T, DP>(o, (const T *)k.o.data + b * k.o.batch + tt * k.o.token + h * k.o.head,
+                           there, half, k.D);
+        if (sizeof(T) == 2)
+            load_column<T, DP>(rest, (const T *)k.rest + ((b * (int64_t)k.Tq + tt) * k.H + h) * k.D,
+                               there, half, k.D);
 #pragma unroll
-    for (int n = 0; n < NC; ++n) {
-        t[n] = ((SHARED ? rb : rb * 4 + wave) * NC + n) * 32 + (lane & 31);
-        there[n] = t[n] < k.Tq;
-        const int64_t tt = t[n];
-        load_column<T, DP>(q[n], (const T *)k.q.data + b * k.q.batch + tt * k.q.token +
-                                     h * k.q.head, there[n], half, k.D);
-        load_column<T, DP>(dout[n], (const T *)k.dout.data + b * k.dout.batch + tt * k.dout.token +
-                                        h * k.dout.head, there[n], half, k.D);
-        // delta = sum_d dout o, with what rounding took from o
-        float sum = 0.0f;
-        {
-            frag o[kPairs<T, DP>], rest[kPairs<T, DP>];
-            load_column<T, DP>(o, (const T *)k.o.data + b * k.o.batch + tt * k.o.token +
-                                      h * k.o.head, there[n], half, k.D);
-            if (sizeof(T) == 2)
-                load_column<T, DP>(rest, (const T *)k.rest + ((b * (int64_t)k.Tq + tt) * k.H + h) *
-                                                                 k.D, there[n], half, k.D);
+        for (int c = 0; c < kPairs<T, DP>; ++c)
 #pragma unroll
-            for (int c = 0; c < kPairs<T, DP>; ++c)
-#pragma unroll
-                for (int i = 0; i < kChunk<T>; ++i) {
-                    float x = (float)o[c][i];
-                    if (sizeof(T) == 2) x = whole_of<T>(o[c][i], rest[c][i]);
-                    sum = fmaf((float)dout[n][c][i], x, sum);
-                }
-        }
-        delta[n] = half_sum(sum);
-        const int64_t row = ((int64_t)b * k.H + h) * k.Tq + tt;
-        lse[n] = there[n] ? k.lse[row] : INFINITY;
-        lse_rest[n] = there[n] && k.lse_rest ? k.lse_rest[row] : 0.0f;
-        large = large || __builtin_amdgcn_ballot_w64(large_sum(lse[n])) != 0;
-        if (there[n] && half == 0 && split == 0 && me == 0) k.delta[row] = delta[n];
-#pragma unroll
-        for (int a = 0; a < kMaxBiasAxes; ++a)
-            qpos[n][a] = BIAS && there[n] && a < k.bias.axes
-                             ? k.bias.qpos[b * k.bias.qbatch + tt * k.bias.axes + a]
-                             : 0;
+            for (int i = 0; i < kChunk<T>; ++i) {
+                float x = (float)o[c][i];
+                if (sizeof(T) == 2) x = whole_of<T>(o[c][i], rest[c][i]);
+                sum = fmaf((float)dout[c][i], x, sum);
+            }
     }
+    const float delta = half_sum(sum);
+    const int64_t row = ((int64_t)b * k.H + h) * k.Tq + tt;
+    const float lse = there ? k.lse[row] : INFINITY;
+    const float lse_rest = there && k.lse_rest ? k.lse_rest[row] : 0.0f;
+    const bool large = __builtin_amdgcn_ballot_w64(large_sum(lse)) != 0;    // (in the wave)
+    int qpos[kMaxBiasAxes];
+    if (there && half == 0 && split == 0 && me == 0) k.delta[row] = delta;
+#pragma unroll
+    for (int a = 0; a < kMaxBiasAxes; ++a)
+        qpos[a] = BIAS && there && a < k.bias.axes
+                      ? k.bias.qpos[b * k.bias.qbatch + tt * k.bias.axes + a]
+                      : 0;
     const int held = entries + 1;
     if (BIAS) {
         load_bias(dense, k.bias, h, k.H, threadIdx.x, THREADS, false);
@@ -408,9 +386,9 @@ __global__ __launch_bounds__(256) void attend_dq_kernel(AttendK k)
     float *mine = hist + wave * 32 * held + (lane & 31);
     double table = 0.0;         // thread e: entry e's sum of the block
 
-    f32x16 acc[NC][DP / 32];
+    f32x16 acc[DP / 32];
     clear(acc);
-    Lift<T, NC, DP / 32> lift;
+    Lift<T, DP / 32> lift;
     lift.start();
     const T *kp = (const T *)k.k.data + b * k.k.batch + kvh * k.k.head;
     const T *vp = (const T *)k.v.data + b * k.v.batch + kvh * k.v.head;
@@ -462,53 +440,42 @@ __global__ __launch_bounds__(256) void attend_dq_kernel(AttendK k)
         const bool more = row0 + STEP < last;
         if (more && AHEAD) fetch(row0 + STEP);
         const T *kt = tiles[me][cur][0], *vt = tiles[me][cur][1];
-        f32x16 s[NC], g[NC];
+        f32x16 s, g;
 #pragma unroll
-        for (int n = 0; n < NC; ++n)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) s[n][i] = g[n][i] = 0.0f;
-        pair_mul<T, DP, NC>(kt, vt, lane, q, dout, s, g, k.D);
+        for (int i = 0; i < 16; ++i) s[i] = g[i] = 0.0f;
+        pair_mul<T, DP>(kt, vt, lane, q, dout, s, g, k.D);
         if constexpr (BIAS) {
-            const int base[NC] = {};
-            add_bias<NC, ROWS>(s, k.scale, kpos[me][cur], 0, half, dense, base, qpos, k.bias.axes,
+            add_bias<ROWS>(s, k.scale, kpos[me][cur], 0, half, dense, 0, qpos, k.bias.axes,
                                k.bias.reach);
         }
         const float unit = BIAS ? 1.0f : k.scale;
         if (large) {
             rare();
 #pragma unroll
-            for (int n = 0; n < NC; ++n)
-#pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    s[n][i] = exponent(s[n][i], unit, lse[n], lse_rest[n], 0.0f);
+            for (int i = 0; i < 16; ++i)
+                s[i] = exponent(s[i], unit, lse, lse_rest, 0.0f);
         }
+        const float by = large ? 1.0f : unit, less = large ? 0.0f : lse;
+        const float left = large ? 0.0f : lse_rest;
 #pragma unroll
-        for (int n = 0; n < NC; ++n) {
-            const float by = large ? 1.0f : unit, less = large ? 0.0f : lse[n];
-            const float left = large ? 0.0f : lse_rest[n];
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                float x = fmaf(s[n][i], by, -less);
-                if (sizeof(T) == 4) x -= left;
-                g[n][i] = __builtin_amdgcn_exp2f(x) * (g[n][i] - delta[n]);
-            }
+        for (int i = 0; i < 16; ++i) {
+            float x = fmaf(s[i], by, -less);
+            if (sizeof(T) == 4) x -= left;
+            g[i] = __builtin_amdgcn_exp2f(x) * (g[i] - delta);
         }
         if (row0 + ROWS > last) {
             rare();
 #pragma unroll
             for (int i = 0; i < 16; ++i)
                 if (row0 + tile_row(i, half) >= last)
-#pragma unroll
-                    for (int n = 0; n < NC; ++n) g[n][i] = 0.0f;
+                    g[i] = 0.0f;
         }
         if constexpr (BIAS) {
-#pragma unroll
-            for (int n = 0; n < NC; ++n)
-                add_table<ROWS>(g[n], kpos[me][cur], 0, half, place, qpos[n], k.bias.axes, k.bias.reach,
-                                mine, 32 * entries);
+            add_table<ROWS>(g, kpos[me][cur], 0, half, place, qpos, k.bias.axes, k.bias.reach,
+                            mine, 32 * entries);
         }
         lift.scale(g, acc);
-        add_cols<T, DP, NC>(kt, lane, g, acc);
+        add_cols<T, DP>(kt, lane, g, acc);
         counted += ROWS;
         if (BUFS == 1) team.meet();
         if (more) {
@@ -533,28 +500,23 @@ __global__ __launch_bounds__(256) void attend_dq_kernel(AttendK k)
     const int64_t rows = (int64_t)k.B * k.H * k.Tq;
     if constexpr (SHARED) {
         float f[DP / 8];
-        join_waves<DP>((float *)&tiles[0][0][0][0], lane, wave, acc[0], lift.back(0), f);
-        if (!there[0]) return;
+        join_waves<DP>((float *)&tiles[0][0][0][0], lane, wave, acc, lift.back(), f);
+        if (!there) return;
         const int d = (2 * wave + half) * (DP / 8);
-        const int64_t row = ((int64_t)b * k.H + h) * k.Tq + t[0];
         if (k.splits > 1)
             store_run<float>(k.part + (split * rows + row) * k.D, d, k.D, f, some * k.plain_scale);
         else
-            store_run<T>((T *)k.dq.data + b * k.dq.batch + (int64_t)t[0] * k.dq.token +
+            store_run<T>((T *)k.dq.data + b * k.dq.batch + tt * k.dq.token +
                              h * k.dq.head, d, k.D, f, some * k.plain_scale);
         return;
     }
-#pragma unroll
-    for (int n = 0; n < NC; ++n) {
-        if (!there[n]) continue;
-        const float by = some * lift.back(n) * k.plain_scale;
-        if (k.splits > 1) {
-            const int64_t row = ((int64_t)b * k.H + h) * k.Tq + t[n];
-            store_column<float, DP>(k.part + (split * rows + row) * k.D, half, k.D, acc[n], by);
-        } else {
-            store_column<T, DP>((T *)k.dq.data + b * k.dq.batch + (int64_t)t[n] * k.dq.token +
-                                    h * k.dq.head, half, k.D, acc[n], by);
-        }
+    if (!there) return;
+    const float by = some * lift.back() * k.plain_scale;
+    if (k.splits > 1) {
+        store_column<float, DP>(k.part + (split * rows + row) * k.D, half, k.D, acc, by);
+    } else {
+        store_column<T, DP>((T *)k.dq.data + b * k.dq.batch + tt * k.dq.token +
+                                h * k.dq.head, half, k.D, acc, by);
     }
 }
 
@@ -601,11 +563,10 @@ struct StageSums {
     }
 };
 
-template <typename T, int DP, int NC, bool BIAS, bool SHARED>
+template <typename T, int DP, bool BIAS, bool SHARED>
 __global__ __launch_bounds__(256) void attend_dkv_kernel(AttendK k)
 {
     typedef typename Matrix<T>::frag frag;
-    static_assert(!SHARED || NC == 1, "waves share 32 columns");
     constexpr int ROWS = attend_kv_rows(DP, sizeof(T), SHARED);
     constexpr int WAVES = SHARED ? 4 : 1, BUFS = SHARED ? 1 : 2;
     constexpr int TILE = ROWS * kStride<T, DP>, STEP = Team<SHARED>::kStep;
@@ -630,32 +591,26 @@ __global__ __launch_bounds__(256) void attend_dkv_kernel(AttendK k)
     const int a_head = max((k.Tq + ROWS - 1) / ROWS, 1);
     const int first = k.from + split * k.per;
     int last = min(k.Tq > 0 ? G * a_head : 0, first + k.per);
-    if (rb * (SHARED ? 32 : 128 * NC) >= len) last = first;
+    if (rb * (SHARED ? 32 : 128) >= len) last = first;
 
-    int t[NC];
-    bool there[NC], seen[NC];
-    frag key[NC][kPairs<T, DP>], val[NC][kPairs<T, DP>];
-    int kpos[NC][kMaxBiasAxes];
+    const int t = (SHARED ? rb : rb * 4 + wave) * 32 + (lane & 31);
+    const bool there = t < k.Tk, seen = t < len;
+    const int64_t tt = t;
+    frag key[kPairs<T, DP>], val[kPairs<T, DP>];
+    load_column<T, DP>(key, (const T *)k.k.data + b * k.k.batch + tt * k.k.token + kvh * k.k.head,
+                       seen, half, k.D);
+    load_column<T, DP>(val, (const T *)k.v.data + b * k.v.batch + tt * k.v.token + kvh * k.v.head,
+                       seen, half, k.D);
+    int kpos[kMaxBiasAxes];
 #pragma unroll
-    for (int n = 0; n < NC; ++n) {
-        t[n] = ((SHARED ? rb : rb * 4 + wave) * NC + n) * 32 + (lane & 31);
-        there[n] = t[n] < k.Tk;
-        seen[n] = t[n] < len;
-        const int64_t tt = t[n];
-        load_column<T, DP>(key[n], (const T *)k.k.data + b * k.k.batch + tt * k.k.token +
-                                       kvh * k.k.head, seen[n], half, k.D);
-        load_column<T, DP>(val[n], (const T *)k.v.data + b * k.v.batch + tt * k.v.token +
-                                       kvh * k.v.head, seen[n], half, k.D);
-#pragma unroll
-        for (int a = 0; a < kMaxBiasAxes; ++a)
-            kpos[n][a] = BIAS && seen[n] && a < k.bias.axes
-                             ? k.bias.kpos[b * k.bias.kbatch + tt * k.bias.axes + a]
-                             : 0;
-    }
-    f32x16 dk[NC][DP / 32], dv[NC][DP / 32];
+    for (int a = 0; a < kMaxBiasAxes; ++a)
+        kpos[a] = BIAS && seen && a < k.bias.axes
+                      ? k.bias.kpos[b * k.bias.kbatch + tt * k.bias.axes + a]
+                      : 0;
+    f32x16 dk[DP / 32], dv[DP / 32];
     clear(dk);
     clear(dv);
-    Lift<T, NC, DP / 32> lift;
+    Lift<T, DP / 32> lift;
     lift.start();
 
     const T *qp = (const T *)k.q.data + b * k.q.batch;
@@ -714,15 +669,12 @@ __global__ __launch_bounds__(256) void attend_dkv_kernel(AttendK k)
             const T *qt = tiles[me][cur][0] + u * 32 * kStride<T, DP>;
             const T *gt = tiles[me][cur][1] + u * 32 * kStride<T, DP>;
             const float *sm = sums[me][cur] + 32 * u;
-            f32x16 p[NC], g[NC];
+            f32x16 p, g;
 #pragma unroll
-            for (int n = 0; n < NC; ++n)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) p[n][i] = g[n][i] = 0.0f;
-            pair_mul<T, DP, NC>(qt, gt, lane, key, val, p, g, k.D);
+            for (int i = 0; i < 16; ++i) p[i] = g[i] = 0.0f;
+            pair_mul<T, DP>(qt, gt, lane, key, val, p, g, k.D);
             if constexpr (BIAS) {
-                const int base[NC] = {};
-                add_bias<NC, ROWS>(p, k.scale, qpos[me][cur], u, half, dense[me], base, kpos,
+                    add_bias<ROWS>(p, k.scale, qpos[me][cur], u, half, dense[me], 0, kpos,
                                    k.bias.axes, k.bias.reach);
             }
             const float unit = BIAS ? 1.0f : k.scale;
@@ -731,10 +683,7 @@ __global__ __launch_bounds__(256) void attend_dkv_kernel(AttendK k)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
                     const int at = tile_row(i, half);
-#pragma unroll
-                    for (int n = 0; n < NC; ++n)
-                        p[n][i] = exponent(p[n][i], unit, sm[at], sm[2 * ROWS + at],
-                                           kWeightLift<T>);
+                    p[i] = exponent(p[i], unit, sm[at], sm[2 * ROWS + at], kWeightLift<T>);
                 }
             }
             const float by = large ? 1.0f : unit;
@@ -743,17 +692,14 @@ __global__ __launch_bounds__(256) void attend_dkv_kernel(AttendK k)
             for (int i = 0; i < 16; ++i) {
                 const int at = tile_row(i, half);
                 const float lse = less[at], delta = sm[ROWS + at];
-#pragma unroll
-                for (int n = 0; n < NC; ++n) {
-                    float x = fmaf(p[n][i], by, -lse);
-                    if (sizeof(T) == 4) x -= left[at];
-                    p[n][i] = __builtin_amdgcn_exp2f(x);
-                    g[n][i] = p[n][i] * (g[n][i] - delta);
-                }
+                float x = fmaf(p[i], by, -lse);
+                if (sizeof(T) == 4) x -= left[at];
+                p[i] = __builtin_amdgcn_exp2f(x);
+                g[i] = p[i] * (g[i] - delta);
             }
-            add_cols<T, DP, NC>(gt, lane, p, dv);
+            add_cols<T, DP>(gt, lane, p, dv);
             lift.scale(g, dk);
-            add_cols<T, DP, NC>(qt, lane, g, dk);
+            add_cols<T, DP>(qt, lane, g, dk);
         }
         if (BUFS == 1) team.meet();
         if (more) {
@@ -766,17 +712,17 @@ __global__ __launch_bounds__(256) void attend_dkv_kernel(AttendK k)
     const float plain = kLifted<T> ? 0x1p-15f : 1.0f;
     const float scale = len == 1 ? 0.0f : k.plain_scale * plain;
     const int64_t rows = (int64_t)k.B * k.Hk * k.Tk;
+    const int64_t row = ((int64_t)b * k.Hk + kvh) * k.Tk + tt;
     if constexpr (SHARED) {
         float f[DP / 8], e[DP / 8];
         float *room = (float *)&tiles[0][0][0][0];
-        join_waves<DP>(room, lane, wave, dk[0], lift.back(0), f);
-        join_waves<DP>(room, lane, wave, dv[0], 1.0f, e);
-        if (!there[0]) return;
-        if (!seen[0])
+        join_waves<DP>(room, lane, wave, dk, lift.back(), f);
+        join_waves<DP>(room, lane, wave, dv, 1.0f, e);
+        if (!there) return;
+        if (!seen)
 #pragma unroll
             for (int i = 0; i < DP / 8; ++i) e[i] = f[i] = 0.0f;
         const int d = (2 * wave + half) * (DP / 8);
-        const int64_t tt = t[0], row = ((int64_t)b * k.Hk + kvh) * k.Tk + tt;
         if (k.splits > 1) {
             store_run<float>(k.part + (split * rows + row) * k.D, d, k.D, f, scale);
             store_run<float>(k.part + ((k.slots + split) * rows + row) * k.D, d, k.D, e, plain);
@@ -788,28 +734,23 @@ __global__ __launch_bounds__(256) void attend_dkv_kernel(AttendK k)
         }
         return;
     }
+    if (!there) return;
+    if (!seen) {
 #pragma unroll
-    for (int n = 0; n < NC; ++n) {
-        if (!there[n]) continue;
-        if (!seen[n]) {
+        for (int d = 0; d < DP / 32; ++d)
 #pragma unroll
-            for (int d = 0; d < DP / 32; ++d)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) dk[n][d][i] = dv[n][d][i] = 0.0f;
-        }
-        const int64_t tt = t[n];
-        const float by = lift.back(n) * scale;
-        if (k.splits > 1) {
-            const int64_t row = ((int64_t)b * k.Hk + kvh) * k.Tk + tt;
-            store_column<float, DP>(k.part + (split * rows + row) * k.D, half, k.D, dk[n], by);
-            store_column<float, DP>(k.part + ((k.slots + split) * rows + row) * k.D, half, k.D,
-                                    dv[n], plain);
-        } else {
-            store_column<T, DP>((T *)k.dk.data + b * k.dk.batch + tt * k.dk.token +
-                                    kvh * k.dk.head, half, k.D, dk[n], by);
-            store_column<T, DP>((T *)k.dv.data + b * k.dv.batch + tt * k.dv.token +
-                                    kvh * k.dv.head, half, k.D, dv[n], plain);
-        }
+            for (int i = 0; i < 16; ++i) dk[d][i] = dv[d][i] = 0.0f;
+    }
+    const float by = lift.back() * scale;
+    if (k.splits > 1) {
+        store_column<float, DP>(k.part + (split * rows + row) * k.D, half, k.D, dk, by);
+        store_column<float, DP>(k.part + ((k.slots + split) * rows + row) * k.D, half, k.D, dv,
+                                plain);
+    } else {
+        store_column<T, DP>((T *)k.dk.data + b * k.dk.batch + tt * k.dk.token + kvh * k.dk.head,
+                            half, k.D, dk, by);
+        store_column<T, DP>((T *)k.dv.data + b * k.dv.batch + tt * k.dv.token + kvh * k.dv.head,
+                            half, k.D, dv, plain);
     }
 }
 
@@ -956,21 +897,19 @@ hipError_t launch_back_q(const AttendK &k, const AttendPlan &p, hipStream_t stre
     const int entries = k.bias.axes * k.bias.buckets;
     typedef std::true_type yes;
     typedef std::false_type no;
-    auto go = [&](auto nc, auto shared) {
-        constexpr int NC = decltype(nc)::value;
+    auto go = [&](auto shared) {
         constexpr bool S = decltype(shared)::value;
         if (grid == 0) return;
         if (k.bias.axes)
-            attend_dq_kernel<T, DP, NC, true, S>
+            attend_dq_kernel<T, DP, true, S>
                 <<<grid, 256, attend_hist_bytes(entries), stream>>>(k);
         else
-            attend_dq_kernel<T, DP, NC, false, S><<<grid, 256, 0, stream>>>(k);
+            attend_dq_kernel<T, DP, false, S><<<grid, 256, 0, stream>>>(k);
     };
-    typedef std::integral_constant<int, 1> one;
     if (p.shared)
-        go(one(), yes());
+        go(yes());
     else
-        go(one(), no());
+        go(no());
     hipError_t e = hipGetLastError();
     if (e == hipSuccess && k.splits > 1) e = launch_sum<T>(k, k.H, k.Tq, k.dq, k.dq, 1, stream);
     if (e == hipSuccess && entries && k.dtable) {
@@ -988,7 +927,7 @@ hipError_t launch_back_kv(const AttendK &k, const AttendPlan &p, hipStream_t str
     const unsigned grid = (unsigned)((int64_t)k.B * k.Hk * k.splits * k.blocks);
     if (grid == 0) return hipSuccess;
     auto go = [&](auto bias, auto shared) {
-        attend_dkv_kernel<T, DP, 1, decltype(bias)::value, decltype(shared)::value>
+        attend_dkv_kernel<T, DP, decltype(bias)::value, decltype(shared)::value>
             <<<grid, 256, 0, stream>>>(k);
     };
     typedef std::true_type yes;

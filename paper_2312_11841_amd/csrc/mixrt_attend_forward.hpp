@@ -337,8 +337,8 @@ __global__ __launch_bounds__(256) void attend_kernel(AttendK k)
         const T *kt = tiles[me][cur][0], *vt = tiles[me][cur][1];
         f32x16 s[NC] = {row_mul<T, DP>(kt, lane, q[0], k.D)};
         if constexpr (BIAS)
-            add_bias<NC, ROWS>(s, k.scale, kpos[me][cur], 0, half, dense, hbase, qpos,
-                               k.bias.axes, k.bias.reach);
+            add_bias<ROWS>(s[0], k.scale, kpos[me][cur], 0, half, dense, hbase[0], qpos[0],
+                           k.bias.axes, k.bias.reach);
         if (row0 + ROWS > w.last) cut_rows(s[0], row0, half, w.last);
         const float unit = BIAS ? 1.0f : k.scale, m = most_of(s[0]) * unit;
         if (far || __builtin_amdgcn_ballot_w64(m > top[0] + kMost<T>) != 0) {
@@ -500,8 +500,8 @@ __global__ __launch_bounds__(256, kFlowWaves<DP>) void attend_flow_kernel(Attend
 #pragma unroll
         for (int u = 0; u < SUBS; ++u) {
             if constexpr (BIAS)
-                add_bias<NC, ROWS>(s, k.scale, kpos[k0], u, half, dense, hbase, qpos, k.bias.axes,
-                                   k.bias.reach);
+                add_bias<ROWS>(s[0], k.scale, kpos[k0], u, half, dense, 0, qpos[0], k.bias.axes,
+                               k.bias.reach);
             if (row0 + 32 * u + 32 > w.last)
 #pragma unroll
                 for (int n = 0; n < NC; ++n) cut_rows(s[n], row0 + 32 * u, half, w.last);

@@ -16,7 +16,7 @@ hipError_t launch_attend(AttendK k, int stage, hipStream_t stream)
     auto plan = stage == kAttendForward ? plan_attend
                 : stage == kAttendBackQ ? plan_attend_dq
                                         : plan_attend_dkv;
-    const AttendPlan p = plan(k.B, k.H, k.Hk, k.Tq, k.Tk, k.D, k.dtype, k.bias.axes,
+    const AttendPlan p = plan(k.B, k.H, k.Hk, k.Tq, k.Tk, k.D, k.dtype,
                               k.bias.axes * k.bias.buckets);
     k.pack = p.pack;
     k.blocks = p.blocks;

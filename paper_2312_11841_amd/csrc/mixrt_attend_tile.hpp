@@ -487,63 +487,47 @@ struct StagePos {
     }
 };
 
-// s[n][i] = s[n][i] scale + the bias of row i of the tile's block u and column n.
-template <int NC, int ROWS>
-__device__ __forceinline__ void add_bias(f32x16 (&s)[NC], float scale, const TilePos<ROWS> &tile,
-                                         int u, int half, const float *dense,
-                                         const int (&base)[NC],
-                                         const int (&column)[NC][kMaxBiasAxes], int axes, int reach)
+// s[i] = s[i] scale + the bias of row i of the tile's block u and the lane's column.
+template <int ROWS>
+__device__ __forceinline__ void add_bias(f32x16 &s, float scale, const TilePos<ROWS> &tile,
+                                         int u, int half, const float *dense, int base,
+                                         const int (&column)[kMaxBiasAxes], int axes, int reach)
 {
     // (an axis that is not there reads places in LDS too, and adds nothing)
-    float level[NC];
+    float level = 0.0f, b[kMaxBiasAxes];
     int kind[kMaxBiasAxes];
 #pragma unroll
     for (int a = 0; a < kMaxBiasAxes; ++a) kind[a] = tile.kind_of(a, u);
 #pragma unroll
-    for (int n = 0; n < NC; ++n) {
-        float b[kMaxBiasAxes];
+    for (int a = 0; a < kMaxBiasAxes; ++a)
+        b[a] = dense[base + a * kReachRow + bias_at(tile.at[a][32 * u], column[a], reach)];
 #pragma unroll
-        for (int a = 0; a < kMaxBiasAxes; ++a)
-            b[a] = dense[base[n] + a * kReachRow +
-                         bias_at(tile.at[a][32 * u], column[n][a], reach)];
-        level[n] = 0.0f;
+    for (int a = 0; a < kMaxBiasAxes; ++a) level += a < axes && kind[a] == kLevel ? b[a] : 0.0f;
 #pragma unroll
-        for (int a = 0; a < kMaxBiasAxes; ++a)
-            level[n] += a < axes && kind[a] == kLevel ? b[a] : 0.0f;
-    }
-#pragma unroll
-    for (int n = 0; n < NC; ++n)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) s[n][i] = fmaf(s[n][i], scale, level[n]);
+    for (int i = 0; i < 16; ++i) s[i] = fmaf(s[i], scale, level);
 #pragma unroll
     for (int a = 0; a < kMaxBiasAxes; ++a) {
         if (a >= axes) break;
         const int32_t *p = &tile.at[a][32 * u + 4 * half];
-        const float *row = dense + a * kReachRow;
+        const float *row = dense + base + a * kReachRow;
         if (kind[a] == kSteps) {
 #pragma unroll
-            for (int n = 0; n < NC; ++n)
+            for (int j = 0; j < 4; ++j) {
+                const float *four = row + bias_at(p[8 * j], column[a], reach, kPad);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const float *b = row + base[n] + bias_at(p[8 * j], column[n][a], reach, kPad);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) s[n][4 * j + i] += b[i];
-                }
+                for (int i = 0; i < 4; ++i) s[4 * j + i] += four[i];
+            }
         } else if (kind[a] == kLevel8) {
 #pragma unroll
-            for (int n = 0; n < NC; ++n)
+            for (int j = 0; j < 4; ++j) {
+                const float one = row[bias_at(p[8 * j], column[a], reach)];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const float b = row[base[n] + bias_at(p[8 * j], column[n][a], reach)];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) s[n][4 * j + i] += b;
-                }
+                for (int i = 0; i < 4; ++i) s[4 * j + i] += one;
+            }
         } else if (kind[a] == kMixed) {
 #pragma unroll
-            for (int n = 0; n < NC; ++n)
-#pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    s[n][i] += row[base[n] + bias_at(p[tile_row(i, 0)], column[n][a], reach)];
+            for (int i = 0; i < 16; ++i)
+                s[i] += row[bias_at(p[tile_row(i, 0)], column[a], reach)];
         }
     }
 }
