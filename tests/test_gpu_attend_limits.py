@@ -537,3 +537,96 @@ def test_heads_without_elements_are_refused_by_name(r):
     for call in (r.attention, r.attention_train):
         with pytest.raises(mixrt.MixrtError, match="head_dim"):
             call(q, q, q)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("shape", [(3, 40, 1), (300, 100, 520)], ids=str)
+def test_gradients_at_scores_of_any_size(r, shape, dtype):
+    """A row that looks at one key passes its dout there, and nothing elsewhere; what the
+    other gradients hold is finite."""
+    dt = DT[dtype]
+    Tq, Tk, H = shape
+    g = _gen(16)
+    D = 16
+    size = {"f32": 1e12, "bf16": 1e12, "f16": 6e4}[dtype]
+    q = torch.randn((1, Tq, 1, D), generator=g).clamp(-1, 1).mul(size).to(dt)
+    k = torch.randn((1, Tk, 1, D), generator=g).clamp(-1, 1).mul(size).to(dt)
+    v, dout = (torch.randn((1, n, 1, D), generator=g).to(dt) for n in (Tk, Tq))
+    s = q[0, :, 0].double() @ k[0, :, 0].double().T
+    best, second = s.topk(2, 1).values.unbind(1)
+    dout[0, (best - second) <= 1e-3 * best.abs()] = 0
+    want = torch.zeros((Tk, D)).double().index_add(0, s.argmax(1), dout[0, :, 0].double())
+    sizes = torch.zeros((Tk, D)).double().index_add(0, s.argmax(1), dout[0, :, 0].double().abs())
+    cq, ck, cv, cd = (t.cuda().expand(-1, -1, H, -1) for t in (q, k, v, dout))
+    o, saved = r.attention_train(cq, ck, cv, scale=1.0)
+    dq, dk, dv = r.attention_backward(cd, cq, ck, cv, o, saved, scale=1.0)
+    for t in (dq, dk, dv):
+        assert torch.equal(t, t[:, :, :1].expand_as(t))
+    if dtype != "f16":      # (a gradient times 6e4 may leave its range)
+        assert all(bool(torch.isfinite(t).all()) for t in (dq, dk))
+    off = (dv[0, :, 0].double().cpu() - want).abs()
+    # weights are 1 to the type's rounding, sums in 32 bits, the rounded result
+    bound = ((Tq + 64) * ref.U + (0 if dtype == "f32" else ref.HALF_UNIT[dt])) * sizes
+    assert bool((off <= bound + ref.HALF_UNIT[dt] * want.abs() + ref.TINY[dt]).all())
+
+
+def test_passes_in_a_captured_step(r):
+    """A step whose walks run in passes, captured: every replay gives the eager bits, with
+    eager work between."""
+    g = _gen(17)
+    H, Tq, Tk, D = 512, 70, 8300, 12
+    stream = torch.cuda.Stream()
+    c = mixrt.Renderer(0, stream=stream)
+    try:
+        q, dout = (torch.randn((1, Tq, H, D), generator=g).cuda() for _ in range(2))
+        k, v = (torch.randn((1, Tk, 1, D), generator=g).cuda().expand(-1, -1, H, -1)
+                for _ in range(2))
+        table = torch.randn((1, 5, H), generator=g).cuda()
+        buckets = torch.randint(0, 5, (1, 21), generator=g).byte().cuda()
+        places = [(torch.arange(n) % 40).int()[:, None].cuda() for n in (Tq, Tk)]
+        bias = mixrt.RelativeBias(table, buckets, *places)
+        torch.cuda.synchronize()
+
+        def step(rr):
+            o, saved = rr.attention_train(q, k, v, bias=bias)
+            return [o, saved.lse, *rr.attention_backward(dout, q, k, v, o, saved, bias=bias)]
+
+        want = step(c)
+        c.sync()            # (before another stream copies them)
+        want = [t.clone() for t in want]
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            out = step(c)
+        for rep in range(3):
+            for t in out:
+                t.zero_()
+            torch.cuda.synchronize()
+            graph.replay()
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(out, want)), rep
+            assert all(torch.equal(a, b) for a, b in zip(step(r), want)), rep
+    finally:
+        c.close()
+
+
+@pytest.mark.parametrize("dtype,queries,keys,lens", [
+    ("f32", 70, 20000, [20000, 9000, 0]), ("f32", 9001, 70, [70, 33, 70]),
+    ("bf16", 70, 140000, [140000, 3, 90000])])
+def test_passes_of_several_entries(r, dtype, queries, keys, lens):
+    """Entries with keys, lengths and rows of their own, and heads that share keys."""
+    dt, H, Hk, D, B = DT[dtype], 512, 256, 10, 3
+    g = _gen(18)
+    q, dout = (torch.randn((B, queries, 1, D), generator=g).to(dt) for _ in range(2))
+    k, v = (torch.randn((B, keys, 1, D), generator=g).to(dt) for _ in range(2))
+    lens = torch.tensor(lens, dtype=torch.int32)
+    say(dtype, queries, keys)
+    cq, cd = (t.cuda().expand(-1, -1, H, -1) for t in (q, dout))
+    ck, cv = (t.cuda().expand(-1, -1, Hk, -1) for t in (k, v))
+    want = ref.attention(q.expand(-1, -1, 2, -1), k, v, dt, lens, dout=dout.expand(-1, -1, 2, -1))
+    o, saved = r.attention_train(cq, ck, cv, lens=lens.cuda())
+    grads = r.attention_backward(cd, cq, ck, cv, o, saved, lens=lens.cuda())
+    for name, got in zip(("o", "dq", "dk", "dv"), (o, *grads)):
+        assert torch.equal(got, got[:, :, :1].expand_as(got)), name
+        value, bound = want[name]
+        _inside(got[:, :, :1], (value[:, :, :1], bound[:, :, :1]), name)
