@@ -574,7 +574,8 @@ __global__ __launch_bounds__(256, kFlowWaves<DP>) void attend_flow_kernel(Attend
 // quads, G groups of them share its splits.  (With the splits of a row one after
 // another, the 113 of one token's 32 heads took 29 us.)  What the passes before left is
 // one part more, and of a pass that is not the last the result is the next one's.
-template <typename T, int G>
+constexpr int kFewParts = 4;
+template <typename T, int G, bool PASSES>
 __device__ __forceinline__ void join_row(const AttendK &k, int64_t row, float (&part)[5][256])
 {
     const int64_t rows = (int64_t)k.B * k.H * k.Tq;
@@ -584,46 +585,65 @@ __device__ __forceinline__ void join_row(const AttendK &k, int64_t row, float (&
     // (blocks that share a row read what one of them writes for the next pass, so there
     // are two places for it)
     const auto lse_of = [&](int s) {
-        return k.part_lse[(s + (s == k.splits ? (k.pass + 1) & 1 : 0)) * rows + row];
+        return k.part_lse[(PASSES && s == k.splits ? s + ((k.pass + 1) & 1) : s) * rows + row];
+    };
+    const int parts = PASSES ? k.parts : k.splits;
+    const auto value_of = [&](int s, float (&f)[4]) {
+        const float *o = k.part + (s * rows + row) * k.D + d;
+        if (d + 4 <= k.D) {
+            load_vec<float, 4>(o, f);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) f[i] = d + i < k.D ? o[i] : 0.0f;
+        }
     };
     // the group's own maximum first: NaN stays
-    float top = -INFINITY;
-    if (there)
-#pragma unroll 4
-        for (int s = g; s < k.parts; s += G) {
-            const float x = lse_of(s).x;
-            top = x > top || x != x ? x : top;
+    float top = -INFINITY, base, a[4] = {0, 0, 0, 0}, w = 0.0f;
+    const auto raise = [&](float x) { top = x > top || x != x ? x : top; };
+    const auto add = [&](const float2 &lse, const float (&f)[4]) {
+        const float e = __builtin_amdgcn_exp2f((lse.x - base) + lse.y);
+        w += e;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) a[i] = fmaf(f[i], e, a[i]);
+    };
+    if (G == 1) {
+        // (few parts: all are on their way before the first is used)
+        constexpr int MOST = kFewParts + PASSES;
+        float2 lse[MOST];
+        float f[MOST][4];
+#pragma unroll
+        for (int s = 0; s < MOST; ++s) {
+            if (!there || s >= parts) continue;
+            lse[s] = lse_of(s);
+            value_of(s, f[s]);
         }
-    float base = top == -INFINITY ? 0.0f : top;
-    float a[4] = {0, 0, 0, 0}, w = 0.0f;
-    if (there)
+#pragma unroll
+        for (int s = 0; s < MOST; ++s)
+            if (there && s < parts) raise(lse[s].x);
+        base = top == -INFINITY ? 0.0f : top;
+#pragma unroll
+        for (int s = 0; s < MOST; ++s)
+            if (there && s < parts) add(lse[s], f[s]);
+    } else {
+        if (there)
 #pragma unroll 4
-        for (int s = g; s < k.parts; s += G) {
-            const float2 lse = lse_of(s);
-            const float e = __builtin_amdgcn_exp2f((lse.x - base) + lse.y);
-            w += e;
-            const float *o = k.part + (s * rows + row) * k.D;
-            if (d + 4 <= k.D) {
+            for (int s = g; s < parts; s += G) raise(lse_of(s).x);
+        base = top == -INFINITY ? 0.0f : top;
+        if (there)
+#pragma unroll 4
+            for (int s = g; s < parts; s += G) {
                 float f[4];
-                load_vec<float, 4>(o + d, f);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) a[i] = fmaf(f[i], e, a[i]);
-            } else {
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (d + i < k.D) a[i] = fmaf(o[d + i], e, a[i]);
+                value_of(s, f);
+                add(lse_of(s), f);
             }
-        }
+    }
     if (G > 1) {
         // then the groups', in order, at their common maximum
         const bool none = top == -INFINITY;
         part[0][threadIdx.x] = top;
         __syncthreads();
         const int first = threadIdx.x - 8 * g;
-        for (int j = 0; j < G; ++j) {
-            const float x = part[0][first + 8 * j];
-            top = x > top || x != x ? x : top;
-        }
+        for (int j = 0; j < G; ++j) raise(part[0][first + 8 * j]);
         const float less = none ? 0.0f : __builtin_amdgcn_exp2f(base - top);
         base = top == -INFINITY ? 0.0f : top;
         __syncthreads();
@@ -647,9 +667,10 @@ __device__ __forceinline__ void join_row(const AttendK &k, int64_t row, float (&
     const float inv = w == 0.0f ? 0.0f : 1.0f / w;
     const int64_t bh = row / k.Tq;
     const int t = (int)(row - bh * k.Tq), b = (int)(bh / k.H), h = (int)(bh - (int64_t)b * k.H);
-    const RowSum sums(base, w, k.last ? INFINITY : -INFINITY);
+    const bool last = !PASSES || k.last;
+    const RowSum sums(base, w, last ? INFINITY : -INFINITY);
     const bool first = lane == 0 && blockIdx.y == 0;
-    if (!k.last) {
+    if (!last) {
         if (first)
             k.part_lse[(k.splits + (k.pass & 1)) * rows + row] = make_float2(sums.lse, sums.rest);
         if (d < k.D)
@@ -672,14 +693,14 @@ __device__ __forceinline__ void join_row(const AttendK &k, int64_t row, float (&
     }
 }
 
-template <typename T, int G>
+template <typename T, int G, bool PASSES>
 __global__ __launch_bounds__(256) void attend_join_kernel(AttendK k)
 {
     constexpr int EACH = 32 / G;
     __shared__ float part[5][256];
     const int64_t rows = (int64_t)k.B * k.H * k.Tq;
     for (int64_t r0 = (int64_t)blockIdx.x * EACH; r0 < rows; r0 += (int64_t)gridDim.x * EACH) {
-        join_row<T, G>(k, r0 + threadIdx.x / (8 * G), part);
+        join_row<T, G, PASSES>(k, r0 + threadIdx.x / (8 * G), part);
         if (G > 1) __syncthreads();     // (part is read to the end)
     }
 }
@@ -688,15 +709,21 @@ template <typename T>
 hipError_t launch_join(const AttendK &k, hipStream_t stream)
 {
     const int64_t rows = (int64_t)k.B * k.H * k.Tq;
-    auto go = [&](auto g) {
+    auto go = [&](auto g, auto passes) {
         constexpr int G = decltype(g)::value, EACH = 32 / G;
-        const unsigned bx = (unsigned)join_blocks((rows + EACH - 1) / EACH);
-        attend_join_kernel<T, G><<<dim3(bx, (unsigned)(k.D + 31) / 32), 256, 0, stream>>>(k);
+        const dim3 grid((unsigned)join_blocks((rows + EACH - 1) / EACH), (unsigned)(k.D + 31) / 32);
+        attend_join_kernel<T, G, decltype(passes)::value><<<grid, 256, 0, stream>>>(k);
     };
-    if (k.splits > 4)
-        go(std::integral_constant<int, 32>());
+    auto groups = [&](auto passes) {
+        if (k.splits > kFewParts)
+            go(std::integral_constant<int, 32>(), passes);
+        else
+            go(std::integral_constant<int, 1>(), passes);
+    };
+    if (k.slots > k.splits)
+        groups(std::true_type());
     else
-        go(std::integral_constant<int, 1>());
+        groups(std::false_type());
     return hipGetLastError();
 }
 
