@@ -18,7 +18,11 @@ template <typename T> inline constexpr float kWeightLift = kLifted<T> ? 15.0f : 
 // they move on to 64.
 constexpr int kHistRows = 1024;
 
-// acc[d][column] += sum over the tile's rows of tile[row][d] p[row][column].
+// acc[d][column] += sum over the tile's rows of tile[row][d] p[row][column].  The 16-bit
+// types round dS, and the weights of dv, once: gradients have a relative error of 2.4e-3
+// in bfloat16, where their own rounding alone makes 1.7e-3.  With a second term they have
+// 1.7e-3, and two 720p views' training step takes 1187 us for 981, one with a bias 968
+// for 925.
 template <typename T, int DP>
 __device__ __forceinline__ void add_cols(const T *tile, int lane, const f32x16 &p,
                                          f32x16 (&acc)[DP / 32])
@@ -89,6 +93,11 @@ __device__ __forceinline__ bool large_sum(float lse)
 {
     return fabsf(lse) >= 256.0f && fabsf(lse) < INFINITY;
 }
+// Whether it is so in any thread of the block; a barrier.
+__device__ __forceinline__ bool block_any(bool x)
+{
+    return __builtin_amdgcn_readfirstlane(__syncthreads_or(x)) != 0;
+}
 __device__ __forceinline__ float exponent(float s, float unit, float lse, float rest, float lifted)
 {
     const float whole = s * unit;
@@ -96,6 +105,14 @@ __device__ __forceinline__ float exponent(float s, float unit, float lse, float 
     const float x = (fabsf(lse) < 0x1p22f ? near : far) - rest;
     return x > lifted ? lifted : x;
 }
+
+// A walk whose lse are all small, whose lse count as large, or that asks for each tile:
+// a block that meets a large one takes the walk written for it, without loads ahead, so
+// that the other has no branch and no more registers (2048 queries over 2000 keys, 32
+// heads of 128 on 8, bf16: the keys' gradient 265 us, with a branch a tile 300).  float32
+// has one walk with a branch, which its products hide.
+enum { kNoLarge, kAllLarge, kSomeLarge };
+template <typename T> inline constexpr bool kTwoWalks = sizeof(T) == 2;
 
 // float16 holds dS only inside a range: its gradients are small where a row looks at
 // many keys, and large where a loss is scaled.  So each column's dS is multiplied by a
@@ -298,11 +315,12 @@ __device__ __forceinline__ void store_column(T *row, int half, int D, const f32x
 // blocks to one place, in no fixed order.  Tiles of 32 rows leave three blocks a CU; of
 // 64 rows two, and slower.
 //
-// Two entries of 3600 queries over 7200 keys, 12 heads of 64 on 3, bf16: 302 us, 790
+// Two entries of 3600 queries over 7200 keys, 12 heads of 64 on 3, bf16: 293 us, 815
 // TFLOP/s.  While a CU is busy its matrix units work 45% of the time, its vector units
-// 52%, its LDS 37%.  With a bias (one entry, 8 heads, three axes): 446 us, 8%, 42% and
-// 31%: the table's sums take LDS, so two blocks run on a CU, and their waves wait 43% of
-// their time, for reads of places that the adds before have written.
+// 52%, its LDS 38%.  With a bias (one entry, 8 heads, three axes): 449 us, 8%, 42% and
+// 31%: each pair of an axis that counts up is read from a place in LDS, added to and
+// written back, by one half of the wave after the other, and the next pairs' reads wait
+// for it (43% of a wave's time); the table's sums take LDS, so two blocks run on a CU.
 
 template <typename T, int DP, bool BIAS, bool SHARED>
 __global__ __launch_bounds__(256) void attend_dq_kernel(AttendK k)
@@ -364,7 +382,6 @@ __global__ __launch_bounds__(256) void attend_dq_kernel(AttendK k)
     const int64_t row = ((int64_t)b * k.H + h) * k.Tq + tt;
     const float lse = there ? k.lse[row] : INFINITY;
     const float lse_rest = there && k.lse_rest ? k.lse_rest[row] : 0.0f;
-    const bool large = __builtin_amdgcn_ballot_w64(large_sum(lse)) != 0;    // (in the wave)
     int qpos[kMaxBiasAxes];
     if (there && half == 0 && split == 0 && me == 0) k.delta[row] = delta;
 #pragma unroll
@@ -397,14 +414,14 @@ __global__ __launch_bounds__(256) void attend_dq_kernel(AttendK k)
     StagePos<BIAS ? ROWS : 1> sp;
     // (all fetched and then put, or one array after the other)
     constexpr bool AHEAD = !SHARED || kFetchAhead<T, DP>;
-    auto fetch = [&](int row) {
+    auto fetch = [&](int row) __attribute__((always_inline)) {
         sk.fetch(stager, kp, k.k.token, row, last, k.D);
         if (!AHEAD) sk.put(stager, tiles[me][0][0]);
         sv.fetch(stager, vp, k.v.token, row, last, k.D);
         if (!AHEAD) sv.put(stager, tiles[me][0][1]);
         if (BIAS) sp.fetch(stager, pp, k.bias.axes, row, last);
     };
-    auto put = [&](int to) {
+    auto put = [&](int to) __attribute__((always_inline)) {
         if (AHEAD) {
             sk.put(stager, tiles[me][to][0]);
             sv.put(stager, tiles[me][to][1]);
@@ -416,8 +433,8 @@ __global__ __launch_bounds__(256) void attend_dq_kernel(AttendK k)
         fetch(row1);
         put(0);
     }
-    if (SHARED && BIAS) __syncthreads();    // (the bias and hist are the block's)
-    team.meet();
+    // (the bias and hist are the block's too)
+    const bool large = block_any(large_sum(lse));
     // each entry's places of all columns; threads start at different columns, as the
     // same column of all entries lies in one bank
     auto collect = [&]() {
@@ -435,60 +452,70 @@ __global__ __launch_bounds__(256) void attend_dq_kernel(AttendK k)
         }
         table += sum;
     };
-    int cur = 0, counted = 0;
-    for (int row0 = row1; row0 < last; row0 += STEP, cur ^= BUFS - 1) {
-        const bool more = row0 + STEP < last;
-        if (more && AHEAD) fetch(row0 + STEP);
-        const T *kt = tiles[me][cur][0], *vt = tiles[me][cur][1];
-        f32x16 s, g;
+    auto walk = [&](auto kind) __attribute__((always_inline)) {
+        constexpr int SUMS = decltype(kind)::value;
+        constexpr bool EARLY = AHEAD && SUMS != kAllLarge;
+        int cur = 0, counted = 0;
+        for (int row0 = row1; row0 < last; row0 += STEP, cur ^= BUFS - 1) {
+            const bool more = row0 + STEP < last;
+            if (more && EARLY) fetch(row0 + STEP);
+            const T *kt = tiles[me][cur][0], *vt = tiles[me][cur][1];
+            f32x16 s, g;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) s[i] = g[i] = 0.0f;
-        pair_mul<T, DP>(kt, vt, lane, q, dout, s, g, k.D);
-        if constexpr (BIAS) {
-            add_bias<ROWS>(s, k.scale, kpos[me][cur], 0, half, dense, 0, qpos, k.bias.axes,
-                               k.bias.reach);
-        }
-        const float unit = BIAS ? 1.0f : k.scale;
-        if (large) {
-            rare();
+            for (int i = 0; i < 16; ++i) s[i] = g[i] = 0.0f;
+            pair_mul<T, DP>(kt, vt, lane, q, dout, s, g, k.D);
+            if constexpr (BIAS) {
+                add_bias<ROWS>(s, k.scale, kpos[me][cur], 0, half, dense, 0, qpos, k.bias.axes,
+                                   k.bias.reach);
+            }
+            const float unit = BIAS ? 1.0f : k.scale;
+            const bool one = SUMS == kAllLarge || (SUMS == kSomeLarge && large);
+            if (one) {
+                rare();
 #pragma unroll
-            for (int i = 0; i < 16; ++i)
-                s[i] = exponent(s[i], unit, lse, lse_rest, 0.0f);
-        }
-        const float by = large ? 1.0f : unit, less = large ? 0.0f : lse;
-        const float left = large ? 0.0f : lse_rest;
+                for (int i = 0; i < 16; ++i) s[i] = exponent(s[i], unit, lse, lse_rest, 0.0f);
+            }
+            const float by = one ? 1.0f : unit, less = one ? 0.0f : lse;
+            const float left = one ? 0.0f : lse_rest;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            float x = fmaf(s[i], by, -less);
-            if (sizeof(T) == 4) x -= left;
-            g[i] = __builtin_amdgcn_exp2f(x) * (g[i] - delta);
-        }
-        if (row0 + ROWS > last) {
-            rare();
+            for (int i = 0; i < 16; ++i) {
+                float x = SUMS == kAllLarge ? s[i] : fmaf(s[i], by, -less);
+                if (sizeof(T) == 4 && SUMS != kAllLarge) x -= left;
+                g[i] = __builtin_amdgcn_exp2f(x) * (g[i] - delta);
+            }
+            if (row0 + ROWS > last) {
+                rare();
 #pragma unroll
-            for (int i = 0; i < 16; ++i)
-                if (row0 + tile_row(i, half) >= last)
-                    g[i] = 0.0f;
+                for (int i = 0; i < 16; ++i)
+                    if (row0 + tile_row(i, half) >= last)
+                        g[i] = 0.0f;
+            }
+            if constexpr (BIAS) {
+                add_table<ROWS>(g, kpos[me][cur], 0, half, place, qpos, k.bias.axes, k.bias.reach,
+                                mine, 32 * entries);
+            }
+            lift.scale(g, acc);
+            add_cols<T, DP>(kt, lane, g, acc);
+            counted += ROWS;
+            if (BUFS == 1) team.meet();
+            if (more) {
+                if (!EARLY) fetch(row0 + STEP);
+                put(cur ^ (BUFS - 1));
+            }
+            team.meet();
+            if (BIAS && !SHARED && counted == kHistRows) {
+                collect();
+                counted = 0;
+                __syncthreads();
+            }
         }
-        if constexpr (BIAS) {
-            add_table<ROWS>(g, kpos[me][cur], 0, half, place, qpos, k.bias.axes, k.bias.reach,
-                            mine, 32 * entries);
-        }
-        lift.scale(g, acc);
-        add_cols<T, DP>(kt, lane, g, acc);
-        counted += ROWS;
-        if (BUFS == 1) team.meet();
-        if (more) {
-            if (!AHEAD) fetch(row0 + STEP);
-            put(cur ^ (BUFS - 1));
-        }
-        team.meet();
-        if (BIAS && !SHARED && counted == kHistRows) {
-            collect();
-            counted = 0;
-            __syncthreads();
-        }
-    }
+    };
+    if constexpr (!kTwoWalks<T>)
+        walk(std::integral_constant<int, kSomeLarge>());
+    else if (large)
+        walk(std::integral_constant<int, kAllLarge>());
+    else
+        walk(std::integral_constant<int, kNoLarge>());
     // the one key of a row has weight 1 whatever its score: no gradient
     const float some = len == 1 ? 0.0f : 1.0f;
     if (BIAS) {
@@ -525,41 +552,36 @@ __global__ __launch_bounds__(256) void attend_dq_kernel(AttendK k)
 // A column is a key, the rows are the queries of all heads that share it, one head after
 // another: S and dP as above, dv += dout^T P, dk += q^T dS, so shared heads need no sums
 // of their own.  The accumulators of dk and dv leave two waves a SIMD at heads of 64.
-// The first example above: 411 us, 775 TFLOP/s; matrix units busy 42% of the time, vector
-// units 44%, LDS 48%, a fifth of that conflicts of the transposing loads.  The second:
-// 231 us, 21%, 39% and 36%.
+// The first example above: 430 us, 740 TFLOP/s; matrix units busy 40% of the time, vector
+// units 40%, LDS 50%, a fifth of that conflicts of the transposing loads.  The second:
+// 249 us, 19%, 39% and 35%.
 
-// lse, delta and what rounding took from lse of a tile's queries, and whether any lse is
-// large.
+// lse and delta of a tile's queries, and where it counts (wanted) what rounding took from
+// lse.
 template <int ROWS>
 struct StageSums {
-    static constexpr int kFloats = 3 * ROWS + 4;
     float lse, delta, rest;
     __device__ __forceinline__ void fetch(int thread, const float *l, const float *d,
-                                          const float *r, int first, int limit, float lifted)
+                                          const float *r, int first, int limit, float lifted,
+                                          bool wanted)
     {
         const int row = first + thread;
         const bool there = thread < ROWS && row < limit;
         // (a row that is not there has weights 0)
-        lse = INFINITY;
-        delta = rest = 0.0f;
-        if (!there) return;
-        const float whole = l[row];
+        const float whole = there ? l[row] : INFINITY;
         lse = whole - lifted;
-        delta = d[row];
-        if (r) rest = r[row];
+        delta = there ? d[row] : 0.0f;
+        if (!wanted) return;
+        rest = there && r ? r[row] : 0.0f;
         if (lifted != 0.0f && whole < INFINITY) rest += (whole - lse) - lifted;
     }
-    __device__ __forceinline__ void put(int thread, float *at) const
+    __device__ __forceinline__ void put(int thread, float *at, bool wanted) const
     {
         if (thread < ROWS) {
             at[thread] = lse;
             at[ROWS + thread] = delta;
-            at[2 * ROWS + thread] = rest;
+            if (wanted) at[2 * ROWS + thread] = rest;
         }
-        if (thread >= 64) return;           // the first wave holds the rows
-        const bool large = __builtin_amdgcn_ballot_w64(thread < ROWS && large_sum(lse)) != 0;
-        if (thread == 0) at[3 * ROWS] = large ? 1.0f : 0.0f;
     }
 };
 
@@ -573,8 +595,9 @@ __global__ __launch_bounds__(256) void attend_dkv_kernel(AttendK k)
     __shared__ __attribute__((aligned(16))) T tiles[WAVES][BUFS][2][TILE];
     __shared__ float dense[WAVES][BIAS ? kMaxBiasAxes * kReachRow : 1];
     __shared__ TilePos<BIAS ? ROWS : 1> qpos[WAVES][BUFS];
-    __shared__ __attribute__((aligned(16))) float sums[WAVES][BUFS][StageSums<ROWS>::kFloats];
-    __shared__ float zeros[ROWS];
+    __shared__ __attribute__((aligned(16))) float sums[WAVES][BUFS][3 * ROWS];
+    constexpr bool TWO = kTwoWalks<T>;
+    __shared__ float zeros[TWO ? 1 : ROWS];
 
     const Team<SHARED> team;
     const int lane = team.lane, wave = team.wave, half = team.half;
@@ -623,7 +646,7 @@ __global__ __launch_bounds__(256) void attend_dkv_kernel(AttendK k)
     // tile i: a head of the group, its rows; all fetched and then put, or one array
     // after the other
     constexpr bool AHEAD = !SHARED || kFetchAhead<T, DP>;
-    auto fetch = [&](int i) {
+    auto fetch = [&](int i, bool rest) __attribute__((always_inline)) {
         const int g = i / a_head, row = (i - g * a_head) * ROWS;
         const int h = kvh * G + g;
         sq.fetch(stager, qp + h * k.q.head, k.q.token, row, k.Tq, k.D);
@@ -632,82 +655,100 @@ __global__ __launch_bounds__(256) void attend_dkv_kernel(AttendK k)
         if (!AHEAD) sg.put(stager, tiles[me][0][1]);
         const int64_t at = sums0 + (int64_t)h * k.Tq;
         ss.fetch(stager, k.lse + at, k.delta + at, k.lse_rest ? k.lse_rest + at : nullptr, row,
-                 k.Tq, kWeightLift<T>);
+                 k.Tq, kWeightLift<T>, rest);
         if (BIAS) sp.fetch(stager, pp, k.bias.axes, row, k.Tq);
     };
-    auto put = [&](int to) {
+    auto put = [&](int to, bool rest) __attribute__((always_inline)) {
         if (AHEAD) {
             sq.put(stager, tiles[me][to][0]);
             sg.put(stager, tiles[me][to][1]);
         }
-        ss.put(stager, sums[me][to]);
+        ss.put(stager, sums[me][to], rest);
         if (BIAS) sp.put(stager, qpos[me][to], k.bias.axes);
     };
     int head = -1;              // whose bias is in LDS
-    if (lane < ROWS) zeros[lane] = 0.0f;    // (by each wave)
+    if (!TWO && lane < ROWS) zeros[lane] = 0.0f;    // (by each wave)
     const int first1 = first + me;
     if (first1 < last) {
-        fetch(first1);
-        put(0);
+        fetch(first1, true);
+        put(0, true);
     }
-    team.meet();
-    int cur = 0;
-    for (int i0 = first1; i0 < last; i0 += STEP, cur ^= BUFS - 1) {
-        const bool more = i0 + STEP < last;
-        const float marked = sums[me][cur][3 * ROWS];
-        if (more && AHEAD) fetch(i0 + STEP);
-        const bool large = __builtin_amdgcn_readfirstlane(__float_as_int(marked)) != 0;
-        if (BIAS && head != i0 / a_head) {      // (the same for all that share it)
-            head = i0 / a_head;
-            // (mirrored: the rows are queries here)
-            load_bias(dense[me], k.bias, kvh * G + head, k.H, stager, Team<SHARED>::kStagers,
-                      true);
-            team.meet();
-        }
-#pragma unroll
-        for (int u = 0; u < ROWS / 32; ++u) {
-            const T *qt = tiles[me][cur][0] + u * 32 * kStride<T, DP>;
-            const T *gt = tiles[me][cur][1] + u * 32 * kStride<T, DP>;
-            const float *sm = sums[me][cur] + 32 * u;
-            f32x16 p, g;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) p[i] = g[i] = 0.0f;
-            pair_mul<T, DP>(qt, gt, lane, key, val, p, g, k.D);
-            if constexpr (BIAS) {
-                    add_bias<ROWS>(p, k.scale, qpos[me][cur], u, half, dense[me], 0, kpos,
-                                   k.bias.axes, k.bias.reach);
+    // whether the block meets a large lse
+    bool some_large = false;
+#pragma unroll 4
+    for (int i = first + threadIdx.x / ROWS; i < last; i += 256 / ROWS) {
+        const int g = i / a_head, row = (i - g * a_head) * ROWS + threadIdx.x % ROWS;
+        if (row < k.Tq)
+            some_large = some_large || large_sum(k.lse[sums0 + (int64_t)(kvh * G + g) * k.Tq + row]);
+    }
+    const bool large = block_any(some_large);
+    auto walk = [&](auto kind) __attribute__((always_inline)) {
+        constexpr int SUMS = decltype(kind)::value;
+        constexpr bool EARLY = AHEAD && SUMS != kAllLarge;
+        const bool one = SUMS == kAllLarge || (SUMS == kSomeLarge && large);
+        const bool rest = one || sizeof(T) == 4;
+        int cur = 0;
+        for (int i0 = first1; i0 < last; i0 += STEP, cur ^= BUFS - 1) {
+            const bool more = i0 + STEP < last;
+            if (more && EARLY) fetch(i0 + STEP, rest);
+            if (BIAS && head != i0 / a_head) {      // (the same for all that share it)
+                head = i0 / a_head;
+                // (mirrored: the rows are queries here)
+                load_bias(dense[me], k.bias, kvh * G + head, k.H, stager, Team<SHARED>::kStagers,
+                          true);
+                team.meet();
             }
-            const float unit = BIAS ? 1.0f : k.scale;
-            if (large) {
-                rare();
+#pragma unroll
+            for (int u = 0; u < ROWS / 32; ++u) {
+                const T *qt = tiles[me][cur][0] + u * 32 * kStride<T, DP>;
+                const T *gt = tiles[me][cur][1] + u * 32 * kStride<T, DP>;
+                const float *sm = sums[me][cur] + 32 * u;
+                f32x16 p, g;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) p[i] = g[i] = 0.0f;
+                pair_mul<T, DP>(qt, gt, lane, key, val, p, g, k.D);
+                if constexpr (BIAS) {
+                    add_bias<ROWS>(p, k.scale, qpos[me][cur], u, half, dense[me], 0, kpos, k.bias.axes,
+                                   k.bias.reach);
+                }
+                const float unit = BIAS ? 1.0f : k.scale;
+                if (one) {
+                    rare();
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const int at = tile_row(i, half);
+                        p[i] = exponent(p[i], unit, sm[at], sm[2 * ROWS + at], kWeightLift<T>);
+                    }
+                }
+                const float by = one ? 1.0f : unit;
+                const float *less = SUMS == kSomeLarge && one ? zeros : sm;
+                const float *left = SUMS == kSomeLarge && one ? zeros : sm + 2 * ROWS;
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
                     const int at = tile_row(i, half);
-                    p[i] = exponent(p[i], unit, sm[at], sm[2 * ROWS + at], kWeightLift<T>);
+                    float x = SUMS == kAllLarge ? p[i] : fmaf(p[i], by, -less[at]);
+                    if (sizeof(T) == 4 && SUMS != kAllLarge) x -= left[at];
+                    p[i] = __builtin_amdgcn_exp2f(x);
+                    g[i] = p[i] * (g[i] - sm[ROWS + at]);
                 }
+                add_cols<T, DP>(gt, lane, p, dv);
+                lift.scale(g, dk);
+                add_cols<T, DP>(qt, lane, g, dk);
             }
-            const float by = large ? 1.0f : unit;
-            const float *less = large ? zeros : sm, *left = large ? zeros : sm + 2 * ROWS;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const int at = tile_row(i, half);
-                const float lse = less[at], delta = sm[ROWS + at];
-                float x = fmaf(p[i], by, -lse);
-                if (sizeof(T) == 4) x -= left[at];
-                p[i] = __builtin_amdgcn_exp2f(x);
-                g[i] = p[i] * (g[i] - delta);
+            if (BUFS == 1) team.meet();
+            if (more) {
+                if (!EARLY) fetch(i0 + STEP, rest);
+                put(cur ^ (BUFS - 1), rest);
             }
-            add_cols<T, DP>(gt, lane, p, dv);
-            lift.scale(g, dk);
-            add_cols<T, DP>(qt, lane, g, dk);
+            team.meet();
         }
-        if (BUFS == 1) team.meet();
-        if (more) {
-            if (!AHEAD) fetch(i0 + STEP);
-            put(cur ^ (BUFS - 1));
-        }
-        team.meet();
-    }
+    };
+    if constexpr (!kTwoWalks<T>)
+        walk(std::integral_constant<int, kSomeLarge>());
+    else if (large)
+        walk(std::integral_constant<int, kAllLarge>());
+    else
+        walk(std::integral_constant<int, kNoLarge>());
     // (one key: as in the queries' gradient)
     const float plain = kLifted<T> ? 0x1p-15f : 1.0f;
     const float scale = len == 1 ? 0.0f : k.plain_scale * plain;
@@ -758,8 +799,8 @@ __global__ __launch_bounds__(256) void attend_dkv_kernel(AttendK k)
 
 // out[b][t][h][d] = sum of the splits' parts [split][b][h][t][d], a quad for G threads,
 // which take every G-th split and join in order; with blockIdx.y = 1 the second array's
-// parts, which follow.  A pass that is not the last leaves its sum as a part.  (256 splits of 40 rows of 128, twice: one thread a quad 71 us,
-// 32 threads 6.7.)
+// parts, which follow.  A pass that is not the last leaves its sum as a part.  (256 splits
+// of 40 rows of 128, twice: one thread a quad 71 us, 32 threads 6.7.)
 template <typename T, int G>
 __device__ __forceinline__ void sum_quad(const float *part, int parts, int64_t rows, int H,
                                          int Tn, int D, const SeqK &out, int64_t at,

@@ -396,6 +396,12 @@ __device__ __forceinline__ void store_rest(T *row, int d, int D, const float *o)
 // stretch of code without branches, so that its reads of LDS run together.  (With a
 // branch an octet they waited for each other: 8160 tokens among themselves, 16 heads of
 // 64 in bf16 and two axes took 897 us a call, without 750.)
+//
+// So the time depends on the width of the views' rows.  An octet that crosses the end of
+// one makes its 32 rows mixed on every axis: the same pairs take 746 us in rows of 120,
+// 728 of 64, 777 of 40, 804 of 24, 791 of 107, 901 of 119 and 945 of 12 or 7; a training
+// step of 3600 queries over 7200 keys with three axes 925 in rows of 80, 898 of 64, 994 of
+// 24, 1058 of 67, 1040 of 79 and 1240 of 12.
 
 constexpr int kPad = 4;                                     // entries beyond either end
 constexpr int kReachRow = 2 * kMaxReach + 2 + 2 * kPad;     // of an axis and head in LDS
