@@ -145,12 +145,20 @@ inline constexpr float kLow = !std::is_same_v<T, f16> ? 0.0f : EXACT ? 11.0f : 7
 // float16 2^15): then the sums so far are brought to it.  That is the first tile and
 // few others.
 template <typename T> inline constexpr float kMost = std::is_same_v<T, f16> ? 15.0f : 8.0f;
+// (float16 has no room for what base + kMost may round up by, beside a large base; the
+// difference does not.  Where both are -inf it is no number.)
+template <typename T>
+__device__ __forceinline__ bool past_base(float m, float top)
+{
+    return std::is_same_v<T, f16> ? m - top > kMost<T> : m > top + kMost<T>;
+}
 template <typename T, bool EXACT, int ND>
 __device__ __forceinline__ void rebase(float m, float &top, float &sum, f32x16 (&acc)[ND])
 {
-    // (the difference is exact where a large base makes the sum base + kMost round up)
-    if (m - top > kMost<T>) {
-        const float to = m - kLow<T, EXACT>, less = __builtin_amdgcn_exp2f(top - to);
+    if (past_base<T>(m, top)) {
+        float to = m - kLow<T, EXACT>;
+        if (past_base<T>(m, to)) to = m;        // (as a large m's difference is rounded)
+        const float less = __builtin_amdgcn_exp2f(top - to);
         sum *= less;
 #pragma unroll
         for (int d = 0; d < ND; ++d)
@@ -274,8 +282,12 @@ inline constexpr int kTerms = !EXACT ? 1 : BIAS && std::is_same_v<T, bf16> ? 3 :
 // vector units busy 30% of the time.  7 crops of 253 tokens over up to 391 keys, 6 heads
 // of 40, f32: 23 us, matrix units busy 22%.  Not SHARED, f32 is bound by the matrix instructions, of 64
 // cycles for two of a head's elements.
+// Waves a SIMD: one token of 32 heads of 128 takes 19.5 us with two and 25 with one, which
+// a few registers too many leave.
+template <typename T, bool SHARED, bool BIAS>
+inline constexpr int kSimpleWaves = SHARED && sizeof(T) == 2 && !BIAS ? 2 : 1;
 template <typename T, int DP, bool SHARED, bool BIAS, bool EXACT>
-__global__ __launch_bounds__(256) void attend_kernel(AttendK k)
+__global__ __launch_bounds__(256, (kSimpleWaves<T, SHARED, BIAS>)) void attend_kernel(AttendK k)
 {
     typedef typename Matrix<T>::frag frag;
     constexpr int ROWS = 32, NC = 1, WAVES = SHARED ? 4 : 1, BUFS = SHARED ? 1 : 2;
@@ -346,7 +358,7 @@ __global__ __launch_bounds__(256) void attend_kernel(AttendK k)
                            k.bias.axes, k.bias.reach);
         if (row0 + ROWS > w.last) cut_rows(s[0], row0, half, w.last);
         const float unit = BIAS ? 1.0f : k.scale, m = most_of(s[0]) * unit;
-        if (far || __builtin_amdgcn_ballot_w64(m > top[0] + kMost<T>) != 0) {
+        if (far || __builtin_amdgcn_ballot_w64(past_base<T>(m, top[0])) != 0) {
             rebase<T, EXACT>(m, top[0], sum[0], acc[0]);
             far = !BIAS && far_base(top[0]);
         }
@@ -516,7 +528,7 @@ __global__ __launch_bounds__(256, kFlowWaves<DP>) void attend_flow_kernel(Attend
 #pragma unroll
             for (int n = 0; n < NC; ++n) {
                 m[n] = most_of(s[n]) * unit;
-                out = out || m[n] > top[n] + kMost<T>;
+                out = out || past_base<T>(m[n], top[n]);
             }
             if (far || __builtin_amdgcn_ballot_w64(out) != 0) {
                 // the values that wait have weights on the old base

@@ -630,3 +630,35 @@ def test_passes_of_several_entries(r, dtype, queries, keys, lens):
         assert torch.equal(got, got[:, :, :1].expand_as(got)), name
         value, bound = want[name]
         _inside(got[:, :, :1], (value[:, :, :1], bound[:, :, :1]), name)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("queries", [1, 130])
+def test_large_biases_that_step_up(r, queries, dtype):
+    """A later key's bias is ahead of the first ones' by 1 to 40 in units of log2, beside
+    2^21 to 2^30, where a sum with the base rounds: outputs stay between the values."""
+    dt = DT[dtype]
+    steps = [(k, d) for k in range(21, 31) for d in range(1, 41)]
+    H, Tk, D = len(steps), 96, 16
+    g = _gen(19)
+    table = torch.zeros((1, 2, H))
+    for i, (k, d) in enumerate(steps):
+        for sign in ((1,) if i % 2 else (-1,)):
+            table[0, 0, i] = sign * 2.0 ** k * math.log(2) * (1 + (i % 7) / 8)
+            table[0, 1, i] = float(table[0, 0, i].double() + d * math.log(2))
+    buckets = torch.tensor([[0, 0, 1]], dtype=torch.uint8)
+    k_pos = torch.zeros((Tk, 1), dtype=torch.int32)
+    k_pos[70] = 1
+    bias = mixrt.RelativeBias(table.cuda(), buckets.cuda(),
+                              torch.zeros((queries, 1), dtype=torch.int32).cuda(), k_pos.cuda())
+    q = torch.zeros((1, queries, 1, D), dtype=dt).cuda().expand(-1, -1, H, -1)
+    k = torch.zeros((1, Tk, 1, D), dtype=dt).cuda().expand(-1, -1, H, -1)
+    v = torch.randn((1, Tk, 1, D), generator=g).to(dt)
+    cv = v.cuda().expand(-1, -1, H, -1)
+    low, high = (t[0, 0].float().cuda() for t in (v.amin(1), v.amax(1)))
+    for o in (r.attention(q, k, cv, bias=bias), r.attention_train(q, k, cv, bias=bias)[0]):
+        o = o.float()
+        assert bool(torch.isfinite(o).all())
+        # (weights rounded to the type are 1 in sum to that)
+        room = 2.0 ** -6 * torch.maximum(low.abs(), high.abs())
+        assert bool((o >= low - room).all()) and bool((o <= high + room).all())
