@@ -21,8 +21,8 @@ constexpr int kHistRows = 1024;
 // acc[d][column] += sum over the tile's rows of tile[row][d] p[row][column].  The 16-bit
 // types round dS, and the weights of dv, once: gradients have a relative error of 2.4e-3
 // in bfloat16, where their own rounding alone makes 1.7e-3.  With a second term they have
-// 1.7e-3, and two 720p views' training step takes 1187 us for 981, one with a bias 968
-// for 925.
+// 1.7e-3, and two 720p views' training step takes 1229 us for 1024, one with a bias 966
+// for 909.
 template <typename T, int DP>
 __device__ __forceinline__ void add_cols(const T *tile, int lane, const f32x16 &p,
                                          f32x16 (&acc)[DP / 32])
@@ -315,12 +315,12 @@ __device__ __forceinline__ void store_column(T *row, int half, int D, const f32x
 // blocks to one place, in no fixed order.  Tiles of 32 rows leave three blocks a CU; of
 // 64 rows two, and slower.
 //
-// Two entries of 3600 queries over 7200 keys, 12 heads of 64 on 3, bf16: 293 us, 815
-// TFLOP/s.  While a CU is busy its matrix units work 45% of the time, its vector units
-// 52%, its LDS 38%.  With a bias (one entry, 8 heads, three axes): 449 us, 8%, 42% and
+// Two entries of 3600 queries over 7200 keys, 12 heads of 64 on 3, bf16: 290 us, 820
+// TFLOP/s.  While a CU is busy its matrix units work 46% of the time, its vector units
+// 52%, its LDS 38%.  With a bias (one entry, 8 heads, three axes): 447 us, 8%, 41% and
 // 31%: each pair of an axis that counts up is read from a place in LDS, added to and
 // written back, by one half of the wave after the other, and the next pairs' reads wait
-// for it (43% of a wave's time); the table's sums take LDS, so two blocks run on a CU.
+// for it (44% of a wave's time); the table's sums take LDS, so two blocks run on a CU.
 
 template <typename T, int DP, bool BIAS, bool SHARED>
 __global__ __launch_bounds__(256) void attend_dq_kernel(AttendK k)
@@ -552,9 +552,9 @@ __global__ __launch_bounds__(256) void attend_dq_kernel(AttendK k)
 // A column is a key, the rows are the queries of all heads that share it, one head after
 // another: S and dP as above, dv += dout^T P, dk += q^T dS, so shared heads need no sums
 // of their own.  The accumulators of dk and dv leave two waves a SIMD at heads of 64.
-// The first example above: 430 us, 740 TFLOP/s; matrix units busy 40% of the time, vector
-// units 40%, LDS 50%, a fifth of that conflicts of the transposing loads.  The second:
-// 249 us, 19%, 39% and 35%.
+// The first example above: 413 us, 770 TFLOP/s; matrix units busy 41% of the time, vector
+// units 42%, LDS 46%, a fifth of that conflicts of the transposing loads.  The second:
+// 243 us, 20%, 40% and 34%.
 
 // lse and delta of a tile's queries, and where it counts (wanted) what rounding took from
 // lse.

@@ -268,8 +268,8 @@ __device__ __forceinline__ void finish_shared(const AttendK &k, const ForwardWor
 // A served weight is rounded to its type, as the result is: the result's relative error
 // is then 2.2e-3 in bfloat16 (one token over 14,400 keys; with a bias 2.3e-3) and 2.9e-4
 // in float16, where its own rounding alone makes 1.7e-3 and 2.1e-4.  A second term takes
-// that away, and 20.4 us for 19.8 there, 833 for 747 with a bias (8160 tokens among
-// themselves, 16 heads of 64), 219 for 160 of 3600 queries over 14,400 keys.
+// that away, and 20.2 us for 19.4 there, 817 for 732 with a bias (8160 tokens among
+// themselves, 16 heads of 64), 224 for 163 of 3600 queries over 14,400 keys.
 template <typename T, bool BIAS, bool EXACT>
 inline constexpr int kTerms = !EXACT ? 1 : BIAS && std::is_same_v<T, bf16> ? 3 : 2;
 
@@ -278,7 +278,7 @@ inline constexpr int kTerms = !EXACT ? 1 : BIAS && std::is_same_v<T, bf16> ? 3 :
 //
 // SHARED is bound by latency: a wave's walk is a few tiles, each read from HBM, put into
 // LDS, multiplied, rebased.  One token of 32 heads of 128 over 14,400 keys of 8 in bf16
-// (59 MB, 10 us at a large copy's rate): 19.5 us a call, 15.5 and 4.6 of join in a trace,
+// (59 MB, 10 us at a large copy's rate): 19.5 us a call, 15.4 and 4.7 of join in a trace,
 // vector units busy 30% of the time.  7 crops of 253 tokens over up to 391 keys, 6 heads
 // of 40, f32: 23 us, matrix units busy 22%.  Not SHARED, f32 is bound by the matrix instructions, of 64
 // cycles for two of a head's elements.
@@ -400,13 +400,13 @@ __global__ __launch_bounds__(256, (kSimpleWaves<T, SHARED, BIAS>)) void attend_k
 // matrix unit works on the scores of the next 32 and on the values of the last 32.
 // Keys lie in LDS one tile ahead, values stay one tile longer (rings of three).
 //
-// 3600 queries over 14,400 keys, 8 heads of 64 in f16: 158 us with its join, 670 TFLOP/s;
-// vector units busy 61% of the time, matrix units 36%.  An exponential takes 8 cycles a wave, so the
+// 3600 queries over 14,400 keys, 8 heads of 64 in f16: 155 to 163 us with its join, 650 to
+// 680 TFLOP/s; vector units busy 61% of the time, matrix units 35%.  An exponential takes 8 cycles a wave, so the
 // weights of 32 x 32 scores take 128 of a SIMD's cycles beside 256 of products, and their
 // scaling, maxima, sums and roundings more than that.  With the bias (8160 tokens among
-// themselves, 16 heads, bf16, two axes): 746 us, 52% and 15%; the bias is read from LDS
+// themselves, 16 heads, bf16, two axes): 728 us, 53% and 15%; the bias is read from LDS
 // between a score and its weight, at addresses formed there, and two waves a SIMD do not
-// hide that chain (44% of a wave's time).  A block's 256
+// hide that chain (42% of a wave's time).  A block's 256
 // columns halve the reads of the tiles (without a bias, from 1024 columns on); with a
 // bias or EXACT a wave has one block of columns, as two do not fit its registers.
 //
@@ -418,7 +418,7 @@ __global__ __launch_bounds__(256, (kSimpleWaves<T, SHARED, BIAS>)) void attend_k
 // With a bias in bfloat16 a third term, of 8 bits like the others: the table's gradient
 // is in 32 bits, and sums what would be left of many rows that cancel (3600 queries over
 // 7200 keys, 8 heads, three axes: a relative error of 1.7e-6 with two terms, 6e-7 to
-// 8e-7 with three, and the training step 873 and 890 us, before lse had a rest).
+// 8e-7 with three, and the training step took 873 and 890 us).
 template <int DP> inline constexpr int kFlowWaves = DP <= 64 ? 2 : 1;   // a SIMD
 template <typename T, int DP, int NC, bool BIAS, bool EXACT>
 __global__ __launch_bounds__(256, kFlowWaves<DP>) void attend_flow_kernel(AttendK k)

@@ -398,10 +398,10 @@ __device__ __forceinline__ void store_rest(T *row, int d, int D, const float *o)
 // 64 in bf16 and two axes took 897 us a call, without 750.)
 //
 // So the time depends on the width of the views' rows.  An octet that crosses the end of
-// one makes its 32 rows mixed on every axis: the same pairs take 746 us in rows of 120,
-// 728 of 64, 777 of 40, 804 of 24, 791 of 107, 901 of 119 and 945 of 12 or 7; a training
-// step of 3600 queries over 7200 keys with three axes 925 in rows of 80, 898 of 64, 994 of
-// 24, 1058 of 67, 1040 of 79 and 1240 of 12.
+// one makes its 32 rows mixed on every axis: about as many pairs take 729 us in rows of
+// 120, 713 of 64, 763 of 40, 789 of 24, 774 of 107, 865 of 119 and 939 of 12 or 7; a
+// training step of 3600 queries over 7200 keys with three axes 907 in rows of 80, 881 of
+// 64, 977 of 24, 1041 of 67, 1022 of 79 and 1219 of 12.
 
 constexpr int kPad = 4;                                     // entries beyond either end
 constexpr int kReachRow = 2 * kMaxReach + 2 + 2 * kPad;     // of an axis and head in LDS
